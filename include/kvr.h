@@ -21,6 +21,14 @@
  *                                            -> kvr_attend_decode
  *   - the same for several query tokens per sequence over one rebuilt cache
  *                                            -> kvr_attend_multi
+ * Around it stand three operators of the uncompressed cache, the one that a prompt fills
+ * and that Algorithm 3 then compresses:
+ *   - norms and rotation of new tokens' queries and keys, and their place in the cache
+ *                                            -> kvr_rotate
+ *   - attention of a prompt's queries, with the Softmax(QK^T) that they accumulate per
+ *     token (Overview, Calculation Phase)    -> kvr_attend_prompt
+ *   - attention of one new token over a paged cache
+ *                                            -> kvr_attend_paged
  *
  * Vocabulary.  A *unit* is one (sequence b, kv head h) of one attention layer;
  * unit index u = b * n_kv_heads + h.  One call works on all units of one layer.
@@ -145,6 +153,47 @@ typedef struct kvr_attend_opts {
   void* prof_start;
   void* prof_stop;
 } kvr_attend_opts;
+
+/*
+ * A layer's uncompressed cache (host memory, plain data).
+ *   k, v       dev [n_pages, Hkv, page_size, D] storage type
+ *   table      dev int32 [B, table_cap]: token j of sequence b is row j % page_size of page
+ *              table[b][j / page_size].  An entry outside [0, n_pages) names no page: its
+ *              tokens are not there, attention passes over them and nothing is stored.  NULL:
+ *              sequence b has the one page b (n_pages >= B, table_cap ignored), which makes
+ *              k, v a dense cache [B, Hkv, page_size, D].
+ *   page_size  tokens a page, >= 1.  A sequence holds at most table_cap * page_size (dense:
+ *              page_size) tokens, which must be no more than 2^30.
+ * Several sequences may name the same page; two that store to one row in the same call
+ * leave it unspecified.
+ */
+typedef struct kvr_pages {
+  void* k;
+  void* v;
+  const int32_t* table;
+  int32_t n_pages, page_size, table_cap;
+} kvr_pages;
+
+/*
+ * What kvr_rotate does to a head's channels (host memory, plain data).
+ *   q_weight, k_weight  dev [D] storage type, 16-byte aligned, or NULL: no norm of the
+ *              queries / of the keys.  Norm: y = x / sqrt(mean(x^2) + eps) * weight over the
+ *              D channels of each head.
+ *   eps        >= 0
+ *   rot_dim    channels 0 .. rot_dim-1 are turned (even, 0 .. D), the others stay
+ *   style      KVR_ROTATE_HALVES: channels i and i + rot_dim/2 make pair i;
+ *              KVR_ROTATE_PAIRS: channels 2i and 2i + 1
+ *   inv_freq   dev float64 [rot_dim / 2] (NULL if rot_dim = 0): pair i of a token at
+ *              position P becomes (x cos a - y sin a, y cos a + x sin a), a = P * inv_freq[i]
+ */
+enum { KVR_ROTATE_HALVES = 0, KVR_ROTATE_PAIRS = 1 };
+typedef struct kvr_rotation {
+  const void* q_weight;
+  const void* k_weight;
+  const double* inv_freq;
+  float eps;
+  int32_t rot_dim, style;
+} kvr_rotation;
 
 /* Library version string (static storage). */
 const char* kvr_version(void);
@@ -427,6 +476,73 @@ int32_t kvr_attend_multi(const kvr_desc* desc, const void* q, int32_t n_q, const
                          const int32_t* vague_pos, const int32_t* n_vague, int32_t vague_cap,
                          float* out, float* scores, int64_t n_cap,
                          void* ws, size_t ws_bytes, void* stream);
+
+/*
+ * New tokens of a batch, in this and the next calls.  Rows 0 .. n_rows-1 hold them, sequence
+ * after sequence:
+ *   q_start    dev int32 [B + 1], not falling: rows q_start[b] .. q_start[b+1]-1 are the newest
+ *              tokens of sequence b (rows before q_start[0] and from q_start[B] on are nobody's:
+ *              not read, and left as they were in the outputs).  Entries are clamped to
+ *              [0, n_rows].  NULL: row b is the newest token of sequence b (n_rows = B).
+ *   n_ctx      dev int32 [B]: tokens of the sequence, the new ones included; the last new row's
+ *              position is n_ctx[b] - 1, the one before it n_ctx[b] - 2, and so on.
+ * n_rows is at most 2^27; n_rows = 0 does nothing.
+ */
+
+/*
+ * Norm and rotation of the new tokens' queries and keys (see kvr_rotation) in one pass, in
+ * float32 with one rounding to the storage type at the end; with `pages`, the keys and values
+ * also go to their places in the cache.  A row whose position is negative or past the cache's
+ * end is stored nowhere there.
+ *   q, k, v    dev [n_rows, Hq or Hkv, D] storage type; a row's heads are dense, rows are
+ *              q_stride, k_stride, v_stride elements apart (a whole number of 16 bytes, no less
+ *              than the heads of a row: parts of one fused projection will do).  q may be NULL,
+ *              or k; v is looked at only where there are pages (stored there as it is).
+ *   q_out      dev [n_rows, Hq, D] dense, written (NULL if q is).  May be q itself.
+ *   k_out      dev [n_rows, Hkv, D] dense, written, or NULL.  May be k itself.
+ *   pages      host, or NULL: k goes to k_out alone
+ */
+int32_t kvr_rotate(const kvr_desc* desc, const kvr_rotation* rot, const void* q, int64_t q_stride,
+                   const void* k, int64_t k_stride, const void* v, int64_t v_stride, int32_t n_rows,
+                   const int32_t* q_start, const int32_t* n_ctx, void* q_out, void* k_out,
+                   const kvr_pages* pages, void* stream);
+
+/*
+ * Causal attention of the new tokens over the cache, which holds them already.  A query at
+ * position P sees the tokens j <= P of its sequence that lie on a page, with window > 0 only
+ * those with j > P - window or j < n_sink (the first tokens stay visible):
+ *     p[t, hq, j] = softmax over visible j of softmax_scale * q[t, hq] . k[j]
+ *     out[t, hq]  = sum_j p[t, hq, j] v[j]
+ * and, if scores is not NULL, every token's cumulative score grows by the sum of p over the new
+ * tokens and the G q heads of its kv head, always in the same order.  A query that sees no token
+ * yields zeros.  n_ctx is clamped to what the cache can hold.  Tokens that no query of a row sees
+ * may hold anything, Inf and NaN too.
+ *   q          dev [n_rows, Hq, D] storage type, read
+ *   pages      host; k, v and table are read
+ *   window     0: no window
+ *   out        dev [n_rows, Hq, D] storage type, written
+ *   scores     dev float32 [B, Hkv, n_cap] read and written, or NULL; positions >= n_cap are
+ *              not accumulated
+ *   ws         per kvr_attend_prompt_workspace_size, with scores = whether there are scores
+ *              (which looks at the sizes of `pages` and at whether it has a table)
+ */
+int32_t kvr_attend_prompt_workspace_size(const kvr_desc* desc, int32_t n_rows, const kvr_pages* pages,
+                                         int32_t window, int32_t n_sink, int32_t scores, size_t* bytes);
+int32_t kvr_attend_prompt(const kvr_desc* desc, const void* q, int32_t n_rows, const int32_t* q_start,
+                          const int32_t* n_ctx, const kvr_pages* pages, int32_t window, int32_t n_sink,
+                          void* out, float* scores, int64_t n_cap, void* ws, size_t ws_bytes, void* stream);
+
+/*
+ * The same for one new token per sequence (row b is sequence b's), by kernels made for it: the
+ * cache is shared out by tokens over the whole chip, whatever the sequences' lengths.
+ *   q, out     dev [B, Hq, D] storage type
+ *   the others as for kvr_attend_prompt
+ */
+int32_t kvr_attend_paged_workspace_size(const kvr_desc* desc, const kvr_pages* pages, int32_t window,
+                                        int32_t n_sink, int32_t scores, size_t* bytes);
+int32_t kvr_attend_paged(const kvr_desc* desc, const void* q, const int32_t* n_ctx, const kvr_pages* pages,
+                         int32_t window, int32_t n_sink, void* out, float* scores, int64_t n_cap, void* ws,
+                         size_t ws_bytes, void* stream);
 
 #ifdef __cplusplus
 }

@@ -42,6 +42,9 @@ EXPORTS = ["kvr_version", "kvr_last_hip_error", "kvr_recent_size", "kvr_hash_par
            "kvr_workspace_size", "kvr_append", "kvr_select", "kvr_encode", "kvr_compact", "kvr_step_update",
            "kvr_swap_back", "kvr_reconstruct", "kvr_attend_decode", "kvr_attend_decode_static",
            "kvr_attend_multi_workspace_size", "kvr_attend_multi"]
+EXPORTS += ["kvr_rotate", "kvr_attend_prompt_workspace_size", "kvr_attend_prompt", "kvr_attend_paged_workspace_size",
+            "kvr_attend_paged"]
+KVR_ROTATE_HALVES, KVR_ROTATE_PAIRS = 0, 1
 KVR_STATIC_SCRATCH_BYTES = 80 << 20
 
 
@@ -62,6 +65,16 @@ class kvr_desc(C.Structure):
 class kvr_attend_opts(C.Structure):
     _fields_ = [("side_stream", C.c_void_p), ("fork_event", C.c_void_p), ("join_event", C.c_void_p),
                 ("prof_start", C.c_void_p), ("prof_stop", C.c_void_p)]
+
+
+class kvr_pages(C.Structure):
+    _fields_ = [("k", C.c_void_p), ("v", C.c_void_p), ("table", C.c_void_p),
+                ("n_pages", C.c_int32), ("page_size", C.c_int32), ("table_cap", C.c_int32)]
+
+
+class kvr_rotation(C.Structure):
+    _fields_ = [("q_weight", C.c_void_p), ("k_weight", C.c_void_p), ("inv_freq", C.c_void_p),
+                ("eps", C.c_float), ("rot_dim", C.c_int32), ("style", C.c_int32)]
 
 
 _fast = None
@@ -171,6 +184,17 @@ def lib() -> C.CDLL:
         L.kvr_attend_multi.restype = i32
         L.kvr_attend_multi.argtypes = [dp, vp, i32, vp, vp, vp, vp, i32, vp, vp, vp, vp, i32, vp, vp, i64,
                                        vp, sz, vp]
+        pp = C.POINTER(kvr_pages)
+        L.kvr_rotate.restype = i32
+        L.kvr_rotate.argtypes = [dp, C.POINTER(kvr_rotation), vp, i64, vp, i64, vp, i64, i32, vp, vp, vp, vp, pp, vp]
+        L.kvr_attend_prompt_workspace_size.restype = i32
+        L.kvr_attend_prompt_workspace_size.argtypes = [dp, i32, pp, i32, i32, i32, C.POINTER(sz)]
+        L.kvr_attend_prompt.restype = i32
+        L.kvr_attend_prompt.argtypes = [dp, vp, i32, vp, vp, pp, i32, i32, vp, vp, i64, vp, sz, vp]
+        L.kvr_attend_paged_workspace_size.restype = i32
+        L.kvr_attend_paged_workspace_size.argtypes = [dp, pp, i32, i32, i32, C.POINTER(sz)]
+        L.kvr_attend_paged.restype = i32
+        L.kvr_attend_paged.argtypes = [dp, vp, vp, pp, i32, i32, vp, vp, i64, vp, sz, vp]
         _load_fast(L)
         _lib = L
     return _lib
@@ -464,3 +488,129 @@ def kvr_attend_multi(desc, q, n_q, n_ctx, k_ret, v_ret, ret_pos, ret_cap, sketch
         _ptr(out, torch.float32, desc.batch * n_q * desc.n_q_heads * D, "out"),
         _ptr(scores, torch.float32, U * n_cap, "scores", True), n_cap, wp, wb, _stream())
     _check("kvr_attend_multi", rc)
+
+
+# ---------------------------------------------------------------------------
+# the uncompressed cache
+def _here(*tensors):
+    """The tensors of a call live on the current device, whose stream it is enqueued on."""
+    there = [t.device for t in tensors if isinstance(t, torch.Tensor) and t.is_cuda]
+    if there and any(x.index != torch.cuda.current_device() for x in there):
+        raise ValueError(f"tensors live on {sorted(set(map(str, there)))}, the current device is "
+                         f"cuda:{torch.cuda.current_device()}")
+
+
+def make_pages(desc, k, v, table=None):
+    """kvr_pages over the pools k, v [n_pages, Hkv, page_size, D] and table int32 [B, table_cap]; without a table the
+    pools are a dense cache [B, Hkv, tokens, D].  The struct keeps the tensors."""
+    dt = _torch_dtype(desc)
+    for t, name in ((k, "k"), (v, "v")):
+        if not isinstance(t, torch.Tensor) or t.dim() != 4:
+            raise ValueError(f"{name} must be a tensor [n_pages, n_kv_heads, page_size, head_dim]")
+        if tuple(t.shape) != tuple(k.shape) or t.shape[1] != desc.n_kv_heads or t.shape[3] != desc.head_dim:
+            raise ValueError(f"{name}: shape {tuple(t.shape)} does not fit the descriptor or the other pool")
+    p = kvr_pages(_ptr(k, dt, 1, "k"), _ptr(v, dt, 1, "v"), None, k.shape[0], k.shape[2], 0)
+    if table is not None:
+        if not isinstance(table, torch.Tensor) or table.dim() != 2 or table.shape[0] < desc.batch:
+            raise ValueError("table must be a tensor [batch, table_cap]")
+        p.table, p.table_cap = _ptr(table, torch.int32, 1, "table"), table.shape[1]
+    p.tensors = (k, v, table)
+    return p
+
+
+def _pages(desc, p, allow_none=False):
+    """A kvr_pages of make_pages that fits this descriptor (it may have been made with another one)."""
+    if p is None and allow_none:
+        return None
+    if not isinstance(p, kvr_pages) or not hasattr(p, "tensors"):
+        raise TypeError("pages must come from make_pages")
+    k, v, table = p.tensors
+    if k.dtype != _torch_dtype(desc) or k.shape[1] != desc.n_kv_heads or (
+            table.shape[0] if table is not None else k.shape[0]) < desc.batch:
+        raise ValueError("pages were made for another kind of descriptor")
+    return C.byref(p)
+
+
+def make_rotation(desc, inv_freq=None, *, q_weight=None, k_weight=None, eps=1e-6, pairs=False):
+    """kvr_rotation: inv_freq float64 [rot_dim / 2] (None: nothing is turned), weights [D] of the norms (None: no norm),
+    pairs: channels 2i and 2i + 1 make a pair instead of i and i + rot_dim / 2.  The struct keeps the tensors."""
+    dt = _torch_dtype(desc)
+    n = 0 if inv_freq is None else inv_freq.numel()
+    r = kvr_rotation(_ptr(q_weight, dt, desc.head_dim, "q_weight", True), _ptr(k_weight, dt, desc.head_dim, "k_weight", True),
+                     _ptr(inv_freq, torch.float64, 1, "inv_freq") if n else None, eps, 2 * n,
+                     KVR_ROTATE_PAIRS if pairs else KVR_ROTATE_HALVES)
+    r.tensors = (inv_freq, q_weight, k_weight)
+    return r
+
+
+def _rows(t, dtype, n_rows, heads, d, name):
+    """Pointer and row stride of [n_rows, heads, D] with dense heads and rows any way apart."""
+    if t is None:
+        return None, 0
+    if not isinstance(t, torch.Tensor):
+        raise TypeError(f"{name} must be a torch tensor")
+    if t.dtype != dtype:
+        raise TypeError(f"{name}: expected {dtype}, got {t.dtype}")
+    if not t.is_cuda:
+        raise ValueError(f"{name} must live in device memory")
+    if t.dim() != 3 or t.shape[0] < n_rows or t.shape[1] != heads or t.shape[2] != d:
+        raise ValueError(f"{name}: shape {tuple(t.shape)}, need [{n_rows}, {heads}, {d}]")
+    if t.stride(2) != 1 or (heads > 1 and t.stride(1) != d):
+        raise ValueError(f"{name}: the heads of a row must be dense")
+    return t.data_ptr(), t.stride(0) if n_rows > 1 else heads * d
+
+
+def kvr_rotate(desc, rot, q, k, v, n_rows, q_start, n_ctx, q_out, k_out=None, pages=None):
+    """As the C call; the rows' strides are the tensors' own."""
+    dt, d = _torch_dtype(desc), desc.head_dim
+    if not isinstance(rot, kvr_rotation):
+        raise TypeError("rot must come from make_rotation")
+    qp, qs = _rows(q, dt, n_rows, desc.n_q_heads, d, "q")
+    kp, ks = _rows(k, dt, n_rows, desc.n_kv_heads, d, "k")
+    vp, vs = _rows(v, dt, n_rows, desc.n_kv_heads, d, "v")
+    _here(q, k, v, n_ctx, q_out, k_out)
+    rc = lib().kvr_rotate(
+        C.byref(desc), C.byref(rot), qp, qs, kp, ks, vp, vs, n_rows,
+        _ptr(q_start, torch.int32, desc.batch + 1, "q_start", True), _ptr(n_ctx, torch.int32, desc.batch, "n_ctx"),
+        _ptr(q_out, dt, n_rows * desc.n_q_heads * d, "q_out", True),
+        _ptr(k_out, dt, n_rows * desc.n_kv_heads * d, "k_out", True), _pages(desc, pages, True), _stream())
+    _check("kvr_rotate", rc)
+
+
+def kvr_attend_prompt_workspace_size(desc, n_rows, pages, window, n_sink, scores) -> int:
+    n = C.c_size_t(0)
+    _check("kvr_attend_prompt_workspace_size", lib().kvr_attend_prompt_workspace_size(
+        C.byref(desc), n_rows, _pages(desc, pages), window, n_sink, int(bool(scores)), C.byref(n)))
+    return n.value
+
+
+def kvr_attend_prompt(desc, q, n_rows, q_start, n_ctx, pages, window, n_sink, out, scores, n_cap, ws):
+    U, dt = desc.batch * desc.n_kv_heads, _torch_dtype(desc)
+    row = desc.n_q_heads * desc.head_dim
+    wp, wb = _ws(ws)
+    _here(q, n_ctx, out, scores, ws)
+    rc = lib().kvr_attend_prompt(
+        C.byref(desc), _ptr(q, dt, n_rows * row, "q"), n_rows,
+        _ptr(q_start, torch.int32, desc.batch + 1, "q_start", True), _ptr(n_ctx, torch.int32, desc.batch, "n_ctx"),
+        _pages(desc, pages), window, n_sink, _ptr(out, dt, n_rows * row, "out"),
+        _ptr(scores, torch.float32, U * n_cap, "scores", True), n_cap, wp, wb, _stream())
+    _check("kvr_attend_prompt", rc)
+
+
+def kvr_attend_paged_workspace_size(desc, pages, window, n_sink, scores) -> int:
+    n = C.c_size_t(0)
+    _check("kvr_attend_paged_workspace_size", lib().kvr_attend_paged_workspace_size(
+        C.byref(desc), _pages(desc, pages), window, n_sink, int(bool(scores)), C.byref(n)))
+    return n.value
+
+
+def kvr_attend_paged(desc, q, n_ctx, pages, window, n_sink, out, scores, n_cap, ws):
+    U, dt = desc.batch * desc.n_kv_heads, _torch_dtype(desc)
+    row = desc.batch * desc.n_q_heads * desc.head_dim
+    wp, wb = _ws(ws)
+    _here(q, n_ctx, out, scores, ws)
+    rc = lib().kvr_attend_paged(
+        C.byref(desc), _ptr(q, dt, row, "q"), _ptr(n_ctx, torch.int32, desc.batch, "n_ctx"), _pages(desc, pages),
+        window, n_sink, _ptr(out, dt, row, "out"), _ptr(scores, torch.float32, U * n_cap, "scores", True), n_cap,
+        wp, wb, _stream())
+    _check("kvr_attend_paged", rc)

@@ -419,4 +419,187 @@ int32_t kvr_attend_multi(const kvr_desc* desc, const void* q, int32_t n_q, const
   return finish(kvr::launch_attend_multi(d, a, n_ctx, n_q, plan, ws, (hipStream_t)stream));
 }
 
+// Sizes of a cache, and the kernels' form of it (its pointers: check_pages).
+static int32_t pages_size(const kvr_desc* desc, const kvr_pages* pages, kvr::DevPages& p) {
+  if (pages == nullptr) return KVR_ERR_INVALID_ARG;
+  if (pages->n_pages < 1 || pages->page_size < 1 || pages->page_size > MAX_TOKENS) return KVR_ERR_INVALID_ARG;
+  long long cap = pages->page_size;
+  if (pages->table != nullptr) {
+    if (pages->table_cap < 1) return KVR_ERR_INVALID_ARG;
+    cap *= pages->table_cap;
+  } else if (pages->n_pages < desc->batch) {
+    return KVR_ERR_INVALID_ARG;
+  }
+  if (cap > MAX_TOKENS) return KVR_ERR_INVALID_ARG;
+  p = kvr::dev_pages(*pages);
+  return KVR_OK;
+}
+
+static int32_t check_pages(const kvr_desc* desc, const kvr_pages* pages, kvr::DevPages& p) {
+  const int32_t rc = pages_size(desc, pages, p);
+  if (rc != KVR_OK) return rc;
+  if (!pages->k || !pages->v || !aligned16(pages->k) || !aligned16(pages->v)) return KVR_ERR_INVALID_ARG;
+  if ((reinterpret_cast<uintptr_t>(pages->table) & 3u) != 0) return KVR_ERR_INVALID_ARG;
+  return KVR_OK;
+}
+
+constexpr int MAX_ROWS_NEW = 1 << 27;
+
+static int32_t check_rows(const kvr_desc* desc, int32_t n_rows, const int32_t* q_start) {
+  if (n_rows < 0 || n_rows > MAX_ROWS_NEW) return KVR_ERR_INVALID_ARG;
+  if (q_start == nullptr && n_rows != desc->batch) return KVR_ERR_INVALID_ARG;
+  return KVR_OK;
+}
+
+int32_t kvr_rotate(const kvr_desc* desc, const kvr_rotation* rot, const void* q, int64_t q_stride, const void* k,
+                   int64_t k_stride, const void* v, int64_t v_stride, int32_t n_rows, const int32_t* q_start,
+                   const int32_t* n_ctx, void* q_out, void* k_out, const kvr_pages* pages, void* stream) {
+  kvr::DevDesc d;
+  int32_t rc = check_desc(desc, d);
+  if (rc != KVR_OK) return rc;
+  if (rot == nullptr || !(rot->eps >= 0.f) || !(rot->eps < 3.0e38f)) return KVR_ERR_INVALID_ARG;
+  if (rot->rot_dim < 0 || rot->rot_dim > KVR_HEAD_DIM || rot->rot_dim % 2 != 0) return KVR_ERR_INVALID_ARG;
+  if (rot->style != KVR_ROTATE_HALVES && rot->style != KVR_ROTATE_PAIRS) return KVR_ERR_INVALID_ARG;
+  if ((rot->rot_dim > 0 && !rot->inv_freq) || (reinterpret_cast<uintptr_t>(rot->inv_freq) & 7u) != 0)
+    return KVR_ERR_INVALID_ARG;
+  if (!aligned16(rot->q_weight) || !aligned16(rot->k_weight)) return KVR_ERR_INVALID_ARG;
+  rc = check_rows(desc, n_rows, q_start);
+  if (rc != KVR_OK) return rc;
+  kvr::RotateArgs a;
+  memset(&a, 0, sizeof(a));
+  if (pages != nullptr && n_rows > 0) {
+    rc = check_pages(desc, pages, a.pages);
+    if (rc != KVR_OK) return rc;
+  }
+  if (n_rows == 0) return KVR_OK;
+  if (!n_ctx || (!q && !k)) return KVR_ERR_INVALID_ARG;
+  if ((q == nullptr) != (q_out == nullptr)) return KVR_ERR_INVALID_ARG;
+  if ((k != nullptr) != (k_out != nullptr || pages != nullptr)) return KVR_ERR_INVALID_ARG;
+  if (pages == nullptr) v = nullptr;
+  else if (v == nullptr) return KVR_ERR_INVALID_ARG;
+  if (!aligned16(q) || !aligned16(k) || !aligned16(v) || !aligned16(q_out) || !aligned16(k_out))
+    return KVR_ERR_INVALID_ARG;
+  const int64_t whole = 16 / (desc->dtype == KVR_F32 ? 4 : 2);
+  const int64_t row_q = (int64_t)d.Hq * KVR_HEAD_DIM, row_kv = (int64_t)d.Hkv * KVR_HEAD_DIM;
+  if (q && (q_stride < row_q || q_stride % whole != 0)) return KVR_ERR_INVALID_ARG;
+  if (k && (k_stride < row_kv || k_stride % whole != 0)) return KVR_ERR_INVALID_ARG;
+  if (v && (v_stride < row_kv || v_stride % whole != 0)) return KVR_ERR_INVALID_ARG;
+  // rows that are read after others were written: only where a row's place stays its own
+  if ((q != nullptr && q == q_out && q_stride != row_q) || (k != nullptr && k == k_out && k_stride != row_kv))
+    return KVR_ERR_INVALID_ARG;
+  a.q = q;
+  a.k = k;
+  a.v = v;
+  a.q_stride = q_stride;
+  a.k_stride = k_stride;
+  a.v_stride = v_stride;
+  a.n_rows = n_rows;
+  a.q_start = q_start;
+  a.n_ctx = n_ctx;
+  a.q_out = q_out;
+  a.k_out = k_out;
+  a.q_weight = rot->q_weight;
+  a.k_weight = rot->k_weight;
+  a.eps = rot->eps;
+  a.inv_freq = rot->inv_freq;
+  a.half = rot->rot_dim / 2;
+  a.n_slots = (q ? d.Hq : 0) + (k ? d.Hkv : 0) + (v ? d.Hkv : 0);
+  a.paged = pages != nullptr;
+  return finish(kvr::launch_rotate(d, desc->dtype, a, rot->style == KVR_ROTATE_PAIRS, (hipStream_t)stream));
+}
+
+static int32_t check_visible(int32_t window, int32_t n_sink, kvr::Visible& vis) {
+  if (window < 0 || n_sink < 0) return KVR_ERR_INVALID_ARG;
+  vis.window = window > MAX_TOKENS ? (int)MAX_TOKENS : window;
+  vis.n_sink = n_sink > MAX_TOKENS ? (int)MAX_TOKENS : n_sink;
+  return KVR_OK;
+}
+
+// the arguments that kvr_attend_prompt and kvr_attend_paged share; n_rows > 0
+static int32_t check_attend(const kvr_desc* desc, const void* q, const int32_t* n_ctx, const kvr_pages* pages, void* out,
+                            float* scores, int64_t n_cap, kvr::PagedArgs& a) {
+  const int32_t rc = check_pages(desc, pages, a.pages);
+  if (rc != KVR_OK) return rc;
+  if (!q || !n_ctx || !out || !aligned16(q) || !aligned16(out)) return KVR_ERR_INVALID_ARG;
+  if (scores != nullptr && (n_cap < 1 || n_cap > MAX_TOKENS)) return KVR_ERR_INVALID_ARG;
+  a.q = q;
+  a.n_ctx = n_ctx;
+  a.out = out;
+  a.scores = scores;
+  a.n_cap = n_cap;
+  return KVR_OK;
+}
+
+static int32_t check_ws(void* ws, size_t ws_bytes, size_t need) {
+  if (need == 0) return KVR_OK;
+  if (ws == nullptr || !aligned16(ws)) return KVR_ERR_INVALID_ARG;
+  return ws_bytes < need ? KVR_ERR_WORKSPACE_TOO_SMALL : KVR_OK;
+}
+
+int32_t kvr_attend_prompt_workspace_size(const kvr_desc* desc, int32_t n_rows, const kvr_pages* pages, int32_t window,
+                                         int32_t n_sink, int32_t scores, size_t* bytes) {
+  kvr::DevDesc d;
+  kvr::DevPages p;
+  kvr::Visible vis;
+  int32_t rc = check_desc(desc, d);
+  if (rc == KVR_OK) rc = pages_size(desc, pages, p);
+  if (rc == KVR_OK) rc = check_visible(window, n_sink, vis);
+  if (rc != KVR_OK) return rc;
+  if (bytes == nullptr || n_rows < 0 || n_rows > MAX_ROWS_NEW) return KVR_ERR_INVALID_ARG;
+  *bytes = n_rows == 0 ? 0 : kvr::attend_prompt_ws(d, desc->dtype, n_rows, p.cap, vis, scores != 0);
+  return KVR_OK;
+}
+
+int32_t kvr_attend_prompt(const kvr_desc* desc, const void* q, int32_t n_rows, const int32_t* q_start,
+                          const int32_t* n_ctx, const kvr_pages* pages, int32_t window, int32_t n_sink, void* out,
+                          float* scores, int64_t n_cap, void* ws, size_t ws_bytes, void* stream) {
+  kvr::DevDesc d;
+  kvr::PagedArgs a;
+  memset(&a, 0, sizeof(a));
+  int32_t rc = check_desc(desc, d);
+  if (rc == KVR_OK) rc = check_visible(window, n_sink, a.vis);
+  if (rc == KVR_OK) rc = check_rows(desc, n_rows, q_start);
+  if (rc != KVR_OK) return rc;
+  if (n_rows == 0) return KVR_OK;
+  rc = check_attend(desc, q, n_ctx, pages, out, scores, n_cap, a);
+  if (rc != KVR_OK) return rc;
+  rc = check_ws(ws, ws_bytes, kvr::attend_prompt_ws(d, desc->dtype, n_rows, a.pages.cap, a.vis, scores != nullptr));
+  if (rc != KVR_OK) return rc;
+  a.n_rows = n_rows;
+  a.q_start = q_start;
+  a.ws = ws;
+  return finish(kvr::launch_attend_prompt(d, desc->dtype, a, (hipStream_t)stream));
+}
+
+int32_t kvr_attend_paged_workspace_size(const kvr_desc* desc, const kvr_pages* pages, int32_t window, int32_t n_sink,
+                                        int32_t scores, size_t* bytes) {
+  kvr::DevDesc d;
+  kvr::DevPages p;
+  kvr::Visible vis;
+  int32_t rc = check_desc(desc, d);
+  if (rc == KVR_OK) rc = pages_size(desc, pages, p);
+  if (rc == KVR_OK) rc = check_visible(window, n_sink, vis);
+  if (rc != KVR_OK) return rc;
+  if (bytes == nullptr) return KVR_ERR_INVALID_ARG;
+  *bytes = kvr::attend_paged_ws(d, desc->dtype, p.cap, vis, scores != 0);
+  return KVR_OK;
+}
+
+int32_t kvr_attend_paged(const kvr_desc* desc, const void* q, const int32_t* n_ctx, const kvr_pages* pages,
+                         int32_t window, int32_t n_sink, void* out, float* scores, int64_t n_cap, void* ws,
+                         size_t ws_bytes, void* stream) {
+  kvr::DevDesc d;
+  kvr::PagedArgs a;
+  memset(&a, 0, sizeof(a));
+  int32_t rc = check_desc(desc, d);
+  if (rc == KVR_OK) rc = check_visible(window, n_sink, a.vis);
+  if (rc == KVR_OK) rc = check_attend(desc, q, n_ctx, pages, out, scores, n_cap, a);
+  if (rc != KVR_OK) return rc;
+  rc = check_ws(ws, ws_bytes, kvr::attend_paged_ws(d, desc->dtype, a.pages.cap, a.vis, scores != nullptr));
+  if (rc != KVR_OK) return rc;
+  a.n_rows = d.B;
+  a.ws = ws;
+  return finish(kvr::launch_attend_paged(d, desc->dtype, a, (hipStream_t)stream));
+}
+
 }  // extern "C"

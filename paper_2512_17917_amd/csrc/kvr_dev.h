@@ -176,6 +176,6 @@ __device__ __forceinline__ uint4 query_piece3(const DevDesc& d, const bf16_t* __
                     med3_pair_bf16(r[0].z, r[1].z, r[2].z), med3_pair_bf16(r[0].w, r[1].w, r[2].w));
 }
 
-__device__ __forceinline__ int clampi(int x, int lo, int hi) { return x < lo ? lo : (x > hi ? hi : x); }
+__host__ __device__ __forceinline__ int clampi(int x, int lo, int hi) { return x < lo ? lo : (x > hi ? hi : x); }
 
 }  // namespace kvr

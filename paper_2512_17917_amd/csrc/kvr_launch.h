@@ -7,6 +7,7 @@
 #include <mutex>
 
 #include "kvr_dev.h"
+#include "kvr_pages.h"
 
 namespace kvr {
 
@@ -216,5 +217,46 @@ hipError_t launch_encode(const DevDesc& d, int dtype, const void* k_src, const v
                          const int32_t* src_slot, const int32_t* tok_pos, const int32_t* count, int cap,
                          void* sk, void* sv, int32_t* out_bucket, uint8_t* out_sign,
                          void* ws, const EncodePlan& plan, hipStream_t st);
+
+// Norm and rotation of new tokens' queries and keys, keys and values into the cache (kvr_rotate)
+struct RotateArgs {
+  const void* q;
+  const void* k;
+  const void* v;
+  long long q_stride, k_stride, v_stride;
+  int n_rows;
+  const int32_t* q_start;
+  const int32_t* n_ctx;
+  void* q_out;
+  void* k_out;
+  const void* q_weight;
+  const void* k_weight;
+  float eps;
+  const double* inv_freq;
+  int half;                          // turned pairs
+  int n_slots;                       // heads of a row: queries, keys, values that go to the pages
+  bool paged;
+  DevPages pages;
+  int parts;                         // waves of a row (set by the launcher)
+};
+hipError_t launch_rotate(const DevDesc& d, int dtype, const RotateArgs& a, bool pairs, hipStream_t st);
+
+// Attention over a paged cache (kvr_attend_paged: one row per sequence; kvr_attend_prompt: rows by q_start)
+struct PagedArgs {
+  const void* q;
+  int n_rows;
+  const int32_t* q_start;
+  const int32_t* n_ctx;
+  DevPages pages;
+  Visible vis;
+  void* out;
+  float* scores;
+  long long n_cap;
+  void* ws;
+};
+size_t attend_prompt_ws(const DevDesc& d, int dtype, long long n_rows, long long cap, const Visible& vis, bool scores);
+hipError_t launch_attend_prompt(const DevDesc& d, int dtype, const PagedArgs& a, hipStream_t st);
+size_t attend_paged_ws(const DevDesc& d, int dtype, long long cap, const Visible& vis, bool scores);
+hipError_t launch_attend_paged(const DevDesc& d, int dtype, const PagedArgs& a, hipStream_t st);
 
 }  // namespace kvr

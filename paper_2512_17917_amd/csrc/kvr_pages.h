@@ -1,0 +1,127 @@
+// Pages of a cache, rows of a ragged batch and the tokens that a query sees: what the kernels around the paged cache
+// share.
+#pragma once
+#include "kvr_dev.h"
+
+namespace kvr {
+
+// kvr_pages as the kernels take it.  Token j of sequence b lies in row j % page_size of page table[b][j / page_size]; without
+// a table sequence b has the one page b.  The quotient by the page size comes from a product: with 2^(s-1) < size <= 2^s and
+// magic = floor(2^(31+s) / size) + 1, (j magic) >> (31 + s) is exact for 0 <= j < 2^31, and magic fits 32 bits.
+struct DevPages {
+  void* k;
+  void* v;
+  const int32_t* table;
+  int n_pages, page_size, table_cap;
+  int cap;                          // tokens a sequence can hold
+  uint32_t magic;
+  int shift;
+};
+
+inline DevPages dev_pages(const kvr_pages& c) {
+  DevPages p;
+  p.k = c.k;
+  p.v = c.v;
+  p.table = c.table;
+  p.n_pages = c.n_pages;
+  p.page_size = c.page_size;
+  p.table_cap = c.table_cap;
+  p.cap = c.table ? c.table_cap * c.page_size : c.page_size;
+  int s = 0;
+  while ((1ll << s) < c.page_size) ++s;
+  p.shift = 31 + s;
+  p.magic = (uint32_t)(((uint64_t)1 << p.shift) / (uint64_t)c.page_size + 1);
+  return p;
+}
+
+__host__ __device__ __forceinline__ int page_index(const DevPages& p, int j) {
+  return (int)(((uint64_t)(uint32_t)j * p.magic) >> p.shift);
+}
+// Row of token j (0 <= j < cap) of sequence b, kv head h, counted in rows of D channels from the pools' start; -1 where the
+// table names no page.
+__host__ __device__ __forceinline__ long long page_row(const DevPages& p, int n_kv_heads, int b, int h, int j) {
+  const int i = page_index(p, j);
+  const int page = p.table ? p.table[(size_t)b * p.table_cap + i] : b;
+  if ((uint32_t)page >= (uint32_t)p.n_pages) return -1;
+  return ((long long)page * n_kv_heads + h) * p.page_size + (j - i * p.page_size);
+}
+
+// New tokens of the batch: rows q_start[b] .. q_start[b + 1] - 1 are sequence b's, or row b where q_start is null.
+struct RowSpan {
+  int first, n;
+};
+__host__ __device__ __forceinline__ RowSpan row_span(const int32_t* q_start, int n_rows, int b) {
+  if (q_start == nullptr) return {b, 1};
+  const int first = clampi(q_start[b], 0, n_rows);
+  return {first, clampi(q_start[b + 1], first, n_rows) - first};
+}
+// Sequence of row `row` (wave-uniform; all lanes call), -1 if it is none's.  Row starts do not fall.
+__device__ __forceinline__ int seq_of_row(const int32_t* q_start, int B, int row) {
+  if (q_start == nullptr) return row < B ? row : -1;
+  const int lane = threadIdx.x & 63;
+  int before = 0;                   // sequences that end at or before the row
+  for (int b0 = 0; b0 < B; b0 += 64) {
+    const bool past = b0 + lane < B && q_start[b0 + lane + 1] <= row;
+    const int n = __popcll(__ballot(past));
+    before += n;
+    if (n < 64) break;
+  }
+  return before < B && q_start[before] <= row ? before : -1;
+}
+
+// Column tile blockIdx.x of a launch: a sequence's new tokens times its kv head's G query heads are columns m = t G + g, in
+// tiles of `per`; tiles are counted sequence after sequence.  b < 0: none left.  (All lanes of a wave call.)
+struct ColTile {
+  int b, m0;
+};
+__device__ __forceinline__ ColTile col_tile(const int32_t* q_start, int n_rows, int B, int G, int per, int tile) {
+  const int lane = threadIdx.x & 63;
+  int base = 0;
+  for (int b0 = 0; b0 < B; b0 += 64) {
+    const int n = b0 + lane < B ? row_span(q_start, n_rows, b0 + lane).n : 0;
+    const int mine = (int)(((long long)n * G + per - 1) / per);
+    int upto = mine;
+#pragma unroll
+    for (int k = 1; k < 64; k <<= 1) {
+      const int x = __shfl_up(upto, k);
+      upto += lane >= k ? x : 0;
+    }
+    const unsigned long long past = __ballot(tile < base + upto);
+    if (past != 0) {
+      const int l = __ffsll(past) - 1;
+      return {b0 + l, (tile - base - __shfl(upto - mine, l)) * per};
+    }
+    base += __shfl(upto, 63);
+  }
+  return {-1, 0};
+}
+constexpr long long col_tiles_most(long long n_rows, int B, int G, int per) {
+  return (n_rows * G + per - 1) / per + B;
+}
+
+// Which tokens a query at position P sees: j <= P, and j > P - window or j < n_sink where there is a window.
+struct Visible {
+  int window, n_sink;               // window 0: none
+};
+__host__ __device__ __forceinline__ bool sees(const Visible& s, int P, int j) {
+  return j <= P && (s.window == 0 || j > P - s.window || j < s.n_sink);
+}
+// Tiles of T tokens (T a power of two) that queries at positions lo .. hi see between them: `ahead` tiles of first tokens from
+// token 0, then tiles from token `start` (a multiple of T) to token hi; those in between no query sees.
+struct TileRange {
+  int ahead, start, n;
+};
+template <int T>
+__host__ __device__ __forceinline__ TileRange tile_range(const Visible& s, int lo, int hi) {
+  if (hi < 0) return {0, 0, 0};
+  int start = 0;
+  if (s.window > 0 && lo >= s.window) start = (lo - s.window + 1) & ~(T - 1);
+  const int ahead = ((s.n_sink < start ? s.n_sink : start) + T - 1) / T;
+  return {ahead, start, ahead + (hi - start) / T + 1};
+}
+template <int T>
+__host__ __device__ __forceinline__ int tile_token(const TileRange& r, int i) {
+  return i < r.ahead ? i * T : r.start + (i - r.ahead) * T;
+}
+
+}  // namespace kvr
