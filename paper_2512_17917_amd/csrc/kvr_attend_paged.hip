@@ -1,0 +1,553 @@
+// Attention of one new token per sequence over a paged cache.
+//
+// A unit (sequence b, kv head h) is the run of 16-token tiles that its query sees (tile_range), four tiles a chunk.  All
+// units' chunks stand in one row, sequence after sequence, and each workgroup takes the same number of neighbours in it:
+// whatever the lengths, the chip is shared out evenly, and only the device has to know them.  Where a workgroup's piece of a
+// unit is not all of it, its maximum, sum and sum of p v go to slot w + u of the workspace (w: workgroup, u: unit; going
+// along the row each next piece raises one of the two, so no two share a slot) and a second kernel joins them.
+//
+// In a workgroup each of the four waves takes a tile at a time with a running maximum and sum.  q.k of the G heads is a
+// matrix product with the keys as the A operand (lane l: token l mod 16, of each 32 channels the eight from 8 (l div 16)):
+// v_mfma_f32_16x16x32_bf16, for float32 storage v_mfma_f32_16x16x4_f32.  Lane l then has the logits of tokens
+// 4 (l div 16) + {0..3} and head l mod 16; the values are read so that it holds channels 8 (l mod 16) .. +7 of the same four
+// tokens, and p v is summed in float32 on the vector units with p broadcast along the 16 lanes (an MFMA would want the
+// values transposed and p rounded).  A tile's keys are asked for as soon as the last one's are used up, its values after the
+// last one's; the table a tile earlier.
+//
+// Scores need the final sum, so logits are kept (G floats a token, through LDS: a store between the loads would make every
+// wait for a load a wait for all) and the second kernel adds exp(s - lse).
+#include "kvr_launch.h"
+
+namespace kvr {
+
+namespace {
+
+typedef __bf16 bf16x8_t __attribute__((ext_vector_type(8)));
+typedef float f32x4_t __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x4_t __attribute__((ext_vector_type(4)));
+
+constexpr int PG_WAVES = 4;
+constexpr int PG_KEEP = 8;          // tiles whose logits a wave keeps in LDS at a time
+constexpr int PG_SLICE = 1024;      // tokens of a workgroup that adds scores
+
+// Workgroups that a CU holds at a time: what the registers of a wave leave (bf16: 32 for a tile, 16 for q, 8 G for the sums)
+constexpr int paged_per_cu(int elem, int G) { return elem == 2 ? (G <= 4 ? 4 : 3) : (G <= 4 ? 3 : 2); }
+
+struct PagedPlan {
+  int wgs;                          // workgroups of the first kernel
+  long long tiles;                  // tiles a unit can have
+  bool join;
+  size_t off_o, off_ml, off_log, total;
+};
+
+PagedPlan paged_plan(const DevDesc& d, int dtype, long long cap, const Visible& vis, bool scores) {
+  PagedPlan p;
+  const long long all = (cap + 15) / 16;
+  p.tiles = all;
+  if (vis.window > 0) {
+    const long long some = ((long long)vis.window + 15) / 16 + 1 + ((long long)vis.n_sink + 15) / 16;
+    p.tiles = some < all ? some : all;
+  }
+  const long long units = (long long)d.B * d.Hkv;
+  const long long chunks = units * ((p.tiles + 3) / 4);
+  const int fill = 256 * paged_per_cu(dtype == KVR_F32 ? 4 : 2, d.G);
+  p.wgs = (int)(chunks < fill ? chunks : fill);
+  p.join = scores || p.tiles > 4;
+  const size_t slots = (size_t)p.wgs + units;
+  auto whole = [](size_t x) { return (x + 255) & ~(size_t)255; };
+  p.off_o = 0;
+  p.off_ml = p.join ? whole(slots * d.G * D * sizeof(float)) : 0;
+  p.off_log = p.off_ml + (p.join ? whole(slots * d.G * 2 * sizeof(float)) : 0);
+  p.total = p.off_log + (scores ? whole((size_t)units * p.tiles * 16 * d.G * sizeof(float)) : 0);
+  return p;
+}
+
+// value held by lane N of the caller's 16-lane row
+template <int N>
+__device__ __forceinline__ float row_bcast(float x) {
+  return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), 0x150 + N, 0xf, 0xf, true));
+}
+template <int G, int I = 0>
+__device__ __forceinline__ void add_pv(float (&acc)[G][8], float p, const float (&v)[8]) {
+  if constexpr (I < G) {
+    const float pg = row_bcast<I>(p);
+#pragma unroll
+    for (int c = 0; c < 8; ++c) acc[I][c] = fmaf(pg, v[c], acc[I][c]);
+    add_pv<G, I + 1>(acc, p, v);
+  }
+}
+template <int G, int I = 0>
+__device__ __forceinline__ void scale_acc(float (&acc)[G][8], float f) {
+  if constexpr (I < G) {
+    const float fg = row_bcast<I>(f);
+#pragma unroll
+    for (int c = 0; c < 8; ++c) acc[I][c] *= fg;
+    scale_acc<G, I + 1>(acc, f);
+  }
+}
+
+// ---- the row of chunks -----------------------------------------------------
+__device__ __forceinline__ TileRange unit_tiles(const PagedArgs& a, int b, int& n) {
+  n = clampi(a.n_ctx[b], 0, a.pages.cap);
+  return tile_range<16>(a.vis, n - 1, n - 1);
+}
+__device__ __forceinline__ int seq_chunks(const PagedArgs& a, int b) {
+  int n;
+  return (unit_tiles(a, b, n).n + 3) >> 2;
+}
+__device__ __forceinline__ long long wave_sum(long long x) {
+#pragma unroll
+  for (int k = 1; k < 64; k <<= 1) x += __shfl_xor(x, k);
+  return x;
+}
+// chunks of all sequences before `upto`, times 1 head
+__device__ __forceinline__ long long chunks_before(const PagedArgs& a, int upto) {
+  const int lane = threadIdx.x & 63;
+  long long sum = 0;
+  for (int b0 = 0; b0 < upto; b0 += 64) sum += b0 + lane < upto ? seq_chunks(a, b0 + lane) : 0;
+  return wave_sum(sum);
+}
+// chunks a workgroup takes
+__device__ __forceinline__ long long piece(long long total, int wgs) { return (total + wgs - 1) / wgs; }
+
+struct Where {
+  int b, h, chunk;
+};
+// place of chunk `at` of the row (at < total)
+__device__ __forceinline__ Where find_chunk(const PagedArgs& a, int B, int heads, long long at) {
+  const int lane = threadIdx.x & 63;
+  long long base = 0;
+  for (int b0 = 0; b0 < B; b0 += 64) {
+    const int mine = b0 + lane < B ? seq_chunks(a, b0 + lane) : 0;
+    long long upto = mine;
+#pragma unroll
+    for (int k = 1; k < 64; k <<= 1) {
+      const long long x = __shfl_up(upto, k);
+      upto += lane >= k ? x : 0;
+    }
+    const unsigned long long past = __ballot(at < (base + upto) * heads);
+    if (past != 0) {
+      const int l = __ffsll(past) - 1;
+      const int n = __shfl(mine, l);
+      const long long off = at - (base + __shfl(upto, l) - n) * heads;
+      return {b0 + l, (int)(off / n), (int)(off % n)};
+    }
+    base += __shfl(upto, 63);
+  }
+  return {B, 0, 0};
+}
+
+// ---- a tile ------------------------------------------------------------------
+// Where a tile's 16 rows are.  ONE: they lie in one page one after another (pages of whole tiles, or a dense cache).
+template <bool ONE>
+struct TileRows {
+  long long row;        // ONE: of the first token; else of token lane mod 16
+  uint32_t there;       // bit i: token i lies on a page
+};
+
+template <bool ONE>
+__device__ __forceinline__ TileRows<ONE> tile_rows(const PagedArgs& a, int heads, int b, int h, int j0, int n, int col) {
+  TileRows<ONE> t;
+  if constexpr (ONE) {
+    const long long r = page_row(a.pages, heads, b, h, j0);
+    t.row = r < 0 ? 0 : r;
+    t.there = r < 0 ? 0u : 0xffffu;
+  } else {
+    const long long r = page_row(a.pages, heads, b, h, min(j0 + col, n - 1));
+    t.row = r < 0 ? 0 : r;
+    t.there = (uint32_t)__ballot(r >= 0) & 0xffffu;
+  }
+  return t;
+}
+
+template <typename T> struct Tile {
+  static constexpr int N = sizeof(T) * 2;       // 16-byte pieces of eight channels of four blocks or tokens
+  u32x4_t k[N], v[N];
+};
+
+// 16 bytes that are read once: they need not stay in L2
+__device__ __forceinline__ u32x4_t once(const void* p) {
+  return __builtin_nontemporal_load(reinterpret_cast<const u32x4_t*>(p));
+}
+
+template <typename T, bool ONE>
+__device__ __forceinline__ void load_k(Tile<T>& t, const void* pool, const TileRows<ONE>& at, int j0, int n, int r16, int col) {
+  constexpr int PER = sizeof(T) / 2;            // pieces of eight channels
+  const T* p = (const T*)pool + at.row * D + (ONE ? min(col, n - 1 - j0) * D : 0) + 8 * r16;
+#pragma unroll
+  for (int i = 0; i < Tile<T>::N; ++i) t.k[i] = once(p + 32 * (i / PER) + 4 * (i % PER));
+}
+template <typename T, bool ONE>
+__device__ __forceinline__ void load_v(Tile<T>& t, const void* pool, const TileRows<ONE>& at, int j0, int n, int r16, int col) {
+  constexpr int PER = sizeof(T) / 2;
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    const T* p = (const T*)pool + 8 * col;
+    if constexpr (ONE) p += at.row * D + min(4 * r16 + j, n - 1 - j0) * D;
+    else p += __shfl(at.row, 4 * r16 + j) * D;
+#pragma unroll
+    for (int i = 0; i < PER; ++i) t.v[j * PER + i] = once(p + 4 * i);
+  }
+}
+
+template <typename T>
+__device__ __forceinline__ void widen(const u32x4_t* piece, float (&o)[8]) {
+  if constexpr (sizeof(T) == 2) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      o[2 * i] = __uint_as_float(piece[0][i] << 16);
+      o[2 * i + 1] = __uint_as_float(piece[0][i] & 0xffff0000u);
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) o[i] = __uint_as_float(piece[i / 4][i % 4]);
+  }
+}
+
+template <typename T>
+__device__ __forceinline__ f32x4_t tile_logits(const u32x4_t (&k)[Tile<T>::N], const u32x4_t (&q)[Tile<T>::N]) {
+  f32x4_t s = {0.f, 0.f, 0.f, 0.f};
+  if constexpr (sizeof(T) == 2) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      s = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, k[i]), __builtin_bit_cast(bf16x8_t, q[i]), s, 0, 0, 0);
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        s = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(k[i][e]), __uint_as_float(q[i][e]), s, 0, 0, 0);
+  }
+  return s;
+}
+
+template <typename T, int G, bool ONE>
+__global__ __launch_bounds__(64 * PG_WAVES, paged_per_cu(sizeof(T), G)) void paged_kernel(DevDesc d, PagedArgs a, float* part_o, float* part_ml, float* logits,
+                                                              long long most_tiles) {
+  __shared__ __align__(16) float s_o[PG_WAVES][G][D];
+  __shared__ float s_m[PG_WAVES][G], s_l[PG_WAVES][G];
+  __shared__ __align__(16) float s_log[PG_WAVES][PG_KEEP * 16 * G];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int r16 = lane >> 4, col = lane & 15;
+  const int w = blockIdx.x;
+  const float NEG_INF = -__builtin_inff();
+
+  // sequences without a token yield zeros
+  for (int b = w; b < d.B; b += gridDim.x)
+    if (a.n_ctx[b] <= 0)
+      for (int i = threadIdx.x; i < d.Hq * D; i += 64 * PG_WAVES) Store<T>::store1((T*)a.out + (size_t)b * d.Hq * D + i, 0.f);
+
+  const long long total = chunks_before(a, d.B) * d.Hkv;
+  const long long per = piece(total, gridDim.x);
+  long long at = (long long)w * per;
+  const long long end = at + per < total ? at + per : total;
+  if (at >= end) return;
+  Where p = find_chunk(a, d.B, d.Hkv, at);
+  while (at < end) {
+    const int b = __builtin_amdgcn_readfirstlane(p.b), h = __builtin_amdgcn_readfirstlane(p.h);
+    const int c0 = __builtin_amdgcn_readfirstlane(p.chunk);
+    int n;
+    const TileRange tr = unit_tiles(a, b, n);
+    const int chunks = (tr.n + 3) >> 2;
+    const int len = (int)(end - at < chunks - c0 ? end - at : chunks - c0);
+    const int u = b * d.Hkv + h;
+    const int t_end = min(4 * (c0 + len), tr.n);
+    const int P = n - 1;
+
+    u32x4_t q[Tile<T>::N];
+    {
+      const T* qp = (const T*)a.q + ((size_t)b * d.Hq + h * G + min(col, G - 1)) * D + 8 * r16;
+      constexpr int PER = sizeof(T) / 2;
+#pragma unroll
+      for (int i = 0; i < Tile<T>::N; ++i) {
+        q[i] = *reinterpret_cast<const u32x4_t*>(qp + 32 * (i / PER) + 4 * (i % PER));
+      }
+    }
+    float acc[G][8];
+#pragma unroll
+    for (int g = 0; g < G; ++g)
+#pragma unroll
+      for (int c = 0; c < 8; ++c) acc[g][c] = 0.f;
+    float m_run = NEG_INF, l_run = 0.f;
+    float* log_unit = logits ? logits + (size_t)u * most_tiles * 16 * G : nullptr;
+    int kept = 0;
+
+    int ti = 4 * c0 + wave;
+    Tile<T> t;
+    TileRows<ONE> next = {};
+    if (ti < t_end) {
+      const int j0 = tile_token<16>(tr, ti);
+      const TileRows<ONE> now = tile_rows<ONE>(a, d.Hkv, b, h, j0, n, col);
+      load_k<T, ONE>(t, a.pages.k, now, j0, n, r16, col);
+      load_v<T, ONE>(t, a.pages.v, now, j0, n, r16, col);
+      uint32_t there = now.there;
+      if (ti + 4 < t_end) next = tile_rows<ONE>(a, d.Hkv, b, h, tile_token<16>(tr, ti + 4), n, col);
+      int j = j0;
+      for (; ti < t_end; ti += 4) {
+        const f32x4_t s4 = tile_logits<T>(t.k, q);
+        const bool more = ti + 4 < t_end;
+        const int jn = more ? tile_token<16>(tr, ti + 4) : j;
+        if (more) load_k<T, ONE>(t, a.pages.k, next, jn, n, r16, col);
+        float s[4];
+        uint32_t dead = 0;
+#pragma unroll
+        for (int x = 0; x < 4; ++x) s[x] = s4[x] * d.scale;
+        // a tile that the query does not see whole
+        const bool whole = j + 15 <= P && there == 0xffffu && (a.vis.window == 0 || j > P - a.vis.window || j + 15 < a.vis.n_sink);
+        if (!whole) {
+#pragma unroll
+          for (int x = 0; x < 4; ++x)
+            if (!sees(a.vis, P, j + 4 * r16 + x) || !((there >> (4 * r16 + x)) & 1)) {
+              s[x] = NEG_INF;
+              dead |= 1u << x;
+            }
+        }
+        if (log_unit && col < G) {
+#pragma unroll
+          for (int x = 0; x < 4; ++x) s_log[wave][(kept * 16 + 4 * r16 + x) * G + col] = s[x];
+        }
+        float mx = fmaxf(fmaxf(s[0], s[1]), fmaxf(s[2], s[3]));
+        mx = fmaxf(mx, __shfl_xor(mx, 16));
+        mx = fmaxf(mx, __shfl_xor(mx, 32));
+        const float m_new = fmaxf(m_run, mx);
+        if (__any(m_new > m_run)) {
+          const float corr = m_run == NEG_INF ? 0.f : __expf(m_run - m_new);
+          l_run *= corr;
+          scale_acc<G>(acc, corr);
+        }
+        m_run = m_new;
+        float pr[4];
+#pragma unroll
+        for (int x = 0; x < 4; ++x) {
+          pr[x] = (dead >> x) & 1 ? 0.f : __expf(s[x] - m_new);
+          l_run += pr[x];
+        }
+#pragma unroll
+        for (int x = 0; x < 4; ++x) {
+          float v[8];
+          widen<T>(&t.v[x * (sizeof(T) / 2)], v);
+          if (!whole) {                     // a token that is not seen may hold anything: weight 0 is not enough
+#pragma unroll
+            for (int c = 0; c < 8; ++c) v[c] = (dead >> x) & 1 ? 0.f : v[c];
+          }
+          add_pv<G>(acc, pr[x], v);
+        }
+        if (more) {
+          load_v<T, ONE>(t, a.pages.v, next, jn, n, r16, col);
+          there = next.there;
+          if (ti + 8 < t_end) next = tile_rows<ONE>(a, d.Hkv, b, h, tile_token<16>(tr, ti + 8), n, col);
+        }
+        j = jn;
+        if (log_unit && (++kept == PG_KEEP || !more)) {
+          __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+          __builtin_amdgcn_wave_barrier();
+          __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+          // tile k of the kept ones is tile ti - 4 (kept - 1 - k): 4 G pieces of 16 bytes each
+          for (int i = lane; i < kept * 4 * G; i += 64) {
+            const int k = i / (4 * G), e = i % (4 * G);
+            *reinterpret_cast<float4*>(log_unit + (size_t)(ti - 4 * (kept - 1 - k)) * 16 * G + 4 * e) =
+                *reinterpret_cast<const float4*>(&s_log[wave][k * 16 * G + 4 * e]);
+          }
+          __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+          __builtin_amdgcn_wave_barrier();
+          kept = 0;
+        }
+      }
+    }
+    // the four waves together
+    l_run += __shfl_xor(l_run, 16);
+    l_run += __shfl_xor(l_run, 32);
+#pragma unroll
+    for (int g = 0; g < G; ++g)
+#pragma unroll
+      for (int c = 0; c < 8; ++c) {
+        acc[g][c] += __shfl_xor(acc[g][c], 16);
+        acc[g][c] += __shfl_xor(acc[g][c], 32);
+      }
+    if (r16 == 0) {
+      if (col < G) {
+        s_m[wave][col] = m_run;
+        s_l[wave][col] = l_run;
+      }
+#pragma unroll
+      for (int g = 0; g < G; ++g) {
+        *reinterpret_cast<float4*>(&s_o[wave][g][8 * col]) = make_float4(acc[g][0], acc[g][1], acc[g][2], acc[g][3]);
+        *reinterpret_cast<float4*>(&s_o[wave][g][8 * col + 4]) = make_float4(acc[g][4], acc[g][5], acc[g][6], acc[g][7]);
+      }
+    }
+    __syncthreads();
+    const bool all = len == chunks;             // the whole unit: no other workgroup has a part of it
+    const size_t slot = (size_t)w + u;
+    for (int i = threadIdx.x; i < G * D; i += 64 * PG_WAVES) {
+      const int g = i / D, c = i % D;
+      float m = s_m[0][g];
+#pragma unroll
+      for (int x = 1; x < PG_WAVES; ++x) m = fmaxf(m, s_m[x][g]);
+      float l = 0.f, o = 0.f;
+#pragma unroll
+      for (int x = 0; x < PG_WAVES; ++x) {
+        const float f = s_m[x][g] == NEG_INF ? 0.f : __expf(s_m[x][g] - m);
+        l = fmaf(f, s_l[x][g], l);
+        o = fmaf(f, s_o[x][g][c], o);
+      }
+      if (all) Store<T>::store1((T*)a.out + ((size_t)b * d.Hq + h * G + g) * D + c, m == NEG_INF ? 0.f : o / l);
+      else part_o[slot * G * D + i] = o;
+      if (part_ml && c == 0) {
+        part_ml[(slot * G + g) * 2] = m;
+        part_ml[(slot * G + g) * 2 + 1] = l;
+      }
+    }
+    __syncthreads();
+    at += len;
+    p.chunk = 0;
+    if (++p.h == d.Hkv) {
+      p.h = 0;
+      do ++p.b;
+      while (at < end && seq_chunks(a, p.b) == 0);
+    }
+  }
+}
+
+// Joins the pieces of units that several workgroups had (workgroups x < G: head x), and adds the scores (the others, 1024
+// tokens each).
+template <typename T, int G>
+__global__ __launch_bounds__(256) void paged_join_kernel(DevDesc d, PagedArgs a, const float* part_o, const float* part_ml,
+                                                         const float* logits, long long most_tiles, int wgs) {
+  __shared__ float s_m[4][G], s_l[4][G], s_sum[D];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int u = blockIdx.y, b = u / d.Hkv, h = u % d.Hkv;
+  const float NEG_INF = -__builtin_inff();
+  int n;
+  const TileRange tr = unit_tiles(a, b, n);
+  if (tr.n == 0) return;
+  const int slice = (int)blockIdx.x - G;
+  if (slice >= 0 && slice * PG_SLICE >= tr.n * 16) return;
+  const int chunks = (tr.n + 3) >> 2;
+  const long long before = chunks_before(a, b);
+  long long total = before;
+  {
+    long long rest = 0;
+    for (int b0 = b; b0 < d.B; b0 += 64) rest += b0 + lane < d.B ? seq_chunks(a, b0 + lane) : 0;
+    total += wave_sum(rest);
+  }
+  const long long per = piece(total * d.Hkv, wgs);
+  const long long s0 = before * d.Hkv + (long long)h * chunks;
+  const int w0 = (int)(s0 / per), w1 = (int)((s0 + chunks - 1) / per);
+  const int parts = w1 - w0 + 1;
+  if (slice < 0 && parts == 1) return;
+  const size_t slot0 = (size_t)w0 + u;
+
+  // maximum and sum over the pieces
+  float m[G], l[G];
+#pragma unroll
+  for (int g = 0; g < G; ++g) {
+    m[g] = NEG_INF;
+    l[g] = 0.f;
+  }
+  for (int i = threadIdx.x; i < parts; i += 256) {
+#pragma unroll
+    for (int g = 0; g < G; ++g) {
+      const float pm = part_ml[((slot0 + i) * G + g) * 2], pl = part_ml[((slot0 + i) * G + g) * 2 + 1];
+      const float mn = fmaxf(m[g], pm);
+      l[g] = (m[g] == NEG_INF ? 0.f : l[g] * __expf(m[g] - mn)) + (pm == NEG_INF ? 0.f : pl * __expf(pm - mn));
+      m[g] = mn;
+    }
+  }
+#pragma unroll
+  for (int g = 0; g < G; ++g) {
+#pragma unroll
+    for (int k = 1; k < 64; k <<= 1) {
+      const float om = __shfl_xor(m[g], k), ol = __shfl_xor(l[g], k);
+      const float mn = fmaxf(m[g], om);
+      l[g] = (m[g] == NEG_INF ? 0.f : l[g] * __expf(m[g] - mn)) + (om == NEG_INF ? 0.f : ol * __expf(om - mn));
+      m[g] = mn;
+    }
+    if (lane == 0) {
+      s_m[wave][g] = m[g];
+      s_l[wave][g] = l[g];
+    }
+  }
+  __syncthreads();
+#pragma unroll
+  for (int g = 0; g < G; ++g) {
+    m[g] = fmaxf(fmaxf(s_m[0][g], s_m[1][g]), fmaxf(s_m[2][g], s_m[3][g]));
+    l[g] = 0.f;
+#pragma unroll
+    for (int x = 0; x < 4; ++x) l[g] += s_m[x][g] == NEG_INF ? 0.f : s_l[x][g] * __expf(s_m[x][g] - m[g]);
+  }
+  if (slice < 0) {
+    const int g = blockIdx.x, c = threadIdx.x & (D - 1), half = threadIdx.x / D;
+    float mg = m[0], lg = l[0];
+#pragma unroll
+    for (int x = 1; x < G; ++x) {
+      mg = x == g ? m[x] : mg;
+      lg = x == g ? l[x] : lg;
+    }
+    float o = 0.f;
+#pragma unroll 4
+    for (int i = half; i < parts; i += 2) {
+      const float pm = part_ml[((slot0 + i) * G + g) * 2];
+      o = fmaf(pm == NEG_INF ? 0.f : __expf(pm - mg), part_o[(slot0 + i) * G * D + g * D + c], o);
+    }
+    if (half == 1) s_sum[c] = o;
+    __syncthreads();
+    if (half == 0)
+      Store<T>::store1((T*)a.out + ((size_t)b * d.Hq + h * G + g) * D + c, mg == NEG_INF ? 0.f : (o + s_sum[c]) / lg);
+    return;
+  }
+  float lse[G];
+#pragma unroll
+  for (int g = 0; g < G; ++g) lse[g] = m[g] == NEG_INF ? __builtin_inff() : m[g] + __logf(l[g]);
+  for (int i = threadIdx.x; i < PG_SLICE; i += 256) {
+    const int e = slice * PG_SLICE + i;
+    if (e >= tr.n * 16) break;
+    const int j = tile_token<16>(tr, e >> 4) + (e & 15);
+    if (j >= n || j >= a.n_cap) continue;
+    const float* lp = logits + ((size_t)u * most_tiles * 16 + e) * G;
+    float sum = 0.f;
+#pragma unroll
+    for (int g = 0; g < G; ++g) sum += __expf(lp[g] - lse[g]);
+    if (sum != 0.f) a.scores[(size_t)u * a.n_cap + j] += sum;
+  }
+}
+
+template <typename T, int G>
+hipError_t launch(const DevDesc& d, const PagedArgs& a, hipStream_t st) {
+  const PagedPlan p = paged_plan(d, sizeof(T) == 4 ? KVR_F32 : KVR_BF16, a.pages.cap, a.vis, a.scores != nullptr);
+  char* base = (char*)a.ws;
+  float* part_o = p.join ? (float*)(base + p.off_o) : nullptr;
+  float* part_ml = p.join ? (float*)(base + p.off_ml) : nullptr;
+  float* logits = a.scores ? (float*)(base + p.off_log) : nullptr;
+  const bool one = a.pages.table == nullptr || a.pages.page_size % 16 == 0;
+  if (one)
+    hipLaunchKernelGGL((paged_kernel<T, G, true>), dim3(p.wgs), dim3(64 * PG_WAVES), 0, st, d, a, part_o, part_ml, logits, p.tiles);
+  else
+    hipLaunchKernelGGL((paged_kernel<T, G, false>), dim3(p.wgs), dim3(64 * PG_WAVES), 0, st, d, a, part_o, part_ml, logits, p.tiles);
+  const hipError_t e = hipGetLastError();
+  if (e != hipSuccess || !p.join) return e;
+  const unsigned slices = a.scores ? (unsigned)((p.tiles * 16 + PG_SLICE - 1) / PG_SLICE) : 0;
+  hipLaunchKernelGGL((paged_join_kernel<T, G>), dim3(G + slices, d.B * d.Hkv), dim3(256), 0, st, d, a, part_o, part_ml, logits,
+                     p.tiles, p.wgs);
+  return hipGetLastError();
+}
+
+template <typename T>
+hipError_t launch_group(const DevDesc& d, const PagedArgs& a, hipStream_t st) {
+  switch (d.G) {
+    case 1: return launch<T, 1>(d, a, st);
+    case 2: return launch<T, 2>(d, a, st);
+    case 4: return launch<T, 4>(d, a, st);
+    default: return launch<T, 8>(d, a, st);
+  }
+}
+
+}  // namespace
+
+size_t attend_paged_ws(const DevDesc& d, int dtype, long long cap, const Visible& vis, bool scores) {
+  return paged_plan(d, dtype, cap, vis, scores).total;
+}
+hipError_t launch_attend_paged(const DevDesc& d, int dtype, const PagedArgs& a, hipStream_t st) {
+  return dtype == KVR_F32 ? launch_group<float>(d, a, st) : launch_group<bf16_t>(d, a, st);
+}
+
+}  // namespace kvr

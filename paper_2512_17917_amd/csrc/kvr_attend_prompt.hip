@@ -225,11 +225,5 @@ size_t attend_prompt_ws(const DevDesc& d, int dtype, long long n_rows, long long
 hipError_t launch_attend_prompt(const DevDesc& d, int dtype, const PagedArgs& a, hipStream_t st) {
   return dtype == KVR_F32 ? launch<float>(d, a, st) : launch<bf16_t>(d, a, st);
 }
-size_t attend_paged_ws(const DevDesc& d, int dtype, long long cap, const Visible& vis, bool scores) {
-  return attend_prompt_ws(d, dtype, d.B, cap, vis, scores);
-}
-hipError_t launch_attend_paged(const DevDesc& d, int dtype, const PagedArgs& a, hipStream_t st) {
-  return launch_attend_prompt(d, dtype, a, st);
-}
 
 }  // namespace kvr
