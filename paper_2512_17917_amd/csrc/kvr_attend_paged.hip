@@ -15,7 +15,8 @@
 // last one's; the table a tile earlier.
 //
 // Scores need the final sum, so logits are kept (G floats a token, through LDS: a store between the loads would make every
-// wait for a load a wait for all) and the second kernel adds exp(s - lse).
+// wait for a load a wait for all) and the second kernel adds exp(s - lse).  All in powers of
+// two: s = (scale / ln 2) q.k.
 #include "kvr_launch.h"
 
 namespace kvr {
@@ -62,6 +63,17 @@ PagedPlan paged_plan(const DevDesc& d, int dtype, long long cap, const Visible& 
   return p;
 }
 
+constexpr float LOG2E = 1.4426950408889634f;
+__device__ __forceinline__ float exp2_(float x) { return __builtin_amdgcn_exp2f(x); }
+
+// largest of lanes l, l ^ 16, l ^ 32, l ^ 48
+__device__ __forceinline__ float rows_max(float x) {
+  auto a = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  x = fmaxf(__uint_as_float(a[0]), __uint_as_float(a[1]));
+  auto b = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return fmaxf(__uint_as_float(b[0]), __uint_as_float(b[1]));
+}
+
 // value held by lane N of the caller's 16-lane row
 template <int N>
 __device__ __forceinline__ float row_bcast(float x) {
@@ -88,7 +100,7 @@ __device__ __forceinline__ void scale_acc(float (&acc)[G][8], float f) {
 
 // ---- the row of chunks -----------------------------------------------------
 __device__ __forceinline__ TileRange unit_tiles(const PagedArgs& a, int b, int& n) {
-  n = clampi(a.n_ctx[b], 0, a.pages.cap);
+  n = clampi(listed(a.n_ctx + b), 0, a.pages.cap);
   return tile_range<16>(a.vis, n - 1, n - 1);
 }
 __device__ __forceinline__ int seq_chunks(const PagedArgs& a, int b) {
@@ -105,7 +117,7 @@ __device__ __forceinline__ long long chunks_before(const PagedArgs& a, int upto)
   const int lane = threadIdx.x & 63;
   long long sum = 0;
   for (int b0 = 0; b0 < upto; b0 += 64) sum += b0 + lane < upto ? seq_chunks(a, b0 + lane) : 0;
-  return wave_sum(sum);
+  return uniform(wave_sum(sum));
 }
 // chunks a workgroup takes
 __device__ __forceinline__ long long piece(long long total, int wgs) { return (total + wgs - 1) / wgs; }
@@ -130,7 +142,7 @@ __device__ __forceinline__ Where find_chunk(const PagedArgs& a, int B, int heads
       const int l = __ffsll(past) - 1;
       const int n = __shfl(mine, l);
       const long long off = at - (base + __shfl(upto, l) - n) * heads;
-      return {b0 + l, (int)(off / n), (int)(off % n)};
+      return {uniform(b0 + l), uniform((int)(off / n)), uniform((int)(off % n))};
     }
     base += __shfl(upto, 63);
   }
@@ -145,18 +157,18 @@ struct TileRows {
   uint32_t there;       // bit i: token i lies on a page
 };
 
+// entry: the table's, of the tile's first token or of token lane mod 16 (which was asked for a tile earlier)
 template <bool ONE>
-__device__ __forceinline__ TileRows<ONE> tile_rows(const PagedArgs& a, int heads, int b, int h, int j0, int n, int col) {
+__device__ __forceinline__ int tile_entry(const PagedArgs& a, int b, int j0, int n, int col) {
+  return page_entry(a.pages, b, ONE ? j0 : min(j0 + col, n - 1));
+}
+template <bool ONE>
+__device__ __forceinline__ TileRows<ONE> tile_rows(const PagedArgs& a, int heads, int entry, int h, int j0, int n, int col) {
   TileRows<ONE> t;
-  if constexpr (ONE) {
-    const long long r = page_row(a.pages, heads, b, h, j0);
-    t.row = r < 0 ? 0 : r;
-    t.there = r < 0 ? 0u : 0xffffu;
-  } else {
-    const long long r = page_row(a.pages, heads, b, h, min(j0 + col, n - 1));
-    t.row = r < 0 ? 0 : r;
-    t.there = (uint32_t)__ballot(r >= 0) & 0xffffu;
-  }
+  const long long r = entry_row(a.pages, heads, entry, h, ONE ? j0 : min(j0 + col, n - 1));
+  t.row = r < 0 ? 0 : r;
+  if constexpr (ONE) t.there = r < 0 ? 0u : 0xffffu;
+  else t.there = (uint32_t)__ballot(r >= 0) & 0xffffu;
   return t;
 }
 
@@ -227,14 +239,16 @@ __global__ __launch_bounds__(64 * PG_WAVES, paged_per_cu(sizeof(T), G)) void pag
   __shared__ __align__(16) float s_o[PG_WAVES][G][D];
   __shared__ float s_m[PG_WAVES][G], s_l[PG_WAVES][G];
   __shared__ __align__(16) float s_log[PG_WAVES][PG_KEEP * 16 * G];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int lane = threadIdx.x & 63, wave = uniform((int)(threadIdx.x >> 6));
   const int r16 = lane >> 4, col = lane & 15;
   const int w = blockIdx.x;
   const float NEG_INF = -__builtin_inff();
+  constexpr int PER = sizeof(T) / 2;                  // 16-byte pieces of eight channels
+  const float scale2 = d.scale * LOG2E;               // logits in powers of two
 
   // sequences without a token yield zeros
   for (int b = w; b < d.B; b += gridDim.x)
-    if (a.n_ctx[b] <= 0)
+    if (listed(a.n_ctx + b) <= 0)
       for (int i = threadIdx.x; i < d.Hq * D; i += 64 * PG_WAVES) Store<T>::store1((T*)a.out + (size_t)b * d.Hq * D + i, 0.f);
 
   const long long total = chunks_before(a, d.B) * d.Hkv;
@@ -244,8 +258,7 @@ __global__ __launch_bounds__(64 * PG_WAVES, paged_per_cu(sizeof(T), G)) void pag
   if (at >= end) return;
   Where p = find_chunk(a, d.B, d.Hkv, at);
   while (at < end) {
-    const int b = __builtin_amdgcn_readfirstlane(p.b), h = __builtin_amdgcn_readfirstlane(p.h);
-    const int c0 = __builtin_amdgcn_readfirstlane(p.chunk);
+    const int b = uniform(p.b), h = uniform(p.h), c0 = uniform(p.chunk);
     int n;
     const TileRange tr = unit_tiles(a, b, n);
     const int chunks = (tr.n + 3) >> 2;
@@ -257,11 +270,8 @@ __global__ __launch_bounds__(64 * PG_WAVES, paged_per_cu(sizeof(T), G)) void pag
     u32x4_t q[Tile<T>::N];
     {
       const T* qp = (const T*)a.q + ((size_t)b * d.Hq + h * G + min(col, G - 1)) * D + 8 * r16;
-      constexpr int PER = sizeof(T) / 2;
 #pragma unroll
-      for (int i = 0; i < Tile<T>::N; ++i) {
-        q[i] = *reinterpret_cast<const u32x4_t*>(qp + 32 * (i / PER) + 4 * (i % PER));
-      }
+      for (int i = 0; i < Tile<T>::N; ++i) q[i] = *reinterpret_cast<const u32x4_t*>(qp + 32 * (i / PER) + 4 * (i % PER));
     }
     float acc[G][8];
 #pragma unroll
@@ -274,24 +284,29 @@ __global__ __launch_bounds__(64 * PG_WAVES, paged_per_cu(sizeof(T), G)) void pag
 
     int ti = 4 * c0 + wave;
     Tile<T> t;
-    TileRows<ONE> next = {};
+    int entry = 0;                         // of the wave's next tile
     if (ti < t_end) {
       const int j0 = tile_token<16>(tr, ti);
-      const TileRows<ONE> now = tile_rows<ONE>(a, d.Hkv, b, h, j0, n, col);
+      TileRows<ONE> now = tile_rows<ONE>(a, d.Hkv, tile_entry<ONE>(a, b, j0, n, col), h, j0, n, col);
       load_k<T, ONE>(t, a.pages.k, now, j0, n, r16, col);
       load_v<T, ONE>(t, a.pages.v, now, j0, n, r16, col);
-      uint32_t there = now.there;
-      if (ti + 4 < t_end) next = tile_rows<ONE>(a, d.Hkv, b, h, tile_token<16>(tr, ti + 4), n, col);
+      if (ti + 4 < t_end) entry = tile_entry<ONE>(a, b, tile_token<16>(tr, ti + 4), n, col);
       int j = j0;
       for (; ti < t_end; ti += 4) {
         const f32x4_t s4 = tile_logits<T>(t.k, q);
         const bool more = ti + 4 < t_end;
         const int jn = more ? tile_token<16>(tr, ti + 4) : j;
-        if (more) load_k<T, ONE>(t, a.pages.k, next, jn, n, r16, col);
+        const uint32_t there = now.there;
+        if (more) {
+          now = tile_rows<ONE>(a, d.Hkv, entry, h, jn, n, col);
+          load_k<T, ONE>(t, a.pages.k, now, jn, n, r16, col);
+          if (ti + 8 < t_end) entry = tile_entry<ONE>(a, b, tile_token<16>(tr, ti + 8), n, col);
+        }
+        __builtin_amdgcn_sched_barrier(0);
         float s[4];
         uint32_t dead = 0;
 #pragma unroll
-        for (int x = 0; x < 4; ++x) s[x] = s4[x] * d.scale;
+        for (int x = 0; x < 4; ++x) s[x] = s4[x] * scale2;
         // a tile that the query does not see whole
         const bool whole = j + 15 <= P && there == 0xffffu && (a.vis.window == 0 || j > P - a.vis.window || j + 15 < a.vis.n_sink);
         if (!whole) {
@@ -300,6 +315,9 @@ __global__ __launch_bounds__(64 * PG_WAVES, paged_per_cu(sizeof(T), G)) void pag
             if (!sees(a.vis, P, j + 4 * r16 + x) || !((there >> (4 * r16 + x)) & 1)) {
               s[x] = NEG_INF;
               dead |= 1u << x;
+              // it may hold anything: weight 0 is not enough
+#pragma unroll
+              for (int i = 0; i < PER; ++i) t.v[x * PER + i] = u32x4_t{0, 0, 0, 0};
             }
         }
         if (log_unit && col < G) {
@@ -307,11 +325,10 @@ __global__ __launch_bounds__(64 * PG_WAVES, paged_per_cu(sizeof(T), G)) void pag
           for (int x = 0; x < 4; ++x) s_log[wave][(kept * 16 + 4 * r16 + x) * G + col] = s[x];
         }
         float mx = fmaxf(fmaxf(s[0], s[1]), fmaxf(s[2], s[3]));
-        mx = fmaxf(mx, __shfl_xor(mx, 16));
-        mx = fmaxf(mx, __shfl_xor(mx, 32));
+        mx = rows_max(mx);
         const float m_new = fmaxf(m_run, mx);
         if (__any(m_new > m_run)) {
-          const float corr = m_run == NEG_INF ? 0.f : __expf(m_run - m_new);
+          const float corr = m_run == NEG_INF ? 0.f : exp2_(m_run - m_new);
           l_run *= corr;
           scale_acc<G>(acc, corr);
         }
@@ -319,24 +336,22 @@ __global__ __launch_bounds__(64 * PG_WAVES, paged_per_cu(sizeof(T), G)) void pag
         float pr[4];
 #pragma unroll
         for (int x = 0; x < 4; ++x) {
-          pr[x] = (dead >> x) & 1 ? 0.f : __expf(s[x] - m_new);
+          pr[x] = (dead >> x) & 1 ? 0.f : exp2_(s[x] - m_new);
           l_run += pr[x];
         }
 #pragma unroll
         for (int x = 0; x < 4; ++x) {
           float v[8];
           widen<T>(&t.v[x * (sizeof(T) / 2)], v);
-          if (!whole) {                     // a token that is not seen may hold anything: weight 0 is not enough
-#pragma unroll
-            for (int c = 0; c < 8; ++c) v[c] = (dead >> x) & 1 ? 0.f : v[c];
-          }
           add_pv<G>(acc, pr[x], v);
+          // one token's floats at a time, and all of them before the next loads: registers
+#pragma unroll
+          for (int g = 0; g < G; ++g)
+#pragma unroll
+            for (int c = 0; c < 8; ++c) asm volatile("" : "+v"(acc[g][c]));
+          __builtin_amdgcn_sched_barrier(0);
         }
-        if (more) {
-          load_v<T, ONE>(t, a.pages.v, next, jn, n, r16, col);
-          there = next.there;
-          if (ti + 8 < t_end) next = tile_rows<ONE>(a, d.Hkv, b, h, tile_token<16>(tr, ti + 8), n, col);
-        }
+        if (more) load_v<T, ONE>(t, a.pages.v, now, jn, n, r16, col);
         j = jn;
         if (log_unit && (++kept == PG_KEEP || !more)) {
           __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
@@ -386,7 +401,7 @@ __global__ __launch_bounds__(64 * PG_WAVES, paged_per_cu(sizeof(T), G)) void pag
       float l = 0.f, o = 0.f;
 #pragma unroll
       for (int x = 0; x < PG_WAVES; ++x) {
-        const float f = s_m[x][g] == NEG_INF ? 0.f : __expf(s_m[x][g] - m);
+        const float f = s_m[x][g] == NEG_INF ? 0.f : exp2_(s_m[x][g] - m);
         l = fmaf(f, s_l[x][g], l);
         o = fmaf(f, s_o[x][g][c], o);
       }
@@ -449,7 +464,7 @@ __global__ __launch_bounds__(256) void paged_join_kernel(DevDesc d, PagedArgs a,
     for (int g = 0; g < G; ++g) {
       const float pm = part_ml[((slot0 + i) * G + g) * 2], pl = part_ml[((slot0 + i) * G + g) * 2 + 1];
       const float mn = fmaxf(m[g], pm);
-      l[g] = (m[g] == NEG_INF ? 0.f : l[g] * __expf(m[g] - mn)) + (pm == NEG_INF ? 0.f : pl * __expf(pm - mn));
+      l[g] = (m[g] == NEG_INF ? 0.f : l[g] * exp2_(m[g] - mn)) + (pm == NEG_INF ? 0.f : pl * exp2_(pm - mn));
       m[g] = mn;
     }
   }
@@ -459,7 +474,7 @@ __global__ __launch_bounds__(256) void paged_join_kernel(DevDesc d, PagedArgs a,
     for (int k = 1; k < 64; k <<= 1) {
       const float om = __shfl_xor(m[g], k), ol = __shfl_xor(l[g], k);
       const float mn = fmaxf(m[g], om);
-      l[g] = (m[g] == NEG_INF ? 0.f : l[g] * __expf(m[g] - mn)) + (om == NEG_INF ? 0.f : ol * __expf(om - mn));
+      l[g] = (m[g] == NEG_INF ? 0.f : l[g] * exp2_(m[g] - mn)) + (om == NEG_INF ? 0.f : ol * exp2_(om - mn));
       m[g] = mn;
     }
     if (lane == 0) {
@@ -473,7 +488,7 @@ __global__ __launch_bounds__(256) void paged_join_kernel(DevDesc d, PagedArgs a,
     m[g] = fmaxf(fmaxf(s_m[0][g], s_m[1][g]), fmaxf(s_m[2][g], s_m[3][g]));
     l[g] = 0.f;
 #pragma unroll
-    for (int x = 0; x < 4; ++x) l[g] += s_m[x][g] == NEG_INF ? 0.f : s_l[x][g] * __expf(s_m[x][g] - m[g]);
+    for (int x = 0; x < 4; ++x) l[g] += s_m[x][g] == NEG_INF ? 0.f : s_l[x][g] * exp2_(s_m[x][g] - m[g]);
   }
   if (slice < 0) {
     const int g = blockIdx.x, c = threadIdx.x & (D - 1), half = threadIdx.x / D;
@@ -487,7 +502,7 @@ __global__ __launch_bounds__(256) void paged_join_kernel(DevDesc d, PagedArgs a,
 #pragma unroll 4
     for (int i = half; i < parts; i += 2) {
       const float pm = part_ml[((slot0 + i) * G + g) * 2];
-      o = fmaf(pm == NEG_INF ? 0.f : __expf(pm - mg), part_o[(slot0 + i) * G * D + g * D + c], o);
+      o = fmaf(pm == NEG_INF ? 0.f : exp2_(pm - mg), part_o[(slot0 + i) * G * D + g * D + c], o);
     }
     if (half == 1) s_sum[c] = o;
     __syncthreads();
@@ -497,7 +512,7 @@ __global__ __launch_bounds__(256) void paged_join_kernel(DevDesc d, PagedArgs a,
   }
   float lse[G];
 #pragma unroll
-  for (int g = 0; g < G; ++g) lse[g] = m[g] == NEG_INF ? __builtin_inff() : m[g] + __logf(l[g]);
+  for (int g = 0; g < G; ++g) lse[g] = m[g] == NEG_INF ? __builtin_inff() : m[g] + __builtin_amdgcn_logf(l[g]);
   for (int i = threadIdx.x; i < PG_SLICE; i += 256) {
     const int e = slice * PG_SLICE + i;
     if (e >= tr.n * 16) break;
@@ -506,7 +521,7 @@ __global__ __launch_bounds__(256) void paged_join_kernel(DevDesc d, PagedArgs a,
     const float* lp = logits + ((size_t)u * most_tiles * 16 + e) * G;
     float sum = 0.f;
 #pragma unroll
-    for (int g = 0; g < G; ++g) sum += __expf(lp[g] - lse[g]);
+    for (int g = 0; g < G; ++g) sum += exp2_(lp[g] - lse[g]);
     if (sum != 0.f) a.scores[(size_t)u * a.n_cap + j] += sum;
   }
 }

@@ -5,6 +5,16 @@
 
 namespace kvr {
 
+// A number of the caller's lists, which no kernel writes: where the address is the same for the whole wave it comes through
+// the scalar unit.
+__host__ __device__ __forceinline__ int32_t listed(const int32_t* p) {
+#ifdef __HIP_DEVICE_COMPILE__
+  return *(const __attribute__((address_space(4))) int32_t*)p;
+#else
+  return *p;
+#endif
+}
+
 // kvr_pages as the kernels take it.  Token j of sequence b lies in row j % page_size of page table[b][j / page_size]; without
 // a table sequence b has the one page b.  The quotient by the page size comes from a product: with 2^(s-1) < size <= 2^s and
 // magic = floor(2^(31+s) / size) + 1, (j magic) >> (31 + s) is exact for 0 <= j < 2^31, and magic fits 32 bits.
@@ -37,13 +47,18 @@ inline DevPages dev_pages(const kvr_pages& c) {
 __host__ __device__ __forceinline__ int page_index(const DevPages& p, int j) {
   return (int)(((uint64_t)(uint32_t)j * p.magic) >> p.shift);
 }
-// Row of token j (0 <= j < cap) of sequence b, kv head h, counted in rows of D channels from the pools' start; -1 where the
+// Page of token j (0 <= j < cap) of sequence b as the table has it
+__host__ __device__ __forceinline__ int page_entry(const DevPages& p, int b, int j) {
+  return p.table ? listed(p.table + (size_t)b * p.table_cap + page_index(p, j)) : b;
+}
+// its row in that page, of kv head h, counted in rows of D channels from the pools' start; -1 where the
 // table names no page.
-__host__ __device__ __forceinline__ long long page_row(const DevPages& p, int n_kv_heads, int b, int h, int j) {
-  const int i = page_index(p, j);
-  const int page = p.table ? p.table[(size_t)b * p.table_cap + i] : b;
+__host__ __device__ __forceinline__ long long entry_row(const DevPages& p, int n_kv_heads, int page, int h, int j) {
   if ((uint32_t)page >= (uint32_t)p.n_pages) return -1;
-  return ((long long)page * n_kv_heads + h) * p.page_size + (j - i * p.page_size);
+  return ((long long)page * n_kv_heads + h) * p.page_size + (j - page_index(p, j) * p.page_size);
+}
+__host__ __device__ __forceinline__ long long page_row(const DevPages& p, int n_kv_heads, int b, int h, int j) {
+  return entry_row(p, n_kv_heads, page_entry(p, b, j), h, j);
 }
 
 // New tokens of the batch: rows q_start[b] .. q_start[b + 1] - 1 are sequence b's, or row b where q_start is null.
@@ -52,8 +67,8 @@ struct RowSpan {
 };
 __host__ __device__ __forceinline__ RowSpan row_span(const int32_t* q_start, int n_rows, int b) {
   if (q_start == nullptr) return {b, 1};
-  const int first = clampi(q_start[b], 0, n_rows);
-  return {first, clampi(q_start[b + 1], first, n_rows) - first};
+  const int first = clampi(listed(q_start + b), 0, n_rows);
+  return {first, clampi(listed(q_start + b + 1), first, n_rows) - first};
 }
 // Sequence of row `row` (wave-uniform; all lanes call), -1 if it is none's.  Row starts do not fall.
 __device__ __forceinline__ int seq_of_row(const int32_t* q_start, int B, int row) {
@@ -61,12 +76,20 @@ __device__ __forceinline__ int seq_of_row(const int32_t* q_start, int B, int row
   const int lane = threadIdx.x & 63;
   int before = 0;                   // sequences that end at or before the row
   for (int b0 = 0; b0 < B; b0 += 64) {
-    const bool past = b0 + lane < B && q_start[b0 + lane + 1] <= row;
+    const bool past = b0 + lane < B && listed(q_start + b0 + lane + 1) <= row;
     const int n = __popcll(__ballot(past));
     before += n;
     if (n < 64) break;
   }
-  return before < B && q_start[before] <= row ? before : -1;
+  return before < B && listed(q_start + before) <= row ? before : -1;
+}
+
+// a value that all lanes of a wave have, for the scalar registers
+__device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
+__device__ __forceinline__ long long uniform(long long x) {
+  const uint32_t lo = (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)x);
+  const uint32_t hi = (uint32_t)__builtin_amdgcn_readfirstlane((int)(x >> 32));
+  return (long long)(((uint64_t)hi << 32) | lo);
 }
 
 // Column tile blockIdx.x of a launch: a sequence's new tokens times its kv head's G query heads are columns m = t G + g, in
