@@ -163,7 +163,7 @@ typedef struct kvr_attend_opts {
  *              sequence b has the one page b (n_pages >= B, table_cap ignored), which makes
  *              k, v a dense cache [B, Hkv, page_size, D].
  *   page_size  tokens a page, >= 1.  A sequence holds at most table_cap * page_size (dense:
- *              page_size) tokens, which must be no more than 2^30.
+ *              page_size) tokens, which must be no more than 2^30; n_pages * Hkv * page_size < 2^31.
  * Several sequences may name the same page; two that store to one row in the same call
  * leave it unspecified.
  */

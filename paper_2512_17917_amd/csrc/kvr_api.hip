@@ -431,6 +431,8 @@ static int32_t pages_size(const kvr_desc* desc, const kvr_pages* pages, kvr::Dev
     return KVR_ERR_INVALID_ARG;
   }
   if (cap > MAX_TOKENS) return KVR_ERR_INVALID_ARG;
+  // rows of the pools, in 31 bits: a pool of more would not fit the memory
+  if ((long long)pages->n_pages * pages->page_size > 0x7fffffffll / desc->n_kv_heads) return KVR_ERR_INVALID_ARG;
   p = kvr::dev_pages(*pages);
   return KVR_OK;
 }

@@ -16,6 +16,9 @@ namespace {
 
 typedef float f32x4_t __attribute__((ext_vector_type(4)));
 
+constexpr float LOG2E = 1.4426950408889634f;
+__device__ __forceinline__ float exp2_(float x) { return __builtin_amdgcn_exp2f(x); }
+
 constexpr int PP_COLS = 16, PP_WAVES = 4;
 
 // 32 channels of a row: 8 (lane div 16) .. +7 of each block of 32
@@ -86,6 +89,7 @@ __global__ __launch_bounds__(64 * PP_WAVES) void prompt_kernel(DevDesc d, PagedA
   const int t_last = (int)((m0 + PP_COLS <= cols ? m0 + PP_COLS - 1 : cols - 1) / d.G);
   const int lo = first + (int)(m0 / d.G), hi = first + t_last;
   const TileRange tr = tile_range<16>(a.vis, lo, hi);
+  const float scale2 = d.scale * LOG2E;
   const size_t at = (size_t)(span.first + (live ? t : 0)) * d.Hq + hk * d.G + g;   // this column's row of q and out
   const T* kp = (const T*)a.pages.k;
   const T* vp = (const T*)a.pages.v;
@@ -108,7 +112,7 @@ __global__ __launch_bounds__(64 * PP_WAVES) void prompt_kernel(DevDesc d, PagedA
 #pragma unroll
     for (int x = 0; x < 4; ++x) {
       const bool ok = sees(a.vis, P, j0 + 4 * r + x) && ((there >> (4 * r + x)) & 1);
-      s[x] = ok ? s4[x] * d.scale : NEG_INF;
+      s[x] = ok ? s4[x] * scale2 : NEG_INF;
       seen4 |= ok ? 1u << x : 0u;
     }
     float mx = fmaxf(fmaxf(s[0], s[1]), fmaxf(s[2], s[3]));
@@ -116,7 +120,7 @@ __global__ __launch_bounds__(64 * PP_WAVES) void prompt_kernel(DevDesc d, PagedA
     mx = fmaxf(mx, __shfl_xor(mx, 32));
     const float m_new = fmaxf(m_run, mx);
     if (__any(m_new > m_run)) {
-      const float corr = m_run == NEG_INF ? 0.f : __expf(m_run - m_new);
+      const float corr = m_run == NEG_INF ? 0.f : exp2_(m_run - m_new);
       l_run *= corr;
 #pragma unroll
       for (int cb = 0; cb < 8; ++cb)
@@ -127,7 +131,7 @@ __global__ __launch_bounds__(64 * PP_WAVES) void prompt_kernel(DevDesc d, PagedA
     f32x4_t p;
 #pragma unroll
     for (int x = 0; x < 4; ++x) {
-      p[x] = (seen4 >> x) & 1 ? __expf(s[x] - m_new) : 0.f;
+      p[x] = (seen4 >> x) & 1 ? exp2_(s[x] - m_new) : 0.f;
       l_run += p[x];
     }
     bool odd = false;
@@ -153,7 +157,7 @@ __global__ __launch_bounds__(64 * PP_WAVES) void prompt_kernel(DevDesc d, PagedA
   for (int cb = 0; cb < 8; ++cb)
 #pragma unroll
     for (int x = 0; x < 4; ++x) Store<T>::store1(out + 16 * cb + 4 * r + x, m_run == NEG_INF ? 0.f : o[cb][x] * inv);
-  if (lse && r == 0) lse[at] = m_run == NEG_INF ? __builtin_inff() : m_run + __logf(l_run);
+  if (lse && r == 0) lse[at] = m_run == NEG_INF ? __builtin_inff() : m_run + __builtin_amdgcn_logf(l_run);
 }
 
 template <typename T>
@@ -177,6 +181,7 @@ __global__ __launch_bounds__(64 * PP_WAVES) void prompt_scores_kernel(DevDesc d,
     const long long past = (long long)j0 + 15 + a.vis.window - first;
     t1 = past < t1 ? past : t1;
   }
+  const float scale2 = d.scale * LOG2E;
   float acc[4] = {0.f, 0.f, 0.f, 0.f};
   const long long cols = t1 * d.G;
   for (long long m0 = t0 * d.G; m0 < cols; m0 += PP_COLS) {
@@ -190,7 +195,7 @@ __global__ __launch_bounds__(64 * PP_WAVES) void prompt_scores_kernel(DevDesc d,
     const f32x4_t s4 = logits16(k, q);
 #pragma unroll
     for (int x = 0; x < 4; ++x)
-      acc[x] += live && sees(a.vis, first + t, j0 + 4 * r + x) ? __expf(s4[x] * d.scale - lc) : 0.f;
+      acc[x] += live && sees(a.vis, first + t, j0 + 4 * r + x) ? exp2_(s4[x] * scale2 - lc) : 0.f;
   }
 #pragma unroll
   for (int x = 0; x < 4; ++x) {
@@ -203,27 +208,33 @@ __global__ __launch_bounds__(64 * PP_WAVES) void prompt_scores_kernel(DevDesc d,
 }
 
 template <typename T>
-hipError_t launch(const DevDesc& d, const PagedArgs& a, hipStream_t st) {
-  float* lse = a.scores ? (float*)a.ws : nullptr;
-  const dim3 block(64 * PP_WAVES);
-  const dim3 grid((unsigned)col_tiles_most(a.n_rows, d.B, d.G, PP_COLS * PP_WAVES), d.Hkv);
-  hipLaunchKernelGGL((prompt_kernel<T>), grid, block, 0, st, d, a, lse);
-  hipError_t e = hipGetLastError();
-  if (e != hipSuccess || a.scores == nullptr) return e;
+hipError_t launch_scores(const DevDesc& d, const PagedArgs& a, const float* lse, hipStream_t st) {
   const long long most = a.n_cap < a.pages.cap ? a.n_cap : a.pages.cap;
-  const dim3 grid2((unsigned)((most + 16 * PP_WAVES - 1) / (16 * PP_WAVES)), d.B * d.Hkv);
-  hipLaunchKernelGGL((prompt_scores_kernel<T>), grid2, block, 0, st, d, a, lse);
+  const dim3 grid((unsigned)((most + 16 * PP_WAVES - 1) / (16 * PP_WAVES)), d.B * d.Hkv);
+  hipLaunchKernelGGL((prompt_scores_kernel<T>), grid, dim3(64 * PP_WAVES), 0, st, d, a, lse);
   return hipGetLastError();
 }
 
 }  // namespace
 
 size_t attend_prompt_ws(const DevDesc& d, int dtype, long long n_rows, long long cap, const Visible& vis, bool scores) {
-  (void)dtype; (void)cap; (void)vis;
+  if (dtype == KVR_BF16) return prompt_bf16_plan(d, n_rows, cap, vis, scores).total;
   return scores ? (size_t)n_rows * d.Hq * sizeof(float) : 0;
 }
+
 hipError_t launch_attend_prompt(const DevDesc& d, int dtype, const PagedArgs& a, hipStream_t st) {
-  return dtype == KVR_F32 ? launch<float>(d, a, st) : launch<bf16_t>(d, a, st);
+  if (dtype == KVR_BF16) {
+    const PromptPlan p = prompt_bf16_plan(d, a.n_rows, a.pages.cap, a.vis, a.scores != nullptr);
+    const hipError_t e = launch_prompt_bf16(d, a, p, st);
+    if (e != hipSuccess || a.scores == nullptr) return e;
+    return launch_scores<bf16_t>(d, a, (const float*)((const char*)a.ws + p.off_lse), st);
+  }
+  float* lse = a.scores ? (float*)a.ws : nullptr;
+  const dim3 grid((unsigned)col_tiles_most(a.n_rows, d.B, d.G, PP_COLS * PP_WAVES), d.Hkv);
+  hipLaunchKernelGGL((prompt_kernel<float>), grid, dim3(64 * PP_WAVES), 0, st, d, a, lse);
+  const hipError_t e = hipGetLastError();
+  if (e != hipSuccess || a.scores == nullptr) return e;
+  return launch_scores<float>(d, a, lse, st);
 }
 
 }  // namespace kvr

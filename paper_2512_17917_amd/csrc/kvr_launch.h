@@ -254,6 +254,14 @@ struct PagedArgs {
   long long n_cap;
   void* ws;
 };
+// bf16 kernel of a prompt's attention: into how many parts a tile's tokens are split, and its workspace (first the columns'
+// maximum plus logarithm of the sum, in powers of two, where scores want them)
+struct PromptPlan {
+  int splits;
+  size_t off_lse, off_o, off_ml, total;
+};
+PromptPlan prompt_bf16_plan(const DevDesc& d, long long n_rows, long long cap, const Visible& vis, bool scores);
+hipError_t launch_prompt_bf16(const DevDesc& d, const PagedArgs& a, const PromptPlan& p, hipStream_t st);
 size_t attend_prompt_ws(const DevDesc& d, int dtype, long long n_rows, long long cap, const Visible& vis, bool scores);
 hipError_t launch_attend_prompt(const DevDesc& d, int dtype, const PagedArgs& a, hipStream_t st);
 size_t attend_paged_ws(const DevDesc& d, int dtype, long long cap, const Visible& vis, bool scores);
