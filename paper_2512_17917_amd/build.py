@@ -24,7 +24,7 @@ CC = "gcc"
 
 SOURCES = ["kvr_api.hip", "kvr_reconstruct.hip", "kvr_attend.hip", "kvr_attend_staged.hip", "kvr_attend_staged64.hip", "kvr_attend_staged16.hip", "kvr_attend_retained.hip", "kvr_select.hip", "kvr_compact.hip",
            "kvr_encode.hip", "kvr_swap.hip", "kvr_attend_multi.hip", "kvr_attend_multi_staged.hip",
-           "kvr_rotate.hip", "kvr_attend_prompt.hip", "kvr_attend_prompt_bf16.hip",
+           "kvr_rotate.hip", "kvr_attend_prompt.hip", "kvr_attend_prompt_bf16.hip", "kvr_attend_prompt_scores.hip",
            "kvr_attend_paged.hip"]
 
 # packed-FP32 instruction selection is switched off on purpose (ordinary float

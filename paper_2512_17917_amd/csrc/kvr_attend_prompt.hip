@@ -227,7 +227,8 @@ hipError_t launch_attend_prompt(const DevDesc& d, int dtype, const PagedArgs& a,
     const PromptPlan p = prompt_bf16_plan(d, a.n_rows, a.pages.cap, a.vis, a.scores != nullptr);
     const hipError_t e = launch_prompt_bf16(d, a, p, st);
     if (e != hipSuccess || a.scores == nullptr) return e;
-    return launch_scores<bf16_t>(d, a, (const float*)((const char*)a.ws + p.off_lse), st);
+    char* base = (char*)a.ws;
+    return launch_prompt_scores_bf16(d, a, p.scores, (const float*)(base + p.off_lse), (float*)(base + p.off_scores), st);
   }
   float* lse = a.scores ? (float*)a.ws : nullptr;
   const dim3 grid((unsigned)col_tiles_most(a.n_rows, d.B, d.G, PP_COLS * PP_WAVES), d.Hkv);

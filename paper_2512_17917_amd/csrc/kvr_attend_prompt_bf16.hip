@@ -19,52 +19,17 @@
 // In tiles that some column does not see whole, rows that nobody sees are cleared in LDS and values that are not finite are
 // taken out (0 x inf would reach every column); what they are to the columns that see them is added apart.
 #include "kvr_launch.h"
+#include "kvr_prompt.h"
 
 namespace kvr {
 
 namespace {
 
-typedef __bf16 bf16x8_t __attribute__((ext_vector_type(8)));
-typedef __bf16 bf16x2_t __attribute__((ext_vector_type(2)));
-typedef float f32x16_t __attribute__((ext_vector_type(16)));
-typedef float f32x2_t __attribute__((ext_vector_type(2)));
-typedef short s16x4_t __attribute__((ext_vector_type(4)));
-typedef uint32_t u32x4_t __attribute__((ext_vector_type(4)));
-
 constexpr int FP_WAVES = 8, FP_COLS = 32 * FP_WAVES, FP_KEYS = 64;
 constexpr int FP_TILE = FP_KEYS * D * 2;                       // bytes of a tile of keys or values
 constexpr int FP_P = FP_KEYS * 32 * 4;                         // a wave's weights, for values that are not finite
 constexpr int FP_LDS = 4 * FP_TILE + FP_WAVES * FP_P + 64;
-constexpr float LOG2E = 1.4426950408889634f;
 constexpr float KEEP_MAX = 8.f;
-
-// 16 bytes a lane from memory to LDS, lane l's to `lds` + 16 l (a wave's number).  The compiler has a builtin for it but waits
-// for all such loads before the next read of LDS, which would be every tile's; here the kernel waits where it must.
-__device__ __forceinline__ void to_lds(const unsigned char* from, uint32_t lds) {
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(lds), "v"(from) : "m0", "memory");
-}
-__device__ __forceinline__ uint32_t lds_offset(const void* p) {
-  return (uint32_t)(uintptr_t)(const __attribute__((address_space(3))) void*)p;
-}
-
-__device__ __forceinline__ float exp2_(float x) { return __builtin_amdgcn_exp2f(x); }
-__device__ __forceinline__ float across_max(float x) {
-  auto a = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
-  return fmaxf(__uint_as_float(a[0]), __uint_as_float(a[1]));
-}
-__device__ __forceinline__ float across_sum(float x) {
-  auto a = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
-  return __uint_as_float(a[0]) + __uint_as_float(a[1]);
-}
-
-// factor of the logits in powers of two (>= 0: its sign and a factor 0 go to the queries' bits)
-struct Scale2 {
-  float c;
-  uint32_t flip, keep;
-};
-__device__ __forceinline__ Scale2 scale2(float scale) {
-  return {scale == 0.f ? 1.f : fabsf(scale) * LOG2E, scale < 0.f ? 0x80008000u : 0u, scale == 0.f ? 0u : 0xffffffffu};
-}
 
 struct PromptOut {
   void* out;
@@ -395,7 +360,7 @@ __global__ __launch_bounds__(256) void prompt_join_kernel(DevDesc d, PagedArgs a
 }  // namespace
 
 PromptPlan prompt_bf16_plan(const DevDesc& d, long long n_rows, long long cap, const Visible& vis, bool scores) {
-  PromptPlan p;
+  PromptPlan p = {};
   const long long tiles = col_tiles_most(n_rows, d.B, d.G, FP_COLS) * d.Hkv;
   long long keys = cap;
   if (vis.window > 0) {
@@ -412,7 +377,9 @@ PromptPlan prompt_bf16_plan(const DevDesc& d, long long n_rows, long long cap, c
   p.off_lse = 0;
   p.off_o = scores ? whole(heads * sizeof(float)) : 0;
   p.off_ml = p.off_o + (p.splits > 1 ? whole(heads * p.splits * D * sizeof(float)) : 0);
-  p.total = p.off_ml + (p.splits > 1 ? whole(heads * p.splits * 2 * sizeof(float)) : 0);
+  p.off_scores = p.off_ml + (p.splits > 1 ? whole(heads * p.splits * 2 * sizeof(float)) : 0);
+  if (scores) p.scores = prompt_scores_plan(d, n_rows, cap);
+  p.total = p.off_scores + p.scores.bytes;
   return p;
 }
 

@@ -1,0 +1,182 @@
+// The cumulative scores that a prompt's queries leave, bf16: score of token j += sum over the columns that see it of
+// exp(s - lse), lse being the logarithm of the column's final sum, which the attention kernel left.
+//
+// A wave owns 64 tokens and keeps their keys in registers, the B operand of S = Q K^T (columns x keys); a workgroup's four
+// waves walk over tiles of 64 columns, whose queries come through LDS, and every lane sums the weights of its own token: no
+// exchange until the end, and the order of a sum is fixed.  Bound by the vector units: an exponential a (column, token), a
+// multiply-add and a sum.  A token early in a prompt has the most columns: its block goes first, and where the blocks of
+// tokens are few its columns are shared out over several workgroups, whose sums a second kernel adds in order.
+#include "kvr_launch.h"
+#include "kvr_prompt.h"
+
+namespace kvr {
+
+namespace {
+
+constexpr int SC_WAVES = 4, SC_KEYS = 64 * SC_WAVES, SC_COLS = 64;
+constexpr int SC_TILE = SC_COLS * D * 2;
+
+__global__ __launch_bounds__(64 * SC_WAVES, 2) void prompt_scores_bf16_kernel(DevDesc d, PagedArgs a, const float* lse, float* part,
+                                                                              int keys_cap) {
+  __shared__ __align__(1024) unsigned char s_q[2 * SC_TILE];
+  __shared__ __align__(16) float s_lse[2][SC_COLS];
+  const int lane = threadIdx.x & 63, wave = uniform((int)(threadIdx.x >> 6));
+  const int half = lane >> 5, col = lane & 31;
+  const int u = blockIdx.y, b = uniform(u / d.Hkv), hk = u - b * d.Hkv;
+  const int gs = __builtin_ctz(d.G);
+  const RowSpan span = row_span(a.q_start, a.n_rows, b);
+  const int n = clampi(listed(a.n_ctx + b), 0, a.pages.cap);
+  const int first = n - span.n;
+  const int j0 = blockIdx.x * SC_KEYS;
+  if (j0 >= n) return;
+  const int jw = j0 + 64 * wave;                     // this wave's tokens
+  // new tokens of which some may see one of the block's
+  const int t0 = max(j0 - first, 0);
+  int t1 = span.n;
+  if (a.vis.window > 0 && j0 >= a.vis.n_sink) t1 = min(t1, j0 + SC_KEYS - 1 + a.vis.window - first);
+  const int cols = t1 << gs;                         // columns t0 G .. cols - 1
+  const int c0 = t0 << gs;
+  const int tiles = cols > c0 ? (cols - c0 + SC_COLS - 1) / SC_COLS : 0;
+  const int per = uniform((int)((tiles + gridDim.z - 1) / gridDim.z));
+  const int i0 = min((int)blockIdx.z * per, tiles), i1 = min(i0 + per, tiles);
+
+  const Scale2 sc = scale2(d.scale);
+  bf16x8_t k[2][8];
+  bool there[2];
+#pragma unroll
+  for (int kb = 0; kb < 2; ++kb) {
+    const int j = jw + 32 * kb + col;
+    const long long r = page_row(a.pages, d.Hkv, b, hk, min(j, n - 1));
+    there[kb] = j < n && r >= 0;
+    const bf16_t* kp = (const bf16_t*)a.pages.k + max(r, 0ll) * D + 8 * half;
+#pragma unroll
+    for (int s = 0; s < 8; ++s) {
+      u32x4_t x = *reinterpret_cast<const u32x4_t*>(kp + 16 * s);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) x[e] = (x[e] ^ sc.flip) & sc.keep;      // (here the keys', the queries go past the registers)
+      k[kb][s] = __builtin_bit_cast(bf16x8_t, x);
+    }
+  }
+
+  // rows of a tile to LDS: 16 columns of 256 bytes a wave, piece c of row r at c ^ (r mod 16)
+  const uint32_t lds0 = lds_offset(s_q);
+  float lse_next = 0.f;
+  auto fetch = [&](int i, int buf) {
+    const int m0 = c0 + i * SC_COLS;
+#pragma unroll
+    for (int x = 0; x < 4; ++x) {
+      const int r = 16 * wave + 4 * x + (lane >> 4);
+      const int m = min(m0 + r, cols - 1);
+      const size_t at = (size_t)(span.first + (m >> gs)) * d.Hq + hk * d.G + (m & (d.G - 1));
+      to_lds((const unsigned char*)a.q + at * (D * 2) + (((lane & 15) ^ (r & 15)) << 4),
+             uniform((int)(lds0 + buf * SC_TILE + (16 * wave + 4 * x) * 256)));
+    }
+    if (wave == 0) {
+      const int m = min(m0 + lane, cols - 1);
+      const float v = lse[(size_t)(span.first + (m >> gs)) * d.Hq + hk * d.G + (m & (d.G - 1))];
+      lse_next = m0 + lane < cols ? v : __builtin_inff();       // weight 0
+    }
+  };
+
+  float acc[2] = {0.f, 0.f};
+  if (i0 < i1) fetch(i0, 0);
+  for (int i = i0; i < i1; ++i) {
+    const int buf = (i - i0) & 1;
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    if (wave == 0) s_lse[buf][lane] = lse_next;
+    __syncthreads();
+    if (i + 1 < i1) fetch(i + 1, buf ^ 1);
+    const int m0 = c0 + i * SC_COLS;
+    const int lo = first + (m0 >> gs), hi = first + ((min(m0 + SC_COLS, cols) - 1) >> gs);   // positions of the columns
+    if (jw > hi || jw >= n || (a.vis.window > 0 && jw + 63 <= lo - a.vis.window && jw >= a.vis.n_sink)) continue;
+    const bool whole = jw + 63 <= lo && (a.vis.window == 0 || jw > hi - a.vis.window || jw + 63 < a.vis.n_sink);
+    const unsigned char* tq = s_q + buf * SC_TILE;
+#pragma unroll
+    for (int cb = 0; cb < 2; ++cb) {
+      f32x16_t s[2];
+#pragma unroll
+      for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+        for (int x = 0; x < 16; ++x) s[kb][x] = 0.f;
+#pragma unroll
+      for (int c = 0; c < 8; ++c) {
+        const bf16x8_t q = *reinterpret_cast<const bf16x8_t*>(tq + (32 * cb + col) * 256 + (((2 * c + half) ^ (col & 15)) << 4));
+#pragma unroll
+        for (int kb = 0; kb < 2; ++kb) s[kb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(q, k[kb][c], s[kb], 0, 0, 0);
+      }
+#pragma unroll
+      for (int x = 0; x < 16; x += 4) {
+        const float4 l = *reinterpret_cast<const float4*>(&s_lse[buf][32 * cb + 2 * x + 4 * half]);
+        const float le[4] = {l.x, l.y, l.z, l.w};
+        if (whole) {
+#pragma unroll
+          for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) acc[kb] += exp2_(fmaf(s[kb][x + e], sc.c, -le[e]));
+        } else {
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const int m = m0 + 32 * cb + 2 * x + 4 * half + e;
+            const int P = first + (m >> gs);
+#pragma unroll
+            for (int kb = 0; kb < 2; ++kb) {
+              const float p = exp2_(fmaf(s[kb][x + e], sc.c, -le[e]));
+              acc[kb] += sees(a.vis, P, jw + 32 * kb + col) ? p : 0.f;
+            }
+          }
+        }
+      }
+    }
+  }
+#pragma unroll
+  for (int kb = 0; kb < 2; ++kb) {
+    const float sum = across_sum(acc[kb]);
+    const int j = jw + 32 * kb + col;
+    if (half == 0 && j < keys_cap) {
+      if (part) part[((size_t)blockIdx.z * gridDim.y + u) * keys_cap + j] = there[kb] ? sum : 0.f;
+      else if (there[kb] && sum != 0.f) a.scores[(size_t)u * a.n_cap + j] += sum;
+    }
+  }
+}
+
+// adds the workgroups' sums of a token, in order
+__global__ __launch_bounds__(256) void scores_add_kernel(DevDesc d, PagedArgs a, const float* part, int keys_cap, int splits) {
+  const int u = blockIdx.y, j = blockIdx.x * 256 + threadIdx.x;
+  const int n = clampi(listed(a.n_ctx + u / d.Hkv), 0, a.pages.cap);
+  if (j >= n || j >= keys_cap) return;
+  float sum = 0.f;
+  for (int s = 0; s < splits; ++s) sum += part[((size_t)s * gridDim.y + u) * keys_cap + j];
+  if (sum != 0.f) a.scores[(size_t)u * a.n_cap + j] += sum;
+}
+
+int scores_keys(long long cap, long long n_cap) { return (int)(cap < n_cap ? cap : n_cap); }
+
+}  // namespace
+
+// n_cap is not known where the workspace is asked for: room for all tokens
+ScoresPlan prompt_scores_plan(const DevDesc& d, long long n_rows, long long cap) {
+  ScoresPlan p;
+  const long long units = (long long)d.B * d.Hkv;
+  const long long blocks = units * ((cap + SC_KEYS - 1) / SC_KEYS);
+  // 1024 pieces of work, two for each workgroup that the chip holds, of eight tiles of columns at least
+  long long s = blocks < 1024 ? (1024 + blocks - 1) / blocks : 1;
+  const long long most = (n_rows * d.G + 8 * SC_COLS - 1) / (8 * SC_COLS);
+  s = s < most ? s : most;
+  p.splits = (int)(s < 1 ? 1 : s > 64 ? 64 : s);
+  p.bytes = p.splits > 1 ? (size_t)p.splits * units * cap * sizeof(float) : 0;
+  return p;
+}
+
+hipError_t launch_prompt_scores_bf16(const DevDesc& d, const PagedArgs& a, const ScoresPlan& p, const float* lse, float* part,
+                                     hipStream_t st) {
+  const int keys = scores_keys(a.pages.cap, a.n_cap);
+  const unsigned units = d.B * d.Hkv;
+  hipLaunchKernelGGL(prompt_scores_bf16_kernel, dim3((keys + SC_KEYS - 1) / SC_KEYS, units, p.splits), dim3(64 * SC_WAVES), 0, st, d,
+                     a, lse, p.splits > 1 ? part : nullptr, keys);
+  const hipError_t e = hipGetLastError();
+  if (e != hipSuccess || p.splits == 1) return e;
+  hipLaunchKernelGGL(scores_add_kernel, dim3((keys + 255) / 256, units), dim3(256), 0, st, d, a, part, keys, p.splits);
+  return hipGetLastError();
+}
+
+}  // namespace kvr

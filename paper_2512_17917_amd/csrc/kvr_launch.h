@@ -256,9 +256,17 @@ struct PagedArgs {
 };
 // bf16 kernel of a prompt's attention: into how many parts a tile's tokens are split, and its workspace (first the columns'
 // maximum plus logarithm of the sum, in powers of two, where scores want them)
+struct ScoresPlan {
+  int splits;                       // workgroups that share the columns of a block of tokens
+  size_t bytes;                     // of their sums
+};
+ScoresPlan prompt_scores_plan(const DevDesc& d, long long n_rows, long long cap);
+hipError_t launch_prompt_scores_bf16(const DevDesc& d, const PagedArgs& a, const ScoresPlan& p, const float* lse, float* part,
+                                     hipStream_t st);
 struct PromptPlan {
   int splits;
-  size_t off_lse, off_o, off_ml, total;
+  ScoresPlan scores;
+  size_t off_lse, off_o, off_ml, off_scores, total;
 };
 PromptPlan prompt_bf16_plan(const DevDesc& d, long long n_rows, long long cap, const Visible& vis, bool scores);
 hipError_t launch_prompt_bf16(const DevDesc& d, const PagedArgs& a, const PromptPlan& p, hipStream_t st);

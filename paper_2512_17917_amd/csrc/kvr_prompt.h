@@ -1,0 +1,44 @@
+// What the two bf16 kernels of a prompt's attention share.
+#pragma once
+#include "kvr_dev.h"
+
+namespace kvr {
+
+typedef __bf16 bf16x8_t __attribute__((ext_vector_type(8)));
+typedef __bf16 bf16x2_t __attribute__((ext_vector_type(2)));
+typedef float f32x16_t __attribute__((ext_vector_type(16)));
+typedef float f32x2_t __attribute__((ext_vector_type(2)));
+typedef short s16x4_t __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x4_t __attribute__((ext_vector_type(4)));
+
+constexpr float LOG2E = 1.4426950408889634f;
+
+// 16 bytes a lane from memory to LDS, lane l's to `lds` + 16 l (a wave's number).  The compiler has a builtin for it but waits
+// for all such loads before the next read of LDS, which would be every tile's; here the kernel waits where it must.
+__device__ __forceinline__ void to_lds(const unsigned char* from, uint32_t lds) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(lds), "v"(from) : "m0", "memory");
+}
+__device__ __forceinline__ uint32_t lds_offset(const void* p) {
+  return (uint32_t)(uintptr_t)(const __attribute__((address_space(3))) void*)p;
+}
+
+__device__ __forceinline__ float exp2_(float x) { return __builtin_amdgcn_exp2f(x); }
+__device__ __forceinline__ float across_max(float x) {
+  auto a = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return fmaxf(__uint_as_float(a[0]), __uint_as_float(a[1]));
+}
+__device__ __forceinline__ float across_sum(float x) {
+  auto a = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return __uint_as_float(a[0]) + __uint_as_float(a[1]);
+}
+
+// factor of the logits in powers of two (>= 0: its sign and a factor 0 go to the queries' bits)
+struct Scale2 {
+  float c;
+  uint32_t flip, keep;
+};
+__device__ __forceinline__ Scale2 scale2(float scale) {
+  return {scale == 0.f ? 1.f : fabsf(scale) * LOG2E, scale < 0.f ? 0x80008000u : 0u, scale == 0.f ? 0u : 0xffffffffu};
+}
+
+}  // namespace kvr
