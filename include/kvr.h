@@ -535,6 +535,8 @@ int32_t kvr_attend_prompt(const kvr_desc* desc, const void* q, int32_t n_rows, c
 /*
  * The same for one new token per sequence (row b is sequence b's), by kernels made for it: the
  * cache is shared out by tokens over the whole chip, whatever the sequences' lengths.
+ * KVR_ERR_UNSUPPORTED where B * Hkv times the tokens that a sequence can hold (with a window: can
+ * show) passes 2^37.
  *   q, out     dev [B, Hq, D] storage type
  *   the others as for kvr_attend_prompt
  */

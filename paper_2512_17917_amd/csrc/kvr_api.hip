@@ -583,6 +583,7 @@ int32_t kvr_attend_paged_workspace_size(const kvr_desc* desc, const kvr_pages* p
   if (rc == KVR_OK) rc = check_visible(window, n_sink, vis);
   if (rc != KVR_OK) return rc;
   if (bytes == nullptr) return KVR_ERR_INVALID_ARG;
+  if (!kvr::attend_paged_fits(d, p.cap, vis)) return KVR_ERR_UNSUPPORTED;
   *bytes = kvr::attend_paged_ws(d, desc->dtype, p.cap, vis, scores != 0);
   return KVR_OK;
 }
@@ -597,6 +598,7 @@ int32_t kvr_attend_paged(const kvr_desc* desc, const void* q, const int32_t* n_c
   if (rc == KVR_OK) rc = check_visible(window, n_sink, a.vis);
   if (rc == KVR_OK) rc = check_attend(desc, q, n_ctx, pages, out, scores, n_cap, a);
   if (rc != KVR_OK) return rc;
+  if (!kvr::attend_paged_fits(d, a.pages.cap, a.vis)) return KVR_ERR_UNSUPPORTED;
   rc = check_ws(ws, ws_bytes, kvr::attend_paged_ws(d, desc->dtype, a.pages.cap, a.vis, scores != nullptr));
   if (rc != KVR_OK) return rc;
   a.n_rows = d.B;

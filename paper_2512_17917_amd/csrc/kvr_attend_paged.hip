@@ -38,7 +38,8 @@ struct PagedPlan {
   int wgs;                          // workgroups of the first kernel
   long long tiles;                  // tiles a unit can have
   bool join;
-  size_t off_o, off_ml, off_log, total;
+  bool fits;                        // the row of chunks in 31 bits
+  size_t off_o, off_ml, off_span, off_log, total;
 };
 
 PagedPlan paged_plan(const DevDesc& d, int dtype, long long cap, const Visible& vis, bool scores) {
@@ -49,8 +50,8 @@ PagedPlan paged_plan(const DevDesc& d, int dtype, long long cap, const Visible& 
     const long long some = ((long long)vis.window + 15) / 16 + 1 + ((long long)vis.n_sink + 15) / 16;
     p.tiles = some < all ? some : all;
   }
-  const long long units = (long long)d.B * d.Hkv;
-  const long long chunks = units * ((p.tiles + 3) / 4);
+  const long long units = (long long)d.B * d.Hkv, chunks = units * ((p.tiles + 3) / 4);
+  p.fits = chunks < 0x7fffffffll;
   const int fill = 256 * paged_per_cu(dtype == KVR_F32 ? 4 : 2, d.G);
   p.wgs = (int)(chunks < fill ? chunks : fill);
   p.join = scores || p.tiles > 4;
@@ -58,7 +59,8 @@ PagedPlan paged_plan(const DevDesc& d, int dtype, long long cap, const Visible& 
   auto whole = [](size_t x) { return (x + 255) & ~(size_t)255; };
   p.off_o = 0;
   p.off_ml = p.join ? whole(slots * d.G * D * sizeof(float)) : 0;
-  p.off_log = p.off_ml + (p.join ? whole(slots * d.G * 2 * sizeof(float)) : 0);
+  p.off_span = p.off_ml + (p.join ? whole(slots * d.G * 2 * sizeof(float)) : 0);
+  p.off_log = p.off_span + (p.join ? whole((size_t)units * 2 * sizeof(int)) : 0);
   p.total = p.off_log + (scores ? whole((size_t)units * p.tiles * 16 * d.G * sizeof(float)) : 0);
   return p;
 }
@@ -107,44 +109,45 @@ __device__ __forceinline__ int seq_chunks(const PagedArgs& a, int b) {
   int n;
   return (unit_tiles(a, b, n).n + 3) >> 2;
 }
-__device__ __forceinline__ long long wave_sum(long long x) {
-#pragma unroll
-  for (int k = 1; k < 64; k <<= 1) x += __shfl_xor(x, k);
-  return x;
-}
-// chunks of all sequences before `upto`, times 1 head
-__device__ __forceinline__ long long chunks_before(const PagedArgs& a, int upto) {
+// (the host has made sure that all chunks there can be fit 31 bits)
+__device__ __forceinline__ int all_chunks(const PagedArgs& a, int B, int heads) {
   const int lane = threadIdx.x & 63;
-  long long sum = 0;
-  for (int b0 = 0; b0 < upto; b0 += 64) sum += b0 + lane < upto ? seq_chunks(a, b0 + lane) : 0;
-  return uniform(wave_sum(sum));
+  int sum = 0;
+  for (int b0 = 0; b0 < B; b0 += 64) sum += b0 + lane < B ? seq_chunks(a, b0 + lane) : 0;
+#pragma unroll
+  for (int k = 1; k < 64; k <<= 1) sum += __shfl_xor(sum, k);
+  return uniform(sum) * heads;
 }
-// chunks a workgroup takes
-__device__ __forceinline__ long long piece(long long total, int wgs) { return (total + wgs - 1) / wgs; }
 
 struct Where {
   int b, h, chunk;
 };
-// place of chunk `at` of the row (at < total)
-__device__ __forceinline__ Where find_chunk(const PagedArgs& a, int B, int heads, long long at) {
+// place of chunk `at` of the row (at < all)
+__device__ __forceinline__ Where find_chunk(const PagedArgs& a, int B, int heads, int at) {
+  if (B == 1) {
+    const int n = seq_chunks(a, 0);
+    const int h = uniform(at / n);
+    return {0, h, at - h * n};
+  }
   const int lane = threadIdx.x & 63;
-  long long base = 0;
+  int base = 0;
   for (int b0 = 0; b0 < B; b0 += 64) {
     const int mine = b0 + lane < B ? seq_chunks(a, b0 + lane) : 0;
-    long long upto = mine;
+    int upto = mine;
 #pragma unroll
     for (int k = 1; k < 64; k <<= 1) {
-      const long long x = __shfl_up(upto, k);
+      const int x = __shfl_up(upto, k);
       upto += lane >= k ? x : 0;
     }
     const unsigned long long past = __ballot(at < (base + upto) * heads);
     if (past != 0) {
       const int l = __ffsll(past) - 1;
-      const int n = __shfl(mine, l);
-      const long long off = at - (base + __shfl(upto, l) - n) * heads;
-      return {uniform(b0 + l), uniform((int)(off / n)), uniform((int)(off % n))};
+      const int n = uniform(__shfl(mine, l));
+      const int off = at - uniform((base + __shfl(upto, l) - n) * heads);
+      const int h = uniform(off / n);
+      return {b0 + l, h, off - h * n};
     }
-    base += __shfl(upto, 63);
+    base += uniform(__shfl(upto, 63));
   }
   return {B, 0, 0};
 }
@@ -234,7 +237,7 @@ __device__ __forceinline__ f32x4_t tile_logits(const u32x4_t (&k)[Tile<T>::N], c
 }
 
 template <typename T, int G, bool ONE>
-__global__ __launch_bounds__(64 * PG_WAVES, paged_per_cu(sizeof(T), G)) void paged_kernel(DevDesc d, PagedArgs a, float* part_o, float* part_ml, float* logits,
+__global__ __launch_bounds__(64 * PG_WAVES, paged_per_cu(sizeof(T), G)) void paged_kernel(DevDesc d, PagedArgs a, float* part_o, float* part_ml, int* span, float* logits,
                                                               long long most_tiles) {
   __shared__ __align__(16) float s_o[PG_WAVES][G][D];
   __shared__ float s_m[PG_WAVES][G], s_l[PG_WAVES][G];
@@ -251,18 +254,18 @@ __global__ __launch_bounds__(64 * PG_WAVES, paged_per_cu(sizeof(T), G)) void pag
     if (listed(a.n_ctx + b) <= 0)
       for (int i = threadIdx.x; i < d.Hq * D; i += 64 * PG_WAVES) Store<T>::store1((T*)a.out + (size_t)b * d.Hq * D + i, 0.f);
 
-  const long long total = chunks_before(a, d.B) * d.Hkv;
-  const long long per = piece(total, gridDim.x);
-  long long at = (long long)w * per;
-  const long long end = at + per < total ? at + per : total;
-  if (at >= end) return;
+  const int total = all_chunks(a, d.B, d.Hkv);
+  const int per = uniform((int)(((unsigned)total + gridDim.x - 1) / gridDim.x));
+  if ((long long)w * per >= total) return;
+  int at = w * per;
+  const int end = total - at < per ? total : at + per;
   Where p = find_chunk(a, d.B, d.Hkv, at);
   while (at < end) {
     const int b = uniform(p.b), h = uniform(p.h), c0 = uniform(p.chunk);
     int n;
     const TileRange tr = unit_tiles(a, b, n);
     const int chunks = (tr.n + 3) >> 2;
-    const int len = (int)(end - at < chunks - c0 ? end - at : chunks - c0);
+    const int len = min(end - at, chunks - c0);
     const int u = b * d.Hkv + h;
     const int t_end = min(4 * (c0 + len), tr.n);
     const int P = n - 1;
@@ -393,6 +396,10 @@ __global__ __launch_bounds__(64 * PG_WAVES, paged_per_cu(sizeof(T), G)) void pag
     __syncthreads();
     const bool all = len == chunks;             // the whole unit: no other workgroup has a part of it
     const size_t slot = (size_t)w + u;
+    if (span && threadIdx.x == 0) {             // which workgroups have parts of the unit
+      if (c0 == 0) span[2 * u] = w;
+      if (c0 + len == chunks) span[2 * u + 1] = w;
+    }
     for (int i = threadIdx.x; i < G * D; i += 64 * PG_WAVES) {
       const int g = i / D, c = i % D;
       float m = s_m[0][g];
@@ -427,102 +434,115 @@ __global__ __launch_bounds__(64 * PG_WAVES, paged_per_cu(sizeof(T), G)) void pag
 // tokens each).
 template <typename T, int G>
 __global__ __launch_bounds__(256) void paged_join_kernel(DevDesc d, PagedArgs a, const float* part_o, const float* part_ml,
-                                                         const float* logits, long long most_tiles, int wgs) {
+                                                         const int* span, const float* logits, long long most_tiles) {
   __shared__ float s_m[4][G], s_l[4][G], s_sum[D];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int u = blockIdx.y, b = u / d.Hkv, h = u % d.Hkv;
+  const int lane = threadIdx.x & 63, wave = uniform((int)(threadIdx.x >> 6));
+  const int u = blockIdx.y, b = uniform(u / d.Hkv), h = u - b * d.Hkv;
   const float NEG_INF = -__builtin_inff();
   int n;
   const TileRange tr = unit_tiles(a, b, n);
   if (tr.n == 0) return;
   const int slice = (int)blockIdx.x - G;
   if (slice >= 0 && slice * PG_SLICE >= tr.n * 16) return;
-  const int chunks = (tr.n + 3) >> 2;
-  const long long before = chunks_before(a, b);
-  long long total = before;
-  {
-    long long rest = 0;
-    for (int b0 = b; b0 < d.B; b0 += 64) rest += b0 + lane < d.B ? seq_chunks(a, b0 + lane) : 0;
-    total += wave_sum(rest);
-  }
-  const long long per = piece(total * d.Hkv, wgs);
-  const long long s0 = before * d.Hkv + (long long)h * chunks;
-  const int w0 = (int)(s0 / per), w1 = (int)((s0 + chunks - 1) / per);
-  const int parts = w1 - w0 + 1;
+  const int w0 = listed(span + 2 * u), parts = listed(span + 2 * u + 1) - w0 + 1;
   if (slice < 0 && parts == 1) return;
   const size_t slot0 = (size_t)w0 + u;
 
-  // maximum and sum over the pieces
-  float m[G], l[G];
-#pragma unroll
-  for (int g = 0; g < G; ++g) {
-    m[g] = NEG_INF;
-    l[g] = 0.f;
-  }
-  for (int i = threadIdx.x; i < parts; i += 256) {
-#pragma unroll
-    for (int g = 0; g < G; ++g) {
-      const float pm = part_ml[((slot0 + i) * G + g) * 2], pl = part_ml[((slot0 + i) * G + g) * 2 + 1];
-      const float mn = fmaxf(m[g], pm);
-      l[g] = (m[g] == NEG_INF ? 0.f : l[g] * exp2_(m[g] - mn)) + (pm == NEG_INF ? 0.f : pl * exp2_(pm - mn));
-      m[g] = mn;
-    }
-  }
-#pragma unroll
-  for (int g = 0; g < G; ++g) {
-#pragma unroll
-    for (int k = 1; k < 64; k <<= 1) {
-      const float om = __shfl_xor(m[g], k), ol = __shfl_xor(l[g], k);
-      const float mn = fmaxf(m[g], om);
-      l[g] = (m[g] == NEG_INF ? 0.f : l[g] * exp2_(m[g] - mn)) + (om == NEG_INF ? 0.f : ol * exp2_(om - mn));
-      m[g] = mn;
-    }
-    if (lane == 0) {
-      s_m[wave][g] = m[g];
-      s_l[wave][g] = l[g];
-    }
-  }
-  __syncthreads();
-#pragma unroll
-  for (int g = 0; g < G; ++g) {
-    m[g] = fmaxf(fmaxf(s_m[0][g], s_m[1][g]), fmaxf(s_m[2][g], s_m[3][g]));
-    l[g] = 0.f;
-#pragma unroll
-    for (int x = 0; x < 4; ++x) l[g] += s_m[x][g] == NEG_INF ? 0.f : s_l[x][g] * exp2_(s_m[x][g] - m[g]);
-  }
   if (slice < 0) {
-    const int g = blockIdx.x, c = threadIdx.x & (D - 1), half = threadIdx.x / D;
-    float mg = m[0], lg = l[0];
+    // the two halves of the workgroup take every other part; 16 of a half's at a time are on their way
+    const int g = blockIdx.x, c = threadIdx.x & (D - 1), odd = threadIdx.x / D;
+    float m = NEG_INF, l = 0.f, o = 0.f;
+    for (int i0 = odd; i0 < parts; i0 += 32) {
+      float pm[16], pl[16], po[16];
 #pragma unroll
-    for (int x = 1; x < G; ++x) {
-      mg = x == g ? m[x] : mg;
-      lg = x == g ? l[x] : lg;
+      for (int x = 0; x < 16; ++x) {
+        const int i = min(i0 + 2 * x, parts - 1);
+        const float2 ml = *reinterpret_cast<const float2*>(part_ml + ((slot0 + i) * G + g) * 2);
+        pm[x] = i0 + 2 * x < parts ? ml.x : NEG_INF;
+        pl[x] = ml.y;
+        po[x] = part_o[((slot0 + i) * G + g) * D + c];
+      }
+      float mn = m;
+#pragma unroll
+      for (int x = 0; x < 16; ++x) mn = fmaxf(mn, pm[x]);
+      if (mn == NEG_INF) continue;
+      const float f = exp2_(m - mn);            // (2^-inf: 0)
+      l *= f;
+      o *= f;
+      m = mn;
+#pragma unroll
+      for (int x = 0; x < 16; ++x) {
+        const float e = exp2_(pm[x] - m);
+        l = fmaf(e, pm[x] == NEG_INF ? 0.f : pl[x], l);
+        o = fmaf(e, pm[x] == NEG_INF ? 0.f : po[x], o);
+      }
     }
-    float o = 0.f;
-#pragma unroll 4
-    for (int i = half; i < parts; i += 2) {
-      const float pm = part_ml[((slot0 + i) * G + g) * 2];
-      o = fmaf(pm == NEG_INF ? 0.f : exp2_(pm - mg), part_o[(slot0 + i) * G * D + g * D + c], o);
+    float* s_ml = &s_m[0][0];                   // [2]
+    if (odd == 1) {
+      s_sum[c] = o;
+      if (c == 0) {
+        s_ml[0] = m;
+        s_l[0][0] = l;
+      }
     }
-    if (half == 1) s_sum[c] = o;
     __syncthreads();
-    if (half == 0)
-      Store<T>::store1((T*)a.out + ((size_t)b * d.Hq + h * G + g) * D + c, mg == NEG_INF ? 0.f : (o + s_sum[c]) / lg);
+    if (odd == 0) {
+      const float m1 = s_ml[0], mn = fmaxf(m, m1);
+      const float f0 = m == NEG_INF ? 0.f : exp2_(m - mn), f1 = m1 == NEG_INF ? 0.f : exp2_(m1 - mn);
+      const float r = (f0 * o + f1 * s_sum[c]) / (f0 * l + f1 * s_l[0][0]);
+      Store<T>::store1((T*)a.out + ((size_t)b * d.Hq + h * G + g) * D + c, mn == NEG_INF ? 0.f : r);
+    }
     return;
   }
+  // a lane has parts of one head: maximum and sum over its own, then over the lanes of that head, then over the waves
+  float m = NEG_INF, l = 0.f;
+  for (int i = threadIdx.x / G; i < parts; i += 256 / G) {
+    const float2 ml = *reinterpret_cast<const float2*>(part_ml + ((slot0 + i) * G + threadIdx.x % G) * 2);
+    const float mn = fmaxf(m, ml.x);
+    l = (m == NEG_INF ? 0.f : l * exp2_(m - mn)) + (ml.x == NEG_INF ? 0.f : ml.y * exp2_(ml.x - mn));
+    m = mn;
+  }
+#pragma unroll
+  for (int k = G; k < 64; k <<= 1) {
+    const float om = __shfl_xor(m, k), ol = __shfl_xor(l, k);
+    const float mn = fmaxf(m, om);
+    l = (m == NEG_INF ? 0.f : l * exp2_(m - mn)) + (om == NEG_INF ? 0.f : ol * exp2_(om - mn));
+    m = mn;
+  }
+  if (lane < G) {
+    s_m[wave][lane] = m;
+    s_l[wave][lane] = l;
+  }
+  __syncthreads();
   float lse[G];
 #pragma unroll
-  for (int g = 0; g < G; ++g) lse[g] = m[g] == NEG_INF ? __builtin_inff() : m[g] + __builtin_amdgcn_logf(l[g]);
-  for (int i = threadIdx.x; i < PG_SLICE; i += 256) {
-    const int e = slice * PG_SLICE + i;
-    if (e >= tr.n * 16) break;
-    const int j = tile_token<16>(tr, e >> 4) + (e & 15);
-    if (j >= n || j >= a.n_cap) continue;
-    const float* lp = logits + ((size_t)u * most_tiles * 16 + e) * G;
+  for (int g = 0; g < G; ++g) {
+    const float mg = fmaxf(fmaxf(s_m[0][g], s_m[1][g]), fmaxf(s_m[2][g], s_m[3][g]));
+    float lg = 0.f;
+#pragma unroll
+    for (int x = 0; x < 4; ++x) lg += s_m[x][g] == NEG_INF ? 0.f : s_l[x][g] * exp2_(s_m[x][g] - mg);
+    lse[g] = mg == NEG_INF ? __builtin_inff() : mg + __builtin_amdgcn_logf(lg);
+  }
+  // four tokens a thread, all their numbers asked for at once
+  float lo[PG_SLICE / 256][G], old[PG_SLICE / 256];
+  int at[PG_SLICE / 256];
+#pragma unroll
+  for (int i = 0; i < PG_SLICE / 256; ++i) {
+    const int e = slice * PG_SLICE + i * 256 + threadIdx.x;
+    const bool in = e < tr.n * 16;
+    const int j = in ? tile_token<16>(tr, e >> 4) + (e & 15) : n;
+    at[i] = in && j < n && j < a.n_cap ? j : -1;
+    const float* lp = logits + ((size_t)u * most_tiles * 16 + (in ? e : 0)) * G;
+#pragma unroll
+    for (int g = 0; g < G; ++g) lo[i][g] = lp[g];
+    old[i] = a.scores[(size_t)u * a.n_cap + max(at[i], 0)];
+  }
+#pragma unroll
+  for (int i = 0; i < PG_SLICE / 256; ++i) {
     float sum = 0.f;
 #pragma unroll
-    for (int g = 0; g < G; ++g) sum += exp2_(lp[g] - lse[g]);
-    if (sum != 0.f) a.scores[(size_t)u * a.n_cap + j] += sum;
+    for (int g = 0; g < G; ++g) sum += exp2_(lo[i][g] - lse[g]);
+    if (at[i] >= 0 && sum != 0.f) a.scores[(size_t)u * a.n_cap + at[i]] = old[i] + sum;
   }
 }
 
@@ -532,17 +552,18 @@ hipError_t launch(const DevDesc& d, const PagedArgs& a, hipStream_t st) {
   char* base = (char*)a.ws;
   float* part_o = p.join ? (float*)(base + p.off_o) : nullptr;
   float* part_ml = p.join ? (float*)(base + p.off_ml) : nullptr;
+  int* span = p.join ? (int*)(base + p.off_span) : nullptr;
   float* logits = a.scores ? (float*)(base + p.off_log) : nullptr;
   const bool one = a.pages.table == nullptr || a.pages.page_size % 16 == 0;
   if (one)
-    hipLaunchKernelGGL((paged_kernel<T, G, true>), dim3(p.wgs), dim3(64 * PG_WAVES), 0, st, d, a, part_o, part_ml, logits, p.tiles);
+    hipLaunchKernelGGL((paged_kernel<T, G, true>), dim3(p.wgs), dim3(64 * PG_WAVES), 0, st, d, a, part_o, part_ml, span, logits, p.tiles);
   else
-    hipLaunchKernelGGL((paged_kernel<T, G, false>), dim3(p.wgs), dim3(64 * PG_WAVES), 0, st, d, a, part_o, part_ml, logits, p.tiles);
+    hipLaunchKernelGGL((paged_kernel<T, G, false>), dim3(p.wgs), dim3(64 * PG_WAVES), 0, st, d, a, part_o, part_ml, span, logits, p.tiles);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess || !p.join) return e;
   const unsigned slices = a.scores ? (unsigned)((p.tiles * 16 + PG_SLICE - 1) / PG_SLICE) : 0;
-  hipLaunchKernelGGL((paged_join_kernel<T, G>), dim3(G + slices, d.B * d.Hkv), dim3(256), 0, st, d, a, part_o, part_ml, logits,
-                     p.tiles, p.wgs);
+  hipLaunchKernelGGL((paged_join_kernel<T, G>), dim3(G + slices, d.B * d.Hkv), dim3(256), 0, st, d, a, part_o, part_ml, span, logits,
+                     p.tiles);
   return hipGetLastError();
 }
 
@@ -558,6 +579,7 @@ hipError_t launch_group(const DevDesc& d, const PagedArgs& a, hipStream_t st) {
 
 }  // namespace
 
+bool attend_paged_fits(const DevDesc& d, long long cap, const Visible& vis) { return paged_plan(d, KVR_BF16, cap, vis, false).fits; }
 size_t attend_paged_ws(const DevDesc& d, int dtype, long long cap, const Visible& vis, bool scores) {
   return paged_plan(d, dtype, cap, vis, scores).total;
 }

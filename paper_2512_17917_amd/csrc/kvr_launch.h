@@ -272,6 +272,7 @@ PromptPlan prompt_bf16_plan(const DevDesc& d, long long n_rows, long long cap, c
 hipError_t launch_prompt_bf16(const DevDesc& d, const PagedArgs& a, const PromptPlan& p, hipStream_t st);
 size_t attend_prompt_ws(const DevDesc& d, int dtype, long long n_rows, long long cap, const Visible& vis, bool scores);
 hipError_t launch_attend_prompt(const DevDesc& d, int dtype, const PagedArgs& a, hipStream_t st);
+bool attend_paged_fits(const DevDesc& d, long long cap, const Visible& vis);
 size_t attend_paged_ws(const DevDesc& d, int dtype, long long cap, const Visible& vis, bool scores);
 hipError_t launch_attend_paged(const DevDesc& d, int dtype, const PagedArgs& a, hipStream_t st);
 

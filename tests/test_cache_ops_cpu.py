@@ -131,6 +131,17 @@ def test_workspace_sizes():
     assert L.kvr_attend_prompt_workspace_size(C.byref(d), -1, C.byref(p), 0, 0, 0, C.byref(n)) == E
 
 
+def test_more_tokens_than_the_chunks_numbers_hold_are_refused():
+    """2^37 tokens of cache (a table that names the same pages again and again)."""
+    d = kvr.make_desc(4096, 8, 8, 1, 1, kvr.KVR_BF16)
+    big, less = _pages(page_size=1024, table_cap=4096), _pages(page_size=1024, table_cap=4095)
+    n = C.c_size_t(0)
+    for p, want in ((big, U), (less, OK)):
+        assert kvr.lib().kvr_attend_paged_workspace_size(C.byref(d), C.byref(p), 0, 0, 0, C.byref(n)) == want
+    assert _paged(desc=d, over=big, n_cap=64) == U and _paged(desc=d, over=less) == W
+    assert _paged(desc=d, over=big, window=5000) == W
+
+
 def test_binding_refuses_what_does_not_fit():
     import torch
     d = _desc()
