@@ -18,6 +18,8 @@
 //
 // In tiles that some column does not see whole, rows that nobody sees are cleared in LDS and values that are not finite are
 // taken out (0 x inf would reach every column); what they are to the columns that see them is added apart.
+#include <type_traits>
+
 #include "kvr_launch.h"
 #include "kvr_prompt.h"
 
@@ -27,8 +29,8 @@ namespace {
 
 constexpr int FP_WAVES = 8, FP_COLS = 32 * FP_WAVES, FP_KEYS = 64;
 constexpr int FP_TILE = FP_KEYS * D * 2;                       // bytes of a tile of keys or values
-constexpr int FP_P = FP_KEYS * 32 * 4;                         // a wave's weights, for values that are not finite
-constexpr int FP_LDS = 4 * FP_TILE + FP_WAVES * FP_P + 64;
+constexpr int FP_BUFS = 4;
+constexpr int FP_LDS = 2 * FP_BUFS * FP_TILE + 2 * FP_BUFS * FP_WAVES;
 constexpr float KEEP_MAX = 8.f;
 
 struct PromptOut {
@@ -38,14 +40,18 @@ struct PromptOut {
   float* part_ml;
 };
 
-template <bool ONE, bool SPLIT>
+// Where the rows of a tile lie: in one page (dense caches, pages of whole tiles), the eight that a wave fetches in one page, or
+// anywhere.
+enum { IN_ONE_PAGE, EIGHT_A_PAGE, ANYWHERE };
+
+template <int ROWS, bool SPLIT>
 __global__ __launch_bounds__(64 * FP_WAVES, 2) void prompt_bf16_kernel(DevDesc d, PagedArgs a, PromptOut po) {
   extern __shared__ __align__(1024) unsigned char s_mem[];
-  unsigned char* s_k = s_mem;                                   // [2][64][256]
-  unsigned char* s_v = s_mem + 2 * FP_TILE;                     // [2][64][256]
-  float* s_p = (float*)(s_mem + 4 * FP_TILE);                   // [8][64][32]
-  unsigned char* s_there = s_mem + 4 * FP_TILE + FP_WAVES * FP_P;    // [2][8]: rows that lie on a page, a byte per wave
-  unsigned char* s_odd = s_there + 16;                          // [2][8]: rows with a value that is not finite
+  unsigned char* s_k = s_mem;                                   // [4][64][256]
+  unsigned char* s_v = s_k + FP_BUFS * FP_TILE;                 // [4][64][256]
+  unsigned char* s_there = s_v + FP_BUFS * FP_TILE;             // [4][8]: rows that lie on a page, a byte per wave
+  unsigned char* s_odd = s_there + FP_BUFS * FP_WAVES;          // [4][8]: rows with a value that is not finite
+  constexpr bool ONE = ROWS == IN_ONE_PAGE;
   const int lane = threadIdx.x & 63, wave = uniform((int)(threadIdx.x >> 6));
   const int half = lane >> 5, col = lane & 31;
   const float NEG_INF = -__builtin_inff();
@@ -87,45 +93,87 @@ __global__ __launch_bounds__(64 * FP_WAVES, 2) void prompt_bf16_kernel(DevDesc d
     q[s] = __builtin_bit_cast(bf16x8_t, x);
   }
 
+  // Tiles that every column of the workgroup sees whole stand side by side, from `in0` to `in1`.  They are worked on first, as
+  // steps 0 .. n_in-1; the others, at the edges of what is seen, are the steps after.  (If a page of theirs is not there, all
+  // are taken as edges.)
+  int in0 = max(i0, tr.ahead);
+  while (a.vis.window > 0 && in0 < i1 && tile_token<FP_KEYS>(tr, in0) <= hi - a.vis.window) ++in0;
+  int in1 = min(i1, tr.ahead + (lo + 1 - tr.start) / FP_KEYS);
+  in1 = max(in0, in1);
+  if (a.pages.table != nullptr && in0 < in1) {
+    const int p0 = page_index(a.pages, tile_token<FP_KEYS>(tr, in0)), p1 = page_index(a.pages, tile_token<FP_KEYS>(tr, in1 - 1) + FP_KEYS - 1);
+    bool lost = false;
+    for (int i = p0 + lane; i <= p1; i += 64)
+      lost = lost || (uint32_t)a.pages.table[(size_t)b * a.pages.table_cap + i] >= (uint32_t)a.pages.n_pages;
+    if (__any(lost)) in1 = in0;
+  }
+  const int n_in = in1 - in0, n_all = i1 - i0;
+  auto token_of = [&](int step) {               // first token of a step's tile
+    const int i = step < n_in ? in0 + step : step - n_in < in0 - i0 ? i0 + (step - n_in) : i0 + step;
+    return tile_token<FP_KEYS>(tr, i);
+  };
+
   // this wave's rows of a tile: 8 wave .. +7, lane l the pieces l mod 16 of row l div 16 (+ 4)
   const int piece = lane & 15;
   const uint32_t lds0 = lds_offset(s_mem);
-  int row[2], entry[2];
-  bool dead[2] = {false, false};
-  auto ask = [&](int i) {                       // the table's entries of tile i
-    const int j0 = tile_token<FP_KEYS>(tr, i);
+  int entry[2] = {0, 0};                        // the table's, of the tile that is fetched next
+  auto ask = [&](int step) {
+    const int j0 = token_of(step);
     if constexpr (ONE) entry[0] = page_entry(a.pages, b, j0);
+    else if constexpr (ROWS == EIGHT_A_PAGE) entry[0] = page_entry(a.pages, b, min(j0 + 8 * wave, (n - 1) & ~7));
     else
 #pragma unroll
       for (int x = 0; x < 2; ++x) entry[x] = page_entry(a.pages, b, min(j0 + 8 * wave + 4 * x + (lane >> 4), n - 1));
   };
-  auto fetch = [&](int i, int buf) {
-    const int j0 = tile_token<FP_KEYS>(tr, i);
-    if constexpr (ONE) {
-      const int r = (int)entry_row(a.pages, d.Hkv, entry[0], hk, j0);
-      row[0] = max(r, 0);
+  // Starts a step's tile on its way to LDS (its entries were asked for; then the next one's are).  Bit x of what it returns:
+  // row 4 x + l div 16 of this lane is no token of the sequence, or its page is not there.
+  auto fetch = [&](int step) {
+    uint32_t dead = 0;
+    if (step >= n_all) return dead;
+    const int j0 = token_of(step), buf = step & (FP_BUFS - 1);
+    const int e[2] = {entry[0], entry[1]};
+    if (step + 1 < n_all) ask(step + 1);
+    int row0 = 0, j8 = 0;
+    bool no_page = false;
+    if constexpr (ROWS != ANYWHERE) {
+      j8 = ONE ? j0 : min(j0 + 8 * wave, (n - 1) & ~7);
+      row0 = (int)entry_row(a.pages, d.Hkv, e[0], hk, j8);
+      no_page = row0 < 0;
+      row0 = max(row0, 0);
     }
 #pragma unroll
     for (int x = 0; x < 2; ++x) {
       const int rr = 8 * wave + 4 * x + (lane >> 4);
       int r;
-      if constexpr (ONE) {
-        r = row[0] + min(rr, n - 1 - j0);
-        dead[x] = j0 + rr >= n;                // (a page that is not there: the whole tile is passed over)
+      if constexpr (ROWS != ANYWHERE) {
+        r = row0 + min(ONE ? rr : rr - 8 * wave, n - 1 - j8);
+        dead |= j0 + rr >= n || no_page ? 1u << x : 0u;
       } else {
-        r = (int)entry_row(a.pages, d.Hkv, entry[x], hk, min(j0 + rr, n - 1));
-        dead[x] = j0 + rr >= n || r < 0;
+        r = (int)entry_row(a.pages, d.Hkv, e[x], hk, min(j0 + rr, n - 1));
+        dead |= j0 + rr >= n || r < 0 ? 1u << x : 0u;
         r = max(r, 0);
       }
       const unsigned char* kp = (const unsigned char*)a.pages.k + (size_t)(uint32_t)r * (D * 2);
       const unsigned char* vp = (const unsigned char*)a.pages.v + (size_t)(uint32_t)r * (D * 2);
       const int to = buf * FP_TILE + (8 * wave + 4 * x) * 256;
       to_lds(kp + ((piece ^ (rr & 15)) << 4), uniform((int)(lds0 + to)));
-      to_lds(vp + ((piece ^ (2 * (rr & 7))) << 4), uniform((int)(lds0 + 2 * FP_TILE + to)));
+      to_lds(vp + ((piece ^ (2 * (rr & 7))) << 4), uniform((int)(lds0 + FP_BUFS * FP_TILE + to)));
     }
+    return dead;
+  };
+  auto barrier = [&] {
+    __builtin_amdgcn_sched_barrier(0);
+    asm volatile("s_barrier" ::: "memory");
+    __builtin_amdgcn_sched_barrier(0);
+  };
+  // waits for this wave's rows of all tiles but, if one more is on its way, the last that it fetched
+  auto arrive = [&](bool more) {
+    if (more) asm volatile("s_waitcnt vmcnt(4)" ::: "memory");
+    else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
   };
 
-  f32x16_t o[4];
+  f32x16_t o[4], s[2];
+  bf16x8_t p[4];
 #pragma unroll
   for (int cb = 0; cb < 4; ++cb)
 #pragma unroll
@@ -135,73 +183,11 @@ __global__ __launch_bounds__(64 * FP_WAVES, 2) void prompt_bf16_kernel(DevDesc d
   // LDS addresses of a lane's operands, relative to a tile
   const int k_row = col * 256, k_swz = col & 15;
   const int v_key = 4 * half + ((lane & 15) >> 2);               // of each group of eight tokens
-  const int v_at = v_key * 256, v_swz = 2 * (v_key & 7);
-  const int v_chunk = 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1), v_byte = 8 * (lane & 1);
+  const int v_at = v_key * 256 + 8 * (lane & 1), v_swz = 2 * (v_key & 7);
+  const int v_chunk = 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1);
 
-  if (i0 < i1) {
-    ask(i0);
-    fetch(i0, 0);
-    if (i0 + 1 < i1) ask(i0 + 1);
-  }
-  bool gone = ONE && i0 < i1 && (uint32_t)page_entry(a.pages, b, tile_token<FP_KEYS>(tr, i0)) >= (uint32_t)a.pages.n_pages;
-  for (int i = i0; i < i1; ++i) {
-    const int buf = (i - i0) & 1;
-    const int j0 = tile_token<FP_KEYS>(tr, i);
-    // does every column see the whole tile?
-    const bool edge = !(j0 + FP_KEYS - 1 <= lo && (a.vis.window == 0 || j0 > hi - a.vis.window || j0 + FP_KEYS - 1 < a.vis.n_sink));
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-    {
-      uint32_t odd = 0;
-#pragma unroll
-      for (int x = 0; x < 2; ++x) {
-        u32x4_t* mine = reinterpret_cast<u32x4_t*>(s_v + buf * FP_TILE + (8 * wave + 4 * x) * 256 + lane * 16);
-        if (__any(dead[x])) {
-          if (dead[x]) *mine = u32x4_t{0, 0, 0, 0};
-        }
-        if (edge) {
-          u32x4_t v = *mine;
-          bool bad = false;
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const uint32_t lo16 = (v[e] & 0x7f80u) == 0x7f80u ? 0x0000ffffu : 0u;
-            const uint32_t hi16 = (v[e] & 0x7f800000u) == 0x7f800000u ? 0xffff0000u : 0u;
-            bad = bad || (lo16 | hi16) != 0;
-            v[e] &= ~(lo16 | hi16);
-          }
-          if (bad && !dead[x]) *mine = v;
-          const unsigned long long who = __ballot(bad && !dead[x]);
-#pragma unroll
-          for (int r = 0; r < 4; ++r) odd |= ((who >> (16 * r)) & 0xffffu) != 0 ? 1u << (4 * x + r) : 0u;
-        }
-      }
-      if (!ONE) {
-        uint32_t there = 0;
-#pragma unroll
-        for (int x = 0; x < 2; ++x) {
-          const unsigned long long who = __ballot(!dead[x]);
-#pragma unroll
-          for (int r = 0; r < 4; ++r) there |= (uint32_t)((who >> (16 * r)) & 1) << (4 * x + r);
-        }
-        if (lane == 0) s_there[8 * buf + wave] = (unsigned char)there;
-      }
-      if (edge && lane == 0) s_odd[8 * buf + wave] = (unsigned char)odd;
-    }
-    __syncthreads();
-    bool next_gone = false;
-    if (i + 1 < i1) {
-      next_gone = ONE && (uint32_t)entry[0] >= (uint32_t)a.pages.n_pages;
-      fetch(i + 1, buf ^ 1);
-      if (i + 2 < i1) ask(i + 2);
-    }
-    const bool skip = gone;
-    gone = next_gone;
-    const bool none = !wave_live || skip || j0 > hi_w ||
-                      (a.vis.window > 0 && j0 + FP_KEYS - 1 <= lo_w - a.vis.window && j0 >= a.vis.n_sink);
-    if (none) continue;
-
-    const unsigned char* tk = s_k + buf * FP_TILE;
-    const unsigned char* tv = s_v + buf * FP_TILE;
-    f32x16_t s[2];
+  auto logits = [&](int step) {                 // s = K Q^T
+    const unsigned char* tk = s_k + (step & (FP_BUFS - 1)) * FP_TILE;
 #pragma unroll
     for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
@@ -213,21 +199,9 @@ __global__ __launch_bounds__(64 * FP_WAVES, 2) void prompt_bf16_kernel(DevDesc d
         const bf16x8_t k = *reinterpret_cast<const bf16x8_t*>(tk + kb * 32 * 256 + k_row + (((2 * c + half) ^ k_swz) << 4));
         s[kb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k, q[c], s[kb], 0, 0, 0);
       }
-    uint64_t there = ~0ull;
-    if (!ONE) there = *reinterpret_cast<const uint64_t*>(s_there + 8 * buf);
-    const bool whole = j0 + FP_KEYS - 1 <= lo_w && (ONE || there == ~0ull) && mw + 32 <= cols &&
-                       (a.vis.window == 0 || j0 > hi_w - a.vis.window || j0 + FP_KEYS - 1 < a.vis.n_sink);
-    if (!whole) {
-#pragma unroll
-      for (int kb = 0; kb < 2; ++kb)
-#pragma unroll
-        for (int x = 0; x < 16; ++x) {
-          const int key = 32 * kb + 8 * (x / 4) + 4 * half + x % 4;
-          const bool ok = sees(a.vis, P, j0 + key) && (ONE || ((there >> key) & 1));
-          s[kb][x] = ok ? s[kb][x] : NEG_INF;
-        }
-    }
-    float mx = NEG_INF;
+  };
+  auto weights = [&] {                          // s -> p, with the running maximum and sum
+    float mx = s[0][0];
 #pragma unroll
     for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
@@ -244,7 +218,6 @@ __global__ __launch_bounds__(64 * FP_WAVES, 2) void prompt_bf16_kernel(DevDesc d
       m_run = m_new;
     }
     const float m_use = m_run == NEG_INF ? 0.f : m_run;
-    bf16x8_t p[4];
 #pragma unroll
     for (int ks = 0; ks < 4; ++ks) {
 #pragma unroll
@@ -257,50 +230,157 @@ __global__ __launch_bounds__(64 * FP_WAVES, 2) void prompt_bf16_kernel(DevDesc d
         p[ks][e + 1] = y[1];
       }
     }
+  };
+  auto add_values = [&](int step) {             // o += V^T p
+    const unsigned char* tv = s_v + (step & (FP_BUFS - 1)) * FP_TILE;
 #pragma unroll
     for (int ks = 0; ks < 4; ++ks)
 #pragma unroll
       for (int cb = 0; cb < 4; ++cb) {
         // tokens 16 ks + {0..3, 8..11} (+ 4 for the upper lanes) of channel 32 cb + lane mod 32
-        const int c = ((4 * cb + v_chunk) ^ v_swz) << 4;
-        const unsigned char* vp = tv + ks * 16 * 256 + v_at + v_byte + c;
         typedef __attribute__((address_space(3))) s16x4_t* lds4;
+        const unsigned char* vp = tv + ks * 16 * 256 + v_at + (((4 * cb + v_chunk) ^ v_swz) << 4);
         const s16x4_t x = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)(vp));
         const s16x4_t y = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)(vp + 8 * 256));
-        typedef short s16x8_t __attribute__((ext_vector_type(8)));
         const s16x8_t v = {x[0], x[1], x[2], x[3], y[0], y[1], y[2], y[3]};
         o[cb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, v), p[ks], o[cb], 0, 0, 0);
       }
-    if (edge) {
-      uint64_t odd = *reinterpret_cast<const uint64_t*>(s_odd + 8 * buf);
-      if (odd != 0) {
-        float* sp = s_p + wave * FP_KEYS * 32;
+  };
+
+  uint32_t d0 = 0, d1 = 0, d2 = 0;              // what fetch said of the last three tiles
+  auto fetch_next = [&](int step) {
+    d0 = d1;
+    d1 = d2;
+    d2 = fetch(step);
+  };
+  if (n_all > 0) {
+    ask(0);
+    fetch_next(0);
+    fetch_next(1);
+  }
+
+  // Tiles that are seen whole.  Waves 0..3 and 4..7, one of each on a SIMD, go half a tile apart: while one has the matrix unit
+  // (values of step i, logits of step i + 1), the other has the vector unit (weights).  Stretch k lies between barriers k and
+  // k + 1 of the loop: the early waves compute the weights of step i in stretch 2 i, the late ones in stretch 2 i + 1.  What is
+  // fetched there, step i + 2 or i + 3, takes the place of a tile whose values were last read two stretches before, and what
+  // has arrived at the stretch's end, step i + 1 or i + 2, is first read in the stretch after or later.
+  if (n_in > 0) {
+    const int late = wave >= FP_WAVES / 2 ? 1 : 0;
+    arrive(1 < n_all);
+    barrier();
+    logits(0);
+    if (late) {
+      fetch_next(2);
+      arrive(2 < n_all);
+      barrier();
+    }
+    for (int i = 0; i < n_in; ++i) {
+      fetch_next(i + 2 + late);
+      weights();
+      arrive(i + 2 + late < n_all);
+      barrier();
+      add_values(i);
+      logits(i + 1);                            // (behind the last step: of what LDS holds, and nobody looks at it)
+      // operands are read four products ahead
+      __builtin_amdgcn_sched_group_barrier(0x100, 8, 0);
 #pragma unroll
-        for (int ks = 0; ks < 4; ++ks)
-#pragma unroll
-          for (int e = 0; e < 8; ++e) sp[(16 * ks + 8 * (e / 4) + 4 * half + e % 4) * 32 + col] = (float)p[ks][e];
-        __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
-        __builtin_amdgcn_wave_barrier();
-        __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
-        while (odd != 0) {
-          const int key = __ffsll((unsigned long long)odd) - 1;
-          odd &= odd - 1;
-          const long long r = page_row(a.pages, d.Hkv, b, hk, j0 + key);
-          if (r < 0 || !sees(a.vis, P, j0 + key)) continue;
-          const float pk = sp[key * 32 + col];
-          const uint32_t* vr = reinterpret_cast<const uint32_t*>((const bf16_t*)a.pages.v + r * D);
-#pragma unroll
-          for (int cb = 0; cb < 4; ++cb)
-#pragma unroll
-            for (int x = 0; x < 16; x += 2) {
-              const uint32_t v = vr[(32 * cb + 8 * (x / 4) + 4 * half + x % 4) / 2];
-              if ((v & 0x7f80u) == 0x7f80u) o[cb][x] = fmaf(pk, __uint_as_float(v << 16), o[cb][x]);
-              if ((v & 0x7f800000u) == 0x7f800000u) o[cb][x + 1] = fmaf(pk, __uint_as_float(v & 0xffff0000u), o[cb][x + 1]);
-            }
-        }
-        __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
-        __builtin_amdgcn_wave_barrier();
+      for (int x = 0; x < 12; ++x) {
+        __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+        __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
       }
+#pragma unroll
+      for (int x = 0; x < 16; ++x) {
+        __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+        __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+      }
+      __builtin_amdgcn_sched_group_barrier(0x008, 4, 0);
+      barrier();
+    }
+    if (!late) {
+      fetch_next(n_in + 2);
+      barrier();
+    }
+  } else if (n_all > 0) {
+    fetch_next(2);
+  }
+
+  // The others: three tiles on their way, one barrier a tile.
+  for (int step = n_in; step < n_all; ++step) {
+    const int buf = step & (FP_BUFS - 1), j0 = token_of(step);
+    if (step + 2 < n_all) asm volatile("s_waitcnt vmcnt(8)" ::: "memory");
+    else if (step + 1 < n_all) asm volatile("s_waitcnt vmcnt(4)" ::: "memory");
+    else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    uint32_t odd = 0, rows = 0;
+#pragma unroll
+    for (int x = 0; x < 2; ++x) {
+      const bool dead = (d0 >> x) & 1;
+      u32x4_t* mine = reinterpret_cast<u32x4_t*>(s_v + buf * FP_TILE + (8 * wave + 4 * x) * 256 + lane * 16);
+      u32x4_t v = *mine;
+      bool bad = false;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const uint32_t lo16 = (v[e] & 0x7f80u) == 0x7f80u ? 0x0000ffffu : 0u;
+        const uint32_t hi16 = (v[e] & 0x7f800000u) == 0x7f800000u ? 0xffff0000u : 0u;
+        bad = bad || (lo16 | hi16) != 0;
+        v[e] = dead ? 0u : v[e] & ~(lo16 | hi16);
+      }
+      if (dead || bad) *mine = v;
+      const unsigned long long alive = __ballot(!dead), who = __ballot(bad && !dead);
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        rows |= (uint32_t)((alive >> (16 * r)) & 1) << (4 * x + r);
+        odd |= ((who >> (16 * r)) & 0xffffu) != 0 ? 1u << (4 * x + r) : 0u;
+      }
+    }
+    if (lane == 0) {
+      s_there[FP_WAVES * buf + wave] = (unsigned char)rows;
+      s_odd[FP_WAVES * buf + wave] = (unsigned char)odd;
+    }
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    barrier();
+    fetch_next(step + 3);
+    const uint64_t there = *reinterpret_cast<const uint64_t*>(s_there + FP_WAVES * buf);
+    if (!wave_live || there == 0 || j0 > hi_w ||
+        (a.vis.window > 0 && j0 + FP_KEYS - 1 <= lo_w - a.vis.window && j0 >= a.vis.n_sink))
+      continue;                                 // no column of this wave sees any of it
+    logits(step);
+#pragma unroll
+    for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+      for (int x = 0; x < 16; ++x) {
+        const int key = 32 * kb + 8 * (x / 4) + 4 * half + x % 4;
+        s[kb][x] = sees(a.vis, P, j0 + key) && ((there >> key) & 1) ? s[kb][x] : NEG_INF;
+      }
+    weights();
+    add_values(step);
+    // values that are not finite, for the columns that see them; their weights once more, from the keys in LDS
+    uint64_t left = *reinterpret_cast<const uint64_t*>(s_odd + FP_WAVES * buf);
+    while (left != 0) {
+      const int key = __ffsll((unsigned long long)left) - 1;
+      left &= left - 1;
+      float x = 0.f;
+#pragma unroll
+      for (int c = 0; c < 8; ++c) {
+        const u32x4_t k = *reinterpret_cast<const u32x4_t*>(s_k + buf * FP_TILE + key * 256 + (((2 * c + half) ^ (key & 15)) << 4));
+        const u32x4_t y = __builtin_bit_cast(u32x4_t, q[c]);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          x = fmaf(__uint_as_float(k[e] << 16), __uint_as_float(y[e] << 16), x);
+          x = fmaf(__uint_as_float(k[e] & 0xffff0000u), __uint_as_float(y[e] & 0xffff0000u), x);
+        }
+      }
+      const float w = exp2_(fmaf(across_sum(x), sc.c, m_run == NEG_INF ? 0.f : -m_run));
+      if (!sees(a.vis, P, j0 + key)) continue;
+      const long long r = page_row(a.pages, d.Hkv, b, hk, j0 + key);
+      const uint32_t* vr = reinterpret_cast<const uint32_t*>((const bf16_t*)a.pages.v + r * D);
+#pragma unroll
+      for (int cb = 0; cb < 4; ++cb)
+#pragma unroll
+        for (int e = 0; e < 16; e += 2) {
+          const uint32_t v = vr[(32 * cb + 8 * (e / 4) + 4 * half + e % 4) / 2];
+          if ((v & 0x7f80u) == 0x7f80u) o[cb][e] = fmaf(w, __uint_as_float(v << 16), o[cb][e]);
+          if ((v & 0x7f800000u) == 0x7f800000u) o[cb][e + 1] = fmaf(w, __uint_as_float(v & 0xffff0000u), o[cb][e + 1]);
+        }
     }
   }
   l_run = across_sum(l_run);
@@ -387,8 +467,9 @@ hipError_t launch_prompt_bf16(const DevDesc& d, const PagedArgs& a, const Prompt
   static std::once_flag once;
   static hipError_t raised = hipSuccess;
   std::call_once(once, [] {
-    for (const void* f : {(const void*)prompt_bf16_kernel<true, false>, (const void*)prompt_bf16_kernel<false, false>,
-                          (const void*)prompt_bf16_kernel<true, true>, (const void*)prompt_bf16_kernel<false, true>}) {
+    for (const void* f : {(const void*)prompt_bf16_kernel<IN_ONE_PAGE, false>, (const void*)prompt_bf16_kernel<IN_ONE_PAGE, true>,
+                          (const void*)prompt_bf16_kernel<EIGHT_A_PAGE, false>, (const void*)prompt_bf16_kernel<EIGHT_A_PAGE, true>,
+                          (const void*)prompt_bf16_kernel<ANYWHERE, false>, (const void*)prompt_bf16_kernel<ANYWHERE, true>}) {
       const hipError_t e = hipFuncSetAttribute(f, hipFuncAttributeMaxDynamicSharedMemorySize, FP_LDS);
       if (e != hipSuccess) raised = e;
     }
@@ -400,15 +481,14 @@ hipError_t launch_prompt_bf16(const DevDesc& d, const PagedArgs& a, const Prompt
   po.lse = a.scores ? (float*)(base + p.off_lse) : nullptr;
   po.part_o = p.splits > 1 ? (float*)(base + p.off_o) : nullptr;
   po.part_ml = p.splits > 1 ? (float*)(base + p.off_ml) : nullptr;
-  const bool one = a.pages.table == nullptr || a.pages.page_size % FP_KEYS == 0;
   const dim3 grid((unsigned)(col_tiles_most(a.n_rows, d.B, d.G, FP_COLS) * d.Hkv), p.splits), block(64 * FP_WAVES);
-  if (p.splits > 1) {
-    if (one) hipLaunchKernelGGL((prompt_bf16_kernel<true, true>), grid, block, FP_LDS, st, d, a, po);
-    else hipLaunchKernelGGL((prompt_bf16_kernel<false, true>), grid, block, FP_LDS, st, d, a, po);
-  } else {
-    if (one) hipLaunchKernelGGL((prompt_bf16_kernel<true, false>), grid, block, FP_LDS, st, d, a, po);
-    else hipLaunchKernelGGL((prompt_bf16_kernel<false, false>), grid, block, FP_LDS, st, d, a, po);
-  }
+  auto launch = [&](auto rows) {
+    if (p.splits > 1) hipLaunchKernelGGL((prompt_bf16_kernel<decltype(rows)::value, true>), grid, block, FP_LDS, st, d, a, po);
+    else hipLaunchKernelGGL((prompt_bf16_kernel<decltype(rows)::value, false>), grid, block, FP_LDS, st, d, a, po);
+  };
+  if (a.pages.table == nullptr || a.pages.page_size % FP_KEYS == 0) launch(std::integral_constant<int, IN_ONE_PAGE>{});
+  else if (a.pages.page_size % 8 == 0) launch(std::integral_constant<int, EIGHT_A_PAGE>{});
+  else launch(std::integral_constant<int, ANYWHERE>{});
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess || p.splits == 1) return e;
   hipLaunchKernelGGL(prompt_join_kernel, dim3((unsigned)(((long long)a.n_rows * d.Hq + 3) / 4)), dim3(256), 0, st, d, a, po, p.splits);
