@@ -13,7 +13,7 @@
 //   The running maximum moves only when it is passed by more than 8 (in powers of two): p then stays below 2^8, and the
 // products, 64 registers, are seldom scaled.
 //
-// LDS rows are 256 bytes, 16 pieces of 16; keys: piece c of row r lies at c ^ (r mod 16), values: at c ^ 2 (r mod 8), so that
+// LDS rows are 256 bytes, 16 pieces of 16; keys: piece c of row r lies at c ^ (r mod 16), values: at c ^ 4 (r mod 4), so that
 // the lanes that are served together find different banks.
 //
 // In tiles that some column does not see whole, rows that nobody sees are cleared in LDS and values that are not finite are
@@ -157,7 +157,7 @@ __global__ __launch_bounds__(64 * FP_WAVES, 2) void prompt_bf16_kernel(DevDesc d
       const unsigned char* vp = (const unsigned char*)a.pages.v + (size_t)(uint32_t)r * (D * 2);
       const int to = buf * FP_TILE + (8 * wave + 4 * x) * 256;
       to_lds(kp + ((piece ^ (rr & 15)) << 4), uniform((int)(lds0 + to)));
-      to_lds(vp + ((piece ^ (2 * (rr & 7))) << 4), uniform((int)(lds0 + FP_BUFS * FP_TILE + to)));
+      to_lds(vp + ((piece ^ (4 * (rr & 3))) << 4), uniform((int)(lds0 + FP_BUFS * FP_TILE + to)));
     }
     return dead;
   };
@@ -183,7 +183,7 @@ __global__ __launch_bounds__(64 * FP_WAVES, 2) void prompt_bf16_kernel(DevDesc d
   // LDS addresses of a lane's operands, relative to a tile
   const int k_row = col * 256, k_swz = col & 15;
   const int v_key = 4 * half + ((lane & 15) >> 2);               // of each group of eight tokens
-  const int v_at = v_key * 256 + 8 * (lane & 1), v_swz = 2 * (v_key & 7);
+  const int v_at = v_key * 256 + 8 * (lane & 1), v_swz = 4 * (v_key & 3);
   const int v_chunk = 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1);
 
   auto logits = [&](int step) {                 // s = K Q^T
