@@ -515,7 +515,8 @@ int32_t kvr_rotate(const kvr_desc* desc, const kvr_rotation* rot, const void* q,
  *     out[t, hq]  = sum_j p[t, hq, j] v[j]
  * and, if scores is not NULL, every token's cumulative score grows by the sum of p over the new
  * tokens and the G q heads of its kv head, always in the same order.  A query that sees no token
- * yields zeros.  n_ctx is clamped to what the cache can hold.  Tokens that no query of a row sees
+ * yields zeros.  n_ctx is clamped to what the cache can hold.  KVR_ERR_UNSUPPORTED where B * Hkv
+ * times the tokens that a sequence can hold passes 2^37.  Tokens that no query of a row sees
  * may hold anything, Inf and NaN too.
  *   q          dev [n_rows, Hq, D] storage type, read
  *   pages      host; k, v and table are read
@@ -535,8 +536,7 @@ int32_t kvr_attend_prompt(const kvr_desc* desc, const void* q, int32_t n_rows, c
 /*
  * The same for one new token per sequence (row b is sequence b's), by kernels made for it: the
  * cache is shared out by tokens over the whole chip, whatever the sequences' lengths.
- * KVR_ERR_UNSUPPORTED where B * Hkv times the tokens that a sequence can hold (with a window: can
- * show) passes 2^37.
+ * (With a window, what passes 2^37 is B * Hkv times the tokens that a sequence can show.)
  *   q, out     dev [B, Hq, D] storage type
  *   the others as for kvr_attend_prompt
  */

@@ -548,6 +548,7 @@ int32_t kvr_attend_prompt_workspace_size(const kvr_desc* desc, int32_t n_rows, c
   if (rc == KVR_OK) rc = check_visible(window, n_sink, vis);
   if (rc != KVR_OK) return rc;
   if (bytes == nullptr || n_rows < 0 || n_rows > MAX_ROWS_NEW) return KVR_ERR_INVALID_ARG;
+  if (!kvr::attend_paged_fits(d, p.cap, kvr::Visible{0, 0})) return KVR_ERR_UNSUPPORTED;
   *bytes = n_rows == 0 ? 0 : kvr::attend_prompt_ws(d, desc->dtype, n_rows, p.cap, vis, scores != 0);
   return KVR_OK;
 }
@@ -565,6 +566,7 @@ int32_t kvr_attend_prompt(const kvr_desc* desc, const void* q, int32_t n_rows, c
   if (n_rows == 0) return KVR_OK;
   rc = check_attend(desc, q, n_ctx, pages, out, scores, n_cap, a);
   if (rc != KVR_OK) return rc;
+  if (!kvr::attend_paged_fits(d, a.pages.cap, kvr::Visible{0, 0})) return KVR_ERR_UNSUPPORTED;
   rc = check_ws(ws, ws_bytes, kvr::attend_prompt_ws(d, desc->dtype, n_rows, a.pages.cap, a.vis, scores != nullptr));
   if (rc != KVR_OK) return rc;
   a.n_rows = n_rows;

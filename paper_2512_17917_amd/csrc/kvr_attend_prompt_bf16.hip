@@ -161,6 +161,30 @@ __global__ __launch_bounds__(64 * FP_WAVES, 2) void prompt_bf16_kernel(DevDesc d
     }
     return dead;
   };
+  // The same for a step before n_in whose successor is one too: tiles follow one another and all their rows are there, so that
+  // only the rows' start, a scalar, is new (not where rows may lie anywhere).
+  const uint32_t in_row[2] = {(uint32_t)(ONE ? 8 * wave : 0) + (lane >> 4), (uint32_t)(ONE ? 8 * wave : 0) + 4 + (lane >> 4)};
+  uint32_t k_off[2], v_off[2];
+#pragma unroll
+  for (int x = 0; x < 2; ++x) {
+    const int rr = 8 * wave + 4 * x + (lane >> 4);
+    k_off[x] = in_row[x] * 256 + ((piece ^ (rr & 15)) << 4);
+    v_off[x] = in_row[x] * 256 + ((piece ^ (4 * (rr & 3))) << 4);
+  }
+  const int j_in = tile_token<FP_KEYS>(tr, in0) + (ONE ? 0 : 8 * wave);
+  auto fetch_in = [&](int step) {
+    const int j = j_in + step * FP_KEYS;
+    const long long r = entry_row(a.pages, d.Hkv, entry[0], hk, j);
+    entry[0] = page_entry(a.pages, b, j + FP_KEYS);
+    const unsigned char* kp = (const unsigned char*)a.pages.k + r * (D * 2);
+    const unsigned char* vp = (const unsigned char*)a.pages.v + r * (D * 2);
+    const uint32_t to = lds0 + (step & (FP_BUFS - 1)) * FP_TILE + 8 * wave * 256;
+#pragma unroll
+    for (int x = 0; x < 2; ++x) {
+      to_lds(kp, k_off[x], uniform((int)(to + x * 1024)));
+      to_lds(vp, v_off[x], uniform((int)(to + FP_BUFS * FP_TILE + x * 1024)));
+    }
+  };
   auto barrier = [&] {
     __builtin_amdgcn_sched_barrier(0);
     asm volatile("s_barrier" ::: "memory");
@@ -275,7 +299,8 @@ __global__ __launch_bounds__(64 * FP_WAVES, 2) void prompt_bf16_kernel(DevDesc d
       barrier();
     }
     for (int i = 0; i < n_in; ++i) {
-      fetch_next(i + 2 + late);
+      if (ROWS != ANYWHERE && i + 3 + late < n_in) fetch_in(i + 2 + late);
+      else fetch_next(i + 2 + late);
       weights();
       arrive(i + 2 + late < n_all);
       barrier();

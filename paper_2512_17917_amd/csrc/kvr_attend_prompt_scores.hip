@@ -14,20 +14,24 @@ namespace kvr {
 namespace {
 
 constexpr int SC_WAVES = 4, SC_KEYS = 64 * SC_WAVES, SC_COLS = 64;
-constexpr int SC_TILE = SC_COLS * D * 2;
+constexpr int SC_TILE = SC_COLS * D * 2, SC_BUFS = 3;
 
 __global__ __launch_bounds__(64 * SC_WAVES, 2) void prompt_scores_bf16_kernel(DevDesc d, PagedArgs a, const float* lse, float* part,
-                                                                              int keys_cap) {
-  __shared__ __align__(1024) unsigned char s_q[2 * SC_TILE];
-  __shared__ __align__(16) float s_lse[2][SC_COLS];
+                                                                              int keys_cap, int splits) {
+  __shared__ __align__(1024) unsigned char s_q[SC_BUFS * SC_TILE];
+  __shared__ __align__(16) float s_lse[SC_BUFS][SC_COLS];
   const int lane = threadIdx.x & 63, wave = uniform((int)(threadIdx.x >> 6));
   const int half = lane >> 5, col = lane & 31;
-  const int u = blockIdx.y, b = uniform(u / d.Hkv), hk = u - b * d.Hkv;
+  // units next to each other: a block of tokens early in a prompt has many times the work of a late one, and neighbours in the
+  // grid go to the chip's dies in turn
+  const int units = d.B * d.Hkv, order = uniform((int)(blockIdx.x / (unsigned)units));
+  const int block = uniform(order / splits), split = order - block * splits;
+  const int u = (int)(blockIdx.x - (unsigned)order * units), b = uniform(u / d.Hkv), hk = u - b * d.Hkv;
   const int gs = __builtin_ctz(d.G);
   const RowSpan span = row_span(a.q_start, a.n_rows, b);
   const int n = clampi(listed(a.n_ctx + b), 0, a.pages.cap);
   const int first = n - span.n;
-  const int j0 = blockIdx.x * SC_KEYS;
+  const int j0 = block * SC_KEYS;
   if (j0 >= n) return;
   const int jw = j0 + 64 * wave;                     // this wave's tokens
   // new tokens of which some may see one of the block's
@@ -37,8 +41,8 @@ __global__ __launch_bounds__(64 * SC_WAVES, 2) void prompt_scores_bf16_kernel(De
   const int cols = t1 << gs;                         // columns t0 G .. cols - 1
   const int c0 = t0 << gs;
   const int tiles = cols > c0 ? (cols - c0 + SC_COLS - 1) / SC_COLS : 0;
-  const int per = uniform((int)((tiles + gridDim.z - 1) / gridDim.z));
-  const int i0 = min((int)blockIdx.z * per, tiles), i1 = min(i0 + per, tiles);
+  const int per = uniform((tiles + splits - 1) / splits);
+  const int i0 = min(split * per, tiles), i1 = min(i0 + per, tiles);
 
   const Scale2 sc = scale2(d.scale);
   bf16x8_t k[2][8];
@@ -60,8 +64,8 @@ __global__ __launch_bounds__(64 * SC_WAVES, 2) void prompt_scores_bf16_kernel(De
 
   // rows of a tile to LDS: 16 columns of 256 bytes a wave, piece c of row r at c ^ (r mod 16)
   const uint32_t lds0 = lds_offset(s_q);
-  float lse_next = 0.f;
-  auto fetch = [&](int i, int buf) {
+  const uint32_t lds1 = lds_offset(s_lse);
+  auto fetch = [&](int i, int buf) {                 // five loads a wave
     const int m0 = c0 + i * SC_COLS;
 #pragma unroll
     for (int x = 0; x < 4; ++x) {
@@ -71,25 +75,25 @@ __global__ __launch_bounds__(64 * SC_WAVES, 2) void prompt_scores_bf16_kernel(De
       to_lds((const unsigned char*)a.q + at * (D * 2) + (((lane & 15) ^ (r & 15)) << 4),
              uniform((int)(lds0 + buf * SC_TILE + (16 * wave + 4 * x) * 256)));
     }
-    if (wave == 0) {
-      const int m = min(m0 + lane, cols - 1);
-      const float v = lse[(size_t)(span.first + (m >> gs)) * d.Hq + hk * d.G + (m & (d.G - 1))];
-      lse_next = m0 + lane < cols ? v : __builtin_inff();       // weight 0
-    }
+    const int m = min(m0 + lane, cols - 1);          // (all waves fetch the same)
+    word_to_lds(lse + (size_t)(span.first + (m >> gs)) * d.Hq + hk * d.G + (m & (d.G - 1)), uniform((int)(lds1 + buf * SC_COLS * 4)));
   };
 
   float acc[2] = {0.f, 0.f};
   if (i0 < i1) fetch(i0, 0);
-  for (int i = i0; i < i1; ++i) {
-    const int buf = (i - i0) & 1;
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-    if (wave == 0) s_lse[buf][lane] = lse_next;
-    __syncthreads();
-    if (i + 1 < i1) fetch(i + 1, buf ^ 1);
+  if (i0 + 1 < i1) fetch(i0 + 1, 1);
+  int buf = 0;
+  for (int i = i0; i < i1; ++i, buf = buf == SC_BUFS - 1 ? 0 : buf + 1) {
+    if (i + 1 < i1) asm volatile("s_waitcnt vmcnt(5)" ::: "memory");
+    else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    __builtin_amdgcn_sched_barrier(0);
+    asm volatile("s_barrier" ::: "memory");
+    __builtin_amdgcn_sched_barrier(0);
+    if (i + 2 < i1) fetch(i + 2, buf == 0 ? SC_BUFS - 1 : buf - 1);
     const int m0 = c0 + i * SC_COLS;
     const int lo = first + (m0 >> gs), hi = first + ((min(m0 + SC_COLS, cols) - 1) >> gs);   // positions of the columns
     if (jw > hi || jw >= n || (a.vis.window > 0 && jw + 63 <= lo - a.vis.window && jw >= a.vis.n_sink)) continue;
-    const bool whole = jw + 63 <= lo && (a.vis.window == 0 || jw > hi - a.vis.window || jw + 63 < a.vis.n_sink);
+    const bool whole = jw + 63 <= lo && m0 + SC_COLS <= cols && (a.vis.window == 0 || jw > hi - a.vis.window || jw + 63 < a.vis.n_sink);
     const unsigned char* tq = s_q + buf * SC_TILE;
 #pragma unroll
     for (int cb = 0; cb < 2; ++cb) {
@@ -104,27 +108,23 @@ __global__ __launch_bounds__(64 * SC_WAVES, 2) void prompt_scores_bf16_kernel(De
 #pragma unroll
         for (int kb = 0; kb < 2; ++kb) s[kb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(q, k[kb][c], s[kb], 0, 0, 0);
       }
+      if (!whole) {
+#pragma unroll
+        for (int x = 0; x < 16; ++x) {
+          const int m = m0 + 32 * cb + 8 * (x / 4) + 4 * half + x % 4;
+          const int P = m < cols ? first + (m >> gs) : -1;
+#pragma unroll
+          for (int kb = 0; kb < 2; ++kb) s[kb][x] = sees(a.vis, P, jw + 32 * kb + col) ? s[kb][x] : -__builtin_inff();
+        }
+      }
 #pragma unroll
       for (int x = 0; x < 16; x += 4) {
         const float4 l = *reinterpret_cast<const float4*>(&s_lse[buf][32 * cb + 2 * x + 4 * half]);
         const float le[4] = {l.x, l.y, l.z, l.w};
-        if (whole) {
 #pragma unroll
-          for (int kb = 0; kb < 2; ++kb)
+        for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
-            for (int e = 0; e < 4; ++e) acc[kb] += exp2_(fmaf(s[kb][x + e], sc.c, -le[e]));
-        } else {
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const int m = m0 + 32 * cb + 2 * x + 4 * half + e;
-            const int P = first + (m >> gs);
-#pragma unroll
-            for (int kb = 0; kb < 2; ++kb) {
-              const float p = exp2_(fmaf(s[kb][x + e], sc.c, -le[e]));
-              acc[kb] += sees(a.vis, P, jw + 32 * kb + col) ? p : 0.f;
-            }
-          }
-        }
+          for (int e = 0; e < 4; ++e) acc[kb] += exp2_(fmaf(s[kb][x + e], sc.c, -le[e]));
       }
     }
   }
@@ -133,7 +133,7 @@ __global__ __launch_bounds__(64 * SC_WAVES, 2) void prompt_scores_bf16_kernel(De
     const float sum = across_sum(acc[kb]);
     const int j = jw + 32 * kb + col;
     if (half == 0 && j < keys_cap) {
-      if (part) part[((size_t)blockIdx.z * gridDim.y + u) * keys_cap + j] = there[kb] ? sum : 0.f;
+      if (part) part[((size_t)split * units + u) * keys_cap + j] = there[kb] ? sum : 0.f;
       else if (there[kb] && sum != 0.f) a.scores[(size_t)u * a.n_cap + j] += sum;
     }
   }
@@ -171,8 +171,8 @@ hipError_t launch_prompt_scores_bf16(const DevDesc& d, const PagedArgs& a, const
                                      hipStream_t st) {
   const int keys = scores_keys(a.pages.cap, a.n_cap);
   const unsigned units = d.B * d.Hkv;
-  hipLaunchKernelGGL(prompt_scores_bf16_kernel, dim3((keys + SC_KEYS - 1) / SC_KEYS, units, p.splits), dim3(64 * SC_WAVES), 0, st, d,
-                     a, lse, p.splits > 1 ? part : nullptr, keys);
+  hipLaunchKernelGGL(prompt_scores_bf16_kernel, dim3((unsigned)((keys + SC_KEYS - 1) / SC_KEYS) * units * p.splits), dim3(64 * SC_WAVES), 0, st, d,
+                     a, lse, p.splits > 1 ? part : nullptr, keys, p.splits);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess || p.splits == 1) return e;
   hipLaunchKernelGGL(scores_add_kernel, dim3((keys + 255) / 256, units), dim3(256), 0, st, d, a, part, keys, p.splits);

@@ -140,6 +140,8 @@ def test_more_tokens_than_the_chunks_numbers_hold_are_refused():
         assert kvr.lib().kvr_attend_paged_workspace_size(C.byref(d), C.byref(p), 0, 0, 0, C.byref(n)) == want
     assert _paged(desc=d, over=big, n_cap=64) == U and _paged(desc=d, over=less) == W
     assert _paged(desc=d, over=big, window=5000) == W
+    rows = dict(n_rows=5, q_start=P)
+    assert _prompt(desc=d, over=big, **rows) == U and _prompt(desc=d, over=less, **rows) == W
 
 
 def test_binding_refuses_what_does_not_fit():
