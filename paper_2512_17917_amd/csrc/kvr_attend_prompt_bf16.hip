@@ -45,7 +45,7 @@ struct PromptOut {
 enum { IN_ONE_PAGE, EIGHT_A_PAGE, ANYWHERE };
 
 template <int ROWS, bool SPLIT>
-__global__ __launch_bounds__(64 * FP_WAVES, 2) void prompt_bf16_kernel(DevDesc d, PagedArgs a, PromptOut po) {
+__global__ __launch_bounds__(64 * FP_WAVES, 2) void prompt_bf16_kernel(DevDesc d, PagedArgs a, PromptOut po, int splits) {
   extern __shared__ __align__(1024) unsigned char s_mem[];
   unsigned char* s_k = s_mem;                                   // [4][64][256]
   unsigned char* s_v = s_k + FP_BUFS * FP_TILE;                 // [4][64][256]
@@ -55,7 +55,10 @@ __global__ __launch_bounds__(64 * FP_WAVES, 2) void prompt_bf16_kernel(DevDesc d
   const int lane = threadIdx.x & 63, wave = uniform((int)(threadIdx.x >> 6));
   const int half = lane >> 5, col = lane & 31;
   const float NEG_INF = -__builtin_inff();
-  const int tile = uniform((int)(blockIdx.x / d.Hkv)), hk = (int)blockIdx.x - tile * d.Hkv;
+  // Heads next to each other in the grid (neighbours go to the chip's dies in turn, so that a die's L2 holds few heads), then the
+  // parts of a tile, then tiles: those that turn out not to be there come last, where they take no compute unit's turn.
+  const int order = uniform((int)(blockIdx.x / (unsigned)d.Hkv)), hk = (int)(blockIdx.x - (unsigned)order * d.Hkv);
+  const int tile = SPLIT ? uniform(order / splits) : order, split = SPLIT ? order - tile * splits : 0;
   const int gs = __builtin_ctz(d.G);                            // G is a power of two
   const ColTile ct = col_tile(a.q_start, a.n_rows, d.B, d.G, FP_COLS, tile);
   const int b = uniform(ct.b);
@@ -77,8 +80,8 @@ __global__ __launch_bounds__(64 * FP_WAVES, 2) void prompt_bf16_kernel(DevDesc d
   const TileRange tr = tile_range<FP_KEYS>(a.vis, lo, hi);
   int i0 = 0, i1 = tr.n;
   if (SPLIT) {
-    const int per = uniform((int)((tr.n + gridDim.y - 1) / gridDim.y));
-    i0 = min((int)blockIdx.y * per, tr.n);
+    const int per = uniform((tr.n + splits - 1) / splits);
+    i0 = min(split * per, tr.n);
     i1 = min(i0 + per, tr.n);
   }
   const size_t at = (size_t)(span.first + t) * d.Hq + hk * d.G + g;
@@ -411,7 +414,7 @@ __global__ __launch_bounds__(64 * FP_WAVES, 2) void prompt_bf16_kernel(DevDesc d
   l_run = across_sum(l_run);
   if (!live) return;
   if (SPLIT) {
-    const size_t slot = (size_t)blockIdx.y * a.n_rows * d.Hq + at;
+    const size_t slot = (size_t)split * a.n_rows * d.Hq + at;
     float* op = po.part_o + slot * D;
 #pragma unroll
     for (int cb = 0; cb < 4; ++cb)
@@ -437,24 +440,40 @@ __global__ __launch_bounds__(64 * FP_WAVES, 2) void prompt_bf16_kernel(DevDesc d
   if (po.lse && half == 0) po.lse[at] = m_run == NEG_INF ? __builtin_inff() : m_run + __builtin_amdgcn_logf(l_run);
 }
 
-// Joins the splits of a row and head: a wave each.
+// Joins the parts of a row and head: a wave each, lane l channels 2 l and 2 l + 1; eight parts' numbers are asked for at once.
 __global__ __launch_bounds__(256) void prompt_join_kernel(DevDesc d, PagedArgs a, PromptOut po, int splits) {
   const int lane = threadIdx.x & 63;
-  const long long at = (long long)blockIdx.x * 4 + (threadIdx.x >> 6);
+  const long long at = (long long)blockIdx.x * 4 + uniform((int)(threadIdx.x >> 6));
   const long long all = (long long)a.n_rows * d.Hq;
   if (at >= all || seq_of_row(a.q_start, d.B, (int)(at / d.Hq)) < 0) return;
   const float NEG_INF = -__builtin_inff();
-  float m = NEG_INF;
-  for (int s = 0; s < splits; ++s) m = fmaxf(m, po.part_ml[2 * (s * all + at)]);
-  float l = 0.f, x = 0.f, y = 0.f;
-  for (int s = 0; s < splits; ++s) {
-    const float pm = po.part_ml[2 * (s * all + at)];
-    if (pm == NEG_INF) continue;
-    const float f = exp2_(pm - m);
-    const float2 v = *reinterpret_cast<const float2*>(po.part_o + (s * all + at) * D + 2 * lane);
-    l = fmaf(f, po.part_ml[2 * (s * all + at) + 1], l);
-    x = fmaf(f, v.x, x);
-    y = fmaf(f, v.y, y);
+  float m = NEG_INF, l = 0.f, x = 0.f, y = 0.f;
+  for (int s0 = 0; s0 < splits; s0 += 8) {
+    float2 ml[8], v[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const long long slot = min(s0 + e, splits - 1) * all + at;
+      ml[e] = *reinterpret_cast<const float2*>(po.part_ml + 2 * slot);
+      v[e] = *reinterpret_cast<const float2*>(po.part_o + slot * D + 2 * lane);
+      if (s0 + e >= splits) ml[e].x = NEG_INF;
+    }
+    float mn = m;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) mn = fmaxf(mn, ml[e].x);
+    if (mn == NEG_INF) continue;
+    const float f = exp2_(m - mn);
+    l *= f;
+    x *= f;
+    y *= f;
+    m = mn;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const bool some = ml[e].x != NEG_INF;       // (a part that saw nothing may hold anything)
+      const float w = exp2_(ml[e].x - m);
+      l = fmaf(w, some ? ml[e].y : 0.f, l);
+      x = fmaf(w, some ? v[e].x : 0.f, x);
+      y = fmaf(w, some ? v[e].y : 0.f, y);
+    }
   }
   const float inv = m == NEG_INF ? 0.f : 1.f / l;
   const bf16x2_t r = __builtin_convertvector((f32x2_t{x * inv, y * inv}), bf16x2_t);
@@ -506,10 +525,10 @@ hipError_t launch_prompt_bf16(const DevDesc& d, const PagedArgs& a, const Prompt
   po.lse = a.scores ? (float*)(base + p.off_lse) : nullptr;
   po.part_o = p.splits > 1 ? (float*)(base + p.off_o) : nullptr;
   po.part_ml = p.splits > 1 ? (float*)(base + p.off_ml) : nullptr;
-  const dim3 grid((unsigned)(col_tiles_most(a.n_rows, d.B, d.G, FP_COLS) * d.Hkv), p.splits), block(64 * FP_WAVES);
+  const dim3 grid((unsigned)(col_tiles_most(a.n_rows, d.B, d.G, FP_COLS) * d.Hkv * p.splits)), block(64 * FP_WAVES);
   auto launch = [&](auto rows) {
-    if (p.splits > 1) hipLaunchKernelGGL((prompt_bf16_kernel<decltype(rows)::value, true>), grid, block, FP_LDS, st, d, a, po);
-    else hipLaunchKernelGGL((prompt_bf16_kernel<decltype(rows)::value, false>), grid, block, FP_LDS, st, d, a, po);
+    if (p.splits > 1) hipLaunchKernelGGL((prompt_bf16_kernel<decltype(rows)::value, true>), grid, block, FP_LDS, st, d, a, po, p.splits);
+    else hipLaunchKernelGGL((prompt_bf16_kernel<decltype(rows)::value, false>), grid, block, FP_LDS, st, d, a, po, p.splits);
   };
   if (a.pages.table == nullptr || a.pages.page_size % FP_KEYS == 0) launch(std::integral_constant<int, IN_ONE_PAGE>{});
   else if (a.pages.page_size % 8 == 0) launch(std::integral_constant<int, EIGHT_A_PAGE>{});
