@@ -448,7 +448,7 @@ static int32_t check_pages(const kvr_desc* desc, const kvr_pages* pages, kvr::De
 constexpr int MAX_ROWS_NEW = 1 << 27;
 
 static int32_t check_rows(const kvr_desc* desc, int32_t n_rows, const int32_t* q_start) {
-  if (n_rows < 0 || n_rows > MAX_ROWS_NEW) return KVR_ERR_INVALID_ARG;
+  if (n_rows < 0 || n_rows > MAX_ROWS_NEW || (long long)n_rows * desc->n_q_heads > 0x7fffffffll) return KVR_ERR_INVALID_ARG;
   if (q_start == nullptr && n_rows != desc->batch) return KVR_ERR_INVALID_ARG;
   return KVR_OK;
 }
@@ -547,7 +547,8 @@ int32_t kvr_attend_prompt_workspace_size(const kvr_desc* desc, int32_t n_rows, c
   if (rc == KVR_OK) rc = pages_size(desc, pages, p);
   if (rc == KVR_OK) rc = check_visible(window, n_sink, vis);
   if (rc != KVR_OK) return rc;
-  if (bytes == nullptr || n_rows < 0 || n_rows > MAX_ROWS_NEW) return KVR_ERR_INVALID_ARG;
+  if (bytes == nullptr || n_rows < 0 || n_rows > MAX_ROWS_NEW || (long long)n_rows * d.Hq > 0x7fffffffll)
+    return KVR_ERR_INVALID_ARG;
   if (!kvr::attend_paged_fits(d, p.cap, kvr::Visible{0, 0})) return KVR_ERR_UNSUPPORTED;
   *bytes = n_rows == 0 ? 0 : kvr::attend_prompt_ws(d, desc->dtype, n_rows, p.cap, vis, scores != 0);
   return KVR_OK;

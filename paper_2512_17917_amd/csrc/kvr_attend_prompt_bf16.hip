@@ -33,6 +33,20 @@ constexpr int FP_BUFS = 4;
 constexpr int FP_LDS = 2 * FP_BUFS * FP_TILE + 2 * FP_BUFS * FP_WAVES;
 constexpr float KEEP_MAX = 8.f;
 
+// Into how many parts the tokens of a tile of columns are split, at most `most`: as many as make the rounds of 256 workgroups
+// (one a CU) times a part's length shortest, four tiles' time being what a workgroup costs besides.
+__device__ __forceinline__ int split_count(const DevDesc& d, const PagedArgs& a, int most) {
+  const TileCount c = count_tiles(a.q_start, a.n_ctx, a.n_rows, d.B, d.G, FP_COLS, a.pages.cap);
+  int keys = c.longest;
+  if (a.vis.window > 0) keys = min((long long)keys, (long long)a.vis.window + a.vis.n_sink + FP_COLS);
+  const int tiles = (keys + FP_KEYS - 1) / FP_KEYS, s = (threadIdx.x & 63) + 1;
+  const long long rounds = ((long long)c.tiles * d.Hkv * s + 255) / 256;
+  const long long cost = rounds * ((tiles + s - 1) / s + 4);
+  const int mine = s <= most && cost < (1ll << 24) ? (int)(cost << 6) + s - 1 : 0x7fffffff;
+  const int best = wave_reduce(mine, [](int x, int y) { return x < y ? x : y; });
+  return best == 0x7fffffff ? 1 : (best & 63) + 1;
+}
+
 struct PromptOut {
   void* out;
   float* lse;              // per row and head: maximum plus logarithm of the sum, in powers of two; or null
@@ -45,7 +59,7 @@ struct PromptOut {
 enum { IN_ONE_PAGE, EIGHT_A_PAGE, ANYWHERE };
 
 template <int ROWS, bool SPLIT>
-__global__ __launch_bounds__(64 * FP_WAVES, 2) void prompt_bf16_kernel(DevDesc d, PagedArgs a, PromptOut po, int splits) {
+__global__ __launch_bounds__(64 * FP_WAVES, 2) void prompt_bf16_kernel(DevDesc d, PagedArgs a, PromptOut po, int most_splits) {
   extern __shared__ __align__(1024) unsigned char s_mem[];
   unsigned char* s_k = s_mem;                                   // [4][64][256]
   unsigned char* s_v = s_k + FP_BUFS * FP_TILE;                 // [4][64][256]
@@ -58,6 +72,7 @@ __global__ __launch_bounds__(64 * FP_WAVES, 2) void prompt_bf16_kernel(DevDesc d
   // Heads next to each other in the grid (neighbours go to the chip's dies in turn, so that a die's L2 holds few heads), then the
   // parts of a tile, then tiles: those that turn out not to be there come last, where they take no compute unit's turn.
   const int order = uniform((int)(blockIdx.x / (unsigned)d.Hkv)), hk = (int)(blockIdx.x - (unsigned)order * d.Hkv);
+  const int splits = SPLIT ? split_count(d, a, most_splits) : 1;
   const int tile = SPLIT ? uniform(order / splits) : order, split = SPLIT ? order - tile * splits : 0;
   const int gs = __builtin_ctz(d.G);                            // G is a power of two
   const ColTile ct = col_tile(a.q_start, a.n_rows, d.B, d.G, FP_COLS, tile);
@@ -67,7 +82,8 @@ __global__ __launch_bounds__(64 * FP_WAVES, 2) void prompt_bf16_kernel(DevDesc d
   const int n = clampi(listed(a.n_ctx + b), 0, a.pages.cap);
   const int first = n - span.n;
   const int cols = span.n * d.G;
-  // the last columns, which see most, go first
+  // A sequence's last columns, which see most, go first.  (Sequences stay one after another: taking the last tiles of all of
+  // them first was 2 % slower over 2 x 8k, their keys and values do not fit an L2 together.)
   const int m0 = ((cols + FP_COLS - 1) / FP_COLS - 1) * FP_COLS - uniform(ct.m0);
   const int mw = m0 + 32 * wave;
   const bool wave_live = mw < cols;
@@ -413,7 +429,7 @@ __global__ __launch_bounds__(64 * FP_WAVES, 2) void prompt_bf16_kernel(DevDesc d
   }
   l_run = across_sum(l_run);
   if (!live) return;
-  if (SPLIT) {
+  if (SPLIT && splits > 1) {
     const size_t slot = (size_t)split * a.n_rows * d.Hq + at;
     float* op = po.part_o + slot * D;
 #pragma unroll
@@ -441,8 +457,10 @@ __global__ __launch_bounds__(64 * FP_WAVES, 2) void prompt_bf16_kernel(DevDesc d
 }
 
 // Joins the parts of a row and head: a wave each, lane l channels 2 l and 2 l + 1; eight parts' numbers are asked for at once.
-__global__ __launch_bounds__(256) void prompt_join_kernel(DevDesc d, PagedArgs a, PromptOut po, int splits) {
+__global__ __launch_bounds__(256) void prompt_join_kernel(DevDesc d, PagedArgs a, PromptOut po, int most_splits) {
   const int lane = threadIdx.x & 63;
+  const int splits = split_count(d, a, most_splits);
+  if (splits == 1) return;                        // written where it was computed
   const long long at = (long long)blockIdx.x * 4 + uniform((int)(threadIdx.x >> 6));
   const long long all = (long long)a.n_rows * d.Hq;
   if (at >= all || seq_of_row(a.q_start, d.B, (int)(at / d.Hq)) < 0) return;
@@ -485,17 +503,18 @@ __global__ __launch_bounds__(256) void prompt_join_kernel(DevDesc d, PagedArgs a
 
 PromptPlan prompt_bf16_plan(const DevDesc& d, long long n_rows, long long cap, const Visible& vis, bool scores) {
   PromptPlan p = {};
-  const long long tiles = col_tiles_most(n_rows, d.B, d.G, FP_COLS) * d.Hkv;
   long long keys = cap;
   if (vis.window > 0) {
-    const long long some = (long long)vis.window + FP_COLS / d.G + vis.n_sink + 2 * FP_KEYS;
+    const long long some = (long long)vis.window + vis.n_sink + FP_COLS;
     keys = some < keys ? some : keys;
   }
-  // few columns: the tokens of a tile of columns to several workgroups, up to two for each CU, 512 tokens each at least
+  // Fewer tiles of columns than CUs: the tokens of a tile to several workgroups (the device knows how many tiles there are),
+  // 512 tokens each at least, up to two workgroups for each CU.
+  const long long tiles = (n_rows * d.G + FP_COLS - 1) / FP_COLS * d.Hkv;
   long long s = tiles < 256 ? 512 / tiles : 1;
   const long long most = keys / 512;
   s = s < most ? s : most;
-  p.splits = (int)(s < 1 ? 1 : s);
+  p.splits = (int)(s < 1 ? 1 : s > 64 ? 64 : s);
   auto whole = [](size_t x) { return (x + 255) & ~(size_t)255; };
   const size_t heads = (size_t)n_rows * d.Hq;
   p.off_lse = 0;

@@ -122,6 +122,27 @@ constexpr long long col_tiles_most(long long n_rows, int B, int G, int per) {
   return (n_rows * G + per - 1) / per + B;
 }
 
+template <typename F>
+__device__ __forceinline__ int wave_reduce(int x, F f) {
+#pragma unroll
+  for (int k = 1; k < 64; k <<= 1) x = f(x, __shfl_xor(x, k));
+  return uniform(x);
+}
+// Number of those tiles, and tokens of the longest sequence that has any.
+struct TileCount {
+  int tiles, longest;
+};
+__device__ __forceinline__ TileCount count_tiles(const int32_t* q_start, const int32_t* n_ctx, int n_rows, int B, int G, int per, int cap) {
+  const int lane = threadIdx.x & 63;
+  int tiles = 0, longest = 0;
+  for (int b = lane; b < B; b += 64) {
+    const int n = row_span(q_start, n_rows, b).n;
+    tiles += (int)(((long long)n * G + per - 1) / per);
+    if (n > 0) longest = max(longest, clampi(listed(n_ctx + b), 0, cap));
+  }
+  return {wave_reduce(tiles, [](int x, int y) { return x + y; }), wave_reduce(longest, [](int x, int y) { return x > y ? x : y; })};
+}
+
 // Which tokens a query at position P sees: j <= P, and j > P - window or j < n_sink where there is a window.
 struct Visible {
   int window, n_sink;               // window 0: none
