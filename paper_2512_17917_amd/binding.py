@@ -6,8 +6,8 @@ pointers, checks dtype / device / contiguity / minimum size, and passes
 `data_ptr()` plus the current torch HIP stream.  Nothing is computed here.
 There is no fallback: if the library is missing, loading raises.
 
-The two calls of a decode step (`kvr_step_update`, `kvr_attend_decode`) are
-checked and made by the extension `_kvr_fast` (csrc/kvr_fast.c), where it was built
+The calls of a decode step (`kvr_step_update`, `kvr_attend_decode`; over an
+uncompressed cache `kvr_rotate`, `kvr_attend_paged`) are checked and made by the extension `_kvr_fast` (csrc/kvr_fast.c), where it was built
 and every argument is as it should be; anything else comes back to the checks here,
 which raise.
 """
@@ -201,7 +201,7 @@ def lib() -> C.CDLL:
 
 
 def _load_fast(L):
-    """The two calls of a decode step make some thirty tensor checks, 0.75 us each in Python; _kvr_fast makes the same
+    """The calls of a decode step make some thirty tensor checks, 0.75 us each in Python; _kvr_fast makes the same
     checks in C and hands back None where one fails, so that the Python code below says what is wrong."""
     global _fast
     if os.path.exists(FAST_PATH):
@@ -211,6 +211,7 @@ def _load_fast(L):
         address = lambda f: C.cast(f, C.c_void_p).value
         m.setup(address(L.kvr_step_update), address(L.kvr_attend_decode), torch.float32, torch.bfloat16, torch.int32,
                 torch.uint8, torch.Tensor)
+        m.setup_cache(address(L.kvr_rotate), address(L.kvr_attend_paged))
         _fast = m
 
 
@@ -515,6 +516,7 @@ def make_pages(desc, k, v, table=None):
             raise ValueError("table must be a tensor [batch, table_cap]")
         p.table, p.table_cap = _ptr(table, torch.int32, 1, "table"), table.shape[1]
     p.tensors = (k, v, table)
+    p.fits = (desc.dtype, desc.n_kv_heads, desc.head_dim, k.shape[0] if table is None else table.shape[0])
     return p
 
 
@@ -522,11 +524,10 @@ def _pages(desc, p, allow_none=False):
     """A kvr_pages of make_pages that fits this descriptor (it may have been made with another one)."""
     if p is None and allow_none:
         return None
-    if not isinstance(p, kvr_pages) or not hasattr(p, "tensors"):
+    if not isinstance(p, kvr_pages) or not hasattr(p, "fits"):
         raise TypeError("pages must come from make_pages")
-    k, v, table = p.tensors
-    if k.dtype != _torch_dtype(desc) or k.shape[1] != desc.n_kv_heads or (
-            table.shape[0] if table is not None else k.shape[0]) < desc.batch:
+    dtype, heads, dim, rows = p.fits
+    if dtype != desc.dtype or heads != desc.n_kv_heads or dim != desc.head_dim or rows < desc.batch:
         raise ValueError("pages were made for another kind of descriptor")
     return C.byref(p)
 
@@ -562,6 +563,14 @@ def _rows(t, dtype, n_rows, heads, d, name):
 
 def kvr_rotate(desc, rot, q, k, v, n_rows, q_start, n_ctx, q_out, k_out=None, pages=None):
     """As the C call; the rows' strides are the tensors' own."""
+    pp = _pages(desc, pages, True)
+    lib()
+    one = q if q is not None else k
+    if _fast is not None and isinstance(desc, kvr_desc) and isinstance(rot, kvr_rotation) and isinstance(one, torch.Tensor) and one.is_cuda:
+        rc = _fast.rotate(C.addressof(desc), C.addressof(rot), C.addressof(pages) if pages is not None else 0,
+                          torch.cuda.current_device(), _stream(), q, k, v, n_rows, q_start, n_ctx, q_out, k_out)
+        if rc is not None:
+            return _check("kvr_rotate", rc)
     dt, d = _torch_dtype(desc), desc.head_dim
     if not isinstance(rot, kvr_rotation):
         raise TypeError("rot must come from make_rotation")
@@ -573,7 +582,7 @@ def kvr_rotate(desc, rot, q, k, v, n_rows, q_start, n_ctx, q_out, k_out=None, pa
         C.byref(desc), C.byref(rot), qp, qs, kp, ks, vp, vs, n_rows,
         _ptr(q_start, torch.int32, desc.batch + 1, "q_start", True), _ptr(n_ctx, torch.int32, desc.batch, "n_ctx"),
         _ptr(q_out, dt, n_rows * desc.n_q_heads * d, "q_out", True),
-        _ptr(k_out, dt, n_rows * desc.n_kv_heads * d, "k_out", True), _pages(desc, pages, True), _stream())
+        _ptr(k_out, dt, n_rows * desc.n_kv_heads * d, "k_out", True), pp, _stream())
     _check("kvr_rotate", rc)
 
 
@@ -605,12 +614,19 @@ def kvr_attend_paged_workspace_size(desc, pages, window, n_sink, scores) -> int:
 
 
 def kvr_attend_paged(desc, q, n_ctx, pages, window, n_sink, out, scores, n_cap, ws):
+    pp = _pages(desc, pages)
+    lib()
+    if _fast is not None and isinstance(desc, kvr_desc) and isinstance(q, torch.Tensor) and q.is_cuda:
+        rc = _fast.attend_paged(C.addressof(desc), C.addressof(pages), torch.cuda.current_device(), _stream(), q, n_ctx, window,
+                                n_sink, out, scores, n_cap, ws)
+        if rc is not None:
+            return _check("kvr_attend_paged", rc)
     U, dt = desc.batch * desc.n_kv_heads, _torch_dtype(desc)
     row = desc.batch * desc.n_q_heads * desc.head_dim
     wp, wb = _ws(ws)
     _here(q, n_ctx, out, scores, ws)
     rc = lib().kvr_attend_paged(
-        C.byref(desc), _ptr(q, dt, row, "q"), _ptr(n_ctx, torch.int32, desc.batch, "n_ctx"), _pages(desc, pages),
+        C.byref(desc), _ptr(q, dt, row, "q"), _ptr(n_ctx, torch.int32, desc.batch, "n_ctx"), pp,
         window, n_sink, _ptr(out, dt, row, "out"), _ptr(scores, torch.float32, U * n_cap, "scores", True), n_cap,
         wp, wb, _stream())
     _check("kvr_attend_paged", rc)

@@ -1,4 +1,5 @@
-/* The two calls of a decode step without the interpreter between the checks: the same checks of every tensor that
+/* The calls of a decode step (the compressed cache's two, and those that put a token into an uncompressed cache and attend
+ * over it) without the interpreter between the checks: the same checks of every tensor that
  * binding._ptr makes (that it is one, type, place, contiguity, size), made through the tensor's own attributes, and the call itself.  A
  * check that fails, or an argument of an unexpected kind, returns None: the caller then takes the Python path, which
  * says what is wrong.  Nothing is kept between calls but the names, the types and the two entry points. */
@@ -15,6 +16,14 @@ typedef int32_t (*attend_fn)(const kvr_desc*, const void*, const void*, const vo
                              const void*, const void*, const int32_t*, const int32_t*, int32_t, float*, float*, int64_t,
                              void*, size_t, const kvr_attend_opts*, void*);
 
+typedef int32_t (*rotate_fn)(const kvr_desc*, const kvr_rotation*, const void*, int64_t, const void*, int64_t, const void*, int64_t,
+                             int32_t, const int32_t*, const int32_t*, void*, void*, const kvr_pages*, void*);
+typedef int32_t (*paged_fn)(const kvr_desc*, const void*, const int32_t*, const kvr_pages*, int32_t, int32_t, void*, float*,
+                            int64_t, void*, size_t, void*);
+
+static PyObject *n_get_device, *n_shape, *n_stride;
+static rotate_fn f_rotate;
+static paged_fn f_paged;
 static PyObject *n_dtype, *n_is_cuda, *n_is_contiguous, *n_numel, *n_data_ptr;
 static PyObject *t_f32, *t_bf16, *t_i32, *t_u8, *t_tensor;
 static step_fn f_step;
@@ -131,9 +140,101 @@ static PyObject* attend_decode(PyObject* self, PyObject* const* a, Py_ssize_t n)
   return PyLong_FromLong(rc);
 }
 
+/* as binding._here: the tensor lives on the current device */
+static int here(PyObject* t, int64_t dev) {
+  int64_t at;
+  return t == Py_None || (asked(t, n_get_device, &at) && at == dev);
+}
+
+static int item(PyObject* seq, Py_ssize_t i, int64_t* v) {
+  return PyTuple_Check(seq) && PyTuple_GET_SIZE(seq) == 3 && integer(PyTuple_GET_ITEM(seq, i), v);
+}
+
+/* as binding._rows: device address and row stride of [n_rows or more, heads, D] with dense heads */
+static int rows(PyObject* t, PyObject* dtype, int64_t n_rows, int64_t heads, int64_t D, int64_t dev, void** p, int64_t* stride) {
+  int64_t n0, n1, n2, s0, s1, s2, a;
+  *p = NULL;
+  *stride = 0;
+  if (t == Py_None) return 1;
+  if (PyObject_IsInstance(t, t_tensor) != 1) return 0;
+  PyObject* dt = PyObject_GetAttr(t, n_dtype);
+  const int same = dt == dtype;
+  Py_XDECREF(dt);
+  if (!same || !truth(PyObject_GetAttr(t, n_is_cuda)) || !here(t, dev)) return 0;
+  PyObject* shape = PyObject_GetAttr(t, n_shape);
+  int ok = shape && item(shape, 0, &n0) && item(shape, 1, &n1) && item(shape, 2, &n2);
+  Py_XDECREF(shape);
+  if (!ok || n0 < n_rows || n1 != heads || n2 != D) return 0;
+  PyObject* strides = PyObject_CallMethodNoArgs(t, n_stride);
+  ok = strides && item(strides, 0, &s0) && item(strides, 1, &s1) && item(strides, 2, &s2);
+  Py_XDECREF(strides);
+  if (!ok || s2 != 1 || (heads > 1 && s1 != D) || !asked(t, n_data_ptr, &a)) return 0;
+  *p = (void*)(uintptr_t)a;
+  *stride = n_rows > 1 ? s0 : heads * D;
+  return 1;
+}
+
+static PyObject* setup_cache(PyObject* self, PyObject* const* a, Py_ssize_t n) {
+  int64_t r, p;
+  if (n != 2 || !integer(a[0], &r) || !integer(a[1], &p)) return PyErr_Format(PyExc_TypeError, "setup_cache");
+  f_rotate = (rotate_fn)(uintptr_t)r;
+  f_paged = (paged_fn)(uintptr_t)p;
+  Py_RETURN_NONE;
+}
+
+/* addresses of desc, rotation and pages (0: none), current device, stream, then binding.kvr_rotate's arguments from q to k_out */
+static PyObject* rotate(PyObject* self, PyObject* const* a, Py_ssize_t n) {
+  int64_t da, ra, pa, dev, st, n_rows, qs, ks, vs;
+  void *q, *k, *v, *start, *nc, *qo, *ko;
+  if (n != 13 || !f_rotate || !integer(a[0], &da) || !integer(a[1], &ra) || !integer(a[2], &pa) || !integer(a[3], &dev) ||
+      !integer(a[4], &st) || !integer(a[8], &n_rows))
+    return refuse();
+  const kvr_desc* d = (const kvr_desc*)(uintptr_t)da;
+  if (!sizes_fit(d, (int64_t[]){n_rows}, 1) || n_rows < 0) return refuse();
+  PyObject* dt = d->dtype == KVR_F32 ? t_f32 : t_bf16;
+  const int64_t D = d->head_dim, Hq = d->n_q_heads, Hkv = d->n_kv_heads;
+  if (!rows(a[5], dt, n_rows, Hq, D, dev, &q, &qs) || !rows(a[6], dt, n_rows, Hkv, D, dev, &k, &ks) ||
+      !rows(a[7], dt, n_rows, Hkv, D, dev, &v, &vs) || !tensor(a[9], t_i32, d->batch + 1, 1, &start, 0) ||
+      !tensor(a[10], t_i32, d->batch, 0, &nc, 0) || !tensor(a[11], dt, n_rows * Hq * D, 1, &qo, 0) ||
+      !tensor(a[12], dt, n_rows * Hkv * D, 1, &ko, 0) || !here(a[9], dev) || !here(a[10], dev) || !here(a[11], dev) || !here(a[12], dev))
+    return refuse();
+  int32_t rc;
+  Py_BEGIN_ALLOW_THREADS
+  rc = f_rotate(d, (const kvr_rotation*)(uintptr_t)ra, q, qs, k, ks, v, vs, (int32_t)n_rows, start, nc, qo, ko,
+                (const kvr_pages*)(uintptr_t)pa, (void*)(uintptr_t)st);
+  Py_END_ALLOW_THREADS
+  return PyLong_FromLong(rc);
+}
+
+/* addresses of desc and pages, current device, stream, then binding.kvr_attend_paged's arguments without pages */
+static PyObject* attend_paged(PyObject* self, PyObject* const* a, Py_ssize_t n) {
+  int64_t da, pa, dev, st, window, n_sink, n_cap, wb = 0;
+  void *q, *nc, *out, *sc, *ws;
+  if (n != 12 || !f_paged || !integer(a[0], &da) || !integer(a[1], &pa) || !integer(a[2], &dev) || !integer(a[3], &st) ||
+      !integer(a[6], &window) || !integer(a[7], &n_sink) || !integer(a[10], &n_cap))
+    return refuse();
+  const kvr_desc* d = (const kvr_desc*)(uintptr_t)da;
+  if (!sizes_fit(d, (int64_t[]){window, n_sink, n_cap}, 3)) return refuse();
+  PyObject* dt = d->dtype == KVR_F32 ? t_f32 : t_bf16;
+  const int64_t U = (int64_t)d->batch * d->n_kv_heads, H = (int64_t)d->batch * d->n_q_heads, D = d->head_dim;
+  if (!tensor(a[4], dt, H * D, 0, &q, 0) || !tensor(a[5], t_i32, d->batch, 0, &nc, 0) || !tensor(a[8], dt, H * D, 0, &out, 0) ||
+      !tensor(a[9], t_f32, U * n_cap, 1, &sc, 0) || !tensor(a[11], t_u8, 0, 1, &ws, &wb) || !here(a[4], dev) || !here(a[5], dev) ||
+      !here(a[8], dev) || !here(a[9], dev) || !here(a[11], dev))
+    return refuse();
+  int32_t rc;
+  Py_BEGIN_ALLOW_THREADS
+  rc = f_paged(d, q, nc, (const kvr_pages*)(uintptr_t)pa, (int32_t)window, (int32_t)n_sink, out, sc, n_cap, ws, (size_t)wb,
+               (void*)(uintptr_t)st);
+  Py_END_ALLOW_THREADS
+  return PyLong_FromLong(rc);
+}
+
 static PyMethodDef methods[] = {{"setup", (PyCFunction)(void*)setup, METH_FASTCALL, 0},
                                 {"step_update", (PyCFunction)(void*)step_update, METH_FASTCALL, 0},
                                 {"attend_decode", (PyCFunction)(void*)attend_decode, METH_FASTCALL, 0},
+                                {"setup_cache", (PyCFunction)(void*)setup_cache, METH_FASTCALL, 0},
+                                {"rotate", (PyCFunction)(void*)rotate, METH_FASTCALL, 0},
+                                {"attend_paged", (PyCFunction)(void*)attend_paged, METH_FASTCALL, 0},
                                 {0, 0, 0, 0}};
 static struct PyModuleDef module = {PyModuleDef_HEAD_INIT, "_kvr_fast", 0, -1, methods, 0, 0, 0, 0};
 
@@ -143,5 +244,8 @@ PyMODINIT_FUNC PyInit__kvr_fast(void) {
   n_is_contiguous = PyUnicode_InternFromString("is_contiguous");
   n_numel = PyUnicode_InternFromString("numel");
   n_data_ptr = PyUnicode_InternFromString("data_ptr");
+  n_get_device = PyUnicode_InternFromString("get_device");
+  n_shape = PyUnicode_InternFromString("shape");
+  n_stride = PyUnicode_InternFromString("stride");
   return PyModule_Create(&module);
 }

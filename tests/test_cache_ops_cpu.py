@@ -156,7 +156,7 @@ def test_binding_refuses_what_does_not_fit():
         kvr.make_pages(d, x[0], x[0])
     with pytest.raises(ValueError):
         kvr.make_rotation(d, torch.zeros(64, dtype=torch.float64))
-    with pytest.raises(ValueError):
+    with pytest.raises(TypeError):
         kvr.kvr_attend_paged(d, x, x, None, 0, 0, x, None, 0, None)
     with pytest.raises(TypeError):
         kvr.kvr_rotate(d, None, x, x, x, 2, None, x, x)
