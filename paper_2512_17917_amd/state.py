@@ -32,6 +32,7 @@ class LayerState:
         self.n_recent, self.k_candidate = int(n_recent), int(k_candidate)
         self.slack = int(slack)
         self.side = side
+        self.k_turned = self.q_turned = None
         # R.size after the last update; the queue itself is "the r_size newest positions"
         self.r_size = self.n_recent
         self.ret_cap, self.vague_cap, self.n_cap, self.evict_cap = int(ret_cap), int(vague_cap), int(n_cap), int(evict_cap)
@@ -116,16 +117,27 @@ class LayerState:
             raise RuntimeError(f"a unit needed {-worst} evictions but evict_cap = {self.evict_cap}, "
                                f"vague_cap = {self.vague_cap}: nothing was evicted there")
 
+    def rotate(self, k_new, q, rotation):
+        """Norm and rotation of one new token per sequence (k_new [B, Hkv, D], q [B, Hq, D] as projected; n_ctx counts
+        the token) -> the key that append takes and the query that attend takes, in buffers that the next call reuses."""
+        if self.k_turned is None:
+            self.k_turned = torch.empty(k_new.shape, dtype=self.dtype, device=self.device)
+            self.q_turned = torch.empty(q.shape, dtype=self.dtype, device=self.device)
+        kvr.kvr_rotate(self.desc, rotation, q, k_new, None, self.desc.batch, None, self.n_ctx, self.q_turned, self.k_turned)
+        return self.k_turned, self.q_turned
+
     def decode_step(self, k_new, v_new, q, *, bump_n_ctx=True, fused=None, replace_rate=None, max_swaps=4,
-                    check=False, opts=None):
-        """append -> select -> encode -> (swap loop, if replace_rate is given) ->
-        attend.  n_ctx counts the new token from here on; pass bump_n_ctx=False when
+                    check=False, opts=None, rotation=None):
+        """(rotate, if a binding.make_rotation is given) -> append -> select -> encode -> (swap loop, if replace_rate
+        is given) -> attend.  n_ctx counts the new token from here on; pass bump_n_ctx=False when
         several layers share one n_ctx tensor that the caller advances once per
         step.  fused: use kvr_step_update for the first three (default: whenever its
         size limits allow).  check: synchronise after the update and raise if a unit
         could not evict (see check_evictions)."""
         if bump_n_ctx:
             self.n_ctx += 1
+        if rotation is not None:
+            k_new, q = self.rotate(k_new, q, rotation)
         # Algorithm 3, first branch: does the Recent queue hand its overhang on to the Candidates?
         self.r_size = kvr.kvr_recent_size(self.r_size + 1, self.n_recent, self.slack)
         if fused is None:
@@ -146,10 +158,11 @@ class LayerState:
     @classmethod
     def from_prefill(cls, desc, K, V, q0, *, n_recent, k_candidate, max_new_tokens, evict_cap=None,
                      init_scores=None, ws_attend=None, ws_encode=None, n_ctx=None, timers=None, slack=0,
-                     side=None):
+                     side=None, q_prompt=None):
         """Compress a prompt's KV cache K, V [B, Hkv, N, D]: cumulative scores are
         initialised with one dense attention pass of q0 (or taken from
-        init_scores [B, Hkv, N]), the Recent and Candidate parts are kept raw and
+        init_scores [B, Hkv, N], or accumulated over the causal attention of all the prompt's
+        queries q_prompt [B, N, Hq, D], whose outputs are then info["out"]; q0 may be None), the Recent and Candidate parts are kept raw and
         moved into ret_cap = n_recent + k_candidate + slack + 1 slots, everything else
         goes into the sketch.  Returns (state, info)."""
         B, Hkv, N, D = K.shape
@@ -170,6 +183,8 @@ class LayerState:
         # 1. cumulative scores of the prompt
         if init_scores is not None:
             st.scores[:, :, :N] = init_scores
+        elif q_prompt is not None:
+            prompt_out = attend_dense_prompt(desc, q_prompt, K, V, st.n_ctx, st.scores)
         else:
             ws = kvr.alloc_workspace(desc, kvr.KVR_OP_ATTEND, N, 0, dev)
             kvr.kvr_attend_decode(desc, q0, K, V, None, N, None, None, None, None, 0, st.out, st.scores,
@@ -198,4 +213,81 @@ class LayerState:
         kvr.kvr_compact(desc, K, V, full_pos, N, ev_slot, st.n_evict, ev_cap, st.k_ret, st.v_ret, st.ret_pos,
                         ret_cap, min(st.r_size + k_candidate, N))
         info = {"evict_slot": ev_slot, "evict_pos": ev_pos, "n_evict": st.n_evict.clone()}
+        if init_scores is None and q_prompt is not None:
+            info["out"] = prompt_out
         return st, info
+
+
+def attend_dense_prompt(desc, q, K, V, n_ctx, scores=None):
+    """Causal attention of all queries q [B, N, Hq, D] of prompts of one length over their dense cache K, V
+    [B, Hkv, N, D]; scores [B, Hkv, n_cap] accumulate.  Returns out, shaped as q."""
+    B, N = q.shape[0], q.shape[1]
+    pages = kvr.make_pages(desc, K, V)
+    q_start = torch.arange(0, B * N + 1, N, dtype=torch.int32, device=q.device)
+    n = kvr.kvr_attend_prompt_workspace_size(desc, B * N, pages, 0, 0, scores is not None)
+    ws = torch.empty(max(n, 256), dtype=torch.uint8, device=q.device)
+    out = torch.empty_like(q)
+    kvr.kvr_attend_prompt(desc, q, B * N, q_start, n_ctx, pages, 0, 0, out, scores,
+                          scores.shape[2] if scores is not None else 0, ws)
+    return out
+
+
+class PagedCache:
+    """The uncompressed, paged cache of one layer and the calls over it: what a prompt fills and decode steps extend
+    until (or instead of) its compression into a LayerState."""
+
+    def __init__(self, desc, *, n_pages, page_size, table_cap, rotation=None, window=0, n_sink=0, scores=True,
+                 device="cuda", n_ctx=None, table=None):
+        """table int32 [B, table_cap] (None: made here, with no page assigned; see assign) and n_ctx int32 [B] may be
+        shared by layers; rotation: a binding.make_rotation (None: queries and keys are cached as they come);
+        scores: accumulate the weights that each token draws."""
+        B, Hkv, D = desc.batch, desc.n_kv_heads, desc.head_dim
+        self.desc, self.window, self.n_sink = desc, int(window), int(n_sink)
+        self.device = torch.device(device)
+        self.dtype = torch.float32 if desc.dtype == kvr.KVR_F32 else torch.bfloat16
+        self.rotation = kvr.make_rotation(desc) if rotation is None else rotation
+        self.k, self.v = (torch.zeros(n_pages, Hkv, page_size, D, dtype=self.dtype, device=self.device) for _ in range(2))
+        self.table = torch.full((B, table_cap), -1, dtype=torch.int32, device=self.device) if table is None else table
+        self.n_ctx = torch.zeros(B, dtype=torch.int32, device=self.device) if n_ctx is None else n_ctx
+        self.pages = kvr.make_pages(desc, self.k, self.v, self.table)
+        self.n_cap = table_cap * page_size
+        self.scores = torch.zeros(B, Hkv, self.n_cap, dtype=torch.float32, device=self.device) if scores else None
+        # one token per sequence: the buffers of every step
+        n = kvr.kvr_attend_paged_workspace_size(desc, self.pages, self.window, self.n_sink, scores)
+        self.ws = torch.empty(max(n, 256), dtype=torch.uint8, device=self.device)
+        self.q = torch.empty(B, desc.n_q_heads, D, dtype=self.dtype, device=self.device)
+        self.out = torch.empty_like(self.q)
+
+    def assign(self, b, first, pages):
+        """Pages (numbers) of sequence b from its `first`-th page on."""
+        self.table[b, first:first + len(pages)] = torch.as_tensor(pages, dtype=torch.int32, device=self.device)
+
+    def prompt(self, q, k, v, q_start):
+        """New tokens by q_start int32 [B + 1] (q [n_rows, Hq, D], k, v [n_rows, Hkv, D] as projected; n_ctx counts
+        them): into the pages, then attention over all of each sequence.  Returns out [n_rows, Hq, D]."""
+        rows = q.shape[0]
+        turned = torch.empty(rows, self.desc.n_q_heads, self.desc.head_dim, dtype=self.dtype, device=self.device)
+        kvr.kvr_rotate(self.desc, self.rotation, q, k, v, rows, q_start, self.n_ctx, turned, None, self.pages)
+        out = torch.zeros_like(turned)
+        n = kvr.kvr_attend_prompt_workspace_size(self.desc, rows, self.pages, self.window, self.n_sink, self.scores is not None)
+        ws = torch.empty(max(n, 256), dtype=torch.uint8, device=self.device)
+        kvr.kvr_attend_prompt(self.desc, turned, rows, q_start, self.n_ctx, self.pages, self.window, self.n_sink, out,
+                              self.scores, self.n_cap, ws)
+        return out
+
+    def decode_step(self, q, k, v, *, bump_n_ctx=True):
+        """One token per sequence (q [B, Hq, D], k, v [B, Hkv, D] as projected) into the pages, then its attention;
+        bump_n_ctx as in LayerState.decode_step.  Returns out [B, Hq, D], reused by the next step."""
+        if bump_n_ctx:
+            self.n_ctx += 1
+        kvr.kvr_rotate(self.desc, self.rotation, q, k, v, self.desc.batch, None, self.n_ctx, self.q, None, self.pages)
+        kvr.kvr_attend_paged(self.desc, self.q, self.n_ctx, self.pages, self.window, self.n_sink, self.out, self.scores,
+                             self.n_cap, self.ws)
+        return self.out
+
+    def dense(self, n_tokens):
+        """Keys and values of the first n_tokens of every sequence as dense caches [B, Hkv, n_tokens, D] (every sequence
+        has them all), for LayerState.from_prefill."""
+        ps = self.k.shape[2]
+        at = self.table[:, :-(-n_tokens // ps)].long()
+        return tuple(x[at].transpose(1, 2).flatten(2, 3)[:, :, :n_tokens].contiguous() for x in (self.k, self.v))
