@@ -1,13 +1,19 @@
-// Attention of a prompt's queries over the cache, and the cumulative scores that they leave.
+// Attention of a prompt's queries over the cache, and the cumulative scores that they leave: float32 storage, and the choice
+// between it and the bf16 kernels.
 //
-// For a kv head, new token t and query head g of the group are column m = t G + g.  A wave takes 16 columns and walks over
-// the tokens they see in tiles of 16 with the running maximum and sum of the softmax.  Logits as keys x columns,
-// S = K Q^T, four channels a step (v_mfma_f32_16x16x4_f32; lane l: token or column l mod 16, and of each 32 channels the
-// eight from 8 (l div 16) on, one a step); they leave lane l with tokens 4 (l div 16) + {0..3} of column l mod 16, which is
-// the operand that O^T = V^T P^T wants, one token of the four a step.  All sums in float32.
+// For a kv head, new token t and query head g of the group are column m = t G + g.  A workgroup has 16 NB columns; its four
+// waves take every fourth of the tiles of 16 tokens that some column sees, each with running maxima and sums of its own, and
+// are joined in LDS (where columns are few, walking over the tokens in turn is what takes the time).  Logits as keys x columns,
+// S = K Q^T, four channels a step (v_mfma_f32_16x16x4_f32; lane l: token or column l mod 16, and of each 32 channels the eight
+// from 8 (l div 16) on, one a step); they leave lane l with tokens 4 (l div 16) + {0..3} of column l mod 16, which is the
+// operand that O^T = V^T P^T wants, one token of the four a step.  Row i of block cb of the eight blocks of O^T is channel
+// 8 i + cb, so that a lane reads eight channels of a token side by side.  A tile's keys are asked for when the last one's are
+// used up, its values likewise.  All sums in float32.  Bound by the matrix units where columns are many (their float32 rate is
+// a sixteenth of bf16's): then two blocks of columns share the keys and values.
 //
 // Scores: sum over columns of p = exp(s - lse), lse the logarithm of the column's final sum.  A second kernel computes the
-// logits once more; a wave owns 16 tokens and walks over the columns that see them, so that the order of a sum is fixed.
+// logits once more; a workgroup owns 16 tokens, its waves take every fourth tile of columns, and the order of a sum is fixed.
+// (Logits and lse in powers of two.)
 #include "kvr_launch.h"
 
 namespace kvr {
@@ -16,202 +22,285 @@ namespace {
 
 typedef float f32x4_t __attribute__((ext_vector_type(4)));
 
+constexpr int PP_WAVES = 4;
 constexpr float LOG2E = 1.4426950408889634f;
 __device__ __forceinline__ float exp2_(float x) { return __builtin_amdgcn_exp2f(x); }
 
-constexpr int PP_COLS = 16, PP_WAVES = 4;
-
 // 32 channels of a row: 8 (lane div 16) .. +7 of each block of 32
-template <typename T>
-__device__ __forceinline__ void load_quarter(const T* row, int r, float (&o)[32]) {
-  constexpr int VEC = Store<T>::VEC;
+__device__ __forceinline__ void load_quarter(const float* row, int r, f32x4_t (&o)[8]) {
 #pragma unroll
-  for (int blk = 0; blk < 4; ++blk)
-#pragma unroll
-    for (int e = 0; e < 8; e += VEC) {
-      float x[VEC];
-      Store<T>::load16(row + 32 * blk + 8 * r + e, x);
-#pragma unroll
-      for (int i = 0; i < VEC; ++i) o[8 * blk + e + i] = x[i];
-    }
+  for (int i = 0; i < 8; ++i) o[i] = *reinterpret_cast<const f32x4_t*>(row + 32 * (i / 2) + 8 * r + 4 * (i % 2));
 }
-
-__device__ __forceinline__ f32x4_t logits16(const float (&k)[32], const float (&q)[32]) {
+__device__ __forceinline__ f32x4_t logits16(const f32x4_t (&k)[8], const f32x4_t (&q)[8]) {
   f32x4_t s = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-  for (int i = 0; i < 32; ++i) s = __builtin_amdgcn_mfma_f32_16x16x4f32(k[i], q[i], s, 0, 0, 0);
+  for (int i = 0; i < 8; ++i)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) s = __builtin_amdgcn_mfma_f32_16x16x4f32(k[i][e], q[i][e], s, 0, 0, 0);
   return s;
 }
-
 __device__ __forceinline__ bool finite(float x) { return (__float_as_uint(x) & 0x7f800000u) != 0x7f800000u; }
 
-// What a tile's tokens with a value that is not finite add to the columns that see them (their products left the matrix
-// instruction out, since 0 x inf there would reach the columns that do not see them).
-template <typename T>
-__device__ __noinline__ void add_not_finite(const T* v_pool, long long row, const f32x4_t p, unsigned seen4, int r, int col,
-                                            f32x4_t (&o)[8]) {
-#pragma unroll
-  for (int kk = 0; kk < 16; ++kk) {
-    const int from = (kk >> 2) * 16 + col;
-    const float pk = __shfl(p[kk & 3], from);
-    const bool seen = (__shfl(seen4, from) >> (kk & 3)) & 1;
-    const long long rk = __shfl(row, kk);
-    if (rk < 0 || !seen) continue;
-#pragma unroll
-    for (int cb = 0; cb < 8; ++cb)
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const float v = Store<T>::load1(v_pool + rk * D + 16 * cb + 4 * r + i);
-        if (!finite(v)) o[cb][i] = fmaf(pk, v, o[cb][i]);
-      }
-  }
-}
-
-template <typename T>
-__global__ __launch_bounds__(64 * PP_WAVES) void prompt_kernel(DevDesc d, PagedArgs a, float* lse) {
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+template <int NB>
+__global__ __launch_bounds__(64 * PP_WAVES) void prompt_f32_kernel(DevDesc d, PagedArgs a, float* lse) {
+  __shared__ __align__(16) float s_o[PP_WAVES][16][D + 4];
+  __shared__ float s_m[PP_WAVES][NB * 16], s_l[PP_WAVES][NB * 16];
+  const int lane = threadIdx.x & 63, wave = uniform((int)(threadIdx.x >> 6));
   const int r = lane >> 4, col = lane & 15;
-  const int hk = blockIdx.y;
-  const float NEG_INF = -__builtin_inff();
-  const ColTile ct = col_tile(a.q_start, a.n_rows, d.B, d.G, PP_COLS * PP_WAVES, blockIdx.x);
-  if (ct.b < 0) return;
-  const int b = ct.b;
+  const int hk = blockIdx.y, gs = __builtin_ctz(d.G);
+  const float NEG_INF = -__builtin_inff(), scale2 = d.scale * LOG2E;
+  const ColTile ct = col_tile(a.q_start, a.n_rows, d.B, d.G, 16 * NB, blockIdx.x);
+  const int b = uniform(ct.b);
+  if (b < 0) return;
   const RowSpan span = row_span(a.q_start, a.n_rows, b);
-  const int n = clampi(a.n_ctx[b], 0, a.pages.cap);
+  const int n = clampi(listed(a.n_ctx + b), 0, a.pages.cap);
   const int first = n - span.n;                       // position of the first new token
-  const long long cols = (long long)span.n * d.G;
-  const long long m0 = (long long)ct.m0 + wave * PP_COLS;
-  if (m0 >= cols) return;                             // whole waves; no barrier below
-  const long long m = m0 + col;
-  const bool live = m < cols;
-  const int t = (int)(m / d.G), g = (int)(m % d.G);
-  const int P = live ? first + t : -1;
-  const int t_last = (int)((m0 + PP_COLS <= cols ? m0 + PP_COLS - 1 : cols - 1) / d.G);
-  const int lo = first + (int)(m0 / d.G), hi = first + t_last;
+  const int cols = span.n << gs, m0 = uniform(ct.m0);
+  const int lo = first + (m0 >> gs), hi = first + ((min(m0 + 16 * NB, cols) - 1) >> gs);
   const TileRange tr = tile_range<16>(a.vis, lo, hi);
-  const float scale2 = d.scale * LOG2E;
-  const size_t at = (size_t)(span.first + (live ? t : 0)) * d.Hq + hk * d.G + g;   // this column's row of q and out
-  const T* kp = (const T*)a.pages.k;
-  const T* vp = (const T*)a.pages.v;
 
-  float q[32];
-  load_quarter((const T*)a.q + at * D, r, q);
-  f32x4_t o[8];
+  int P[NB];
+  size_t at[NB];                                      // this lane's columns: position, row of q and out
+  bool live[NB];
+  f32x4_t q[NB][8], o[NB][8];
+  float m_run[NB], l_run[NB];
 #pragma unroll
-  for (int cb = 0; cb < 8; ++cb) o[cb] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-  float m_run = NEG_INF, l_run = 0.f;
-  for (int i = 0; i < tr.n; ++i) {
-    const int j0 = tile_token<16>(tr, i);
-    const long long row = j0 + col < n ? page_row(a.pages, d.Hkv, b, hk, j0 + col) : -1;
-    const unsigned long long there = __ballot(row >= 0);
-    float k[32];
-    load_quarter(kp + (row < 0 ? 0 : row) * D, r, k);
-    const f32x4_t s4 = logits16(k, q);
-    float s[4];
-    unsigned seen4 = 0;
+  for (int nb = 0; nb < NB; ++nb) {
+    const int m = m0 + 16 * nb + col;
+    live[nb] = m < cols;
+    const int t = live[nb] ? m >> gs : 0;
+    P[nb] = live[nb] ? first + t : -1;
+    at[nb] = (size_t)(span.first + t) * d.Hq + hk * d.G + (live[nb] ? m & (d.G - 1) : 0);
+    load_quarter((const float*)a.q + at[nb] * D, r, q[nb]);
+#pragma unroll
+    for (int cb = 0; cb < 8; ++cb) o[nb][cb] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+    m_run[nb] = NEG_INF;
+    l_run[nb] = 0.f;
+  }
+  const float* kp = (const float*)a.pages.k;
+  const float* vp = (const float*)a.pages.v;
+
+  auto row_of = [&](int i) {                          // of token lane mod 16 of tile i, -1: none
+    const int j = tile_token<16>(tr, i) + col;
+    return j < n ? page_row(a.pages, d.Hkv, b, hk, j) : -1ll;
+  };
+  f32x4_t k[8], v[4][2];
+  auto load_v = [&](long long row) {
 #pragma unroll
     for (int x = 0; x < 4; ++x) {
-      const bool ok = sees(a.vis, P, j0 + 4 * r + x) && ((there >> (4 * r + x)) & 1);
-      s[x] = ok ? s4[x] * scale2 : NEG_INF;
-      seen4 |= ok ? 1u << x : 0u;
+      const float* p = vp + max(__shfl(row, 4 * r + x), 0ll) * D + 8 * col;
+      v[x][0] = *reinterpret_cast<const f32x4_t*>(p);
+      v[x][1] = *reinterpret_cast<const f32x4_t*>(p + 4);
     }
-    float mx = fmaxf(fmaxf(s[0], s[1]), fmaxf(s[2], s[3]));
-    mx = fmaxf(mx, __shfl_xor(mx, 16));
-    mx = fmaxf(mx, __shfl_xor(mx, 32));
-    const float m_new = fmaxf(m_run, mx);
-    if (__any(m_new > m_run)) {
-      const float corr = m_run == NEG_INF ? 0.f : exp2_(m_run - m_new);
-      l_run *= corr;
+  };
+  int i = wave;
+  long long row = -1, row_next = -1;
+  if (i < tr.n) {
+    row = row_of(i);
+    load_quarter(kp + max(row, 0ll) * D, r, k);
+    load_v(row);
+    if (i + PP_WAVES < tr.n) row_next = row_of(i + PP_WAVES);
+  }
+  for (; i < tr.n; i += PP_WAVES) {
+    const int j0 = tile_token<16>(tr, i);
+    const bool more = i + PP_WAVES < tr.n;
+    const unsigned long long there = __ballot(row >= 0) & 0xffffu;
+    f32x4_t s[NB];
+#pragma unroll
+    for (int nb = 0; nb < NB; ++nb) s[nb] = logits16(k, q[nb]);
+    if (more) load_quarter(kp + max(row_next, 0ll) * D, r, k);
+    const bool whole = j0 + 15 <= lo && there == 0xffffu && m0 + 16 * NB <= cols &&
+                       (a.vis.window == 0 || j0 > hi - a.vis.window || j0 + 15 < a.vis.n_sink);
+    uint32_t seen[NB];
+    bool odd = false;
+#pragma unroll
+    for (int nb = 0; nb < NB; ++nb) {
+      seen[nb] = 0xfu;
+#pragma unroll
+      for (int x = 0; x < 4; ++x) s[nb][x] *= scale2;
+    }
+    if (!whole) {
+#pragma unroll
+      for (int nb = 0; nb < NB; ++nb) {
+        seen[nb] = 0;
+#pragma unroll
+        for (int x = 0; x < 4; ++x) {
+          const bool ok = sees(a.vis, P[nb], j0 + 4 * r + x) && ((there >> (4 * r + x)) & 1);
+          s[nb][x] = ok ? s[nb][x] : NEG_INF;
+          seen[nb] |= ok ? 1u << x : 0u;
+        }
+      }
+      // 0 x inf would reach the columns that do not see such a value: it is left out here and added apart
+#pragma unroll
+      for (int x = 0; x < 4; ++x)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          const float y = v[x][e / 4][e % 4];
+          const bool dead = !((there >> (4 * r + x)) & 1);
+          odd = odd || (!dead && !finite(y));
+          v[x][e / 4][e % 4] = dead || !finite(y) ? 0.f : y;
+        }
+    }
+    f32x4_t p[NB];
+#pragma unroll
+    for (int nb = 0; nb < NB; ++nb) {
+      float mx = fmaxf(fmaxf(s[nb][0], s[nb][1]), fmaxf(s[nb][2], s[nb][3]));
+      mx = fmaxf(mx, __shfl_xor(mx, 16));
+      mx = fmaxf(mx, __shfl_xor(mx, 32));
+      const float m_new = fmaxf(m_run[nb], mx);
+      if (__any(m_new > m_run[nb])) {
+        const float corr = m_run[nb] == NEG_INF ? 0.f : exp2_(m_run[nb] - m_new);
+        l_run[nb] *= corr;
+#pragma unroll
+        for (int cb = 0; cb < 8; ++cb)
+#pragma unroll
+          for (int x = 0; x < 4; ++x) o[nb][cb][x] *= corr;
+      }
+      m_run[nb] = m_new;
+#pragma unroll
+      for (int x = 0; x < 4; ++x) {
+        p[nb][x] = (seen[nb] >> x) & 1 ? exp2_(s[nb][x] - m_new) : 0.f;
+        l_run[nb] += p[nb][x];
+      }
+    }
+#pragma unroll
+    for (int x = 0; x < 4; ++x)
 #pragma unroll
       for (int cb = 0; cb < 8; ++cb)
 #pragma unroll
-        for (int x = 0; x < 4; ++x) o[cb][x] *= corr;
-    }
-    m_run = m_new;
-    f32x4_t p;
+        for (int nb = 0; nb < NB; ++nb)
+          o[nb][cb] = __builtin_amdgcn_mfma_f32_16x16x4f32(v[x][cb / 4][cb % 4], p[nb][x], o[nb][cb], 0, 0, 0);
+    if (__any(odd)) {
+#pragma unroll 1
+      for (int kk = 0; kk < 16; ++kk) {
+        const int from = (kk >> 2) * 16 + col;
+        const long long rk = __shfl(row, kk);
+        if (rk < 0) continue;                         // (the same for all lanes)
 #pragma unroll
-    for (int x = 0; x < 4; ++x) {
-      p[x] = (seen4 >> x) & 1 ? exp2_(s[x] - m_new) : 0.f;
-      l_run += p[x];
-    }
-    bool odd = false;
+        for (int nb = 0; nb < NB; ++nb) {
+          const float mine = (kk & 3) == 0 ? p[nb][0] : (kk & 3) == 1 ? p[nb][1] : (kk & 3) == 2 ? p[nb][2] : p[nb][3];
+          const float pk = __shfl(mine, from);
+          const bool sk = (__shfl((int)seen[nb], from) >> (kk & 3)) & 1;
 #pragma unroll
-    for (int x = 0; x < 4; ++x) {
-      const long long rv = __shfl(row, 4 * r + x);
+          for (int x = 0; x < 4; ++x)
 #pragma unroll
-      for (int cb = 0; cb < 8; ++cb) {
-        float v = Store<T>::load1(vp + (rv < 0 ? 0 : rv) * D + 16 * cb + col);
-        if (rv < 0) v = 0.f;
-        if (!finite(v)) { odd = true; v = 0.f; }
-        o[cb] = __builtin_amdgcn_mfma_f32_16x16x4f32(v, p[x], o[cb], 0, 0, 0);
+            for (int cb = 0; cb < 8; ++cb) {
+              const float y = vp[rk * D + 8 * (4 * r + x) + cb];
+              if (sk && !finite(y)) o[nb][cb][x] = fmaf(pk, y, o[nb][cb][x]);
+            }
+        }
       }
     }
-    if (__any(odd)) add_not_finite(vp, row, p, seen4, r, col, o);
+    if (more) {
+      load_v(row_next);
+      row = row_next;
+      if (i + 2 * PP_WAVES < tr.n) row_next = row_of(i + 2 * PP_WAVES);
+    }
   }
-  l_run += __shfl_xor(l_run, 16);
-  l_run += __shfl_xor(l_run, 32);
-  if (!live) return;
-  const float inv = m_run == NEG_INF ? 0.f : 1.f / l_run;          // no token seen: zeros
-  T* out = (T*)a.out + at * D;
+  // the four waves together, a block of columns at a time: thread t has channels 8 (t mod 16) .. +7 of column t div 16
 #pragma unroll
-  for (int cb = 0; cb < 8; ++cb)
+  for (int nb = 0; nb < NB; ++nb) {
+    l_run[nb] += __shfl_xor(l_run[nb], 16);
+    l_run[nb] += __shfl_xor(l_run[nb], 32);
+    if (r == 0) {
+      s_m[wave][16 * nb + col] = m_run[nb];
+      s_l[wave][16 * nb + col] = l_run[nb];
+    }
+  }
 #pragma unroll
-    for (int x = 0; x < 4; ++x) Store<T>::store1(out + 16 * cb + 4 * r + x, m_run == NEG_INF ? 0.f : o[cb][x] * inv);
-  if (lse && r == 0) lse[at] = m_run == NEG_INF ? __builtin_inff() : m_run + __builtin_amdgcn_logf(l_run);
+  for (int nb = 0; nb < NB; ++nb) {
+    __syncthreads();
+#pragma unroll
+    for (int x = 0; x < 4; ++x) {
+      float* to = &s_o[wave][col][8 * (4 * r + x)];
+      *reinterpret_cast<float4*>(to) = make_float4(o[nb][0][x], o[nb][1][x], o[nb][2][x], o[nb][3][x]);
+      *reinterpret_cast<float4*>(to + 4) = make_float4(o[nb][4][x], o[nb][5][x], o[nb][6][x], o[nb][7][x]);
+    }
+    __syncthreads();
+    const int c = threadIdx.x >> 4, ch = 8 * (threadIdx.x & 15), m = m0 + 16 * nb + c;
+    if (m < cols) {
+      float mx = NEG_INF;
+#pragma unroll
+      for (int w = 0; w < PP_WAVES; ++w) mx = fmaxf(mx, s_m[w][16 * nb + c]);
+      float l = 0.f, sum[8] = {};
+#pragma unroll
+      for (int w = 0; w < PP_WAVES; ++w) {
+        const float f = s_m[w][16 * nb + c] == NEG_INF ? 0.f : exp2_(s_m[w][16 * nb + c] - mx);
+        l = fmaf(f, s_l[w][16 * nb + c], l);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) sum[e] = fmaf(f, s_o[w][c][ch + e], sum[e]);
+      }
+      const float inv = mx == NEG_INF ? 0.f : 1.f / l;          // no token seen: zeros
+      const size_t to = (size_t)(span.first + (m >> gs)) * d.Hq + hk * d.G + (m & (d.G - 1));
+      float4* out = reinterpret_cast<float4*>((float*)a.out + to * D + ch);
+      out[0] = make_float4(sum[0] * inv, sum[1] * inv, sum[2] * inv, sum[3] * inv);
+      out[1] = make_float4(sum[4] * inv, sum[5] * inv, sum[6] * inv, sum[7] * inv);
+      if (lse && ch == 0) lse[to] = mx == NEG_INF ? __builtin_inff() : mx + __builtin_amdgcn_logf(l);
+    }
+  }
 }
 
-template <typename T>
-__global__ __launch_bounds__(64 * PP_WAVES) void prompt_scores_kernel(DevDesc d, PagedArgs a, const float* lse) {
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int r = lane >> 4, col = lane & 15;
-  const int b = blockIdx.y / d.Hkv, hk = blockIdx.y % d.Hkv;
+__global__ __launch_bounds__(64 * PP_WAVES) void prompt_scores_f32_kernel(DevDesc d, PagedArgs a, const float* lse) {
+  __shared__ float s_sum[PP_WAVES][16];
+  const int lane = threadIdx.x & 63, wave = uniform((int)(threadIdx.x >> 6));
+  const int r = lane >> 4, col = lane & 15, gs = __builtin_ctz(d.G);
+  const int u = blockIdx.y, b = uniform(u / d.Hkv), hk = u - b * d.Hkv;
   const RowSpan span = row_span(a.q_start, a.n_rows, b);
-  const int n = clampi(a.n_ctx[b], 0, a.pages.cap);
+  const int n = clampi(listed(a.n_ctx + b), 0, a.pages.cap);
   const int first = n - span.n;
-  const int j0 = (blockIdx.x * PP_WAVES + wave) * 16;
+  const int j0 = blockIdx.x * 16;
   if (j0 >= n) return;
-  const long long row = j0 + col < n ? page_row(a.pages, d.Hkv, b, hk, j0 + col) : -1;
-  const unsigned long long there = __ballot(row >= 0);
-  float k[32];
-  load_quarter((const T*)a.pages.k + (row < 0 ? 0 : row) * D, r, k);
-  // tokens whose queries may see this tile
-  const long long t0 = j0 > first ? j0 - first : 0;
-  long long t1 = span.n;
-  if (a.vis.window > 0 && j0 >= a.vis.n_sink) {
-    const long long past = (long long)j0 + 15 + a.vis.window - first;
-    t1 = past < t1 ? past : t1;
-  }
   const float scale2 = d.scale * LOG2E;
+  const long long row = j0 + col < n ? page_row(a.pages, d.Hkv, b, hk, j0 + col) : -1;
+  f32x4_t k[8], q[8];
+  load_quarter((const float*)a.pages.k + max(row, 0ll) * D, r, k);
+  // new tokens of which some may see one of the tile's
+  const int t0 = max(j0 - first, 0);
+  int t1 = span.n;
+  if (a.vis.window > 0 && j0 >= a.vis.n_sink) t1 = min(t1, j0 + 15 + a.vis.window - first);
+  const int cols = t1 << gs;
+  auto column = [&](int m0) {
+    const int m = min(m0 + col, cols - 1);
+    return (size_t)(span.first + (m >> gs)) * d.Hq + hk * d.G + (m & (d.G - 1));
+  };
   float acc[4] = {0.f, 0.f, 0.f, 0.f};
-  const long long cols = t1 * d.G;
-  for (long long m0 = t0 * d.G; m0 < cols; m0 += PP_COLS) {
-    const long long m = m0 + col;
-    const bool live = m < cols;
-    const int t = (int)(m / d.G), g = (int)(m % d.G);
-    const size_t at = (size_t)(span.first + (live ? t : 0)) * d.Hq + hk * d.G + g;
-    float q[32];
-    load_quarter((const T*)a.q + at * D, r, q);
-    const float lc = live ? lse[at] : 0.f;
+  int m0 = (t0 << gs) + 16 * wave;
+  float lc = 0.f;
+  if (m0 < cols) {
+    load_quarter((const float*)a.q + column(m0) * D, r, q);
+    lc = lse[column(m0)];
+  }
+  for (; m0 < cols; m0 += 16 * PP_WAVES) {
     const f32x4_t s4 = logits16(k, q);
+    const float l0 = lc;
+    if (m0 + 16 * PP_WAVES < cols) {
+      load_quarter((const float*)a.q + column(m0 + 16 * PP_WAVES) * D, r, q);
+      lc = lse[column(m0 + 16 * PP_WAVES)];
+    }
+    const int m = m0 + col, P = m < cols ? first + (m >> gs) : -1;
 #pragma unroll
-    for (int x = 0; x < 4; ++x)
-      acc[x] += live && sees(a.vis, first + t, j0 + 4 * r + x) ? exp2_(s4[x] * scale2 - lc) : 0.f;
+    for (int x = 0; x < 4; ++x) acc[x] += sees(a.vis, P, j0 + 4 * r + x) ? exp2_(s4[x] * scale2 - l0) : 0.f;
   }
 #pragma unroll
   for (int x = 0; x < 4; ++x) {
 #pragma unroll
-    for (int k2 = 1; k2 < 16; k2 <<= 1) acc[x] += __shfl_xor(acc[x], k2);
-    const int j = j0 + 4 * r + x;
-    if (col == 0 && j < n && j < a.n_cap && ((there >> (4 * r + x)) & 1))
-      a.scores[((size_t)b * d.Hkv + hk) * a.n_cap + j] += acc[x];
+    for (int z = 1; z < 16; z <<= 1) acc[x] += __shfl_xor(acc[x], z);
+    if (col == 0) s_sum[wave][4 * r + x] = acc[x];
+  }
+  __syncthreads();
+  const int j = j0 + lane;
+  if (wave == 0 && lane < 16 && j < n && j < a.n_cap && row >= 0) {
+    float sum = 0.f;
+#pragma unroll
+    for (int w = 0; w < PP_WAVES; ++w) sum += s_sum[w][lane];
+    if (sum != 0.f) a.scores[(size_t)u * a.n_cap + j] += sum;
   }
 }
 
-template <typename T>
-hipError_t launch_scores(const DevDesc& d, const PagedArgs& a, const float* lse, hipStream_t st) {
-  const long long most = a.n_cap < a.pages.cap ? a.n_cap : a.pages.cap;
-  const dim3 grid((unsigned)((most + 16 * PP_WAVES - 1) / (16 * PP_WAVES)), d.B * d.Hkv);
-  hipLaunchKernelGGL((prompt_scores_kernel<T>), grid, dim3(64 * PP_WAVES), 0, st, d, a, lse);
+template <int NB>
+hipError_t launch_f32(const DevDesc& d, const PagedArgs& a, float* lse, hipStream_t st) {
+  const dim3 grid((unsigned)col_tiles_most(a.n_rows, d.B, d.G, 16 * NB), d.Hkv);
+  hipLaunchKernelGGL((prompt_f32_kernel<NB>), grid, dim3(64 * PP_WAVES), 0, st, d, a, lse);
   return hipGetLastError();
 }
 
@@ -231,11 +320,13 @@ hipError_t launch_attend_prompt(const DevDesc& d, int dtype, const PagedArgs& a,
     return launch_prompt_scores_bf16(d, a, p.scores, (const float*)(base + p.off_lse), (float*)(base + p.off_scores), st);
   }
   float* lse = a.scores ? (float*)a.ws : nullptr;
-  const dim3 grid((unsigned)col_tiles_most(a.n_rows, d.B, d.G, PP_COLS * PP_WAVES), d.Hkv);
-  hipLaunchKernelGGL((prompt_kernel<float>), grid, dim3(64 * PP_WAVES), 0, st, d, a, lse);
-  const hipError_t e = hipGetLastError();
+  // two blocks of columns a workgroup once that leaves two workgroups for each CU
+  const bool wide = (long long)a.n_rows * d.Hq >= 512 * 32;
+  const hipError_t e = wide ? launch_f32<2>(d, a, lse, st) : launch_f32<1>(d, a, lse, st);
   if (e != hipSuccess || a.scores == nullptr) return e;
-  return launch_scores<float>(d, a, lse, st);
+  const long long most = a.n_cap < a.pages.cap ? a.n_cap : a.pages.cap;
+  hipLaunchKernelGGL(prompt_scores_f32_kernel, dim3((unsigned)((most + 15) / 16), d.B * d.Hkv), dim3(64 * PP_WAVES), 0, st, d, a, lse);
+  return hipGetLastError();
 }
 
 }  // namespace kvr
