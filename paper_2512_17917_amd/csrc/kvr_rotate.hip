@@ -9,7 +9,8 @@
 //
 // A wave takes one row.  Its 64 lanes compute the row's at most 64 angles, one each, hand them round through LDS, and each
 // lane keeps the 16 numbers of its channels for all heads of the row; a head is 16 lanes (bf16) or 32 (float32) of 16 bytes.
-// Bound by HBM for many rows.  Where rows are few, a row's heads are shared out over waves.
+// The heads' 16 bytes are asked for four turns at a time.  Sums over a head, and channels half a head away, go through lane
+// rotations rather than LDS.  Bound by HBM for many rows.  Where rows are few, a row's heads are shared out over waves.
 #include "kvr_launch.h"
 #include "kvr_pages.h"
 
@@ -19,7 +20,46 @@ namespace {
 
 constexpr int ROT_WAVES = 4;
 
-enum { ROT_NEIGHBOURS, ROT_LANES, ROT_ANY };   // where a channel's partner is: next to it, whole lanes away, anywhere
+// where a channel's partner is: next to it, half a head away, whole lanes away, anywhere
+enum { ROT_NEIGHBOURS, ROT_HALF, ROT_LANES, ROT_ANY };
+constexpr int ROT_AHEAD = 4;
+
+typedef uint32_t u32x4_t __attribute__((ext_vector_type(4)));
+typedef __bf16 bf16x2_t __attribute__((ext_vector_type(2)));
+typedef float f32x2_t __attribute__((ext_vector_type(2)));
+
+template <typename T, int N> struct Widen;
+template <int N> struct Widen<bf16_t, N> {
+  __device__ static __forceinline__ void from(const u32x4_t& v, float (&o)[N]) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      o[2 * i] = __uint_as_float(v[i] << 16);
+      o[2 * i + 1] = __uint_as_float(v[i] & 0xffff0000u);
+    }
+  }
+  __device__ static __forceinline__ u32x4_t to(const float (&o)[N]) {
+    u32x4_t v;
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      v[i] = __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2_t{o[2 * i], o[2 * i + 1]}), bf16x2_t));
+    return v;
+  }
+};
+template <int N> struct Widen<float, N> {
+  __device__ static __forceinline__ void from(const u32x4_t& v, float (&o)[N]) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) o[i] = __uint_as_float(v[i]);
+  }
+  __device__ static __forceinline__ u32x4_t to(const float (&o)[N]) {
+    return u32x4_t{__float_as_uint(o[0]), __float_as_uint(o[1]), __float_as_uint(o[2]), __float_as_uint(o[3])};
+  }
+};
+
+// value of the lane N places on in the caller's 16 lanes
+template <int N>
+__device__ __forceinline__ float row_ror(float x) {
+  return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), 0x120 + N, 0xf, 0xf, true));
+}
 
 // what this wave wrote to LDS is what its lanes read from here on
 __device__ __forceinline__ void wave_sync() {
@@ -31,9 +71,18 @@ __device__ __forceinline__ void wave_sync() {
 // sum over the 16 or 32 lanes of a head
 template <int N>
 __device__ __forceinline__ float head_sum(float x) {
-#pragma unroll
-  for (int m = 1; m < N; m <<= 1) x += __shfl_xor(x, m);
+  x += row_ror<8>(x);
+  x += row_ror<4>(x);
+  x += row_ror<2>(x);
+  x += row_ror<1>(x);
+  if constexpr (N == 32) x += __shfl_xor(x, 16);
   return x;
+}
+// value of the lane half a head away
+template <int N>
+__device__ __forceinline__ float across_head(float x) {
+  if constexpr (N == 16) return row_ror<8>(x);
+  else return __shfl_xor(x, 16);
 }
 
 template <typename T, int MODE>
@@ -41,14 +90,14 @@ __global__ __launch_bounds__(64 * ROT_WAVES) void rotate_kernel(DevDesc d, Rotat
   constexpr int VEC = Store<T>::VEC, LANES = D / VEC, HEADS = 64 / LANES;   // lanes a head, heads a wave
   __shared__ float s_cs[ROT_WAVES][2][D / 2];
   __shared__ float s_x[MODE == ROT_ANY ? ROT_WAVES : 1][MODE == ROT_ANY ? HEADS * D : 1];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int lane = threadIdx.x & 63, wave = uniform((int)(threadIdx.x >> 6));
   const long long item = (long long)blockIdx.x * ROT_WAVES + wave;
-  const int row = (int)(item / a.parts), part = (int)(item % a.parts);
+  const int row = uniform((int)(item / a.parts)), part = uniform((int)(item % a.parts));
   if (row >= a.n_rows) return;                 // whole waves; no workgroup barrier below
-  const int b = seq_of_row(a.q_start, d.B, row);
+  const int b = uniform(seq_of_row(a.q_start, d.B, row));
   if (b < 0) return;
   const RowSpan span = row_span(a.q_start, a.n_rows, b);
-  const int pos = clampi(a.n_ctx[b], -(1 << 30), 0x7fffffff) - span.n + (row - span.first);
+  const int pos = clampi(listed(a.n_ctx + b), -(1 << 30), 0x7fffffff) - span.n + (row - span.first);
 
   const int c0 = (lane % LANES) * VEC;
   float cs[VEC], sn[VEC];
@@ -93,60 +142,74 @@ __global__ __launch_bounds__(64 * ROT_WAVES) void rotate_kernel(DevDesc d, Rotat
   const bool fits = a.paged && pos >= 0 && pos < a.pages.cap;
 
   const int iters = (a.n_slots + HEADS - 1) / HEADS;
-  for (int it = part; it < iters; it += a.parts) {
-    const int slot = it * HEADS + lane / LANES;
-    const bool live = slot < a.n_slots;
-    const int nq = a.q ? d.Hq : 0, nk = a.k ? d.Hkv : 0;
-    const int kind = slot < nq ? 0 : slot < nq + nk ? 1 : 2;
-    const int head = kind == 0 ? slot : kind == 1 ? slot - nq : slot - nq - nk;
-    const T* src = kind == 0 ? (const T*)a.q + row * a.q_stride
-                 : kind == 1 ? (const T*)a.k + row * a.k_stride
-                             : (const T*)a.v + row * a.v_stride;
-    float x[VEC];
-    if (live) Store<T>::load16(src + (size_t)head * D + c0, x);
-    else
+  const int nq = a.q ? d.Hq : 0, nk = a.k ? d.Hkv : 0;
+  long long place = -1;                        // of head 0's row in the pages; head h's is h page_size rows on
+  if (fits) place = page_row(a.pages, d.Hkv, b, 0, pos);
+  // head of a slot: kind 0: queries, 1: keys, 2: values
+  auto slot_of = [&](int it) { return it * HEADS + lane / LANES; };
+  for (int it0 = part; it0 < iters; it0 += a.parts * ROT_AHEAD) {
+    u32x4_t in[ROT_AHEAD];
 #pragma unroll
-      for (int i = 0; i < VEC; ++i) x[i] = 0.f;
-    float y[VEC];
-    float sq = 0.f;
+    for (int u = 0; u < ROT_AHEAD; ++u) {
+      const int slot = min(slot_of(it0 + u * a.parts), a.n_slots - 1);
+      const T* src = slot < nq        ? (const T*)a.q + row * a.q_stride + (size_t)slot * D
+                     : slot < nq + nk ? (const T*)a.k + row * a.k_stride + (size_t)(slot - nq) * D
+                                      : (const T*)a.v + row * a.v_stride + (size_t)(slot - nq - nk) * D;
+      in[u] = *reinterpret_cast<const u32x4_t*>(src + c0);
+    }
 #pragma unroll
-    for (int i = 0; i < VEC; ++i) sq = fmaf(x[i], x[i], sq);
-    sq = head_sum<LANES>(sq);
-    const bool norm = kind == 0 ? a.q_weight != nullptr : a.k_weight != nullptr;
-    const float rs = norm ? rsqrtf(sq * (1.f / D) + a.eps) : 1.f;
+    for (int u = 0; u < ROT_AHEAD; ++u) {
+      if (it0 + u * a.parts >= iters) break;
+      const int slot = slot_of(it0 + u * a.parts);
+      const bool live = slot < a.n_slots;
+      const int kind = slot < nq ? 0 : slot < nq + nk ? 1 : 2;
+      u32x4_t out = in[u];
+      if (!__all(kind == 2)) {
+        float x[VEC], y[VEC], z[VEC], o[VEC];
+        Widen<T, VEC>::from(in[u], x);
+        float sq = 0.f;
 #pragma unroll
-    for (int i = 0; i < VEC; ++i) y[i] = norm ? x[i] * rs * (kind == 0 ? wq[i] : wk[i]) : x[i];
-    float z[VEC];
-    if constexpr (MODE == ROT_NEIGHBOURS) {
+        for (int i = 0; i < VEC; ++i) sq = fmaf(x[i], x[i], sq);
+        sq = head_sum<LANES>(sq);
+        const bool norm = kind == 0 ? a.q_weight != nullptr : a.k_weight != nullptr;
+        const float rs = norm ? rsqrtf(sq * (1.f / D) + a.eps) : 1.f;
 #pragma unroll
-      for (int i = 0; i < VEC; ++i) z[i] = y[i ^ 1];
-    } else if constexpr (MODE == ROT_LANES) {
+        for (int i = 0; i < VEC; ++i) y[i] = norm ? x[i] * rs * (kind == 0 ? wq[i] : wk[i]) : x[i];
+        if constexpr (MODE == ROT_NEIGHBOURS) {
 #pragma unroll
-      for (int i = 0; i < VEC; ++i) z[i] = __shfl(y[i], partner);
-    } else {
-      float* xs = s_x[wave] + (lane / LANES) * D;
-      wave_sync();
+          for (int i = 0; i < VEC; ++i) z[i] = y[i ^ 1];
+        } else if constexpr (MODE == ROT_HALF) {
 #pragma unroll
-      for (int i = 0; i < VEC; ++i) xs[c0 + i] = y[i];
-      wave_sync();
+          for (int i = 0; i < VEC; ++i) z[i] = across_head<LANES>(y[i]);
+        } else if constexpr (MODE == ROT_LANES) {
 #pragma unroll
-      for (int i = 0; i < VEC; ++i) {
-        const int c = c0 + i;
-        z[i] = xs[c < a.half ? c + a.half : c < 2 * a.half ? c - a.half : c];
+          for (int i = 0; i < VEC; ++i) z[i] = __shfl(y[i], partner);
+        } else {
+          float* xs = s_x[wave] + (lane / LANES) * D;
+          wave_sync();
+#pragma unroll
+          for (int i = 0; i < VEC; ++i) xs[c0 + i] = y[i];
+          wave_sync();
+#pragma unroll
+          for (int i = 0; i < VEC; ++i) {
+            const int c = c0 + i;
+            z[i] = xs[c < a.half ? c + a.half : c < 2 * a.half ? c - a.half : c];
+          }
+        }
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) {
+          const float turned = fmaf(z[i], sn[i], y[i] * cs[i]);
+          o[i] = c0 + i < 2 * a.half ? turned : y[i];
+        }
+        const u32x4_t v = Widen<T, VEC>::to(o);
+        if (kind < 2) out = v;
       }
-    }
-    float o[VEC];
-#pragma unroll
-    for (int i = 0; i < VEC; ++i) {
-      const float turned = fmaf(z[i], sn[i], y[i] * cs[i]);
-      o[i] = kind == 2 ? x[i] : c0 + i < 2 * a.half ? turned : y[i];
-    }
-    if (!live) continue;
-    if (kind == 0) Store<T>::store16((T*)a.q_out + ((size_t)row * d.Hq + head) * D + c0, o);
-    if (kind == 1 && a.k_out) Store<T>::store16((T*)a.k_out + ((size_t)row * d.Hkv + head) * D + c0, o);
-    if (kind >= 1 && fits) {
-      const long long r = page_row(a.pages, d.Hkv, b, head, pos);
-      if (r >= 0) Store<T>::store16((T*)(kind == 1 ? a.pages.k : a.pages.v) + r * D + c0, o);
+      if (!live) continue;
+      const int head = kind == 0 ? slot : kind == 1 ? slot - nq : slot - nq - nk;
+      if (kind == 0) *reinterpret_cast<u32x4_t*>((T*)a.q_out + ((size_t)row * d.Hq + head) * D + c0) = out;
+      if (kind == 1 && a.k_out) *reinterpret_cast<u32x4_t*>((T*)a.k_out + ((size_t)row * d.Hkv + head) * D + c0) = out;
+      if (kind >= 1 && place >= 0)
+        *reinterpret_cast<u32x4_t*>((T*)(kind == 1 ? a.pages.k : a.pages.v) + (place + (long long)head * a.pages.page_size) * D + c0) = out;
     }
   }
 }
@@ -156,6 +219,8 @@ void launch_mode(const DevDesc& d, const RotateArgs& a, bool pairs, unsigned gri
   const dim3 block(64 * ROT_WAVES);
   if (pairs || a.half == 0)
     hipLaunchKernelGGL((rotate_kernel<T, ROT_NEIGHBOURS>), dim3(grid), block, 0, st, d, a);
+  else if (a.half == D / 2)
+    hipLaunchKernelGGL((rotate_kernel<T, ROT_HALF>), dim3(grid), block, 0, st, d, a);
   else if (a.half % Store<T>::VEC == 0)
     hipLaunchKernelGGL((rotate_kernel<T, ROT_LANES>), dim3(grid), block, 0, st, d, a);
   else
