@@ -492,7 +492,8 @@ int32_t kvr_attend_multi(const kvr_desc* desc, const void* q, int32_t n_q, const
 /*
  * Norm and rotation of the new tokens' queries and keys (see kvr_rotation) in one pass, in
  * float32 with one rounding to the storage type at the end; with `pages`, the keys and values
- * also go to their places in the cache.  A row whose position is negative or past the cache's
+ * also go to their places in the cache.  Inputs and outputs overlap only where the next lines
+ * say so.  A row whose position is negative or past the cache's
  * end is stored nowhere there.
  *   q, k, v    dev [n_rows, Hq or Hkv, D] storage type; a row's heads are dense, rows are
  *              q_stride, k_stride, v_stride elements apart (a whole number of 16 bytes, no less
@@ -521,7 +522,7 @@ int32_t kvr_rotate(const kvr_desc* desc, const kvr_rotation* rot, const void* q,
  *   q          dev [n_rows, Hq, D] storage type, read
  *   pages      host; k, v and table are read
  *   window     0: no window
- *   out        dev [n_rows, Hq, D] storage type, written
+ *   out        dev [n_rows, Hq, D] storage type, written; no part of q
  *   scores     dev float32 [B, Hkv, n_cap] read and written, or NULL; positions >= n_cap are
  *              not accumulated
  *   ws         per kvr_attend_prompt_workspace_size, with scores = whether there are scores

@@ -501,6 +501,14 @@ def _here(*tensors):
                          f"cuda:{torch.cuda.current_device()}")
 
 
+def _one_device(*tensors):
+    """Index of the device that the tensors share, None if there are none."""
+    there = {t.device.index for t in tensors if t is not None}
+    if len(there) > 1:
+        raise ValueError("the tensors live on different devices")
+    return there.pop() if there else None
+
+
 def make_pages(desc, k, v, table=None):
     """kvr_pages over the pools k, v [n_pages, Hkv, page_size, D] and table int32 [B, table_cap]; without a table the
     pools are a dense cache [B, Hkv, tokens, D].  The struct keeps the tensors."""
@@ -517,6 +525,7 @@ def make_pages(desc, k, v, table=None):
         p.table, p.table_cap = _ptr(table, torch.int32, 1, "table"), table.shape[1]
     p.tensors = (k, v, table)
     p.fits = (desc.dtype, desc.n_kv_heads, desc.head_dim, k.shape[0] if table is None else table.shape[0])
+    p.dev = _one_device(k, v, table)
     return p
 
 
@@ -529,6 +538,8 @@ def _pages(desc, p, allow_none=False):
     dtype, heads, dim, rows = p.fits
     if dtype != desc.dtype or heads != desc.n_kv_heads or dim != desc.head_dim or rows < desc.batch:
         raise ValueError("pages were made for another kind of descriptor")
+    if p.dev != torch.cuda.current_device():
+        raise ValueError(f"the pages live on cuda:{p.dev}, the current device is cuda:{torch.cuda.current_device()}")
     return C.byref(p)
 
 
@@ -541,6 +552,7 @@ def make_rotation(desc, inv_freq=None, *, q_weight=None, k_weight=None, eps=1e-6
                      _ptr(inv_freq, torch.float64, 1, "inv_freq") if n else None, eps, 2 * n,
                      KVR_ROTATE_PAIRS if pairs else KVR_ROTATE_HALVES)
     r.tensors = (inv_freq, q_weight, k_weight)
+    r.dev = _one_device(*r.tensors)
     return r
 
 
@@ -563,17 +575,19 @@ def _rows(t, dtype, n_rows, heads, d, name):
 
 def kvr_rotate(desc, rot, q, k, v, n_rows, q_start, n_ctx, q_out, k_out=None, pages=None):
     """As the C call; the rows' strides are the tensors' own."""
+    if not isinstance(rot, kvr_rotation) or not hasattr(rot, "tensors"):
+        raise TypeError("rot must come from make_rotation")
     pp = _pages(desc, pages, True)
+    if rot.dev is not None and rot.dev != torch.cuda.current_device():
+        raise ValueError(f"the rotation lives on cuda:{rot.dev}, the current device is cuda:{torch.cuda.current_device()}")
     lib()
     one = q if q is not None else k
-    if _fast is not None and isinstance(desc, kvr_desc) and isinstance(rot, kvr_rotation) and isinstance(one, torch.Tensor) and one.is_cuda:
+    if _fast is not None and isinstance(desc, kvr_desc) and isinstance(one, torch.Tensor) and one.is_cuda:
         rc = _fast.rotate(C.addressof(desc), C.addressof(rot), C.addressof(pages) if pages is not None else 0,
                           torch.cuda.current_device(), _stream(), q, k, v, n_rows, q_start, n_ctx, q_out, k_out)
         if rc is not None:
             return _check("kvr_rotate", rc)
     dt, d = _torch_dtype(desc), desc.head_dim
-    if not isinstance(rot, kvr_rotation):
-        raise TypeError("rot must come from make_rotation")
     qp, qs = _rows(q, dt, n_rows, desc.n_q_heads, d, "q")
     kp, ks = _rows(k, dt, n_rows, desc.n_kv_heads, d, "k")
     vp, vs = _rows(v, dt, n_rows, desc.n_kv_heads, d, "v")

@@ -522,7 +522,7 @@ static int32_t check_attend(const kvr_desc* desc, const void* q, const int32_t* 
                             float* scores, int64_t n_cap, kvr::PagedArgs& a) {
   const int32_t rc = check_pages(desc, pages, a.pages);
   if (rc != KVR_OK) return rc;
-  if (!q || !n_ctx || !out || !aligned16(q) || !aligned16(out)) return KVR_ERR_INVALID_ARG;
+  if (!q || !n_ctx || !out || q == out || !aligned16(q) || !aligned16(out)) return KVR_ERR_INVALID_ARG;
   if (scores != nullptr && (n_cap < 1 || n_cap > MAX_TOKENS)) return KVR_ERR_INVALID_ARG;
   a.q = q;
   a.n_ctx = n_ctx;

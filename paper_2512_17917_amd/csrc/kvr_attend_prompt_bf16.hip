@@ -527,17 +527,23 @@ PromptPlan prompt_bf16_plan(const DevDesc& d, long long n_rows, long long cap, c
 }
 
 hipError_t launch_prompt_bf16(const DevDesc& d, const PagedArgs& a, const PromptPlan& p, hipStream_t st) {
-  static std::once_flag once;
-  static hipError_t raised = hipSuccess;
-  std::call_once(once, [] {
+  // a launch may ask for more than 64 KB of LDS where the kernel's limit was raised, on each device for itself
+  constexpr int DEVICES = 64;
+  static std::once_flag once[DEVICES];
+  static hipError_t raised[DEVICES];
+  int dev = 0;
+  hipError_t e = hipGetDevice(&dev);
+  if (e != hipSuccess) return e;
+  if (dev < 0 || dev >= DEVICES) return hipErrorInvalidDevice;
+  std::call_once(once[dev], [&] {
     for (const void* f : {(const void*)prompt_bf16_kernel<IN_ONE_PAGE, false>, (const void*)prompt_bf16_kernel<IN_ONE_PAGE, true>,
                           (const void*)prompt_bf16_kernel<EIGHT_A_PAGE, false>, (const void*)prompt_bf16_kernel<EIGHT_A_PAGE, true>,
                           (const void*)prompt_bf16_kernel<ANYWHERE, false>, (const void*)prompt_bf16_kernel<ANYWHERE, true>}) {
-      const hipError_t e = hipFuncSetAttribute(f, hipFuncAttributeMaxDynamicSharedMemorySize, FP_LDS);
-      if (e != hipSuccess) raised = e;
+      const hipError_t x = hipFuncSetAttribute(f, hipFuncAttributeMaxDynamicSharedMemorySize, FP_LDS);
+      if (x != hipSuccess) raised[dev] = x;
     }
   });
-  if (raised != hipSuccess) return raised;
+  if (raised[dev] != hipSuccess) return raised[dev];
   char* base = (char*)a.ws;
   PromptOut po;
   po.out = a.out;
@@ -552,7 +558,7 @@ hipError_t launch_prompt_bf16(const DevDesc& d, const PagedArgs& a, const Prompt
   if (a.pages.table == nullptr || a.pages.page_size % FP_KEYS == 0) launch(std::integral_constant<int, IN_ONE_PAGE>{});
   else if (a.pages.page_size % 8 == 0) launch(std::integral_constant<int, EIGHT_A_PAGE>{});
   else launch(std::integral_constant<int, ANYWHERE>{});
-  const hipError_t e = hipGetLastError();
+  e = hipGetLastError();
   if (e != hipSuccess || p.splits == 1) return e;
   hipLaunchKernelGGL(prompt_join_kernel, dim3((unsigned)(((long long)a.n_rows * d.Hq + 3) / 4)), dim3(256), 0, st, d, a, po, p.splits);
   return hipGetLastError();

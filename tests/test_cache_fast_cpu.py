@@ -173,6 +173,23 @@ def test_paged_refusals(fast, case):
     assert not got
 
 
+def test_another_device_is_refused(fast, monkeypatch):
+    """Pages, weights or frequencies of one device in a call on another; tensors of two devices in one struct."""
+    m, got = fast
+    d = _desc()
+    pages, a = _pages(d), list(_paged_args().values())
+    inv = Fake(torch.float64, (64,), 0xc000)
+    rot = kvr.make_rotation(d, inv)
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 1)
+    with pytest.raises(ValueError):
+        kvr.kvr_attend_paged(d, *a[:2], pages, *a[2:])
+    with pytest.raises(ValueError):
+        kvr.kvr_rotate(d, rot, *_rotate_args().values())
+    with pytest.raises(ValueError):
+        kvr.make_rotation(d, inv, q_weight=Fake(torch.bfloat16, (128,), 1, dev=1))
+    assert not got
+
+
 def test_pages_of_another_descriptor(fast):
     d = _desc()
     pages = _pages(d)

@@ -40,14 +40,14 @@ def _rotate(desc=None, rot=None, pages=None, **kw):
 
 
 def _prompt(desc=None, over=None, **kw):
-    a = dict(q=P, n_rows=2, q_start=None, n_ctx=P, pages=C.byref(over or _pages()), window=0, n_sink=0, out=P, scores=P,
+    a = dict(q=P, n_rows=2, q_start=None, n_ctx=P, pages=C.byref(over or _pages()), window=0, n_sink=0, out=P + 16, scores=P,
              n_cap=64, ws=P, ws_bytes=0)             # too small a workspace: nothing is ever launched
     a.update(kw)
     return kvr.lib().kvr_attend_prompt(C.byref(desc or _desc()), *a.values(), None)
 
 
 def _paged(desc=None, over=None, **kw):
-    a = dict(q=P, n_ctx=P, pages=C.byref(over or _pages()), window=0, n_sink=0, out=P, scores=P, n_cap=64, ws=P, ws_bytes=0)
+    a = dict(q=P, n_ctx=P, pages=C.byref(over or _pages()), window=0, n_sink=0, out=P + 16, scores=P, n_cap=64, ws=P, ws_bytes=0)
     a.update(kw)
     return kvr.lib().kvr_attend_paged(C.byref(desc or _desc()), *a.values(), None)
 
@@ -94,7 +94,7 @@ def test_no_rows_are_no_work():
 @pytest.mark.parametrize("call", [_prompt, _paged])
 def test_bad_attention_is_refused(call):
     assert call() == W                                    # as it should be but for the workspace
-    for bad in (dict(q=None), dict(q=ODD), dict(n_ctx=None), dict(out=None), dict(out=ODD), dict(pages=None), dict(window=-1),
+    for bad in (dict(q=None), dict(q=ODD), dict(n_ctx=None), dict(out=None), dict(out=ODD), dict(out=P), dict(pages=None), dict(window=-1),
                 dict(n_sink=-1), dict(n_cap=0), dict(n_cap=(1 << 30) + 1), dict(ws=None), dict(ws=ODD)):
         assert call(**bad) == E, bad
     for field, value, code in (("head_dim", 64, U), ("n_q_heads", 6, U), ("batch", 0, E), ("dtype", 7, E)):

@@ -251,6 +251,46 @@ def test_prompt(case, wild):
     _check("prompt", dtype, heads, page, n, new, window, sink, n_cap, lead=lead, seed=case, wild=wild)
 
 
+LONG = [  # many tiles that all columns see whole, and few columns over many tokens, whose tiles are split
+    (BF, (8, 2), 0, [1100], [1100], 0, 0, 1100),
+    (BF, (8, 2), 16, [1100, 300], [1100, 290], 0, 0, 1100),
+    (BF, (4, 4), 64, [900], [900], 300, 5, 900),
+    (BF, (8, 1), 5, [700, 20], [700, 20], 0, 0, 700),
+    (BF, (8, 2), 16, [6000, 5001], [3, 20], 0, 0, 6000),
+    (BF, (8, 8), 64, [9000], [1], 0, 0, 9000),
+    (BF, (8, 2), 7, [4100], [33], 0, 0, 4100),
+    (BF, (4, 2), 128, [5000, 4000, 0], [130, 2, 0], 3000, 70, 5000),
+    (F32, (4, 2), 16, [1500, 600], [20, 600], 0, 0, 1500),
+]
+
+
+@pytest.mark.parametrize("case", range(len(LONG)))
+def test_long_prompts(case):
+    dtype, heads, page, n, new, window, sink, n_cap = LONG[case]
+    _check("prompt", dtype, heads, page, n, new, window, sink, n_cap, seed=200 + case)
+
+
+@pytest.mark.parametrize("which", ["prompt", "paged"])
+@pytest.mark.parametrize("dtype", [BF, F32])
+def test_many_sequences(which, dtype):
+    """More sequences than a wave has lanes, empty ones and ones without new tokens among them."""
+    n = [(37 * b) % 90 for b in range(150)]
+    new = [min(x, (11 * b) % 7) for b, x in enumerate(n)] if which == "prompt" else None
+    _check(which, dtype, (4, 2), 16, n, new, 0, 0, 90, seed=77)
+    _check(which, dtype, (4, 2), 16, n, new, 20, 2, 90, seed=78, lead=4 if new else 0)
+
+
+@pytest.mark.parametrize("page", [8, 16, 7, 64])
+def test_a_page_in_the_middle_is_not_there(page):
+    """Where the tokens are many, and few columns see them all, whole and split."""
+    def edit(kp, vp, table):
+        table[0, (400 // page) + 1] = -1
+        table[0, 900 // page] = kp.shape[0] + 5
+    for n, new in ((1000, 8), (1000, 400), (2600, 4)):
+        _check("prompt", BF, (8, 2), page, [n], [new], 0, 0, n, seed=31 + page, edit=edit)
+    _check("paged", BF, (8, 2), page, [1000], None, 0, 0, 1000, seed=31 + page, edit=edit)
+
+
 @pytest.mark.parametrize("which", ["prompt", "paged"])
 @pytest.mark.parametrize("dtype", [BF, F32])
 def test_pages_that_are_not_there(which, dtype):
