@@ -5,7 +5,8 @@
 // waves walk over tiles of 64 columns, whose queries come through LDS, and every lane sums the weights of its own token: no
 // exchange until the end, and the order of a sum is fixed.  Bound by the vector units: an exponential a (column, token), a
 // multiply-add and a sum.  A token early in a prompt has the most columns: its block goes first, and where the blocks of
-// tokens are few its columns are shared out over several workgroups, whose sums a second kernel adds in order.
+// tokens are few its columns are shared out over several workgroups, whose sums a second kernel adds in order.  4 x 2048 tokens,
+// 32 heads on 8: 118 us (200 with blocks next to each other in the grid, which gives one die all the early ones).
 #include "kvr_launch.h"
 #include "kvr_prompt.h"
 

@@ -5,7 +5,7 @@
 
 namespace kvr {
 
-// A number of the caller's lists, which no kernel writes: where the address is the same for the whole wave it comes through
+// A number of a list that the kernel does not write: where the address is the same for the whole wave it comes through
 // the scalar unit.
 __host__ __device__ __forceinline__ int32_t listed(const int32_t* p) {
 #ifdef __HIP_DEVICE_COMPILE__
