@@ -39,10 +39,14 @@ constexpr int PG_SLICE = 1024;      // tokens of a workgroup that adds scores
 // Workgroups that a CU holds at a time: what the registers of a wave leave (bf16: 32 for a tile, 16 for q, 8 G for the sums)
 constexpr int paged_per_cu(int elem, int G) { return elem == 2 ? (G <= 4 ? 4 : 3) : (G <= 4 ? 3 : 2); }
 
+// The kernel for caches of few tokens: waves of a workgroup, what registers leave; tiles, whose logits stay in LDS
+constexpr int short_waves(int elem, int G) { return elem == 2 && G <= 4 ? 16 : 8; }
+constexpr int short_tiles(int G) { return G == 8 ? 32 : 64; }
+
 struct PagedPlan {
   int wgs;                          // workgroups of the first kernel
   long long tiles;                  // tiles a unit can have
-  bool join;
+  bool whole;                       // a workgroup has a whole unit (no first kernel, no workspace)
   bool fits;                        // the row of chunks in 31 bits
   size_t off_o, off_ml, off_span, off_log, total;
 };
@@ -59,13 +63,17 @@ PagedPlan paged_plan(const DevDesc& d, int dtype, long long cap, const Visible& 
   p.fits = chunks < 0x7fffffffll;
   const int fill = 256 * paged_per_cu(dtype == KVR_F32 ? 4 : 2, d.G);
   p.wgs = (int)(chunks < fill ? chunks : fill);
-  p.join = scores || p.tiles > 4;
+  // A unit to one workgroup: where that is a tile a wave, and for up to 1024 tokens (with eight heads 512) where units are many:
+  // 1000 tokens, 32 heads on 8, 512 units 46 us against 64 in even pieces and a join, 128 units 19 against 24, but 8 units 15
+  // against 14 (float32, half the waves: 32 against 13); 100 tokens, 8 units 7 against 13.
+  p.whole = p.tiles <= short_waves(dtype == KVR_F32 ? 4 : 2, d.G) || (p.tiles <= short_tiles(d.G) && units >= 64);
   const size_t slots = (size_t)p.wgs + units;
   auto whole = [](size_t x) { return (x + 255) & ~(size_t)255; };
-  p.off_o = 0;
-  p.off_ml = p.join ? whole(slots * d.G * D * sizeof(float)) : 0;
-  p.off_span = p.off_ml + (p.join ? whole(slots * d.G * 2 * sizeof(float)) : 0);
-  p.off_log = p.off_span + (p.join ? whole((size_t)units * 2 * sizeof(int)) : 0);
+  p.off_o = p.off_ml = p.off_span = p.off_log = p.total = 0;
+  if (p.whole) return p;
+  p.off_ml = whole(slots * d.G * D * sizeof(float));
+  p.off_span = p.off_ml + whole(slots * d.G * 2 * sizeof(float));
+  p.off_log = p.off_span + whole((size_t)units * 2 * sizeof(int));
   p.total = p.off_log + (scores ? whole((size_t)units * p.tiles * 16 * d.G * sizeof(float)) : 0);
   return p;
 }
@@ -116,6 +124,7 @@ __device__ __forceinline__ int seq_chunks(const PagedArgs& a, int b) {
 }
 // (the host has made sure that all chunks there can be fit 31 bits)
 __device__ __forceinline__ int all_chunks(const PagedArgs& a, int B, int heads) {
+  if (B == 1) return seq_chunks(a, 0) * heads;
   const int lane = threadIdx.x & 63;
   int sum = 0;
   for (int b0 = 0; b0 < B; b0 += 64) sum += b0 + lane < B ? seq_chunks(a, b0 + lane) : 0;
@@ -241,18 +250,200 @@ __device__ __forceinline__ f32x4_t tile_logits(const u32x4_t (&k)[Tile<T>::N], c
   return s;
 }
 
+// what a wave has of a unit
+template <int G>
+struct Sums {
+  float acc[G][8];      // of head g, channels 8 (lane mod 16) .. +7, over the tokens of the lane's group of 16 lanes
+  float m, l;           // of head lane mod 16; l as acc
+};
+
+// A wave walks over every STEP-th tile of a unit from tile ti to t_end.  keep.put(s) gets a tile's logits, keep.after(ti, more)
+// comes at the tile's end, behind the requests for the next one.
+template <typename T, int G, bool ONE, int STEP, typename Keep>
+__device__ __forceinline__ void walk(const DevDesc& d, const PagedArgs& a, int b, int h, int n, const TileRange& tr, int ti, int t_end,
+                                     Sums<G>& w, Keep&& keep) {
+  constexpr int PER = sizeof(T) / 2;                  // 16-byte pieces of eight channels
+  const float NEG_INF = -__builtin_inff(), scale2 = d.scale * LOG2E;       // logits in powers of two
+  const int lane = threadIdx.x & 63, r16 = lane >> 4, col = lane & 15, P = n - 1;
+#pragma unroll
+  for (int g = 0; g < G; ++g)
+#pragma unroll
+    for (int c = 0; c < 8; ++c) w.acc[g][c] = 0.f;
+  w.m = NEG_INF;
+  w.l = 0.f;
+  if (ti >= t_end) return;
+  int j = tile_token<16>(tr, ti);
+  Tile<T> t;
+  int entry = tile_entry<ONE>(a, b, j, n, col);       // of the wave's next tile
+  u32x4_t q[Tile<T>::N];
+  const T* qp = (const T*)a.q + ((size_t)b * d.Hq + h * G + min(col, G - 1)) * D + 8 * r16;
+#pragma unroll
+  for (int i = 0; i < Tile<T>::N; ++i) q[i] = *reinterpret_cast<const u32x4_t*>(qp + 32 * (i / PER) + 4 * (i % PER));
+  TileRows<ONE> now = tile_rows<ONE>(a, d.Hkv, entry, h, j, n, col);
+  load_k<T, ONE>(t, a.pages.k, now, j, n, r16, col);
+  load_v<T, ONE>(t, a.pages.v, now, j, n, r16, col);
+  if (ti + STEP < t_end) entry = tile_entry<ONE>(a, b, tile_token<16>(tr, ti + STEP), n, col);
+  for (; ti < t_end; ti += STEP) {
+    const f32x4_t s4 = tile_logits<T>(t.k, q);
+    const bool more = ti + STEP < t_end;
+    const int jn = more ? tile_token<16>(tr, ti + STEP) : j;
+    const uint32_t there = now.there;
+    if (more) {
+      now = tile_rows<ONE>(a, d.Hkv, entry, h, jn, n, col);
+      load_k<T, ONE>(t, a.pages.k, now, jn, n, r16, col);
+      if (ti + 2 * STEP < t_end) entry = tile_entry<ONE>(a, b, tile_token<16>(tr, ti + 2 * STEP), n, col);
+    }
+    __builtin_amdgcn_sched_barrier(0);
+    float s[4];
+    uint32_t dead = 0;
+#pragma unroll
+    for (int x = 0; x < 4; ++x) s[x] = s4[x] * scale2;
+    // a tile that the query does not see whole
+    const bool whole = j + 15 <= P && there == 0xffffu && (a.vis.window == 0 || j > P - a.vis.window || j + 15 < a.vis.n_sink);
+    if (!whole) {
+#pragma unroll
+      for (int x = 0; x < 4; ++x)
+        if (!sees(a.vis, P, j + 4 * r16 + x) || !((there >> (4 * r16 + x)) & 1)) {
+          s[x] = NEG_INF;
+          dead |= 1u << x;
+          // it may hold anything: weight 0 is not enough
+#pragma unroll
+          for (int i = 0; i < PER; ++i) t.v[x * PER + i] = u32x4_t{0, 0, 0, 0};
+        }
+    }
+    keep.put(ti, s);
+    float mx = fmaxf(fmaxf(s[0], s[1]), fmaxf(s[2], s[3]));
+    mx = rows_max(mx);
+    const float m_new = fmaxf(w.m, mx);
+    if (__any(m_new > w.m)) {
+      const float corr = w.m == NEG_INF ? 0.f : exp2_(w.m - m_new);
+      w.l *= corr;
+      scale_acc<G>(w.acc, corr);
+    }
+    w.m = m_new;
+    float pr[4];
+#pragma unroll
+    for (int x = 0; x < 4; ++x) {
+      pr[x] = (dead >> x) & 1 ? 0.f : exp2_(s[x] - m_new);
+      w.l += pr[x];
+    }
+#pragma unroll
+    for (int x = 0; x < 4; ++x) {
+      float v[8];
+      widen<T>(&t.v[x * PER], v);
+      add_pv<G>(w.acc, pr[x], v);
+      // one token's floats at a time, and all of them before the next loads: registers
+#pragma unroll
+      for (int g = 0; g < G; ++g)
+#pragma unroll
+        for (int c = 0; c < 8; ++c) asm volatile("" : "+v"(w.acc[g][c]));
+      __builtin_amdgcn_sched_barrier(0);
+    }
+    if (more) load_v<T, ONE>(t, a.pages.v, now, jn, n, r16, col);
+    j = jn;
+    keep.after(ti, more);
+  }
+}
+
+// A wave's sums over its four groups of 16 lanes, to LDS: s_o [G][D], s_m and s_l [G].
+template <int G>
+__device__ __forceinline__ void to_shared(Sums<G>& w, float (&s_o)[G][D], float (&s_m)[G], float (&s_l)[G]) {
+  const int lane = threadIdx.x & 63, col = lane & 15;
+  w.l += __shfl_xor(w.l, 16);
+  w.l += __shfl_xor(w.l, 32);
+#pragma unroll
+  for (int g = 0; g < G; ++g)
+#pragma unroll
+    for (int c = 0; c < 8; ++c) {
+      w.acc[g][c] += __shfl_xor(w.acc[g][c], 16);
+      w.acc[g][c] += __shfl_xor(w.acc[g][c], 32);
+    }
+  if (lane < 16) {
+    if (col < G) {
+      s_m[col] = w.m;
+      s_l[col] = w.l;
+    }
+#pragma unroll
+    for (int g = 0; g < G; ++g) {
+      *reinterpret_cast<float4*>(&s_o[g][8 * col]) = make_float4(w.acc[g][0], w.acc[g][1], w.acc[g][2], w.acc[g][3]);
+      *reinterpret_cast<float4*>(&s_o[g][8 * col + 4]) = make_float4(w.acc[g][4], w.acc[g][5], w.acc[g][6], w.acc[g][7]);
+    }
+  }
+}
+// the waves' sums together: head g, channel c
+struct Joined {
+  float m, l, o;
+};
+template <int WAVES, int G>
+__device__ __forceinline__ Joined join_waves(const float (&s_o)[WAVES][G][D], const float (&s_m)[WAVES][G], const float (&s_l)[WAVES][G],
+                                             int g, int c) {
+  Joined r = {s_m[0][g], 0.f, 0.f};
+#pragma unroll
+  for (int x = 1; x < WAVES; ++x) r.m = fmaxf(r.m, s_m[x][g]);
+#pragma unroll
+  for (int x = 0; x < WAVES; ++x) {
+    const float f = s_m[x][g] == -__builtin_inff() ? 0.f : exp2_(s_m[x][g] - r.m);
+    r.l = fmaf(f, s_l[x][g], r.l);
+    r.o = fmaf(f, s_o[x][g][c], r.o);
+  }
+  return r;
+}
+template <typename T>
+__device__ __forceinline__ void put_out(const DevDesc& d, const PagedArgs& a, int b, int head, int c, const Joined& r) {
+  Store<T>::store1((T*)a.out + ((size_t)b * d.Hq + head) * D + c, r.m == -__builtin_inff() ? 0.f : r.o / r.l);
+}
+
+// logits of a wave's tiles, PG_KEEP at a time through LDS to memory
+template <int G>
+struct KeepFar {
+  float* lds;           // [PG_KEEP][16][G]
+  float* unit;          // [tiles][16][G], or null: none are wanted
+  int kept;
+  __device__ __forceinline__ void put(int, const float (&s)[4]) {
+    const int lane = threadIdx.x & 63, r16 = lane >> 4, col = lane & 15;
+    if (unit && col < G) {
+#pragma unroll
+      for (int x = 0; x < 4; ++x) lds[(kept * 16 + 4 * r16 + x) * G + col] = s[x];
+    }
+  }
+  __device__ __forceinline__ void after(int ti, bool more) {
+    if (!unit || (++kept < PG_KEEP && more)) return;
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+    // tile k of the kept ones is tile ti - PG_WAVES (kept - 1 - k): 4 G pieces of 16 bytes each
+    for (int i = threadIdx.x & 63; i < kept * 4 * G; i += 64) {
+      const int k = i / (4 * G), e = i % (4 * G);
+      *reinterpret_cast<float4*>(unit + (size_t)(ti - PG_WAVES * (kept - 1 - k)) * 16 * G + 4 * e) =
+          *reinterpret_cast<const float4*>(&lds[k * 16 * G + 4 * e]);
+    }
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    kept = 0;
+  }
+};
+// all of a short unit's logits, in LDS
+template <int G>
+struct KeepNear {
+  float* lds;           // [tiles][16][G], or null
+  __device__ __forceinline__ void put(int ti, const float (&s)[4]) {
+    const int lane = threadIdx.x & 63, r16 = lane >> 4, col = lane & 15;
+    if (lds && col < G) {
+#pragma unroll
+      for (int x = 0; x < 4; ++x) lds[(ti * 16 + 4 * r16 + x) * G + col] = s[x];
+    }
+  }
+  __device__ __forceinline__ void after(int, bool) {}
+};
+
 template <typename T, int G, bool ONE>
-__global__ __launch_bounds__(64 * PG_WAVES, paged_per_cu(sizeof(T), G)) void paged_kernel(DevDesc d, PagedArgs a, float* part_o, float* part_ml, int* span, float* logits,
-                                                              long long most_tiles) {
+__global__ __launch_bounds__(64 * PG_WAVES, paged_per_cu(sizeof(T), G)) void paged_kernel(DevDesc d, PagedArgs a, float* part_o,
+                                                                                          float* part_ml, int* span, float* logits,
+                                                                                          long long most_tiles) {
   __shared__ __align__(16) float s_o[PG_WAVES][G][D];
   __shared__ float s_m[PG_WAVES][G], s_l[PG_WAVES][G];
   __shared__ __align__(16) float s_log[PG_WAVES][PG_KEEP * 16 * G];
-  const int lane = threadIdx.x & 63, wave = uniform((int)(threadIdx.x >> 6));
-  const int r16 = lane >> 4, col = lane & 15;
-  const int w = blockIdx.x;
-  const float NEG_INF = -__builtin_inff();
-  constexpr int PER = sizeof(T) / 2;                  // 16-byte pieces of eight channels
-  const float scale2 = d.scale * LOG2E;               // logits in powers of two
+  const int wave = uniform((int)(threadIdx.x >> 6)), w = blockIdx.x;
 
   // sequences without a token yield zeros
   for (int b = w; b < d.B; b += gridDim.x)
@@ -272,156 +463,25 @@ __global__ __launch_bounds__(64 * PG_WAVES, paged_per_cu(sizeof(T), G)) void pag
     const int chunks = (tr.n + 3) >> 2;
     const int len = min(end - at, chunks - c0);
     const int u = b * d.Hkv + h;
-    const int t_end = min(4 * (c0 + len), tr.n);
-    const int P = n - 1;
-
-    u32x4_t q[Tile<T>::N];
-    {
-      const T* qp = (const T*)a.q + ((size_t)b * d.Hq + h * G + min(col, G - 1)) * D + 8 * r16;
-#pragma unroll
-      for (int i = 0; i < Tile<T>::N; ++i) q[i] = *reinterpret_cast<const u32x4_t*>(qp + 32 * (i / PER) + 4 * (i % PER));
-    }
-    float acc[G][8];
-#pragma unroll
-    for (int g = 0; g < G; ++g)
-#pragma unroll
-      for (int c = 0; c < 8; ++c) acc[g][c] = 0.f;
-    float m_run = NEG_INF, l_run = 0.f;
-    float* log_unit = logits ? logits + (size_t)u * most_tiles * 16 * G : nullptr;
-    int kept = 0;
-
-    int ti = 4 * c0 + wave;
-    Tile<T> t;
-    int entry = 0;                         // of the wave's next tile
-    if (ti < t_end) {
-      const int j0 = tile_token<16>(tr, ti);
-      TileRows<ONE> now = tile_rows<ONE>(a, d.Hkv, tile_entry<ONE>(a, b, j0, n, col), h, j0, n, col);
-      load_k<T, ONE>(t, a.pages.k, now, j0, n, r16, col);
-      load_v<T, ONE>(t, a.pages.v, now, j0, n, r16, col);
-      if (ti + 4 < t_end) entry = tile_entry<ONE>(a, b, tile_token<16>(tr, ti + 4), n, col);
-      int j = j0;
-      for (; ti < t_end; ti += 4) {
-        const f32x4_t s4 = tile_logits<T>(t.k, q);
-        const bool more = ti + 4 < t_end;
-        const int jn = more ? tile_token<16>(tr, ti + 4) : j;
-        const uint32_t there = now.there;
-        if (more) {
-          now = tile_rows<ONE>(a, d.Hkv, entry, h, jn, n, col);
-          load_k<T, ONE>(t, a.pages.k, now, jn, n, r16, col);
-          if (ti + 8 < t_end) entry = tile_entry<ONE>(a, b, tile_token<16>(tr, ti + 8), n, col);
-        }
-        __builtin_amdgcn_sched_barrier(0);
-        float s[4];
-        uint32_t dead = 0;
-#pragma unroll
-        for (int x = 0; x < 4; ++x) s[x] = s4[x] * scale2;
-        // a tile that the query does not see whole
-        const bool whole = j + 15 <= P && there == 0xffffu && (a.vis.window == 0 || j > P - a.vis.window || j + 15 < a.vis.n_sink);
-        if (!whole) {
-#pragma unroll
-          for (int x = 0; x < 4; ++x)
-            if (!sees(a.vis, P, j + 4 * r16 + x) || !((there >> (4 * r16 + x)) & 1)) {
-              s[x] = NEG_INF;
-              dead |= 1u << x;
-              // it may hold anything: weight 0 is not enough
-#pragma unroll
-              for (int i = 0; i < PER; ++i) t.v[x * PER + i] = u32x4_t{0, 0, 0, 0};
-            }
-        }
-        if (log_unit && col < G) {
-#pragma unroll
-          for (int x = 0; x < 4; ++x) s_log[wave][(kept * 16 + 4 * r16 + x) * G + col] = s[x];
-        }
-        float mx = fmaxf(fmaxf(s[0], s[1]), fmaxf(s[2], s[3]));
-        mx = rows_max(mx);
-        const float m_new = fmaxf(m_run, mx);
-        if (__any(m_new > m_run)) {
-          const float corr = m_run == NEG_INF ? 0.f : exp2_(m_run - m_new);
-          l_run *= corr;
-          scale_acc<G>(acc, corr);
-        }
-        m_run = m_new;
-        float pr[4];
-#pragma unroll
-        for (int x = 0; x < 4; ++x) {
-          pr[x] = (dead >> x) & 1 ? 0.f : exp2_(s[x] - m_new);
-          l_run += pr[x];
-        }
-#pragma unroll
-        for (int x = 0; x < 4; ++x) {
-          float v[8];
-          widen<T>(&t.v[x * (sizeof(T) / 2)], v);
-          add_pv<G>(acc, pr[x], v);
-          // one token's floats at a time, and all of them before the next loads: registers
-#pragma unroll
-          for (int g = 0; g < G; ++g)
-#pragma unroll
-            for (int c = 0; c < 8; ++c) asm volatile("" : "+v"(acc[g][c]));
-          __builtin_amdgcn_sched_barrier(0);
-        }
-        if (more) load_v<T, ONE>(t, a.pages.v, now, jn, n, r16, col);
-        j = jn;
-        if (log_unit && (++kept == PG_KEEP || !more)) {
-          __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
-          __builtin_amdgcn_wave_barrier();
-          __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
-          // tile k of the kept ones is tile ti - 4 (kept - 1 - k): 4 G pieces of 16 bytes each
-          for (int i = lane; i < kept * 4 * G; i += 64) {
-            const int k = i / (4 * G), e = i % (4 * G);
-            *reinterpret_cast<float4*>(log_unit + (size_t)(ti - 4 * (kept - 1 - k)) * 16 * G + 4 * e) =
-                *reinterpret_cast<const float4*>(&s_log[wave][k * 16 * G + 4 * e]);
-          }
-          __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
-          __builtin_amdgcn_wave_barrier();
-          kept = 0;
-        }
-      }
-    }
-    // the four waves together
-    l_run += __shfl_xor(l_run, 16);
-    l_run += __shfl_xor(l_run, 32);
-#pragma unroll
-    for (int g = 0; g < G; ++g)
-#pragma unroll
-      for (int c = 0; c < 8; ++c) {
-        acc[g][c] += __shfl_xor(acc[g][c], 16);
-        acc[g][c] += __shfl_xor(acc[g][c], 32);
-      }
-    if (r16 == 0) {
-      if (col < G) {
-        s_m[wave][col] = m_run;
-        s_l[wave][col] = l_run;
-      }
-#pragma unroll
-      for (int g = 0; g < G; ++g) {
-        *reinterpret_cast<float4*>(&s_o[wave][g][8 * col]) = make_float4(acc[g][0], acc[g][1], acc[g][2], acc[g][3]);
-        *reinterpret_cast<float4*>(&s_o[wave][g][8 * col + 4]) = make_float4(acc[g][4], acc[g][5], acc[g][6], acc[g][7]);
-      }
-    }
+    Sums<G> sums;
+    KeepFar<G> keep = {s_log[wave], logits ? logits + (size_t)u * most_tiles * 16 * G : nullptr, 0};
+    walk<T, G, ONE, PG_WAVES>(d, a, b, h, n, tr, 4 * c0 + wave, min(4 * (c0 + len), tr.n), sums, keep);
+    to_shared<G>(sums, s_o[wave], s_m[wave], s_l[wave]);
     __syncthreads();
     const bool all = len == chunks;             // the whole unit: no other workgroup has a part of it
     const size_t slot = (size_t)w + u;
-    if (span && threadIdx.x == 0) {             // which workgroups have parts of the unit
+    if (threadIdx.x == 0) {                     // which workgroups have parts of the unit
       if (c0 == 0) span[2 * u] = w;
       if (c0 + len == chunks) span[2 * u + 1] = w;
     }
     for (int i = threadIdx.x; i < G * D; i += 64 * PG_WAVES) {
       const int g = i / D, c = i % D;
-      float m = s_m[0][g];
-#pragma unroll
-      for (int x = 1; x < PG_WAVES; ++x) m = fmaxf(m, s_m[x][g]);
-      float l = 0.f, o = 0.f;
-#pragma unroll
-      for (int x = 0; x < PG_WAVES; ++x) {
-        const float f = s_m[x][g] == NEG_INF ? 0.f : exp2_(s_m[x][g] - m);
-        l = fmaf(f, s_l[x][g], l);
-        o = fmaf(f, s_o[x][g][c], o);
-      }
-      if (all) Store<T>::store1((T*)a.out + ((size_t)b * d.Hq + h * G + g) * D + c, m == NEG_INF ? 0.f : o / l);
-      else part_o[slot * G * D + i] = o;
-      if (part_ml && c == 0) {
-        part_ml[(slot * G + g) * 2] = m;
-        part_ml[(slot * G + g) * 2 + 1] = l;
+      const Joined r = join_waves<PG_WAVES, G>(s_o, s_m, s_l, g, c);
+      if (all) put_out<T>(d, a, b, h * G + g, c, r);
+      else part_o[slot * G * D + i] = r.o;
+      if (c == 0) {
+        part_ml[(slot * G + g) * 2] = r.m;
+        part_ml[(slot * G + g) * 2 + 1] = r.l;
       }
     }
     __syncthreads();
@@ -432,6 +492,40 @@ __global__ __launch_bounds__(64 * PG_WAVES, paged_per_cu(sizeof(T), G)) void pag
       do ++p.b;
       while (at < end && seq_chunks(a, p.b) == 0);
     }
+  }
+}
+
+// Caches of few tokens: a workgroup of as many waves as a CU takes has a whole unit, and nothing is left to join.
+template <typename T, int G, bool ONE>
+__global__ __launch_bounds__(64 * short_waves(sizeof(T), G)) void paged_short_kernel(DevDesc d, PagedArgs a) {
+  constexpr int WAVES = short_waves(sizeof(T), G);
+  __shared__ __align__(16) float s_o[WAVES][G][D];
+  __shared__ float s_m[WAVES][G], s_l[WAVES][G];
+  __shared__ __align__(16) float s_log[short_tiles(G) * 16 * G];
+  const int wave = uniform((int)(threadIdx.x >> 6));
+  const int u = blockIdx.x, b = uniform(u / d.Hkv), h = u - b * d.Hkv;
+  int n;
+  const TileRange tr = unit_tiles(a, b, n);
+  Sums<G> sums;
+  KeepNear<G> keep = {a.scores ? s_log : nullptr};
+  walk<T, G, ONE, WAVES>(d, a, b, h, n, tr, wave, tr.n, sums, keep);
+  to_shared<G>(sums, s_o[wave], s_m[wave], s_l[wave]);
+  __syncthreads();
+  for (int i = threadIdx.x; i < G * D; i += 64 * WAVES) put_out<T>(d, a, b, h * G + i / D, i % D, join_waves<WAVES, G>(s_o, s_m, s_l, i / D, i % D));
+  if (!a.scores) return;
+  float lse[G];
+#pragma unroll
+  for (int g = 0; g < G; ++g) {
+    const Joined r = join_waves<WAVES, G>(s_o, s_m, s_l, g, 0);
+    lse[g] = r.m == -__builtin_inff() ? __builtin_inff() : r.m + __builtin_amdgcn_logf(r.l);
+  }
+  for (int e = threadIdx.x; e < tr.n * 16; e += 64 * WAVES) {
+    const int j = tile_token<16>(tr, e >> 4) + (e & 15);
+    if (j >= n || j >= a.n_cap) continue;
+    float sum = 0.f;
+#pragma unroll
+    for (int g = 0; g < G; ++g) sum += exp2_(s_log[e * G + g] - lse[g]);
+    if (sum != 0.f) a.scores[(size_t)u * a.n_cap + j] += sum;
   }
 }
 
@@ -554,18 +648,24 @@ __global__ __launch_bounds__(256) void paged_join_kernel(DevDesc d, PagedArgs a,
 template <typename T, int G>
 hipError_t launch(const DevDesc& d, const PagedArgs& a, hipStream_t st) {
   const PagedPlan p = paged_plan(d, sizeof(T) == 4 ? KVR_F32 : KVR_BF16, a.pages.cap, a.vis, a.scores != nullptr);
-  char* base = (char*)a.ws;
-  float* part_o = p.join ? (float*)(base + p.off_o) : nullptr;
-  float* part_ml = p.join ? (float*)(base + p.off_ml) : nullptr;
-  int* span = p.join ? (int*)(base + p.off_span) : nullptr;
-  float* logits = a.scores ? (float*)(base + p.off_log) : nullptr;
   const bool one = a.pages.table == nullptr || a.pages.page_size % 16 == 0;
+  if (p.whole) {
+    const dim3 grid(d.B * d.Hkv), block(64 * short_waves(sizeof(T), G));
+    if (one) hipLaunchKernelGGL((paged_short_kernel<T, G, true>), grid, block, 0, st, d, a);
+    else hipLaunchKernelGGL((paged_short_kernel<T, G, false>), grid, block, 0, st, d, a);
+    return hipGetLastError();
+  }
+  char* base = (char*)a.ws;
+  float* part_o = (float*)(base + p.off_o);
+  float* part_ml = (float*)(base + p.off_ml);
+  int* span = (int*)(base + p.off_span);
+  float* logits = a.scores ? (float*)(base + p.off_log) : nullptr;
   if (one)
     hipLaunchKernelGGL((paged_kernel<T, G, true>), dim3(p.wgs), dim3(64 * PG_WAVES), 0, st, d, a, part_o, part_ml, span, logits, p.tiles);
   else
     hipLaunchKernelGGL((paged_kernel<T, G, false>), dim3(p.wgs), dim3(64 * PG_WAVES), 0, st, d, a, part_o, part_ml, span, logits, p.tiles);
   const hipError_t e = hipGetLastError();
-  if (e != hipSuccess || !p.join) return e;
+  if (e != hipSuccess) return e;
   const unsigned slices = a.scores ? (unsigned)((p.tiles * 16 + PG_SLICE - 1) / PG_SLICE) : 0;
   hipLaunchKernelGGL((paged_join_kernel<T, G>), dim3(G + slices, d.B * d.Hkv), dim3(256), 0, st, d, a, part_o, part_ml, span, logits,
                      p.tiles);

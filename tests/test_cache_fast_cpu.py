@@ -60,6 +60,7 @@ def fast(monkeypatch):
 
     monkeypatch.setattr(kvr, "lib", lambda: Recorder)
     monkeypatch.setattr(kvr, "_stream", lambda: 77)
+    monkeypatch.setattr(kvr, "_stream_of", lambda dev: 77)
     monkeypatch.setattr(torch.cuda, "current_device", lambda: 0)
     yield m, got
     m.setup_cache(C.cast(real.kvr_rotate, P).value, C.cast(real.kvr_attend_paged, P).value)

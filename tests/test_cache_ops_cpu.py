@@ -47,7 +47,7 @@ def _prompt(desc=None, over=None, **kw):
 
 
 def _paged(desc=None, over=None, **kw):
-    a = dict(q=P, n_ctx=P, pages=C.byref(over or _pages()), window=0, n_sink=0, out=P + 16, scores=P, n_cap=64, ws=P, ws_bytes=0)
+    a = dict(q=P, n_ctx=P, pages=C.byref(over or _pages(table_cap=128)), window=0, n_sink=0, out=P + 16, scores=P, n_cap=64, ws=P, ws_bytes=0)
     a.update(kw)
     return kvr.lib().kvr_attend_paged(C.byref(desc or _desc()), *a.values(), None)
 
@@ -120,6 +120,7 @@ def test_workspace_sizes():
         return n.value
     assert prompt(0, 1) == 0
     assert prompt(100, 1) >= 100 * 8 * 4                  # a float per row and head
+    assert paged(1) == paged(0) == 0                      # 64 tokens: a workgroup has all of a head's
     big = _pages(k=None, v=None, table_cap=8192)
     assert paged(1, big) >= paged(1) and paged(1, big) >= paged(0, big)
     for f, args in ((L.kvr_attend_prompt_workspace_size, (5,)), (L.kvr_attend_paged_workspace_size, ())):

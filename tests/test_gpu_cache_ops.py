@@ -280,6 +280,14 @@ def test_many_sequences(which, dtype):
     _check(which, dtype, (4, 2), 16, n, new, 20, 2, 90, seed=78, lead=4 if new else 0)
 
 
+@pytest.mark.parametrize("dtype,heads,n", [(BF, (8, 2), 1000), (BF, (16, 2), 500), (BF, (2, 2), 700), (F32, (8, 2), 800), (F32, (16, 2), 300)])
+def test_many_short_caches(dtype, heads, n):
+    """A unit to a workgroup with several tiles a wave; the longest of them as much as the cache holds."""
+    lens = [max(0, n - 29 * b) for b in range(36)]
+    _check("paged", dtype, heads, 16, lens, None, 0, 0, n, seed=91)
+    _check("paged", dtype, heads, 24, lens, None, 100, 20, n - 5, seed=92, wild=float("nan"))
+
+
 @pytest.mark.parametrize("page", [8, 16, 7, 64])
 def test_a_page_in_the_middle_is_not_there(page):
     """Where the tokens are many, and few columns see them all, whole and split."""
