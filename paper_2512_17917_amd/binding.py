@@ -7,7 +7,7 @@ pointers, checks dtype / device / contiguity / minimum size, and passes
 There is no fallback: if the library is missing, loading raises.
 
 The calls of a decode step (`kvr_step_update`, `kvr_attend_decode`; over an
-uncompressed cache `kvr_rotate`, `kvr_attend_paged`) are checked and made by the extension `_kvr_fast` (csrc/kvr_fast.c), where it was built
+uncompressed cache `kvr_rotate`, `kvr_attend_paged`, `kvr_attend_prompt`) are checked and made by the extension `_kvr_fast` (csrc/kvr_fast.c), where it was built
 and every argument is as it should be; anything else comes back to the checks here,
 which raise.
 """
@@ -211,7 +211,7 @@ def _load_fast(L):
         address = lambda f: C.cast(f, C.c_void_p).value
         m.setup(address(L.kvr_step_update), address(L.kvr_attend_decode), torch.float32, torch.bfloat16, torch.int32,
                 torch.uint8, torch.Tensor)
-        m.setup_cache(address(L.kvr_rotate), address(L.kvr_attend_paged))
+        m.setup_cache(address(L.kvr_rotate), address(L.kvr_attend_paged), address(L.kvr_attend_prompt))
         _fast = m
 
 
@@ -600,7 +600,7 @@ def kvr_rotate(desc, rot, q, k, v, n_rows, q_start, n_ctx, q_out, k_out=None, pa
     qp, qs = _rows(q, dt, n_rows, desc.n_q_heads, d, "q")
     kp, ks = _rows(k, dt, n_rows, desc.n_kv_heads, d, "k")
     vp, vs = _rows(v, dt, n_rows, desc.n_kv_heads, d, "v")
-    _here(q, k, v, n_ctx, q_out, k_out, *rot.tensors)
+    _here(q, k, v, q_start, n_ctx, q_out, k_out, *rot.tensors)
     rc = lib().kvr_rotate(
         C.byref(desc), C.byref(rot), qp, qs, kp, ks, vp, vs, n_rows,
         _ptr(q_start, torch.int32, desc.batch + 1, "q_start", True), _ptr(n_ctx, torch.int32, desc.batch, "n_ctx"),
@@ -617,14 +617,22 @@ def kvr_attend_prompt_workspace_size(desc, n_rows, pages, window, n_sink, scores
 
 
 def kvr_attend_prompt(desc, q, n_rows, q_start, n_ctx, pages, window, n_sink, out, scores, n_cap, ws):
+    pp = _pages(desc, pages)
+    lib()
+    if _fast is not None and isinstance(desc, kvr_desc) and isinstance(q, torch.Tensor) and q.is_cuda:
+        dev = pages.dev                              # the current one, as _pages has found
+        rc = _fast.attend_prompt(C.addressof(desc), C.addressof(pages), dev, _stream_of(dev), q, n_rows, q_start, n_ctx, window,
+                                 n_sink, out, scores, n_cap, ws)
+        if rc is not None:
+            return _check("kvr_attend_prompt", rc)
     U, dt = desc.batch * desc.n_kv_heads, _torch_dtype(desc)
     row = desc.n_q_heads * desc.head_dim
     wp, wb = _ws(ws)
-    _here(q, n_ctx, out, scores, ws)
+    _here(q, q_start, n_ctx, out, scores, ws)
     rc = lib().kvr_attend_prompt(
         C.byref(desc), _ptr(q, dt, n_rows * row, "q"), n_rows,
         _ptr(q_start, torch.int32, desc.batch + 1, "q_start", True), _ptr(n_ctx, torch.int32, desc.batch, "n_ctx"),
-        _pages(desc, pages), window, n_sink, _ptr(out, dt, n_rows * row, "out"),
+        pp, window, n_sink, _ptr(out, dt, n_rows * row, "out"),
         _ptr(scores, torch.float32, U * n_cap, "scores", True), n_cap, wp, wb, _stream())
     _check("kvr_attend_prompt", rc)
 

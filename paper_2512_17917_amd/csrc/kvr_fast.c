@@ -21,6 +21,10 @@ typedef int32_t (*rotate_fn)(const kvr_desc*, const kvr_rotation*, const void*, 
 typedef int32_t (*paged_fn)(const kvr_desc*, const void*, const int32_t*, const kvr_pages*, int32_t, int32_t, void*, float*,
                             int64_t, void*, size_t, void*);
 
+typedef int32_t (*prompt_fn)(const kvr_desc*, const void*, int32_t, const int32_t*, const int32_t*, const kvr_pages*, int32_t, int32_t,
+                             void*, float*, int64_t, void*, size_t, void*);
+
+static prompt_fn f_prompt;
 static PyObject *n_get_device, *n_shape, *n_stride;
 static rotate_fn f_rotate;
 static paged_fn f_paged;
@@ -175,10 +179,11 @@ static int rows(PyObject* t, PyObject* dtype, int64_t n_rows, int64_t heads, int
 }
 
 static PyObject* setup_cache(PyObject* self, PyObject* const* a, Py_ssize_t n) {
-  int64_t r, p;
-  if (n != 2 || !integer(a[0], &r) || !integer(a[1], &p)) return PyErr_Format(PyExc_TypeError, "setup_cache");
+  int64_t r, p, m;
+  if (n != 3 || !integer(a[0], &r) || !integer(a[1], &p) || !integer(a[2], &m)) return PyErr_Format(PyExc_TypeError, "setup_cache");
   f_rotate = (rotate_fn)(uintptr_t)r;
   f_paged = (paged_fn)(uintptr_t)p;
+  f_prompt = (prompt_fn)(uintptr_t)m;
   Py_RETURN_NONE;
 }
 
@@ -229,12 +234,36 @@ static PyObject* attend_paged(PyObject* self, PyObject* const* a, Py_ssize_t n) 
   return PyLong_FromLong(rc);
 }
 
+/* addresses of desc and pages, current device, stream, then binding.kvr_attend_prompt's arguments without pages */
+static PyObject* attend_prompt(PyObject* self, PyObject* const* a, Py_ssize_t n) {
+  int64_t da, pa, dev, st, n_rows, window, n_sink, n_cap, wb = 0;
+  void *q, *start, *nc, *out, *sc, *ws;
+  if (n != 14 || !f_prompt || !integer(a[0], &da) || !integer(a[1], &pa) || !integer(a[2], &dev) || !integer(a[3], &st) ||
+      !integer(a[5], &n_rows) || !integer(a[8], &window) || !integer(a[9], &n_sink) || !integer(a[12], &n_cap))
+    return refuse();
+  const kvr_desc* d = (const kvr_desc*)(uintptr_t)da;
+  if (!sizes_fit(d, (int64_t[]){n_rows, window, n_sink, n_cap}, 4) || n_rows < 0) return refuse();
+  PyObject* dt = d->dtype == KVR_F32 ? t_f32 : t_bf16;
+  const int64_t U = (int64_t)d->batch * d->n_kv_heads, H = n_rows * d->n_q_heads, D = d->head_dim;
+  if (!tensor(a[4], dt, H * D, 0, &q, 0) || !tensor(a[6], t_i32, d->batch + 1, 1, &start, 0) || !tensor(a[7], t_i32, d->batch, 0, &nc, 0) ||
+      !tensor(a[10], dt, H * D, 0, &out, 0) || !tensor(a[11], t_f32, U * n_cap, 1, &sc, 0) || !tensor(a[13], t_u8, 0, 1, &ws, &wb) ||
+      !here(a[4], dev) || !here(a[6], dev) || !here(a[7], dev) || !here(a[10], dev) || !here(a[11], dev) || !here(a[13], dev))
+    return refuse();
+  int32_t rc;
+  Py_BEGIN_ALLOW_THREADS
+  rc = f_prompt(d, q, (int32_t)n_rows, start, nc, (const kvr_pages*)(uintptr_t)pa, (int32_t)window, (int32_t)n_sink, out, sc, n_cap, ws,
+                (size_t)wb, (void*)(uintptr_t)st);
+  Py_END_ALLOW_THREADS
+  return PyLong_FromLong(rc);
+}
+
 static PyMethodDef methods[] = {{"setup", (PyCFunction)(void*)setup, METH_FASTCALL, 0},
                                 {"step_update", (PyCFunction)(void*)step_update, METH_FASTCALL, 0},
                                 {"attend_decode", (PyCFunction)(void*)attend_decode, METH_FASTCALL, 0},
                                 {"setup_cache", (PyCFunction)(void*)setup_cache, METH_FASTCALL, 0},
                                 {"rotate", (PyCFunction)(void*)rotate, METH_FASTCALL, 0},
                                 {"attend_paged", (PyCFunction)(void*)attend_paged, METH_FASTCALL, 0},
+                                {"attend_prompt", (PyCFunction)(void*)attend_prompt, METH_FASTCALL, 0},
                                 {0, 0, 0, 0}};
 static struct PyModuleDef module = {PyModuleDef_HEAD_INIT, "_kvr_fast", 0, -1, methods, 0, 0, 0, 0};
 

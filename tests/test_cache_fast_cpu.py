@@ -1,4 +1,4 @@
-"""The C route of kvr_rotate and kvr_attend_paged takes what the Python checks take and hands back the rest.  On the CPU:
+"""The C route of kvr_rotate, kvr_attend_paged and kvr_attend_prompt takes what the Python checks take and hands back the rest.  On the CPU:
 objects that answer like device tensors, and a library whose entry points only record their arguments."""
 import ctypes as C
 import os
@@ -52,18 +52,20 @@ def fast(monkeypatch):
     m, got = kvr._fast, []
     rot = C.CFUNCTYPE(I, P, P, P, L, P, L, P, L, I, P, P, P, P, P, P)(lambda *a: got.append(a) or 0)
     att = C.CFUNCTYPE(I, P, P, P, P, I, I, P, P, L, P, C.c_size_t, P)(lambda *a: got.append(a) or 0)
-    m.setup_cache(C.cast(rot, P).value, C.cast(att, P).value)
+    pro = C.CFUNCTYPE(I, P, P, I, P, P, P, I, I, P, P, L, P, C.c_size_t, P)(lambda *a: got.append(a) or 0)
+    m.setup_cache(C.cast(rot, P).value, C.cast(att, P).value, C.cast(pro, P).value)
 
     class Recorder:
         kvr_rotate = staticmethod(lambda *a: got.append(tuple(_plain(x) for x in a)) or 0)
         kvr_attend_paged = staticmethod(lambda *a: got.append(tuple(_plain(x) for x in a)) or 0)
+        kvr_attend_prompt = staticmethod(lambda *a: got.append(tuple(_plain(x) for x in a)) or 0)
 
     monkeypatch.setattr(kvr, "lib", lambda: Recorder)
     monkeypatch.setattr(kvr, "_stream", lambda: 77)
     monkeypatch.setattr(kvr, "_stream_of", lambda dev: 77)
     monkeypatch.setattr(torch.cuda, "current_device", lambda: 0)
     yield m, got
-    m.setup_cache(C.cast(real.kvr_rotate, P).value, C.cast(real.kvr_attend_paged, P).value)
+    m.setup_cache(*[C.cast(f, P).value for f in (real.kvr_rotate, real.kvr_attend_paged, real.kvr_attend_prompt)])
 
 
 def _plain(x):
@@ -171,6 +173,44 @@ def test_paged_refusals(fast, case):
     assert m.attend_paged(C.addressof(d), C.addressof(pages), 0, 77, *a) is None and not got
     with pytest.raises((TypeError, ValueError)):
         kvr.kvr_attend_paged(d, *a[:2], pages, *a[2:])
+    assert not got
+
+
+def _prompt_args(**kw):
+    bf, i32 = torch.bfloat16, torch.int32
+    a = dict(q=Fake(bf, (7, 8, 128), 0x1000), n_rows=7, q_start=Fake(i32, (4,), 0x4000), n_ctx=Fake(i32, (3,), 0x5000), window=5,
+             n_sink=2, out=Fake(bf, (7, 8, 128), 0x6000), scores=Fake(torch.float32, (3, 2, 40), 0x7000), n_cap=40,
+             ws=Fake(torch.uint8, (999,), 0x8000))
+    a.update(kw)
+    return a
+
+
+def test_prompt_both_routes_pass_the_same(fast, monkeypatch):
+    m, got = fast
+    d = _desc()
+    pages = _pages(d)
+    for kw in (dict(), dict(scores=None, n_cap=0), dict(ws=None), dict(q_start=None, n_rows=3), dict(n_rows=0)):
+        del got[:]
+        a = list(_prompt_args(**kw).values())
+        with monkeypatch.context() as p:
+            one, two = _both(p, lambda: kvr.kvr_attend_prompt(d, *a[:4], pages, *a[4:]), got)
+        assert one == two
+
+
+BAD_PROMPT = [dict(q=Fake(torch.bfloat16, (6, 8, 128), 1)), dict(out=Fake(torch.float32, (7, 8, 128), 1)), dict(n_ctx=None),
+              dict(q_start=Fake(torch.int32, (3,), 1)), dict(scores=Fake(torch.float32, (3, 2, 39), 1)),
+              dict(q_start=Fake(torch.int32, (4,), 1, dev=1)), dict(ws=Fake(torch.uint8, (9,), 1, dev=1)), dict(q=None)]
+
+
+@pytest.mark.parametrize("case", range(len(BAD_PROMPT)))
+def test_prompt_refusals(fast, case):
+    m, got = fast
+    d = _desc()
+    pages = _pages(d)
+    a = list(_prompt_args(**BAD_PROMPT[case]).values())
+    assert m.attend_prompt(C.addressof(d), C.addressof(pages), 0, 77, *a) is None and not got
+    with pytest.raises((TypeError, ValueError)):
+        kvr.kvr_attend_prompt(d, *a[:4], pages, *a[4:])
     assert not got
 
 
