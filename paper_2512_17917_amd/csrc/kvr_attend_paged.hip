@@ -128,9 +128,7 @@ __device__ __forceinline__ int all_chunks(const PagedArgs& a, int B, int heads) 
   const int lane = threadIdx.x & 63;
   int sum = 0;
   for (int b0 = 0; b0 < B; b0 += 64) sum += b0 + lane < B ? seq_chunks(a, b0 + lane) : 0;
-#pragma unroll
-  for (int k = 1; k < 64; k <<= 1) sum += __shfl_xor(sum, k);
-  return uniform(sum) * heads;
+  return __builtin_amdgcn_readlane(lanes_upto(sum), 63) * heads;
 }
 
 struct Where {
@@ -147,12 +145,7 @@ __device__ __forceinline__ Where find_chunk(const PagedArgs& a, int B, int heads
   int base = 0;
   for (int b0 = 0; b0 < B; b0 += 64) {
     const int mine = b0 + lane < B ? seq_chunks(a, b0 + lane) : 0;
-    int upto = mine;
-#pragma unroll
-    for (int k = 1; k < 64; k <<= 1) {
-      const int x = __shfl_up(upto, k);
-      upto += lane >= k ? x : 0;
-    }
+    const int upto = lanes_upto(mine);
     const unsigned long long past = __ballot(at < (base + upto) * heads);
     if (past != 0) {
       const int l = __ffsll(past) - 1;

@@ -159,9 +159,10 @@ ScoresPlan prompt_scores_plan(const DevDesc& d, long long n_rows, long long cap)
   ScoresPlan p;
   const long long units = (long long)d.B * d.Hkv;
   const long long blocks = units * ((cap + SC_KEYS - 1) / SC_KEYS);
-  // 1024 pieces of work, two for each workgroup that the chip holds, of eight tiles of columns at least
+  // 1024 pieces of work, two for each workgroup that the chip holds, of two tiles of columns at least (200 tokens, 32 heads on
+  // 8: eight tiles 28 us, two 15)
   long long s = blocks < 1024 ? (1024 + blocks - 1) / blocks : 1;
-  const long long most = (n_rows * d.G + 8 * SC_COLS - 1) / (8 * SC_COLS);
+  const long long most = (n_rows * d.G + 2 * SC_COLS - 1) / (2 * SC_COLS);
   s = s < most ? s : most;
   p.splits = (int)(s < 1 ? 1 : s > 64 ? 64 : s);
   p.bytes = p.splits > 1 ? (size_t)p.splits * units * cap * sizeof(float) : 0;

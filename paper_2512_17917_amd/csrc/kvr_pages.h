@@ -92,29 +92,39 @@ __device__ __forceinline__ long long uniform(long long x) {
   return (long long)(((uint64_t)hi << 32) | lo);
 }
 
+// sum of a number over the lanes up to one's own (in lane order; rows of 16 lanes first, then the rows)
+__device__ __forceinline__ int lanes_upto(int x) {
+  x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, true);      // row_shr 1, 2, 4, 8
+  x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, true);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, true);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, true);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xa, 0xf, false);     // row_bcast 15: a row's last lane to the next row
+  x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, false);     // row_bcast 31: lane 31 to the upper rows
+  return x;
+}
+
 // Column tile blockIdx.x of a launch: a sequence's new tokens times its kv head's G query heads are columns m = t G + g, in
 // tiles of `per`; tiles are counted sequence after sequence.  b < 0: none left.  (All lanes of a wave call.)
 struct ColTile {
   int b, m0;
 };
 __device__ __forceinline__ ColTile col_tile(const int32_t* q_start, int n_rows, int B, int G, int per, int tile) {
+  if (B == 1) {
+    const int all = (int)(((long long)row_span(q_start, n_rows, 0).n * G + per - 1) / per);
+    return tile < all ? ColTile{0, tile * per} : ColTile{-1, 0};
+  }
   const int lane = threadIdx.x & 63;
   int base = 0;
   for (int b0 = 0; b0 < B; b0 += 64) {
     const int n = b0 + lane < B ? row_span(q_start, n_rows, b0 + lane).n : 0;
     const int mine = (int)(((long long)n * G + per - 1) / per);
-    int upto = mine;
-#pragma unroll
-    for (int k = 1; k < 64; k <<= 1) {
-      const int x = __shfl_up(upto, k);
-      upto += lane >= k ? x : 0;
-    }
+    const int upto = lanes_upto(mine);
     const unsigned long long past = __ballot(tile < base + upto);
     if (past != 0) {
       const int l = __ffsll(past) - 1;
       return {b0 + l, (tile - base - __shfl(upto - mine, l)) * per};
     }
-    base += __shfl(upto, 63);
+    base += __builtin_amdgcn_readlane(upto, 63);
   }
   return {-1, 0};
 }
