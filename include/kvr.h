@@ -515,10 +515,11 @@ int32_t kvr_rotate(const kvr_desc* desc, const kvr_rotation* rot, const void* q,
  *     p[t, hq, j] = softmax over visible j of softmax_scale * q[t, hq] . k[j]
  *     out[t, hq]  = sum_j p[t, hq, j] v[j]
  * and, if scores is not NULL, every token's cumulative score grows by the sum of p over the new
- * tokens and the G q heads of its kv head, always in the same order.  A query that sees no token
- * yields zeros.  n_ctx is clamped to what the cache can hold.  KVR_ERR_UNSUPPORTED where B * Hkv
- * times the tokens that a sequence can hold passes 2^37.  Tokens that no query of a row sees
- * may hold anything, Inf and NaN too.
+ * tokens and the G q heads of its kv head, always in the same order.  A query that sees no token,
+ * or none whose logit is above -Inf, yields zeros; NaN among the logits that it sees gives NaN in
+ * its output and in the scores of the tokens that it sees.  n_ctx is clamped to what the cache
+ * can hold.  KVR_ERR_UNSUPPORTED where B * Hkv times the tokens that a sequence can hold passes
+ * 2^37.  Tokens that no query of a row sees may hold anything, Inf and NaN too.
  *   q          dev [n_rows, Hq, D] storage type, read
  *   pages      host; k, v and table are read
  *   window     0: no window

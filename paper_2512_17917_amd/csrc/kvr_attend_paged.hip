@@ -314,10 +314,11 @@ __device__ __forceinline__ void walk(const DevDesc& d, const PagedArgs& a, int b
       scale_acc<G>(w.acc, corr);
     }
     w.m = m_new;
+    const float m_use = m_new == NEG_INF ? 0.f : m_new;       // (no logit above -inf so far: weights of 0, not of inf - inf)
     float pr[4];
 #pragma unroll
     for (int x = 0; x < 4; ++x) {
-      pr[x] = (dead >> x) & 1 ? 0.f : exp2_(s[x] - m_new);
+      pr[x] = (dead >> x) & 1 ? 0.f : exp2_(s[x] - m_use);
       w.l += pr[x];
     }
 #pragma unroll
@@ -363,7 +364,8 @@ __device__ __forceinline__ void to_shared(Sums<G>& w, float (&s_o)[G][D], float 
     }
   }
 }
-// the waves' sums together: head g, channel c
+// The waves' sums together: head g, channel c.  (Without a logit above -inf the maximum is -inf and the sum 0, or NaN where
+// one is NaN: parts go in with a factor 0, not unseen, here and wherever parts are joined.)
 struct Joined {
   float m, l, o;
 };
@@ -383,7 +385,7 @@ __device__ __forceinline__ Joined join_waves(const float (&s_o)[WAVES][G][D], co
 }
 template <typename T>
 __device__ __forceinline__ void put_out(const DevDesc& d, const PagedArgs& a, int b, int head, int c, const Joined& r) {
-  Store<T>::store1((T*)a.out + ((size_t)b * d.Hq + head) * D + c, r.m == -__builtin_inff() ? 0.f : r.o / r.l);
+  Store<T>::store1((T*)a.out + ((size_t)b * d.Hq + head) * D + c, r.l == 0.f ? 0.f : r.o / r.l);
 }
 
 // logits of a wave's tiles, PG_KEEP at a time through LDS to memory
@@ -488,6 +490,9 @@ __global__ __launch_bounds__(64 * PG_WAVES, paged_per_cu(sizeof(T), G)) void pag
   }
 }
 
+// (a token that is not seen has none, also where the sum is NaN)
+__device__ __forceinline__ float weight_of(float s, float lse) { return s == -__builtin_inff() ? 0.f : exp2_(s - lse); }
+
 // Caches of few tokens: a workgroup of as many waves as a CU takes has a whole unit, and nothing is left to join.
 template <typename T, int G, bool ONE>
 __global__ __launch_bounds__(64 * short_waves(sizeof(T), G)) void paged_short_kernel(DevDesc d, PagedArgs a) {
@@ -510,14 +515,14 @@ __global__ __launch_bounds__(64 * short_waves(sizeof(T), G)) void paged_short_ke
 #pragma unroll
   for (int g = 0; g < G; ++g) {
     const Joined r = join_waves<WAVES, G>(s_o, s_m, s_l, g, 0);
-    lse[g] = r.m == -__builtin_inff() ? __builtin_inff() : r.m + __builtin_amdgcn_logf(r.l);
+    lse[g] = r.l == 0.f ? __builtin_inff() : r.m + __builtin_amdgcn_logf(r.l);
   }
   for (int e = threadIdx.x; e < tr.n * 16; e += 64 * WAVES) {
     const int j = tile_token<16>(tr, e >> 4) + (e & 15);
     if (j >= n || j >= a.n_cap) continue;
     float sum = 0.f;
 #pragma unroll
-    for (int g = 0; g < G; ++g) sum += exp2_(s_log[e * G + g] - lse[g]);
+    for (int g = 0; g < G; ++g) sum += weight_of(s_log[e * G + g], lse[g]);
     if (sum != 0.f) a.scores[(size_t)u * a.n_cap + j] += sum;
   }
 }
@@ -551,22 +556,22 @@ __global__ __launch_bounds__(256) void paged_join_kernel(DevDesc d, PagedArgs a,
         const int i = min(i0 + 2 * x, parts - 1);
         const float2 ml = *reinterpret_cast<const float2*>(part_ml + ((slot0 + i) * G + g) * 2);
         pm[x] = i0 + 2 * x < parts ? ml.x : NEG_INF;
-        pl[x] = ml.y;
-        po[x] = part_o[((slot0 + i) * G + g) * D + c];
+        pl[x] = i0 + 2 * x < parts ? ml.y : 0.f;
+        const float po_i = part_o[((slot0 + i) * G + g) * D + c];
+        po[x] = i0 + 2 * x < parts ? po_i : 0.f;
       }
       float mn = m;
 #pragma unroll
       for (int x = 0; x < 16; ++x) mn = fmaxf(mn, pm[x]);
-      if (mn == NEG_INF) continue;
-      const float f = exp2_(m - mn);            // (2^-inf: 0)
+      const float m_use = mn == NEG_INF ? 0.f : mn, f = exp2_(m - m_use);            // (2^-inf: 0)
       l *= f;
       o *= f;
       m = mn;
 #pragma unroll
       for (int x = 0; x < 16; ++x) {
-        const float e = exp2_(pm[x] - m);
-        l = fmaf(e, pm[x] == NEG_INF ? 0.f : pl[x], l);
-        o = fmaf(e, pm[x] == NEG_INF ? 0.f : po[x], o);
+        const float e = exp2_(pm[x] - m_use);
+        l = fmaf(e, pl[x], l);
+        o = fmaf(e, po[x], o);
       }
     }
     float* s_ml = &s_m[0][0];                   // [2]
@@ -581,8 +586,8 @@ __global__ __launch_bounds__(256) void paged_join_kernel(DevDesc d, PagedArgs a,
     if (odd == 0) {
       const float m1 = s_ml[0], mn = fmaxf(m, m1);
       const float f0 = m == NEG_INF ? 0.f : exp2_(m - mn), f1 = m1 == NEG_INF ? 0.f : exp2_(m1 - mn);
-      const float r = (f0 * o + f1 * s_sum[c]) / (f0 * l + f1 * s_l[0][0]);
-      Store<T>::store1((T*)a.out + ((size_t)b * d.Hq + h * G + g) * D + c, mn == NEG_INF ? 0.f : r);
+      const float sum = f0 * l + f1 * s_l[0][0], r = (f0 * o + f1 * s_sum[c]) / sum;
+      Store<T>::store1((T*)a.out + ((size_t)b * d.Hq + h * G + g) * D + c, sum == 0.f ? 0.f : r);
     }
     return;
   }
@@ -591,14 +596,14 @@ __global__ __launch_bounds__(256) void paged_join_kernel(DevDesc d, PagedArgs a,
   for (int i = threadIdx.x / G; i < parts; i += 256 / G) {
     const float2 ml = *reinterpret_cast<const float2*>(part_ml + ((slot0 + i) * G + threadIdx.x % G) * 2);
     const float mn = fmaxf(m, ml.x);
-    l = (m == NEG_INF ? 0.f : l * exp2_(m - mn)) + (ml.x == NEG_INF ? 0.f : ml.y * exp2_(ml.x - mn));
+    l = l * (m == NEG_INF ? 0.f : exp2_(m - mn)) + ml.y * (ml.x == NEG_INF ? 0.f : exp2_(ml.x - mn));
     m = mn;
   }
 #pragma unroll
   for (int k = G; k < 64; k <<= 1) {
     const float om = __shfl_xor(m, k), ol = __shfl_xor(l, k);
     const float mn = fmaxf(m, om);
-    l = (m == NEG_INF ? 0.f : l * exp2_(m - mn)) + (om == NEG_INF ? 0.f : ol * exp2_(om - mn));
+    l = l * (m == NEG_INF ? 0.f : exp2_(m - mn)) + ol * (om == NEG_INF ? 0.f : exp2_(om - mn));
     m = mn;
   }
   if (lane < G) {
@@ -612,8 +617,8 @@ __global__ __launch_bounds__(256) void paged_join_kernel(DevDesc d, PagedArgs a,
     const float mg = fmaxf(fmaxf(s_m[0][g], s_m[1][g]), fmaxf(s_m[2][g], s_m[3][g]));
     float lg = 0.f;
 #pragma unroll
-    for (int x = 0; x < 4; ++x) lg += s_m[x][g] == NEG_INF ? 0.f : s_l[x][g] * exp2_(s_m[x][g] - mg);
-    lse[g] = mg == NEG_INF ? __builtin_inff() : mg + __builtin_amdgcn_logf(lg);
+    for (int x = 0; x < 4; ++x) lg += s_l[x][g] * (s_m[x][g] == NEG_INF ? 0.f : exp2_(s_m[x][g] - mg));
+    lse[g] = lg == 0.f ? __builtin_inff() : mg + __builtin_amdgcn_logf(lg);
   }
   // four tokens a thread, all their numbers asked for at once
   float lo[PG_SLICE / 256][G], old[PG_SLICE / 256];
@@ -633,7 +638,7 @@ __global__ __launch_bounds__(256) void paged_join_kernel(DevDesc d, PagedArgs a,
   for (int i = 0; i < PG_SLICE / 256; ++i) {
     float sum = 0.f;
 #pragma unroll
-    for (int g = 0; g < G; ++g) sum += exp2_(lo[i][g] - lse[g]);
+    for (int g = 0; g < G; ++g) sum += weight_of(lo[i][g], lse[g]);
     if (at[i] >= 0 && sum != 0.f) a.scores[(size_t)u * a.n_cap + at[i]] = old[i] + sum;
   }
 }

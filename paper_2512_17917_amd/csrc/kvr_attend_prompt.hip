@@ -135,10 +135,11 @@ __global__ __launch_bounds__(64 * PP_WAVES) void prompt_f32_kernel(DevDesc d, Pa
         for (int x = 0; x < 4; ++x) o[cb][x] *= corr;
     }
     m_run = m_new;
+    const float m_use = m_new == NEG_INF ? 0.f : m_new;       // (no logit above -inf so far: weights of 0)
     f32x4_t p;
 #pragma unroll
     for (int x = 0; x < 4; ++x) {
-      p[x] = (seen >> x) & 1 ? exp2_(s[x] - m_new) : 0.f;
+      p[x] = (seen >> x) & 1 ? exp2_(s[x] - m_use) : 0.f;
       l_run += p[x];
     }
 #pragma unroll
@@ -196,12 +197,12 @@ __global__ __launch_bounds__(64 * PP_WAVES) void prompt_f32_kernel(DevDesc d, Pa
 #pragma unroll
     for (int e = 0; e < 8; ++e) sum[e] = fmaf(f, s_o[w][c][ch + e], sum[e]);
   }
-  const float inv = mx == NEG_INF ? 0.f : 1.f / l;          // no token seen: zeros
+  const float inv = l == 0.f ? 0.f : 1.f / l;               // no token seen: zeros
   const size_t to = (size_t)(span.first + (mc >> gs)) * d.Hq + hk * d.G + (mc & (d.G - 1));
   float4* out = reinterpret_cast<float4*>((float*)a.out + to * D + ch);
   out[0] = make_float4(sum[0] * inv, sum[1] * inv, sum[2] * inv, sum[3] * inv);
   out[1] = make_float4(sum[4] * inv, sum[5] * inv, sum[6] * inv, sum[7] * inv);
-  if (lse && ch == 0) lse[to] = mx == NEG_INF ? __builtin_inff() : mx + __builtin_amdgcn_logf(l);
+  if (lse && ch == 0) lse[to] = l == 0.f ? __builtin_inff() : mx + __builtin_amdgcn_logf(l);
 }
 
 __global__ __launch_bounds__(64 * PP_WAVES) void prompt_scores_f32_kernel(DevDesc d, PagedArgs a, const float* lse) {

@@ -447,7 +447,7 @@ __global__ __launch_bounds__(64 * FP_WAVES, 2) void prompt_bf16_kernel(DevDesc d
     }
     return;
   }
-  const float inv = m_run == NEG_INF ? 0.f : 1.f / l_run;
+  const float inv = l_run == 0.f ? 0.f : 1.f / l_run;
   uint2* out = reinterpret_cast<uint2*>((bf16_t*)po.out + at * D);
 #pragma unroll
   for (int cb = 0; cb < 4; ++cb)
@@ -457,7 +457,7 @@ __global__ __launch_bounds__(64 * FP_WAVES, 2) void prompt_bf16_kernel(DevDesc d
       const bf16x2_t y1 = __builtin_convertvector((f32x2_t{o[cb][x + 2] * inv, o[cb][x + 3] * inv}), bf16x2_t);
       out[(32 * cb + 8 * (x / 4) + 4 * half) / 4] = make_uint2(__builtin_bit_cast(uint32_t, y0), __builtin_bit_cast(uint32_t, y1));
     }
-  if (po.lse && half == 0) po.lse[at] = m_run == NEG_INF ? __builtin_inff() : m_run + __builtin_amdgcn_logf(l_run);
+  if (po.lse && half == 0) po.lse[at] = l_run == 0.f ? __builtin_inff() : m_run + __builtin_amdgcn_logf(l_run);
 }
 
 // Joins the parts of a row and head: a wave each, lane l channels 2 l and 2 l + 1; eight parts' numbers are asked for at once.
@@ -477,30 +477,31 @@ __global__ __launch_bounds__(256) void prompt_join_kernel(DevDesc d, PagedArgs a
       const long long slot = min(s0 + e, splits - 1) * all + at;
       ml[e] = *reinterpret_cast<const float2*>(po.part_ml + 2 * slot);
       v[e] = *reinterpret_cast<const float2*>(po.part_o + slot * D + 2 * lane);
-      if (s0 + e >= splits) ml[e].x = NEG_INF;
+      if (s0 + e >= splits) {
+        ml[e] = make_float2(NEG_INF, 0.f);
+        v[e] = make_float2(0.f, 0.f);
+      }
     }
     float mn = m;
 #pragma unroll
     for (int e = 0; e < 8; ++e) mn = fmaxf(mn, ml[e].x);
-    if (mn == NEG_INF) continue;
-    const float f = exp2_(m - mn);
+    const float m_use = mn == NEG_INF ? 0.f : mn, f = exp2_(m - m_use);
     l *= f;
     x *= f;
     y *= f;
     m = mn;
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
-      const bool some = ml[e].x != NEG_INF;       // (a part that saw nothing may hold anything)
-      const float w = exp2_(ml[e].x - m);
-      l = fmaf(w, some ? ml[e].y : 0.f, l);
-      x = fmaf(w, some ? v[e].x : 0.f, x);
-      y = fmaf(w, some ? v[e].y : 0.f, y);
+      const float w = exp2_(ml[e].x - m_use);     // (a part without a logit above -inf: 0 times sums of 0, or of NaN)
+      l = fmaf(w, ml[e].y, l);
+      x = fmaf(w, v[e].x, x);
+      y = fmaf(w, v[e].y, y);
     }
   }
-  const float inv = m == NEG_INF ? 0.f : 1.f / l;
+  const float inv = l == 0.f ? 0.f : 1.f / l;
   const bf16x2_t r = __builtin_convertvector((f32x2_t{x * inv, y * inv}), bf16x2_t);
   reinterpret_cast<uint32_t*>((bf16_t*)po.out + at * D)[lane] = __builtin_bit_cast(uint32_t, r);
-  if (po.lse && lane == 0) po.lse[at] = m == NEG_INF ? __builtin_inff() : m + __builtin_amdgcn_logf(l);
+  if (po.lse && lane == 0) po.lse[at] = l == 0.f ? __builtin_inff() : m + __builtin_amdgcn_logf(l);
 }
 
 }  // namespace

@@ -7,6 +7,8 @@
 // multiply-add and a sum.  A token early in a prompt has the most columns: its block goes first, and where the blocks of
 // tokens are few its columns are shared out over several workgroups, whose sums a second kernel adds in order.  4 x 2048 tokens,
 // 32 heads on 8: 118 us (200 with blocks next to each other in the grid, which gives one die all the early ones).
+#include <type_traits>
+
 #include "kvr_launch.h"
 #include "kvr_prompt.h"
 
@@ -118,15 +120,23 @@ __global__ __launch_bounds__(64 * SC_WAVES, 2) void prompt_scores_bf16_kernel(De
           for (int kb = 0; kb < 2; ++kb) s[kb][x] = sees(a.vis, P, jw + 32 * kb + col) ? s[kb][x] : -__builtin_inff();
         }
       }
+      // (a token that is not seen has no weight, also where the column's sum is NaN)
+      auto add = [&](auto all_seen) {
 #pragma unroll
-      for (int x = 0; x < 16; x += 4) {
-        const float4 l = *reinterpret_cast<const float4*>(&s_lse[buf][32 * cb + 2 * x + 4 * half]);
-        const float le[4] = {l.x, l.y, l.z, l.w};
+        for (int x = 0; x < 16; x += 4) {
+          const float4 l = *reinterpret_cast<const float4*>(&s_lse[buf][32 * cb + 2 * x + 4 * half]);
+          const float le[4] = {l.x, l.y, l.z, l.w};
 #pragma unroll
-        for (int kb = 0; kb < 2; ++kb)
+          for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
-          for (int e = 0; e < 4; ++e) acc[kb] += exp2_(fmaf(s[kb][x + e], sc.c, -le[e]));
-      }
+            for (int e = 0; e < 4; ++e) {
+              const float w = exp2_(fmaf(s[kb][x + e], sc.c, -le[e]));
+              acc[kb] += decltype(all_seen)::value || s[kb][x + e] != -__builtin_inff() ? w : 0.f;
+            }
+        }
+      };
+      if (whole) add(std::true_type{});
+      else add(std::false_type{});
     }
   }
 #pragma unroll

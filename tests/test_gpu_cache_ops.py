@@ -325,6 +325,90 @@ def test_values_that_later_queries_alone_see(dtype, value):
     _check("prompt", dtype, (8, 2), 16, [130], [130], 20, 2, 130, seed=4, edit=edit)
 
 
+# the calls' routes: few tokens, many, and few columns over many
+ROUTES = [("prompt", BF, [100, 32], [100, 32]), ("prompt", BF, [3000, 32], [4, 3]), ("prompt", F32, [130, 32], [130, 32]),
+          ("paged", BF, [100, 32], None), ("paged", BF, [3000, 32], None), ("paged", F32, [100, 32], None), ("paged", F32, [3000, 32], None)]
+
+
+def _odd_call(which, dtype, n, new, change):
+    """-> result of a call on operands that change(q, kp, vp, table) has altered, and of float64 on what it returns."""
+    g = torch.Generator().manual_seed(17)
+    q_start = None if new is None else _starts(new)
+    rows = 2 if new is None else q_start[-1]
+    kp, vp, table = _cache(g, 2, 2, max(n), 16, dtype)
+    q = _normal(g, rows, 8, D, dtype=dtype)
+    d = kvr.make_desc(2, 8, 2, 1, 1, dtype)
+    as_if = change(q, kp, vp, table)
+    old = torch.rand(2, 2, max(n), generator=g)
+    q_d, kp_d, vp_d, table_d, sc = _dev(q, kp, vp, table, old)
+    qs = None if q_start is None else torch.tensor(q_start, dtype=torch.int32).cuda()
+    nc = torch.tensor(n, dtype=torch.int32).cuda()
+    out = _attend(which, d, q_d, rows, qs, nc, kvr.make_pages(d, kp_d, vp_d, table_d), 0, 0, sc, max(n))
+    ref = R.attend(*as_if, n, q_start, d.softmax_scale, 0, 0, max(n), 2)
+    tol, tol_s = R.attend_bounds(ref, dtype, old)
+    off = (out.cpu().double() - ref["out"]).abs() / tol
+    off_s = (sc.cpu().double() - old.double() - ref["scores"]).abs() / tol_s
+    return out.cpu(), sc.cpu(), off, off_s, q_start
+
+
+@pytest.mark.parametrize("case", range(len(ROUTES)))
+def test_logits_of_minus_infinity(case):
+    """Tokens whose logit is -inf for every head weigh nothing, also where they come first or fill tiles; a query that sees
+    no others yields zeros (the second sequence)."""
+    which, dtype, n, new = ROUTES[case]
+
+    def change(q, kp, vp, table):
+        q[..., 0] = -1
+        less = table.clone()
+        for b, pages in ((0, [0, 1, 2, 3, 5]), (1, [0, 1])):
+            for i in pages:
+                kp[int(table[b, i]), :, :, 0] = float("inf")
+                less[b, i] = -1
+        return q, kp, vp, less
+
+    out, sc, off, off_s, q_start = _odd_call(which, dtype, n, new, change)
+    assert float(off.max()) <= 1 and float(off_s.max()) <= 1
+    second = out[1:] if new is None else out[q_start[1]:]
+    assert not bool(second.any())
+
+
+@pytest.mark.parametrize("case", range(len(ROUTES)))
+def test_nan_in_a_query_or_a_key_stays_with_who_sees_it(case):
+    which, dtype, n, new = ROUTES[case]
+    first = n[0] - (1 if new is None else new[0])                # position of the first sequence's first row
+    row, head = (0, 3) if new is None else (new[0] // 2, 3)
+
+    def query(q, kp, vp, table):
+        clean = q.clone(), kp, vp, table
+        q[row, head, 77] = float("nan")
+        return clean
+
+    out, sc, off, off_s, _ = _odd_call(which, dtype, n, new, query)
+    assert bool(out[row, head].isnan().all())
+    off[row, head] = 0
+    assert float(off.max()) <= 1
+    sees = first + row + 1
+    assert bool(sc[0, 0, :sees].isnan().all())
+    off_s[0, 0, :sees] = 0
+    assert float(off_s.max()) <= 1
+
+    j = max(first + row, 0)                                      # a token that the rows from `row` on see
+
+    def key(q, kp, vp, table):
+        clean = q, kp.clone(), vp, table
+        kp[int(table[0, j // 16]), 1, j % 16, 5] = float("nan")
+        return clean
+
+    out, sc, off, off_s, q_start = _odd_call(which, dtype, n, new, key)
+    end = 1 if new is None else q_start[1]
+    assert bool(out[row:end, 4:].isnan().all())
+    off[row:end, 4:] = 0
+    assert float(off.max()) <= 1
+    assert bool(sc[0, 1, :n[0]].isnan().all())
+    off_s[0, 1] = 0
+    assert float(off_s.max()) <= 1
+
+
 @pytest.mark.parametrize("which", ["prompt", "paged"])
 @pytest.mark.parametrize("scale", [0.0, -0.05, 0.5])
 def test_scales(which, scale):
