@@ -65,30 +65,116 @@ __global__ __launch_bounds__(64 * SC_WAVES, 2) void prompt_scores_bf16_kernel(De
     }
   }
 
-  // rows of a tile to LDS: 16 columns of 256 bytes a wave, piece c of row r at c ^ (r mod 16)
+  // Rows of a tile to LDS: 16 columns of 256 bytes a wave, piece c of row r at c ^ (r mod 16).  A tile holds whole tokens (G
+  // divides 64): from one to the next only the rows' start, a scalar, is new, until the last, which may be short.
   const uint32_t lds0 = lds_offset(s_q);
   const uint32_t lds1 = lds_offset(s_lse);
+  auto row_at = [&](int m) { return (size_t)(m >> gs) * d.Hq + (m & (d.G - 1)); };         // of column m, from column 0's
+  const size_t at0 = (size_t)span.first * d.Hq + hk * d.G;
+  uint32_t q_off[4];
+#pragma unroll
+  for (int x = 0; x < 4; ++x) {
+    const int r = 16 * wave + 4 * x + (lane >> 4);
+    q_off[x] = (uint32_t)row_at(r) * (D * 2) + (((lane & 15) ^ (r & 15)) << 4);
+  }
+  const uint32_t lse_off = (uint32_t)row_at(lane) * 4;
   auto fetch = [&](int i, int buf) {                 // five loads a wave
     const int m0 = c0 + i * SC_COLS;
+    const uint32_t to_q = lds0 + buf * SC_TILE + 16 * wave * 256, to_lse = lds1 + buf * SC_COLS * 4;
+    if (m0 + SC_COLS <= cols) {
+      const size_t at = at0 + row_at(m0);
+      const unsigned char* from = (const unsigned char*)a.q + at * (D * 2);
+#pragma unroll
+      for (int x = 0; x < 4; ++x) to_lds(from, q_off[x], uniform((int)(to_q + 4 * x * 256)));
+      word_to_lds(lse + at, lse_off, uniform((int)to_lse));        // (all waves fetch the same)
+      return;
+    }
 #pragma unroll
     for (int x = 0; x < 4; ++x) {
       const int r = 16 * wave + 4 * x + (lane >> 4);
-      const int m = min(m0 + r, cols - 1);
-      const size_t at = (size_t)(span.first + (m >> gs)) * d.Hq + hk * d.G + (m & (d.G - 1));
-      to_lds((const unsigned char*)a.q + at * (D * 2) + (((lane & 15) ^ (r & 15)) << 4),
-             uniform((int)(lds0 + buf * SC_TILE + (16 * wave + 4 * x) * 256)));
+      to_lds((const unsigned char*)a.q + (at0 + row_at(min(m0 + r, cols - 1))) * (D * 2) + (((lane & 15) ^ (r & 15)) << 4),
+             uniform((int)(to_q + 4 * x * 256)));
     }
-    const int m = min(m0 + lane, cols - 1);          // (all waves fetch the same)
-    word_to_lds(lse + (size_t)(span.first + (m >> gs)) * d.Hq + hk * d.G + (m & (d.G - 1)), uniform((int)(lds1 + buf * SC_COLS * 4)));
+    word_to_lds(lse + at0 + row_at(min(m0 + lane, cols - 1)), uniform((int)to_lse));
   };
 
+  // the columns that see a lane's token: seen_n[] from seen0[] on (the same as `sees`: new tokens t with j <= first + t < j + window)
+  int seen0[2];
+  uint32_t seen_n[2];
+#pragma unroll
+  for (int kb = 0; kb < 2; ++kb) {
+    const int j = jw + 32 * kb + col, t_from = clampi(j - first, 0, span.n);
+    const int t_upto = a.vis.window > 0 && j >= a.vis.n_sink ? (int)min((long long)j + a.vis.window - first, (long long)span.n) : span.n;
+    seen0[kb] = t_from << gs;
+    seen_n[kb] = t_upto > t_from ? (uint32_t)(t_upto - t_from) << gs : 0u;
+  }
+
   float acc[2] = {0.f, 0.f};
+  int buf = 0;
+  uint32_t q_at[8], l_at;                            // of a lane's operands in LDS
+  auto find = [&] {
+#pragma unroll
+    for (int c = 0; c < 8; ++c) {
+      q_at[c] = buf * SC_TILE + col * 256 + (((2 * c + half) ^ (col & 15)) << 4);
+      asm volatile("" : "+v"(q_at[c]));              // (before the products, not among them)
+    }
+    l_at = buf * (SC_COLS / 4) + half;
+    asm volatile("" : "+v"(l_at));
+  };
+  auto product = [&](f32x16_t (&s)[2], int cb) {     // s = Q K^T of 32 columns
+#pragma unroll
+    for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+      for (int x = 0; x < 16; ++x) s[kb][x] = 0.f;
+#pragma unroll
+    for (int c = 0; c < 8; ++c) {
+      const bf16x8_t q = *reinterpret_cast<const bf16x8_t*>(s_q + q_at[c] + 32 * 256 * cb);
+#pragma unroll
+      for (int kb = 0; kb < 2; ++kb) s[kb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(q, k[kb][c], s[kb], 0, 0, 0);
+    }
+  };
+  auto sums = [&](float (&le)[16], int cb) {         // the columns' lse
+#pragma unroll
+    for (int x = 0; x < 16; x += 4) {
+      const float4 l = reinterpret_cast<const float4*>(&s_lse[0][0])[l_at + 8 * cb + x / 2];
+      le[x] = l.x, le[x + 1] = l.y, le[x + 2] = l.z, le[x + 3] = l.w;
+    }
+  };
+  auto add = [&](const f32x16_t (&s)[2], const float (&le)[16]) {
+#pragma unroll
+    for (int x = 0; x < 16; ++x)
+#pragma unroll
+      for (int kb = 0; kb < 2; ++kb) acc[kb] += exp2_(fmaf(s[kb][x], sc.c, -le[x]));
+  };
+  // a half's products between a half's weights, twelve reads of LDS
+  auto interleave = [&](auto half) {
+    constexpr int H = decltype(half)::value;
+    __builtin_amdgcn_sched_group_barrier(0x100, 4, H);
+#pragma unroll
+    for (int x = 0; x < 8; ++x) {
+      __builtin_amdgcn_sched_group_barrier(0x008, 1, H);
+      __builtin_amdgcn_sched_group_barrier(0x002, 6, H);
+      __builtin_amdgcn_sched_group_barrier(0x100, 1, H);
+    }
+#pragma unroll
+    for (int x = 0; x < 8; ++x) {
+      __builtin_amdgcn_sched_group_barrier(0x008, 1, H);
+      __builtin_amdgcn_sched_group_barrier(0x002, 6, H);
+    }
+  };
+
+  // The weights of a half tile, 32 columns, are computed beside the products of the next: those of a tile's second half
+  // wait for the next tile that the wave sees whole.
+  f32x16_t s0[2], s1[2];
+  float le0[16], le1[16];
+#pragma unroll
+  for (int x = 0; x < 16; ++x) s1[0][x] = s1[1][x] = -__builtin_inff(), le1[x] = 0.f;
   if (i0 < i1) fetch(i0, 0);
   if (i0 + 1 < i1) fetch(i0 + 1, 1);
-  int buf = 0;
   for (int i = i0; i < i1; ++i, buf = buf == SC_BUFS - 1 ? 0 : buf + 1) {
-    if (i + 1 < i1) asm volatile("s_waitcnt vmcnt(5)" ::: "memory");
-    else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    // this tile has come, and this wave's reads of the last one are done
+    if (i + 1 < i1) asm volatile("s_waitcnt vmcnt(5) lgkmcnt(0)" ::: "memory");
+    else asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
     __builtin_amdgcn_sched_barrier(0);
     asm volatile("s_barrier" ::: "memory");
     __builtin_amdgcn_sched_barrier(0);
@@ -96,49 +182,38 @@ __global__ __launch_bounds__(64 * SC_WAVES, 2) void prompt_scores_bf16_kernel(De
     const int m0 = c0 + i * SC_COLS;
     const int lo = first + (m0 >> gs), hi = first + ((min(m0 + SC_COLS, cols) - 1) >> gs);   // positions of the columns
     if (jw > hi || jw >= n || (a.vis.window > 0 && jw + 63 <= lo - a.vis.window && jw >= a.vis.n_sink)) continue;
-    const bool whole = jw + 63 <= lo && m0 + SC_COLS <= cols && (a.vis.window == 0 || jw > hi - a.vis.window || jw + 63 < a.vis.n_sink);
-    const unsigned char* tq = s_q + buf * SC_TILE;
+    if (jw + 63 <= lo && m0 + SC_COLS <= cols && (a.vis.window == 0 || jw > hi - a.vis.window || jw + 63 < a.vis.n_sink)) {
+      find();
+      __builtin_amdgcn_sched_barrier(0);
+      product(s0, 0);
+      add(s1, le1);
+      sums(le0, 0);
+      interleave(std::integral_constant<int, 0>{});
+      __builtin_amdgcn_sched_barrier(0);
+      product(s1, 1);
+      add(s0, le0);
+      sums(le1, 1);
+      interleave(std::integral_constant<int, 1>{});
+      __builtin_amdgcn_sched_barrier(0);
+      continue;
+    }
+    find();
 #pragma unroll
     for (int cb = 0; cb < 2; ++cb) {
-      f32x16_t s[2];
+      product(s0, cb);
+      sums(le0, cb);
 #pragma unroll
-      for (int kb = 0; kb < 2; ++kb)
-#pragma unroll
-        for (int x = 0; x < 16; ++x) s[kb][x] = 0.f;
-#pragma unroll
-      for (int c = 0; c < 8; ++c) {
-        const bf16x8_t q = *reinterpret_cast<const bf16x8_t*>(tq + (32 * cb + col) * 256 + (((2 * c + half) ^ (col & 15)) << 4));
-#pragma unroll
-        for (int kb = 0; kb < 2; ++kb) s[kb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(q, k[kb][c], s[kb], 0, 0, 0);
-      }
-      if (!whole) {
+      for (int kb = 0; kb < 2; ++kb) {
+        const int from = seen0[kb] - (m0 + 32 * cb + 4 * half);
 #pragma unroll
         for (int x = 0; x < 16; ++x) {
-          const int m = m0 + 32 * cb + 8 * (x / 4) + 4 * half + x % 4;
-          const int P = m < cols ? first + (m >> gs) : -1;
-#pragma unroll
-          for (int kb = 0; kb < 2; ++kb) s[kb][x] = sees(a.vis, P, jw + 32 * kb + col) ? s[kb][x] : -__builtin_inff();
+          const float w = exp2_(fmaf(s0[kb][x], sc.c, -le0[x]));
+          acc[kb] += (uint32_t)(8 * (x / 4) + x % 4 - from) < seen_n[kb] ? w : 0.f;      // (not w times 0: w may be NaN)
         }
       }
-      // (a token that is not seen has no weight, also where the column's sum is NaN)
-      auto add = [&](auto all_seen) {
-#pragma unroll
-        for (int x = 0; x < 16; x += 4) {
-          const float4 l = *reinterpret_cast<const float4*>(&s_lse[buf][32 * cb + 2 * x + 4 * half]);
-          const float le[4] = {l.x, l.y, l.z, l.w};
-#pragma unroll
-          for (int kb = 0; kb < 2; ++kb)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              const float w = exp2_(fmaf(s[kb][x + e], sc.c, -le[e]));
-              acc[kb] += decltype(all_seen)::value || s[kb][x + e] != -__builtin_inff() ? w : 0.f;
-            }
-        }
-      };
-      if (whole) add(std::true_type{});
-      else add(std::false_type{});
     }
   }
+  add(s1, le1);
 #pragma unroll
   for (int kb = 0; kb < 2; ++kb) {
     const float sum = across_sum(acc[kb]);
