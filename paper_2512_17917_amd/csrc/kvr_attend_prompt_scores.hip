@@ -244,9 +244,9 @@ ScoresPlan prompt_scores_plan(const DevDesc& d, long long n_rows, long long cap)
   ScoresPlan p;
   const long long units = (long long)d.B * d.Hkv;
   const long long blocks = units * ((cap + SC_KEYS - 1) / SC_KEYS);
-  // 1024 pieces of work, two for each workgroup that the chip holds, of two tiles of columns at least (200 tokens, 32 heads on
-  // 8: eight tiles 28 us, two 15)
-  long long s = blocks < 1024 ? (1024 + blocks - 1) / blocks : 1;
+  // 768 pieces of work, three for two workgroups that the chip holds (2 x 600 tokens, 32 heads on 8, the whole call: 1024 pieces
+  // 53 us, 768 49, 512 48; 4 x 2k 274, 275, 282), of two tiles of columns at least (200 tokens: four 33 us, two 30)
+  long long s = blocks < 768 ? (768 + blocks - 1) / blocks : 1;
   const long long most = (n_rows * d.G + 2 * SC_COLS - 1) / (2 * SC_COLS);
   s = s < most ? s : most;
   p.splits = (int)(s < 1 ? 1 : s > 64 ? 64 : s);
