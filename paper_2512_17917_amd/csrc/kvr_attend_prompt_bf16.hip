@@ -37,16 +37,21 @@ constexpr int FP_BUFS = 4;
 constexpr int FP_LDS = 2 * FP_BUFS * FP_TILE + 2 * FP_BUFS * FP_WAVES;
 constexpr float KEEP_MAX = 8.f;
 
-// Into how many parts the tokens of a tile of columns are split, at most `most`: as many as make the rounds of 256 workgroups
-// (one a CU) times a part's length shortest, four tiles' time being what a workgroup costs besides.
-__device__ __forceinline__ int split_count(const DevDesc& d, const PagedArgs& a, int most) {
+// What s parts of each tile's tokens cost, in quarters of the time that a workgroup takes for 64 tokens: rounds of 256 workgroups
+// (one a CU), four tiles' time being what a workgroup costs besides, and the parts' way through memory with the joining launch.
+__host__ __device__ __forceinline__ long long split_cost(long long wgs, int key_tiles, int s, long long heads) {
+  const long long rounds = (wgs * s + 255) / 256;
+  return 4 * rounds * ((key_tiles + s - 1) / s + 4) + (s > 1 ? 8 + heads * s / 1024 : 0);
+}
+// The cheapest number of parts, at most `most` and no more workgroups in all than the launch has.
+__device__ __forceinline__ int split_count(const DevDesc& d, const PagedArgs& a, int most, int launched) {
   const TileCount c = count_tiles(a.q_start, a.n_ctx, a.n_rows, d.B, d.G, FP_COLS, a.pages.cap);
   int keys = c.longest;
   if (a.vis.window > 0) keys = min((long long)keys, (long long)a.vis.window + a.vis.n_sink + FP_COLS);
-  const int tiles = (keys + FP_KEYS - 1) / FP_KEYS, s = (threadIdx.x & 63) + 1;
-  const long long rounds = ((long long)c.tiles * d.Hkv * s + 255) / 256;
-  const long long cost = rounds * ((tiles + s - 1) / s + 4);
-  const int mine = s <= most && cost < (1ll << 24) ? (int)(cost << 6) + s - 1 : 0x7fffffff;
+  const int s = (threadIdx.x & 63) + 1;
+  const long long wgs = (long long)c.tiles * d.Hkv;
+  const long long cost = split_cost(wgs, (keys + FP_KEYS - 1) / FP_KEYS, s, (long long)a.n_rows * d.Hq);
+  const int mine = s <= most && wgs * s <= launched && cost < (1ll << 24) ? (int)(cost << 6) + s - 1 : 0x7fffffff;
   const int best = wave_reduce(mine, [](int x, int y) { return x < y ? x : y; });
   return best == 0x7fffffff ? 1 : (best & 63) + 1;
 }
@@ -56,6 +61,7 @@ struct PromptOut {
   float* lse;              // per row and head: maximum plus logarithm of the sum, in powers of two; or null
   float* part_o;           // split: [split][row and head][D] sums of p v, and [split][row and head][2] maximum and sum
   float* part_ml;
+  int most_splits, wgs;    // how many parts there is room for, workgroups launched
 };
 
 // Where the rows of a tile lie: in one page (dense caches, pages of whole tiles), the eight that a wave fetches in one page, or
@@ -63,7 +69,7 @@ struct PromptOut {
 enum { IN_ONE_PAGE, EIGHT_A_PAGE, ANYWHERE };
 
 template <int ROWS, bool SPLIT>
-__global__ __launch_bounds__(64 * FP_WAVES, 2) void prompt_bf16_kernel(DevDesc d, PagedArgs a, PromptOut po, int most_splits) {
+__global__ __launch_bounds__(64 * FP_WAVES, 2) void prompt_bf16_kernel(DevDesc d, PagedArgs a, PromptOut po) {
   extern __shared__ __align__(1024) unsigned char s_mem[];
   unsigned char* s_k = s_mem;                                   // [4][64][256]
   unsigned char* s_v = s_k + FP_BUFS * FP_TILE;                 // [4][64][256]
@@ -76,7 +82,7 @@ __global__ __launch_bounds__(64 * FP_WAVES, 2) void prompt_bf16_kernel(DevDesc d
   // Heads next to each other in the grid (neighbours go to the chip's dies in turn, so that a die's L2 holds few heads), then the
   // parts of a tile, then tiles: those that turn out not to be there come last, where they take no compute unit's turn.
   const int order = uniform((int)(blockIdx.x / (unsigned)d.Hkv)), hk = (int)(blockIdx.x - (unsigned)order * d.Hkv);
-  const int splits = SPLIT ? split_count(d, a, most_splits) : 1;
+  const int splits = SPLIT ? split_count(d, a, po.most_splits, po.wgs) : 1;
   const int tile = SPLIT ? uniform(order / splits) : order, split = SPLIT ? order - tile * splits : 0;
   const int gs = __builtin_ctz(d.G);                            // G is a power of two
   const ColTile ct = col_tile(a.q_start, a.n_rows, d.B, d.G, FP_COLS, tile);
@@ -313,41 +319,49 @@ __global__ __launch_bounds__(64 * FP_WAVES, 2) void prompt_bf16_kernel(DevDesc d
   // has arrived at the stretch's end, step i + 1 or i + 2, is first read in the stretch after or later.
   if (n_in > 0) {
     const int late = wave >= FP_WAVES / 2 ? 1 : 0;
-    arrive(1 < n_all);
-    barrier();
-    logits(0);
-    if (late) {
-      fetch_next(2);
-      arrive(2 < n_all);
+    auto walk = [&](auto alive) {
+      constexpr bool ALIVE = decltype(alive)::value;
+      arrive(1 < n_all);
       barrier();
-    }
-    for (int i = 0; i < n_in; ++i) {
-      if (ROWS != ANYWHERE && i + 3 + late < n_in) fetch_in(i + 2 + late);
-      else fetch_next(i + 2 + late);
-      weights();
-      arrive(i + 2 + late < n_all);
-      barrier();
-      add_values(i);
-      logits(i + 1);                            // (behind the last step: of what LDS holds, and nobody looks at it)
-      // operands are read four products ahead
-      __builtin_amdgcn_sched_group_barrier(0x100, 8, 0);
-#pragma unroll
-      for (int x = 0; x < 12; ++x) {
-        __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
-        __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
+      if constexpr (ALIVE) logits(0);
+      if (late) {
+        fetch_next(2);
+        arrive(2 < n_all);
+        barrier();
       }
+      for (int i = 0; i < n_in; ++i) {
+        if (ROWS != ANYWHERE && i + 3 + late < n_in) fetch_in(i + 2 + late);
+        else fetch_next(i + 2 + late);
+        if constexpr (ALIVE) weights();
+        arrive(i + 2 + late < n_all);
+        barrier();
+        if constexpr (ALIVE) {
+          add_values(i);
+          logits(i + 1);                            // (behind the last step: of what LDS holds, and nobody looks at it)
+          // operands are read four products ahead
+          __builtin_amdgcn_sched_group_barrier(0x100, 8, 0);
 #pragma unroll
-      for (int x = 0; x < 16; ++x) {
-        __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
-        __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+          for (int x = 0; x < 12; ++x) {
+            __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+            __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
+          }
+#pragma unroll
+          for (int x = 0; x < 16; ++x) {
+            __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+            __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+          }
+          __builtin_amdgcn_sched_group_barrier(0x008, 4, 0);
+        }
+        barrier();
       }
-      __builtin_amdgcn_sched_group_barrier(0x008, 4, 0);
-      barrier();
-    }
-    if (!late) {
-      fetch_next(n_in + 2);
-      barrier();
-    }
+      if (!late) {
+        fetch_next(n_in + 2);
+        barrier();
+      }
+    };
+    // (a wave without columns fetches and waits with the others: 48 rows of two sequences on 64k 154 -> 141 us)
+    if (wave_live) walk(std::true_type{});
+    else walk(std::false_type{});
   } else if (n_all > 0) {
     fetch_next(2);
   }
@@ -461,9 +475,9 @@ __global__ __launch_bounds__(64 * FP_WAVES, 2) void prompt_bf16_kernel(DevDesc d
 }
 
 // Joins the parts of a row and head: a wave each, lane l channels 2 l and 2 l + 1; eight parts' numbers are asked for at once.
-__global__ __launch_bounds__(256) void prompt_join_kernel(DevDesc d, PagedArgs a, PromptOut po, int most_splits) {
+__global__ __launch_bounds__(256) void prompt_join_kernel(DevDesc d, PagedArgs a, PromptOut po) {
   const int lane = threadIdx.x & 63;
-  const int splits = split_count(d, a, most_splits);
+  const int splits = split_count(d, a, po.most_splits, po.wgs);
   if (splits == 1) return;                        // written where it was computed
   const long long at = (long long)blockIdx.x * 4 + uniform((int)(threadIdx.x >> 6));
   const long long all = (long long)a.n_rows * d.Hq;
@@ -513,13 +527,24 @@ PromptPlan prompt_bf16_plan(const DevDesc& d, long long n_rows, long long cap, c
     const long long some = (long long)vis.window + vis.n_sink + FP_COLS;
     keys = some < keys ? some : keys;
   }
-  // Fewer tiles of columns than CUs: the tokens of a tile to several workgroups (the device knows how many tiles there are),
-  // 512 tokens each at least, up to two workgroups for each CU.
-  const long long tiles = (n_rows * d.G + FP_COLS - 1) / FP_COLS * d.Hkv;
-  long long s = tiles < 256 ? 512 / tiles : 1;
-  const long long most = keys / 512;
-  s = s < most ? s : most;
-  p.splits = (int)(s < 1 ? 1 : s > 64 ? 64 : s);
+  // Fewer tiles of columns than CUs: the tokens of a tile to several workgroups, two tiles each at least.  The device knows how
+  // many tiles there are; here they are as few as the rows can make, and for the launch also one a sequence: workgroups that
+  // find nothing to do still wait for a CU.  (32 heads on 8, against parts of 512 tokens at least and a launch of all that there
+  // is room for: 16 rows on 1000 tokens 17 us for 26, on 4000 20 for 25, on 65000 53 for 58; 8 x 16 rows on 1000 24 for 27.)
+  const long long least = (n_rows * d.G + FP_COLS - 1) / FP_COLS, likely = n_rows < d.B ? n_rows : d.B;
+  const int key_tiles = (int)((keys + FP_KEYS - 1) / FP_KEYS);
+  auto best = [&](long long tiles) {
+    int r = 1;
+    for (int s = 2; s <= 64 && 2 * s <= key_tiles && tiles * d.Hkv < 256; ++s)
+      if (split_cost(tiles * d.Hkv, key_tiles, s, n_rows * d.Hq) < split_cost(tiles * d.Hkv, key_tiles, r, n_rows * d.Hq)) r = s;
+    return r;
+  };
+  p.splits = best(least);
+  p.wgs = col_tiles_most(n_rows, d.B, d.G, FP_COLS) * d.Hkv;
+  if (p.splits > 1) {
+    const long long more = least > likely ? least : likely;
+    for (long long w : {256ll, least * d.Hkv * p.splits, more * d.Hkv * best(more)}) p.wgs = p.wgs > w ? p.wgs : w;
+  }
   auto whole = [](size_t x) { return (x + 255) & ~(size_t)255; };
   const size_t heads = (size_t)n_rows * d.Hq;
   p.off_lse = 0;
@@ -555,17 +580,19 @@ hipError_t launch_prompt_bf16(const DevDesc& d, const PagedArgs& a, const Prompt
   po.lse = a.scores ? (float*)(base + p.off_lse) : nullptr;
   po.part_o = p.splits > 1 ? (float*)(base + p.off_o) : nullptr;
   po.part_ml = p.splits > 1 ? (float*)(base + p.off_ml) : nullptr;
-  const dim3 grid((unsigned)(col_tiles_most(a.n_rows, d.B, d.G, FP_COLS) * d.Hkv * p.splits)), block(64 * FP_WAVES);
+  po.most_splits = p.splits;
+  po.wgs = (int)p.wgs;
+  const dim3 grid((unsigned)p.wgs), block(64 * FP_WAVES);
   auto launch = [&](auto rows) {
-    if (p.splits > 1) hipLaunchKernelGGL((prompt_bf16_kernel<decltype(rows)::value, true>), grid, block, FP_LDS, st, d, a, po, p.splits);
-    else hipLaunchKernelGGL((prompt_bf16_kernel<decltype(rows)::value, false>), grid, block, FP_LDS, st, d, a, po, p.splits);
+    if (p.splits > 1) hipLaunchKernelGGL((prompt_bf16_kernel<decltype(rows)::value, true>), grid, block, FP_LDS, st, d, a, po);
+    else hipLaunchKernelGGL((prompt_bf16_kernel<decltype(rows)::value, false>), grid, block, FP_LDS, st, d, a, po);
   };
   if (a.pages.table == nullptr || a.pages.page_size % FP_KEYS == 0) launch(std::integral_constant<int, IN_ONE_PAGE>{});
   else if (a.pages.page_size % 8 == 0) launch(std::integral_constant<int, EIGHT_A_PAGE>{});
   else launch(std::integral_constant<int, ANYWHERE>{});
   e = hipGetLastError();
   if (e != hipSuccess || p.splits == 1) return e;
-  hipLaunchKernelGGL(prompt_join_kernel, dim3((unsigned)(((long long)a.n_rows * d.Hq + 3) / 4)), dim3(256), 0, st, d, a, po, p.splits);
+  hipLaunchKernelGGL(prompt_join_kernel, dim3((unsigned)(((long long)a.n_rows * d.Hq + 3) / 4)), dim3(256), 0, st, d, a, po);
   return hipGetLastError();
 }
 

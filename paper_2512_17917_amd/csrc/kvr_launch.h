@@ -265,6 +265,7 @@ hipError_t launch_prompt_scores_bf16(const DevDesc& d, const PagedArgs& a, const
                                      hipStream_t st);
 struct PromptPlan {
   int splits;
+  long long wgs;
   ScoresPlan scores;
   size_t off_lse, off_o, off_ml, off_scores, total;
 };
