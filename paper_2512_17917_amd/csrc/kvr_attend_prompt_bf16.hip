@@ -535,7 +535,7 @@ PromptPlan prompt_bf16_plan(const DevDesc& d, long long n_rows, long long cap, c
   const int key_tiles = (int)((keys + FP_KEYS - 1) / FP_KEYS);
   auto best = [&](long long tiles) {
     int r = 1;
-    for (int s = 2; s <= 64 && 2 * s <= key_tiles && tiles * d.Hkv < 256; ++s)
+    for (int s = 2; s <= 64 && 2 * s <= key_tiles && tiles * d.Hkv < 256 && tiles * d.Hkv * s <= 1024; ++s)      // (134 MB)
       if (split_cost(tiles * d.Hkv, key_tiles, s, n_rows * d.Hq) < split_cost(tiles * d.Hkv, key_tiles, r, n_rows * d.Hq)) r = s;
     return r;
   };
