@@ -555,10 +555,17 @@ __global__ __launch_bounds__(256) void paged_join_kernel(DevDesc d, PagedArgs a,
       for (int x = 0; x < 16; ++x) {
         const int i = min(i0 + 2 * x, parts - 1);
         const float2 ml = *reinterpret_cast<const float2*>(part_ml + ((slot0 + i) * G + g) * 2);
-        pm[x] = i0 + 2 * x < parts ? ml.x : NEG_INF;
-        pl[x] = i0 + 2 * x < parts ? ml.y : 0.f;
-        const float po_i = part_o[((slot0 + i) * G + g) * D + c];
-        po[x] = i0 + 2 * x < parts ? po_i : 0.f;
+        pm[x] = ml.x;
+        pl[x] = ml.y;
+        po[x] = part_o[((slot0 + i) * G + g) * D + c];
+      }
+#pragma unroll
+      for (int x = 0; x < 16; ++x) {            // (asked for all the same: no branch around a load)
+        asm volatile("" : "+v"(pm[x]), "+v"(pl[x]), "+v"(po[x]));
+        const bool in = i0 + 2 * x < parts;
+        pm[x] = in ? pm[x] : NEG_INF;
+        pl[x] = in ? pl[x] : 0.f;
+        po[x] = in ? po[x] : 0.f;
       }
       float mn = m;
 #pragma unroll
