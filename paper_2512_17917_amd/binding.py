@@ -6,8 +6,9 @@ pointers, checks dtype / device / contiguity / minimum size, and passes
 `data_ptr()` plus the current torch HIP stream.  Nothing is computed here.
 There is no fallback: if the library is missing, loading raises.
 
-The calls of a decode step (`kvr_step_update`, `kvr_attend_decode`; over an
-uncompressed cache `kvr_rotate`, `kvr_attend_paged`, `kvr_attend_prompt`) are checked and made by the extension `_kvr_fast` (csrc/kvr_fast.c), where it was built
+The calls of a decode step (`kvr_step_update`, `kvr_attend_decode`) and those over an
+uncompressed cache (`kvr_rotate`, `kvr_attend_paged`, `kvr_attend_prompt`) are checked and
+made by the extension `_kvr_fast` (csrc/kvr_fast.c), where it was built
 and every argument is as it should be; anything else comes back to the checks here,
 which raise.
 """

@@ -19,7 +19,7 @@
 // two: s = (scale / ln 2) q.k.
 //
 // Bound by HBM: 131072 tokens of 8 kv heads, 4 query heads each, 537 MB in 103 us = 5.2 TB/s, the join 7.6 us more; 16 x 32768
-// with scores 450 + 23 us (2.18 GB).  Two things made that of 246 and 936 us: what is the same for a wave computed on the
+// with scores 454 + 20 us (2.18 GB).  Two things made that of 246 and 936 us: what is the same for a wave computed on the
 // scalar unit, and sums pinned before the next tile's loads, which otherwise keep a tile's 32 floats and the products alive
 // past them (200 registers, 89 of them in scratch memory, where 128 do).
 #include "kvr_launch.h"
