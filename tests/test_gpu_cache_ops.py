@@ -270,6 +270,23 @@ def test_long_prompts(case):
     _check("prompt", dtype, heads, page, n, new, window, sink, n_cap, seed=200 + case)
 
 
+PARTS = [  # heads, page, lengths, new, window, sinks: few columns, whose tokens several workgroups share
+    ((8, 2), 16, [1000] * 8, [16] * 8, 0, 0),
+    ((8, 2), 16, [1200, 0, 3, 2500], [16, 0, 3, 1], 0, 0),
+    ((6, 3), 24, [1500, 130], [40, 2], 0, 0),                   # three kv heads: no whole number of them in the launch
+    ((8, 1), 16, [300] * 69 + [2000], [0] * 69 + [4], 0, 0),    # one sequence of many has new tokens
+    ((8, 2), 16, [129, 128], [1, 128], 0, 0),
+    ((16, 2), 64, [3000], [70], 700, 130),
+    ((4, 4), 0, [2000], [200], 0, 0),
+]
+
+
+@pytest.mark.parametrize("case", range(len(PARTS)))
+def test_parts_of_few_columns(case):
+    heads, page, n, new, window, sink = PARTS[case]
+    _check("prompt", BF, heads, page, n, new, window, sink, max(n), seed=300 + case, lead=2)
+
+
 @pytest.mark.parametrize("which", ["prompt", "paged"])
 @pytest.mark.parametrize("dtype", [BF, F32])
 def test_many_sequences(which, dtype):
