@@ -218,6 +218,16 @@ hipError_t launch_encode(const DevDesc& d, int dtype, const void* k_src, const v
                          void* sk, void* sv, int32_t* out_bucket, uint8_t* out_sign,
                          void* ws, const EncodePlan& plan, hipStream_t st);
 
+// A dimension of a launch holds fewer than 2^32 threads (past that the number wraps and the rest never starts): n workgroups of at
+// most 512 as `x` a row and `rows` rows in another dimension; those behind the last find nothing to do.
+struct GridRows {
+  unsigned x, rows;
+};
+inline GridRows grid_rows(long long n) {
+  constexpr long long MOST = 1 << 22;
+  return n <= MOST ? GridRows{(unsigned)n, 1} : GridRows{(unsigned)MOST, (unsigned)((n + MOST - 1) / MOST)};
+}
+
 // Norm and rotation of new tokens' queries and keys, keys and values into the cache (kvr_rotate)
 struct RotateArgs {
   const void* q;

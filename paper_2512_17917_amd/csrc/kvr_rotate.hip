@@ -93,7 +93,7 @@ __global__ __launch_bounds__(64 * ROT_WAVES) void rotate_kernel(DevDesc d, Rotat
   __shared__ float s_cs[ROT_WAVES][2][D / 2];
   __shared__ float s_x[MODE == ROT_ANY ? ROT_WAVES : 1][MODE == ROT_ANY ? HEADS * D : 1];
   const int lane = threadIdx.x & 63, wave = uniform((int)(threadIdx.x >> 6));
-  const long long item = (long long)blockIdx.x * ROT_WAVES + wave;
+  const long long item = ((long long)blockIdx.y * gridDim.x + blockIdx.x) * ROT_WAVES + wave;
   const int row = uniform((int)(item / a.parts)), part = uniform((int)(item % a.parts));
   if (row >= a.n_rows) return;                 // whole waves; no workgroup barrier below
   const int b = uniform(seq_of_row(a.q_start, d.B, row));
@@ -217,16 +217,16 @@ __global__ __launch_bounds__(64 * ROT_WAVES) void rotate_kernel(DevDesc d, Rotat
 }
 
 template <typename T>
-void launch_mode(const DevDesc& d, const RotateArgs& a, bool pairs, unsigned grid, hipStream_t st) {
+void launch_mode(const DevDesc& d, const RotateArgs& a, bool pairs, dim3 grid, hipStream_t st) {
   const dim3 block(64 * ROT_WAVES);
   if (pairs || a.half == 0)
-    hipLaunchKernelGGL((rotate_kernel<T, ROT_NEIGHBOURS>), dim3(grid), block, 0, st, d, a);
+    hipLaunchKernelGGL((rotate_kernel<T, ROT_NEIGHBOURS>), grid, block, 0, st, d, a);
   else if (a.half == D / 2)
-    hipLaunchKernelGGL((rotate_kernel<T, ROT_HALF>), dim3(grid), block, 0, st, d, a);
+    hipLaunchKernelGGL((rotate_kernel<T, ROT_HALF>), grid, block, 0, st, d, a);
   else if (a.half % Store<T>::VEC == 0)
-    hipLaunchKernelGGL((rotate_kernel<T, ROT_LANES>), dim3(grid), block, 0, st, d, a);
+    hipLaunchKernelGGL((rotate_kernel<T, ROT_LANES>), grid, block, 0, st, d, a);
   else
-    hipLaunchKernelGGL((rotate_kernel<T, ROT_ANY>), dim3(grid), block, 0, st, d, a);
+    hipLaunchKernelGGL((rotate_kernel<T, ROT_ANY>), grid, block, 0, st, d, a);
 }
 
 }  // namespace
@@ -238,7 +238,8 @@ hipError_t launch_rotate(const DevDesc& d, int dtype, const RotateArgs& args, bo
   // few rows: the heads of a row to as many waves as make up 4096, four for each SIMD of the chip
   const long long want = (4096 + a.n_rows - 1) / a.n_rows;
   a.parts = (int)(want < iters ? want : iters);
-  const unsigned grid = (unsigned)(((long long)a.n_rows * a.parts + ROT_WAVES - 1) / ROT_WAVES);
+  const GridRows rows = grid_rows(((long long)a.n_rows * a.parts + ROT_WAVES - 1) / ROT_WAVES);
+  const dim3 grid(rows.x, rows.rows);
   if (dtype == KVR_F32) launch_mode<float>(d, a, pairs, grid, st);
   else launch_mode<bf16_t>(d, a, pairs, grid, st);
   return hipGetLastError();
