@@ -48,7 +48,7 @@ __global__ __launch_bounds__(64 * PP_WAVES) void prompt_f32_kernel(DevDesc d, Pa
   const int r = lane >> 4, col = lane & 15;
   const int hk = blockIdx.y, gs = __builtin_ctz(d.G);
   const float NEG_INF = -__builtin_inff(), scale2 = d.scale * LOG2E;
-  const ColTile ct = col_tile(a.q_start, a.n_rows, d.B, d.G, 16, blockIdx.x);
+  const ColTile ct = col_tile(a.q_start, a.n_rows, d.B, d.G, 16, (int)(blockIdx.z * gridDim.x + blockIdx.x));
   const int b = uniform(ct.b);
   if (b < 0) return;
   const RowSpan span = row_span(a.q_start, a.n_rows, b);
@@ -213,7 +213,7 @@ __global__ __launch_bounds__(64 * PP_WAVES) void prompt_scores_f32_kernel(DevDes
   const RowSpan span = row_span(a.q_start, a.n_rows, b);
   const int n = clampi(listed(a.n_ctx + b), 0, a.pages.cap);
   const int first = n - span.n;
-  const int j0 = blockIdx.x * 16;
+  const int j0 = (int)(blockIdx.z * gridDim.x + blockIdx.x) * 16;
   if (j0 >= n) return;
   const float scale2 = d.scale * LOG2E;
   const long long row = j0 + col < n ? page_row(a.pages, d.Hkv, b, hk, j0 + col) : -1;
@@ -222,7 +222,7 @@ __global__ __launch_bounds__(64 * PP_WAVES) void prompt_scores_f32_kernel(DevDes
   // new tokens of which some may see one of the tile's
   const int t0 = max(j0 - first, 0);
   int t1 = span.n;
-  if (a.vis.window > 0 && j0 >= a.vis.n_sink) t1 = min(t1, j0 + 15 + a.vis.window - first);
+  if (a.vis.window > 0 && j0 >= a.vis.n_sink) t1 = (int)min((long long)t1, (long long)j0 + 15 + a.vis.window - first);
   const int cols = t1 << gs;
   auto column = [&](int m0) {
     const int m = min(m0 + col, cols - 1);
@@ -278,12 +278,13 @@ hipError_t launch_attend_prompt(const DevDesc& d, int dtype, const PagedArgs& a,
     return launch_prompt_scores_bf16(d, a, p.scores, (const float*)(base + p.off_lse), (float*)(base + p.off_scores), st);
   }
   float* lse = a.scores ? (float*)a.ws : nullptr;
-  const dim3 grid((unsigned)col_tiles_most(a.n_rows, d.B, d.G, 16), d.Hkv);
-  hipLaunchKernelGGL(prompt_f32_kernel, grid, dim3(64 * PP_WAVES), 0, st, d, a, lse);
+  const GridRows cols = grid_rows(col_tiles_most(a.n_rows, d.B, d.G, 16));
+  hipLaunchKernelGGL(prompt_f32_kernel, dim3(cols.x, d.Hkv, cols.rows), dim3(64 * PP_WAVES), 0, st, d, a, lse);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess || a.scores == nullptr) return e;
   const long long most = a.n_cap < a.pages.cap ? a.n_cap : a.pages.cap;
-  hipLaunchKernelGGL(prompt_scores_f32_kernel, dim3((unsigned)((most + 15) / 16), d.B * d.Hkv), dim3(64 * PP_WAVES), 0, st, d, a, lse);
+  const GridRows tiles = grid_rows((most + 15) / 16);
+  hipLaunchKernelGGL(prompt_scores_f32_kernel, dim3(tiles.x, d.B * d.Hkv, tiles.rows), dim3(64 * PP_WAVES), 0, st, d, a, lse);
   return hipGetLastError();
 }
 
