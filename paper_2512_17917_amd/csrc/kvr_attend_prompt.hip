@@ -265,17 +265,18 @@ __global__ __launch_bounds__(64 * PP_WAVES) void prompt_scores_f32_kernel(DevDes
 }  // namespace
 
 size_t attend_prompt_ws(const DevDesc& d, int dtype, long long n_rows, long long cap, const Visible& vis, bool scores) {
-  if (dtype == KVR_BF16) return prompt_bf16_plan(d, n_rows, cap, vis, scores).total;
+  // (how many places for scores there will be is not known here: for all tokens that there is room for)
+  if (dtype == KVR_BF16) return prompt_bf16_plan(d, n_rows, cap, vis, scores ? cap : 0).total;
   return scores ? (size_t)n_rows * d.Hq * sizeof(float) : 0;
 }
 
 hipError_t launch_attend_prompt(const DevDesc& d, int dtype, const PagedArgs& a, hipStream_t st) {
   if (dtype == KVR_BF16) {
-    const PromptPlan p = prompt_bf16_plan(d, a.n_rows, a.pages.cap, a.vis, a.scores != nullptr);
+    const PromptPlan p = prompt_bf16_plan(d, a.n_rows, a.pages.cap, a.vis, a.scores ? a.n_cap : 0);
     const hipError_t e = launch_prompt_bf16(d, a, p, st);
     if (e != hipSuccess || a.scores == nullptr) return e;
     char* base = (char*)a.ws;
-    return launch_prompt_scores_bf16(d, a, p.scores, (const float*)(base + p.off_lse), (float*)(base + p.off_scores), st);
+    return launch_prompt_scores_bf16(d, a, p.scores, (const float*)(base + p.off_lse), base + p.off_scores, st);
   }
   float* lse = a.scores ? (float*)a.ws : nullptr;
   const GridRows cols = grid_rows(col_tiles_most(a.n_rows, d.B, d.G, 16));

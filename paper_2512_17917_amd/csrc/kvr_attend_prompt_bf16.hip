@@ -62,6 +62,8 @@ struct PromptOut {
   float* part_o;           // split: [split][row and head][D] sums of p v, and [split][row and head][2] maximum and sum
   float* part_ml;
   int most_splits, wgs;    // how many parts there is room for, workgroups launched
+  ScoresWork* work;        // what the scores' pass has to do, or null
+  int keys, most_scores_splits, scores_wgs;
 };
 
 // Where the rows of a tile lie: in one page (dense caches, pages of whole tiles), the eight that a wave fetches in one page, or
@@ -82,6 +84,7 @@ __global__ __launch_bounds__(64 * FP_WAVES, 2) void prompt_bf16_kernel(DevDesc d
   // Heads next to each other in the grid (neighbours go to the chip's dies in turn, so that a die's L2 holds few heads), then the
   // parts of a tile, then tiles: those that turn out not to be there come last, where they take no compute unit's turn.
   const int order = uniform((int)(blockIdx.x / (unsigned)d.Hkv)), hk = (int)(blockIdx.x - (unsigned)order * d.Hkv);
+  if (po.work && blockIdx.x == gridDim.x - 1 && wave == 0) find_scores_work(d, a, po.keys, po.most_scores_splits, po.scores_wgs, po.work);
   const int splits = SPLIT ? split_count(d, a, po.most_splits, po.wgs) : 1;
   const int tile = SPLIT ? uniform(order / splits) : order, split = SPLIT ? order - tile * splits : 0;
   const int gs = __builtin_ctz(d.G);                            // G is a power of two
@@ -520,7 +523,7 @@ __global__ __launch_bounds__(256) void prompt_join_kernel(DevDesc d, PagedArgs a
 
 }  // namespace
 
-PromptPlan prompt_bf16_plan(const DevDesc& d, long long n_rows, long long cap, const Visible& vis, bool scores) {
+PromptPlan prompt_bf16_plan(const DevDesc& d, long long n_rows, long long cap, const Visible& vis, long long n_cap) {
   PromptPlan p = {};
   long long keys = cap;
   if (vis.window > 0) {
@@ -548,10 +551,10 @@ PromptPlan prompt_bf16_plan(const DevDesc& d, long long n_rows, long long cap, c
   auto whole = [](size_t x) { return (x + 255) & ~(size_t)255; };
   const size_t heads = (size_t)n_rows * d.Hq;
   p.off_lse = 0;
-  p.off_o = scores ? whole(heads * sizeof(float)) : 0;
+  p.off_o = n_cap > 0 ? whole(heads * sizeof(float)) : 0;
   p.off_ml = p.off_o + (p.splits > 1 ? whole(heads * p.splits * D * sizeof(float)) : 0);
   p.off_scores = p.off_ml + (p.splits > 1 ? whole(heads * p.splits * 2 * sizeof(float)) : 0);
-  if (scores) p.scores = prompt_scores_plan(d, n_rows, cap);
+  if (n_cap > 0) p.scores = prompt_scores_plan(d, n_rows, n_cap < cap ? n_cap : cap);
   p.total = p.off_scores + p.scores.bytes;
   return p;
 }
@@ -582,6 +585,10 @@ hipError_t launch_prompt_bf16(const DevDesc& d, const PagedArgs& a, const Prompt
   po.part_ml = p.splits > 1 ? (float*)(base + p.off_ml) : nullptr;
   po.most_splits = p.splits;
   po.wgs = (int)p.wgs;
+  po.work = a.scores ? (ScoresWork*)(base + p.off_scores) : nullptr;
+  po.keys = p.scores.keys;
+  po.most_scores_splits = p.scores.most_splits;
+  po.scores_wgs = p.scores.wgs;
   const dim3 grid((unsigned)p.wgs), block(64 * FP_WAVES);
   auto launch = [&](auto rows) {
     if (p.splits > 1) hipLaunchKernelGGL((prompt_bf16_kernel<decltype(rows)::value, true>), grid, block, FP_LDS, st, d, a, po);

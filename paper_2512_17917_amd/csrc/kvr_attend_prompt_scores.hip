@@ -5,7 +5,10 @@
 // waves walk over tiles of 64 columns, whose queries come through LDS, and every lane sums the weights of its own token: no
 // exchange until the end, and the order of a sum is fixed.  A token early in a prompt has the most columns: its block goes
 // first, and where the blocks of tokens are few its columns are shared out over several workgroups, whose sums a second kernel
-// adds in order.
+// adds in order.  Which blocks there are, and into how many parts they are cut, goes by the sequences' lengths, which only the device
+// knows (a cache has room for far more): the attention kernel's last workgroup finds it out on the way.  2048 tokens, 32 heads on
+// 8, the whole call: 96 us with room for 2k, 32k or 131k tokens (cut by the room: 96, 225, 225); 2 x 600: 47, 60, 68 (46, 97, 97);
+// one of 5000 and 15 of 100: 738, 578, 582 (735 each).
 //
 // The products of half a tile stand between the weights of the half before (an exponential, a multiply-add and a sum a number:
 // the vector unit has as much to do as the matrix unit).  4 x 2048 tokens, 32 heads on 8: the call takes 78 us more than
@@ -21,36 +24,60 @@ namespace kvr {
 
 namespace {
 
-constexpr int SC_WAVES = 4, SC_KEYS = 64 * SC_WAVES, SC_COLS = 64;
+constexpr int SC_WAVES = 4, SC_COLS = 64;
+static_assert(SC_KEYS == 64 * SC_WAVES);
 constexpr int SC_TILE = SC_COLS * D * 2, SC_BUFS = 3;
 
-__global__ __launch_bounds__(64 * SC_WAVES, 2) void prompt_scores_bf16_kernel(DevDesc d, PagedArgs a, const float* lse, float* part,
-                                                                              int keys_cap, int splits) {
-  __shared__ __align__(1024) unsigned char s_q[SC_BUFS * SC_TILE];
-  __shared__ __align__(16) float s_lse[SC_BUFS][SC_COLS];
+// A piece of the work: part `split` of the columns that see block `rank` (of the sequence's, `blocks`) of a unit's tokens.
+struct Piece {
+  int u, b, hk, rank, split, splits;
+  Blocks blocks;
+  bool any, last;                                    // whether there is one at this place, and none at this one or any behind
+};
+__device__ __forceinline__ Piece piece_at(const DevDesc& d, const PagedArgs& a, const ScoresWork* w, int keys, int order, int u) {
+  Piece p;
+  p.u = u;
+  p.b = uniform(u / d.Hkv);
+  p.hk = u - p.b * d.Hkv;
+  p.blocks = seq_blocks(a, p.b, keys);
+  p.splits = listed(&w->splits);
+  p.rank = uniform(order / p.splits);
+  p.split = order - p.rank * p.splits;
+  p.any = p.rank < p.blocks.n;
+  p.last = p.rank >= listed(&w->longest);
+  return p;
+}
+struct ScoresArgs {
+  DevDesc d;
+  PagedArgs a;
+  const float* lse;
+  const ScoresWork* work;
+  float* part;                                       // sums of pieces whose block has several: SC_KEYS each, block after block
+  int keys;
+};
+
+__device__ __forceinline__ void scores_piece(const ScoresArgs& args, const Piece& me, unsigned char (&s_q)[SC_BUFS * SC_TILE],
+                                             float (&s_lse)[SC_BUFS][SC_COLS]) {
+  const DevDesc& d = args.d;
+  const PagedArgs& a = args.a;
+  const float* lse = args.lse;
   const int lane = threadIdx.x & 63, wave = uniform((int)(threadIdx.x >> 6));
   const int half = lane >> 5, col = lane & 31;
-  // units next to each other: a block of tokens early in a prompt has many times the work of a late one, and neighbours in the
-  // grid go to the chip's dies in turn
-  const int units = d.B * d.Hkv, order = uniform((int)(blockIdx.x / (unsigned)units));
-  const int block = uniform(order / splits), split = order - block * splits;
-  const int u = (int)(blockIdx.x - (unsigned)order * units), b = uniform(u / d.Hkv), hk = u - b * d.Hkv;
+  const int b = me.b, hk = me.hk;
   const int gs = __builtin_ctz(d.G);
-  const RowSpan span = row_span(a.q_start, a.n_rows, b);
-  const int n = clampi(listed(a.n_ctx + b), 0, a.pages.cap);
-  const int first = n - span.n;
-  const int j0 = block * SC_KEYS;
-  if (j0 >= n) return;
+  const RowSpan span = me.blocks.span;
+  const int n = me.blocks.tokens, first = n - span.n;
+  const int j0 = tile_token<SC_KEYS>(me.blocks.range, me.rank);
   const int jw = j0 + 64 * wave;                     // this wave's tokens
   // new tokens of which some may see one of the block's
   const int t0 = max(j0 - first, 0);
   int t1 = span.n;
-  if (a.vis.window > 0 && j0 >= a.vis.n_sink) t1 = min(t1, j0 + SC_KEYS - 1 + a.vis.window - first);
+  if (a.vis.window > 0 && j0 >= a.vis.n_sink) t1 = (int)min((long long)t1, (long long)j0 + SC_KEYS - 1 + a.vis.window - first);
   const int cols = t1 << gs;                         // columns t0 G .. cols - 1
   const int c0 = t0 << gs;
   const int tiles = cols > c0 ? (cols - c0 + SC_COLS - 1) / SC_COLS : 0;
-  const int per = uniform((tiles + splits - 1) / splits);
-  const int i0 = min(split * per, tiles), i1 = min(i0 + per, tiles);
+  const int per = uniform((tiles + me.splits - 1) / me.splits);
+  const int i0 = min(me.split * per, tiles), i1 = min(i0 + per, tiles);
 
   const Scale2 sc = scale2(d.scale);
   bf16x8_t k[2][8];
@@ -219,55 +246,113 @@ __global__ __launch_bounds__(64 * SC_WAVES, 2) void prompt_scores_bf16_kernel(De
     }
   }
   add(s1, le1);
+  float* part = nullptr;
+  if (me.splits > 1) part = args.part + (((size_t)listed(args.work->before + b) * d.Hkv + (size_t)hk * me.blocks.n + me.rank) * me.splits + me.split) * SC_KEYS;
 #pragma unroll
   for (int kb = 0; kb < 2; ++kb) {
     const float sum = across_sum(acc[kb]);
     const int j = jw + 32 * kb + col;
-    if (half == 0 && j < keys_cap) {
-      if (part) part[((size_t)split * units + u) * keys_cap + j] = there[kb] ? sum : 0.f;
-      else if (there[kb] && sum != 0.f) a.scores[(size_t)u * a.n_cap + j] += sum;
+    if (half == 0) {
+      if (part) part[64 * wave + 32 * kb + col] = there[kb] ? sum : 0.f;
+      else if (there[kb] && sum != 0.f && j < args.keys) a.scores[(size_t)me.u * a.n_cap + j] += sum;
     }
   }
 }
 
-// adds the workgroups' sums of a token, in order
-__global__ __launch_bounds__(256) void scores_add_kernel(DevDesc d, PagedArgs a, const float* part, int keys_cap, int splits) {
-  const int u = blockIdx.y, j = blockIdx.x * 256 + threadIdx.x;
-  const int n = clampi(listed(a.n_ctx + u / d.Hkv), 0, a.pages.cap);
-  if (j >= n || j >= keys_cap) return;
-  float sum = 0.f;
-  for (int s = 0; s < splits; ++s) sum += part[((size_t)s * gridDim.y + u) * keys_cap + j];
-  if (sum != 0.f) a.scores[(size_t)u * a.n_cap + j] += sum;
+// A workgroup a piece; those past the launch's end (sequences of very many tokens between them) are walked over by a launch of its own
+// (WALK: a loop around it all costs the products 6 %).
+template <bool WALK>
+__global__ __launch_bounds__(64 * SC_WAVES, 2) void prompt_scores_bf16_kernel(ScoresArgs given) {
+  __shared__ __align__(1024) unsigned char s_q[SC_BUFS * SC_TILE];
+  __shared__ __align__(16) float s_lse[SC_BUFS][SC_COLS];
+  // Units next to each other: a block of tokens early in a prompt has many times the work of a late one, and neighbours in the
+  // grid go to the chip's dies in turn.
+  const unsigned units = given.d.B * given.d.Hkv;
+  const unsigned at = (WALK ? SC_MOST_WGS : 0) + blockIdx.x;
+  int order = uniform((int)(at / units)), u = (int)(at - (unsigned)order * units);
+  if constexpr (!WALK) {
+    const Piece me = piece_at(given.d, given.a, given.work, given.keys, order, u);
+    if (me.any) scores_piece(given, me, s_q, s_lse);
+  } else {
+    for (;;) {
+      // the arguments once more for each piece: kept from one to the next, they would take the scalar registers
+      typedef const __attribute__((address_space(4))) ScoresArgs* Args;
+      Args from = (Args)__builtin_amdgcn_kernarg_segment_ptr();
+      asm volatile("" : "+s"(from));
+      const ScoresArgs args = *(const ScoresArgs*)from;
+      const Piece me = piece_at(args.d, args.a, args.work, args.keys, order, u);
+      if (me.last) return;
+      if (me.any) {
+        scores_piece(args, me, s_q, s_lse);
+        // the next piece's queries take the place of this one's
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        __builtin_amdgcn_s_barrier();
+      }
+      const unsigned all = args.d.B * args.d.Hkv;
+      const int rows = (int)(gridDim.x / all);
+      order += rows;
+      u += (int)(gridDim.x - rows * all);
+      if (u >= (int)all) u -= all, ++order;
+    }
+  }
 }
 
-int scores_keys(long long cap, long long n_cap) { return (int)(cap < n_cap ? cap : n_cap); }
+// adds the workgroups' sums of a token, in order: a workgroup a block
+__global__ __launch_bounds__(256) void scores_add_kernel(ScoresArgs args) {
+  const DevDesc& d = args.d;
+  const int splits = listed(&args.work->splits), at = blockIdx.x;
+  if (splits == 1 || at >= listed(&args.work->all)) return;
+  const int lane = threadIdx.x & 63;
+  int b = -1;                                        // the last sequence with no more than `at` blocks before it
+  for (int b0 = 0; b0 < d.B; b0 += 64) {
+    const int some = __popcll(__ballot(b0 + lane < d.B && args.work->before[b0 + lane] * d.Hkv <= at));
+    b += some;
+    if (some < 64) break;
+  }
+  b = uniform(b);
+  const Blocks blocks = seq_blocks(args.a, b, args.keys);
+  const int left = at - listed(args.work->before + b) * d.Hkv, h = uniform(left / blocks.n), rank = left - h * blocks.n;
+  const int j = tile_token<SC_KEYS>(blocks.range, rank) + threadIdx.x;
+  if (j >= blocks.tokens || j >= args.keys) return;
+  const float* p = args.part + (size_t)at * splits * SC_KEYS + threadIdx.x;
+  float sum = 0.f;
+  for (int s = 0; s < splits; ++s) sum += p[(size_t)s * SC_KEYS];
+  if (sum != 0.f) args.a.scores[((size_t)b * d.Hkv + h) * args.a.n_cap + j] += sum;
+}
 
 }  // namespace
 
-// n_cap is not known where the workspace is asked for: room for all tokens
-ScoresPlan prompt_scores_plan(const DevDesc& d, long long n_rows, long long cap) {
+// A part has two tiles of columns at least (200 tokens, 32 heads on 8: four tiles 33 us, two 30).
+ScoresPlan prompt_scores_plan(const DevDesc& d, long long n_rows, long long keys) {
   ScoresPlan p;
-  const long long units = (long long)d.B * d.Hkv;
-  const long long blocks = units * ((cap + SC_KEYS - 1) / SC_KEYS);
-  // 768 pieces of work, three for two workgroups that the chip holds (2 x 600 tokens, 32 heads on 8, the whole call: 1024 pieces
-  // 53 us, 768 49, 512 48; 4 x 2k 274, 275, 282), of two tiles of columns at least (200 tokens: four 33 us, two 30)
-  long long s = blocks < 768 ? (768 + blocks - 1) / blocks : 1;
+  p.keys = (int)keys;
+  const long long blocks = (long long)d.B * d.Hkv * ((keys + SC_KEYS - 1) / SC_KEYS);       // there are at most
   const long long most = (n_rows * d.G + 2 * SC_COLS - 1) / (2 * SC_COLS);
-  s = s < most ? s : most;
-  p.splits = (int)(s < 1 ? 1 : s > 64 ? 64 : s);
-  p.bytes = p.splits > 1 ? (size_t)p.splits * units * cap * sizeof(float) : 0;
+  p.most_splits = (int)(most < 1 ? 1 : most > 64 ? 64 : most);
+  // Blocks that are cut are fewer than SC_PIECES, their parts fewer than SC_PIECES and as many again.
+  const long long few = blocks < SC_PIECES - 1 ? blocks : SC_PIECES - 1;
+  const long long parts = SC_PIECES + few < few * p.most_splits ? SC_PIECES + few : few * p.most_splits;
+  p.add_wgs = p.most_splits > 1 ? (int)few : 0;
+  p.off_part = (sizeof(ScoresWork) + (size_t)d.B * sizeof(int) + 255) & ~(size_t)255;
+  p.bytes = p.off_part + (p.most_splits > 1 ? (size_t)parts * SC_KEYS * sizeof(float) : 0);
+  // As many workgroups as there can be pieces where sequences are alike, within bounds: those that find nothing to do cost 0.65 ns
+  // each (2 x 9000 tokens' cache with 36 new rows: room for 131k a sequence in place of 9k, 6100 workgroups and 4 us more)
+  const long long wgs = SC_PIECES + blocks < blocks * p.most_splits ? SC_PIECES + blocks : blocks * p.most_splits;
+  p.wgs = (int)(wgs < SC_MOST_WGS ? wgs : SC_MOST_WGS);
+  p.walk = blocks > SC_MOST_WGS;
   return p;
 }
 
-hipError_t launch_prompt_scores_bf16(const DevDesc& d, const PagedArgs& a, const ScoresPlan& p, const float* lse, float* part,
-                                     hipStream_t st) {
-  const int keys = scores_keys(a.pages.cap, a.n_cap);
-  const unsigned units = d.B * d.Hkv;
-  hipLaunchKernelGGL(prompt_scores_bf16_kernel, dim3((unsigned)((keys + SC_KEYS - 1) / SC_KEYS) * units * p.splits), dim3(64 * SC_WAVES), 0, st, d,
-                     a, lse, p.splits > 1 ? part : nullptr, keys, p.splits);
-  const hipError_t e = hipGetLastError();
-  if (e != hipSuccess || p.splits == 1) return e;
-  hipLaunchKernelGGL(scores_add_kernel, dim3((keys + 255) / 256, units), dim3(256), 0, st, d, a, part, keys, p.splits);
+hipError_t launch_prompt_scores_bf16(const DevDesc& d, const PagedArgs& a, const ScoresPlan& p, const float* lse, char* ws, hipStream_t st) {
+  const ScoresArgs args = {d, a, lse, (const ScoresWork*)ws, (float*)(ws + p.off_part), p.keys};
+  hipLaunchKernelGGL(prompt_scores_bf16_kernel<false>, dim3(p.wgs), dim3(64 * SC_WAVES), 0, st, args);
+  hipError_t e = hipGetLastError();
+  if (e == hipSuccess && p.walk) {
+    hipLaunchKernelGGL(prompt_scores_bf16_kernel<true>, dim3(2048), dim3(64 * SC_WAVES), 0, st, args);
+    e = hipGetLastError();
+  }
+  if (e != hipSuccess || p.add_wgs == 0) return e;
+  hipLaunchKernelGGL(scores_add_kernel, dim3(p.add_wgs), dim3(256), 0, st, args);
   return hipGetLastError();
 }
 

@@ -267,19 +267,35 @@ struct PagedArgs {
 // bf16 kernel of a prompt's attention: into how many parts a tile's tokens are split, and its workspace (first the columns'
 // maximum plus logarithm of the sum, in powers of two, where scores want them)
 struct ScoresPlan {
-  int splits;                       // workgroups that share the columns of a block of tokens
-  size_t bytes;                     // of their sums
+  int keys;                         // tokens of a sequence whose scores may have to be added
+  int most_splits;                  // workgroups that may share the columns of a block of tokens
+  int wgs, add_wgs;                 // of the launch, and of the one that adds their sums (0: none)
+  bool walk;                        // whether there may be more pieces than that
+  size_t off_part, bytes;           // workspace: ScoresWork (kvr_prompt.h), then those sums
 };
-ScoresPlan prompt_scores_plan(const DevDesc& d, long long n_rows, long long cap);
-hipError_t launch_prompt_scores_bf16(const DevDesc& d, const PagedArgs& a, const ScoresPlan& p, const float* lse, float* part,
-                                     hipStream_t st);
+// Pieces of work that the scores' pass is cut into: three for two workgroups that the chip holds (2 x 600 tokens, 32 heads on 8, the
+// whole call: 1024 pieces 53 us, 768 49, 512 48; 4 x 2k 274, 275, 282).
+constexpr int SC_PIECES = 768;
+constexpr int SC_MOST_WGS = 16384;  // of its launch
+// Parts of each of `blocks` blocks of tokens (of what there is, not of what there is room for); a launch of wgs workgroups has one for
+// each of the longest sequence's `longest` blocks, all units alike, in its parts.
+__host__ __device__ inline int scores_splits(int blocks, int longest, int units, int most, int wgs) {
+  int s = blocks < SC_PIECES && blocks > 0 ? (SC_PIECES + blocks - 1) / blocks : 1;
+  s = s < most ? s : most;
+  const long long row = (long long)longest * units;
+  return s * row > wgs ? (row >= wgs ? 1 : wgs / (int)row) : s;
+}
+struct ScoresWork;
+ScoresPlan prompt_scores_plan(const DevDesc& d, long long n_rows, long long keys);
+hipError_t launch_prompt_scores_bf16(const DevDesc& d, const PagedArgs& a, const ScoresPlan& p, const float* lse, char* ws, hipStream_t st);
 struct PromptPlan {
   int splits;
   long long wgs;
   ScoresPlan scores;
   size_t off_lse, off_o, off_ml, off_scores, total;
 };
-PromptPlan prompt_bf16_plan(const DevDesc& d, long long n_rows, long long cap, const Visible& vis, bool scores);
+// n_cap: places for scores, 0: none are wanted
+PromptPlan prompt_bf16_plan(const DevDesc& d, long long n_rows, long long cap, const Visible& vis, long long n_cap);
 hipError_t launch_prompt_bf16(const DevDesc& d, const PagedArgs& a, const PromptPlan& p, hipStream_t st);
 size_t attend_prompt_ws(const DevDesc& d, int dtype, long long n_rows, long long cap, const Visible& vis, bool scores);
 hipError_t launch_attend_prompt(const DevDesc& d, int dtype, const PagedArgs& a, hipStream_t st);

@@ -177,5 +177,15 @@ template <int T>
 __host__ __device__ __forceinline__ int tile_token(const TileRange& r, int i) {
   return i < r.ahead ? i * T : r.start + (i - r.ahead) * T;
 }
+// how many of them start before token `end` (> 0)
+template <int T>
+__host__ __device__ __forceinline__ int tiles_before(const TileRange& r, int end) {
+  if (end <= r.start) {
+    const int n = (end - 1) / T + 1;
+    return n < r.ahead ? n : r.ahead;
+  }
+  const int n = r.ahead + (end - 1 - r.start) / T + 1;
+  return n < r.n ? n : r.n;
+}
 
 }  // namespace kvr

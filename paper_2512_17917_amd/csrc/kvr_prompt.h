@@ -1,6 +1,6 @@
 // What the two bf16 kernels of a prompt's attention share.
 #pragma once
-#include "kvr_dev.h"
+#include "kvr_launch.h"
 
 namespace kvr {
 
@@ -50,6 +50,49 @@ struct Scale2 {
 };
 __device__ __forceinline__ Scale2 scale2(float scale) {
   return {scale == 0.f ? 1.f : fabsf(scale) * LOG2E, scale < 0.f ? 0x80008000u : 0u, scale == 0.f ? 0u : 0xffffffffu};
+}
+
+// ---- what the pass that adds scores has to do --------------------------------
+constexpr int SC_KEYS = 256;        // tokens of a block, which a workgroup of that pass has
+
+// A sequence's blocks of tokens that some of its new tokens see and whose scores are wanted (tokens before `keys`).
+struct Blocks {
+  RowSpan span;
+  int tokens;                       // of the sequence
+  TileRange range;
+  int n;                            // of the range's tiles the first ones
+};
+__device__ __forceinline__ Blocks seq_blocks(const PagedArgs& a, int b, int keys) {
+  Blocks r;
+  r.span = row_span(a.q_start, a.n_rows, b);
+  r.tokens = clampi(listed(a.n_ctx + b), 0, a.pages.cap);
+  r.range = tile_range<SC_KEYS>(a.vis, r.tokens - r.span.n, r.tokens - 1);
+  r.n = r.span.n > 0 ? tiles_before<SC_KEYS>(r.range, keys) : 0;
+  return r;
+}
+// Only the device knows how much there is to do; the attention kernel finds it out and leaves it in the workspace.
+struct ScoresWork {
+  int all, longest, splits;         // blocks of all units, of the longest sequence, parts that each block's columns are cut into
+  int before[];                     // [B] blocks of a head in the sequences before
+};
+// (a wave)
+__device__ __forceinline__ void find_scores_work(const DevDesc& d, const PagedArgs& a, int keys, int most_splits, int wgs, ScoresWork* w) {
+  const int lane = threadIdx.x & 63;
+  int sum = 0, longest = 0;
+  for (int b0 = 0; b0 < d.B; b0 += 64) {
+    const int n = b0 + lane < d.B ? seq_blocks(a, b0 + lane, keys).n : 0;
+    const int upto = lanes_upto(n);
+    if (b0 + lane < d.B) w->before[b0 + lane] = sum + upto - n;
+    sum += __builtin_amdgcn_readlane(upto, 63);
+    longest = max(longest, n);
+  }
+  longest = wave_reduce(longest, [](int x, int y) { return x > y ? x : y; });
+  sum *= d.Hkv;                     // (the host has made sure that it fits)
+  if (lane == 0) {
+    w->all = sum;
+    w->longest = longest;
+    w->splits = scores_splits(sum, longest, d.B * d.Hkv, most_splits, wgs);
+  }
 }
 
 }  // namespace kvr
