@@ -486,7 +486,8 @@ int32_t kvr_attend_multi(const kvr_desc* desc, const void* q, int32_t n_q, const
  *              [0, n_rows].  NULL: row b is the newest token of sequence b (n_rows = B).
  *   n_ctx      dev int32 [B]: tokens of the sequence, the new ones included; the last new row's
  *              position is n_ctx[b] - 1, the one before it n_ctx[b] - 2, and so on.
- * n_rows is at most 2^27, n_rows * Hq below 2^31; n_rows = 0 does nothing.
+ * n_rows is at most 2^27, n_rows * Hq below 2^31, for kvr_attend_prompt at most 2^30; n_rows = 0
+ * does nothing.
  */
 
 /*

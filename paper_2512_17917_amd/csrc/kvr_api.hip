@@ -446,9 +446,11 @@ static int32_t check_pages(const kvr_desc* desc, const kvr_pages* pages, kvr::De
 }
 
 constexpr int MAX_ROWS_NEW = 1 << 27;
+// (attention launches two threads a row and head, fewer than 2^32; q and out of more would not fit the memory)
+constexpr long long MAX_HEADS_ROTATED = 0x7fffffffll, MAX_HEADS_ATTENDED = 1ll << 30;
 
-static int32_t check_rows(const kvr_desc* desc, int32_t n_rows, const int32_t* q_start) {
-  if (n_rows < 0 || n_rows > MAX_ROWS_NEW || (long long)n_rows * desc->n_q_heads > 0x7fffffffll) return KVR_ERR_INVALID_ARG;
+static int32_t check_rows(const kvr_desc* desc, int32_t n_rows, const int32_t* q_start, long long most_heads) {
+  if (n_rows < 0 || n_rows > MAX_ROWS_NEW || (long long)n_rows * desc->n_q_heads > most_heads) return KVR_ERR_INVALID_ARG;
   if (q_start == nullptr && n_rows != desc->batch) return KVR_ERR_INVALID_ARG;
   return KVR_OK;
 }
@@ -465,7 +467,7 @@ int32_t kvr_rotate(const kvr_desc* desc, const kvr_rotation* rot, const void* q,
   if ((rot->rot_dim > 0 && !rot->inv_freq) || (reinterpret_cast<uintptr_t>(rot->inv_freq) & 7u) != 0)
     return KVR_ERR_INVALID_ARG;
   if (!aligned16(rot->q_weight) || !aligned16(rot->k_weight)) return KVR_ERR_INVALID_ARG;
-  rc = check_rows(desc, n_rows, q_start);
+  rc = check_rows(desc, n_rows, q_start, MAX_HEADS_ROTATED);
   if (rc != KVR_OK) return rc;
   kvr::RotateArgs a;
   memset(&a, 0, sizeof(a));
@@ -547,7 +549,7 @@ int32_t kvr_attend_prompt_workspace_size(const kvr_desc* desc, int32_t n_rows, c
   if (rc == KVR_OK) rc = pages_size(desc, pages, p);
   if (rc == KVR_OK) rc = check_visible(window, n_sink, vis);
   if (rc != KVR_OK) return rc;
-  if (bytes == nullptr || n_rows < 0 || n_rows > MAX_ROWS_NEW || (long long)n_rows * d.Hq > 0x7fffffffll)
+  if (bytes == nullptr || n_rows < 0 || n_rows > MAX_ROWS_NEW || (long long)n_rows * d.Hq > MAX_HEADS_ATTENDED)
     return KVR_ERR_INVALID_ARG;
   if (!kvr::attend_paged_fits(d, p.cap, kvr::Visible{0, 0})) return KVR_ERR_UNSUPPORTED;
   *bytes = n_rows == 0 ? 0 : kvr::attend_prompt_ws(d, desc->dtype, n_rows, p.cap, vis, scores != 0);
@@ -562,7 +564,7 @@ int32_t kvr_attend_prompt(const kvr_desc* desc, const void* q, int32_t n_rows, c
   memset(&a, 0, sizeof(a));
   int32_t rc = check_desc(desc, d);
   if (rc == KVR_OK) rc = check_visible(window, n_sink, a.vis);
-  if (rc == KVR_OK) rc = check_rows(desc, n_rows, q_start);
+  if (rc == KVR_OK) rc = check_rows(desc, n_rows, q_start, MAX_HEADS_ATTENDED);
   if (rc != KVR_OK) return rc;
   if (n_rows == 0) return KVR_OK;
   rc = check_attend(desc, q, n_ctx, pages, out, scores, n_cap, a);

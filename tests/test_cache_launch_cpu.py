@@ -119,3 +119,14 @@ def test_tiles_that_start_before_a_token(ask):
         (0, 1, 300, 1000), (0, 1, 256, 700, 5000), (-3, 0, 255, 1500, 4000), (0, 255, 900), (1, 256, 257, 1400, 2000, 9000))]
     for case, (n, *tiles) in zip(cases, ask([("t " + " ".join(map(str, c))) for c in cases])):
         assert n == sum(t < case[4] for t in tiles), case
+
+
+def test_more_rows_and_heads_than_attention_is_launched_for_are_refused():
+    """2^30 rows times heads: 256 GiB of queries in bf16, twice that with the outputs."""
+    d, n = kvr.make_desc(1, 12, 3, 1, 1, kvr.KVR_BF16), C.c_size_t(0)
+    p = kvr.kvr_pages(0x10000, 0x10000, 0x10000, 10, 64, 100)
+    P = 0x10000
+    for rows, want, call in (((1 << 30) // 12, kvr.KVR_OK, kvr.KVR_ERR_WORKSPACE_TOO_SMALL), ((1 << 30) // 12 + 1, kvr.KVR_ERR_INVALID_ARG, kvr.KVR_ERR_INVALID_ARG),
+                             (1 << 27, kvr.KVR_ERR_INVALID_ARG, kvr.KVR_ERR_INVALID_ARG)):
+        assert kvr.lib().kvr_attend_prompt_workspace_size(C.byref(d), rows, C.byref(p), 0, 0, 1, C.byref(n)) == want
+        assert kvr.lib().kvr_attend_prompt(C.byref(d), P, rows, P, P, C.byref(p), 0, 0, P + 16, P, 64, P, 0, None) == call
