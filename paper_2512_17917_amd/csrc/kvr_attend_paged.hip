@@ -490,8 +490,12 @@ __global__ __launch_bounds__(64 * PG_WAVES, paged_per_cu(sizeof(T), G)) void pag
   }
 }
 
-// (a token that is not seen has none, also where the sum is NaN)
-__device__ __forceinline__ float weight_of(float s, float lse) { return s == -__builtin_inff() ? 0.f : exp2_(s - lse); }
+// What a token's score grows by, `sum` of its weights exp(s - lse): a token that is not seen has logits of -inf, as a seen one may have,
+// so where a lse is NaN the sums of both are, and only the seen one's counts.
+__device__ __forceinline__ bool counts(const PagedArgs& a, float sum, int b, int P, int j) {
+  if (sum == sum) return sum != 0.f;
+  return sees(a.vis, P, j) && (uint32_t)page_entry(a.pages, b, j) < (uint32_t)a.pages.n_pages;
+}
 
 // Caches of few tokens: a workgroup of as many waves as a CU takes has a whole unit, and nothing is left to join.
 template <typename T, int G, bool ONE>
@@ -522,8 +526,8 @@ __global__ __launch_bounds__(64 * short_waves(sizeof(T), G)) void paged_short_ke
     if (j >= n || j >= a.n_cap) continue;
     float sum = 0.f;
 #pragma unroll
-    for (int g = 0; g < G; ++g) sum += weight_of(s_log[e * G + g], lse[g]);
-    if (sum != 0.f) a.scores[(size_t)u * a.n_cap + j] += sum;
+    for (int g = 0; g < G; ++g) sum += exp2_(s_log[e * G + g] - lse[g]);
+    if (counts(a, sum, b, n - 1, j)) a.scores[(size_t)u * a.n_cap + j] += sum;
   }
 }
 
@@ -645,8 +649,8 @@ __global__ __launch_bounds__(256) void paged_join_kernel(DevDesc d, PagedArgs a,
   for (int i = 0; i < PG_SLICE / 256; ++i) {
     float sum = 0.f;
 #pragma unroll
-    for (int g = 0; g < G; ++g) sum += weight_of(lo[i][g], lse[g]);
-    if (at[i] >= 0 && sum != 0.f) a.scores[(size_t)u * a.n_cap + at[i]] = old[i] + sum;
+    for (int g = 0; g < G; ++g) sum += exp2_(lo[i][g] - lse[g]);
+    if (at[i] >= 0 && counts(a, sum, b, n - 1, at[i])) a.scores[(size_t)u * a.n_cap + at[i]] = old[i] + sum;
   }
 }
 
