@@ -561,6 +561,7 @@ def make_rotation(desc, inv_freq=None, *, q_weight=None, k_weight=None, eps=1e-6
                      _ptr(inv_freq, torch.float64, 1, "inv_freq") if n else None, eps, 2 * n,
                      KVR_ROTATE_PAIRS if pairs else KVR_ROTATE_HALVES)
     r.tensors = (inv_freq, q_weight, k_weight)
+    r.weights = None if q_weight is None and k_weight is None else desc.dtype
     r.dev = _one_device(*r.tensors)
     return r
 
@@ -586,6 +587,8 @@ def kvr_rotate(desc, rot, q, k, v, n_rows, q_start, n_ctx, q_out, k_out=None, pa
     """As the C call; the rows' strides are the tensors' own."""
     if not isinstance(rot, kvr_rotation) or not hasattr(rot, "tensors"):
         raise TypeError("rot must come from make_rotation")
+    if rot.weights is not None and rot.weights != desc.dtype:
+        raise ValueError("the rotation's weights were made for another kind of descriptor")
     pp = _pages(desc, pages, True)
     lib()
     one = q if q is not None else k
