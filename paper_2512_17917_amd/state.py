@@ -286,8 +286,14 @@ class PagedCache:
         return self.out
 
     def dense(self, n_tokens):
-        """Keys and values of the first n_tokens of every sequence as dense caches [B, Hkv, n_tokens, D] (every sequence
-        has them all), for LayerState.from_prefill."""
+        """Keys and values of the first n_tokens of every sequence as dense caches [B, Hkv, n_tokens, D], for
+        LayerState.from_prefill.  Raises ValueError where a sequence does not have them all, tokens whose page is not there
+        among them; looks at the table and n_ctx for that, so it synchronises."""
         ps = self.k.shape[2]
-        at = self.table[:, :-(-n_tokens // ps)].long()
+        if n_tokens < 1 or -(-n_tokens // ps) > self.table.shape[1]:
+            raise ValueError(f"n_tokens = {n_tokens}: a sequence has room for 1 .. {self.table.shape[1] * ps}")
+        B = self.desc.batch
+        at = self.table[:B, :-(-n_tokens // ps)].long()
+        if not bool(((at >= 0) & (at < self.k.shape[0])).all() & (self.n_ctx[:B] >= n_tokens).all()):
+            raise ValueError(f"not every sequence has its first {n_tokens} tokens in the cache")
         return tuple(x[at].transpose(1, 2).flatten(2, 3)[:, :, :n_tokens].contiguous() for x in (self.k, self.v))

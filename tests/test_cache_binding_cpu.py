@@ -3,6 +3,7 @@ import pytest
 import torch
 
 from paper_2512_17917_amd import binding as kvr
+from paper_2512_17917_amd.state import PagedCache
 from tests.test_cache_fast_cpu import Fake, _desc, _rotate_args, fast        # noqa: F401
 
 
@@ -29,3 +30,31 @@ def test_a_rotation_whose_weights_are_of_another_type_is_refused(fast, monkeypat
         kvr.kvr_rotate(used, kvr.make_rotation(made, inv), *a.values())
         assert len(got) == 1
         got.clear()
+
+
+def _cache_of(table, n_ctx, n_pages=5, page=4):
+    """A PagedCache on the CPU, of which `dense` alone is called."""
+    c = PagedCache.__new__(PagedCache)
+    c.desc = _desc()
+    c.desc.batch = len(table)
+    c.k, c.v = torch.randn(2, n_pages, 2, page, 8)
+    c.table, c.n_ctx = torch.tensor(table, dtype=torch.int32), torch.tensor(n_ctx, dtype=torch.int32)
+    return c
+
+
+def test_dense_takes_tokens_that_are_there():
+    c = _cache_of([[3, 0, -1], [4, 1, 9]], [7, 8])
+    for n in (1, 4, 5, 7):
+        for got, pool in zip(c.dense(n), (c.k, c.v)):
+            for b, pages in enumerate(([3, 0], [4, 1])):
+                assert torch.equal(got[b], torch.cat([pool[p] for p in pages], 1)[:, :n]), n
+
+
+@pytest.mark.parametrize("table,n_ctx,n", [([[3, -1, 2], [4, 1, 0]], [9, 9], 5),       # no page: not the pool's last one
+                                           ([[3, 1, 2], [4, 5, 0]], [9, 9], 5),        # past the pool
+                                           ([[3, 1, 2], [4, 0, 0]], [9, 4], 5),        # tokens that have not come yet
+                                           ([[3, 1], [4, 0]], [8, 8], 9),              # more than the table holds
+                                           ([[3, 1], [4, 0]], [8, 8], 0), ([[3, 1], [4, 0]], [8, 8], -1)])
+def test_dense_refuses_tokens_that_are_not(table, n_ctx, n):
+    with pytest.raises(ValueError):
+        _cache_of(table, n_ctx).dense(n)
