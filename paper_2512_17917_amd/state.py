@@ -166,6 +166,8 @@ class LayerState:
         moved into ret_cap = n_recent + k_candidate + slack + 1 slots, everything else
         goes into the sketch.  Returns (state, info)."""
         B, Hkv, N, D = K.shape
+        if init_scores is None and q_prompt is not None and tuple(q_prompt.shape) != (desc.batch, N, desc.n_q_heads, D):
+            raise ValueError(f"q_prompt: shape {tuple(q_prompt.shape)}, need {(desc.batch, N, desc.n_q_heads, D)}")
         dev = K.device
         R = n_recent + k_candidate
         ret_cap = R + slack + 1

@@ -3,7 +3,7 @@ import pytest
 import torch
 
 from paper_2512_17917_amd import binding as kvr
-from paper_2512_17917_amd.state import PagedCache
+from paper_2512_17917_amd.state import LayerState, PagedCache
 from tests.test_cache_fast_cpu import Fake, _desc, _rotate_args, fast        # noqa: F401
 
 
@@ -58,3 +58,27 @@ def test_dense_takes_tokens_that_are_there():
 def test_dense_refuses_tokens_that_are_not(table, n_ctx, n):
     with pytest.raises(ValueError):
         _cache_of(table, n_ctx).dense(n)
+
+
+def _no_device(monkeypatch):
+    """The calls into the library record themselves; tensors may live anywhere."""
+    calls = []
+    for name in ("kvr_attend_prompt", "kvr_attend_paged", "kvr_rotate", "kvr_attend_decode"):
+        monkeypatch.setattr(kvr, name, lambda *a, _n=name: calls.append(_n))
+    for name in ("kvr_attend_prompt_workspace_size", "kvr_attend_paged_workspace_size"):
+        monkeypatch.setattr(kvr, name, lambda *a: 0)
+    monkeypatch.setattr(kvr, "make_pages", lambda *a: None)
+    monkeypatch.setattr(kvr, "alloc_workspace", lambda *a: torch.empty(256, dtype=torch.uint8))
+    return calls
+
+
+@pytest.mark.parametrize("shape", [(2, 8, 8, 128), (2, 10, 8, 128), (1, 9, 8, 128), (3, 9, 8, 128), (2, 9, 4, 128), (18, 8, 128)])
+def test_a_prompt_has_a_query_for_each_of_its_tokens(monkeypatch, shape):
+    """Fewer rows would be taken for the newest tokens', more for tokens before the first: from_prefill's scores would lack them."""
+    calls = _no_device(monkeypatch)
+    d = kvr.make_desc(2, 8, 2, 3, 5, torch.bfloat16, seed=1)
+    K, V = torch.zeros(2, 2, 2, 9, 128, dtype=torch.bfloat16)
+    q = torch.zeros(shape, dtype=torch.bfloat16)
+    with pytest.raises(ValueError):
+        LayerState.from_prefill(d, K, V, None, n_recent=4, k_candidate=2, max_new_tokens=1, q_prompt=q)
+    assert not calls
