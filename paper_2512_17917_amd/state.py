@@ -244,6 +244,8 @@ class PagedCache:
         shared by layers; rotation: a binding.make_rotation (None: queries and keys are cached as they come);
         scores: accumulate the weights that each token draws."""
         B, Hkv, D = desc.batch, desc.n_kv_heads, desc.head_dim
+        if table is not None and (table.dim() != 2 or table.shape[1] != table_cap):
+            raise ValueError(f"table: shape {tuple(table.shape)}, need [{B}, {table_cap}]")
         self.desc, self.window, self.n_sink = desc, int(window), int(n_sink)
         self.device = torch.device(device)
         self.dtype = torch.float32 if desc.dtype == kvr.KVR_F32 else torch.bfloat16

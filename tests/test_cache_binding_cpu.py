@@ -82,3 +82,18 @@ def test_a_prompt_has_a_query_for_each_of_its_tokens(monkeypatch, shape):
     with pytest.raises(ValueError):
         LayerState.from_prefill(d, K, V, None, n_recent=4, k_candidate=2, max_new_tokens=1, q_prompt=q)
     assert not calls
+
+
+def test_a_given_table_has_the_width_that_it_is_said_to_have(monkeypatch):
+    """With more columns than table_cap, tokens past table_cap * page_size would be attended but their scores dropped."""
+    _no_device(monkeypatch)
+    d = kvr.make_desc(2, 8, 2, 3, 5, torch.bfloat16, seed=1)
+    make = lambda table, **kw: PagedCache(d, n_pages=4, page_size=16, table_cap=6, device="cpu", table=table, **kw)
+    monkeypatch.setattr(kvr, "make_rotation", lambda *a: None)
+    for cols in (5, 7):
+        with pytest.raises(ValueError):
+            make(torch.zeros(2, cols, dtype=torch.int32))
+    for rows in (2, 3):
+        c = make(torch.zeros(rows, 6, dtype=torch.int32))
+        assert c.scores.shape == (2, 2, 96)
+    assert make(None).table.shape == (2, 6)
