@@ -264,6 +264,8 @@ class PagedCache:
 
     def assign(self, b, first, pages):
         """Pages (numbers) of sequence b from its `first`-th page on."""
+        if first < 0 or first + len(pages) > self.table.shape[1]:
+            raise ValueError(f"pages {first} .. {first + len(pages) - 1} of a sequence that has room for {self.table.shape[1]}")
         self.table[b, first:first + len(pages)] = torch.as_tensor(pages, dtype=torch.int32, device=self.device)
 
     def prompt(self, q, k, v, q_start):

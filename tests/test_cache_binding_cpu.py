@@ -97,3 +97,16 @@ def test_a_given_table_has_the_width_that_it_is_said_to_have(monkeypatch):
         c = make(torch.zeros(rows, 6, dtype=torch.int32))
         assert c.scores.shape == (2, 2, 96)
     assert make(None).table.shape == (2, 6)
+
+
+@pytest.mark.parametrize("first,pages", [(6, [3]), (5, [1, 2]), (-1, [3]), (-2, [1, 2]), (7, [3])])
+def test_pages_past_the_table_are_refused(first, pages):
+    """One page just past the end was assigned nowhere, without a word."""
+    c = _cache_of([[-1] * 6, [-1] * 6], [0, 0])
+    c.device = torch.device("cpu")
+    with pytest.raises(ValueError):
+        c.assign(1, first, pages)
+    assert bool((c.table == -1).all())
+    c.assign(1, 4, [2, 0])
+    c.assign(0, 6, [])
+    assert c.table.tolist() == [[-1] * 6, [-1] * 4 + [2, 0]]
