@@ -519,8 +519,10 @@ int32_t kvr_rotate(const kvr_desc* desc, const kvr_rotation* rot, const void* q,
  * tokens and the G q heads of its kv head, always in the same order.  A query that sees no token,
  * or none whose logit is above -Inf, yields zeros; NaN among the logits that it sees gives NaN in
  * its output and in the scores of the tokens that it sees.  n_ctx is clamped to what the cache
- * can hold.  KVR_ERR_UNSUPPORTED where B * Hkv times the tokens that a sequence can hold passes
- * 2^37.  Tokens that no query of a row sees may hold anything, Inf and NaN too.
+ * can hold.  Logits, sums and products are float32; where the storage type is bf16, this call (not
+ * kvr_attend_paged) rounds p to bf16 for its product with v, which adds up to half a step of the type,
+ * 2^-8, relative to sum_j p |v[j]|.  KVR_ERR_UNSUPPORTED where B * Hkv times the tokens that a sequence
+ * can hold passes 2^37.  Tokens that no query of a row sees may hold anything, Inf and NaN too.
  *   q          dev [n_rows, Hq, D] storage type, read
  *   pages      host; k, v and table are read
  *   window     0: no window

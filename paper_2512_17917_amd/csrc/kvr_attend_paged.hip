@@ -63,7 +63,8 @@ PagedPlan paged_plan(const DevDesc& d, int dtype, long long cap, const Visible& 
   p.fits = chunks < 0x7fffffffll;
   const int fill = 256 * paged_per_cu(dtype == KVR_F32 ? 4 : 2, d.G);
   p.wgs = (int)(chunks < fill ? chunks : fill);
-  // A unit to one workgroup: where that is a tile a wave, and for up to 1024 tokens (with eight heads 512) where units are many:
+  // A unit to one workgroup: where that is a tile a wave, and for up to 1024 tokens (with eight heads 512) where units are many.
+  // That goes by the tokens that there is room for: short sequences in a large cache take even pieces and the join.
   // 1000 tokens, 32 heads on 8, 512 units 46 us against 64 in even pieces and a join, 128 units 19 against 24, but 8 units 15
   // against 14 (float32, half the waves: 32 against 13); 100 tokens, 8 units 7 against 13.
   p.whole = p.tiles <= short_waves(dtype == KVR_F32 ? 4 : 2, d.G) || (p.tiles <= short_tiles(d.G) && units >= 64);

@@ -318,8 +318,10 @@ __global__ __launch_bounds__(64 * FP_WAVES, 2) void prompt_bf16_kernel(DevDesc d
   // Tiles that are seen whole.  Waves 0..3 and 4..7, one of each on a SIMD, go half a tile apart: while one has the matrix unit
   // (values of step i, logits of step i + 1), the other has the vector unit (weights).  Stretch k lies between barriers k and
   // k + 1 of the loop: the early waves compute the weights of step i in stretch 2 i, the late ones in stretch 2 i + 1.  What is
-  // fetched there, step i + 2 or i + 3, takes the place of a tile whose values were last read two stretches before, and what
-  // has arrived at the stretch's end, step i + 1 or i + 2, is first read in the stretch after or later.
+  // fetched there takes the place of a tile whose values were last read by the late waves, in stretch 2 step: step i + 2, fetched by
+  // the early waves in stretch 2 i, that of step i - 2, two stretches before; step i + 3, by the late ones in stretch 2 i + 1, that of
+  // step i - 1, one stretch before (a wave comes to the barrier between with its products issued, whose operands have been read).
+  // What has arrived at the stretch's end, step i + 1 or i + 2, is first read in the stretch after or later.
   if (n_in > 0) {
     const int late = wave >= FP_WAVES / 2 ? 1 : 0;
     auto walk = [&](auto alive) {

@@ -2,7 +2,7 @@
  * over it) without the interpreter between the checks: the same checks of every tensor that
  * binding._ptr makes (that it is one, type, place, contiguity, size), made through the tensor's own attributes, and the call itself.  A
  * check that fails, or an argument of an unexpected kind, returns None: the caller then takes the Python path, which
- * says what is wrong.  Nothing is kept between calls but the names, the types and the two entry points. */
+ * says what is wrong.  Nothing is kept between calls but the names, the types and the five entry points. */
 #define PY_SSIZE_T_CLEAN
 #include <Python.h>
 #include <stdint.h>
