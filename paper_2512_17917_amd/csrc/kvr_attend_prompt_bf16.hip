@@ -15,7 +15,7 @@
 //
 // Bound by power: 2 x 8192 tokens, 32 heads on 8, causal, take 1.00 ms = 1.10 PFLOP/s (a matrix product of 8192^3 reaches 1.21
 // to 1.30 here), the same kernel on zeros 0.77 ms, where the clock stays up (the product: 0.63 for 0.90).  The matrix units are
-// busy 57 % of the cycles.  With all waves in step 1.11 ms; without a loop of their own for the tiles seen whole 1.13.
+// busy 54 to 57 % of the cycles.  With all waves in step 1.11 ms; without a loop of their own for the tiles seen whole 1.13.
 //
 // LDS rows are 256 bytes, 16 pieces of 16; keys: piece c of row r lies at c ^ (r mod 16), values: at c ^ 4 (r mod 4), so that
 // the lanes that are served together find different banks.
