@@ -242,7 +242,9 @@ class PagedCache:
                  device="cuda", n_ctx=None, table=None):
         """table int32 [B, table_cap] (None: made here, with no page assigned; see assign) and n_ctx int32 [B] may be
         shared by layers; rotation: a binding.make_rotation (None: queries and keys are cached as they come);
-        scores: accumulate the weights that each token draws."""
+        scores: accumulate the weights that each token draws.  Tokens past table_cap * page_size are stored nowhere and
+        attention takes the sequence to end there: the caller, who advances n_ctx, keeps it within.  A place of the batch
+        that passes to another sequence keeps its scores until the caller clears them."""
         B, Hkv, D = desc.batch, desc.n_kv_heads, desc.head_dim
         if table is not None and (table.dim() != 2 or table.shape[1] != table_cap):
             raise ValueError(f"table: shape {tuple(table.shape)}, need [{B}, {table_cap}]")
