@@ -21,10 +21,12 @@
  *                                            -> kvr_attend_decode
  *   - the same for several query tokens per sequence over one rebuilt cache
  *                                            -> kvr_attend_multi
- * Around it stand three operators of the uncompressed cache, the one that a prompt fills
+ * Around it stand operators of the uncompressed cache, the one that a prompt fills
  * and that Algorithm 3 then compresses:
  *   - norms and rotation of new tokens' queries and keys, and their place in the cache
  *                                            -> kvr_rotate
+ *   - the same by positions on several axes (time, line and column of a picture's or a
+ *     video's tokens)                        -> kvr_rotate_axes
  *   - attention of a prompt's queries, with the Softmax(QK^T) that they accumulate per
  *     token (Overview, Calculation Phase)    -> kvr_attend_prompt
  *   - attention of one new token over a paged cache
@@ -194,6 +196,17 @@ typedef struct kvr_rotation {
   float eps;
   int32_t rot_dim, style;
 } kvr_rotation;
+
+/*
+ * Axes of positions (host memory, plain data): pair i of a kvr_rotation is turned by the position on axis axis[i].
+ *   n_axes     1 .. KVR_MAX_AXES
+ *   axis       below n_axes for each of the rotation's rot_dim / 2 pairs (the others are not looked at)
+ */
+#define KVR_MAX_AXES 8
+typedef struct kvr_axes {
+  int32_t n_axes;
+  uint8_t axis[KVR_HEAD_DIM / 2];
+} kvr_axes;
 
 /* Library version string (static storage). */
 const char* kvr_version(void);
@@ -508,6 +521,21 @@ int32_t kvr_rotate(const kvr_desc* desc, const kvr_rotation* rot, const void* q,
                    const void* k, int64_t k_stride, const void* v, int64_t v_stride, int32_t n_rows,
                    const int32_t* q_start, const int32_t* n_ctx, void* q_out, void* k_out,
                    const kvr_pages* pages, void* stream);
+
+/*
+ * kvr_rotate with positions of the caller's on several axes: pair i of row r is turned by the angle
+ * pos[axes->axis[i]][r] * inv_freq[i].  Where a row goes in the cache is given by q_start and n_ctx as ever; a row whose
+ * positions are its place in the sequence on every axis becomes what kvr_rotate makes of it, bit for bit.
+ *   pos        dev int32 [n_axes][n_rows], any values; an axis' row is dense, pos_stride elements (not looked at for
+ *              one axis; 0: one row for all axes) behind the axis' before it.  Not looked at where rot_dim = 0
+ *   n_rows, q_start, n_ctx   as for kvr_rotate.  Without pages n_ctx is not looked at and may be NULL, and with q_start NULL
+ *              all n_rows rows are turned, whatever the batch (the patches of a picture, before they are anybody's tokens)
+ *   the others as for kvr_rotate
+ */
+int32_t kvr_rotate_axes(const kvr_desc* desc, const kvr_rotation* rot, const kvr_axes* axes, const int32_t* pos,
+                        int64_t pos_stride, const void* q, int64_t q_stride, const void* k, int64_t k_stride,
+                        const void* v, int64_t v_stride, int32_t n_rows, const int32_t* q_start,
+                        const int32_t* n_ctx, void* q_out, void* k_out, const kvr_pages* pages, void* stream);
 
 /*
  * Causal attention of the new tokens over the cache, which holds them already.  A query at

@@ -44,7 +44,8 @@ EXPORTS = ["kvr_version", "kvr_last_hip_error", "kvr_recent_size", "kvr_hash_par
            "kvr_swap_back", "kvr_reconstruct", "kvr_attend_decode", "kvr_attend_decode_static",
            "kvr_attend_multi_workspace_size", "kvr_attend_multi"]
 EXPORTS += ["kvr_rotate", "kvr_attend_prompt_workspace_size", "kvr_attend_prompt", "kvr_attend_paged_workspace_size",
-            "kvr_attend_paged"]
+            "kvr_attend_paged", "kvr_rotate_axes"]
+KVR_MAX_AXES = 8
 KVR_ROTATE_HALVES, KVR_ROTATE_PAIRS = 0, 1
 KVR_STATIC_SCRATCH_BYTES = 80 << 20
 
@@ -76,6 +77,10 @@ class kvr_pages(C.Structure):
 class kvr_rotation(C.Structure):
     _fields_ = [("q_weight", C.c_void_p), ("k_weight", C.c_void_p), ("inv_freq", C.c_void_p),
                 ("eps", C.c_float), ("rot_dim", C.c_int32), ("style", C.c_int32)]
+
+
+class kvr_axes(C.Structure):
+    _fields_ = [("n_axes", C.c_int32), ("axis", C.c_uint8 * (KVR_HEAD_DIM // 2))]
 
 
 _fast = None
@@ -188,6 +193,9 @@ def lib() -> C.CDLL:
         pp = C.POINTER(kvr_pages)
         L.kvr_rotate.restype = i32
         L.kvr_rotate.argtypes = [dp, C.POINTER(kvr_rotation), vp, i64, vp, i64, vp, i64, i32, vp, vp, vp, vp, pp, vp]
+        L.kvr_rotate_axes.restype = i32
+        L.kvr_rotate_axes.argtypes = [dp, C.POINTER(kvr_rotation), C.POINTER(kvr_axes), vp, i64, vp, i64, vp, i64, vp, i64, i32,
+                                      vp, vp, vp, vp, pp, vp]
         L.kvr_attend_prompt_workspace_size.restype = i32
         L.kvr_attend_prompt_workspace_size.argtypes = [dp, i32, pp, i32, i32, i32, C.POINTER(sz)]
         L.kvr_attend_prompt.restype = i32
@@ -213,6 +221,7 @@ def _load_fast(L):
         m.setup(address(L.kvr_step_update), address(L.kvr_attend_decode), torch.float32, torch.bfloat16, torch.int32,
                 torch.uint8, torch.Tensor)
         m.setup_cache(address(L.kvr_rotate), address(L.kvr_attend_paged), address(L.kvr_attend_prompt))
+        m.setup_more(address(L.kvr_rotate_axes))
         _fast = m
 
 
@@ -583,12 +592,16 @@ def _rows(t, dtype, n_rows, heads, d, name):
     return t.data_ptr(), t.stride(0) if n_rows > 1 else heads * d
 
 
-def kvr_rotate(desc, rot, q, k, v, n_rows, q_start, n_ctx, q_out, k_out=None, pages=None):
-    """As the C call; the rows' strides are the tensors' own."""
+def _rotation(desc, rot):
     if not isinstance(rot, kvr_rotation) or not hasattr(rot, "tensors"):
         raise TypeError("rot must come from make_rotation")
     if rot.weights is not None and rot.weights != desc.dtype:
         raise ValueError("the rotation's weights were made for another kind of descriptor")
+
+
+def kvr_rotate(desc, rot, q, k, v, n_rows, q_start, n_ctx, q_out, k_out=None, pages=None):
+    """As the C call; the rows' strides are the tensors' own."""
+    _rotation(desc, rot)
     pp = _pages(desc, pages, True)
     lib()
     one = q if q is not None else k
@@ -611,6 +624,60 @@ def kvr_rotate(desc, rot, q, k, v, n_rows, q_start, n_ctx, q_out, k_out=None, pa
         _ptr(q_out, dt, n_rows * desc.n_q_heads * d, "q_out", True),
         _ptr(k_out, dt, n_rows * desc.n_kv_heads * d, "k_out", True), pp, _stream())
     _check("kvr_rotate", rc)
+
+
+def make_axes(axis, n_axes=None):
+    """kvr_axes: the axis of each turned pair of channels, as many as the rotation has; n_axes: how many axes there are
+    (None: the largest of them and those before it)."""
+    axis = [int(x) for x in axis]
+    n = max(axis, default=0) + 1 if n_axes is None else int(n_axes)
+    if not 1 <= n <= KVR_MAX_AXES or len(axis) > KVR_HEAD_DIM // 2 or any(not 0 <= x < n for x in axis):
+        raise ValueError(f"axes: {len(axis)} pairs of at most {KVR_HEAD_DIM // 2}, axes 0 .. {n - 1} of at most {KVR_MAX_AXES}")
+    a = kvr_axes(n, (C.c_uint8 * (KVR_HEAD_DIM // 2))(*axis))
+    a.pairs = len(axis)
+    return a
+
+
+def kvr_rotate_axes(desc, rot, axes, pos, q, k, v, n_rows, q_start, n_ctx, q_out, k_out=None, pages=None):
+    """As the C call; the rows' strides are the tensors' own.  pos int32 [n_axes, n_rows or more], the rows of an axis dense."""
+    _rotation(desc, rot)
+    if not isinstance(axes, kvr_axes) or not hasattr(axes, "pairs"):
+        raise TypeError("axes must come from make_axes")
+    if axes.pairs != rot.rot_dim // 2:
+        raise ValueError(f"axes of {axes.pairs} pairs, the rotation turns {rot.rot_dim // 2}")
+    pp = _pages(desc, pages, True)
+    lib()
+    one = q if q is not None else k
+    if _fast is not None and isinstance(desc, kvr_desc) and isinstance(one, torch.Tensor) and one.is_cuda:
+        dev = torch.cuda.current_device()
+        if rot.dev is not None and rot.dev != dev:
+            raise ValueError(f"the rotation lives on cuda:{rot.dev}, the current device is cuda:{dev}")
+        rc = _fast.rotate_axes(C.addressof(desc), C.addressof(rot), C.addressof(pages) if pages is not None else 0, dev,
+                               _stream_of(dev), q, k, v, n_rows, q_start, n_ctx, q_out, k_out, C.addressof(axes), pos)
+        if rc is not None:
+            return _check("kvr_rotate_axes", rc)
+    dt, d = _torch_dtype(desc), desc.head_dim
+    qp, qs = _rows(q, dt, n_rows, desc.n_q_heads, d, "q")
+    kp, ks = _rows(k, dt, n_rows, desc.n_kv_heads, d, "k")
+    vp, vs = _rows(v, dt, n_rows, desc.n_kv_heads, d, "v")
+    if pos is None and rot.rot_dim:
+        raise ValueError("pos is required")
+    if pos is not None:
+        if not isinstance(pos, torch.Tensor) or pos.dtype != torch.int32:
+            raise TypeError("pos must be an int32 tensor")
+        if not pos.is_cuda:
+            raise ValueError("pos must live in device memory")
+        if pos.dim() != 2 or pos.shape[0] < axes.n_axes or pos.shape[1] < n_rows or (pos.stride(1) != 1 and pos.shape[1] > 1):
+            raise ValueError(f"pos: shape {tuple(pos.shape)}, need [{axes.n_axes}, {n_rows}] with dense rows")
+    _here(q, k, v, q_start, n_ctx, q_out, k_out, pos, *rot.tensors)
+    rc = lib().kvr_rotate_axes(
+        C.byref(desc), C.byref(rot), C.byref(axes), pos.data_ptr() if pos is not None else None,
+        pos.stride(0) if pos is not None else 0, qp, qs, kp, ks, vp, vs, n_rows,
+        _ptr(q_start, torch.int32, desc.batch + 1, "q_start", True),
+        _ptr(n_ctx, torch.int32, desc.batch, "n_ctx", pages is None),
+        _ptr(q_out, dt, n_rows * desc.n_q_heads * d, "q_out", True),
+        _ptr(k_out, dt, n_rows * desc.n_kv_heads * d, "k_out", True), pp, _stream())
+    _check("kvr_rotate_axes", rc)
 
 
 def kvr_attend_prompt_workspace_size(desc, n_rows, pages, window, n_sink, scores) -> int:

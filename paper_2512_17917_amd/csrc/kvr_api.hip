@@ -455,9 +455,11 @@ static int32_t check_rows(const kvr_desc* desc, int32_t n_rows, const int32_t* q
   return KVR_OK;
 }
 
-int32_t kvr_rotate(const kvr_desc* desc, const kvr_rotation* rot, const void* q, int64_t q_stride, const void* k,
-                   int64_t k_stride, const void* v, int64_t v_stride, int32_t n_rows, const int32_t* q_start,
-                   const int32_t* n_ctx, void* q_out, void* k_out, const kvr_pages* pages, void* stream) {
+// kvr_rotate, and with `axes` kvr_rotate_axes
+static int32_t rotate_rows(const kvr_desc* desc, const kvr_rotation* rot, const kvr_axes* axes, const int32_t* pos, int64_t pos_stride,
+                           const void* q, int64_t q_stride, const void* k, int64_t k_stride, const void* v, int64_t v_stride,
+                           int32_t n_rows, const int32_t* q_start, const int32_t* n_ctx, void* q_out, void* k_out,
+                           const kvr_pages* pages, void* stream) {
   kvr::DevDesc d;
   int32_t rc = check_desc(desc, d);
   if (rc != KVR_OK) return rc;
@@ -467,16 +469,32 @@ int32_t kvr_rotate(const kvr_desc* desc, const kvr_rotation* rot, const void* q,
   if ((rot->rot_dim > 0 && !rot->inv_freq) || (reinterpret_cast<uintptr_t>(rot->inv_freq) & 7u) != 0)
     return KVR_ERR_INVALID_ARG;
   if (!aligned16(rot->q_weight) || !aligned16(rot->k_weight)) return KVR_ERR_INVALID_ARG;
-  rc = check_rows(desc, n_rows, q_start, MAX_HEADS_ROTATED);
-  if (rc != KVR_OK) return rc;
   kvr::RotateArgs a;
   memset(&a, 0, sizeof(a));
+  const bool placed = axes == nullptr || pages != nullptr;       // whether rows have to be their sequences' tokens
+  if (axes != nullptr) {
+    if (axes->n_axes < 1 || axes->n_axes > KVR_MAX_AXES) return KVR_ERR_INVALID_ARG;
+    for (int i = 0; i < rot->rot_dim / 2; ++i) {
+      if (axes->axis[i] >= axes->n_axes) return KVR_ERR_INVALID_ARG;
+      a.axis[i / 16] |= (uint64_t)axes->axis[i] << (4 * (i % 16));
+    }
+    if (rot->rot_dim > 0 && n_rows > 0) {
+      if (!pos || (reinterpret_cast<uintptr_t>(pos) & 3u) != 0) return KVR_ERR_INVALID_ARG;
+      if (axes->n_axes > 1 && (pos_stride < 0 || pos_stride > (int64_t)1 << 40)) return KVR_ERR_INVALID_ARG;
+    }
+    a.axes = true;
+    a.axis_pos = pos;
+    a.axis_stride = axes->n_axes > 1 ? pos_stride : 0;
+  }
+  // (without a cache and a list of starts the rows are nobody's in particular, however many there are)
+  rc = check_rows(desc, n_rows, placed || q_start != nullptr ? q_start : &desc->batch, MAX_HEADS_ROTATED);
+  if (rc != KVR_OK) return rc;
   if (pages != nullptr && n_rows > 0) {
     rc = check_pages(desc, pages, a.pages);
     if (rc != KVR_OK) return rc;
   }
   if (n_rows == 0) return KVR_OK;
-  if (!n_ctx || (!q && !k)) return KVR_ERR_INVALID_ARG;
+  if ((placed && !n_ctx) || (!q && !k)) return KVR_ERR_INVALID_ARG;
   if ((q == nullptr) != (q_out == nullptr)) return KVR_ERR_INVALID_ARG;
   if ((k != nullptr) != (k_out != nullptr || pages != nullptr)) return KVR_ERR_INVALID_ARG;
   if (pages == nullptr) v = nullptr;
@@ -510,6 +528,22 @@ int32_t kvr_rotate(const kvr_desc* desc, const kvr_rotation* rot, const void* q,
   a.n_slots = (q ? d.Hq : 0) + (k ? d.Hkv : 0) + (v ? d.Hkv : 0);
   a.paged = pages != nullptr;
   return finish(kvr::launch_rotate(d, desc->dtype, a, rot->style == KVR_ROTATE_PAIRS, (hipStream_t)stream));
+}
+
+int32_t kvr_rotate(const kvr_desc* desc, const kvr_rotation* rot, const void* q, int64_t q_stride, const void* k,
+                   int64_t k_stride, const void* v, int64_t v_stride, int32_t n_rows, const int32_t* q_start,
+                   const int32_t* n_ctx, void* q_out, void* k_out, const kvr_pages* pages, void* stream) {
+  return rotate_rows(desc, rot, nullptr, nullptr, 0, q, q_stride, k, k_stride, v, v_stride, n_rows, q_start, n_ctx, q_out, k_out,
+                     pages, stream);
+}
+
+int32_t kvr_rotate_axes(const kvr_desc* desc, const kvr_rotation* rot, const kvr_axes* axes, const int32_t* pos, int64_t pos_stride,
+                        const void* q, int64_t q_stride, const void* k, int64_t k_stride, const void* v, int64_t v_stride,
+                        int32_t n_rows, const int32_t* q_start, const int32_t* n_ctx, void* q_out, void* k_out,
+                        const kvr_pages* pages, void* stream) {
+  if (axes == nullptr) return KVR_ERR_INVALID_ARG;
+  return rotate_rows(desc, rot, axes, pos, pos_stride, q, q_stride, k, k_stride, v, v_stride, n_rows, q_start, n_ctx, q_out, k_out,
+                     pages, stream);
 }
 
 static int32_t check_visible(int32_t window, int32_t n_sink, kvr::Visible& vis) {

@@ -24,7 +24,12 @@ typedef int32_t (*paged_fn)(const kvr_desc*, const void*, const int32_t*, const 
 typedef int32_t (*prompt_fn)(const kvr_desc*, const void*, int32_t, const int32_t*, const int32_t*, const kvr_pages*, int32_t, int32_t,
                              void*, float*, int64_t, void*, size_t, void*);
 
+typedef int32_t (*rotate_axes_fn)(const kvr_desc*, const kvr_rotation*, const kvr_axes*, const int32_t*, int64_t, const void*, int64_t,
+                                  const void*, int64_t, const void*, int64_t, int32_t, const int32_t*, const int32_t*, void*, void*,
+                                  const kvr_pages*, void*);
+
 static prompt_fn f_prompt;
+static rotate_axes_fn f_rotate_axes;
 static PyObject *n_get_device, *n_shape, *n_stride;
 static rotate_fn f_rotate;
 static paged_fn f_paged;
@@ -187,29 +192,72 @@ static PyObject* setup_cache(PyObject* self, PyObject* const* a, Py_ssize_t n) {
   Py_RETURN_NONE;
 }
 
-/* addresses of desc, rotation and pages (0: none), current device, stream, then binding.kvr_rotate's arguments from q to k_out */
-static PyObject* rotate(PyObject* self, PyObject* const* a, Py_ssize_t n) {
-  int64_t da, ra, pa, dev, st, n_rows, qs, ks, vs;
-  void *q, *k, *v, *start, *nc, *qo, *ko;
-  if (n != 13 || !f_rotate || !integer(a[0], &da) || !integer(a[1], &ra) || !integer(a[2], &pa) || !integer(a[3], &dev) ||
-      !integer(a[4], &st) || !integer(a[8], &n_rows))
+static PyObject* setup_more(PyObject* self, PyObject* const* a, Py_ssize_t n) {
+  int64_t r;
+  if (n != 1 || !integer(a[0], &r)) return PyErr_Format(PyExc_TypeError, "setup_more");
+  f_rotate_axes = (rotate_axes_fn)(uintptr_t)r;
+  Py_RETURN_NONE;
+}
+
+/* device address and stride of positions [n_axes or more, n_rows or more] with dense rows; none where no pair is turned */
+static int positions(PyObject* t, int64_t n_axes, int64_t n_rows, int64_t dev, int none_ok, void** p, int64_t* stride) {
+  int64_t n0, n1, s0, s1, a;
+  *p = NULL;
+  *stride = 0;
+  if (t == Py_None) return none_ok;
+  if (PyObject_IsInstance(t, t_tensor) != 1) return 0;
+  PyObject* dt = PyObject_GetAttr(t, n_dtype);
+  const int same = dt == t_i32;
+  Py_XDECREF(dt);
+  if (!same || !truth(PyObject_GetAttr(t, n_is_cuda)) || !here(t, dev)) return 0;
+  PyObject* shape = PyObject_GetAttr(t, n_shape);
+  int ok = shape && PyTuple_Check(shape) && PyTuple_GET_SIZE(shape) == 2 && integer(PyTuple_GET_ITEM(shape, 0), &n0) &&
+           integer(PyTuple_GET_ITEM(shape, 1), &n1);
+  Py_XDECREF(shape);
+  if (!ok || n0 < n_axes || n1 < n_rows) return 0;
+  PyObject* strides = PyObject_CallMethodNoArgs(t, n_stride);
+  ok = strides && PyTuple_Check(strides) && PyTuple_GET_SIZE(strides) == 2 && integer(PyTuple_GET_ITEM(strides, 0), &s0) &&
+       integer(PyTuple_GET_ITEM(strides, 1), &s1);
+  Py_XDECREF(strides);
+  if (!ok || (s1 != 1 && n1 > 1) || !asked(t, n_data_ptr, &a)) return 0;
+  *p = (void*)(uintptr_t)a;
+  *stride = s0;
+  return 1;
+}
+
+/* addresses of desc, rotation and pages (0: none), current device, stream, then binding.kvr_rotate's arguments from q to k_out; for
+ * kvr_rotate_axes the address of the axes and the positions behind them */
+static PyObject* rotate_any(PyObject* const* a, Py_ssize_t n, int with_axes) {
+  int64_t da, ra, pa, dev, st, n_rows, qs, ks, vs, xa = 0, xs = 0;
+  void *q, *k, *v, *start, *nc, *qo, *ko, *pos = NULL;
+  if (n != (with_axes ? 15 : 13) || !(with_axes ? f_rotate_axes != NULL : f_rotate != NULL) || !integer(a[0], &da) ||
+      !integer(a[1], &ra) || !integer(a[2], &pa) || !integer(a[3], &dev) || !integer(a[4], &st) || !integer(a[8], &n_rows) ||
+      (with_axes && !integer(a[13], &xa)))
     return refuse();
   const kvr_desc* d = (const kvr_desc*)(uintptr_t)da;
+  const kvr_rotation* rot = (const kvr_rotation*)(uintptr_t)ra;
+  const kvr_axes* axes = (const kvr_axes*)(uintptr_t)xa;
   if (!sizes_fit(d, (int64_t[]){n_rows}, 1) || n_rows < 0) return refuse();
   PyObject* dt = d->dtype == KVR_F32 ? t_f32 : t_bf16;
   const int64_t D = d->head_dim, Hq = d->n_q_heads, Hkv = d->n_kv_heads;
   if (!rows(a[5], dt, n_rows, Hq, D, dev, &q, &qs) || !rows(a[6], dt, n_rows, Hkv, D, dev, &k, &ks) ||
       !rows(a[7], dt, n_rows, Hkv, D, dev, &v, &vs) || !tensor(a[9], t_i32, d->batch + 1, 1, &start, 0) ||
-      !tensor(a[10], t_i32, d->batch, 0, &nc, 0) || !tensor(a[11], dt, n_rows * Hq * D, 1, &qo, 0) ||
-      !tensor(a[12], dt, n_rows * Hkv * D, 1, &ko, 0) || !here(a[9], dev) || !here(a[10], dev) || !here(a[11], dev) || !here(a[12], dev))
+      !tensor(a[10], t_i32, d->batch, with_axes && pa == 0, &nc, 0) || !tensor(a[11], dt, n_rows * Hq * D, 1, &qo, 0) ||
+      !tensor(a[12], dt, n_rows * Hkv * D, 1, &ko, 0) || !here(a[9], dev) || !here(a[10], dev) || !here(a[11], dev) || !here(a[12], dev) ||
+      (with_axes && !positions(a[14], axes->n_axes, n_rows, dev, rot->rot_dim == 0, &pos, &xs)))
     return refuse();
   int32_t rc;
   Py_BEGIN_ALLOW_THREADS
-  rc = f_rotate(d, (const kvr_rotation*)(uintptr_t)ra, q, qs, k, ks, v, vs, (int32_t)n_rows, start, nc, qo, ko,
-                (const kvr_pages*)(uintptr_t)pa, (void*)(uintptr_t)st);
+  if (with_axes)
+    rc = f_rotate_axes(d, rot, axes, pos, xs, q, qs, k, ks, v, vs, (int32_t)n_rows, start, nc, qo, ko, (const kvr_pages*)(uintptr_t)pa,
+                       (void*)(uintptr_t)st);
+  else
+    rc = f_rotate(d, rot, q, qs, k, ks, v, vs, (int32_t)n_rows, start, nc, qo, ko, (const kvr_pages*)(uintptr_t)pa, (void*)(uintptr_t)st);
   Py_END_ALLOW_THREADS
   return PyLong_FromLong(rc);
 }
+static PyObject* rotate(PyObject* self, PyObject* const* a, Py_ssize_t n) { return rotate_any(a, n, 0); }
+static PyObject* rotate_axes(PyObject* self, PyObject* const* a, Py_ssize_t n) { return rotate_any(a, n, 1); }
 
 /* addresses of desc and pages, current device, stream, then binding.kvr_attend_paged's arguments without pages */
 static PyObject* attend_paged(PyObject* self, PyObject* const* a, Py_ssize_t n) {
@@ -261,6 +309,8 @@ static PyMethodDef methods[] = {{"setup", (PyCFunction)(void*)setup, METH_FASTCA
                                 {"step_update", (PyCFunction)(void*)step_update, METH_FASTCALL, 0},
                                 {"attend_decode", (PyCFunction)(void*)attend_decode, METH_FASTCALL, 0},
                                 {"setup_cache", (PyCFunction)(void*)setup_cache, METH_FASTCALL, 0},
+                                {"setup_more", (PyCFunction)(void*)setup_more, METH_FASTCALL, 0},
+                                {"rotate_axes", (PyCFunction)(void*)rotate_axes, METH_FASTCALL, 0},
                                 {"rotate", (PyCFunction)(void*)rotate, METH_FASTCALL, 0},
                                 {"attend_paged", (PyCFunction)(void*)attend_paged, METH_FASTCALL, 0},
                                 {"attend_prompt", (PyCFunction)(void*)attend_prompt, METH_FASTCALL, 0},

@@ -248,6 +248,11 @@ struct RotateArgs {
   bool paged;
   DevPages pages;
   int parts;                         // waves of a row (set by the launcher)
+  // positions on several axes (otherwise a token's place in its sequence): of row r on axis x axis_pos[x axis_stride + r]
+  bool axes;
+  const int32_t* axis_pos;
+  long long axis_stride;
+  uint64_t axis[4];                  // axis of pair i: bits 4 (i mod 16) of axis[i / 16]
 };
 hipError_t launch_rotate(const DevDesc& d, int dtype, const RotateArgs& a, bool pairs, hipStream_t st);
 

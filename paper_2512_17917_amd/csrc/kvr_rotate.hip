@@ -7,6 +7,9 @@
 // at the store.  The angle in whole turns, pos inv_freq / 2 pi, is taken in float64 and reduced there to an eighth of a turn
 // about a multiple of a quarter: at position 2^20 a float32 product would be off by a sixteenth of a radian.
 //
+// Positions on several axes (kvr_rotate_axes): the lane that computes pair i's angle asks for its row's position on the pair's
+// axis, four bits of the 64 pairs' list in the kernel's arguments; where the row goes in the cache has nothing to do with them.
+//
 // A wave takes one row.  Its 64 lanes compute the row's at most 64 angles, one each, hand them round through LDS, and each
 // lane keeps the 16 numbers of its channels for all heads of the row; a head is 16 lanes (bf16) or 32 (float32) of 16 bytes.
 // The heads' 16 bytes are asked for four turns at a time.  Sums over a head, and channels half a head away, go through lane
@@ -87,7 +90,7 @@ __device__ __forceinline__ float across_head(float x) {
   else return __shfl_xor(x, 16);
 }
 
-template <typename T, int MODE>
+template <typename T, int MODE, bool AXES>
 __global__ __launch_bounds__(64 * ROT_WAVES) void rotate_kernel(DevDesc d, RotateArgs a) {
   constexpr int VEC = Store<T>::VEC, LANES = D / VEC, HEADS = 64 / LANES;   // lanes a head, heads a wave
   __shared__ float s_cs[ROT_WAVES][2][D / 2];
@@ -96,17 +99,27 @@ __global__ __launch_bounds__(64 * ROT_WAVES) void rotate_kernel(DevDesc d, Rotat
   const long long item = ((long long)blockIdx.y * gridDim.x + blockIdx.x) * ROT_WAVES + wave;
   const int row = uniform((int)(item / a.parts)), part = uniform((int)(item % a.parts));
   if (row >= a.n_rows) return;                 // whole waves; no workgroup barrier below
-  const int b = uniform(seq_of_row(a.q_start, d.B, row));
-  if (b < 0) return;
-  const RowSpan span = row_span(a.q_start, a.n_rows, b);
-  const int pos = clampi(listed(a.n_ctx + b), -(1 << 30), 0x7fffffff) - span.n + (row - span.first);
+  int b = 0, pos = 0;                          // (several axes and no cache: whose row it is matters only for rows of nobody)
+  if (!AXES || a.paged || a.q_start != nullptr) {
+    b = uniform(seq_of_row(a.q_start, d.B, row));
+    if (b < 0) return;
+  }
+  if (!AXES || a.paged) {
+    const RowSpan span = row_span(a.q_start, a.n_rows, b);
+    pos = clampi(listed(a.n_ctx + b), -(1 << 30), 0x7fffffff) - span.n + (row - span.first);
+  }
 
   const int c0 = (lane % LANES) * VEC;
   float cs[VEC], sn[VEC];
   if (a.half > 0) {
     if (lane < a.half) {
       constexpr double PER_TURN = 0.15915494309189533577;       // 1 / (2 pi)
-      double t = (double)pos * (a.inv_freq[lane] * PER_TURN);
+      int turn = pos;                           // the position that the pair is turned by
+      if constexpr (AXES) {
+        const uint64_t four = lane < 32 ? (lane < 16 ? a.axis[0] : a.axis[1]) : (lane < 48 ? a.axis[2] : a.axis[3]);
+        turn = a.axis_pos[(long long)((four >> (4 * (lane & 15))) & 15) * a.axis_stride + row];
+      }
+      double t = (double)turn * (a.inv_freq[lane] * PER_TURN);
       t -= rint(t);
       const double quarter = rint(4.0 * t);
       const float x = (float)(2.0 * (t - 0.25 * quarter));      // half turns, |x| <= 1/4
@@ -216,17 +229,22 @@ __global__ __launch_bounds__(64 * ROT_WAVES) void rotate_kernel(DevDesc d, Rotat
   }
 }
 
-template <typename T>
+template <typename T, bool AXES>
 void launch_mode(const DevDesc& d, const RotateArgs& a, bool pairs, dim3 grid, hipStream_t st) {
   const dim3 block(64 * ROT_WAVES);
   if (pairs || a.half == 0)
-    hipLaunchKernelGGL((rotate_kernel<T, ROT_NEIGHBOURS>), grid, block, 0, st, d, a);
+    hipLaunchKernelGGL((rotate_kernel<T, ROT_NEIGHBOURS, AXES>), grid, block, 0, st, d, a);
   else if (a.half == D / 2)
-    hipLaunchKernelGGL((rotate_kernel<T, ROT_HALF>), grid, block, 0, st, d, a);
+    hipLaunchKernelGGL((rotate_kernel<T, ROT_HALF, AXES>), grid, block, 0, st, d, a);
   else if (a.half % Store<T>::VEC == 0)
-    hipLaunchKernelGGL((rotate_kernel<T, ROT_LANES>), grid, block, 0, st, d, a);
+    hipLaunchKernelGGL((rotate_kernel<T, ROT_LANES, AXES>), grid, block, 0, st, d, a);
   else
-    hipLaunchKernelGGL((rotate_kernel<T, ROT_ANY>), grid, block, 0, st, d, a);
+    hipLaunchKernelGGL((rotate_kernel<T, ROT_ANY, AXES>), grid, block, 0, st, d, a);
+}
+template <typename T>
+void launch_type(const DevDesc& d, const RotateArgs& a, bool pairs, dim3 grid, hipStream_t st) {
+  if (a.axes) launch_mode<T, true>(d, a, pairs, grid, st);
+  else launch_mode<T, false>(d, a, pairs, grid, st);
 }
 
 }  // namespace
@@ -240,8 +258,8 @@ hipError_t launch_rotate(const DevDesc& d, int dtype, const RotateArgs& args, bo
   a.parts = (int)(want < iters ? want : iters);
   const GridRows rows = grid_rows(((long long)a.n_rows * a.parts + ROT_WAVES - 1) / ROT_WAVES);
   const dim3 grid(rows.x, rows.rows);
-  if (dtype == KVR_F32) launch_mode<float>(d, a, pairs, grid, st);
-  else launch_mode<bf16_t>(d, a, pairs, grid, st);
+  if (dtype == KVR_F32) launch_type<float>(d, a, pairs, grid, st);
+  else launch_type<bf16_t>(d, a, pairs, grid, st);
   return hipGetLastError();
 }
 
