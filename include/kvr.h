@@ -31,6 +31,8 @@
  *     token (Overview, Calculation Phase)    -> kvr_attend_prompt
  *   - attention of one new token over a paged cache
  *                                            -> kvr_attend_paged
+ *   - both where sequences of the batch begin with the same tokens, which are read once
+ *                                            -> kvr_attend_shared
  *
  * Vocabulary.  A *unit* is one (sequence b, kv head h) of one attention layer;
  * unit index u = b * n_kv_heads + h.  One call works on all units of one layer.
@@ -207,6 +209,21 @@ typedef struct kvr_axes {
   int32_t n_axes;
   uint8_t axis[KVR_HEAD_DIM / 2];
 } kvr_axes;
+
+/*
+ * Sequences that begin with the same tokens (host memory, plain data): group g is the sequences start[g] .. start[g+1]-1,
+ * whose first n_shared[g] tokens are the same, keys and values alike.
+ *   start      dev int32 [n_groups + 1], not falling; entries are clamped to [0, B]
+ *   n_shared   dev int32 [n_groups], clamped to what a sequence can hold
+ *   n_groups   0 .. B.  Sequences of no group, and of a group of one, share nothing
+ * The tokens may lie on pages that the sequences' table rows name together (a last page that they fill in part is then a
+ * copy of each its own), or be copies throughout; one sequence's are read for all.
+ */
+typedef struct kvr_groups {
+  const int32_t* start;
+  const int32_t* n_shared;
+  int32_t n_groups;
+} kvr_groups;
 
 /* Library version string (static storage). */
 const char* kvr_version(void);
@@ -578,6 +595,26 @@ int32_t kvr_attend_paged_workspace_size(const kvr_desc* desc, const kvr_pages* p
 int32_t kvr_attend_paged(const kvr_desc* desc, const void* q, const int32_t* n_ctx, const kvr_pages* pages,
                          int32_t window, int32_t n_sink, void* out, float* scores, int64_t n_cap, void* ws,
                          size_t ws_bytes, void* stream);
+
+/*
+ * kvr_attend_prompt (with q_start) and kvr_attend_paged (without: row b is the newest token of sequence b) for sequences
+ * that begin with the same tokens: out and scores are theirs, but what a group shares is read once for all its rows, and
+ * what each sequence has behind it beside that.  A sequence with a new row among the shared tokens is attended by itself,
+ * as one of no group is.  bf16: p is rounded to bf16 for its product with v, as in kvr_attend_prompt.
+ * Made for few new tokens a sequence; for long ones with q_start kvr_attend_prompt does as well.
+ *   groups     host, or NULL: nothing is shared
+ *   n_rows     n_rows * Hq is at most 2^28 here
+ *   ws         per kvr_attend_shared_workspace_size, with scores = whether there are scores (of `groups` the sizes are looked at)
+ *   the others as for kvr_attend_prompt.  KVR_ERR_UNSUPPORTED also where 2 (n_rows G / 16 + B + 1) Hkv times a 64th of the
+ *              tokens that a sequence can hold passes 2^31
+ */
+int32_t kvr_attend_shared_workspace_size(const kvr_desc* desc, int32_t n_rows, const kvr_pages* pages,
+                                         const kvr_groups* groups, int32_t window, int32_t n_sink, int32_t scores,
+                                         size_t* bytes);
+int32_t kvr_attend_shared(const kvr_desc* desc, const void* q, int32_t n_rows, const int32_t* q_start,
+                          const int32_t* n_ctx, const kvr_pages* pages, const kvr_groups* groups, int32_t window,
+                          int32_t n_sink, void* out, float* scores, int64_t n_cap, void* ws, size_t ws_bytes,
+                          void* stream);
 
 #ifdef __cplusplus
 }

@@ -44,7 +44,7 @@ EXPORTS = ["kvr_version", "kvr_last_hip_error", "kvr_recent_size", "kvr_hash_par
            "kvr_swap_back", "kvr_reconstruct", "kvr_attend_decode", "kvr_attend_decode_static",
            "kvr_attend_multi_workspace_size", "kvr_attend_multi"]
 EXPORTS += ["kvr_rotate", "kvr_attend_prompt_workspace_size", "kvr_attend_prompt", "kvr_attend_paged_workspace_size",
-            "kvr_attend_paged", "kvr_rotate_axes"]
+            "kvr_attend_paged", "kvr_rotate_axes", "kvr_attend_shared_workspace_size", "kvr_attend_shared"]
 KVR_MAX_AXES = 8
 KVR_ROTATE_HALVES, KVR_ROTATE_PAIRS = 0, 1
 KVR_STATIC_SCRATCH_BYTES = 80 << 20
@@ -81,6 +81,10 @@ class kvr_rotation(C.Structure):
 
 class kvr_axes(C.Structure):
     _fields_ = [("n_axes", C.c_int32), ("axis", C.c_uint8 * (KVR_HEAD_DIM // 2))]
+
+
+class kvr_groups(C.Structure):
+    _fields_ = [("start", C.c_void_p), ("n_shared", C.c_void_p), ("n_groups", C.c_int32)]
 
 
 _fast = None
@@ -204,6 +208,11 @@ def lib() -> C.CDLL:
         L.kvr_attend_paged_workspace_size.argtypes = [dp, pp, i32, i32, i32, C.POINTER(sz)]
         L.kvr_attend_paged.restype = i32
         L.kvr_attend_paged.argtypes = [dp, vp, vp, pp, i32, i32, vp, vp, i64, vp, sz, vp]
+        gp = C.POINTER(kvr_groups)
+        L.kvr_attend_shared_workspace_size.restype = i32
+        L.kvr_attend_shared_workspace_size.argtypes = [dp, i32, pp, gp, i32, i32, i32, C.POINTER(sz)]
+        L.kvr_attend_shared.restype = i32
+        L.kvr_attend_shared.argtypes = [dp, vp, i32, vp, vp, pp, gp, i32, i32, vp, vp, i64, vp, sz, vp]
         _load_fast(L)
         _lib = L
     return _lib
@@ -221,7 +230,7 @@ def _load_fast(L):
         m.setup(address(L.kvr_step_update), address(L.kvr_attend_decode), torch.float32, torch.bfloat16, torch.int32,
                 torch.uint8, torch.Tensor)
         m.setup_cache(address(L.kvr_rotate), address(L.kvr_attend_paged), address(L.kvr_attend_prompt))
-        m.setup_more(address(L.kvr_rotate_axes))
+        m.setup_more(address(L.kvr_rotate_axes), address(L.kvr_attend_shared))
         _fast = m
 
 
@@ -733,3 +742,51 @@ def kvr_attend_paged(desc, q, n_ctx, pages, window, n_sink, out, scores, n_cap, 
         window, n_sink, _ptr(out, dt, row, "out"), _ptr(scores, torch.float32, U * n_cap, "scores", True), n_cap,
         wp, wb, _stream())
     _check("kvr_attend_paged", rc)
+
+
+def make_groups(start, n_shared):
+    """kvr_groups: sequences start[g] .. start[g + 1] - 1 have their first n_shared[g] tokens in common (int32 device tensors
+    [n_groups + 1] and [n_groups]).  The struct keeps the tensors, whose contents may change from call to call."""
+    n = n_shared.numel() if isinstance(n_shared, torch.Tensor) else 0
+    g = kvr_groups(_ptr(start, torch.int32, n + 1, "start"), _ptr(n_shared, torch.int32, 0, "n_shared"), n)
+    g.tensors = (start, n_shared)
+    g.dev = _one_device(start, n_shared)
+    return g
+
+
+def _groups(groups):
+    if groups is None:
+        return None
+    if not isinstance(groups, kvr_groups) or not hasattr(groups, "tensors"):
+        raise TypeError("groups must come from make_groups")
+    if groups.dev != torch.cuda.current_device():
+        raise ValueError(f"the groups live on cuda:{groups.dev}, the current device is cuda:{torch.cuda.current_device()}")
+    return C.byref(groups)
+
+
+def kvr_attend_shared_workspace_size(desc, n_rows, pages, groups, window, n_sink, scores) -> int:
+    n = C.c_size_t(0)
+    _check("kvr_attend_shared_workspace_size", lib().kvr_attend_shared_workspace_size(
+        C.byref(desc), n_rows, _pages(desc, pages), _groups(groups), window, n_sink, int(bool(scores)), C.byref(n)))
+    return n.value
+
+
+def kvr_attend_shared(desc, q, n_rows, q_start, n_ctx, pages, groups, window, n_sink, out, scores, n_cap, ws):
+    pp, gp = _pages(desc, pages), _groups(groups)
+    lib()
+    if _fast is not None and isinstance(desc, kvr_desc) and isinstance(q, torch.Tensor) and q.is_cuda:
+        dev = pages.dev                              # the current one, as _pages has found
+        rc = _fast.attend_shared(C.addressof(desc), C.addressof(pages), dev, _stream_of(dev), q, n_rows, q_start, n_ctx, window,
+                                 n_sink, out, scores, n_cap, ws, C.addressof(groups) if groups is not None else 0)
+        if rc is not None:
+            return _check("kvr_attend_shared", rc)
+    U, dt = desc.batch * desc.n_kv_heads, _torch_dtype(desc)
+    row = desc.n_q_heads * desc.head_dim
+    wp, wb = _ws(ws)
+    _here(q, q_start, n_ctx, out, scores, ws)
+    rc = lib().kvr_attend_shared(
+        C.byref(desc), _ptr(q, dt, n_rows * row, "q"), n_rows,
+        _ptr(q_start, torch.int32, desc.batch + 1, "q_start", True), _ptr(n_ctx, torch.int32, desc.batch, "n_ctx"),
+        pp, gp, window, n_sink, _ptr(out, dt, n_rows * row, "out"),
+        _ptr(scores, torch.float32, U * n_cap, "scores", True), n_cap, wp, wb, _stream())
+    _check("kvr_attend_shared", rc)

@@ -645,4 +645,56 @@ int32_t kvr_attend_paged(const kvr_desc* desc, const void* q, const int32_t* n_c
   return finish(kvr::launch_attend_paged(d, desc->dtype, a, (hipStream_t)stream));
 }
 
+static int32_t groups_size(const kvr_desc* desc, const kvr_groups* groups) {
+  return groups != nullptr && (groups->n_groups < 0 || groups->n_groups > desc->batch) ? KVR_ERR_INVALID_ARG : KVR_OK;
+}
+
+constexpr long long MAX_HEADS_SHARED = 1ll << 28;
+
+int32_t kvr_attend_shared_workspace_size(const kvr_desc* desc, int32_t n_rows, const kvr_pages* pages, const kvr_groups* groups,
+                                         int32_t window, int32_t n_sink, int32_t scores, size_t* bytes) {
+  kvr::DevDesc d;
+  kvr::DevPages p;
+  kvr::Visible vis;
+  int32_t rc = check_desc(desc, d);
+  if (rc == KVR_OK) rc = pages_size(desc, pages, p);
+  if (rc == KVR_OK) rc = groups_size(desc, groups);
+  if (rc == KVR_OK) rc = check_visible(window, n_sink, vis);
+  if (rc != KVR_OK) return rc;
+  if (bytes == nullptr || n_rows < 0 || n_rows > MAX_ROWS_NEW || (long long)n_rows * d.Hq > MAX_HEADS_SHARED) return KVR_ERR_INVALID_ARG;
+  if (!kvr::attend_shared_fits(d, n_rows, p.cap)) return KVR_ERR_UNSUPPORTED;
+  *bytes = n_rows == 0 ? 0 : kvr::attend_shared_ws(d, desc->dtype, n_rows, p.cap, scores != 0);
+  return KVR_OK;
+}
+
+int32_t kvr_attend_shared(const kvr_desc* desc, const void* q, int32_t n_rows, const int32_t* q_start, const int32_t* n_ctx,
+                          const kvr_pages* pages, const kvr_groups* groups, int32_t window, int32_t n_sink, void* out, float* scores,
+                          int64_t n_cap, void* ws, size_t ws_bytes, void* stream) {
+  kvr::DevDesc d;
+  kvr::SharedArgs s;
+  memset(&s, 0, sizeof(s));
+  int32_t rc = check_desc(desc, d);
+  if (rc == KVR_OK) rc = check_visible(window, n_sink, s.a.vis);
+  if (rc == KVR_OK) rc = check_rows(desc, n_rows, q_start, MAX_HEADS_SHARED);
+  if (rc == KVR_OK) rc = groups_size(desc, groups);
+  if (rc != KVR_OK) return rc;
+  if (n_rows == 0) return KVR_OK;
+  rc = check_attend(desc, q, n_ctx, pages, out, scores, n_cap, s.a);
+  if (rc != KVR_OK) return rc;
+  if (groups != nullptr && groups->n_groups > 0) {
+    if (!groups->start || !groups->n_shared || ((reinterpret_cast<uintptr_t>(groups->start) | reinterpret_cast<uintptr_t>(groups->n_shared)) & 3u) != 0)
+      return KVR_ERR_INVALID_ARG;
+    s.start = groups->start;
+    s.n_shared = groups->n_shared;
+    s.n_groups = groups->n_groups;
+  }
+  if (!kvr::attend_shared_fits(d, n_rows, s.a.pages.cap)) return KVR_ERR_UNSUPPORTED;
+  rc = check_ws(ws, ws_bytes, kvr::attend_shared_ws(d, desc->dtype, n_rows, s.a.pages.cap, scores != nullptr));
+  if (rc != KVR_OK) return rc;
+  s.a.n_rows = n_rows;
+  s.a.q_start = q_start;
+  s.a.ws = ws;
+  return finish(kvr::launch_attend_shared(d, desc->dtype, s, (hipStream_t)stream));
+}
+
 }  // extern "C"

@@ -270,6 +270,13 @@ size_t attend_prompt_ws(const DevDesc& d, int dtype, long long n_rows, long long
   return scores ? (size_t)n_rows * d.Hq * sizeof(float) : 0;
 }
 
+hipError_t launch_prompt_scores_f32(const DevDesc& d, const PagedArgs& a, const float* lse, hipStream_t st) {
+  const long long most = a.n_cap < a.pages.cap ? a.n_cap : a.pages.cap;
+  const GridRows tiles = grid_rows((most + 15) / 16);
+  hipLaunchKernelGGL(prompt_scores_f32_kernel, dim3(tiles.x, d.B * d.Hkv, tiles.rows), dim3(64 * PP_WAVES), 0, st, d, a, lse);
+  return hipGetLastError();
+}
+
 hipError_t launch_attend_prompt(const DevDesc& d, int dtype, const PagedArgs& a, hipStream_t st) {
   if (dtype == KVR_BF16) {
     const PromptPlan p = prompt_bf16_plan(d, a.n_rows, a.pages.cap, a.vis, a.scores ? a.n_cap : 0);
@@ -282,11 +289,7 @@ hipError_t launch_attend_prompt(const DevDesc& d, int dtype, const PagedArgs& a,
   const GridRows cols = grid_rows(col_tiles_most(a.n_rows, d.B, d.G, 16));
   hipLaunchKernelGGL(prompt_f32_kernel, dim3(cols.x, d.Hkv, cols.rows), dim3(64 * PP_WAVES), 0, st, d, a, lse);
   const hipError_t e = hipGetLastError();
-  if (e != hipSuccess || a.scores == nullptr) return e;
-  const long long most = a.n_cap < a.pages.cap ? a.n_cap : a.pages.cap;
-  const GridRows tiles = grid_rows((most + 15) / 16);
-  hipLaunchKernelGGL(prompt_scores_f32_kernel, dim3(tiles.x, d.B * d.Hkv, tiles.rows), dim3(64 * PP_WAVES), 0, st, d, a, lse);
-  return hipGetLastError();
+  return e != hipSuccess || a.scores == nullptr ? e : launch_prompt_scores_f32(d, a, lse, st);
 }
 
 }  // namespace kvr

@@ -28,7 +28,11 @@ typedef int32_t (*rotate_axes_fn)(const kvr_desc*, const kvr_rotation*, const kv
                                   const void*, int64_t, const void*, int64_t, int32_t, const int32_t*, const int32_t*, void*, void*,
                                   const kvr_pages*, void*);
 
+typedef int32_t (*shared_fn)(const kvr_desc*, const void*, int32_t, const int32_t*, const int32_t*, const kvr_pages*, const kvr_groups*,
+                             int32_t, int32_t, void*, float*, int64_t, void*, size_t, void*);
+
 static prompt_fn f_prompt;
+static shared_fn f_shared;
 static rotate_axes_fn f_rotate_axes;
 static PyObject *n_get_device, *n_shape, *n_stride;
 static rotate_fn f_rotate;
@@ -193,9 +197,10 @@ static PyObject* setup_cache(PyObject* self, PyObject* const* a, Py_ssize_t n) {
 }
 
 static PyObject* setup_more(PyObject* self, PyObject* const* a, Py_ssize_t n) {
-  int64_t r;
-  if (n != 1 || !integer(a[0], &r)) return PyErr_Format(PyExc_TypeError, "setup_more");
+  int64_t r, t;
+  if (n != 2 || !integer(a[0], &r) || !integer(a[1], &t)) return PyErr_Format(PyExc_TypeError, "setup_more");
   f_rotate_axes = (rotate_axes_fn)(uintptr_t)r;
+  f_shared = (shared_fn)(uintptr_t)t;
   Py_RETURN_NONE;
 }
 
@@ -282,12 +287,14 @@ static PyObject* attend_paged(PyObject* self, PyObject* const* a, Py_ssize_t n) 
   return PyLong_FromLong(rc);
 }
 
-/* addresses of desc and pages, current device, stream, then binding.kvr_attend_prompt's arguments without pages */
-static PyObject* attend_prompt(PyObject* self, PyObject* const* a, Py_ssize_t n) {
-  int64_t da, pa, dev, st, n_rows, window, n_sink, n_cap, wb = 0;
+/* addresses of desc and pages, current device, stream, then binding.kvr_attend_prompt's arguments without pages; for kvr_attend_shared
+ * the address of the groups (0: none) behind them */
+static PyObject* attend_rows(PyObject* const* a, Py_ssize_t n, int shared) {
+  int64_t da, pa, dev, st, n_rows, window, n_sink, n_cap, ga = 0, wb = 0;
   void *q, *start, *nc, *out, *sc, *ws;
-  if (n != 14 || !f_prompt || !integer(a[0], &da) || !integer(a[1], &pa) || !integer(a[2], &dev) || !integer(a[3], &st) ||
-      !integer(a[5], &n_rows) || !integer(a[8], &window) || !integer(a[9], &n_sink) || !integer(a[12], &n_cap))
+  if (n != (shared ? 15 : 14) || !(shared ? f_shared != NULL : f_prompt != NULL) || !integer(a[0], &da) || !integer(a[1], &pa) ||
+      !integer(a[2], &dev) || !integer(a[3], &st) || !integer(a[5], &n_rows) || !integer(a[8], &window) || !integer(a[9], &n_sink) ||
+      !integer(a[12], &n_cap) || (shared && !integer(a[14], &ga)))
     return refuse();
   const kvr_desc* d = (const kvr_desc*)(uintptr_t)da;
   if (!sizes_fit(d, (int64_t[]){n_rows, window, n_sink, n_cap}, 4) || n_rows < 0) return refuse();
@@ -299,11 +306,17 @@ static PyObject* attend_prompt(PyObject* self, PyObject* const* a, Py_ssize_t n)
     return refuse();
   int32_t rc;
   Py_BEGIN_ALLOW_THREADS
-  rc = f_prompt(d, q, (int32_t)n_rows, start, nc, (const kvr_pages*)(uintptr_t)pa, (int32_t)window, (int32_t)n_sink, out, sc, n_cap, ws,
-                (size_t)wb, (void*)(uintptr_t)st);
+  if (shared)
+    rc = f_shared(d, q, (int32_t)n_rows, start, nc, (const kvr_pages*)(uintptr_t)pa, (const kvr_groups*)(uintptr_t)ga, (int32_t)window,
+                  (int32_t)n_sink, out, sc, n_cap, ws, (size_t)wb, (void*)(uintptr_t)st);
+  else
+    rc = f_prompt(d, q, (int32_t)n_rows, start, nc, (const kvr_pages*)(uintptr_t)pa, (int32_t)window, (int32_t)n_sink, out, sc, n_cap, ws,
+                  (size_t)wb, (void*)(uintptr_t)st);
   Py_END_ALLOW_THREADS
   return PyLong_FromLong(rc);
 }
+static PyObject* attend_prompt(PyObject* self, PyObject* const* a, Py_ssize_t n) { return attend_rows(a, n, 0); }
+static PyObject* attend_shared(PyObject* self, PyObject* const* a, Py_ssize_t n) { return attend_rows(a, n, 1); }
 
 static PyMethodDef methods[] = {{"setup", (PyCFunction)(void*)setup, METH_FASTCALL, 0},
                                 {"step_update", (PyCFunction)(void*)step_update, METH_FASTCALL, 0},
@@ -313,6 +326,7 @@ static PyMethodDef methods[] = {{"setup", (PyCFunction)(void*)setup, METH_FASTCA
                                 {"rotate_axes", (PyCFunction)(void*)rotate_axes, METH_FASTCALL, 0},
                                 {"rotate", (PyCFunction)(void*)rotate, METH_FASTCALL, 0},
                                 {"attend_paged", (PyCFunction)(void*)attend_paged, METH_FASTCALL, 0},
+                                {"attend_shared", (PyCFunction)(void*)attend_shared, METH_FASTCALL, 0},
                                 {"attend_prompt", (PyCFunction)(void*)attend_prompt, METH_FASTCALL, 0},
                                 {0, 0, 0, 0}};
 static struct PyModuleDef module = {PyModuleDef_HEAD_INIT, "_kvr_fast", 0, -1, methods, 0, 0, 0, 0};

@@ -304,6 +304,20 @@ PromptPlan prompt_bf16_plan(const DevDesc& d, long long n_rows, long long cap, c
 hipError_t launch_prompt_bf16(const DevDesc& d, const PagedArgs& a, const PromptPlan& p, hipStream_t st);
 size_t attend_prompt_ws(const DevDesc& d, int dtype, long long n_rows, long long cap, const Visible& vis, bool scores);
 hipError_t launch_attend_prompt(const DevDesc& d, int dtype, const PagedArgs& a, hipStream_t st);
+hipError_t launch_prompt_scores_f32(const DevDesc& d, const PagedArgs& a, const float* lse, hipStream_t st);
+
+// Attention where groups of sequences begin with the same tokens (kvr_attend_shared)
+struct SharedArgs {
+  PagedArgs a;
+  const int32_t* start;             // of the groups, [n_groups + 1]
+  const int32_t* n_shared;
+  int n_groups;
+  int least;                        // fewer tokens in common than this are not worth a pass of their own
+};
+// false: more tiles of columns and tokens than the kernels count
+bool attend_shared_fits(const DevDesc& d, long long n_rows, long long cap);
+size_t attend_shared_ws(const DevDesc& d, int dtype, long long n_rows, long long cap, bool scores);
+hipError_t launch_attend_shared(const DevDesc& d, int dtype, const SharedArgs& s, hipStream_t st);
 bool attend_paged_fits(const DevDesc& d, long long cap, const Visible& vis);
 size_t attend_paged_ws(const DevDesc& d, int dtype, long long cap, const Visible& vis, bool scores);
 hipError_t launch_attend_paged(const DevDesc& d, int dtype, const PagedArgs& a, hipStream_t st);

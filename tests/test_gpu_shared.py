@@ -1,0 +1,249 @@
+"""kvr_attend_shared against float64 (tests/cache_ref.py), which knows nothing of groups: the sequences' own table rows."""
+import math
+
+import pytest
+import torch
+
+from paper_2512_17917_amd import binding as kvr
+from tests import cache_ref as R
+
+pytestmark = [pytest.mark.gpu, pytest.mark.timeout(300)]
+D = 128
+BF, F32 = torch.bfloat16, torch.float32
+
+
+class Batch:
+    """Groups as lists of (tokens, new rows) with the tokens that they have in common: [(common, [(n, y), ...]), ...]; their
+    pools, table, lengths and queries on the CPU."""
+
+    def __init__(self, groups, heads, page, dtype, seed, *, lead=0, trail=0, alone=(), rows=True, room=0):
+        """alone: sequences of no group, behind the groups; rows: by q_start (else one row a sequence); room: tokens that a
+        sequence can hold past its longest."""
+        g = self.g = torch.Generator().manual_seed(seed)
+        self.dtype, (self.Hq, self.Hkv), self.page = dtype, heads, page
+        seqs = [s for _, m in groups for s in m] + list(alone)
+        self.n, new = [n for n, _ in seqs], [y for _, y in seqs]
+        self.B, self.start, self.common = len(seqs), [0], [c for c, _ in groups]
+        for _, m in groups:
+            self.start.append(self.start[-1] + len(m))
+        self.q_start = None
+        self.rows = self.B
+        if rows:
+            self.q_start = [lead]
+            for y in new:
+                self.q_start.append(self.q_start[-1] + y)
+            self.rows = self.q_start[-1] + trail
+        each = -(-(max(self.n) + room) // page) or 1
+        table = torch.full((self.B, each), -1, dtype=torch.int32)
+        used, copies = 0, []
+        of = [i for i, (_, m) in enumerate(groups) for _ in m] + [None] * len(alone)
+        whole = {}                                               # a group's pages that are filled by what it has in common
+        for b in range(self.B):
+            have = -(-self.n[b] // page)
+            c = self.common[of[b]] if of[b] is not None else 0
+            for i in range(have):
+                if of[b] is not None and (i + 1) * page <= c and (of[b], i) in whole:
+                    table[b, i] = whole[of[b], i]
+                    continue
+                table[b, i] = used
+                if of[b] is not None and i * page < c:
+                    if (of[b], i) in whole:                      # the page that the common tokens end in: a copy
+                        copies.append((used, whole[of[b], i], c - i * page))
+                    else:
+                        whole[of[b], i] = used
+                used += 1
+        order = torch.randperm(used + 2, generator=g)
+        self.table = torch.where(table >= 0, order.to(torch.int32)[table.clamp(min=0).long()], table)
+        self.k, self.v = (torch.randn(used + 2, self.Hkv, page, D, generator=g).to(dtype) for _ in range(2))
+        for to, src, m in copies:
+            for pool in (self.k, self.v):
+                pool[order[to], :, :m] = pool[order[src], :, :m]
+        self.q = torch.randn(self.rows, self.Hq, D, generator=g).to(dtype)
+        self.cap = each * page
+        self.n_cap = self.cap
+
+    def check(self, window=0, sink=0, scores=True, scale=None, start=None, common=None, groups=True, nan=(), finite_k=None):
+        """nan: (sequence, kv head, query heads) whose logits have a NaN that the reference leaves out.  finite_k: keys by which
+        a logit's rounding error is bounded where some are infinite (a logit of -Inf has none)."""
+        d = kvr.make_desc(self.B, self.Hq, self.Hkv, 1, 1, self.dtype, softmax_scale=scale)
+        i32 = lambda x: torch.tensor(x, dtype=torch.int32).cuda()
+        pages = kvr.make_pages(d, self.k.cuda(), self.v.cuda(), self.table.cuda())
+        grp = kvr.make_groups(i32(self.start if start is None else start), i32(self.common if common is None else common)) if groups else None
+        old = torch.rand(self.B, self.Hkv, self.n_cap, generator=self.g) if scores else None
+        sc = old.cuda() if scores else None
+        out = torch.full((self.rows, self.Hq, D), 7.0, dtype=self.dtype).cuda()
+        n = kvr.kvr_attend_shared_workspace_size(d, self.rows, pages, grp, window, sink, scores)
+        ws = torch.randint(0, 256, (max(n, 256),), dtype=torch.uint8).cuda()
+        qs = None if self.q_start is None else i32(self.q_start)
+        kvr.kvr_attend_shared(d, self.q.cuda(), self.rows, qs, i32(self.n), pages, grp, window, sink, out, sc, self.n_cap if scores else 0, ws)
+        torch.cuda.synchronize()
+        ref = R.attend(self.q, self.k, self.v, self.table, self.n, self.q_start, d.softmax_scale, window, sink, self.n_cap, self.Hkv)
+        if finite_k is not None:
+            ref["e"] = R.attend(self.q, finite_k, self.v, self.table, self.n, self.q_start, d.softmax_scale, window, sink, self.n_cap, self.Hkv)["e"]
+        for b, h, heads in nan:
+            ref["out"][b, heads] = math.nan
+            ref["scores"][b, h, :self.n[b]] = math.nan
+        tol, tol_s = R.attend_bounds(ref, self.dtype, old)
+        out = out.cpu()
+        mine = ref["rows"]
+        nan = ref["out"].isnan()
+        assert torch.equal(out.isnan() & mine[:, None, None], nan & mine[:, None, None])
+        err = (out.double() - ref["out"]).abs()
+        fin = torch.isfinite(ref["out"]) & mine[:, None, None]
+        assert bool((err <= tol)[fin].all()), float((err - tol)[fin].max())
+        inf = torch.isinf(ref["out"]) & mine[:, None, None]
+        assert torch.equal(out[inf].double(), ref["out"][inf])
+        assert bool((out[~mine] == 7.0).all())
+        if scores:
+            grown = sc.cpu().double() - old.double()
+            ok = (grown - ref["scores"]).abs() <= tol_s
+            assert bool((ok | ref["scores"].isnan()).all()), float(((grown - ref["scores"]).abs() - tol_s).nan_to_num().max())
+            assert torch.equal(grown.isnan(), ref["scores"].isnan())
+        return out, sc
+
+
+def one(*n):
+    return [(x, 1) for x in n]
+
+
+CASES = [  # groups, heads, page, lead, trail, alone, by q_start
+    ([(1000, one(1001, 1040, 1500, 1000))], (32, 8), 16, 0, 0, (), False),           # the last has no token of its own
+    ([(300, one(301, 420)), (0, one(70, 1)), (64, one(65, 64, 200))], (8, 2), 64, 0, 0, one(90, 0), False),
+    ([(129, one(130, 0, 50, 700, 129))], (8, 8), 24, 0, 0, (), False),               # an empty row, and one that is shorter than what is shared
+    ([(500, one(501)), (77, one(78, 79, 0))], (16, 2), 7, 0, 0, (), False),          # a group of one; pages of an odd size
+    ([(200, [(210, 5), (200, 1), (333, 30), (201, 0)])], (32, 8), 32, 3, 2, [(40, 40)], True),
+    ([(640, [(700, 60)] * 9)], (16, 2), 64, 0, 0, (), True),                         # 480 rows of 8 heads: several tiles of columns
+    ([(250, [(260, 20), (251, 1), (900, 300)])], (4, 4), 1, 0, 5, (), True),          # the first has new rows among what is shared
+    ([(2048, one(*range(2049, 2100)))], (64, 8), 128, 0, 0, (), False),               # 408 columns
+    ([(3000, one(*[3000 + 7 * i for i in range(1, 40)])), (100, one(101, 102))], (8, 1), 48, 0, 0, one(1, 2, 3), False),
+]
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("window,sink", [(0, 0), (100, 0), (33, 4), (600, 130), (1, 0), (1, 3)])
+@pytest.mark.parametrize("case", range(len(CASES)))
+def test_against_each_sequence_by_itself(case, window, sink, dtype):
+    groups, heads, page, lead, trail, alone, rows = CASES[case]
+    b = Batch(groups, heads, page, dtype, 40 + case, lead=lead, trail=trail, alone=alone, rows=rows)
+    b.check(window, sink)
+    b.check(window, sink, scores=False)
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+def test_no_groups_and_groups_that_share_nothing(dtype):
+    b = Batch([(0, one(200, 31, 0, 900))], (8, 2), 16, dtype, 3, rows=False)
+    none, sc0 = b.check(groups=False)
+    for start, common in (([0, 4], [0]), ([0, 1, 2, 3, 4], [500, 31, 7, 2]), ([2, 2, 2], [9, 9]), ([4, 9], [8])):
+        b.g.manual_seed(3)
+        b.check(start=start, common=common)
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+def test_starts_that_go_past_the_batch_and_more_in_common_than_there_is_room_for(dtype):
+    b = Batch([(96, one(100, 120, 97))], (8, 2), 32, dtype, 8, rows=False)
+    b.check(start=[-5, 77], common=[96])
+    b.check(start=[0, 3], common=[1 << 30])           # (more than each has: each by itself)
+    b.check(start=[0, 3], common=[-4])
+    b.check(start=[0, 1, 3], common=[96, 90])
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("page", [8, 64, 5])
+def test_pages_that_are_not_there(dtype, page):
+    """Among what is shared (for all alike) and among a sequence's own."""
+    b = Batch([(320, one(400, 321, 500))], (8, 2), page, dtype, 12, rows=False)
+    b.table[:, 1] = -1
+    b.table[:, 192 // page] = 1 << 20
+    b.table[0, 384 // page] = -7
+    b.table[2, 448 // page:] = -1
+    b.check()
+    b.check(150, 20)
+    b.table[:, :320 // page] = -1                     # nothing of it
+    b.check()
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("window,sink", [(0, 0), (120, 3)])
+@pytest.mark.parametrize("what", [math.inf, -math.inf, math.nan])
+def test_values_that_are_not_finite(dtype, window, sink, what):
+    """Where no query sees them they do nothing; where one does they are its, not its neighbours'."""
+    b = Batch([(200, [(230, 9), (203, 3), (420, 1)])], (8, 2), 16, dtype, 15)
+    rows = [R.token_row(b.k, b.table, i, j) for i, j in ((0, 229), (0, 225), (2, 419), (2, 390))]
+    shared = R.token_row(b.k, b.table, 0, 150)
+    for page, row in rows + [shared]:
+        b.v[page, 1, row, 5] = what
+        b.v[page, 0, row, 127] = what
+    # and tokens of nobody: behind the sequences' ends, and of pages that nobody names
+    for i, n in enumerate(b.n):
+        page, row = R.token_row(b.k, b.table, i, n - 1)
+        b.k[page, :, row + 1:] = what
+        b.v[page, :, row + 1:] = what
+    named = set(b.table.flatten().tolist())
+    for page in set(range(b.k.shape[0])) - named:
+        b.k[page] = b.v[page] = what
+    b.check(window, sink)
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("where", ["shared", "own"])
+def test_logits_that_are_not_finite(dtype, where):
+    """NaN among the logits of one sequence's query, -Inf among all of another's."""
+    b = Batch([(130, one(190, 131, 250))], (4, 2), 16, dtype, 16, rows=False)
+    page, row = R.token_row(b.k, b.table, 0, 100 if where == "shared" else 180)
+    if where == "shared":
+        b.q[0, 1, 3] = math.nan
+        b.check(nan=[(0, 0, [1])])
+    else:
+        b.k[page, 1, row, 0] = math.nan
+        b.check(nan=[(0, 1, [2, 3])])
+    b2 = Batch([(130, one(190, 131, 250))], (4, 2), 16, dtype, 17, rows=False)
+    page, row = R.token_row(b2.k, b2.table, 0, 100 if where == "shared" else 180)
+    b2.k[page, 1, row] = 0
+    k0 = b2.k.clone()
+    b2.k[page, 1, row, 0] = -math.inf
+    b2.q[:, :, 0] = b2.q[:, :, 0].abs() + 1
+    b2.check(finite_k=k0)
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("scale", [0.0, -0.2, 3.0])
+def test_scales(dtype, scale):
+    Batch([(150, one(190, 151, 250)), (33, one(40, 41))], (8, 2), 16, dtype, 18, rows=False).check(scale=scale)
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+def test_a_first_token_that_draws_most_weight_and_logits_far_apart(dtype):
+    """The maximum in what is shared for some heads, in a sequence's own for others."""
+    b = Batch([(700, one(900, 701, 780))], (8, 2), 16, dtype, 19, rows=False)
+    for h, (i, j) in enumerate(((0, 0), (0, 850))):
+        page, row = R.token_row(b.k, b.table, i, j)
+        b.k[page, h, row] = b.q[0, 4 * h] * 9
+    b.check()
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+def test_the_same_call_gives_the_same_bits(dtype):
+    b = Batch([(1500, one(*range(1501, 1520))), (90, one(100, 91))], (8, 2), 16, dtype, 20, rows=False)
+    got = []
+    for _ in range(3):
+        b.g.manual_seed(1)
+        got.append(b.check())
+    for out, sc in got[1:]:
+        assert torch.equal(out, got[0][0]) and torch.equal(sc, got[0][1])
+
+
+def test_a_place_for_fewer_scores_than_tokens():
+    for dtype in (BF, F32):
+        b = Batch([(300, one(400, 330))], (8, 2), 16, dtype, 21, rows=False)
+        b.n_cap = 250
+        b.check()
+        b.n_cap = 310
+        b.check(64, 4)
+
+
+@pytest.mark.parametrize("dtype,groups,heads", [
+    (BF, [(30000, one(30100, 30001, 30500))], (8, 2)), (F32, [(9000, one(9100, 9001))], (4, 4)),
+    (BF, [(20, one(*[21 + i % 50 for i in range(300)]))], (4, 1)), (F32, [(20, one(*[21 + i % 50 for i in range(150)]))], (4, 1)),
+    (BF, [(5 + i, one(6 + i, 7 + i, 90)) for i in range(70)], (2, 2))])
+def test_long_ones_and_many(dtype, groups, heads):
+    Batch(groups, heads, 16, dtype, 22, rows=False).check()
