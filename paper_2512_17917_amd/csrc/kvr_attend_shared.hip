@@ -1,22 +1,27 @@
 // Attention where groups of sequences begin with the same tokens: those are read once for all of a group's queries, each
 // sequence's own tokens beside them, in one launch (kvr_shared.h says how the work is cut); a second one joins the pieces.
 //
-// bf16.  A workgroup has 256 columns of a unit, eight waves of 32, and walks over the unit's tokens in tiles of 64, which go
-// from the pages straight to LDS, three tiles ahead and past the ends of units.  A wave computes S = K Q^T (keys x columns,
-// v_mfma_f32_32x32x16_bf16; Q stays in registers), so that a lane holds logits of one column alone; the registers of S,
-// exponentiated and rounded to bf16, are the B operand of O^T = V^T P as they lie, with ds_read_b64_tr_b16 fetching the values
-// in the same order of tokens.
+// bf16.  A workgroup has up to 256 columns of a unit and walks over the unit's tokens in tiles of 64, which go from the pages
+// straight to LDS, three tiles ahead and past the ends of units.  A wave has 32 columns, and where columns are up to 128 two
+// waves share them and have half the tokens each.
+// A wave computes S = K Q^T (keys x columns, v_mfma_f32_16x16x32_bf16; Q stays in registers), so that a lane holds logits of
+// one column alone; the registers of S, exponentiated and rounded to bf16, are the B operand of O^T = V^T P as they lie (its k
+// index may be counted in any order as long as V^T has the same), with ds_read_b64_tr_b16 fetching groups of four tokens.
 //   Rounding p to bf16: the matrix unit takes nothing wider at this rate; the error is half a step of the output's type at
 // most, relative to sum p |v|.  Their sum is taken in float32 before it.
 //   The running maximum moves only when it is passed by more than 8 (in powers of two): p then stays below 2^8.
-// LDS rows are 256 bytes, 16 pieces of 16; keys: piece c of row r lies at c ^ (r mod 16), values: at c ^ 4 (r mod 4), so that
-// the lanes that are served together find different banks.
+// At a unit's end waves with the same columns are joined in the tile's place in LDS, which is free until the next step.
+//
+// LDS rows are 256 bytes, 16 pieces of 16; keys: piece c of row r lies at c ^ (r mod 16), values: at c ^ 4 (r mod 4) ^ 2 (r / 4 mod
+// 2), so that the lanes that are served together find different banks.
 // Rows that no column may see (past the tokens, before a sequence's own, on a page that is not there) are cleared in LDS; in
 // tiles that some columns see and others do not, values that are not finite are too, since 0 times them would reach every
 // column, and are added for the columns that see them afterwards.
 //
 // float32.  A workgroup has 16 columns; its four waves take 16 of a tile's 64 tokens each, with running maxima and sums of
 // their own, and are joined in LDS at a piece's end (the layouts are those of the float32 kernel for prompts).
+#include <type_traits>
+
 #include "kvr_prompt.h"
 #include "kvr_shared.h"
 
@@ -27,7 +32,23 @@ namespace {
 constexpr int SH_WAVES = 8, SH_COLS = 32 * SH_WAVES, SH_KEYS = 64;
 constexpr int SH_TILE = SH_KEYS * D * 2;                       // bytes of a tile of keys or values
 constexpr int SH_BUFS = 4;
-constexpr int SH_LDS = 2 * SH_BUFS * SH_TILE + 2 * SH_BUFS * SH_WAVES;
+constexpr int SH_FEW = 16;                                      // columns whose queries come through LDS, four units ahead
+constexpr int SH_QUERIES = SH_FEW * D * 2;
+constexpr int SH_LIST = 128, SH_LIST_ANY = 24;                  // tiles that are listed at a time (where rows lie anywhere)
+constexpr int SH_ROWS = SH_LIST * 8 > SH_LIST_ANY * SH_KEYS ? SH_LIST * 8 : SH_LIST_ANY * SH_KEYS;      // numbers of their rows' places
+struct SharedLds {
+  unsigned char k[SH_BUFS][SH_TILE], v[SH_BUFS][SH_TILE];
+  unsigned char q[SH_BUFS][SH_QUERIES];                         // queries of units of few columns
+  Piece list[PIECES];
+  int upto[PIECES];                                             // tiles of the list's pieces up to one's end
+  int row[SH_ROWS];                                             // of tiles: eight rows' first, or every row
+  int4 tile[SH_LIST];                                           // rows that some column may see (two words), first token, flags
+  float2 ml[SH_WAVES][32];                                      // waves' maxima and sums
+  int4 share;
+  unsigned char odd[SH_BUFS][SH_WAVES];                         // rows with a value that is not finite, a byte a wave
+};
+constexpr int SH_LDS = sizeof(SharedLds);
+static_assert(SH_LDS <= 160 * 1024);
 constexpr float KEEP_MAX = 8.f;
 constexpr int SF_WAVES = 4, SF_COLS = 16, SF_KEYS = 64;
 typedef float f32x4_t __attribute__((ext_vector_type(4)));
@@ -44,10 +65,10 @@ struct SharedOut {
   int keys, most_scores_splits, scores_wgs;
 };
 
-// Position of a row of group u.g, -1 if its sequence does not have the tokens in common (all lanes call, each with its row)
-__device__ __forceinline__ int position_in_group(const DevDesc& d, const SharedArgs& s, const Unit& u, int row) {
+// Position of a row of group g, -1 if its sequence does not have the tokens in common (all lanes call, each with its row)
+__device__ __forceinline__ int position_in_group(const DevDesc& d, const SharedArgs& s, int g, int row) {
   const int lane = threadIdx.x & 63;
-  const Group x = group_at(s, d.B, u.g);
+  const Group x = group_at(s, d.B, g);
   int b = row;
   if (s.a.q_start != nullptr) {
     b = x.b0;
@@ -62,318 +83,467 @@ __device__ __forceinline__ int position_in_group(const DevDesc& d, const SharedA
   return m.from > 0 ? m.n - m.span.n + (row - m.span.first) : -1;
 }
 
-// Where the rows of a tile lie: in one page (dense caches, pages of whole tiles), the eight that a wave fetches in one page, or
-// anywhere.
-enum { IN_ONE_PAGE, EIGHT_A_PAGE, ANYWHERE };
+// a piece of the list, in scalar registers
+__device__ __forceinline__ Piece listed_piece(const Piece* p) {
+  const int4* from = reinterpret_cast<const int4*>(p);
+  const int4 x = from[0], y = from[1], z = from[2], t = from[3];
+  return Piece{uniform(x.x), uniform(x.y), uniform(x.z), uniform(x.w), uniform(y.x), uniform(y.y), uniform(y.z), uniform(y.w),
+               uniform(z.x), uniform(z.y), uniform(z.z), uniform(z.w), uniform(t.x), uniform(t.y), uniform(t.z), uniform(t.w)};
+}
+__device__ __forceinline__ Run run_of_piece(const Piece& p) { return Run{p.ahead0, p.ahead, p.start, p.i1}; }
+
+// Where the rows of a tile lie: eight side by side (pages of whole eights), or anywhere.
+enum { EIGHT_A_PAGE, ANYWHERE };
+// What is known of a tile: all columns see it whole, some see what others do not, it is its piece's first or last; it is no tile of
+// tokens but of queries, 128 of the piece's columns (where they are more than come beside the tokens).  The piece's number goes with it.
+enum { WHOLE = 1, APART = 2, FIRST = 4, LAST = 8, QUERIES = 16, NUMBER = 8 };
+
+__device__ __forceinline__ float rows_max(float x) {            // largest of lanes l, l ^ 16, l ^ 32, l ^ 48
+  x = across_max(x);
+  auto b = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return fmaxf(__uint_as_float(b[0]), __uint_as_float(b[1]));
+}
+__device__ __forceinline__ float rows_sum(float x) {
+  x = across_sum(x);
+  auto b = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return __uint_as_float(b[0]) + __uint_as_float(b[1]);
+}
 
 template <int ROWS>
 __global__ __launch_bounds__(64 * SH_WAVES, 2) void shared_bf16_kernel(DevDesc d, SharedArgs args, SharedOut so) {
   extern __shared__ __align__(1024) unsigned char s_mem[];
-  unsigned char* s_k = s_mem;                                   // [4][64][256]
-  unsigned char* s_v = s_k + SH_BUFS * SH_TILE;                 // [4][64][256]
-  unsigned char* s_there = s_v + SH_BUFS * SH_TILE;             // [4][8]: rows that some column may see, a byte per wave
-  unsigned char* s_odd = s_there + SH_BUFS * SH_WAVES;          // [4][8]: rows with a value that is not finite
-  constexpr bool ONE = ROWS == IN_ONE_PAGE;
+  SharedLds& lds = *reinterpret_cast<SharedLds*>(s_mem);
   const PagedArgs& a = args.a;
   const int lane = threadIdx.x & 63, wave = uniform((int)(threadIdx.x >> 6)), w = blockIdx.x;
-  const int half = lane >> 5, col = lane & 31;
+  const int r4 = lane >> 4, col = lane & 15;
   const int gs = __builtin_ctz(d.G);                            // G is a power of two
   const float NEG_INF = -__builtin_inff();
-  if (so.work && blockIdx.x == gridDim.x - 1 && wave == 0) find_scores_work(d, a, so.keys, so.most_scores_splits, so.scores_wgs, so.work);
-  const int total = RowBf16::all(d, args);
-  const int per = uniform((int)(((unsigned)total + gridDim.x - 1) / gridDim.x));
-  if ((long long)w * per >= total) return;
-  const int n_all = min(per, total - w * per);
-
-  Unit cu, fu;                                  // of the tile that is worked on, of the one that is fetched next
-  int ci, fi;                                   // which of their tiles
-  fu = RowBf16::find(d, args, w * per, fi);
-  cu = fu;
-  ci = fi;
-
-  const int piece = lane & 15;
-  const uint32_t lds0 = lds_offset(s_mem);
-  int entry[2] = {0, 0};                        // the table's, of the tile that is fetched next
-  auto ask = [&] {
-    const int j0 = run_token<SH_KEYS>(fu.run, fi);
-    if constexpr (ONE) entry[0] = page_entry(a.pages, fu.b, j0);
-    else if constexpr (ROWS == EIGHT_A_PAGE) entry[0] = page_entry(a.pages, fu.b, min(j0 + 8 * wave, (fu.lim - 1) & ~7));
-    else
-#pragma unroll
-      for (int x = 0; x < 2; ++x) entry[x] = page_entry(a.pages, fu.b, min(j0 + 8 * wave + 4 * x + (lane >> 4), fu.lim - 1));
-  };
-  // Starts a step's tile on its way to LDS.  Bit x of what it returns: no column may see row 4 x + l div 16 of this wave's.
-  auto fetch = [&](int step) {
-    uint32_t dead = 0;
-    if (step >= n_all) return dead;
-    const int j0 = run_token<SH_KEYS>(fu.run, fi), buf = step & (SH_BUFS - 1), lim = fu.lim;
-    int row0 = 0, j8 = 0;
-    bool no_page = false;
-    if constexpr (ROWS != ANYWHERE) {
-      j8 = ONE ? j0 : min(j0 + 8 * wave, (lim - 1) & ~7);
-      row0 = (int)entry_row(a.pages, d.Hkv, entry[0], fu.h, j8);
-      no_page = row0 < 0;
-      row0 = max(row0, 0);
-    }
-#pragma unroll
-    for (int x = 0; x < 2; ++x) {
-      const int rr = 8 * wave + 4 * x + (lane >> 4);
-      int r;
-      bool gone;
-      if constexpr (ROWS != ANYWHERE) {
-        r = row0 + min(ONE ? rr : rr - 8 * wave, lim - 1 - j8);
-        gone = no_page;
-      } else {
-        r = (int)entry_row(a.pages, d.Hkv, entry[x], fu.h, min(j0 + rr, lim - 1));
-        gone = r < 0;
-        r = max(r, 0);
-      }
-      dead |= gone || j0 + rr >= lim || j0 + rr < fu.from ? 1u << x : 0u;
-      const unsigned char* kp = (const unsigned char*)a.pages.k + (size_t)(uint32_t)r * (D * 2);
-      const unsigned char* vp = (const unsigned char*)a.pages.v + (size_t)(uint32_t)r * (D * 2);
-      const int to = buf * SH_TILE + (8 * wave + 4 * x) * 256;
-      to_lds(kp + ((piece ^ (rr & 15)) << 4), uniform((int)(lds0 + to)));
-      to_lds(vp + ((piece ^ (4 * (rr & 3))) << 4), uniform((int)(lds0 + SH_BUFS * SH_TILE + to)));
-    }
-    if (step + 1 < n_all) {
-      if (++fi == fu.run.n) {
-        RowBf16::next(d, args, fu);
-        fi = 0;
-      }
-      ask();
-    }
-    return dead;
-  };
-
-  const Scale2 sc = scale2(d.scale);
-  bf16x8_t q[8], p[4];
-  f32x16_t o[4], s[2];
-  float m_run, l_run;
-  bool wave_live, live;
-  int P;                                        // position of this lane's column (what it sees of the unit's tokens)
-  auto begin = [&] {
-    const int m = cu.ct * SH_COLS + 32 * wave + col;
-    wave_live = cu.ct * SH_COLS + 32 * wave < cu.cols;
-    live = m < cu.cols;
-    const int row = cu.row0 + (live ? m >> gs : 0);
-    P = !live ? -1 : cu.own ? cu.lo + (m >> gs) : 0x7fffffff;
-    if (!cu.own && a.vis.window > 0) {
-      const int at = position_in_group(d, args, cu, row);
-      P = live ? at : -1;
-    }
-    m_run = NEG_INF;
-    l_run = 0.f;
-#pragma unroll
-    for (int cb = 0; cb < 4; ++cb)
-#pragma unroll
-      for (int x = 0; x < 16; ++x) o[cb][x] = 0.f;
-    if (!wave_live) return;
-    const bf16_t* qp = (const bf16_t*)a.q + ((size_t)row * d.Hq + cu.h * d.G + (live ? m & (d.G - 1) : 0)) * D + 8 * half;
-#pragma unroll
-    for (int c = 0; c < 8; ++c) {
-      u32x4_t x = *reinterpret_cast<const u32x4_t*>(qp + 16 * c);
-#pragma unroll
-      for (int e = 0; e < 4; ++e) x[e] = (x[e] ^ sc.flip) & sc.keep;
-      q[c] = __builtin_bit_cast(bf16x8_t, x);
-    }
-  };
-  auto finish = [&](bool first, bool last) {    // whether the piece has the unit's first tile, and its last
-    const int c0 = RowBf16::place(d, a.n_rows, cu.own, cu.row0, cu.cols, cu.ct, cu.h);
-    if (threadIdx.x == 0 && cu.ct * SH_COLS < cu.cols) {
-      if (first) so.span[2 * (size_t)c0] = w;
-      if (last) so.span[2 * (size_t)c0 + 1] = w;
-    }
-    if (!wave_live) return;
-    l_run = across_sum(l_run);
-    if (!live) return;
-    const size_t slot = (size_t)SH_COLS * w + c0 + 32 * wave + col;
-    float* op = so.part_o + slot * D;
-#pragma unroll
-    for (int cb = 0; cb < 4; ++cb)
-#pragma unroll
-      for (int x = 0; x < 16; x += 4)
-        *reinterpret_cast<float4*>(op + 32 * cb + 8 * (x / 4) + 4 * half) = make_float4(o[cb][x], o[cb][x + 1], o[cb][x + 2], o[cb][x + 3]);
-    if (half == 0) *reinterpret_cast<float2*>(so.part_ml + 2 * slot) = make_float2(m_run, l_run);
-  };
-
-  // LDS addresses of a lane's operands, relative to a tile
-  const int k_row = col * 256, k_swz = col & 15;
-  const int v_key = 4 * half + ((lane & 15) >> 2);               // of each group of eight tokens
-  const int v_at = v_key * 256 + 8 * (lane & 1), v_swz = 4 * (v_key & 3);
-  const int v_chunk = 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1);
-  auto logits = [&](int buf) {                  // s = K Q^T
-    const unsigned char* tk = s_k + buf * SH_TILE;
-#pragma unroll
-    for (int kb = 0; kb < 2; ++kb)
-#pragma unroll
-      for (int x = 0; x < 16; ++x) s[kb][x] = 0.f;
-#pragma unroll
-    for (int c = 0; c < 8; ++c)
-#pragma unroll
-      for (int kb = 0; kb < 2; ++kb) {
-        const bf16x8_t k = *reinterpret_cast<const bf16x8_t*>(tk + kb * 32 * 256 + k_row + (((2 * c + half) ^ k_swz) << 4));
-        s[kb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k, q[c], s[kb], 0, 0, 0);
-      }
-  };
-  auto weights = [&] {                          // s -> p, with the running maximum and sum
-    float mx = s[0][0];
-#pragma unroll
-    for (int kb = 0; kb < 2; ++kb)
-#pragma unroll
-      for (int x = 0; x < 16; ++x) mx = fmaxf(mx, s[kb][x]);
-    mx = across_max(mx) * sc.c;
-    if (__any(mx > m_run + KEEP_MAX) || __any(m_run == NEG_INF && mx > NEG_INF)) {
-      const float m_new = fmaxf(m_run, mx);
-      const float corr = m_run == NEG_INF ? 0.f : exp2_(m_run - m_new);
-      l_run *= corr;
-#pragma unroll
-      for (int cb = 0; cb < 4; ++cb)
-#pragma unroll
-        for (int x = 0; x < 16; ++x) o[cb][x] *= corr;
-      m_run = m_new;
-    }
-    const float m_use = m_run == NEG_INF ? 0.f : m_run;
-#pragma unroll
-    for (int ks = 0; ks < 4; ++ks) {
-#pragma unroll
-      for (int e = 0; e < 8; e += 2) {
-        const f32x2_t x = {exp2_(fmaf(s[ks >> 1][8 * (ks & 1) + e], sc.c, -m_use)),
-                           exp2_(fmaf(s[ks >> 1][8 * (ks & 1) + e + 1], sc.c, -m_use))};
-        const bf16x2_t y = __builtin_convertvector(x, bf16x2_t);
-        l_run += x[0] + x[1];
-        p[ks][e] = y[0];
-        p[ks][e + 1] = y[1];
-      }
-    }
-  };
-  auto add_values = [&](int buf) {              // o += V^T p
-    const unsigned char* tv = s_v + buf * SH_TILE;
-#pragma unroll
-    for (int ks = 0; ks < 4; ++ks)
-#pragma unroll
-      for (int cb = 0; cb < 4; ++cb) {
-        // tokens 16 ks + {0..3, 8..11} (+ 4 for the upper lanes) of channel 32 cb + lane mod 32
-        typedef __attribute__((address_space(3))) s16x4_t* lds4;
-        const unsigned char* vp = tv + ks * 16 * 256 + v_at + (((4 * cb + v_chunk) ^ v_swz) << 4);
-        const s16x4_t x = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)(vp));
-        const s16x4_t y = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)(vp + 8 * 256));
-        const s16x8_t v = {x[0], x[1], x[2], x[3], y[0], y[1], y[2], y[3]};
-        o[cb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, v), p[ks], o[cb], 0, 0, 0);
-      }
-  };
-
-  uint32_t d0 = 0, d1 = 0, d2 = 0;              // what fetch said of the last three tiles
-  auto fetch_next = [&](int step) {
-    d0 = d1;
-    d1 = d2;
-    d2 = fetch(step);
-  };
-  ask();
-  fetch_next(0);
-  fetch_next(1);
-  fetch_next(2);
-  bool fresh = true;
-  int piece0 = ci;
-  for (int step = 0; step < n_all; ++step) {
-    const int buf = step & (SH_BUFS - 1), j0 = run_token<SH_KEYS>(cu.run, ci);
-    if (fresh) {
-      begin();
-      fresh = false;
-      piece0 = ci;
-    }
-    // a tile that all columns see whole, and one of which some see what others do not
-    const bool whole = cu.own ? j0 >= cu.from && j0 + SH_KEYS - 1 <= cu.lo &&
-                                    (a.vis.window == 0 || j0 > cu.hi - a.vis.window || j0 + SH_KEYS - 1 < a.vis.n_sink)
-                              : a.vis.window == 0 && j0 + SH_KEYS - 1 < cu.lim;
-    const bool apart = !whole && (a.vis.window > 0 || (cu.own && cu.lo < cu.hi));
-    if (step + 2 < n_all) asm volatile("s_waitcnt vmcnt(8)" ::: "memory");
-    else if (step + 1 < n_all) asm volatile("s_waitcnt vmcnt(4)" ::: "memory");
-    else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-    uint32_t odd = 0, rows = 0xffu;
-    if (apart || __any(d0 != 0)) {
-      rows = 0;
-#pragma unroll
-      for (int x = 0; x < 2; ++x) {
-        const bool dead = (d0 >> x) & 1;
-        u32x4_t* mine = reinterpret_cast<u32x4_t*>(s_v + buf * SH_TILE + (8 * wave + 4 * x) * 256 + lane * 16);
-        u32x4_t v = *mine;
-        bool bad = false;
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const uint32_t lo16 = (v[e] & 0x7f80u) == 0x7f80u ? 0x0000ffffu : 0u;
-          const uint32_t hi16 = (v[e] & 0x7f800000u) == 0x7f800000u ? 0xffff0000u : 0u;
-          bad = bad || (apart && (lo16 | hi16) != 0);
-          v[e] = dead ? 0u : apart ? v[e] & ~(lo16 | hi16) : v[e];
-        }
-        if (dead || bad) *mine = v;
-        const unsigned long long alive = __ballot(!dead), who = __ballot(bad && !dead);
-#pragma unroll
-        for (int r = 0; r < 4; ++r) {
-          rows |= (uint32_t)((alive >> (16 * r)) & 1) << (4 * x + r);
-          odd |= ((who >> (16 * r)) & 0xffffu) != 0 ? 1u << (4 * x + r) : 0u;
-        }
-      }
-    }
-    if (lane == 0) {
-      s_there[SH_WAVES * buf + wave] = (unsigned char)rows;
-      s_odd[SH_WAVES * buf + wave] = (unsigned char)odd;
-    }
+  if (so.work && blockIdx.x == gridDim.x - 1 && wave == 1) find_scores_work(d, a, so.keys, so.most_scores_splits, so.scores_wgs, so.work);
+  auto barrier = [&] {
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
     __builtin_amdgcn_sched_barrier(0);
     asm volatile("s_barrier" ::: "memory");
     __builtin_amdgcn_sched_barrier(0);
-    fetch_next(step + 3);
-    const uint64_t there = *reinterpret_cast<const uint64_t*>(s_there + SH_WAVES * buf);
-    if (wave_live && there != 0) {
-      logits(buf);
-      if (!whole || there != ~0ull) {
-#pragma unroll
-        for (int kb = 0; kb < 2; ++kb)
-#pragma unroll
-          for (int x = 0; x < 16; ++x) {
-            const int key = 32 * kb + 8 * (x / 4) + 4 * half + x % 4;
-            s[kb][x] = sees(a.vis, P, j0 + key) && ((there >> key) & 1) ? s[kb][x] : NEG_INF;
-          }
+  };
+  Share mine = {0, 0, 0, 0};
+
+  // ---- tiles ----
+  constexpr int MOST = ROWS == EIGHT_A_PAGE ? SH_LIST : SH_LIST_ANY;
+  auto query_tiles = [&](int cols, int ct) {
+    const int some = cols - ct * SH_COLS;
+    return some <= SH_FEW ? 0 : some <= SH_COLS / 2 ? 1 : 2;
+  };
+  // The list of pieces, and how many tiles they have (wave 0 finds it out; all get it).
+  auto list_pieces = [&] {
+    if (wave == 0) {
+      RowBf16::list(d, args, mine, lds.list);
+      const Piece& f = lds.list[lane];
+      const int n = lane < mine.n && f.i0 < f.i1 ? f.i1 - f.i0 + query_tiles(f.cols, f.ct) : 0;
+      lds.upto[lane] = lanes_upto(n);
+      if (lane == 0) lds.share = make_int4(mine.at, mine.upto, mine.end, mine.n);
+    }
+    barrier();
+    const int4 x = lds.share;
+    mine = Share{uniform(x.x), uniform(x.y), uniform(x.z), uniform(x.w)};
+  };
+  // Lists tiles t0 .. t0 + n - 1 of the pieces: where their rows are, who sees them.
+  auto list_tiles = [&](int t0, int n) {
+    constexpr int EACH = ROWS == EIGHT_A_PAGE ? 8 : SH_KEYS;    // threads a tile
+    for (int i = threadIdx.x; i < n * EACH; i += 64 * SH_WAVES) {
+      const int t = i / EACH, x = i % EACH;
+      int p = 0;
+#pragma unroll 1
+      for (int k = PIECES / 2; k > 0; k >>= 1)
+        if (lds.upto[p + k - 1] <= t0 + t) p += k;
+      const Piece& f = lds.list[p];
+      const int at = f.i1 - (lds.upto[p] - (t0 + t));           // (tiles of queries: before i0)
+      int flags = at + 1 == f.i1 ? LAST : 0, j0 = at - f.i0 + query_tiles(f.cols, f.ct);
+      flags |= (j0 == 0 ? FIRST : 0) | p << NUMBER;
+      uint64_t there = ~0ull;
+      long long r = 0;
+      if (at < f.i0) {
+        flags |= QUERIES;
+      } else {
+        j0 = run_token<SH_KEYS>(Run{f.ahead0, f.ahead, f.start, 0}, at);
+        const int j63 = j0 + SH_KEYS - 1, lim = f.lim, from = f.from;
+        const bool own = (f.bits & PIECE_OWN) != 0;
+        const bool whole = own ? j0 >= from && j63 <= f.lo && (a.vis.window == 0 || j0 > f.hi - a.vis.window || j63 < a.vis.n_sink)
+                               : a.vis.window == 0 && j63 < lim;
+        const bool apart = !whole && (a.vis.window > 0 || (own && f.lo < f.hi));
+        flags |= (whole ? WHOLE : 0) | (apart ? APART : 0);
+        const int j = ROWS == EIGHT_A_PAGE ? j0 + 8 * x : j0 + x;
+        r = page_row(a.pages, d.Hkv, f.b, f.h, min(j, ROWS == EIGHT_A_PAGE ? (lim - 1) & ~7 : lim - 1));
+        const int n0 = clampi(from - j, 0, 8), n1 = clampi(lim - j, 0, 8);
+        there = r < 0 ? 0u : ((1u << n1) - 1u) & ~((1u << n0) - 1u);
       }
-      weights();
-      add_values(buf);
-      // values that are not finite, for the columns that see them; their weights once more, from the keys in LDS
-      uint64_t left = apart ? *reinterpret_cast<const uint64_t*>(s_odd + SH_WAVES * buf) : 0;
-      while (left != 0) {
-        const int key = __ffsll((unsigned long long)left) - 1;
-        left &= left - 1;
+      if constexpr (ROWS == EIGHT_A_PAGE) {
+        reinterpret_cast<unsigned char*>(&lds.tile[t])[x] = (unsigned char)there;
+      } else {
+        const uint64_t all = __ballot(there & 1);               // (a wave has a tile)
+        if (x == 0) *reinterpret_cast<uint64_t*>(&lds.tile[t]) = all;
+      }
+      lds.row[i] = (int)max(r, 0ll);
+      if (x == 0) {
+        lds.tile[t].z = j0;
+        lds.tile[t].w = flags;
+      }
+    }
+  };
+  // Starts listed tile t on its way to LDS: this wave's rows 8 wave .. +7, lane l the pieces l mod 16 of row l div 16 (+ 4), or 16
+  // columns' queries.
+  const uint32_t lds0 = lds_offset(s_mem);
+  const uint32_t k_in = (col ^ ((8 * wave + r4) & 15)) << 4, v_in = (col ^ (4 * r4)) << 4;
+  auto fetch = [&](int t, int n) {
+    if (t >= n) return;
+    const int flags = uniform(lds.tile[t].w);
+    const uint32_t to = lds0 + (t & (SH_BUFS - 1)) * SH_TILE + 8 * wave * 256;
+    if (flags & (FIRST | QUERIES)) {
+      const int now = flags >> NUMBER;
+      const Piece& f = lds.list[now];
+      const int c0 = uniform(f.ct) * SH_COLS, some = min(uniform(f.cols) - c0, SH_COLS), h = uniform(f.h), row0 = uniform(f.row0);
+      const bool few = some <= SH_FEW;
+      if (!few || wave < 4) {
+        const int first = few ? 4 * wave : (uniform(lds.tile[t].z) << 7) + 16 * wave;
+        const uint32_t place = few ? lds_offset(lds.q[now & (SH_BUFS - 1)]) + 4 * wave * 256
+                                   : lds0 + (t & (SH_BUFS - 1)) * SH_TILE + (wave & 3) * 4096 + (wave >> 2) * SH_BUFS * SH_TILE;
+        for (int x = 0; x < (few ? 1 : 4); ++x) {
+          const int at = first + 4 * x + r4, m = c0 + min(at, some - 1);
+          const unsigned char* from = (const unsigned char*)a.q + ((size_t)(row0 + (m >> gs)) * d.Hq + h * d.G + (m & (d.G - 1))) * (D * 2);
+          to_lds(from + ((col ^ (at & 15)) << 4), uniform((int)(place + x * 1024)));
+        }
+      }
+      if (!few) return;
+    }
+    if constexpr (ROWS == EIGHT_A_PAGE) {
+      const uint32_t row = (uint32_t)uniform(lds.row[8 * t + wave]);
+      const unsigned char* kp = (const unsigned char*)a.pages.k + (size_t)row * (D * 2);
+      const unsigned char* vp = (const unsigned char*)a.pages.v + (size_t)row * (D * 2);
+#pragma unroll
+      for (int x = 0; x < 2; ++x) {
+        to_lds(kp, (k_in ^ (x << 6)) + (4 * x + r4) * 256, uniform((int)(to + x * 1024)));
+        to_lds(vp, (v_in ^ (x << 5)) + (4 * x + r4) * 256, uniform((int)(to + SH_BUFS * SH_TILE + x * 1024)));
+      }
+    } else {
+#pragma unroll
+      for (int x = 0; x < 2; ++x) {
+        const size_t at = (size_t)(uint32_t)lds.row[SH_KEYS * t + 8 * wave + 4 * x + r4] * (D * 2);
+        to_lds((const unsigned char*)a.pages.k + at + (k_in ^ (x << 6)), uniform((int)(to + x * 1024)));
+        to_lds((const unsigned char*)a.pages.v + at + (v_in ^ (x << 5)), uniform((int)(to + SH_BUFS * SH_TILE + x * 1024)));
+      }
+    }
+  };
+
+  // ---- a unit's columns ----
+  const Scale2 sc = scale2(d.scale);
+  bf16x8_t q[2][4];                             // of two blocks of 16 columns
+  f32x4_t o[2][8];
+  float m_run[2], l_run[2];
+  int P[2];                                     // position of this lane's columns (what they see of the unit's tokens)
+  int now = 0;                                  // the piece that is worked on
+  int shares = 1, key0 = 0, col0 = 0;           // waves with this one's columns, its first token of a tile and its first column
+  bool wave_live = false;
+  auto take_queries = [&](const unsigned char* from, uint32_t bank) {      // of this wave's columns; bank: bytes from columns 0 .. 63 to the others
+#pragma unroll
+    for (int n = 0; n < 2; ++n)
+#pragma unroll
+      for (int c = 0; c < 4; ++c) {
+        const int at = (col0 + 16 * n + col) & (SH_COLS / 2 - 1);
+        u32x4_t x = *reinterpret_cast<const u32x4_t*>(from + (at >> 6) * bank + (at & 63) * 256 + (((4 * c + r4) ^ (at & 15)) << 4));
+#pragma unroll
+        for (int e = 0; e < 4; ++e) x[e] = (x[e] ^ sc.flip) & sc.keep;
+        q[n][c] = __builtin_bit_cast(bf16x8_t, x);
+      }
+  };
+  auto begin = [&](int piece) {
+    now = piece;
+    const Piece& u = lds.list[now];
+    const int ct = uniform(u.ct), cols = uniform(u.cols), own = uniform(u.bits) & PIECE_OWN, lo = uniform(u.lo), row0 = uniform(u.row0);
+    const int some = min(cols - ct * SH_COLS, SH_COLS);
+    shares = some <= SH_COLS / 2 ? 2 : 1;
+    key0 = shares == 2 ? 32 * (wave & 1) : 0;
+    col0 = 32 * (shares == 2 ? wave >> 1 : wave);
+    wave_live = col0 < some;
+#pragma unroll
+    for (int n = 0; n < 2; ++n) {
+      const int at = col0 + 16 * n + col, m = ct * SH_COLS + at;
+      const bool live = at < some;
+      P[n] = !live ? -1 : own ? lo + (m >> gs) : 0x7fffffff;
+      m_run[n] = NEG_INF;
+      l_run[n] = 0.f;
+#pragma unroll
+      for (int cb = 0; cb < 8; ++cb) o[n][cb] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+    }
+    if (!own && a.vis.window > 0) {
+      const int g = uniform(u.g);
+#pragma unroll 1
+      for (int n = 0; n < 2; ++n) {
+        const int at = col0 + 16 * n + col, m = ct * SH_COLS + at;
+        const int p = position_in_group(d, args, g, row0 + (at < some ? m >> gs : 0));
+        if (n == 0) P[0] = at < some ? p : -1;
+        else P[1] = at < some ? p : -1;
+      }
+    }
+    // (few columns: the second block's are none, and get what lies there)
+    if (some <= SH_FEW && wave_live) take_queries(lds.q[now & (SH_BUFS - 1)], 0);
+  };
+  // (buf: the tile's place, which is free once all have read it)
+  auto finish = [&](int buf) {
+    const Piece& u = lds.list[now];
+    const int bits = uniform(u.bits), ct = uniform(u.ct), cols = uniform(u.cols), row0 = uniform(u.row0), h = uniform(u.h);
+    const int some = min(cols - ct * SH_COLS, SH_COLS);
+    const int c0 = RowBf16::place(d, a.n_rows, (bits & PIECE_OWN) != 0, row0, cols, ct, h);
+    const size_t slot0 = (size_t)SH_COLS * w + c0;
+    if (threadIdx.x == 0) {
+      if (bits & PIECE_FIRST) so.span[2 * (size_t)c0] = w;
+      if (bits & PIECE_LAST) so.span[2 * (size_t)c0 + 1] = w;
+    }
+    const bool second = shares == 2 && (wave & 1);
+    if (shares == 2) barrier();                 // (all have read the tile)
+#pragma unroll
+    for (int n = 0; n < 2; ++n) {
+      const int at = col0 + 16 * n + col;
+      float* op = so.part_o + (slot0 + at) * D + 4 * r4;
+      float m = m_run[n], l = rows_sum(l_run[n]);
+      if (shares == 2) {
+        // of two waves with the same columns the first gets the lower channels of both, the second the upper ones
+        const int slot = some > 64 ? wave : 4 * n + wave;       // 4 KB each, 32 in all
+        f32x4_t* to = reinterpret_cast<f32x4_t*>(slot < 4 ? lds.k[buf] + slot * 4096 : lds.v[buf] + (slot - 4) * 4096);
+        f32x4_t* of = reinterpret_cast<f32x4_t*>((slot ^ 1) < 4 ? lds.k[buf] + (slot ^ 1) * 4096 : lds.v[buf] + ((slot ^ 1) - 4) * 4096);
+        if (wave_live) {
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            to[i * 64 + lane] = second ? o[n][i] : o[n][4 + i];
+            o[n][i] = second ? o[n][4 + i] : o[n][i];
+          }
+          if (r4 == 0) lds.ml[wave][16 * n + col] = make_float2(m, l);
+        }
+        barrier();
+        const float2 ml = lds.ml[wave ^ 1][16 * n + col];
+        const float mx = fmaxf(m, ml.x), m_use = mx == NEG_INF ? 0.f : mx;
+        const float f = exp2_(m - m_use), g = exp2_(ml.x - m_use);
+        l = fmaf(g, ml.y, f * l);
+        m = mx;
+        if (wave_live)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) o[n][i] = o[n][i] * f + of[i * 64 + lane] * g;
+        if (n == 0 && some > 64) barrier();
+      }
+      if (!wave_live || at >= some) continue;
+      if (second) op += 64;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) *reinterpret_cast<f32x4_t*>(op + 16 * i) = o[n][i];
+      if (shares == 1)
+#pragma unroll
+        for (int i = 4; i < 8; ++i) *reinterpret_cast<f32x4_t*>(op + 16 * i) = o[n][i];
+      if (r4 == 0 && !second) *reinterpret_cast<float2*>(so.part_ml + 2 * (slot0 + at)) = make_float2(m, l);
+    }
+  };
+
+  // ---- 32 columns and 32 tokens of a tile ----
+  // LDS addresses of a lane's operands, relative to a tile: keys' row l mod 16 of a block, values' row 4 (l div 16) + l mod 16 div 4;
+  // the others are these with some bits turned (formed anew in each step: kept, they would take the registers of the sums)
+  const uint32_t k_at = col * 256 + ((r4 ^ col) << 4);
+  const uint32_t v_at = (4 * r4 + (col >> 2)) * 256 + 8 * (lane & 1) + (((4 * (col >> 2)) ^ (2 * (r4 & 1))) << 4) + (((col & 3) >> 1) << 4);
+  auto work = [&](int buf, int key0, int j0, int flags, uint64_t there) {
+    constexpr int N = 2, B = 2;
+    typedef __attribute__((address_space(3))) s16x4_t* lds4;
+    typedef __attribute__((address_space(3))) bf16x8_t* lds8;
+    uint32_t tk = lds0 + buf * SH_TILE + key0 * 256 + k_at, tv = lds0 + (SH_BUFS + buf) * SH_TILE + key0 * 256 + v_at;
+    asm volatile("" : "+v"(tk), "+v"(tv));
+    f32x4_t s[N][B];
+    bf16x8_t k[4][B];
+#pragma unroll
+    for (int c = 0; c < 4; ++c)
+#pragma unroll
+      for (int b = 0; b < B; ++b) k[c][b] = *((lds8)(uintptr_t)(tk ^ (c << 6)) + b * 256);
+#pragma unroll
+    for (int n = 0; n < N; ++n)
+#pragma unroll
+      for (int b = 0; b < B; ++b) s[n][b] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int c = 0; c < 4; ++c)
+#pragma unroll
+      for (int b = 0; b < B; ++b)
+#pragma unroll
+        for (int n = 0; n < N; ++n) s[n][b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k[c][b], q[n][c], s[n][b], 0, 0, 0);
+    // the values are asked for before the weights are known: four tokens of each block, of channel 16 cb + lane mod 16
+    s16x4_t v[8][2];
+#pragma unroll
+    for (int cb = 0; cb < 8; ++cb) {
+      const lds4 vp = (lds4)(uintptr_t)(tv ^ (cb << 5));
+      v[cb][0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(vp);
+      v[cb][1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(vp + 512);
+    }
+    __builtin_amdgcn_sched_barrier(0);
+    if (!(flags & WHOLE) || there != ~0ull) {
+#pragma unroll
+      for (int n = 0; n < N; ++n)
+#pragma unroll
+        for (int b = 0; b < B; ++b)
+#pragma unroll
+          for (int x = 0; x < 4; ++x) {
+            const int key = key0 + 16 * b + 4 * r4 + x;
+            s[n][b][x] = sees(a.vis, P[n], j0 + key) && ((there >> key) & 1) ? s[n][b][x] : NEG_INF;
+          }
+    }
+    // s -> p, with the running maximum and sum
+    float mx[N];
+    bool moves = false;
+#pragma unroll
+    for (int n = 0; n < N; ++n) {
+      mx[n] = s[n][0][0];
+#pragma unroll
+      for (int b = 0; b < B; ++b)
+#pragma unroll
+        for (int x = 0; x < 4; ++x) mx[n] = fmaxf(mx[n], s[n][b][x]);
+      mx[n] = rows_max(mx[n]) * sc.c;
+      moves = moves || mx[n] > m_run[n] + KEEP_MAX || (m_run[n] == NEG_INF && mx[n] > NEG_INF);
+    }
+    if (__any(moves)) {
+#pragma unroll
+      for (int n = 0; n < N; ++n) {
+        const float m_new = fmaxf(m_run[n], mx[n]);
+        const float corr = m_run[n] == NEG_INF ? 0.f : exp2_(m_run[n] - m_new);
+        l_run[n] *= corr;
+#pragma unroll
+        for (int cb = 0; cb < 8; ++cb) o[n][cb] *= corr;
+        m_run[n] = m_new;
+      }
+    }
+    bf16x8_t p[N];
+#pragma unroll
+    for (int n = 0; n < N; ++n) {
+      const float m_use = m_run[n] == NEG_INF ? 0.f : m_run[n];
+#pragma unroll
+      for (int b = 0; b < B; ++b)
+#pragma unroll
+        for (int x = 0; x < 4; x += 2) {
+          const f32x2_t y = {exp2_(fmaf(s[n][b][x], sc.c, -m_use)), exp2_(fmaf(s[n][b][x + 1], sc.c, -m_use))};
+          const bf16x2_t z = __builtin_convertvector(y, bf16x2_t);
+          l_run[n] += y[0] + y[1];
+          p[n][4 * b + x] = z[0];
+          p[n][4 * b + x + 1] = z[1];
+        }
+    }
+    // o += V^T p
+#pragma unroll
+    for (int cb = 0; cb < 8; ++cb) {
+      const s16x4_t x = v[cb][0], y = v[cb][1];
+      const s16x8_t both = {x[0], x[1], x[2], x[3], y[0], y[1], y[2], y[3]};
+#pragma unroll
+      for (int n = 0; n < N; ++n) o[n][cb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, both), p[n], o[n][cb], 0, 0, 0);
+    }
+  };
+  // Values that are not finite, for the columns that see them; their weights once more, from the keys in LDS.
+  auto add_odd = [&](int buf, int j0) {
+    uint64_t left = *reinterpret_cast<const uint64_t*>(lds.odd[buf]);
+    left = left >> key0 & (shares == 1 ? ~0ull : 0xffffffffull);
+    if (left == 0) return;
+    const int b = uniform(lds.list[now].b), h = uniform(lds.list[now].h);
+    while (left != 0) {
+      const int key = uniform(key0 + __ffsll((unsigned long long)left) - 1);
+      left &= left - 1;
+      const long long row = page_row(a.pages, d.Hkv, b, h, j0 + key);
+      const uint32_t* vr = reinterpret_cast<const uint32_t*>((const bf16_t*)a.pages.v + row * D);
+#pragma unroll
+      for (int n = 0; n < 2; ++n) {
         float x = 0.f;
 #pragma unroll
-        for (int c = 0; c < 8; ++c) {
-          const u32x4_t k = *reinterpret_cast<const u32x4_t*>(s_k + buf * SH_TILE + key * 256 + (((2 * c + half) ^ (key & 15)) << 4));
-          const u32x4_t y = __builtin_bit_cast(u32x4_t, q[c]);
+        for (int c = 0; c < 4; ++c) {
+          const u32x4_t k = *reinterpret_cast<const u32x4_t*>(lds.k[buf] + key * 256 + (((4 * c + r4) ^ (key & 15)) << 4));
+          const u32x4_t y = __builtin_bit_cast(u32x4_t, q[n][c]);
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
             x = fmaf(__uint_as_float(k[e] << 16), __uint_as_float(y[e] << 16), x);
             x = fmaf(__uint_as_float(k[e] & 0xffff0000u), __uint_as_float(y[e] & 0xffff0000u), x);
           }
         }
-        const float weight = exp2_(fmaf(across_sum(x), sc.c, m_run == NEG_INF ? 0.f : -m_run));
-        if (!sees(a.vis, P, j0 + key)) continue;
-        const long long r = page_row(a.pages, d.Hkv, cu.b, cu.h, j0 + key);
-        const uint32_t* vr = reinterpret_cast<const uint32_t*>((const bf16_t*)a.pages.v + r * D);
+        float weight = exp2_(fmaf(rows_sum(x), sc.c, m_run[n] == NEG_INF ? 0.f : -m_run[n]));
+        const bool sees_it = sees(a.vis, P[n], j0 + key);
 #pragma unroll
-        for (int cb = 0; cb < 4; ++cb)
+        for (int cb = 0; cb < 8; ++cb) {
+          const uint2 v = *reinterpret_cast<const uint2*>(vr + 8 * cb + 2 * r4);
+          const uint32_t two[2] = {v.x, v.y};
 #pragma unroll
-          for (int e = 0; e < 16; e += 2) {
-            const uint32_t v = vr[(32 * cb + 8 * (e / 4) + 4 * half + e % 4) / 2];
-            if ((v & 0x7f80u) == 0x7f80u) o[cb][e] = fmaf(weight, __uint_as_float(v << 16), o[cb][e]);
-            if ((v & 0x7f800000u) == 0x7f800000u) o[cb][e + 1] = fmaf(weight, __uint_as_float(v & 0xffff0000u), o[cb][e + 1]);
+          for (int e = 0; e < 4; e += 2) {
+            const uint32_t y = two[e / 2];
+            if (sees_it && (y & 0x7f80u) == 0x7f80u) o[n][cb][e] = fmaf(weight, __uint_as_float(y << 16), o[n][cb][e]);
+            if (sees_it && (y & 0x7f800000u) == 0x7f800000u) o[n][cb][e + 1] = fmaf(weight, __uint_as_float(y & 0xffff0000u), o[n][cb][e + 1]);
           }
+          __builtin_amdgcn_sched_barrier(0);
+        }
       }
     }
-    const bool last = ci + 1 == cu.run.n;
-    if (last || step + 1 == n_all) finish(piece0 == 0, last);
-    if (++ci == cu.run.n && step + 1 < n_all) {
-      RowBf16::next(d, args, cu);
-      ci = 0;
-      fresh = true;
+  };
+
+  // Steps.  A tile's place is taken by the one fetched three steps before its turn comes: the one whose products all waves had behind
+  // them at the barrier before.
+  for (;;) {
+    list_pieces();
+    if (mine.n == 0) return;
+    const int all = uniform(lds.upto[mine.n - 1]);
+    for (int t0 = 0; t0 < all; t0 += MOST) {
+      const int n = min(MOST, all - t0);
+      list_tiles(t0, n);
+      barrier();
+      int4 next = lds.tile[0];
+#pragma unroll 1
+      for (int step = -3; step < n; ++step) {
+        const int buf = step & (SH_BUFS - 1);
+        const int flags = uniform(next.w);
+        const uint32_t there0 = (uint32_t)uniform(next.x), there1 = (uint32_t)uniform(next.y);
+        const int j0 = uniform(next.z);
+        if (step >= 0) {
+          if (step + 2 < n) asm volatile("s_waitcnt vmcnt(8)" ::: "memory");
+          else if (step + 1 < n) asm volatile("s_waitcnt vmcnt(4)" ::: "memory");
+          else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+          const uint32_t rows = ((wave < 4 ? there0 : there1) >> (8 * (wave & 3))) & 0xffu;
+          if ((flags & APART) || rows != 0xffu) {
+            uint32_t odd = 0;
+#pragma unroll
+            for (int x = 0; x < 2; ++x) {
+              const bool dead = !((rows >> (4 * x + r4)) & 1);
+              u32x4_t* mine_v = reinterpret_cast<u32x4_t*>(lds.v[buf] + (8 * wave + 4 * x) * 256 + lane * 16);
+              u32x4_t v = *mine_v;
+              bool bad = false;
+#pragma unroll
+              for (int e = 0; e < 4; ++e) {
+                const uint32_t lo16 = (v[e] & 0x7f80u) == 0x7f80u ? 0x0000ffffu : 0u;
+                const uint32_t hi16 = (v[e] & 0x7f800000u) == 0x7f800000u ? 0xffff0000u : 0u;
+                bad = bad || ((flags & APART) && (lo16 | hi16) != 0);
+                v[e] = dead ? 0u : (flags & APART) ? v[e] & ~(lo16 | hi16) : v[e];
+              }
+              if (dead || bad) *mine_v = v;
+              const unsigned long long who = __ballot(bad && !dead);
+#pragma unroll
+              for (int r = 0; r < 4; ++r) odd |= ((who >> (16 * r)) & 0xffffu) != 0 ? 1u << (4 * x + r) : 0u;
+            }
+            if (lane == 0) lds.odd[buf][wave] = (unsigned char)odd;
+          }
+          barrier();
+        }
+        fetch(step + 3, n);
+        if (step < 0) continue;
+        if (step + 1 < n) next = lds.tile[step + 1];
+        if (flags & FIRST) begin(flags >> NUMBER);
+        if (flags & QUERIES) {
+          if (wave_live && (col0 >> 7) == j0) take_queries(lds.k[buf], SH_BUFS * SH_TILE);
+          continue;
+        }
+        if (wave_live && (there0 | there1) != 0) {
+          const uint64_t there = (uint64_t)there1 << 32 | there0;
+#pragma unroll 1
+          for (int key = key0; key < SH_KEYS; key += 32) {      // (64 tokens at once take more registers than there are)
+            work(buf, key, j0, flags, there);
+            if (shares == 2) break;
+          }
+          if (flags & APART) add_odd(buf, j0);
+        }
+        if (flags & LAST) finish(buf);
+      }
+      barrier();                                // (the lists and all tiles are used up)
     }
+    if (mine.upto >= mine.end) return;
   }
 }
 
@@ -388,27 +558,41 @@ __device__ __forceinline__ bool finite(float x) { return (__float_as_uint(x) & 0
 __global__ __launch_bounds__(64 * SF_WAVES) void shared_f32_kernel(DevDesc d, SharedArgs args, SharedOut so) {
   __shared__ __align__(16) float s_o[SF_WAVES][16][D + 4];
   __shared__ float s_m[SF_WAVES][16], s_l[SF_WAVES][16];
+  __shared__ __align__(16) Piece s_list[PIECES];
+  __shared__ __align__(16) int4 s_share;
   const PagedArgs& a = args.a;
   const int lane = threadIdx.x & 63, wave = uniform((int)(threadIdx.x >> 6)), wg = blockIdx.x;
   const int r = lane >> 4, col = lane & 15;
   const int gs = __builtin_ctz(d.G);
   const float NEG_INF = -__builtin_inff(), scale2 = d.scale * LOG2E;
-  const int total = RowF32::all(d, args);
-  const int per = uniform((int)(((unsigned)total + gridDim.x - 1) / gridDim.x));
-  if ((long long)wg * per >= total) return;
-  int left = min(per, total - wg * per), i0;
-  Unit u = RowF32::find(d, args, wg * per, i0);
+  Share mine = {0, 0, 0, 0};
+  int now = 0;
   const float* kp = (const float*)a.pages.k;
   const float* vp = (const float*)a.pages.v;
-  while (left > 0) {
-    const int i1 = min(u.run.n, i0 + left);
-    left -= i1 - i0;
+  for (bool begun = false;; ++now) {
+    if (now == mine.n) {                                // the next list, or the first
+      if (begun && mine.upto >= mine.end) return;
+      if (wave == 0) {
+        RowF32::list(d, args, mine, s_list);
+        if (lane == 0) s_share = make_int4(mine.at, mine.upto, mine.end, mine.n);
+      }
+      __syncthreads();
+      mine = Share{uniform(s_share.x), uniform(s_share.y), uniform(s_share.z), uniform(s_share.w)};
+      begun = true;
+      now = 0;
+      if (mine.n == 0) return;
+    }
+    const Piece u = listed_piece(s_list + now);
+    if (u.i0 >= u.i1) continue;
+    const Run run = run_of_piece(u);
+    const bool own = (u.bits & PIECE_OWN) != 0;
+    const int i0 = u.i0, i1 = u.i1;
     const int m = u.ct * SF_COLS + col;                 // this lane's column
     const bool live = m < u.cols;
     const int row_q = u.row0 + (live ? m >> gs : 0);
-    int P = !live ? -1 : u.own ? u.lo + (m >> gs) : 0x7fffffff;
-    if (!u.own && a.vis.window > 0) {
-      const int at = position_in_group(d, args, u, row_q);
+    int P = !live ? -1 : own ? u.lo + (m >> gs) : 0x7fffffff;
+    if (!own && a.vis.window > 0) {
+      const int at = position_in_group(d, args, u.g, row_q);
       P = live ? at : -1;
     }
     f32x4_t q[8], o[8];
@@ -418,7 +602,7 @@ __global__ __launch_bounds__(64 * SF_WAVES) void shared_f32_kernel(DevDesc d, Sh
     float m_run = NEG_INF, l_run = 0.f;
 
     auto row_of = [&](int i) {                          // of token lane mod 16 of this wave's part of tile i, -1: no column may see it
-      const int j = run_token<SF_KEYS>(u.run, i) + 16 * wave + col;
+      const int j = run_token<SF_KEYS>(run, i) + 16 * wave + col;
       return j >= u.from && j < u.lim ? page_row(a.pages, d.Hkv, u.b, u.h, j) : -1ll;
     };
     f32x4_t k[8], v[4][2];
@@ -435,14 +619,18 @@ __global__ __launch_bounds__(64 * SF_WAVES) void shared_f32_kernel(DevDesc d, Sh
     load_v(row);
     if (i0 + 1 < i1) row_next = row_of(i0 + 1);
     for (int i = i0; i < i1; ++i) {
-      const int j0 = run_token<SF_KEYS>(u.run, i) + 16 * wave;
+      const int j0 = run_token<SF_KEYS>(run, i) + 16 * wave;
       const bool more = i + 1 < i1;
       const unsigned long long there = __ballot(row >= 0) & 0xffffu;
-      f32x4_t s = {0.f, 0.f, 0.f, 0.f};
+      // (four sums of 32 channels each: a chain of 128 products loses twice the bits)
+      f32x4_t s4[4];
+#pragma unroll
+      for (int y = 0; y < 4; ++y) s4[y] = f32x4_t{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
       for (int c = 0; c < 8; ++c)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) s = __builtin_amdgcn_mfma_f32_16x16x4f32(k[c][e], q[c][e], s, 0, 0, 0);
+        for (int e = 0; e < 4; ++e) s4[e] = __builtin_amdgcn_mfma_f32_16x16x4f32(k[c][e], q[c][e], s4[e], 0, 0, 0);
+      f32x4_t s = (s4[0] + s4[1]) + (s4[2] + s4[3]);
       if (more) load_quarter(kp + max(row_next, 0ll) * D, r, k);
       uint32_t seen = 0;
       bool odd = false;
@@ -526,10 +714,10 @@ __global__ __launch_bounds__(64 * SF_WAVES) void shared_f32_kernel(DevDesc d, Sh
       *reinterpret_cast<float4*>(to + 4) = make_float4(o[4][x], o[5][x], o[6][x], o[7][x]);
     }
     __syncthreads();
-    const int c0 = RowF32::place(d, a.n_rows, u.own, u.row0, u.cols, u.ct, u.h);
-    if (threadIdx.x == 0 && u.ct * SF_COLS < u.cols) {
-      if (i0 == 0) so.span[2 * (size_t)c0] = wg;
-      if (i1 == u.run.n) so.span[2 * (size_t)c0 + 1] = wg;
+    const int c0 = RowF32::place(d, a.n_rows, own, u.row0, u.cols, u.ct, u.h);
+    if (threadIdx.x == 0) {
+      if (u.bits & PIECE_FIRST) so.span[2 * (size_t)c0] = wg;
+      if (u.bits & PIECE_LAST) so.span[2 * (size_t)c0 + 1] = wg;
     }
     const int c = threadIdx.x >> 4, ch = 8 * (threadIdx.x & 15);
     if (u.ct * SF_COLS + c < u.cols) {
@@ -551,8 +739,6 @@ __global__ __launch_bounds__(64 * SF_WAVES) void shared_f32_kernel(DevDesc d, Sh
       if (ch == 0) *reinterpret_cast<float2*>(so.part_ml + 2 * slot) = make_float2(mx, l);
     }
     __syncthreads();
-    i0 = 0;
-    if (left > 0) RowF32::next(d, args, u);
   }
 }
 
@@ -634,10 +820,10 @@ struct SharedPlan {
   size_t off_ml, off_span, off_lse, off_scores, total;
 };
 
-// the most tiles of columns and tokens that there can be
+// the longest row that there can be
 long long most_tiles(const DevDesc& d, long long n_rows, long long cap, int cols, int keys) {
   const long long col_tiles = 2 * ((n_rows * d.G + cols - 1) / cols + d.B);
-  return col_tiles * d.Hkv * ((cap + keys - 1) / keys + 2);
+  return col_tiles * d.Hkv * (RowBf16::MOST_WEIGHT * ((cap + keys - 1) / keys + 2) + RowBf16::COST);
 }
 
 SharedPlan shared_plan(const DevDesc& d, int dtype, long long n_rows, long long cap, long long n_cap) {
@@ -708,8 +894,7 @@ hipError_t launch_attend_shared(const DevDesc& d, int dtype, const SharedArgs& g
   }
   e = raise_lds([] {
     hipError_t bad = hipSuccess;
-    for (const void* f : {(const void*)shared_bf16_kernel<IN_ONE_PAGE>, (const void*)shared_bf16_kernel<EIGHT_A_PAGE>,
-                          (const void*)shared_bf16_kernel<ANYWHERE>}) {
+    for (const void* f : {(const void*)shared_bf16_kernel<EIGHT_A_PAGE>, (const void*)shared_bf16_kernel<ANYWHERE>}) {
       const hipError_t x = hipFuncSetAttribute(f, hipFuncAttributeMaxDynamicSharedMemorySize, SH_LDS);
       if (x != hipSuccess) bad = x;
     }
@@ -719,8 +904,7 @@ hipError_t launch_attend_shared(const DevDesc& d, int dtype, const SharedArgs& g
   auto launch = [&](auto rows) {
     hipLaunchKernelGGL((shared_bf16_kernel<decltype(rows)::value>), dim3(p.wgs), dim3(64 * SH_WAVES), SH_LDS, st, d, s, so);
   };
-  if (a.pages.table == nullptr || a.pages.page_size % SH_KEYS == 0) launch(std::integral_constant<int, IN_ONE_PAGE>{});
-  else if (a.pages.page_size % 8 == 0) launch(std::integral_constant<int, EIGHT_A_PAGE>{});
+  if (a.pages.page_size % 8 == 0) launch(std::integral_constant<int, EIGHT_A_PAGE>{});
   else launch(std::integral_constant<int, ANYWHERE>{});
   e = hipGetLastError();
   if (e != hipSuccess) return e;

@@ -4,7 +4,9 @@
 // heads); what a sequence has behind them is its own.  A *unit* is a kv head and a tile of COLS columns, of a group over the
 // tokens in common or of a sequence over its own.  A unit's tokens are a run of tiles of KEYS tokens; all units' tiles stand in
 // one row (groups first; of a group or a sequence tile of columns after tile of columns, head after head), and each workgroup
-// takes the same number of neighbours in it, whatever the lengths, which only the device knows.
+// takes the same share of it, whatever the lengths, which only the device knows.  The row is measured in what the work costs: a
+// unit's start and end count as a tile, and a tile of many columns, which the matrix units take longer for than the memory, as one
+// and a half (in halves of a tile: COST and weight).
 //
 // A workgroup's piece of a unit leaves its columns' maximum, sum and sum of p v in the workspace, columns COLS w + c .. of it
 // (w: the workgroup, c: columns of the units before): going along the row each next piece raises w by one or c by the columns
@@ -69,20 +71,33 @@ __host__ __device__ __forceinline__ Member member_at(const SharedArgs& s, int b,
   return r;
 }
 
-struct Unit {
-  bool own;
-  int id;                           // sequence, or group
-  int g;                            // own: the first group that ends behind the sequence
+// A piece of a unit, as a workgroup lists those that it has: tiles i0 .. i1-1 of its run.
+struct Piece {
+  int bits;                         // OWN: of a sequence; FIRST, LAST: it has the unit's first tile, its last
+  int g;                            // the group (of a sequence: not looked at)
   int ct, h;                        // tile of columns, kv head
   int b;                            // whose table is read
   int row0, cols;                   // first row and all columns of the group or sequence
   int from, lim;                    // its tokens are from .. lim-1
-  int lo, hi;                       // own: positions of the first and the last row
-  Run run;
+  int lo, hi;                       // OWN: positions of the first and the last row
+  int ahead0, ahead, start;         // the run
+  int i0, i1;
+};
+enum { PIECE_OWN = 1, PIECE_FIRST = 2, PIECE_LAST = 4 };
+constexpr int PIECES = 64, PIECE_WORDS = sizeof(Piece) / 4;      // a list's length at most
+static_assert(PIECE_WORDS == 16);
+
+// A workgroup's part of the row: at .. end-1, of which the list has what lies before `upto`, in n pieces.  Pieces without a tile
+// are among them.
+struct Share {
+  int at, upto, end, n;
 };
 
 template <int COLS, int KEYS>
 struct WorkRow {
+  static constexpr int COST = 2, MOST_WEIGHT = 3;
+  __host__ __device__ static __forceinline__ int weight(int cols) { return cols > COLS / 2 && COLS > 64 ? 3 : 2; }
+
   __host__ __device__ static __forceinline__ int col_tiles(int rows, int G) { return (int)(((long long)rows * G + COLS - 1) / COLS); }
   __host__ __device__ static __forceinline__ Run group_run(const SharedArgs& s, const Group& g) {
     return g.common > 0 && g.rows > 0 ? run_of<KEYS>(s.a.vis, 0, g.common, g.common - 1) : Run{0, 0, 0, 0};
@@ -90,91 +105,92 @@ struct WorkRow {
   __host__ __device__ static __forceinline__ Run member_run(const SharedArgs& s, const Member& m) {
     return m.span.n > 0 ? run_of<KEYS>(s.a.vis, m.from, m.n - m.span.n, m.n - 1) : Run{0, 0, 0, 0};
   }
-
-  // ---- a unit and the one behind it (the same for a wave) ----
-  // (from here on units whose run is empty are left out; there is one, as the caller knows)
-  __host__ __device__ static __forceinline__ bool set_group(const DevDesc& d, const SharedArgs& s, Unit& u, int g) {
-    const Group x = group_at(s, d.B, g);
-    u.run = group_run(s, x);
-    if (u.run.n == 0) return false;
-    u.own = false;
-    u.id = u.g = g;
-    u.row0 = x.row0;
-    u.cols = x.rows * d.G;
-    u.from = 0;
-    u.lim = x.common;
-    u.lo = u.hi = 0;
-    u.b = x.b0;                     // the first that has the tokens
-    for (int b = x.b0; b < x.b1; ++b)
-      if (member_at(s, b, x.common).from > 0) {
-        u.b = b;
-        break;
-      }
-    return true;
-  }
-  __host__ __device__ static __forceinline__ bool set_member(const DevDesc& d, const SharedArgs& s, Unit& u, int b, int g) {
-    int common = 0;
-    for (; g < s.n_groups; ++g) {
-      const Group x = group_at(s, d.B, g);
-      if (b < x.b1) {
-        if (b >= x.b0) common = x.common;
-        break;
-      }
-    }
-    const Member m = member_at(s, b, common);
-    u.g = g;
-    u.run = member_run(s, m);
-    if (u.run.n == 0) return false;
-    u.own = true;
-    u.id = u.b = b;
-    u.row0 = m.span.first;
-    u.cols = m.span.n * d.G;
-    u.from = m.from;
-    u.lim = m.n;
-    u.lo = m.n - m.span.n;
-    u.hi = m.n - 1;
-    return true;
-  }
-  __host__ __device__ static __forceinline__ void next(const DevDesc& d, const SharedArgs& s, Unit& u) {
-    if (++u.h < d.Hkv) return;
-    u.h = 0;
-    if (++u.ct * COLS < u.cols) return;
-    u.ct = 0;
-    int b = u.own ? u.id + 1 : 0, g = u.g;
-    if (!u.own) {
-      while (++g < s.n_groups)
-        if (set_group(d, s, u, g)) return;
-      g = 0;
-    }
-    for (; b < d.B; ++b) {
-      if (set_member(d, s, u, b, g)) return;
-      g = u.g;
-    }
-    nothing(u);
-  }
-  // a unit without columns: behind the last, which a row that counts otherwise than its lists say (starts that fall) may lead to
-  __host__ __device__ static __forceinline__ void nothing(Unit& u) {
-    u.own = true;
-    u.id = 0x3fffffff;
-    u.b = u.row0 = u.cols = u.from = u.lo = u.hi = 0;
-    u.lim = 1;
-    u.run = Run{0, 0, 0, 1};
-  }
-  // columns of the units before it
+  // columns of the units before one
   __host__ __device__ static __forceinline__ int place(const DevDesc& d, int n_rows, bool own, int row0, int cols, int ct, int h) {
     const int mine = cols - ct * COLS < COLS ? cols - ct * COLS : COLS;
     return ((own ? n_rows : 0) + row0) * d.Hq + ct * COLS * d.Hkv + h * mine;
   }
 
-  // ---- the row (all lanes of a wave call) ----
-  // tiles of a head of sequence b0 + lane, and the first group that ends behind it; g0: the first group that may hold one of
-  // the 64, kept from call to call
-  struct Tiles {
-    int n, g;
+  // A group or a sequence in the row: what its units have in common.
+  struct Entry {
+    int own, id;                    // of a sequence, its number; or the group's
+    int row0, cols, from, lim, lo;
+    Run run;
+    int units, weight;
   };
-  __device__ static __forceinline__ Tiles members_tiles(const DevDesc& d, const SharedArgs& s, int b0, int& g0) {
+  __host__ __device__ static __forceinline__ int unit_length(const Entry& e) { return e.run.n * e.weight + COST; }
+  __host__ __device__ static __forceinline__ Entry no_entry() { return Entry{1, 0, 0, 0, 0, 1, 0, Run{0, 0, 0, 0}, 0, 1}; }
+  __host__ __device__ static __forceinline__ Entry group_entry(const DevDesc& d, const SharedArgs& s, int g) {
+    const Group x = group_at(s, d.B, g);
+    Entry e;
+    e.own = 0;
+    e.id = g;
+    e.row0 = x.row0;
+    e.cols = x.rows * d.G;
+    e.from = 0;
+    e.lim = x.common;
+    e.lo = 0;
+    e.run = group_run(s, x);
+    e.units = e.run.n > 0 ? col_tiles(x.rows, d.G) * d.Hkv : 0;
+    e.weight = weight(e.cols);
+    return e;
+  }
+  __host__ __device__ static __forceinline__ Entry member_entry(const DevDesc& d, const SharedArgs& s, int b, int common) {
+    const Member m = member_at(s, b, common);
+    Entry e;
+    e.own = 1;
+    e.id = b;
+    e.row0 = m.span.first;
+    e.cols = m.span.n * d.G;
+    e.from = m.from;
+    e.lim = m.n;
+    e.lo = m.n - m.span.n;
+    e.run = member_run(s, m);
+    e.units = e.run.n > 0 ? col_tiles(m.span.n, d.G) * d.Hkv : 0;
+    e.weight = weight(e.cols);
+    return e;
+  }
+  // The piece of unit `unit` (of the entry's), which begins at `first` in the row, that lies within at .. end-1.
+  __host__ __device__ static __forceinline__ Piece piece_of(const DevDesc& d, const SharedArgs& s, const Entry& e, int unit, int first, int at, int end) {
+    // a tile is the workgroup's in whose part of the row it begins
+    auto tile = [&](int x) {
+      const int t = x - first - COST;
+      return t <= 0 ? 0 : (t + e.weight - 1) / e.weight < e.run.n ? (t + e.weight - 1) / e.weight : e.run.n;
+    };
+    Piece p;
+    p.i0 = tile(at);
+    p.i1 = tile(end);
+    p.bits = (e.own ? PIECE_OWN : 0) | (p.i0 == 0 ? PIECE_FIRST : 0) | (p.i1 == e.run.n ? PIECE_LAST : 0);
+    p.g = p.b = e.id;
+    if (!e.own) {                   // the table of the first sequence that has the tokens
+      const Group x = group_at(s, d.B, e.id);
+      p.b = x.b0;
+      for (int b = x.b0; b < x.b1; ++b)
+        if (member_at(s, b, x.common).from > 0) {
+          p.b = b;
+          break;
+        }
+    }
+    p.ct = unit / d.Hkv;
+    p.h = unit - p.ct * d.Hkv;
+    p.row0 = e.row0;
+    p.cols = e.cols;
+    p.from = e.from;
+    p.lim = e.lim;
+    p.lo = e.lo;
+    p.hi = e.lim - 1;
+    p.ahead0 = e.run.ahead0;
+    p.ahead = e.run.ahead;
+    p.start = e.run.start;
+    return p;
+  }
+
+  // ---- the row, 64 entries at a time, one a lane (all lanes of a wave call) ----
+  // how many tokens sequence b0 + lane's group has in common; g0: the first group that may hold one of the 64, kept from call to
+  // call
+  __device__ static __forceinline__ int commons(const DevDesc& d, const SharedArgs& s, int b0, int& g0) {
     const int lane = threadIdx.x & 63, b = b0 + lane;
-    int common = 0, last = g0, mine = g0;
+    int common = 0, last = g0;
     for (int g = g0; g < s.n_groups; g += 64) {
       Group x = {d.B, d.B, 0, 0, 0};
       if (g + lane < s.n_groups) x = group_at(s, d.B, g + lane);
@@ -182,64 +198,85 @@ struct WorkRow {
       for (int i = 0; i < n; ++i) {
         const int lo = __builtin_amdgcn_readlane(x.b0, i), hi = __builtin_amdgcn_readlane(x.b1, i);
         const int c = __builtin_amdgcn_readlane(x.common, i);
-        if (b >= hi) mine = g + i + 1;
-        else if (b >= lo) common = c;
+        if (b >= lo && b < hi) common = c;
       }
       if (n > 0) last = g + n - 1;
       if (n < 64) break;
     }
     g0 = uniform(last);
-    if (b >= d.B) return {0, mine};
-    const Member m = member_at(s, b, common);
-    return {member_run(s, m).n * col_tiles(m.span.n, d.G), mine};
+    return common;
   }
-  __device__ static __forceinline__ int group_tiles(const DevDesc& d, const SharedArgs& s, int g) {
-    if (g >= s.n_groups) return 0;
-    const Group x = group_at(s, d.B, g);
-    return group_run(s, x).n * col_tiles(x.rows, d.G);
-  }
-  // (the host has made sure that all tiles there can be fit 31 bits)
-  __device__ static __forceinline__ int all(const DevDesc& d, const SharedArgs& s) {
+  // The workgroup's part of the row (r.end = 0 asks for it), and the pieces of its next ones, as many as the list holds.  (The host has
+  // made sure that the row's length fits 31 bits.)
+  __device__ static __forceinline__ void list(const DevDesc& d, const SharedArgs& s, Share& r, Piece* to) {
     const int lane = threadIdx.x & 63;
-    int sum = 0;
-    for (int g = 0; g < s.n_groups; g += 64) sum += group_tiles(d, s, g + lane);
-    for (int b = 0, g = 0; b < d.B; b += 64) sum += members_tiles(d, s, b, g).n;
-    return __builtin_amdgcn_readlane(lanes_upto(sum), 63) * d.Hkv;
-  }
-  // the unit that tile `at` (< all) of the row belongs to, and which of its tiles that is
-  __device__ static __forceinline__ Unit find(const DevDesc& d, const SharedArgs& s, int at, int& tile) {
-    const int lane = threadIdx.x & 63;
-    int base = 0, own = 0, id = 0, off = 0, g = 0;
-    auto search = [&](int mine, int first) {
-      const int upto = lanes_upto(mine);
-      const unsigned long long past = __ballot(at < (base + upto) * d.Hkv);
-      if (past != 0) {
-        const int l = __ffsll(past) - 1;
-        id = first + l;
-        off = at - (base + __builtin_amdgcn_readlane(upto - mine, l)) * d.Hkv;
+    const int of_groups = (s.n_groups + 63) >> 6, chunks = of_groups + ((d.B + 63) >> 6);
+    for (int pass = r.end == 0 ? 0 : 1; pass < 2; ++pass) {
+      int base = 0, have = 0, g0 = 0;
+      for (int c = 0; c < chunks; ++c) {
+        Entry e = no_entry();
+        if (c < of_groups) {
+          if (64 * c + lane < s.n_groups) e = group_entry(d, s, 64 * c + lane);
+        } else {
+          const int b0 = 64 * (c - of_groups), common = commons(d, s, b0, g0);
+          if (b0 + lane < d.B) e = member_entry(d, s, b0 + lane, common);
+        }
+        const int length = unit_length(e) * e.units, upto = lanes_upto(length);
+        const int here = __builtin_amdgcn_readlane(upto, 63);
+        if (pass == 0 || base + here <= r.upto) {
+          base += here;
+          continue;
+        }
+        // the unit that r.upto lies in, among the chunk's
+        const int units_upto = lanes_upto(e.units), units_here = __builtin_amdgcn_readlane(units_upto, 63), off = r.upto - base;
+        const int l0 = uniform((int)__ffsll(__ballot(off < upto)) - 1);
+        const int u = __builtin_amdgcn_readlane(units_upto - e.units, l0) +
+                      uniform((off - __builtin_amdgcn_readlane(upto - length, l0)) / __builtin_amdgcn_readlane(unit_length(e), l0)) + lane - have;
+        // each lane behind those that have a piece takes the next unit: it is the entry's whose units end behind it
+        int l = 0;
+#pragma unroll 1
+        for (int k = 32; k > 0; k >>= 1)
+          if (__shfl(units_upto, l + k - 1) <= u) l += k;
+        Entry x;
+        x.own = __shfl(e.own, l);
+        x.id = __shfl(e.id, l);
+        x.row0 = __shfl(e.row0, l);
+        x.cols = __shfl(e.cols, l);
+        x.from = __shfl(e.from, l);
+        x.lim = __shfl(e.lim, l);
+        x.lo = __shfl(e.lo, l);
+        x.run.ahead0 = __shfl(e.run.ahead0, l);
+        x.run.ahead = __shfl(e.run.ahead, l);
+        x.run.start = __shfl(e.run.start, l);
+        x.run.n = __shfl(e.run.n, l);
+        x.weight = __shfl(e.weight, l);
+        const int unit = u - __shfl(units_upto - e.units, l);
+        const int first = base + __shfl(upto - length, l) + unit * unit_length(x);
+        const bool mine = lane >= have && u < units_here && first < r.end;
+        int last = r.upto;
+        if (mine) {
+          to[lane] = piece_of(d, s, x, unit, first, r.upto, r.end);
+          last = min(first + unit_length(x), r.end);
+        }
+        have += __popcll(__ballot(mine));
+        r.upto = __builtin_amdgcn_readlane(last, max(have - 1, 0));
+        base += here;
+        if (have == PIECES || r.upto >= r.end) break;
       }
-      base += __builtin_amdgcn_readlane(upto, 63);
-      return past != 0;
-    };
-    bool found = false;
-    for (int i = 0; i < s.n_groups && !found; i += 64) found = search(group_tiles(d, s, i + lane), i);
-    if (!found) {
-      own = 1;
-      for (int b = 0, gg = 0; b < d.B && !found; b += 64) {
-        const Tiles t = members_tiles(d, s, b, gg);
-        found = search(t.n, b);
-        if (found) g = __builtin_amdgcn_readlane(t.g, uniform(id) & 63);
+      if (pass == 0) {
+        // (no less than a tile of the heaviest: of a unit's workgroups each has a tile, as who joins their pieces relies on)
+        const int per = max(MOST_WEIGHT, uniform((int)(((unsigned)base + gridDim.x - 1) / gridDim.x)));
+        const long long at = (long long)blockIdx.x * per;
+        if (at >= base) {
+          r = Share{0, 0, 0, 0};
+          return;
+        }
+        r.at = r.upto = (int)at;
+        r.end = min(per, base - r.at) + r.at;
+      } else {
+        r.n = uniform(have);
       }
     }
-    id = uniform(id);
-    Unit u;
-    u.ct = u.h = 0;
-    if (!(own ? set_member(d, s, u, id, uniform(g)) : set_group(d, s, u, id))) nothing(u);
-    const int unit = uniform(uniform(off) / u.run.n);
-    tile = uniform(off) - unit * u.run.n;
-    u.ct = uniform(unit / d.Hkv);
-    u.h = unit - u.ct * d.Hkv;
-    return u;
   }
 };
 
