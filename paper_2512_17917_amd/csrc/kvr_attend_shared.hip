@@ -820,10 +820,11 @@ struct SharedPlan {
   size_t off_ml, off_span, off_lse, off_scores, total;
 };
 
-// the longest row that there can be
+// the longest row that there can be (the scores' rows have tiles of more columns and heavier ones)
+constexpr int MOST_WEIGHT = 3, MOST_COST = 6;
 long long most_tiles(const DevDesc& d, long long n_rows, long long cap, int cols, int keys) {
   const long long col_tiles = 2 * ((n_rows * d.G + cols - 1) / cols + d.B);
-  return col_tiles * d.Hkv * (RowBf16::MOST_WEIGHT * ((cap + keys - 1) / keys + 2) + RowBf16::COST);
+  return col_tiles * d.Hkv * (MOST_WEIGHT * ((cap + keys - 1) / keys + 2) + MOST_COST);
 }
 
 SharedPlan shared_plan(const DevDesc& d, int dtype, long long n_rows, long long cap, long long n_cap) {
@@ -842,20 +843,6 @@ SharedPlan shared_plan(const DevDesc& d, int dtype, long long n_rows, long long 
   if (n_cap > 0 && !f32) p.scores = prompt_scores_plan(d, n_rows, n_cap < cap ? n_cap : cap);
   p.total = p.off_scores + p.scores.bytes;
   return p;
-}
-
-template <typename F>
-hipError_t raise_lds(F kernels) {
-  // a launch may ask for more than 64 KB of LDS where the kernel's limit was raised, on each device for itself
-  constexpr int DEVICES = 64;
-  static std::once_flag once[DEVICES];
-  static hipError_t raised[DEVICES];
-  int dev = 0;
-  const hipError_t e = hipGetDevice(&dev);
-  if (e != hipSuccess) return e;
-  if (dev < 0 || dev >= DEVICES) return hipErrorInvalidDevice;
-  std::call_once(once[dev], [&] { raised[dev] = kernels(); });
-  return raised[dev];
 }
 
 }  // namespace
@@ -878,7 +865,8 @@ hipError_t launch_attend_shared(const DevDesc& d, int dtype, const SharedArgs& g
   so.part_ml = (float*)(base + p.off_ml);
   so.span = (int*)(base + p.off_span);
   so.lse = a.scores ? (float*)(base + p.off_lse) : nullptr;
-  so.work = a.scores && dtype == KVR_BF16 ? (ScoresWork*)(base + p.off_scores) : nullptr;
+  const bool single = a.q_start == nullptr;                     // one new token per sequence: a pass of its own for its scores
+  so.work = a.scores && !single && dtype == KVR_BF16 ? (ScoresWork*)(base + p.off_scores) : nullptr;
   so.keys = p.scores.keys;
   so.most_scores_splits = p.scores.most_splits;
   so.scores_wgs = p.scores.wgs;
@@ -890,27 +878,22 @@ hipError_t launch_attend_shared(const DevDesc& d, int dtype, const SharedArgs& g
     if (e != hipSuccess) return e;
     hipLaunchKernelGGL((shared_join_kernel<float, SF_COLS, SF_KEYS>), join, dim3(256), 0, st, d, s, so);
     e = hipGetLastError();
-    return e != hipSuccess || !a.scores ? e : launch_prompt_scores_f32(d, a, so.lse, st);
+    if (e != hipSuccess || !a.scores) return e;
+    return single ? launch_shared_scores(d, dtype, s, so.lse, st) : launch_prompt_scores_f32(d, a, so.lse, st);
   }
-  e = raise_lds([] {
-    hipError_t bad = hipSuccess;
-    for (const void* f : {(const void*)shared_bf16_kernel<EIGHT_A_PAGE>, (const void*)shared_bf16_kernel<ANYWHERE>}) {
-      const hipError_t x = hipFuncSetAttribute(f, hipFuncAttributeMaxDynamicSharedMemorySize, SH_LDS);
-      if (x != hipSuccess) bad = x;
-    }
-    return bad;
-  });
-  if (e != hipSuccess) return e;
   auto launch = [&](auto rows) {
-    hipLaunchKernelGGL((shared_bf16_kernel<decltype(rows)::value>), dim3(p.wgs), dim3(64 * SH_WAVES), SH_LDS, st, d, s, so);
+    constexpr int ROWS = decltype(rows)::value;
+    const hipError_t x = raise_lds_limit((const void*)shared_bf16_kernel<ROWS>, SH_LDS);
+    if (x != hipSuccess) return x;
+    hipLaunchKernelGGL((shared_bf16_kernel<ROWS>), dim3(p.wgs), dim3(64 * SH_WAVES), SH_LDS, st, d, s, so);
+    return hipGetLastError();
   };
-  if (a.pages.page_size % 8 == 0) launch(std::integral_constant<int, EIGHT_A_PAGE>{});
-  else launch(std::integral_constant<int, ANYWHERE>{});
-  e = hipGetLastError();
+  e = a.pages.page_size % 8 == 0 ? launch(std::integral_constant<int, EIGHT_A_PAGE>{}) : launch(std::integral_constant<int, ANYWHERE>{});
   if (e != hipSuccess) return e;
   hipLaunchKernelGGL((shared_join_kernel<bf16_t, SH_COLS, SH_KEYS>), join, dim3(256), 0, st, d, s, so);
   e = hipGetLastError();
-  return e != hipSuccess || !a.scores ? e : launch_prompt_scores_bf16(d, a, p.scores, so.lse, base + p.off_scores, st);
+  if (e != hipSuccess || !a.scores) return e;
+  return single ? launch_shared_scores(d, dtype, s, so.lse, st) : launch_prompt_scores_bf16(d, a, p.scores, so.lse, base + p.off_scores, st);
 }
 
 }  // namespace kvr

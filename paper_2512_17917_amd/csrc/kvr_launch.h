@@ -314,6 +314,8 @@ struct SharedArgs {
   int n_groups;
   int least;                        // fewer tokens in common than this are not worth a pass of their own
 };
+// (one new token per sequence)
+hipError_t launch_shared_scores(const DevDesc& d, int dtype, const SharedArgs& s, const float* lse, hipStream_t st);
 // false: more tiles of columns and tokens than the kernels count
 bool attend_shared_fits(const DevDesc& d, long long n_rows, long long cap);
 size_t attend_shared_ws(const DevDesc& d, int dtype, long long n_rows, long long cap, bool scores);

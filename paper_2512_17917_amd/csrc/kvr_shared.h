@@ -93,10 +93,14 @@ struct Share {
   int at, upto, end, n;
 };
 
-template <int COLS, int KEYS>
+// SCORES: the row of the pass that adds scores, which takes longer with every column
+template <int COLS, int KEYS, bool SCORES = false>
 struct WorkRow {
-  static constexpr int COST = 2, MOST_WEIGHT = 3;
-  __host__ __device__ static __forceinline__ int weight(int cols) { return cols > COLS / 2 && COLS > 64 ? 3 : 2; }
+  static constexpr int COST = SCORES ? 6 : 2, MOST_WEIGHT = SCORES ? 2 + COLS / 16 : 3;
+  __host__ __device__ static __forceinline__ int weight(int cols) {
+    if (SCORES) return 2 + (cols < COLS ? cols : COLS) / 16;
+    return cols > COLS / 2 && COLS > 64 ? 3 : 2;
+  }
 
   __host__ __device__ static __forceinline__ int col_tiles(int rows, int G) { return (int)(((long long)rows * G + COLS - 1) / COLS); }
   __host__ __device__ static __forceinline__ Run group_run(const SharedArgs& s, const Group& g) {
@@ -279,6 +283,25 @@ struct WorkRow {
     }
   }
 };
+
+// A kernel may be launched with more than 64 KB of LDS where its limit was raised, on each device for itself.
+inline hipError_t raise_lds_limit(const void* kernel, int bytes) {
+  constexpr int DEVICES = 64, KERNELS = 16;
+  static std::mutex lock;
+  static const void* known[DEVICES][KERNELS];
+  int dev = 0;
+  hipError_t e = hipGetDevice(&dev);
+  if (e != hipSuccess) return e;
+  if (dev < 0 || dev >= DEVICES) return hipErrorInvalidDevice;
+  const std::lock_guard<std::mutex> held(lock);
+  int i = 0;
+  while (i < KERNELS && known[dev][i] != nullptr && known[dev][i] != kernel) ++i;
+  if (i == KERNELS) return hipErrorInvalidValue;
+  if (known[dev][i] == kernel) return hipSuccess;
+  e = hipFuncSetAttribute(kernel, hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
+  if (e == hipSuccess) known[dev][i] = kernel;
+  return e;
+}
 
 // the group that sequence b is in, -1 if in none (wave-uniform b; all lanes call)
 __device__ __forceinline__ int group_of_seq(const SharedArgs& s, int B, int b) {
