@@ -193,9 +193,19 @@ __global__ __launch_bounds__(64 * SH_WAVES, 2) void shared_bf16_kernel(DevDesc d
   // columns' queries.
   const uint32_t lds0 = lds_offset(s_mem);
   const uint32_t k_in = (col ^ ((8 * wave + r4) & 15)) << 4, v_in = (col ^ (4 * r4)) << 4;
+  int f_flags, f_row[2];                        // of the tile that is fetched next, as LDS has them
+  auto ask = [&](int t) {
+    f_flags = lds.tile[t].w;
+    if constexpr (ROWS == EIGHT_A_PAGE) {
+      f_row[0] = lds.row[8 * t + wave];
+    } else {
+      f_row[0] = lds.row[SH_KEYS * t + 8 * wave + r4];
+      f_row[1] = lds.row[SH_KEYS * t + 8 * wave + 4 + r4];
+    }
+  };
   auto fetch = [&](int t, int n) {
     if (t >= n) return;
-    const int flags = uniform(lds.tile[t].w);
+    const int flags = uniform(f_flags);
     const uint32_t to = lds0 + (t & (SH_BUFS - 1)) * SH_TILE + 8 * wave * 256;
     if (flags & (FIRST | QUERIES)) {
       const int now = flags >> NUMBER;
@@ -215,7 +225,7 @@ __global__ __launch_bounds__(64 * SH_WAVES, 2) void shared_bf16_kernel(DevDesc d
       if (!few) return;
     }
     if constexpr (ROWS == EIGHT_A_PAGE) {
-      const uint32_t row = (uint32_t)uniform(lds.row[8 * t + wave]);
+      const uint32_t row = (uint32_t)uniform(f_row[0]);
       const unsigned char* kp = (const unsigned char*)a.pages.k + (size_t)row * (D * 2);
       const unsigned char* vp = (const unsigned char*)a.pages.v + (size_t)row * (D * 2);
 #pragma unroll
@@ -226,7 +236,7 @@ __global__ __launch_bounds__(64 * SH_WAVES, 2) void shared_bf16_kernel(DevDesc d
     } else {
 #pragma unroll
       for (int x = 0; x < 2; ++x) {
-        const size_t at = (size_t)(uint32_t)lds.row[SH_KEYS * t + 8 * wave + 4 * x + r4] * (D * 2);
+        const size_t at = (size_t)(uint32_t)f_row[x] * (D * 2);
         to_lds((const unsigned char*)a.pages.k + at + (k_in ^ (x << 6)), uniform((int)(to + x * 1024)));
         to_lds((const unsigned char*)a.pages.v + at + (v_in ^ (x << 5)), uniform((int)(to + SH_BUFS * SH_TILE + x * 1024)));
       }
@@ -301,6 +311,7 @@ __global__ __launch_bounds__(64 * SH_WAVES, 2) void shared_bf16_kernel(DevDesc d
     if (shares == 2) barrier();                 // (all have read the tile)
 #pragma unroll
     for (int n = 0; n < 2; ++n) {
+      if (n == 1 && some <= SH_FEW) break;
       const int at = col0 + 16 * n + col;
       float* op = so.part_o + (slot0 + at) * D + 4 * r4;
       float m = m_run[n], l = rows_sum(l_run[n]);
@@ -386,23 +397,19 @@ __global__ __launch_bounds__(64 * SH_WAVES, 2) void shared_bf16_kernel(DevDesc d
             s[n][b][x] = sees(a.vis, P[n], j0 + key) && ((there >> key) & 1) ? s[n][b][x] : NEG_INF;
           }
     }
-    // s -> p, with the running maximum and sum
+    // s -> p, with the running maximum and sum.  (A lane's own maximum shows whether the column's may have been passed.)
     float mx[N];
     bool moves = false;
 #pragma unroll
     for (int n = 0; n < N; ++n) {
-      mx[n] = s[n][0][0];
-#pragma unroll
-      for (int b = 0; b < B; ++b)
-#pragma unroll
-        for (int x = 0; x < 4; ++x) mx[n] = fmaxf(mx[n], s[n][b][x]);
-      mx[n] = rows_max(mx[n]) * sc.c;
-      moves = moves || mx[n] > m_run[n] + KEEP_MAX || (m_run[n] == NEG_INF && mx[n] > NEG_INF);
+      mx[n] = fmaxf(fmaxf(s[n][0][0], s[n][0][1]), fmaxf(s[n][0][2], s[n][0][3]));
+      mx[n] = fmaxf(fmaxf(fmaxf(mx[n], s[n][1][0]), fmaxf(s[n][1][1], s[n][1][2])), s[n][1][3]) * sc.c;
+      moves = moves || mx[n] > m_run[n] + KEEP_MAX;             // (at first: above -inf)
     }
     if (__any(moves)) {
 #pragma unroll
       for (int n = 0; n < N; ++n) {
-        const float m_new = fmaxf(m_run[n], mx[n]);
+        const float m_new = fmaxf(m_run[n], rows_max(mx[n]));
         const float corr = m_run[n] == NEG_INF ? 0.f : exp2_(m_run[n] - m_new);
         l_run[n] *= corr;
 #pragma unroll
@@ -487,6 +494,7 @@ __global__ __launch_bounds__(64 * SH_WAVES, 2) void shared_bf16_kernel(DevDesc d
       list_tiles(t0, n);
       barrier();
       int4 next = lds.tile[0];
+      ask(0);
 #pragma unroll 1
       for (int step = -3; step < n; ++step) {
         const int buf = step & (SH_BUFS - 1);
@@ -523,6 +531,7 @@ __global__ __launch_bounds__(64 * SH_WAVES, 2) void shared_bf16_kernel(DevDesc d
           barrier();
         }
         fetch(step + 3, n);
+        ask(min(step + 4, n - 1));
         if (step < 0) continue;
         if (step + 1 < n) next = lds.tile[step + 1];
         if (flags & FIRST) begin(flags >> NUMBER);
