@@ -34,6 +34,7 @@ constexpr int SH_TILE = SH_KEYS * D * 2;                       // bytes of a til
 constexpr int SH_BUFS = 4;
 constexpr int SH_FEW = 16;                                      // columns whose queries come through LDS, four units ahead
 constexpr int SH_QUERIES = SH_FEW * D * 2;
+typedef WorkRow<SH_COLS, SH_KEYS> RowBf16;
 constexpr int SH_LIST = 128, SH_LIST_ANY = 24;                  // tiles that are listed at a time (where rows lie anywhere)
 constexpr int SH_ROWS = SH_LIST * 8 > SH_LIST_ANY * SH_KEYS ? SH_LIST * 8 : SH_LIST_ANY * SH_KEYS;      // numbers of their rows' places
 struct SharedLds {
@@ -44,17 +45,16 @@ struct SharedLds {
   int row[SH_ROWS];                                             // of tiles: eight rows' first, or every row
   int4 tile[SH_LIST];                                           // rows that some column may see (two words), first token, flags
   float2 ml[SH_WAVES][32];                                      // waves' maxima and sums
-  int4 share;
+  RowBf16::Scratch scratch;
   unsigned char odd[SH_BUFS][SH_WAVES];                         // rows with a value that is not finite, a byte a wave
 };
 constexpr int SH_LDS = sizeof(SharedLds);
 static_assert(SH_LDS <= 160 * 1024);
 constexpr float KEEP_MAX = 8.f;
 constexpr int SF_WAVES = 4, SF_COLS = 16, SF_KEYS = 64;
+typedef WorkRow<SF_COLS, SF_KEYS> RowF32;
 typedef float f32x4_t __attribute__((ext_vector_type(4)));
 
-typedef WorkRow<SH_COLS, SH_KEYS> RowBf16;
-typedef WorkRow<SF_COLS, SF_KEYS> RowF32;
 
 struct SharedOut {
   float* part_o;           // of the pieces: [place][D] sums of p v, and [place][2] maximum and sum
@@ -133,18 +133,16 @@ __global__ __launch_bounds__(64 * SH_WAVES, 2) void shared_bf16_kernel(DevDesc d
     const int some = cols - ct * SH_COLS;
     return some <= SH_FEW ? 0 : some <= SH_COLS / 2 ? 1 : 2;
   };
-  // The list of pieces, and how many tiles they have (wave 0 finds it out; all get it).
+  // The list of pieces, and how many tiles they have.
   auto list_pieces = [&] {
+    mine.at = mine.upto;
+    RowBf16::list<SH_WAVES>(d, args, mine, lds.list, &lds.scratch);
     if (wave == 0) {
-      RowBf16::list(d, args, mine, lds.list);
       const Piece& f = lds.list[lane];
       const int n = lane < mine.n && f.i0 < f.i1 ? f.i1 - f.i0 + query_tiles(f.cols, f.ct) : 0;
       lds.upto[lane] = lanes_upto(n);
-      if (lane == 0) lds.share = make_int4(mine.at, mine.upto, mine.end, mine.n);
     }
     barrier();
-    const int4 x = lds.share;
-    mine = Share{uniform(x.x), uniform(x.y), uniform(x.z), uniform(x.w)};
   };
   // Lists tiles t0 .. t0 + n - 1 of the pieces: where their rows are, who sees them.
   auto list_tiles = [&](int t0, int n) {
@@ -152,9 +150,11 @@ __global__ __launch_bounds__(64 * SH_WAVES, 2) void shared_bf16_kernel(DevDesc d
     for (int i = threadIdx.x; i < n * EACH; i += 64 * SH_WAVES) {
       const int t = i / EACH, x = i % EACH;
       int p = 0;
-#pragma unroll 1
-      for (int k = PIECES / 2; k > 0; k >>= 1)
-        if (lds.upto[p + k - 1] <= t0 + t) p += k;
+#pragma unroll
+      for (int k = PIECES / 4; k > 0; k >>= 2) {
+        const int y0 = lds.upto[p + k - 1], y1 = lds.upto[p + 2 * k - 1], y2 = lds.upto[p + 3 * k - 1];
+        p += y2 <= t0 + t ? 3 * k : y1 <= t0 + t ? 2 * k : y0 <= t0 + t ? k : 0;
+      }
       const Piece& f = lds.list[p];
       const int at = f.i1 - (lds.upto[p] - (t0 + t));           // (tiles of queries: before i0)
       int flags = at + 1 == f.i1 ? LAST : 0, j0 = at - f.i0 + query_tiles(f.cols, f.ct);
@@ -568,7 +568,7 @@ __global__ __launch_bounds__(64 * SF_WAVES) void shared_f32_kernel(DevDesc d, Sh
   __shared__ __align__(16) float s_o[SF_WAVES][16][D + 4];
   __shared__ float s_m[SF_WAVES][16], s_l[SF_WAVES][16];
   __shared__ __align__(16) Piece s_list[PIECES];
-  __shared__ __align__(16) int4 s_share;
+  __shared__ RowF32::Scratch s_scratch;
   const PagedArgs& a = args.a;
   const int lane = threadIdx.x & 63, wave = uniform((int)(threadIdx.x >> 6)), wg = blockIdx.x;
   const int r = lane >> 4, col = lane & 15;
@@ -581,12 +581,8 @@ __global__ __launch_bounds__(64 * SF_WAVES) void shared_f32_kernel(DevDesc d, Sh
   for (bool begun = false;; ++now) {
     if (now == mine.n) {                                // the next list, or the first
       if (begun && mine.upto >= mine.end) return;
-      if (wave == 0) {
-        RowF32::list(d, args, mine, s_list);
-        if (lane == 0) s_share = make_int4(mine.at, mine.upto, mine.end, mine.n);
-      }
-      __syncthreads();
-      mine = Share{uniform(s_share.x), uniform(s_share.y), uniform(s_share.z), uniform(s_share.w)};
+      mine.at = mine.upto;
+      RowF32::list<SF_WAVES>(d, args, mine, s_list, &s_scratch);
       begun = true;
       now = 0;
       if (mine.n == 0) return;
@@ -830,7 +826,7 @@ struct SharedPlan {
 };
 
 // the longest row that there can be (the scores' rows have tiles of more columns and heavier ones)
-constexpr int MOST_WEIGHT = 3, MOST_COST = 6;
+constexpr int MOST_WEIGHT = 7, MOST_COST = 12;
 long long most_tiles(const DevDesc& d, long long n_rows, long long cap, int cols, int keys) {
   const long long col_tiles = 2 * ((n_rows * d.G + cols - 1) / cols + d.B);
   return col_tiles * d.Hkv * (MOST_WEIGHT * ((cap + keys - 1) / keys + 2) + MOST_COST);

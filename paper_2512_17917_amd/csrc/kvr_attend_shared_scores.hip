@@ -25,7 +25,7 @@ struct ScoresLds {
   float lse[SS_COLS<T>];
   int pos[SS_COLS<T>];                              // last token that a column sees, -1: none of the unit's
   Piece list[PIECES];
-  int4 share;
+  typename WorkRow<SS_COLS<T>, SS_KEYS, true>::Scratch scratch;
 };
 
 // tokens of a wave's turn: keys of as many blocks of 16 as registers hold
@@ -44,13 +44,8 @@ __global__ __launch_bounds__(64 * SS_WAVES, 4) void shared_scores_kernel(DevDesc
   const float scale2 = d.scale * LOG2E;
   Share mine = {0, 0, 0, 0};
   for (;;) {
-    if (wave == 0) {
-      Row::list(d, args, mine, lds.list);
-      if (lane == 0) lds.share = make_int4(mine.at, mine.upto, mine.end, mine.n);
-    }
-    __syncthreads();
-    const int4 share = lds.share;
-    mine = Share{uniform(share.x), uniform(share.y), uniform(share.z), uniform(share.w)};
+    mine.at = mine.upto;
+    Row::template list<SS_WAVES>(d, args, mine, lds.list, &lds.scratch);
     if (mine.n == 0) return;
     for (int now = 0; now < mine.n; ++now) {
       const Piece& u = lds.list[now];

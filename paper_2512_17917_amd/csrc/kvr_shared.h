@@ -4,9 +4,9 @@
 // heads); what a sequence has behind them is its own.  A *unit* is a kv head and a tile of COLS columns, of a group over the
 // tokens in common or of a sequence over its own.  A unit's tokens are a run of tiles of KEYS tokens; all units' tiles stand in
 // one row (groups first; of a group or a sequence tile of columns after tile of columns, head after head), and each workgroup
-// takes the same share of it, whatever the lengths, which only the device knows.  The row is measured in what the work costs: a
-// unit's start and end count as a tile, and a tile of many columns, which the matrix units take longer for than the memory, as one
-// and a half (in halves of a tile: COST and weight).
+// takes the same share of it, whatever the lengths, which only the device knows.  The row is measured in what the work costs, in
+// quarters of a tile of few columns: a unit's start and end are COST of them, a tile of many columns, which the matrix units take
+// longer for than the memory, `weight`.
 //
 // A workgroup's piece of a unit leaves its columns' maximum, sum and sum of p v in the workspace, columns COLS w + c .. of it
 // (w: the workgroup, c: columns of the units before): going along the row each next piece raises w by one or c by the columns
@@ -63,11 +63,12 @@ struct Member {
   RowSpan span;
   int n, from;
 };
+__host__ __device__ __forceinline__ bool has_common(const Member& m, int common) { return m.span.n > 0 && m.n - m.span.n >= common; }
 __host__ __device__ __forceinline__ Member member_at(const SharedArgs& s, int b, int common) {
   Member r;
   r.span = row_span(s.a.q_start, s.a.n_rows, b);
   r.n = clampi(listed(s.a.n_ctx + b), 0, s.a.pages.cap);
-  r.from = r.span.n > 0 && r.n - r.span.n >= common ? common : 0;
+  r.from = has_common(r, common) ? common : 0;
   return r;
 }
 
@@ -87,8 +88,7 @@ enum { PIECE_OWN = 1, PIECE_FIRST = 2, PIECE_LAST = 4 };
 constexpr int PIECES = 64, PIECE_WORDS = sizeof(Piece) / 4;      // a list's length at most
 static_assert(PIECE_WORDS == 16);
 
-// A workgroup's part of the row: at .. end-1, of which the list has what lies before `upto`, in n pieces.  Pieces without a tile
-// are among them.
+// A workgroup's part of the row: at .. end-1, of which the list has at .. upto-1 in n pieces.  Pieces without a tile are among them.
 struct Share {
   int at, upto, end, n;
 };
@@ -96,10 +96,10 @@ struct Share {
 // SCORES: the row of the pass that adds scores, which takes longer with every column
 template <int COLS, int KEYS, bool SCORES = false>
 struct WorkRow {
-  static constexpr int COST = SCORES ? 6 : 2, MOST_WEIGHT = SCORES ? 2 + COLS / 16 : 3;
+  static constexpr int COST = SCORES ? 12 : 5, LIGHT = 4, HEAVY = 7;
   __host__ __device__ static __forceinline__ int weight(int cols) {
-    if (SCORES) return 2 + (cols < COLS ? cols : COLS) / 16;
-    return cols > COLS / 2 && COLS > 64 ? 3 : 2;
+    if (SCORES) return LIGHT + (cols < COLS ? cols : COLS) / 8;
+    return cols > COLS / 2 && COLS > 64 ? HEAVY : LIGHT;
   }
 
   __host__ __device__ static __forceinline__ int col_tiles(int rows, int G) { return (int)(((long long)rows * G + COLS - 1) / COLS); }
@@ -118,12 +118,13 @@ struct WorkRow {
   // A group or a sequence in the row: what its units have in common.
   struct Entry {
     int own, id;                    // of a sequence, its number; or the group's
+    int b;                          // whose table is read
     int row0, cols, from, lim, lo;
     Run run;
     int units, weight;
   };
   __host__ __device__ static __forceinline__ int unit_length(const Entry& e) { return e.run.n * e.weight + COST; }
-  __host__ __device__ static __forceinline__ Entry no_entry() { return Entry{1, 0, 0, 0, 0, 1, 0, Run{0, 0, 0, 0}, 0, 1}; }
+  __host__ __device__ static __forceinline__ Entry no_entry() { return Entry{1, 0, 0, 0, 0, 0, 1, 0, Run{0, 0, 0, 0}, 0, 1}; }
   __host__ __device__ static __forceinline__ Entry group_entry(const DevDesc& d, const SharedArgs& s, int g) {
     const Group x = group_at(s, d.B, g);
     Entry e;
@@ -137,13 +138,18 @@ struct WorkRow {
     e.run = group_run(s, x);
     e.units = e.run.n > 0 ? col_tiles(x.rows, d.G) * d.Hkv : 0;
     e.weight = weight(e.cols);
+    e.b = x.b0;                     // the first that has the tokens
+    for (int b = x.b0; b < x.b1 && e.units > 0; ++b)
+      if (member_at(s, b, x.common).from > 0) {
+        e.b = b;
+        break;
+      }
     return e;
   }
-  __host__ __device__ static __forceinline__ Entry member_entry(const DevDesc& d, const SharedArgs& s, int b, int common) {
-    const Member m = member_at(s, b, common);
+  __host__ __device__ static __forceinline__ Entry member_entry(const DevDesc& d, const SharedArgs& s, int b, const Member& m) {
     Entry e;
     e.own = 1;
-    e.id = b;
+    e.id = e.b = b;
     e.row0 = m.span.first;
     e.cols = m.span.n * d.G;
     e.from = m.from;
@@ -155,7 +161,7 @@ struct WorkRow {
     return e;
   }
   // The piece of unit `unit` (of the entry's), which begins at `first` in the row, that lies within at .. end-1.
-  __host__ __device__ static __forceinline__ Piece piece_of(const DevDesc& d, const SharedArgs& s, const Entry& e, int unit, int first, int at, int end) {
+  __host__ __device__ static __forceinline__ Piece piece_of(const DevDesc& d, const Entry& e, int unit, int first, int at, int end) {
     // a tile is the workgroup's in whose part of the row it begins
     auto tile = [&](int x) {
       const int t = x - first - COST;
@@ -165,16 +171,8 @@ struct WorkRow {
     p.i0 = tile(at);
     p.i1 = tile(end);
     p.bits = (e.own ? PIECE_OWN : 0) | (p.i0 == 0 ? PIECE_FIRST : 0) | (p.i1 == e.run.n ? PIECE_LAST : 0);
-    p.g = p.b = e.id;
-    if (!e.own) {                   // the table of the first sequence that has the tokens
-      const Group x = group_at(s, d.B, e.id);
-      p.b = x.b0;
-      for (int b = x.b0; b < x.b1; ++b)
-        if (member_at(s, b, x.common).from > 0) {
-          p.b = b;
-          break;
-        }
-    }
+    p.g = e.id;
+    p.b = e.b;
     p.ct = unit / d.Hkv;
     p.h = unit - p.ct * d.Hkv;
     p.row0 = e.row0;
@@ -190,12 +188,17 @@ struct WorkRow {
   }
 
   // ---- the row, 64 entries at a time, one a lane (all lanes of a wave call) ----
-  // how many tokens sequence b0 + lane's group has in common; g0: the first group that may hold one of the 64, kept from call to
-  // call
-  __device__ static __forceinline__ int commons(const DevDesc& d, const SharedArgs& s, int b0, int& g0) {
+  // how many tokens sequence b0 + lane's group has in common
+  __device__ static __forceinline__ int commons(const DevDesc& d, const SharedArgs& s, int b0) {
     const int lane = threadIdx.x & 63, b = b0 + lane;
-    int common = 0, last = g0;
-    for (int g = g0; g < s.n_groups; g += 64) {
+    int g = 0;
+    for (int hi = s.n_groups; hi - g > 64;) {                    // the first group that ends behind b0, or one before it
+      const int mid = (g + hi) >> 1;
+      if (clampi(listed(s.start + mid), 0, d.B) <= b0) g = mid;
+      else hi = mid;
+    }
+    int common = 0;
+    for (; g < s.n_groups; g += 64) {
       Group x = {d.B, d.B, 0, 0, 0};
       if (g + lane < s.n_groups) x = group_at(s, d.B, g + lane);
       const int n = __popcll(__ballot(x.b0 < b0 + 64 && x.b0 < d.B));
@@ -204,81 +207,120 @@ struct WorkRow {
         const int c = __builtin_amdgcn_readlane(x.common, i);
         if (b >= lo && b < hi) common = c;
       }
-      if (n > 0) last = g + n - 1;
       if (n < 64) break;
     }
-    g0 = uniform(last);
     return common;
   }
-  // The workgroup's part of the row (r.end = 0 asks for it), and the pieces of its next ones, as many as the list holds.  (The host has
-  // made sure that the row's length fits 31 bits.)
-  __device__ static __forceinline__ void list(const DevDesc& d, const SharedArgs& s, Share& r, Piece* to) {
-    const int lane = threadIdx.x & 63;
-    const int of_groups = (s.n_groups + 63) >> 6, chunks = of_groups + ((d.B + 63) >> 6);
+  // What the waves tell each other.
+  struct Scratch {
+    int length[16], heavy[16], pieces[16], upto;
+  };
+  // The workgroup's part of the row (r.end = 0 asks for it), and the pieces of its next ones, as many as the list holds; all waves
+  // call, each with 64 entries of the row at a time.  (The host has made sure that the row's length fits 31 bits.)
+  template <int WAVES>
+  __device__ static __forceinline__ void list(const DevDesc& d, const SharedArgs& s, Share& r, Piece* to, Scratch* x) {
+    const int lane = threadIdx.x & 63, wave = uniform((int)(threadIdx.x >> 6));
+    const int of_groups = (s.n_groups + 63) >> 6, chunks = of_groups + ((d.B + 63) >> 6), rounds = (chunks + WAVES - 1) / WAVES;
+    Entry e = no_entry();
+    int length = 0, upto = 0, units_upto = 0;
+    bool known = false;
     for (int pass = r.end == 0 ? 0 : 1; pass < 2; ++pass) {
-      int base = 0, have = 0, g0 = 0;
-      for (int c = 0; c < chunks; ++c) {
-        Entry e = no_entry();
-        if (c < of_groups) {
-          if (64 * c + lane < s.n_groups) e = group_entry(d, s, 64 * c + lane);
-        } else {
-          const int b0 = 64 * (c - of_groups), common = commons(d, s, b0, g0);
-          if (b0 + lane < d.B) e = member_entry(d, s, b0 + lane, common);
+      int base0 = 0, have = 0, least = LIGHT;
+      for (int round = 0; round < rounds; ++round) {
+        if (!known) {
+          const int c = round * WAVES + wave;
+          e = no_entry();
+          if (c < of_groups) {
+            if (64 * c + lane < s.n_groups) e = group_entry(d, s, 64 * c + lane);
+          } else if (c < chunks) {
+            const int b0 = 64 * (c - of_groups), b = b0 + lane;
+            Member m = {{0, 0}, 0, 0};          // (asked for beside the groups)
+            if (b < d.B) m = member_at(s, b, 0);
+            const int common = commons(d, s, b0);
+            m.from = has_common(m, common) ? common : 0;
+            if (b < d.B) e = member_entry(d, s, b, m);
+          }
+          length = unit_length(e) * e.units;
+          upto = lanes_upto(length);
+          units_upto = lanes_upto(e.units);
+          known = rounds == 1;
         }
-        const int length = unit_length(e) * e.units, upto = lanes_upto(length);
         const int here = __builtin_amdgcn_readlane(upto, 63);
-        if (pass == 0 || base + here <= r.upto) {
-          base += here;
+        __syncthreads();
+        const bool heavy = __any(e.units > 0 && e.weight > LIGHT);
+        if (lane == 0) {
+          x->length[wave] = here;
+          x->heavy[wave] = heavy;
+        }
+        __syncthreads();
+        const int theirs = lane < WAVES ? x->length[lane] : 0, sum = lanes_upto(theirs);
+        const int base = base0 + __builtin_amdgcn_readlane(sum - theirs, wave);
+        base0 += __builtin_amdgcn_readlane(sum, 63);
+        if (pass == 0) {
+          if (__any(lane < WAVES && x->heavy[lane] != 0)) least = HEAVY;
           continue;
         }
-        // the unit that r.upto lies in, among the chunk's
-        const int units_upto = lanes_upto(e.units), units_here = __builtin_amdgcn_readlane(units_upto, 63), off = r.upto - base;
-        const int l0 = uniform((int)__ffsll(__ballot(off < upto)) - 1);
-        const int u = __builtin_amdgcn_readlane(units_upto - e.units, l0) +
-                      uniform((off - __builtin_amdgcn_readlane(upto - length, l0)) / __builtin_amdgcn_readlane(unit_length(e), l0)) + lane - have;
-        // each lane behind those that have a piece takes the next unit: it is the entry's whose units end behind it
-        int l = 0;
-#pragma unroll 1
-        for (int k = 32; k > 0; k >>= 1)
-          if (__shfl(units_upto, l + k - 1) <= u) l += k;
-        Entry x;
-        x.own = __shfl(e.own, l);
-        x.id = __shfl(e.id, l);
-        x.row0 = __shfl(e.row0, l);
-        x.cols = __shfl(e.cols, l);
-        x.from = __shfl(e.from, l);
-        x.lim = __shfl(e.lim, l);
-        x.lo = __shfl(e.lo, l);
-        x.run.ahead0 = __shfl(e.run.ahead0, l);
-        x.run.ahead = __shfl(e.run.ahead, l);
-        x.run.start = __shfl(e.run.start, l);
-        x.run.n = __shfl(e.run.n, l);
-        x.weight = __shfl(e.weight, l);
-        const int unit = u - __shfl(units_upto - e.units, l);
-        const int first = base + __shfl(upto - length, l) + unit * unit_length(x);
-        const bool mine = lane >= have && u < units_here && first < r.end;
-        int last = r.upto;
-        if (mine) {
-          to[lane] = piece_of(d, s, x, unit, first, r.upto, r.end);
-          last = min(first + unit_length(x), r.end);
+        // which of this wave's units lie within at .. end-1
+        const int lo = max(r.at, base) - base, hi = min(r.end, base + here) - base;
+        auto unit_at = [&](int off) {
+          const int l = uniform((int)__ffsll(__ballot(off < upto)) - 1);
+          return __builtin_amdgcn_readlane(units_upto - e.units, l) +
+                 uniform((off - __builtin_amdgcn_readlane(upto - length, l)) / __builtin_amdgcn_readlane(unit_length(e), l));
+        };
+        int u0 = 0, n = 0;
+        if (lo < hi) {
+          u0 = unit_at(lo);
+          n = unit_at(hi - 1) - u0 + 1;
         }
-        have += __popcll(__ballot(mine));
-        r.upto = __builtin_amdgcn_readlane(last, max(have - 1, 0));
-        base += here;
-        if (have == PIECES || r.upto >= r.end) break;
+        if (lane == 0) x->pieces[wave] = n;
+        __syncthreads();
+        const int many = lane < WAVES ? x->pieces[lane] : 0, before = lanes_upto(many);
+        const int slot = have + __builtin_amdgcn_readlane(before - many, wave) + lane, u = u0 + lane;
+        have += __builtin_amdgcn_readlane(before, 63);
+        if (n > 0) {
+          int l = 0;                            // whose units end behind the lane's
+#pragma unroll
+          for (int k = 16; k > 0; k >>= 2) {
+            const int y0 = __shfl(units_upto, l + k - 1), y1 = __shfl(units_upto, l + 2 * k - 1), y2 = __shfl(units_upto, l + 3 * k - 1);
+            l += y2 <= u ? 3 * k : y1 <= u ? 2 * k : y0 <= u ? k : 0;
+          }
+          Entry y;
+          y.own = __shfl(e.own, l);
+          y.id = __shfl(e.id, l);
+          y.b = __shfl(e.b, l);
+          y.row0 = __shfl(e.row0, l);
+          y.cols = __shfl(e.cols, l);
+          y.from = __shfl(e.from, l);
+          y.lim = __shfl(e.lim, l);
+          y.lo = __shfl(e.lo, l);
+          y.run.ahead0 = __shfl(e.run.ahead0, l);
+          y.run.ahead = __shfl(e.run.ahead, l);
+          y.run.start = __shfl(e.run.start, l);
+          y.run.n = __shfl(e.run.n, l);
+          y.weight = __shfl(e.weight, l);
+          const int unit = u - __shfl(units_upto - e.units, l);
+          const int first = base + __shfl(upto - length, l) + unit * unit_length(y);
+          if (lane < n && slot < PIECES) {
+            to[slot] = piece_of(d, y, unit, first, r.at, r.end);
+            if (slot == PIECES - 1) x->upto = min(first + unit_length(y), r.end);
+          }
+        }
+        if (have >= PIECES || base0 >= r.end) break;
       }
       if (pass == 0) {
         // (no less than a tile of the heaviest: of a unit's workgroups each has a tile, as who joins their pieces relies on)
-        const int per = max(MOST_WEIGHT, uniform((int)(((unsigned)base + gridDim.x - 1) / gridDim.x)));
+        const int per = max(least, uniform((int)(((unsigned)base0 + gridDim.x - 1) / gridDim.x)));
         const long long at = (long long)blockIdx.x * per;
-        if (at >= base) {
+        if (at >= base0) {
           r = Share{0, 0, 0, 0};
           return;
         }
-        r.at = r.upto = (int)at;
-        r.end = min(per, base - r.at) + r.at;
+        r.at = (int)at;
+        r.end = min(per, base0 - r.at) + r.at;
       } else {
-        r.n = uniform(have);
+        __syncthreads();
+        r.n = min(have, PIECES);
+        r.upto = have >= PIECES ? uniform(x->upto) : r.end;
       }
     }
   }
