@@ -663,7 +663,7 @@ int32_t kvr_attend_shared_workspace_size(const kvr_desc* desc, int32_t n_rows, c
   if (rc != KVR_OK) return rc;
   if (bytes == nullptr || n_rows < 0 || n_rows > MAX_ROWS_NEW || (long long)n_rows * d.Hq > MAX_HEADS_SHARED) return KVR_ERR_INVALID_ARG;
   if (!kvr::attend_shared_fits(d, n_rows, p.cap)) return KVR_ERR_UNSUPPORTED;
-  *bytes = n_rows == 0 ? 0 : kvr::attend_shared_ws(d, desc->dtype, n_rows, p.cap, scores != 0);
+  *bytes = n_rows == 0 ? 0 : kvr::attend_shared_ws(d, desc->dtype, n_rows, p.cap, vis, groups ? groups->n_groups : 0, scores != 0);
   return KVR_OK;
 }
 
@@ -689,7 +689,7 @@ int32_t kvr_attend_shared(const kvr_desc* desc, const void* q, int32_t n_rows, c
     s.n_groups = groups->n_groups;
   }
   if (!kvr::attend_shared_fits(d, n_rows, s.a.pages.cap)) return KVR_ERR_UNSUPPORTED;
-  rc = check_ws(ws, ws_bytes, kvr::attend_shared_ws(d, desc->dtype, n_rows, s.a.pages.cap, scores != nullptr));
+  rc = check_ws(ws, ws_bytes, kvr::attend_shared_ws(d, desc->dtype, n_rows, s.a.pages.cap, s.a.vis, s.n_groups, scores != nullptr));
   if (rc != KVR_OK) return rc;
   s.a.n_rows = n_rows;
   s.a.q_start = q_start;

@@ -855,14 +855,45 @@ SharedPlan shared_plan(const DevDesc& d, int dtype, long long n_rows, long long 
 bool attend_shared_fits(const DevDesc& d, long long n_rows, long long cap) {
   return most_tiles(d, n_rows, cap, SF_COLS, SF_KEYS) < 0x7fffffffll && attend_paged_fits(d, cap, Visible{0, 0});
 }
-size_t attend_shared_ws(const DevDesc& d, int dtype, long long n_rows, long long cap, bool scores) {
-  return shared_plan(d, dtype, n_rows, cap, scores ? cap : 0).total;
+// Whose kernels a call takes.  Small caches are read sooner by every sequence for itself: what counts is the cache that a batch of
+// the longest sequences would read, by the room that it has (the lengths only the device knows).  One token per sequence, 32 heads on 8,
+// each for itself and shared: 66 MB (4 x 4000) 19.9 and 21.7 us, 68 MB (16 x 1000) 22.2 and 20.1, 131 MB (2 x 16000) 37.5 and
+// 31.7; with scores, whose pass is a launch more, 131 MB 40.0 and 43.9, 265 MB (16 x 4000) 45.6 and 36.6; float32 66 MB 23.0 and
+// 29.9, 132 MB 40.4 and 31.1.  Several tokens: the prompt's kernel pads a sequence's columns to 256, and is as fast where they are many
+// (8 x 4000 tokens with 2 rows each, 8 columns, 32.1 and 24.1, with 6 rows 32.4 and 31.9, with 12 35.9 and 41.5; 8 x 16000 with 12
+// 87 and 64, with 24 92 and 98).  In float32 it does not share out long caches, and is bound by products where its 16
+// columns a workgroup fill the chip (8 x 4000 with 6 rows, 96 workgroups, 180 and 82; with 24, 384, 195 and 250; 2 x 200 with 6 16.0
+// and 16.6, 8 x 200 16.5 and 26.4).
+enum Route { SHARED, PAGED, PROMPT };
+static Route route(const DevDesc& d, int dtype, long long n_rows, long long cap, const Visible& vis, int n_groups, bool single, bool scores) {
+  long long tokens = cap;
+  if (vis.window > 0 && (long long)vis.window + vis.n_sink < tokens) tokens = (long long)vis.window + vis.n_sink;
+  const long long mb = (long long)d.B * d.Hkv * tokens * D * 2 * (dtype == KVR_F32 ? 4 : 2) / 1000000;
+  if (single) return n_groups == 0 || mb < (scores ? 192 : 72) ? PAGED : SHARED;
+  if (n_groups == 0) return PROMPT;
+  if (dtype == KVR_F32) return tokens < 512 || n_rows * d.Hq / 16 >= 256 ? PROMPT : SHARED;
+  const long long cols = n_rows * d.G / d.B;                    // of a sequence
+  return cols > 64 || mb < 64 + 3 * cols ? PROMPT : SHARED;
 }
 
-hipError_t launch_attend_shared(const DevDesc& d, int dtype, const SharedArgs& given, hipStream_t st) {
-  SharedArgs s = given;
+size_t attend_shared_ws(const DevDesc& d, int dtype, long long n_rows, long long cap, const Visible& vis, int n_groups, bool scores) {
+  size_t most = 0;                                              // (one row a sequence may come with starts or without)
+  for (int single = 0; single < (n_rows == d.B ? 2 : 1); ++single) {
+    const Route r = route(d, dtype, n_rows, cap, vis, n_groups, single != 0, scores);
+    const size_t n = r == PAGED    ? attend_paged_ws(d, dtype, cap, vis, scores)
+                     : r == PROMPT ? attend_prompt_ws(d, dtype, n_rows, cap, vis, scores)
+                                   : shared_plan(d, dtype, n_rows, cap, scores ? cap : 0).total;
+    most = n > most ? n : most;
+  }
+  return most;
+}
+
+hipError_t launch_attend_shared(const DevDesc& d, int dtype, const SharedArgs& s, hipStream_t st) {
   const PagedArgs& a = s.a;
-  s.least = 1;
+  const bool single = a.q_start == nullptr;                     // one new token per sequence
+  const Route r = route(d, dtype, a.n_rows, a.pages.cap, a.vis, s.n_groups, single, a.scores != nullptr);
+  if (r == PAGED) return launch_attend_paged(d, dtype, a, st);
+  if (r == PROMPT) return launch_attend_prompt(d, dtype, a, st);
   const SharedPlan p = shared_plan(d, dtype, a.n_rows, a.pages.cap, a.scores ? a.n_cap : 0);
   char* base = (char*)a.ws;
   SharedOut so;
@@ -870,7 +901,6 @@ hipError_t launch_attend_shared(const DevDesc& d, int dtype, const SharedArgs& g
   so.part_ml = (float*)(base + p.off_ml);
   so.span = (int*)(base + p.off_span);
   so.lse = a.scores ? (float*)(base + p.off_lse) : nullptr;
-  const bool single = a.q_start == nullptr;                     // one new token per sequence: a pass of its own for its scores
   so.work = a.scores && !single && dtype == KVR_BF16 ? (ScoresWork*)(base + p.off_scores) : nullptr;
   so.keys = p.scores.keys;
   so.most_scores_splits = p.scores.most_splits;

@@ -312,13 +312,12 @@ struct SharedArgs {
   const int32_t* start;             // of the groups, [n_groups + 1]
   const int32_t* n_shared;
   int n_groups;
-  int least;                        // fewer tokens in common than this are not worth a pass of their own
 };
 // (one new token per sequence)
 hipError_t launch_shared_scores(const DevDesc& d, int dtype, const SharedArgs& s, const float* lse, hipStream_t st);
 // false: more tiles of columns and tokens than the kernels count
 bool attend_shared_fits(const DevDesc& d, long long n_rows, long long cap);
-size_t attend_shared_ws(const DevDesc& d, int dtype, long long n_rows, long long cap, bool scores);
+size_t attend_shared_ws(const DevDesc& d, int dtype, long long n_rows, long long cap, const Visible& vis, int n_groups, bool scores);
 hipError_t launch_attend_shared(const DevDesc& d, int dtype, const SharedArgs& s, hipStream_t st);
 bool attend_paged_fits(const DevDesc& d, long long cap, const Visible& vis);
 size_t attend_paged_ws(const DevDesc& d, int dtype, long long cap, const Visible& vis, bool scores);

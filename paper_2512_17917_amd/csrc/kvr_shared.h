@@ -5,7 +5,7 @@
 // tokens in common or of a sequence over its own.  A unit's tokens are a run of tiles of KEYS tokens; all units' tiles stand in
 // one row (groups first; of a group or a sequence tile of columns after tile of columns, head after head), and each workgroup
 // takes the same share of it, whatever the lengths, which only the device knows.  The row is measured in what the work costs, in
-// quarters of a tile of few columns: a unit's start and end are COST of them, a tile of many columns, which the matrix units take
+// quarters of a tile of few columns: a unit's start and end are `cost` of them, a tile of many columns, which the matrix units take
 // longer for than the memory, `weight`.
 //
 // A workgroup's piece of a unit leaves its columns' maximum, sum and sum of p v in the workspace, columns COLS w + c .. of it
@@ -39,7 +39,8 @@ __host__ __device__ __forceinline__ int run_token(const Run& r, int i) {
   return i < r.ahead ? r.ahead0 + i * T : r.start + (i - r.ahead) * T;
 }
 
-// A group: sequences b0 .. b1-1, their rows, and how many tokens they have in common (0: nothing is shared, or not to advantage)
+// A group: sequences b0 .. b1-1, their rows, and how many tokens they have in common (0: nothing is shared, or not to advantage: a
+// pass over them takes about as long as four tiles of 64 tokens more)
 struct Group {
   int b0, b1, row0, rows, common;
 };
@@ -48,7 +49,7 @@ __host__ __device__ __forceinline__ Group group_at(const SharedArgs& s, int B, i
   r.b0 = clampi(listed(s.start + g), 0, B);
   r.b1 = clampi(listed(s.start + g + 1), r.b0, B);
   const int n = clampi(listed(s.n_shared + g), 0, s.a.pages.cap);
-  r.common = r.b1 - r.b0 < 2 || n < s.least ? 0 : n;
+  r.common = (long long)(r.b1 - r.b0 - 1) * (n >> 6) < 4 ? 0 : n;
   if (s.a.q_start == nullptr) {
     r.row0 = r.b0;
     r.rows = r.b1 - r.b0;
@@ -96,7 +97,9 @@ struct Share {
 // SCORES: the row of the pass that adds scores, which takes longer with every column
 template <int COLS, int KEYS, bool SCORES = false>
 struct WorkRow {
-  static constexpr int COST = SCORES ? 12 : 5, LIGHT = 4, HEAVY = 7;
+  static constexpr int LIGHT = 4, HEAVY = 7;
+  // (queries of more than 16 columns are steps of their own, and more of them are joined and written at the end)
+  __host__ __device__ static __forceinline__ int cost(int cols) { return SCORES || cols > 16 ? 12 : 5; }
   __host__ __device__ static __forceinline__ int weight(int cols) {
     if (SCORES) return LIGHT + (cols < COLS ? cols : COLS) / 8;
     return cols > COLS / 2 && COLS > 64 ? HEAVY : LIGHT;
@@ -123,7 +126,7 @@ struct WorkRow {
     Run run;
     int units, weight;
   };
-  __host__ __device__ static __forceinline__ int unit_length(const Entry& e) { return e.run.n * e.weight + COST; }
+  __host__ __device__ static __forceinline__ int unit_length(const Entry& e) { return e.run.n * e.weight + cost(e.cols); }
   __host__ __device__ static __forceinline__ Entry no_entry() { return Entry{1, 0, 0, 0, 0, 0, 1, 0, Run{0, 0, 0, 0}, 0, 1}; }
   __host__ __device__ static __forceinline__ Entry group_entry(const DevDesc& d, const SharedArgs& s, int g) {
     const Group x = group_at(s, d.B, g);
@@ -164,7 +167,7 @@ struct WorkRow {
   __host__ __device__ static __forceinline__ Piece piece_of(const DevDesc& d, const Entry& e, int unit, int first, int at, int end) {
     // a tile is the workgroup's in whose part of the row it begins
     auto tile = [&](int x) {
-      const int t = x - first - COST;
+      const int t = x - first - cost(e.cols);
       return t <= 0 ? 0 : (t + e.weight - 1) / e.weight < e.run.n ? (t + e.weight - 1) / e.weight : e.run.n;
     };
     Piece p;

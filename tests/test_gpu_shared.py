@@ -1,4 +1,7 @@
-"""kvr_attend_shared against float64 (tests/cache_ref.py), which knows nothing of groups: the sequences' own table rows."""
+"""kvr_attend_shared against float64 (tests/cache_ref.py), which knows nothing of groups: the sequences' own table rows.
+
+The call goes by the room of a cache: small ones are read by every sequence for itself.  ROOM tokens more than the longest
+sequence has (the table's entries for them name no page) make the small batches here take the kernels for long ones."""
 import math
 
 import pytest
@@ -10,13 +13,14 @@ from tests import cache_ref as R
 pytestmark = [pytest.mark.gpu, pytest.mark.timeout(300)]
 D = 128
 BF, F32 = torch.bfloat16, torch.float32
+ROOM = 200000
 
 
 class Batch:
     """Groups as lists of (tokens, new rows) with the tokens that they have in common: [(common, [(n, y), ...]), ...]; their
     pools, table, lengths and queries on the CPU."""
 
-    def __init__(self, groups, heads, page, dtype, seed, *, lead=0, trail=0, alone=(), rows=True, room=0):
+    def __init__(self, groups, heads, page, dtype, seed, *, lead=0, trail=0, alone=(), rows=True, room=ROOM):
         """alone: sequences of no group, behind the groups; rows: by q_start (else one row a sequence); room: tokens that a
         sequence can hold past its longest."""
         g = self.g = torch.Generator().manual_seed(seed)
@@ -60,7 +64,7 @@ class Batch:
                 pool[order[to], :, :m] = pool[order[src], :, :m]
         self.q = torch.randn(self.rows, self.Hq, D, generator=g).to(dtype)
         self.cap = each * page
-        self.n_cap = self.cap
+        self.n_cap = min(self.cap, max(self.n) + 30)
 
     def check(self, window=0, sink=0, scores=True, scale=None, start=None, common=None, groups=True, nan=(), finite_k=None):
         """nan: (sequence, kv head, query heads) whose logits have a NaN that the reference leaves out.  finite_k: keys by which
@@ -112,19 +116,74 @@ CASES = [  # groups, heads, page, lead, trail, alone, by q_start
     ([(129, one(130, 0, 50, 700, 129))], (8, 8), 24, 0, 0, (), False),               # an empty row, and one that is shorter than what is shared
     ([(500, one(501)), (77, one(78, 79, 0))], (16, 2), 7, 0, 0, (), False),          # a group of one; pages of an odd size
     ([(200, [(210, 5), (200, 1), (333, 30), (201, 0)])], (32, 8), 32, 3, 2, [(40, 40)], True),
-    ([(640, [(700, 60)] * 9)], (16, 2), 64, 0, 0, (), True),                         # 480 rows of 8 heads: several tiles of columns
-    ([(250, [(260, 20), (251, 1), (900, 300)])], (4, 4), 1, 0, 5, (), True),          # the first has new rows among what is shared
+    ([(640, [(700, 8)] * 9)], (16, 2), 64, 0, 0, (), True),                          # 72 rows of 8 heads: several tiles of columns
+    ([(640, [(700, 60)] * 9)], (16, 2), 64, 0, 0, (), True),                         # too many rows to share
+    ([(250, [(260, 20), (251, 1), (900, 100)])], (2, 2), 1, 0, 5, (), True),          # the first has new rows among what is shared
+    ([(64, one(65, 70, 64, 90, 128, 129)), (65, one(66, 67, 68, 69, 70)), (128, one(129, 130, 131))], (4, 2), 8, 0, 0, (), False),
+    ([(200, [(203, 3), (210, 2), (201, 1), (264, 33)] * 3)], (4, 1), 16, 0, 0, (), True),      # 117 columns
+    ([(300, one(*[301 + i for i in range(6)])), (300, one(*[310 + i for i in range(12)])), (300, one(*[301 + i for i in range(30)]))],
+     (8, 2), 16, 0, 0, (), False),                                                   # 24, 48 and 120 columns
     ([(2048, one(*range(2049, 2100)))], (64, 8), 128, 0, 0, (), False),               # 408 columns
     ([(3000, one(*[3000 + 7 * i for i in range(1, 40)])), (100, one(101, 102))], (8, 1), 48, 0, 0, one(1, 2, 3), False),
 ]
 
 
 @pytest.mark.parametrize("dtype", [BF, F32])
-@pytest.mark.parametrize("window,sink", [(0, 0), (100, 0), (33, 4), (600, 130), (1, 0), (1, 3)])
 @pytest.mark.parametrize("case", range(len(CASES)))
-def test_against_each_sequence_by_itself(case, window, sink, dtype):
+def test_against_each_sequence_by_itself(case, dtype):
     groups, heads, page, lead, trail, alone, rows = CASES[case]
     b = Batch(groups, heads, page, dtype, 40 + case, lead=lead, trail=trail, alone=alone, rows=rows)
+    b.check()
+    b.check(scores=False)
+
+
+def _many(rows, members, common):
+    """A group, its sequences' own tokens from none (a sequence that is shorter than what it shares) to 300."""
+    return common, [(max(common + 37 * i % 301 - (9 if i == 3 else 0), 0), 1 + i % rows) for i in range(members)]
+
+
+WINDOWS = [  # rows of a sequence at most, groups, heads, page, window, first tokens: batches whose windows make a cache worth sharing
+    (1, [_many(1, 40, 500), _many(1, 35, 129), _many(1, 30, 64), _many(1, 25, 1000)], (16, 8), 16, 400, 0),
+    (1, [_many(1, 60, 450), _many(1, 66, 430)], (8, 8), 24, 390, 4),
+    (1, [_many(1, 70, 640), _many(1, 30, 131)], (64, 8), 5, 500, 130),
+    (1, [_many(1, 560, 70)], (8, 8), 16, 90, 3),
+    (4, [_many(4, 40, 500), _many(4, 35, 129), _many(4, 30, 64), _many(4, 25, 1000)], (16, 8), 8, 260, 20),
+    (9, [_many(9, 20, 900)], (4, 4), 64, 530, 3),
+]
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("case", range(len(WINDOWS)))
+def test_windows(case, dtype):
+    """With pages that are not there, and values that are not finite where some columns see them and others do not."""
+    most, groups, heads, page, window, sink = WINDOWS[case]
+    b = Batch(groups, heads, page, dtype, 80 + case, rows=most > 1, room=0)
+    b.check(window, sink)
+    b.check(window, sink, scores=False)
+    for i, (c, (first, end)) in enumerate(zip(b.common, zip(b.start, b.start[1:]))):
+        if i % 2 == 0:                                           # a page of what is shared
+            at = max(c - window, 0) // page + 1
+            if (at + 1) * page <= c:
+                b.table[first:end, at] = -1
+        for j, what in ((c - 1, math.nan), (max(c - window + 100, 0), math.inf), (sink // 2, -math.inf)):
+            for s in range(first, end):                          # (copies of a page that is filled in part have it too)
+                at = R.token_row(b.k, b.table, s, j) if j < b.n[s] else None
+                if at is not None:
+                    b.v[at[0], 1, at[1], 64 + i] = what
+        last = end - 1
+        at = R.token_row(b.k, b.table, last, b.n[last] - 1)
+        if at is not None:
+            b.v[at[0], 0, at[1], 3] = math.inf
+    b.check(window, sink)
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("window,sink", [(0, 0), (600, 130), (33, 4), (1, 0), (1, 3)])
+@pytest.mark.parametrize("case", range(len(CASES)))
+def test_small_caches(case, window, sink, dtype):
+    """Those that every sequence reads for itself."""
+    groups, heads, page, lead, trail, alone, rows = CASES[case]
+    b = Batch(groups, heads, page, dtype, 60 + case, lead=lead, trail=trail, alone=alone, rows=rows, room=0)
     b.check(window, sink)
     b.check(window, sink, scores=False)
 
@@ -140,11 +199,11 @@ def test_no_groups_and_groups_that_share_nothing(dtype):
 
 @pytest.mark.parametrize("dtype", [BF, F32])
 def test_starts_that_go_past_the_batch_and_more_in_common_than_there_is_room_for(dtype):
-    b = Batch([(96, one(100, 120, 97))], (8, 2), 32, dtype, 8, rows=False)
+    b = Batch([(96, one(100, 120, 97, 98, 99, 96))], (8, 2), 32, dtype, 8, rows=False)
     b.check(start=[-5, 77], common=[96])
-    b.check(start=[0, 3], common=[1 << 30])           # (more than each has: each by itself)
-    b.check(start=[0, 3], common=[-4])
-    b.check(start=[0, 1, 3], common=[96, 90])
+    b.check(start=[0, 6], common=[1 << 30])           # (more than each has: each by itself)
+    b.check(start=[0, 6], common=[-4])
+    b.check(start=[0, 1, 6], common=[96, 90])
 
 
 @pytest.mark.parametrize("dtype", [BF, F32])
@@ -157,18 +216,16 @@ def test_pages_that_are_not_there(dtype, page):
     b.table[0, 384 // page] = -7
     b.table[2, 448 // page:] = -1
     b.check()
-    b.check(150, 20)
     b.table[:, :320 // page] = -1                     # nothing of it
     b.check()
 
 
 @pytest.mark.parametrize("dtype", [BF, F32])
-@pytest.mark.parametrize("window,sink", [(0, 0), (120, 3)])
 @pytest.mark.parametrize("what", [math.inf, -math.inf, math.nan])
-def test_values_that_are_not_finite(dtype, window, sink, what):
+def test_values_that_are_not_finite(dtype, what):
     """Where no query sees them they do nothing; where one does they are its, not its neighbours'."""
-    b = Batch([(200, [(230, 9), (203, 3), (420, 1)])], (8, 2), 16, dtype, 15)
-    rows = [R.token_row(b.k, b.table, i, j) for i, j in ((0, 229), (0, 225), (2, 419), (2, 390))]
+    b = Batch([(320, [(350, 9), (323, 3), (540, 1)])], (8, 2), 16, dtype, 15)
+    rows = [R.token_row(b.k, b.table, i, j) for i, j in ((0, 349), (0, 345), (2, 539), (2, 510))]
     shared = R.token_row(b.k, b.table, 0, 150)
     for page, row in rows + [shared]:
         b.v[page, 1, row, 5] = what
@@ -181,14 +238,14 @@ def test_values_that_are_not_finite(dtype, window, sink, what):
     named = set(b.table.flatten().tolist())
     for page in set(range(b.k.shape[0])) - named:
         b.k[page] = b.v[page] = what
-    b.check(window, sink)
+    b.check()
 
 
 @pytest.mark.parametrize("dtype", [BF, F32])
 @pytest.mark.parametrize("where", ["shared", "own"])
 def test_logits_that_are_not_finite(dtype, where):
     """NaN among the logits of one sequence's query, -Inf among all of another's."""
-    b = Batch([(130, one(190, 131, 250))], (4, 2), 16, dtype, 16, rows=False)
+    b = Batch([(130, one(190, 131, 250, 140))], (4, 2), 16, dtype, 16, rows=False)
     page, row = R.token_row(b.k, b.table, 0, 100 if where == "shared" else 180)
     if where == "shared":
         b.q[0, 1, 3] = math.nan
@@ -196,7 +253,7 @@ def test_logits_that_are_not_finite(dtype, where):
     else:
         b.k[page, 1, row, 0] = math.nan
         b.check(nan=[(0, 1, [2, 3])])
-    b2 = Batch([(130, one(190, 131, 250))], (4, 2), 16, dtype, 17, rows=False)
+    b2 = Batch([(130, one(190, 131, 250, 140))], (4, 2), 16, dtype, 17, rows=False)
     page, row = R.token_row(b2.k, b2.table, 0, 100 if where == "shared" else 180)
     b2.k[page, 1, row] = 0
     k0 = b2.k.clone()
@@ -208,7 +265,7 @@ def test_logits_that_are_not_finite(dtype, where):
 @pytest.mark.parametrize("dtype", [BF, F32])
 @pytest.mark.parametrize("scale", [0.0, -0.2, 3.0])
 def test_scales(dtype, scale):
-    Batch([(150, one(190, 151, 250)), (33, one(40, 41))], (8, 2), 16, dtype, 18, rows=False).check(scale=scale)
+    Batch([(150, one(190, 151, 250, 152)), (33, one(40, 41))], (8, 2), 16, dtype, 18, rows=False).check(scale=scale)
 
 
 @pytest.mark.parametrize("dtype", [BF, F32])
@@ -238,12 +295,12 @@ def test_a_place_for_fewer_scores_than_tokens():
         b.n_cap = 250
         b.check()
         b.n_cap = 310
-        b.check(64, 4)
+        b.check()
 
 
 @pytest.mark.parametrize("dtype,groups,heads", [
     (BF, [(30000, one(30100, 30001, 30500))], (8, 2)), (F32, [(9000, one(9100, 9001))], (4, 4)),
     (BF, [(20, one(*[21 + i % 50 for i in range(300)]))], (4, 1)), (F32, [(20, one(*[21 + i % 50 for i in range(150)]))], (4, 1)),
-    (BF, [(5 + i, one(6 + i, 7 + i, 90)) for i in range(70)], (2, 2))])
+    (BF, [(5 + i, one(6 + i, 7 + i, 90)) for i in range(70)], (2, 2)), (BF, [(100 + i, one(*[101 + i + j for j in range(6)])) for i in range(150)], (2, 2))])
 def test_long_ones_and_many(dtype, groups, heads):
     Batch(groups, heads, 16, dtype, 22, rows=False).check()
