@@ -600,13 +600,14 @@ int32_t kvr_attend_paged(const kvr_desc* desc, const void* q, const int32_t* n_c
  * kvr_attend_prompt (with q_start) and kvr_attend_paged (without: row b is the newest token of sequence b) for sequences
  * that begin with the same tokens: out and scores are theirs, but what a group shares is read once for all its rows, and
  * what each sequence has behind it beside that.  A sequence with a new row among the shared tokens is attended by itself,
- * as one of no group is.  bf16: p is rounded to bf16 for its product with v, as in kvr_attend_prompt.
- * Made for few new tokens a sequence; for long ones with q_start kvr_attend_prompt does as well.
+ * as one of no group is.  A call whose room is too small for sharing to pay, or whose sequences have many new tokens each, takes
+ * the kernels of those two (by sizes alone, so that a captured call is right for whatever the device holds later).  bf16: p may be
+ * rounded to bf16 for its product with v, as in kvr_attend_prompt.  One call gives the same bits each time.
  *   groups     host, or NULL: nothing is shared
- *   n_rows     n_rows * Hq is at most 2^28 here
+ *   n_rows     n_rows * Hq is at most 2^28 here; without q_start n_rows = B
  *   ws         per kvr_attend_shared_workspace_size, with scores = whether there are scores (of `groups` the sizes are looked at)
- *   the others as for kvr_attend_prompt.  KVR_ERR_UNSUPPORTED also where 2 (n_rows G / 16 + B + 1) Hkv times a 64th of the
- *              tokens that a sequence can hold passes 2^31
+ *   the others as for kvr_attend_prompt.  KVR_ERR_UNSUPPORTED also where 2 (n_rows G / 16 + B) Hkv (7 (C / 64 + 2) + 12), each
+ *              quotient rounded up, reaches 2^31 - 1 (C: the tokens that a sequence can hold)
  */
 int32_t kvr_attend_shared_workspace_size(const kvr_desc* desc, int32_t n_rows, const kvr_pages* pages,
                                          const kvr_groups* groups, int32_t window, int32_t n_sink, int32_t scores,

@@ -57,6 +57,7 @@ typedef float f32x4_t __attribute__((ext_vector_type(4)));
 
 
 struct SharedOut {
+  int wgs;                 // workgroups of the first launch
   float* part_o;           // of the pieces: [place][D] sums of p v, and [place][2] maximum and sum
   float* part_ml;
   int* span;               // [place of a unit's first column][2]: the first and the last workgroup that has a piece of it
@@ -252,11 +253,15 @@ __global__ __launch_bounds__(64 * SH_WAVES, 2) void shared_bf16_kernel(DevDesc d
   int now = 0;                                  // the piece that is worked on
   int shares = 1, key0 = 0, col0 = 0;           // waves with this one's columns, its first token of a tile and its first column
   bool wave_live = false;
-  auto take_queries = [&](const unsigned char* from, uint32_t bank) {      // of this wave's columns; bank: bytes from columns 0 .. 63 to the others
+  auto take_queries = [&](const unsigned char* from, uint32_t bank, bool few) {      // of this wave's columns; bank: bytes from columns 0 .. 63 to the others
 #pragma unroll
     for (int n = 0; n < 2; ++n)
 #pragma unroll
       for (int c = 0; c < 4; ++c) {
+        if (n == 1 && few) {                    // (none.  Whatever lies there instead would decide when the maxima move: zeros, which never do)
+          q[n][c] = bf16x8_t{};
+          continue;
+        }
         const int at = (col0 + 16 * n + col) & (SH_COLS / 2 - 1);
         u32x4_t x = *reinterpret_cast<const u32x4_t*>(from + (at >> 6) * bank + (at & 63) * 256 + (((4 * c + r4) ^ (at & 15)) << 4));
 #pragma unroll
@@ -293,8 +298,7 @@ __global__ __launch_bounds__(64 * SH_WAVES, 2) void shared_bf16_kernel(DevDesc d
         else P[1] = at < some ? p : -1;
       }
     }
-    // (few columns: the second block's are none, and get what lies there)
-    if (some <= SH_FEW && wave_live) take_queries(lds.q[now & (SH_BUFS - 1)], 0);
+    if (some <= SH_FEW && wave_live) take_queries(lds.q[now & (SH_BUFS - 1)], 0, true);
   };
   // (buf: the tile's place, which is free once all have read it)
   auto finish = [&](int buf) {
@@ -536,7 +540,7 @@ __global__ __launch_bounds__(64 * SH_WAVES, 2) void shared_bf16_kernel(DevDesc d
         if (step + 1 < n) next = lds.tile[step + 1];
         if (flags & FIRST) begin(flags >> NUMBER);
         if (flags & QUERIES) {
-          if (wave_live && (col0 >> 7) == j0) take_queries(lds.k[buf], SH_BUFS * SH_TILE);
+          if (wave_live && (col0 >> 7) == j0) take_queries(lds.k[buf], SH_BUFS * SH_TILE, false);
           continue;
         }
         if (wave_live && (there0 | there1) != 0) {
@@ -772,8 +776,8 @@ __global__ __launch_bounds__(256) void shared_join_kernel(DevDesc d, SharedArgs 
     const int row0 = own ? mem.span.first : x.row0, cols = (own ? mem.span.n : x.rows) * d.G;
     const int m = (row - row0) * d.G + gq, ct = m / COLS;
     const int c0 = Row::place(d, a.n_rows, own, row0, cols, ct, h);
-    const int w0 = listed(so.span + 2 * (size_t)c0);
-    n[own] = listed(so.span + 2 * (size_t)c0 + 1) - w0 + 1;
+    const int w0 = clampi(listed(so.span + 2 * (size_t)c0), 0, so.wgs - 1);      // (starts that fall, against the contract, leave others')
+    n[own] = clampi(listed(so.span + 2 * (size_t)c0 + 1), w0, so.wgs - 1) - w0 + 1;
     first[own] = (size_t)COLS * w0 + c0 + (m - ct * COLS);
   }
   const int all = n[0] + n[1];
@@ -897,6 +901,7 @@ hipError_t launch_attend_shared(const DevDesc& d, int dtype, const SharedArgs& s
   const SharedPlan p = shared_plan(d, dtype, a.n_rows, a.pages.cap, a.scores ? a.n_cap : 0);
   char* base = (char*)a.ws;
   SharedOut so;
+  so.wgs = p.wgs;
   so.part_o = (float*)base;
   so.part_ml = (float*)(base + p.off_ml);
   so.span = (int*)(base + p.off_span);

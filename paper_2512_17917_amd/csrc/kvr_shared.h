@@ -141,12 +141,11 @@ struct WorkRow {
     e.run = group_run(s, x);
     e.units = e.run.n > 0 ? col_tiles(x.rows, d.G) * d.Hkv : 0;
     e.weight = weight(e.cols);
-    e.b = x.b0;                     // the first that has the tokens
-    for (int b = x.b0; b < x.b1 && e.units > 0; ++b)
-      if (member_at(s, b, x.common).from > 0) {
-        e.b = b;
-        break;
-      }
+    e.b = x.b0;                     // the first that has the tokens behind which its rows lie; without one there is nothing to do
+    if (e.units > 0) {
+      while (e.b < x.b1 && member_at(s, e.b, x.common).from == 0) ++e.b;
+      if (e.b == x.b1) e.units = 0;
+    }
     return e;
   }
   __host__ __device__ static __forceinline__ Entry member_entry(const DevDesc& d, const SharedArgs& s, int b, const Member& m) {

@@ -17,6 +17,16 @@ def _zeros(dev, *shapes):
     return out
 
 
+def _rotate(desc, rotation, axes, pos, *args):
+    """kvr_rotate, or by positions on several axes."""
+    if (axes is None) != (pos is None):
+        raise ValueError("axes and pos come together")
+    if axes is None:
+        kvr.kvr_rotate(desc, rotation, *args)
+    else:
+        kvr.kvr_rotate_axes(desc, rotation, axes, pos, *args)
+
+
 class LayerState:
     """All per-unit buffers of one layer, unit-major [B, Hkv, ...]."""
 
@@ -117,18 +127,19 @@ class LayerState:
             raise RuntimeError(f"a unit needed {-worst} evictions but evict_cap = {self.evict_cap}, "
                                f"vague_cap = {self.vague_cap}: nothing was evicted there")
 
-    def rotate(self, k_new, q, rotation):
+    def rotate(self, k_new, q, rotation, axes=None, pos=None):
         """Norm and rotation of one new token per sequence (k_new [B, Hkv, D], q [B, Hq, D] as projected; n_ctx counts
-        the token) -> the key that append takes and the query that attend takes, in buffers that the next call reuses."""
+        the token) -> the key that append takes and the query that attend takes, in buffers that the next call reuses.
+        axes, a binding.make_axes, and pos int32 [n_axes, B]: by these positions instead of the tokens' places."""
         if self.k_turned is None:
             self.k_turned = torch.empty(k_new.shape, dtype=self.dtype, device=self.device)
             self.q_turned = torch.empty(q.shape, dtype=self.dtype, device=self.device)
-        kvr.kvr_rotate(self.desc, rotation, q, k_new, None, self.desc.batch, None, self.n_ctx, self.q_turned, self.k_turned)
+        _rotate(self.desc, rotation, axes, pos, q, k_new, None, self.desc.batch, None, self.n_ctx, self.q_turned, self.k_turned)
         return self.k_turned, self.q_turned
 
     def decode_step(self, k_new, v_new, q, *, bump_n_ctx=True, fused=None, replace_rate=None, max_swaps=4,
-                    check=False, opts=None, rotation=None):
-        """(rotate, if a binding.make_rotation is given) -> append -> select -> encode -> (swap loop, if replace_rate
+                    check=False, opts=None, rotation=None, axes=None, pos=None):
+        """(rotate, if a binding.make_rotation is given, by axes and pos if those are) -> append -> select -> encode -> (swap loop, if replace_rate
         is given) -> attend.  n_ctx counts the new token from here on; pass bump_n_ctx=False when
         several layers share one n_ctx tensor that the caller advances once per
         step.  fused: use kvr_step_update for the first three (default: whenever its
@@ -137,7 +148,7 @@ class LayerState:
         if bump_n_ctx:
             self.n_ctx += 1
         if rotation is not None:
-            k_new, q = self.rotate(k_new, q, rotation)
+            k_new, q = self.rotate(k_new, q, rotation, axes, pos)
         # Algorithm 3, first branch: does the Recent queue hand its overhang on to the Candidates?
         self.r_size = kvr.kvr_recent_size(self.r_size + 1, self.n_recent, self.slack)
         if fused is None:
@@ -239,9 +250,10 @@ class PagedCache:
     until (or instead of) its compression into a LayerState."""
 
     def __init__(self, desc, *, n_pages, page_size, table_cap, rotation=None, window=0, n_sink=0, scores=True,
-                 device="cuda", n_ctx=None, table=None):
+                 device="cuda", n_ctx=None, table=None, axes=None):
         """table int32 [B, table_cap] (None: made here, with no page assigned; see assign) and n_ctx int32 [B] may be
         shared by layers; rotation: a binding.make_rotation (None: queries and keys are cached as they come);
+        axes: a binding.make_axes (the rotation goes by positions on several axes, which each call then takes as pos);
         scores: accumulate the weights that each token draws.  Tokens past table_cap * page_size are stored nowhere and
         attention takes the sequence to end there: the caller, who advances n_ctx, keeps it within.  A place of the batch
         that passes to another sequence keeps its scores until the caller clears them."""
@@ -252,6 +264,7 @@ class PagedCache:
         self.device = torch.device(device)
         self.dtype = torch.float32 if desc.dtype == kvr.KVR_F32 else torch.bfloat16
         self.rotation = kvr.make_rotation(desc) if rotation is None else rotation
+        self.axes, self.groups, self.ws_shared = axes, None, None
         self.k, self.v = (torch.zeros(n_pages, Hkv, page_size, D, dtype=self.dtype, device=self.device) for _ in range(2))
         self.table = torch.full((B, table_cap), -1, dtype=torch.int32, device=self.device) if table is None else table
         self.n_ctx = torch.zeros(B, dtype=torch.int32, device=self.device) if n_ctx is None else n_ctx
@@ -270,25 +283,79 @@ class PagedCache:
             raise ValueError(f"pages {first} .. {first + len(pages) - 1} of a sequence that has room for {self.table.shape[1]}")
         self.table[b, first:first + len(pages)] = torch.as_tensor(pages, dtype=torch.int32, device=self.device)
 
-    def prompt(self, q, k, v, q_start):
+    def begin_with(self, b, source, n_tokens, page=None):
+        """Sequence b begins with the first n_tokens of sequence `source`, and has nothing else yet: its row of the table
+        names the source's pages, but where the last is not filled by these tokens, they are copied to `page`, one of the
+        cache's that nobody names.  What the tokens have drawn is b's too, its other scores are cleared.  The caller sets n_ctx
+        and assigns the pages for what follows; layers that share a table make the same call each."""
+        ps = self.k.shape[2]
+        full, rest = divmod(int(n_tokens), ps)
+        if b == source or not (0 <= b < self.desc.batch and 0 <= source < self.desc.batch):
+            raise ValueError(f"sequence {b} of {source}: two of 0 .. {self.desc.batch - 1}")
+        if n_tokens < 0 or full + (rest > 0) > self.table.shape[1]:
+            raise ValueError(f"{n_tokens} tokens for a sequence that has room for 0 .. {self.table.shape[1] * ps}")
+        if rest and (page is None or not 0 <= page < self.k.shape[0]):
+            raise ValueError(f"{rest} tokens are on a page filled in part: a page of 0 .. {self.k.shape[0] - 1} to copy them to")
+        self.table[b] = -1
+        self.table[b, :full] = self.table[source, :full]
+        if rest:
+            at = self.table[source, full:full + 1].long()
+            there = (at >= 0) & (at < self.k.shape[0])           # (else b's tokens are on no page either)
+            for pool in (self.k, self.v):
+                pool[page, :, :rest] = pool.index_select(0, torch.where(there, at, 0))[0, :, :rest]
+            self.table[b, full] = torch.where(there, page, -1)[0]
+        if self.scores is not None:
+            self.scores[b, :, :n_tokens] = self.scores[source, :, :n_tokens]
+            self.scores[b, :, n_tokens:] = 0
+
+    def share(self, start, n_shared):
+        """From here on what a group's sequences have in common is read once for all of them: sequences start[g] ..
+        start[g + 1] - 1 begin with the same n_shared[g] tokens (see begin_with).  int32 device tensors are taken as they
+        are, and a call goes by what they hold then, a captured one too; lists are copied; no groups, or None, ends it."""
+        self.groups = None
+        if start is None:
+            return
+        i32 = lambda x: x if isinstance(x, torch.Tensor) else torch.tensor(x, dtype=torch.int32, device=self.device)
+        groups = kvr.make_groups(i32(start), i32(n_shared))
+        if groups.n_groups == 0:
+            return
+        if self.ws_shared is None:                  # of every step; it is the same size for all groups
+            self.ws_shared = self._room_to_share(groups, self.desc.batch)
+        self.groups = groups
+
+    def _room_to_share(self, groups, rows):
+        n = kvr.kvr_attend_shared_workspace_size(self.desc, rows, self.pages, groups, self.window, self.n_sink, self.scores is not None)
+        return torch.empty(max(n, 256), dtype=torch.uint8, device=self.device)
+
+    def prompt(self, q, k, v, q_start, pos=None):
         """New tokens by q_start int32 [B + 1] (q [n_rows, Hq, D], k, v [n_rows, Hkv, D] as projected; n_ctx counts
-        them): into the pages, then attention over all of each sequence.  Returns out [n_rows, Hq, D]."""
+        them): into the pages, then attention over all of each sequence.  pos int32 [n_axes, n_rows]: the rows' positions
+        where the cache has axes.  Returns out [n_rows, Hq, D]."""
         rows = q.shape[0]
         turned = torch.empty(rows, self.desc.n_q_heads, self.desc.head_dim, dtype=self.dtype, device=self.device)
-        kvr.kvr_rotate(self.desc, self.rotation, q, k, v, rows, q_start, self.n_ctx, turned, None, self.pages)
+        _rotate(self.desc, self.rotation, self.axes, pos, q, k, v, rows, q_start, self.n_ctx, turned, None, self.pages)
         out = torch.zeros_like(turned)
+        if self.groups is not None:
+            ws = self._room_to_share(self.groups, rows)
+            kvr.kvr_attend_shared(self.desc, turned, rows, q_start, self.n_ctx, self.pages, self.groups, self.window, self.n_sink, out,
+                                  self.scores, self.n_cap, ws)
+            return out
         n = kvr.kvr_attend_prompt_workspace_size(self.desc, rows, self.pages, self.window, self.n_sink, self.scores is not None)
         ws = torch.empty(max(n, 256), dtype=torch.uint8, device=self.device)
         kvr.kvr_attend_prompt(self.desc, turned, rows, q_start, self.n_ctx, self.pages, self.window, self.n_sink, out,
                               self.scores, self.n_cap, ws)
         return out
 
-    def decode_step(self, q, k, v, *, bump_n_ctx=True):
+    def decode_step(self, q, k, v, *, bump_n_ctx=True, pos=None):
         """One token per sequence (q [B, Hq, D], k, v [B, Hkv, D] as projected) into the pages, then its attention;
-        bump_n_ctx as in LayerState.decode_step.  Returns out [B, Hq, D], reused by the next step."""
+        bump_n_ctx as in LayerState.decode_step, pos int32 [n_axes, B] as in prompt.  Returns out [B, Hq, D], reused by the next step."""
         if bump_n_ctx:
             self.n_ctx += 1
-        kvr.kvr_rotate(self.desc, self.rotation, q, k, v, self.desc.batch, None, self.n_ctx, self.q, None, self.pages)
+        _rotate(self.desc, self.rotation, self.axes, pos, q, k, v, self.desc.batch, None, self.n_ctx, self.q, None, self.pages)
+        if self.groups is not None:
+            kvr.kvr_attend_shared(self.desc, self.q, self.desc.batch, None, self.n_ctx, self.pages, self.groups, self.window,
+                                  self.n_sink, self.out, self.scores, self.n_cap, self.ws_shared)
+            return self.out
         kvr.kvr_attend_paged(self.desc, self.q, self.n_ctx, self.pages, self.window, self.n_sink, self.out, self.scores,
                              self.n_cap, self.ws)
         return self.out
