@@ -66,12 +66,12 @@ struct SharedOut {
   int keys, most_scores_splits, scores_wgs;
 };
 
-// Position of a row of group g, -1 if its sequence does not have the tokens in common (all lanes call, each with its row)
-__device__ __forceinline__ int position_in_group(const DevDesc& d, const SharedArgs& s, int g, int row) {
+// Position of a row of group g, -1 if its sequence does not have the `common` tokens (all lanes call, each with its row)
+__device__ __forceinline__ int position_in_group(const DevDesc& d, const SharedArgs& s, int g, int common, int row) {
   const int lane = threadIdx.x & 63;
-  const Group x = group_at(s, d.B, g);
   int b = row;
   if (s.a.q_start != nullptr) {
+    const Group x = group_at(s, d.B, g);
     b = x.b0;
     for (int i0 = x.b0; i0 < x.b1; i0 += 64) {
       const int end = i0 + lane < x.b1 ? listed(s.a.q_start + i0 + lane + 1) : 0x7fffffff;
@@ -79,8 +79,8 @@ __device__ __forceinline__ int position_in_group(const DevDesc& d, const SharedA
       for (int i = 0; i < n; ++i) b += __builtin_amdgcn_readlane(end, i) <= row ? 1 : 0;
     }
   }
-  if (b < x.b0 || b >= x.b1) return -1;
-  const Member m = member_at(s, b, x.common);
+  if (b >= d.B) return -1;
+  const Member m = member_at(s, b, common);
   return m.from > 0 ? m.n - m.span.n + (row - m.span.first) : -1;
 }
 
@@ -273,7 +273,7 @@ __global__ __launch_bounds__(64 * SH_WAVES, 2) void shared_bf16_kernel(DevDesc d
     now = piece;
     const Piece& u = lds.list[now];
     const int ct = uniform(u.ct), cols = uniform(u.cols), own = uniform(u.bits) & PIECE_OWN, lo = uniform(u.lo), row0 = uniform(u.row0);
-    const int some = min(cols - ct * SH_COLS, SH_COLS);
+    const int some = min(cols - ct * SH_COLS, SH_COLS), lim = uniform(u.lim);
     shares = some <= SH_COLS / 2 ? 2 : 1;
     key0 = shares == 2 ? 32 * (wave & 1) : 0;
     col0 = 32 * (shares == 2 ? wave >> 1 : wave);
@@ -290,10 +290,10 @@ __global__ __launch_bounds__(64 * SH_WAVES, 2) void shared_bf16_kernel(DevDesc d
     }
     if (!own && a.vis.window > 0) {
       const int g = uniform(u.g);
-#pragma unroll 1
+#pragma unroll
       for (int n = 0; n < 2; ++n) {
         const int at = col0 + 16 * n + col, m = ct * SH_COLS + at;
-        const int p = position_in_group(d, args, g, row0 + (at < some ? m >> gs : 0));
+        const int p = position_in_group(d, args, g, lim, row0 + (at < some ? m >> gs : 0));
         if (n == 0) P[0] = at < some ? p : -1;
         else P[1] = at < some ? p : -1;
       }
@@ -398,8 +398,18 @@ __global__ __launch_bounds__(64 * SH_WAVES, 2) void shared_bf16_kernel(DevDesc d
 #pragma unroll
           for (int x = 0; x < 4; ++x) {
             const int key = key0 + 16 * b + 4 * r4 + x;
-            s[n][b][x] = sees(a.vis, P[n], j0 + key) && ((there >> key) & 1) ? s[n][b][x] : NEG_INF;
+            s[n][b][x] = sees(a.vis, P[n], j0 + key) ? s[n][b][x] : NEG_INF;
           }
+      if (there != ~0ull) {
+#pragma unroll
+        for (int b = 0; b < B; ++b) {
+          const uint32_t four = (uint32_t)(there >> (key0 + 16 * b + 4 * r4));
+#pragma unroll
+          for (int n = 0; n < N; ++n)
+#pragma unroll
+            for (int x = 0; x < 4; ++x) s[n][b][x] = (four >> x) & 1 ? s[n][b][x] : NEG_INF;
+        }
+      }
     }
     // s -> p, with the running maximum and sum.  (A lane's own maximum shows whether the column's may have been passed.)
     float mx[N];
@@ -511,24 +521,30 @@ __global__ __launch_bounds__(64 * SH_WAVES, 2) void shared_bf16_kernel(DevDesc d
           else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
           const uint32_t rows = ((wave < 4 ? there0 : there1) >> (8 * (wave & 3))) & 0xffu;
           if ((flags & APART) || rows != 0xffu) {
-            uint32_t odd = 0;
+            uint32_t odd = 0, hit = 0;
+            u32x4_t* mine_v = reinterpret_cast<u32x4_t*>(lds.v[buf] + 8 * wave * 256 + lane * 16);
+            u32x4_t v[2] = {mine_v[0], mine_v[64]};
+            if (flags & APART) {                // (an exponent of ones carries into the sign's place)
 #pragma unroll
-            for (int x = 0; x < 2; ++x) {
-              const bool dead = !((rows >> (4 * x + r4)) & 1);
-              u32x4_t* mine_v = reinterpret_cast<u32x4_t*>(lds.v[buf] + (8 * wave + 4 * x) * 256 + lane * 16);
-              u32x4_t v = *mine_v;
-              bool bad = false;
+              for (int e = 0; e < 4; ++e) hit |= ((v[0][e] & 0x7f807f80u) + 0x00800080u) | ((v[1][e] & 0x7f807f80u) + 0x00800080u);
+            }
+            if (rows != 0xffu || __any((hit & 0x80008000u) != 0)) {
 #pragma unroll
-              for (int e = 0; e < 4; ++e) {
-                const uint32_t lo16 = (v[e] & 0x7f80u) == 0x7f80u ? 0x0000ffffu : 0u;
-                const uint32_t hi16 = (v[e] & 0x7f800000u) == 0x7f800000u ? 0xffff0000u : 0u;
-                bad = bad || ((flags & APART) && (lo16 | hi16) != 0);
-                v[e] = dead ? 0u : (flags & APART) ? v[e] & ~(lo16 | hi16) : v[e];
+              for (int x = 0; x < 2; ++x) {
+                const bool dead = !((rows >> (4 * x + r4)) & 1);
+                bool bad = false;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                  const uint32_t lo16 = (v[x][e] & 0x7f80u) == 0x7f80u ? 0x0000ffffu : 0u;
+                  const uint32_t hi16 = (v[x][e] & 0x7f800000u) == 0x7f800000u ? 0xffff0000u : 0u;
+                  bad = bad || ((flags & APART) && (lo16 | hi16) != 0);
+                  v[x][e] = dead ? 0u : (flags & APART) ? v[x][e] & ~(lo16 | hi16) : v[x][e];
+                }
+                if (dead || bad) mine_v[64 * x] = v[x];
+                const unsigned long long who = __ballot(bad && !dead);
+#pragma unroll
+                for (int r = 0; r < 4; ++r) odd |= ((who >> (16 * r)) & 0xffffu) != 0 ? 1u << (4 * x + r) : 0u;
               }
-              if (dead || bad) *mine_v = v;
-              const unsigned long long who = __ballot(bad && !dead);
-#pragma unroll
-              for (int r = 0; r < 4; ++r) odd |= ((who >> (16 * r)) & 0xffffu) != 0 ? 1u << (4 * x + r) : 0u;
             }
             if (lane == 0) lds.odd[buf][wave] = (unsigned char)odd;
           }
@@ -601,7 +617,7 @@ __global__ __launch_bounds__(64 * SF_WAVES) void shared_f32_kernel(DevDesc d, Sh
     const int row_q = u.row0 + (live ? m >> gs : 0);
     int P = !live ? -1 : own ? u.lo + (m >> gs) : 0x7fffffff;
     if (!own && a.vis.window > 0) {
-      const int at = position_in_group(d, args, u.g, row_q);
+      const int at = position_in_group(d, args, u.g, u.lim, row_q);
       P = live ? at : -1;
     }
     f32x4_t q[8], o[8];
@@ -751,17 +767,19 @@ __global__ __launch_bounds__(64 * SF_WAVES) void shared_f32_kernel(DevDesc d, Sh
   }
 }
 
-// ---- the pieces of a row and head joined: a wave each, lane l channels 2 l and 2 l + 1; eight pieces' numbers are asked for at once
-template <typename T, int COLS, int KEYS>
+// ---- the pieces of a row and head joined: by WAVES waves, which take eight pieces in turn and ask for all their numbers at once; lane
+// l has channels 2 l and 2 l + 1.  Bound by round trips: lengths, span, then eight pieces a trip.
+template <typename T, int COLS, int KEYS, int WAVES>
 __global__ __launch_bounds__(256) void shared_join_kernel(DevDesc d, SharedArgs args, SharedOut so) {
   typedef WorkRow<COLS, KEYS> Row;
+  __shared__ float2 s_o[WAVES][64], s_ml[WAVES];
   const PagedArgs& a = args.a;
-  const int lane = threadIdx.x & 63;
-  const long long at = (long long)blockIdx.x * 4 + uniform((int)(threadIdx.x >> 6));
+  const int lane = threadIdx.x & 63, wave = uniform((int)(threadIdx.x >> 6)), part = WAVES == 1 ? 0 : wave;
+  const long long at = WAVES == 1 ? (long long)blockIdx.x * 4 + wave : blockIdx.x;
   if (at >= (long long)a.n_rows * d.Hq) return;
   const int row = uniform((int)(at / d.Hq)), hq = (int)(at - (long long)row * d.Hq);
   const int b = uniform(seq_of_row(a.q_start, d.B, row));
-  if (b < 0) return;
+  if (b < 0) return;                              // (all of a row's waves)
   const int h = uniform(hq / d.G), gq = hq - h * d.G;
   Group x = {0, 0, 0, 0, 0};
   const int g = group_of_seq(args, d.B, b);
@@ -783,7 +801,7 @@ __global__ __launch_bounds__(256) void shared_join_kernel(DevDesc d, SharedArgs 
   const int all = n[0] + n[1];
   const float NEG_INF = -__builtin_inff();
   float m = NEG_INF, l = 0.f, y0 = 0.f, y1 = 0.f;
-  for (int i0 = 0; i0 < all; i0 += 8) {
+  for (int i0 = 8 * part; i0 < all; i0 += 8 * WAVES) {
     float2 ml[8], v[8];
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
@@ -812,6 +830,27 @@ __global__ __launch_bounds__(256) void shared_join_kernel(DevDesc d, SharedArgs 
       y1 = fmaf(wt, v[e].y, y1);
     }
   }
+  if constexpr (WAVES > 1) {
+    s_o[part][lane] = make_float2(y0, y1);
+    if (lane == 0) s_ml[part] = make_float2(m, l);
+    __syncthreads();
+    if (part > 0) return;
+    float mn = m;
+#pragma unroll
+    for (int e = 1; e < WAVES; ++e) mn = fmaxf(mn, s_ml[e].x);
+    const float m_use = mn == NEG_INF ? 0.f : mn, f = exp2_(m - m_use);
+    l *= f;
+    y0 *= f;
+    y1 *= f;
+    m = mn;
+#pragma unroll
+    for (int e = 1; e < WAVES; ++e) {
+      const float wt = exp2_(s_ml[e].x - m_use);
+      l = fmaf(wt, s_ml[e].y, l);
+      y0 = fmaf(wt, s_o[e][lane].x, y0);
+      y1 = fmaf(wt, s_o[e][lane].y, y1);
+    }
+  }
   const float inv = l == 0.f ? 0.f : 1.f / l;
   if constexpr (sizeof(T) == 2) {
     const bf16x2_t r = __builtin_convertvector((f32x2_t{y0 * inv, y1 * inv}), bf16x2_t);
@@ -820,6 +859,16 @@ __global__ __launch_bounds__(256) void shared_join_kernel(DevDesc d, SharedArgs 
     *reinterpret_cast<float2*>((float*)a.out + at * D + 2 * lane) = make_float2(y0 * inv, y1 * inv);
   }
   if (so.lse && lane == 0) so.lse[at] = l == 0.f ? __builtin_inff() : m + __builtin_amdgcn_logf(l);
+}
+
+template <typename T, int COLS, int KEYS>
+hipError_t launch_join(const DevDesc& d, const SharedArgs& s, const SharedOut& so, hipStream_t st) {
+  const long long heads = (long long)s.a.n_rows * d.Hq;
+  // (one wave or four, whole calls: 64 rows and heads of 66 pieces 113 and 111 us, 512 of 30 95.6 and 94.7, 1792 105.8 and 107.6,
+  // 2048 78.1 and 79.3)
+  if (heads <= 1024) hipLaunchKernelGGL((shared_join_kernel<T, COLS, KEYS, 4>), dim3((unsigned)heads), dim3(256), 0, st, d, s, so);
+  else hipLaunchKernelGGL((shared_join_kernel<T, COLS, KEYS, 1>), dim3((unsigned)((heads + 3) / 4)), dim3(256), 0, st, d, s, so);
+  return hipGetLastError();
 }
 
 // ---- host ------------------------------------------------------------------------
@@ -910,14 +959,12 @@ hipError_t launch_attend_shared(const DevDesc& d, int dtype, const SharedArgs& s
   so.keys = p.scores.keys;
   so.most_scores_splits = p.scores.most_splits;
   so.scores_wgs = p.scores.wgs;
-  const dim3 join((unsigned)(((long long)a.n_rows * d.Hq + 3) / 4));
   hipError_t e;
   if (dtype == KVR_F32) {
     hipLaunchKernelGGL(shared_f32_kernel, dim3(p.wgs), dim3(64 * SF_WAVES), 0, st, d, s, so);
     e = hipGetLastError();
     if (e != hipSuccess) return e;
-    hipLaunchKernelGGL((shared_join_kernel<float, SF_COLS, SF_KEYS>), join, dim3(256), 0, st, d, s, so);
-    e = hipGetLastError();
+    e = launch_join<float, SF_COLS, SF_KEYS>(d, s, so, st);
     if (e != hipSuccess || !a.scores) return e;
     return single ? launch_shared_scores(d, dtype, s, so.lse, st) : launch_prompt_scores_f32(d, a, so.lse, st);
   }
@@ -930,8 +977,7 @@ hipError_t launch_attend_shared(const DevDesc& d, int dtype, const SharedArgs& s
   };
   e = a.pages.page_size % 8 == 0 ? launch(std::integral_constant<int, EIGHT_A_PAGE>{}) : launch(std::integral_constant<int, ANYWHERE>{});
   if (e != hipSuccess) return e;
-  hipLaunchKernelGGL((shared_join_kernel<bf16_t, SH_COLS, SH_KEYS>), join, dim3(256), 0, st, d, s, so);
-  e = hipGetLastError();
+  e = launch_join<bf16_t, SH_COLS, SH_KEYS>(d, s, so, st);
   if (e != hipSuccess || !a.scores) return e;
   return single ? launch_shared_scores(d, dtype, s, so.lse, st) : launch_prompt_scores_bf16(d, a, p.scores, so.lse, base + p.off_scores, st);
 }
