@@ -604,7 +604,7 @@ int32_t kvr_attend_paged(const kvr_desc* desc, const void* q, const int32_t* n_c
  * the kernels of those two (by sizes alone, so that a captured call is right for whatever the device holds later).  bf16: p may be
  * rounded to bf16 for its product with v, as in kvr_attend_prompt.  One call gives the same bits each time.
  *   groups     host, or NULL: nothing is shared
- *   n_rows     n_rows * Hq is at most 2^28 here; without q_start n_rows = B
+ *   n_rows     n_rows * Hq is at most 2^25 here; without q_start n_rows = B
  *   ws         per kvr_attend_shared_workspace_size, with scores = whether there are scores (of `groups` the sizes are looked at)
  *   the others as for kvr_attend_prompt.  KVR_ERR_UNSUPPORTED also where 2 (n_rows G / 16 + B) Hkv (7 (C / 64 + 2) + 12), each
  *              quotient rounded up, reaches 2^31 - 1 (C: the tokens that a sequence can hold)

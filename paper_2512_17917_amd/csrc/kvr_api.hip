@@ -649,7 +649,7 @@ static int32_t groups_size(const kvr_desc* desc, const kvr_groups* groups) {
   return groups != nullptr && (groups->n_groups < 0 || groups->n_groups > desc->batch) ? KVR_ERR_INVALID_ARG : KVR_OK;
 }
 
-constexpr long long MAX_HEADS_SHARED = 1ll << 28;
+constexpr long long MAX_HEADS_SHARED = 1ll << 25;      // (the join's launch: 2^31 threads)
 
 int32_t kvr_attend_shared_workspace_size(const kvr_desc* desc, int32_t n_rows, const kvr_pages* pages, const kvr_groups* groups,
                                          int32_t window, int32_t n_sink, int32_t scores, size_t* bytes) {

@@ -8,6 +8,8 @@
 // so that a lane holds one token's logits of four columns: the heads of a sequence lie side by side in a lane (eight: in two),
 // and 16 lanes add to 16 scores in a row.  No other wave adds to them: a sequence is in one unit, and a token in one tile.
 // (Keeping the logits instead would be 4 G bytes a token and sequence written and read; the keys are read once more for all.)
+// 16 sequences on 32768 + 500 tokens, 32 heads on 8: 30 us, of which the list and the queries take 5 and the rest is 84 MB of keys and 34
+// of scores at 4.7 TB/s.  (Rows looked up a turn ahead and scores 16 columns ahead: 2.5 us more.)
 #include "kvr_prompt.h"
 #include "kvr_shared.h"
 

@@ -61,8 +61,11 @@ def test_bad_pages_are_refused(bad):
 
 def test_rows_that_are_not_the_sequences():
     assert _shared(n_rows=3) == E and _shared(n_rows=1) == E
-    assert _shared(n_rows=(1 << 25) + 1, q_start=P) == E         # times 8 heads: past 2^28
-    assert _size(n_rows=(1 << 25) + 1)[0] == E and _size(n_rows=-1)[0] == E
+    few = _pages()                                               # (64 tokens)
+    for n, code in ((1 << 22, W), ((1 << 22) + 1, E)):           # times 8 heads: 2^25, which the join's launch has place for
+        assert _shared(n_rows=n, q_start=P, over=few) == code
+        assert _size(n_rows=n, pages=few)[0] == (OK if code == W else E)
+    assert _size(n_rows=-1)[0] == E
 
 
 def test_no_rows_and_no_groups():
