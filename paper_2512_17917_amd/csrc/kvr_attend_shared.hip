@@ -774,6 +774,54 @@ __global__ __launch_bounds__(64 * SF_WAVES) void shared_f32_kernel(DevDesc d, Sh
   }
 }
 
+// Adds pieces i0 .. i0 + 7, and so on every `step`, of those that stand from first[0] and then from first[1] on, to a maximum, sum and
+// this lane's two channels.
+__device__ __forceinline__ void add_pieces(const SharedOut& so, const int (&n)[2], const size_t (&first)[2], int cols, int all, int start, int step,
+                                           int lane, float& m, float& l, float& y0, float& y1) {
+  const float NEG_INF = -__builtin_inff();
+  for (int i0 = start; i0 < all; i0 += step) {
+    float2 ml[8], v[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const int i = min(i0 + e, all - 1);
+      const size_t slot = i < n[0] ? first[0] + (size_t)cols * i : first[1] + (size_t)cols * (i - n[0]);
+      ml[e] = *reinterpret_cast<const float2*>(so.part_ml + 2 * slot);
+      v[e] = *reinterpret_cast<const float2*>(so.part_o + slot * D + 2 * lane);
+      if (i0 + e >= all) {
+        ml[e] = make_float2(NEG_INF, 0.f);
+        v[e] = make_float2(0.f, 0.f);
+      }
+    }
+    float mn = m;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) mn = fmaxf(mn, ml[e].x);
+    const float m_use = mn == NEG_INF ? 0.f : mn, f = exp2_(m - m_use);
+    l *= f;
+    y0 *= f;
+    y1 *= f;
+    m = mn;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const float wt = exp2_(ml[e].x - m_use);    // (a piece without a logit above -inf: 0 times sums of 0, or of NaN)
+      l = fmaf(wt, ml[e].y, l);
+      y0 = fmaf(wt, v[e].x, y0);
+      y1 = fmaf(wt, v[e].y, y1);
+    }
+  }
+}
+// out and lse of a row and head
+template <typename T>
+__device__ __forceinline__ void write_joined(const PagedArgs& a, const SharedOut& so, size_t at, int lane, float m, float l, float y0, float y1) {
+  const float inv = l == 0.f ? 0.f : 1.f / l;
+  if constexpr (sizeof(T) == 2) {
+    const bf16x2_t r = __builtin_convertvector((f32x2_t{y0 * inv, y1 * inv}), bf16x2_t);
+    reinterpret_cast<uint32_t*>((bf16_t*)a.out + at * D)[lane] = __builtin_bit_cast(uint32_t, r);
+  } else {
+    *reinterpret_cast<float2*>((float*)a.out + at * D + 2 * lane) = make_float2(y0 * inv, y1 * inv);
+  }
+  if (so.lse && lane == 0) so.lse[at] = l == 0.f ? __builtin_inff() : m + __builtin_amdgcn_logf(l);
+}
+
 // ---- the pieces of a row and head joined: by WAVES waves, which take eight pieces in turn and ask for all their numbers at once; lane
 // l has channels 2 l and 2 l + 1.  Bound by round trips: lengths, span, then eight pieces a trip.
 template <typename T, int COLS, int KEYS, int WAVES>
@@ -808,35 +856,7 @@ __global__ __launch_bounds__(256) void shared_join_kernel(DevDesc d, SharedArgs 
   const int all = n[0] + n[1];
   const float NEG_INF = -__builtin_inff();
   float m = NEG_INF, l = 0.f, y0 = 0.f, y1 = 0.f;
-  for (int i0 = 8 * part; i0 < all; i0 += 8 * WAVES) {
-    float2 ml[8], v[8];
-#pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      const int i = min(i0 + e, all - 1);
-      const size_t slot = i < n[0] ? first[0] + (size_t)COLS * i : first[1] + (size_t)COLS * (i - n[0]);
-      ml[e] = *reinterpret_cast<const float2*>(so.part_ml + 2 * slot);
-      v[e] = *reinterpret_cast<const float2*>(so.part_o + slot * D + 2 * lane);
-      if (i0 + e >= all) {
-        ml[e] = make_float2(NEG_INF, 0.f);
-        v[e] = make_float2(0.f, 0.f);
-      }
-    }
-    float mn = m;
-#pragma unroll
-    for (int e = 0; e < 8; ++e) mn = fmaxf(mn, ml[e].x);
-    const float m_use = mn == NEG_INF ? 0.f : mn, f = exp2_(m - m_use);
-    l *= f;
-    y0 *= f;
-    y1 *= f;
-    m = mn;
-#pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      const float wt = exp2_(ml[e].x - m_use);    // (a piece without a logit above -inf: 0 times sums of 0, or of NaN)
-      l = fmaf(wt, ml[e].y, l);
-      y0 = fmaf(wt, v[e].x, y0);
-      y1 = fmaf(wt, v[e].y, y1);
-    }
-  }
+  add_pieces(so, n, first, COLS, all, 8 * part, 8 * WAVES, lane, m, l, y0, y1);
   if constexpr (WAVES > 1) {
     s_o[part][lane] = make_float2(y0, y1);
     if (lane == 0) s_ml[part] = make_float2(m, l);
@@ -858,18 +878,203 @@ __global__ __launch_bounds__(256) void shared_join_kernel(DevDesc d, SharedArgs 
       y1 = fmaf(wt, s_o[e][lane].y, y1);
     }
   }
-  const float inv = l == 0.f ? 0.f : 1.f / l;
-  if constexpr (sizeof(T) == 2) {
-    const bf16x2_t r = __builtin_convertvector((f32x2_t{y0 * inv, y1 * inv}), bf16x2_t);
-    reinterpret_cast<uint32_t*>((bf16_t*)a.out + at * D)[lane] = __builtin_bit_cast(uint32_t, r);
-  } else {
-    *reinterpret_cast<float2*>((float*)a.out + at * D + 2 * lane) = make_float2(y0 * inv, y1 * inv);
+  write_joined<T>(a, so, (size_t)at, lane, m, l, y0, y1);
+}
+
+// ---- the same for many sequences of one new row each, with their own tokens where those are few: four waves for a sequence and kv head
+// take 64 tokens each, keys and values straight from the pages.
+// (As units these are a tile or two and a start and an end that cost more than those: 1212 sequences with 94 tokens each behind 768, 16
+// heads on 8, with scores, 348 and 210 us, 378 with one behind 878 134 and 79; a large batch is at the bytes of its ends, 4 to 5 TB/s.)
+// Logits as S = Q K^T, four heads of a token in a lane; softmax with a token a lane; p v in float32, 16 bytes of a row a lane; then a wave
+// joins a head's parts with the pieces of what is shared, and the tokens' scores are added, whose logits the lanes still have.
+constexpr int SO_WAVES = 4, SO_MOST = 64 * SO_WAVES;
+template <typename F>
+__device__ __forceinline__ float lanes16(float x, F f) {        // over the 16 lanes of a row
+  x = f(x, __uint_as_float(__builtin_amdgcn_update_dpp(0, __float_as_uint(x), 0x128, 0xf, 0xf, false)));
+  x = f(x, __uint_as_float(__builtin_amdgcn_update_dpp(0, __float_as_uint(x), 0x124, 0xf, 0xf, false)));
+  x = f(x, __uint_as_float(__builtin_amdgcn_update_dpp(0, __float_as_uint(x), 0x122, 0xf, 0xf, false)));
+  return f(x, __uint_as_float(__builtin_amdgcn_update_dpp(0, __float_as_uint(x), 0x121, 0xf, 0xf, false)));
+}
+
+template <typename T, int G, int COLS, int KEYS>
+__global__ __launch_bounds__(64 * SO_WAVES, 4) void shared_own_kernel(DevDesc d, SharedArgs args, SharedOut so) {
+  typedef WorkRow<COLS, KEYS> Row;
+  constexpr int ROW = D * (int)sizeof(T), STEPS = ROW / 64;
+  constexpr int IN_ROW = ROW / 16, ROWS = 64 / IN_ROW, CH = 16 / (int)sizeof(T);       // lanes a row of values, rows at once, channels a lane
+  __shared__ __align__(16) float s_p[SO_WAVES][64][G];          // logits, then weights, of a token
+  __shared__ __align__(16) float s_o[SO_WAVES][G][D];
+  __shared__ float2 s_ml[SO_WAVES][G];
+  __shared__ float s_lse[G];
+  const PagedArgs& a = args.a;
+  const int lane = threadIdx.x & 63, wave = uniform((int)(threadIdx.x >> 6));
+  const int r4 = lane >> 4, col = lane & 15;
+  const int b = uniform((int)(blockIdx.x / (unsigned)d.Hkv)), h = (int)blockIdx.x - b * d.Hkv;
+  const float NEG_INF = -__builtin_inff(), scale2 = d.scale * LOG2E;
+  Group x = {0, 0, 0, 0, 0};
+  const int g0 = group_of_seq(args, d.B, b);
+  if (g0 >= 0) x = group_at(args, d.B, g0);
+  const Member mem = member_at(args, b, b >= x.b0 && b < x.b1 ? x.common : 0);
+  const int n = mem.n, from = mem.from;
+  const int own = own_in_join(args, mem) ? n - from : 0, chunks = (own + 63) >> 6;
+  const int j = from + 64 * wave + lane, some = min(max(own - 64 * wave, 0), 64);      // this lane's token, and how many its wave has
+  int row = -1;                                                 // where it lies, if the sequence's query sees it
+  if (lane < some) {
+    const long long r = page_row(a.pages, d.Hkv, b, h, j);
+    row = sees(a.vis, n - 1, j) ? (int)r : -1;
   }
-  if (so.lse && lane == 0) so.lse[at] = l == 0.f ? __builtin_inff() : m + __builtin_amdgcn_logf(l);
+  const size_t head0 = (size_t)b * d.Hq + h * G;
+  // logits
+  if (some > 0) {
+    u32x4_t q[STEPS];
+#pragma unroll
+    for (int c = 0; c < STEPS; ++c)
+      q[c] = col < G ? *reinterpret_cast<const u32x4_t*>((const unsigned char*)a.q + (head0 + col) * ROW + 64 * c + 16 * r4) : u32x4_t{0, 0, 0, 0};
+#pragma unroll
+    for (int t0 = 0; t0 < 64; t0 += 16) {
+      if (t0 >= some) break;
+      const int at = __shfl(row, t0 + col);
+      const unsigned char* kp = (const unsigned char*)a.pages.k + (size_t)max(at, 0) * ROW + 16 * r4;
+      u32x4_t k[STEPS];
+#pragma unroll
+      for (int c = 0; c < STEPS; ++c) k[c] = *reinterpret_cast<const u32x4_t*>(kp + 64 * c);
+      f32x4_t s = {0.f, 0.f, 0.f, 0.f};
+      if constexpr (sizeof(T) == 2) {
+#pragma unroll
+        for (int c = 0; c < STEPS; ++c)
+          s = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, q[c]), __builtin_bit_cast(bf16x8_t, k[c]), s, 0, 0, 0);
+      } else {
+        f32x4_t t[4] = {s, s, s, s};
+#pragma unroll
+        for (int c = 0; c < STEPS; ++c)
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            t[e] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(q[c][e]), __uint_as_float(k[c][e]), t[e], 0, 0, 0);
+        s = (t[0] + t[1]) + (t[2] + t[3]);
+      }
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        if (4 * r4 + e < G) s_p[wave][t0 + col][4 * r4 + e] = s[e] * scale2;
+    }
+  }
+  __syncthreads();
+  // weights
+  float lg[G];
+#pragma unroll
+  for (int g = 0; g < G; ++g) lg[g] = row >= 0 ? s_p[wave][lane][g] : NEG_INF;
+  if (some > 0) {
+#pragma unroll
+    for (int g = 0; g < G; ++g) {
+      const float m = rows_max(lanes16(lg[g], [](float u, float v) { return fmaxf(u, v); })), m_use = m == NEG_INF ? 0.f : m;
+      const float p = exp2_(lg[g] - m_use), l = rows_sum(lanes16(p, [](float u, float v) { return u + v; }));
+      s_p[wave][lane][g] = p;
+      if (lane == 0) s_ml[wave][g] = make_float2(m, l);
+    }
+  }
+  __syncthreads();
+  // p v
+  if (some > 0) {
+    float o[G][CH];
+#pragma unroll
+    for (int g = 0; g < G; ++g)
+#pragma unroll
+      for (int c = 0; c < CH; ++c) o[g][c] = 0.f;
+    constexpr int AHEAD = 8;
+    for (int t0 = 0; t0 < some; t0 += AHEAD * ROWS) {
+      u32x4_t v[AHEAD];
+      int at[AHEAD];
+#pragma unroll
+      for (int i = 0; i < AHEAD; ++i) {
+        at[i] = __shfl(row, t0 + ROWS * i + lane / IN_ROW);
+        v[i] = at[i] >= 0 ? *reinterpret_cast<const u32x4_t*>((const unsigned char*)a.pages.v + (size_t)at[i] * ROW + lane % IN_ROW * 16) : u32x4_t{0, 0, 0, 0};
+      }
+#pragma unroll
+      for (int i = 0; i < AHEAD; ++i) {
+        const float* p = s_p[wave][t0 + ROWS * i + lane / IN_ROW];
+        float y[CH];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          if constexpr (sizeof(T) == 2) {
+            y[2 * e] = __uint_as_float(v[i][e] << 16);
+            y[2 * e + 1] = __uint_as_float(v[i][e] & 0xffff0000u);
+          } else {
+            y[e] = __uint_as_float(v[i][e]);
+          }
+        }
+#pragma unroll
+        for (int g = 0; g < G; ++g)
+#pragma unroll
+          for (int c = 0; c < CH; ++c) o[g][c] = fmaf(p[g], y[c], o[g][c]);
+      }
+    }
+#pragma unroll
+    for (int g = 0; g < G; ++g)
+#pragma unroll
+      for (int c = 0; c < CH; ++c) {
+        if (sizeof(T) == 2) o[g][c] = rows_sum(o[g][c]);
+        else o[g][c] = across_sum(o[g][c]);
+      }
+    if (lane < IN_ROW)
+#pragma unroll
+      for (int g = 0; g < G; ++g)
+#pragma unroll
+        for (int c = 0; c < CH; c += 4) *reinterpret_cast<f32x4_t*>(&s_o[wave][g][CH * lane + c]) = f32x4_t{o[g][c], o[g][c + 1], o[g][c + 2], o[g][c + 3]};
+  }
+  __syncthreads();
+  // the parts of a head
+  for (int g = wave; g < G; g += SO_WAVES) {
+    int pieces[2] = {0, 0};
+    size_t first[2] = {0, 0};
+#pragma unroll
+    for (int mine = 0; mine < 2; ++mine) {
+      if (mine ? Row::member_run(args, mem).n == 0 : from == 0 || Row::group_run(args, x).n == 0) continue;
+      const int row0 = mine ? b : x.row0, cols = (mine ? 1 : x.rows) * G;
+      const int m = (b - row0) * G + g, ct = m / COLS;
+      const int c0 = Row::place(d, a.n_rows, mine, row0, cols, ct, h);
+      const int w0 = clampi(listed(so.span + 2 * (size_t)c0), 0, so.wgs - 1);
+      pieces[mine] = clampi(listed(so.span + 2 * (size_t)c0 + 1), w0, so.wgs - 1) - w0 + 1;
+      first[mine] = (size_t)COLS * w0 + c0 + (m - ct * COLS);
+    }
+    const int all = pieces[0] + pieces[1];
+    float m = NEG_INF, l = 0.f, y0 = 0.f, y1 = 0.f;
+    for (int i = 0; i < chunks; ++i) m = fmaxf(m, s_ml[i][g].x);
+    float m_use = m == NEG_INF ? 0.f : m;
+    for (int i = 0; i < chunks; ++i) {
+      const float2 ml = s_ml[i][g], v = *reinterpret_cast<const float2*>(&s_o[i][g][2 * lane]);
+      const float f = exp2_(ml.x - m_use);
+      l = fmaf(f, ml.y, l);
+      y0 = fmaf(f, v.x, y0);
+      y1 = fmaf(f, v.y, y1);
+    }
+    add_pieces(so, pieces, first, COLS, all, 0, 8, lane, m, l, y0, y1);
+    const size_t at = head0 + g;
+    write_joined<T>(a, so, at, lane, m, l, y0, y1);
+    if (lane == 0) s_lse[g] = l == 0.f ? __builtin_inff() : m + __builtin_amdgcn_logf(l);
+  }
+  // its own tokens' scores
+  if (a.scores == nullptr) return;
+  __syncthreads();
+  if (row < 0 || j >= a.n_cap) return;
+  float sum = 0.f;
+#pragma unroll
+  for (int g = 0; g < G; ++g) sum += exp2_(lg[g] - s_lse[g]);
+  a.scores[((size_t)b * d.Hkv + h) * a.n_cap + j] += sum;
+}
+
+template <typename T, int COLS, int KEYS>
+hipError_t launch_own(const DevDesc& d, const SharedArgs& s, const SharedOut& so, hipStream_t st) {
+  const dim3 grid((unsigned)(d.B * d.Hkv)), block(64 * SO_WAVES);
+  switch (d.G) {
+    case 1: hipLaunchKernelGGL((shared_own_kernel<T, 1, COLS, KEYS>), grid, block, 0, st, d, s, so); break;
+    case 2: hipLaunchKernelGGL((shared_own_kernel<T, 2, COLS, KEYS>), grid, block, 0, st, d, s, so); break;
+    case 4: hipLaunchKernelGGL((shared_own_kernel<T, 4, COLS, KEYS>), grid, block, 0, st, d, s, so); break;
+    default: hipLaunchKernelGGL((shared_own_kernel<T, 8, COLS, KEYS>), grid, block, 0, st, d, s, so);
+  }
+  return hipGetLastError();
 }
 
 template <typename T, int COLS, int KEYS>
 hipError_t launch_join(const DevDesc& d, const SharedArgs& s, const SharedOut& so, hipStream_t st) {
+  if (s.own_most > 0) return launch_own<T, COLS, KEYS>(d, s, so, st);
   const long long heads = (long long)s.a.n_rows * d.Hq;
   // (one wave or four, whole calls: 64 rows and heads of 66 pieces 113 and 111 us, 512 of 30 95.6 and 94.7, 1792 105.8 and 107.6,
   // 2048 78.1 and 79.3)
@@ -948,9 +1153,14 @@ size_t attend_shared_ws(const DevDesc& d, int dtype, long long n_rows, long long
   return most;
 }
 
-hipError_t launch_attend_shared(const DevDesc& d, int dtype, const SharedArgs& s, hipStream_t st) {
+hipError_t launch_attend_shared(const DevDesc& d, int dtype, const SharedArgs& given, hipStream_t st) {
+  SharedArgs s = given;
   const PagedArgs& a = s.a;
   const bool single = a.q_start == nullptr;                     // one new token per sequence
+  const long long units = (long long)d.B * d.Hkv;
+  // (units of their own and in the join, 32 heads on 8, 4096 shared: 32 sequences with 8 or 60 tokens more each 27 and 29 to 32 us, with scores,
+  // whose pass is rid of them too, 46 and 49; 64 34 and 36, 74 and 64; 128 48 and 44; 256 75 and 63, with 200 tokens 104 and 97)
+  s.own_most = single && units >= (a.scores ? 512 : 1024) && units <= 1 << 23 ? SO_MOST : 0;
   const Route r = route(d, dtype, a.n_rows, a.pages.cap, a.vis, s.n_groups, single, a.scores != nullptr);
   if (r == PAGED) return launch_attend_paged(d, dtype, a, st);
   if (r == PROMPT) return launch_attend_prompt(d, dtype, a, st);

@@ -3,7 +3,7 @@
 // sum, which the attention kernels left.
 //
 // The row of units is that of the attention (kvr_shared.h); what is shared is read once for a group here too, its keys alone.
-// A workgroup puts the queries of its unit's columns into LDS (64 KB) and its waves take every eighth tile of 64 tokens, each for itself:
+// A workgroup puts the queries of its unit's columns into LDS and its waves take every eighth tile of 64 tokens, each for itself:
 // keys in registers, straight from the pages, S = Q K^T (columns x keys, v_mfma_f32_16x16x32_bf16, or four channels a step in float32),
 // so that a lane holds one token's logits of four columns: the heads of a sequence lie side by side in a lane (eight: in two),
 // and 16 lanes add to 16 scores in a row.  No other wave adds to them: a sequence is in one unit, and a token in one tile.
@@ -18,16 +18,18 @@ namespace kvr {
 namespace {
 
 constexpr int SS_WAVES = 8, SS_KEYS = 64;
-template <typename T> constexpr int SS_COLS = sizeof(T) == 2 ? 256 : 128;        // of a workgroup: 64 KB of queries
+// Columns of a workgroup.  (Keys are read once for so many; more of them, with 256 in bf16, leave too few waves with a chain of scores read
+// and written each: 128 sequences on 4096 + 60 tokens 93 and 77 us for the whole call, 16 on 32768 + 500 95 either way.)
+constexpr int SS_COLS = 64;
 typedef float f32x4_t __attribute__((ext_vector_type(4)));
 
 template <typename T>
 struct ScoresLds {
-  unsigned char q[SS_COLS<T>][D * sizeof(T)];       // piece c (16 bytes) of column m at c ^ (m mod 16)
-  float lse[SS_COLS<T>];
-  int pos[SS_COLS<T>];                              // last token that a column sees, -1: none of the unit's
+  unsigned char q[SS_COLS][D * sizeof(T)];       // piece c (16 bytes) of column m at c ^ (m mod 16)
+  float lse[SS_COLS];
+  int pos[SS_COLS];                              // last token that a column sees, -1: none of the unit's
   Piece list[PIECES];
-  typename WorkRow<SS_COLS<T>, SS_KEYS, true>::Scratch scratch;
+  typename WorkRow<SS_COLS, SS_KEYS, true>::Scratch scratch;
 };
 
 // tokens of a wave's turn: keys of as many blocks of 16 as registers hold
@@ -37,7 +39,7 @@ template <typename T, int G>
 __global__ __launch_bounds__(64 * SS_WAVES, 4) void shared_scores_kernel(DevDesc d, SharedArgs args, const float* lse) {
   extern __shared__ __align__(1024) unsigned char s_mem[];
   ScoresLds<T>& lds = *reinterpret_cast<ScoresLds<T>*>(s_mem);
-  typedef WorkRow<SS_COLS<T>, SS_KEYS, true> Row;
+  typedef WorkRow<SS_COLS, SS_KEYS, true> Row;
   constexpr int BLOCKS = SS_BLOCKS<T>, TURNS = 4 / BLOCKS, STEPS = D * (int)sizeof(T) / 64;      // turns a tile, 64-byte steps of a row
   constexpr int ROW = D * sizeof(T);
   const PagedArgs& a = args.a;
@@ -53,7 +55,7 @@ __global__ __launch_bounds__(64 * SS_WAVES, 4) void shared_scores_kernel(DevDesc
       const Piece& u = lds.list[now];
       const int i0 = uniform(u.i0), i1 = uniform(u.i1);
       if (i0 >= i1) continue;
-      const int own = uniform(u.bits) & PIECE_OWN, c0 = uniform(u.ct) * SS_COLS<T>, some = min(uniform(u.cols) - c0, SS_COLS<T>);
+      const int own = uniform(u.bits) & PIECE_OWN, c0 = uniform(u.ct) * SS_COLS, some = min(uniform(u.cols) - c0, SS_COLS);
       const int h = uniform(u.h), row0 = uniform(u.row0), b = uniform(u.b), from = uniform(u.from), lim = uniform(u.lim), hi = uniform(u.hi);
       const Run run = {uniform(u.ahead0), uniform(u.ahead), uniform(u.start), 0};
       // the columns: their queries, lse and last tokens (a row is a sequence's only one)

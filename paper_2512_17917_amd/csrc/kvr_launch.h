@@ -312,6 +312,7 @@ struct SharedArgs {
   const int32_t* start;             // of the groups, [n_groups + 1]
   const int32_t* n_shared;
   int n_groups;
+  int own_most;                     // a sequence with no more own tokens than these is no unit: the join attends to them (one row each)
 };
 // (one new token per sequence)
 hipError_t launch_shared_scores(const DevDesc& d, int dtype, const SharedArgs& s, const float* lse, hipStream_t st);

@@ -73,6 +73,9 @@ __host__ __device__ __forceinline__ Member member_at(const SharedArgs& s, int b,
   return r;
 }
 
+// whether the join attends to a sequence's own tokens (the sinks among them that its window leaves)
+__host__ __device__ __forceinline__ bool own_in_join(const SharedArgs& s, const Member& m) { return s.own_most > 0 && m.n - m.from <= s.own_most; }
+
 // A piece of a unit, as a workgroup lists those that it has: tiles i0 .. i1-1 of its run.
 struct Piece {
   int bits;                         // OWN: of a sequence; FIRST, LAST: it has the unit's first tile, its last
@@ -110,7 +113,7 @@ struct WorkRow {
     return g.common > 0 && g.rows > 0 ? run_of<KEYS>(s.a.vis, 0, g.common, g.common - 1) : Run{0, 0, 0, 0};
   }
   __host__ __device__ static __forceinline__ Run member_run(const SharedArgs& s, const Member& m) {
-    return m.span.n > 0 ? run_of<KEYS>(s.a.vis, m.from, m.n - m.span.n, m.n - 1) : Run{0, 0, 0, 0};
+    return m.span.n > 0 && !own_in_join(s, m) ? run_of<KEYS>(s.a.vis, m.from, m.n - m.span.n, m.n - 1) : Run{0, 0, 0, 0};
   }
   // columns of the units before one
   __host__ __device__ static __forceinline__ int place(const DevDesc& d, int n_rows, bool own, int row0, int cols, int ct, int h) {

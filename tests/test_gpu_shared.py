@@ -304,3 +304,49 @@ def test_a_place_for_fewer_scores_than_tokens():
     (BF, [(5 + i, one(6 + i, 7 + i, 90)) for i in range(70)], (2, 2)), (BF, [(100 + i, one(*[101 + i + j for j in range(6)])) for i in range(150)], (2, 2))])
 def test_long_ones_and_many(dtype, groups, heads):
     Batch(groups, heads, 16, dtype, 22, rows=False).check()
+
+
+def _ends(members, common, most):
+    """Sequences with ends of one token to `most` behind what they share, one without, one shorter, one empty."""
+    n = [common + 1 + (i * i * 13 + 5 * i) % most for i in range(members)]
+    n[1], n[2], n[3 % members] = common, max(common - 70, 0), 0
+    n[4], n[5] = common + 256, common + 257                     # as many as the join takes, and one more
+    return common, one(*n)
+
+
+ENDS = [  # groups, heads, page, window, first tokens: sequences times kv heads from 512 on, whose last tokens the join attends to
+    ([_ends(64, 500, 200)], (8, 8), 16, 0, 0),
+    ([_ends(40, 640, 300), _ends(30, 64, 90)], (16, 8), 24, 0, 0),
+    ([_ends(66, 300, 64)], (32, 8), 5, 0, 0),
+    ([_ends(20, 1000, 256), _ends(49, 3, 300)], (64, 8), 64, 0, 0),
+    ([_ends(64, 500, 300)], (32, 8), 16, 150, 5),
+    ([_ends(70, 200, 300)], (8, 8), 7, 30, 230),
+]
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("case", range(len(ENDS)))
+def test_many_sequences_with_short_ends(case, dtype):
+    """Also with pages that are not there, values that are not finite, and fewer scores than tokens."""
+    groups, heads, page, window, sink = ENDS[case]
+    b = Batch(groups, heads, page, dtype, 90 + case, rows=False, room=20000 if window == 0 else 30000)
+    out, sc = b.check(window, sink)
+    b.g.manual_seed(90)
+    first = b.check(window, sink)
+    b.g.manual_seed(90)
+    again = b.check(window, sink)
+    assert all(torch.equal(x, y) for x, y in zip(first, again))
+    b.check(window, sink, scores=False)
+    for s in range(6, 20, 3):                                    # pages behind what is shared
+        last = (b.n[s] - 1) // page
+        if last * page >= groups[0][0]:
+            b.table[s, last] = -1 if s % 2 else 1 << 20
+    for s, what in ((7, math.inf), (8, math.nan), (10, -math.inf)):
+        at = R.token_row(b.v, b.table, s, b.n[s] - 1)
+        if at is not None and b.n[s] > groups[0][0]:
+            b.v[at[0], 2, at[1], 77] = what
+            if b.n[s] % page:                                    # and behind its end
+                b.k[at[0], :, b.n[s] % page:] = math.nan
+                b.v[at[0], :, b.n[s] % page:] = math.nan
+    b.n_cap = groups[0][0] + 40
+    b.check(window, sink)

@@ -276,7 +276,7 @@ PROBE = r"""
 #include <cstdio>
 #include <vector>
 #include "kvr_shared.h"
-// One batch: which row, workgroups, B G Hkv n_rows cap window n_sink n_groups, then n_ctx, whether there are starts and they, groups' starts, tokens in
+// One batch: which row, workgroups, B G Hkv n_rows cap window n_sink n_groups, own tokens that the join takes, then n_ctx, whether there are starts and they, groups' starts, tokens in
 // common -> a line a piece: workgroup, of a sequence, its or the group's number, tile of columns, head, columns' place, columns, bits, from, lim, run, i0, i1
 using namespace kvr;
 template <typename Row, int COLS>
@@ -318,7 +318,7 @@ int main() {
   while (std::scanf("%d %d", &which, &wgs) == 2) {
     DevDesc d = {};
     SharedArgs s = {};
-    if (std::scanf("%d %d %d %d %d %d %d %d", &d.B, &d.G, &d.Hkv, &s.a.n_rows, &s.a.pages.cap, &s.a.vis.window, &s.a.vis.n_sink, &s.n_groups) != 8) return 1;
+    if (std::scanf("%d %d %d %d %d %d %d %d %d", &d.B, &d.G, &d.Hkv, &s.a.n_rows, &s.a.pages.cap, &s.a.vis.window, &s.a.vis.n_sink, &s.n_groups, &s.own_most) != 9) return 1;
     d.Hq = d.G * d.Hkv;
     auto list = [](int n) {
       std::vector<int32_t> x(n + 1);
@@ -335,7 +335,7 @@ int main() {
     s.n_shared = common.data();
     if (which == 0) pieces<WorkRow<256, 64>, 256>(d, s, wgs);
     else if (which == 1) pieces<WorkRow<16, 64>, 16>(d, s, wgs);
-    else pieces<WorkRow<256, 64, true>, 256>(d, s, wgs);
+    else pieces<WorkRow<64, 64, true>, 64>(d, s, wgs);
   }
 }
 """
@@ -374,10 +374,13 @@ def _batches():
     return out
 
 
-@pytest.mark.parametrize("which,cols,wgs", [(0, 256, 256), (1, 16, 512), (2, 256, 512), (0, 256, 3), (1, 16, 1)])
-def test_every_tile_of_every_unit_is_taken_once(ask, which, cols, wgs):
+@pytest.mark.parametrize("most_own", [0, 256])
+@pytest.mark.parametrize("which,cols,wgs", [(0, 256, 256), (1, 16, 512), (2, 64, 512), (0, 256, 3), (1, 16, 1)])
+def test_every_tile_of_every_unit_is_taken_once(ask, which, cols, wgs, most_own):
     for B, G, Hkv, n_rows, cap, window, sink, n, q_start, cuts, common, y in _batches():
-        words = [which, wgs, B, G, Hkv, n_rows, cap, window, sink, len(common), *n, int(q_start is not None), *(q_start or []), *cuts, *common]
+        if most_own and q_start is not None:
+            continue                                             # (one new row a sequence alone)
+        words = [which, wgs, B, G, Hkv, n_rows, cap, window, sink, len(common), most_own, *n, int(q_start is not None), *(q_start or []), *cuts, *common]
         lines = ask(" ".join(map(str, words)))
         assert lines[-1] == "end"
         length = int(lines[0])
@@ -420,4 +423,9 @@ def test_every_tile_of_every_unit_is_taken_once(ask, which, cols, wgs):
                     for k in range(u["tiles"]):
                         at = ahead0 + 64 * k if k < ahead else start + 64 * (k - ahead)
                         held += range(max(at, u["lo"]), min(at + 64, u["lim"]))
+                if most_own and (1, b, 0, 0) not in units:       # the join's: its last tokens, no more than it takes
+                    left = seen - set(held)
+                    assert not left or m - min(left) <= most_own
+                    assert not left or not held or max(held) < min(left)
+                    held += left
                 assert len(held) == len(set(held)) and seen <= set(held), (b, t)
