@@ -1126,7 +1126,8 @@ bool attend_shared_fits(const DevDesc& d, long long n_rows, long long cap) {
 // 31.7; with scores, whose pass is a launch more, 131 MB 40.0 and 43.9, 265 MB (16 x 4000) 45.6 and 36.6; float32 66 MB 23.0 and
 // 29.9, 132 MB 40.4 and 31.1.  Several tokens: the prompt's kernel pads a sequence's columns to 256, and is as fast where they are many
 // (8 x 4000 tokens with 2 rows each, 8 columns, 32.1 and 24.1, with 6 rows 32.4 and 31.9, with 12 35.9 and 41.5; 8 x 16000 with 12
-// 87 and 64, with 24 92 and 98).  In float32 it does not share out long caches, and is bound by products where its 16
+// 87 and 64, with 24 92 and 98; many sequences, whose starts and ends add up: 64 of 100 + 400 with 3 rows 36 and 54, 128 of 500 + 100 with 4 76
+// and 68, with 16 83 and 143, of 2000 + 100 with 4 187 and 85).  In float32 it does not share out long caches, and is bound by products where its 16
 // columns a workgroup fill the chip (8 x 4000 with 6 rows, 96 workgroups, 180 and 82; with 24, 384, 195 and 250; 2 x 200 with 6 16.0
 // and 16.6, 8 x 200 16.5 and 26.4).
 enum Route { SHARED, PAGED, PROMPT };
@@ -1138,7 +1139,7 @@ static Route route(const DevDesc& d, int dtype, long long n_rows, long long cap,
   if (n_groups == 0) return PROMPT;
   if (dtype == KVR_F32) return tokens < 512 || n_rows * d.Hq / 16 >= 256 ? PROMPT : SHARED;
   const long long cols = n_rows * d.G / d.B;                    // of a sequence
-  return cols > 64 || mb < 64 + 3 * cols ? PROMPT : SHARED;
+  return cols > 64 || mb < 64 + 3 * cols + (long long)d.B * d.Hkv / 13 ? PROMPT : SHARED;
 }
 
 size_t attend_shared_ws(const DevDesc& d, int dtype, long long n_rows, long long cap, const Visible& vis, int n_groups, bool scores) {

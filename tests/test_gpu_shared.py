@@ -149,6 +149,7 @@ WINDOWS = [  # rows of a sequence at most, groups, heads, page, window, first to
     (1, [_many(1, 560, 70)], (8, 8), 16, 90, 3),
     (4, [_many(4, 40, 500), _many(4, 35, 129), _many(4, 30, 64), _many(4, 25, 1000)], (16, 8), 8, 260, 20),
     (9, [_many(9, 20, 900)], (4, 4), 64, 530, 3),
+    (5, [_many(5, 60, 900), _many(5, 50, 640)], (8, 8), 16, 700, 9),
 ]
 
 
@@ -350,3 +351,19 @@ def test_many_sequences_with_short_ends(case, dtype):
                 b.v[at[0], :, b.n[s] % page:] = math.nan
     b.n_cap = groups[0][0] + 40
     b.check(window, sink)
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+def test_logits_that_are_not_finite_among_many_short_ends(dtype):
+    """NaN in one sequence's query, in a key of another's end, and -Inf as the only logits of a third (one token of its own, no group)."""
+    b = Batch([_ends(64, 200, 150)], (16, 8), 16, dtype, 97, alone=one(1, 40), rows=False, room=20000)
+    b.q[9, 5, 3] = math.nan
+    page, row = R.token_row(b.k, b.table, 12, b.n[12] - 1)
+    b.k[page, 3, row, 0] = math.nan
+    page, row = R.token_row(b.k, b.table, 64, 0)
+    b.k[page, 1, row] = 0
+    k0 = b.k.clone()
+    b.k[page, 1, row, 0] = -math.inf
+    b.q[64, 2:4, 0] = b.q[64, 2:4, 0].abs() + 1
+    k0 = torch.nan_to_num(k0)
+    b.check(nan=[(9, 2, [5]), (12, 3, [6, 7])], finite_k=k0)
