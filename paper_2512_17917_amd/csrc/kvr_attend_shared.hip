@@ -1123,8 +1123,10 @@ bool attend_shared_fits(const DevDesc& d, long long n_rows, long long cap) {
 // Whose kernels a call takes.  Small caches are read sooner by every sequence for itself: what counts is the cache that a batch of
 // the longest sequences would read, by the room that it has (the lengths only the device knows).  One token per sequence, 32 heads on 8,
 // each for itself and shared: 66 MB (4 x 4000) 19.9 and 21.7 us, 68 MB (16 x 1000) 22.2 and 20.1, 131 MB (2 x 16000) 37.5 and
-// 31.7; with scores, whose pass is a launch more, 131 MB 40.0 and 43.9, 265 MB (16 x 4000) 45.6 and 36.6; float32 66 MB 23.0 and
-// 29.9, 132 MB 40.4 and 31.1.  Several tokens: the prompt's kernel pads a sequence's columns to 256, and is as fast where they are many
+// 31.7; with scores, whose pass is a launch more, 131 MB 40.0 and 43.9, 145 MB (32 x 1100) 47.1 and 41.1; float32 66 MB 23.0 and
+// 29.9, 132 MB 40.4 and 31.1.  Room for few tokens, where the paged kernels need one launch: 134 MB (64 x 500) 22.3 and 34.1, with scores 29.3 and
+// 43.9, 268 MB (128 x 500) 45.6 and 38.3, 58.5 and 54.2; 98 MB (250 x 90, whose ends the join takes) 25.4 and 17.9; float32 268 MB (64 x 500)
+// 37.9 and 46.2, 42.6 and 63.8, 838 MB (808 x 19) 157 and 111.  Several tokens: the prompt's kernel pads a sequence's columns to 256, and is as fast where they are many
 // (8 x 4000 tokens with 2 rows each, 8 columns, 32.1 and 24.1, with 6 rows 32.4 and 31.9, with 12 35.9 and 41.5; 8 x 16000 with 12
 // 87 and 64, with 24 92 and 98; many sequences, whose starts and ends add up: 64 of 100 + 400 with 3 rows 36 and 54, 128 of 500 + 100 with 4 76
 // and 68, with 16 83 and 143, of 2000 + 100 with 4 187 and 85).  In float32 it does not share out long caches, and is bound by products where its 16
@@ -1135,7 +1137,12 @@ static Route route(const DevDesc& d, int dtype, long long n_rows, long long cap,
   long long tokens = cap;
   if (vis.window > 0 && (long long)vis.window + vis.n_sink < tokens) tokens = (long long)vis.window + vis.n_sink;
   const long long mb = (long long)d.B * d.Hkv * tokens * D * 2 * (dtype == KVR_F32 ? 4 : 2) / 1000000;
-  if (single) return n_groups == 0 || mb < (scores ? 192 : 72) ? PAGED : SHARED;
+  if (single) {
+    const bool f32 = dtype == KVR_F32;
+    long long least = scores ? (f32 ? 192 : 136) : 72;
+    if (tokens <= 512) least = f32 ? (scores ? 384 : 288) : scores ? 192 : (long long)d.B * d.Hkv < 1024 ? 144 : 72;
+    return n_groups == 0 || mb < least ? PAGED : SHARED;
+  }
   if (n_groups == 0) return PROMPT;
   if (dtype == KVR_F32) return tokens < 512 || n_rows * d.Hq / 16 >= 256 ? PROMPT : SHARED;
   const long long cols = n_rows * d.G / d.B;                    // of a sequence

@@ -322,6 +322,8 @@ ENDS = [  # groups, heads, page, window, first tokens: sequences times kv heads 
     ([_ends(20, 1000, 256), _ends(49, 3, 300)], (64, 8), 64, 0, 0),
     ([_ends(64, 500, 300)], (32, 8), 16, 150, 5),
     ([_ends(70, 200, 300)], (8, 8), 7, 30, 230),
+    ([_ends(64, 900, 300)], (32, 8), 16, 700, 5),
+    ([_ends(70, 450, 300)], (8, 8), 7, 300, 500),
 ]
 
 
