@@ -293,3 +293,51 @@ def test_a_dense_cache_of_copies(dtype):
     ref = R.attend(q, k[:, :, :2701].contiguous(), v[:, :, :2701].contiguous(), None, n, None, d.softmax_scale, 0, 0, 2700, HKV)
     tol = _near(out, ref, dtype)
     assert bool(((sc.cpu().double() - ref["scores"]).abs() <= tol).all())
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+def test_a_captured_call_of_many_sequences_follows_lengths_and_groups(dtype):
+    """Ends that the join attends to become longer than it takes, and shorter again; groups come and go."""
+    g = torch.Generator().manual_seed(35)
+    B, Hq, Hkv, pool = 64, 16, 8, 400
+    d = kvr.make_desc(B, Hq, Hkv, 1, 1, dtype)
+    k, v = (torch.randn(pool, Hkv, PAGE, D, generator=g).to(dtype).cuda() for _ in range(2))
+    table = torch.randint(0, pool, (B, 2000), generator=g, dtype=torch.int32)
+    table[:, :30] = table[0, :30]                                # 480 tokens
+    pages = kvr.make_pages(d, k, v, table.cuda())
+    q = torch.randn(B, Hq, D, generator=g).to(dtype).cuda()
+    i32 = lambda n: torch.zeros(n, dtype=torch.int32, device="cuda")
+    n_ctx, start, common = i32(B), i32(3), i32(2)
+    groups = kvr.make_groups(start, common)
+    out, scores = torch.empty_like(q), torch.empty(B, Hkv, 1500, device="cuda")
+    ws = torch.empty(kvr.kvr_attend_shared_workspace_size(d, B, pages, groups, 0, 0, True), dtype=torch.uint8, device="cuda")
+    run = lambda: kvr.kvr_attend_shared(d, q, B, None, n_ctx, pages, groups, 0, 0, out, scores, 1500, ws)
+    steps = [([481 + i for i in range(B)], [0, 40, 64], [480, 480]), ([481 + 9 * i for i in range(B)], [0, 64, 64], [480, 0]),
+             ([20 * i for i in range(B)], [0, 10, 64], [0, 480]), ([0] * B, [0, 64, 64], [480, 0]), ([1400 - i for i in range(B)], [3, 3, 3], [480, 480]),
+             ([481 + i for i in range(B)], [0, 40, 64], [480, 480])]
+
+    def set_to(n, s, c):
+        for to, x in ((n_ctx, n), (start, s), (common, c)):
+            to.copy_(torch.tensor(x, dtype=torch.int32))
+        out.fill_(3.0)
+        scores.fill_(0.5)
+    set_to(*steps[0])
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        run()
+    want = []
+    for s in steps:
+        set_to(*s)
+        ws.fill_(255)
+        run()
+        want.append((out.clone(), scores.clone()))
+    for s, (o, sc) in zip(steps, want):
+        set_to(*s)
+        ws.random_(0, 255)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, o) and torch.equal(scores, sc)
+        _ = (out.float() @ out.float().transpose(1, 2)).sum().item()
+    ref = R.attend(q.cpu(), k.cpu(), v.cpu(), table, steps[2][0], None, d.softmax_scale, 0, 0, 1500, Hkv)
+    tol = _near(want[2][0], ref, dtype, torch.full((B, Hkv, 1500), 0.5))
+    assert bool(((want[2][1].cpu().double() - 0.5 - ref["scores"]).abs() <= tol).all())
