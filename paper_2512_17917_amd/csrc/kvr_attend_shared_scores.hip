@@ -159,9 +159,7 @@ __global__ __launch_bounds__(64 * SS_WAVES, 4) void shared_scores_kernel(DevDesc
 template <typename T, int G>
 hipError_t launch(const DevDesc& d, const SharedArgs& s, const float* lse, hipStream_t st) {
   constexpr int LDS = sizeof(ScoresLds<T>);
-  static_assert(LDS <= 80 * 1024);
-  const hipError_t e = raise_lds_limit((const void*)shared_scores_kernel<T, G>, LDS);
-  if (e != hipSuccess) return e;
+  static_assert(LDS <= 64 * 1024);              // (which a launch may have as it is)
   hipLaunchKernelGGL((shared_scores_kernel<T, G>), dim3(512), dim3(64 * SS_WAVES), LDS, st, d, s, lse);
   return hipGetLastError();
 }

@@ -333,7 +333,7 @@ struct WorkRow {
 
 // A kernel may be launched with more than 64 KB of LDS where its limit was raised, on each device for itself.
 inline hipError_t raise_lds_limit(const void* kernel, int bytes) {
-  constexpr int DEVICES = 64, KERNELS = 16;
+  constexpr int DEVICES = 64, KERNELS = 4;
   static std::mutex lock;
   static const void* known[DEVICES][KERNELS];
   int dev = 0;
