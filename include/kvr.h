@@ -601,8 +601,9 @@ int32_t kvr_attend_paged(const kvr_desc* desc, const void* q, const int32_t* n_c
  * that begin with the same tokens: out and scores are theirs, but what a group shares is read once for all its rows, and
  * what each sequence has behind it beside that.  A sequence with a new row among the shared tokens is attended by itself,
  * as one of no group is.  A call whose room is too small for sharing to pay, or whose sequences have many new tokens each, takes
- * the kernels of those two (by sizes alone, so that a captured call is right for whatever the device holds later).  bf16: p may be
- * rounded to bf16 for its product with v, as in kvr_attend_prompt.  One call gives the same bits each time.
+ * the kernels of those two (by sizes alone, so that a captured call is right for whatever the device holds later).  bf16: with
+ * q_start p may be rounded to bf16 for its product with v, as in kvr_attend_prompt; without, it is within 2^-15 of itself.  One call
+ * gives the same bits each time.
  *   groups     host, or NULL: nothing is shared
  *   n_rows     n_rows * Hq is at most 2^25 here; without q_start n_rows = B
  *   ws         per kvr_attend_shared_workspace_size, with scores = whether there are scores (of `groups` the sizes are looked at)

@@ -12,10 +12,13 @@
 // straight to LDS, three tiles ahead and past the ends of units.  A wave has 32 columns, and where columns are up to 128 two
 // waves share them and have half the tokens each.
 // A wave computes S = K Q^T (keys x columns, v_mfma_f32_16x16x32_bf16; Q stays in registers), so that a lane holds logits of
-// one column alone; the registers of S, exponentiated and rounded to bf16, are the B operand of O^T = V^T P as they lie (its k
+// one column alone; the registers of S, exponentiated and in bf16, are the B operand of O^T = V^T P as they lie (its k
 // index may be counted in any order as long as V^T has the same), with ds_read_b64_tr_b16 fetching groups of four tokens.
-//   Rounding p to bf16: the matrix unit takes nothing wider at this rate; the error is half a step of the output's type at
-// most, relative to sum p |v|.  Their sum is taken in float32 before it.
+//   p goes to the matrix unit as two bf16 numbers: its upper 16 bits, and the rest, rounded, which leaves an error of 2^-15 p at
+// most.  Their sum, and that of p for l, are in float32.  The rest is taken of p (1 + 2^-20), so that it is never 0 beside an upper part: 0
+// times an infinite value, which belongs to the column, would be NaN (it still is below 2^-106 of the largest weight, where bf16 ends).
+// One number in bf16 was off by half its step, 2^-8, and with it sums that cancel; it took 79 us for 64 on 8k (two: 81), 136 for 256
+// on 4k (145), 46 for 8 x 6 rows on 16k (51), where the bytes bound it the same.
 //   The running maximum moves only when it is passed by more than 8 (in powers of two): p then stays below 2^8.
 // At a unit's end waves with the same columns are joined in the tile's place in LDS, which is free until the next step.
 //
@@ -58,6 +61,7 @@ struct SharedLds {
 constexpr int SH_LDS = sizeof(SharedLds);
 static_assert(SH_LDS <= 160 * 1024);
 constexpr float KEEP_MAX = 8.f;
+constexpr float SPLIT = 1.f + 0x1p-20f;                         // (see p above)
 constexpr int SF_WAVES = 4, SF_COLS = 16, SF_KEYS = 64;
 typedef WorkRow<SF_COLS, SF_KEYS> RowF32;
 typedef float f32x4_t __attribute__((ext_vector_type(4)));
@@ -438,7 +442,7 @@ __global__ __launch_bounds__(64 * SH_WAVES, 2) void shared_bf16_kernel(DevDesc d
         m_run[n] = m_new;
       }
     }
-    bf16x8_t p[N];
+    bf16x8_t p[N], rest[N];
 #pragma unroll
     for (int n = 0; n < N; ++n) {
       const float m_use = m_run[n] == NEG_INF ? 0.f : m_run[n];
@@ -447,19 +451,25 @@ __global__ __launch_bounds__(64 * SH_WAVES, 2) void shared_bf16_kernel(DevDesc d
 #pragma unroll
         for (int x = 0; x < 4; x += 2) {
           const f32x2_t y = {exp2_(fmaf(s[n][b][x], sc.c, -m_use)), exp2_(fmaf(s[n][b][x + 1], sc.c, -m_use))};
-          const bf16x2_t z = __builtin_convertvector(y, bf16x2_t);
+          const uint32_t y0 = __float_as_uint(y[0]), y1 = __float_as_uint(y[1]);
+          const f32x2_t left = {fmaf(y[0], SPLIT, -__uint_as_float(y0 & 0xffff0000u)), fmaf(y[1], SPLIT, -__uint_as_float(y1 & 0xffff0000u))};
+          const bf16x2_t upper = __builtin_bit_cast(bf16x2_t, __builtin_amdgcn_perm(y1, y0, 0x07060302u)), lower = __builtin_convertvector(left, bf16x2_t);
           l_run[n] += y[0] + y[1];
-          p[n][4 * b + x] = z[0];
-          p[n][4 * b + x + 1] = z[1];
+          p[n][4 * b + x] = upper[0];
+          p[n][4 * b + x + 1] = upper[1];
+          rest[n][4 * b + x] = lower[0];
+          rest[n][4 * b + x + 1] = lower[1];
         }
     }
     // o += V^T p
 #pragma unroll
     for (int cb = 0; cb < 8; ++cb) {
       const s16x4_t x = v[cb][0], y = v[cb][1];
-      const s16x8_t both = {x[0], x[1], x[2], x[3], y[0], y[1], y[2], y[3]};
+      const bf16x8_t both = __builtin_bit_cast(bf16x8_t, (s16x8_t{x[0], x[1], x[2], x[3], y[0], y[1], y[2], y[3]}));
 #pragma unroll
-      for (int n = 0; n < N; ++n) o[n][cb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, both), p[n], o[n][cb], 0, 0, 0);
+      for (int n = 0; n < N; ++n) o[n][cb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(both, p[n], o[n][cb], 0, 0, 0);
+#pragma unroll
+      for (int n = 0; n < N; ++n) o[n][cb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(both, rest[n], o[n][cb], 0, 0, 0);
     }
   };
   // Values that are not finite, for the columns that see them; their weights once more, from the keys in LDS.

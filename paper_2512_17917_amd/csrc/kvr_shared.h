@@ -100,7 +100,7 @@ struct Share {
 // SCORES: the row of the pass that adds scores, which takes longer with every column
 template <int COLS, int KEYS, bool SCORES = false>
 struct WorkRow {
-  static constexpr int LIGHT = 4, HEAVY = 7;
+  static constexpr int LIGHT = 4, HEAVY = 10;
   // (queries of more than 16 columns are steps of their own, and more of them are joined and written at the end)
   __host__ __device__ static __forceinline__ int cost(int cols) { return SCORES || cols > 16 ? 12 : 5; }
   __host__ __device__ static __forceinline__ int weight(int cols) {
