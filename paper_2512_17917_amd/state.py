@@ -148,7 +148,12 @@ class LayerState:
         if bump_n_ctx:
             self.n_ctx += 1
         if rotation is not None:
-            k_new, q = self.rotate(k_new, q, rotation, axes, pos)
+            try:
+                k_new, q = self.rotate(k_new, q, rotation, axes, pos)
+            except Exception:                                  # refused: the token is not counted, and may be given again
+                if bump_n_ctx:
+                    self.n_ctx -= 1
+                raise
         # Algorithm 3, first branch: does the Recent queue hand its overhang on to the Candidates?
         self.r_size = kvr.kvr_recent_size(self.r_size + 1, self.n_recent, self.slack)
         if fused is None:
@@ -351,6 +356,14 @@ class PagedCache:
         bump_n_ctx as in LayerState.decode_step, pos int32 [n_axes, B] as in prompt.  Returns out [B, Hq, D], reused by the next step."""
         if bump_n_ctx:
             self.n_ctx += 1
+        try:
+            return self._step(q, k, v, pos)
+        except Exception:                                      # refused: the token is not counted, and may be given again
+            if bump_n_ctx:
+                self.n_ctx -= 1
+            raise
+
+    def _step(self, q, k, v, pos):
         _rotate(self.desc, self.rotation, self.axes, pos, q, k, v, self.desc.batch, None, self.n_ctx, self.q, None, self.pages)
         if self.groups is not None:
             kvr.kvr_attend_shared(self.desc, self.q, self.desc.batch, None, self.n_ctx, self.pages, self.groups, self.window,

@@ -1,0 +1,47 @@
+"""Decode steps that are refused, on the CPU: the token is not counted, so that the same step with right arguments follows."""
+import pytest
+import torch
+
+from paper_2512_17917_amd import binding as kvr
+from paper_2512_17917_amd.state import LayerState, PagedCache
+
+AXES = kvr.make_axes([0] * 64)
+POS = torch.zeros(1, 2, dtype=torch.int32)
+
+
+def _paged(axes=None):
+    c = PagedCache.__new__(PagedCache)
+    c.desc = kvr.make_desc(2, 8, 2, 3, 5, torch.bfloat16, seed=1)
+    c.rotation, c.n_ctx, c.q, c.pages, c.groups, c.axes = kvr.make_rotation(c.desc), torch.full((2,), 7, dtype=torch.int32), None, None, None, axes
+    return c
+
+
+def _layer():
+    s = LayerState.__new__(LayerState)
+    s.desc = kvr.make_desc(2, 8, 2, 3, 5, torch.bfloat16, seed=1)
+    s.device, s.dtype = torch.device("cpu"), torch.bfloat16
+    s.k_turned, s.q_turned, s.n_ctx, s.r_size = None, None, torch.full((2,), 7, dtype=torch.int32), 3
+    return s
+
+
+TOKENS = torch.zeros(2, 2, 128, dtype=torch.bfloat16), torch.zeros(2, 2, 128, dtype=torch.bfloat16), torch.zeros(2, 8, 128, dtype=torch.bfloat16)
+
+
+@pytest.mark.parametrize("axes,pos", [(AXES, None), (None, POS), (AXES, POS), (None, None)])
+@pytest.mark.parametrize("bump", [True, False])
+def test_a_refused_step_of_the_cache_counts_no_token(axes, pos, bump):
+    """Half a pair, and (both or none) tensors that are not on the GPU."""
+    c = _paged(axes)
+    k, v, q = TOKENS
+    with pytest.raises(Exception):
+        c.decode_step(q, k, v, bump_n_ctx=bump, pos=pos)
+    assert c.n_ctx.tolist() == [7, 7]
+
+
+@pytest.mark.parametrize("axes,pos", [(AXES, None), (None, POS), (AXES, POS), (None, None)])
+@pytest.mark.parametrize("bump", [True, False])
+def test_a_refused_step_of_a_layer_counts_no_token(axes, pos, bump):
+    s = _layer()
+    with pytest.raises(Exception):
+        s.decode_step(*TOKENS, bump_n_ctx=bump, rotation=kvr.make_rotation(s.desc), axes=axes, pos=pos)
+    assert s.n_ctx.tolist() == [7, 7] and s.r_size == 3
