@@ -139,12 +139,15 @@ class LayerState:
 
     def decode_step(self, k_new, v_new, q, *, bump_n_ctx=True, fused=None, replace_rate=None, max_swaps=4,
                     check=False, opts=None, rotation=None, axes=None, pos=None):
-        """(rotate, if a binding.make_rotation is given, by axes and pos if those are) -> append -> select -> encode -> (swap loop, if replace_rate
+        """(rotate, if a binding.make_rotation is given, by axes and pos if those are, which are refused without one)
+        -> append -> select -> encode -> (swap loop, if replace_rate
         is given) -> attend.  n_ctx counts the new token from here on; pass bump_n_ctx=False when
         several layers share one n_ctx tensor that the caller advances once per
         step.  fused: use kvr_step_update for the first three (default: whenever its
         size limits allow).  check: synchronise after the update and raise if a unit
         could not evict (see check_evictions)."""
+        if rotation is None and (axes is not None or pos is not None):
+            raise ValueError("axes and pos are a rotation's, and there is none")
         if bump_n_ctx:
             self.n_ctx += 1
         if rotation is not None:

@@ -45,3 +45,16 @@ def test_a_refused_step_of_a_layer_counts_no_token(axes, pos, bump):
     with pytest.raises(Exception):
         s.decode_step(*TOKENS, bump_n_ctx=bump, rotation=kvr.make_rotation(s.desc), axes=axes, pos=pos)
     assert s.n_ctx.tolist() == [7, 7] and s.r_size == 3
+
+
+@pytest.mark.parametrize("axes,pos", [(AXES, None), (None, POS), (AXES, POS)])
+def test_axes_and_positions_without_a_rotation_are_refused(axes, pos):
+    """(They would be dropped, and the token attended to as it comes.)"""
+    s = _layer()
+    s.step_update = s.append = s.attend = lambda *a, **kw: None
+    s.n_recent, s.slack, s.ret_cap, s.evict_cap = 4, 0, 10, 8
+    with pytest.raises(ValueError):
+        s.decode_step(*TOKENS, axes=axes, pos=pos)
+    assert s.n_ctx.tolist() == [7, 7] and s.r_size == 3
+    s.decode_step(*TOKENS)
+    assert s.n_ctx.tolist() == [8, 8]
