@@ -132,8 +132,9 @@ class LayerState:
         the token) -> the key that append takes and the query that attend takes, in buffers that the next call reuses.
         axes, a binding.make_axes, and pos int32 [n_axes, B]: by these positions instead of the tokens' places."""
         if self.k_turned is None:
-            self.k_turned = torch.empty(k_new.shape, dtype=self.dtype, device=self.device)
-            self.q_turned = torch.empty(q.shape, dtype=self.dtype, device=self.device)
+            d = self.desc
+            self.k_turned, self.q_turned = (torch.empty(d.batch, heads, d.head_dim, dtype=self.dtype, device=self.device)
+                                            for heads in (d.n_kv_heads, d.n_q_heads))
         _rotate(self.desc, rotation, axes, pos, q, k_new, None, self.desc.batch, None, self.n_ctx, self.q_turned, self.k_turned)
         return self.k_turned, self.q_turned
 

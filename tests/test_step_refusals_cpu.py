@@ -58,3 +58,13 @@ def test_axes_and_positions_without_a_rotation_are_refused(axes, pos):
     assert s.n_ctx.tolist() == [7, 7] and s.r_size == 3
     s.decode_step(*TOKENS)
     assert s.n_ctx.tolist() == [8, 8]
+
+
+def test_a_refused_rotation_leaves_buffers_of_the_right_size():
+    """(Too small ones, made after the operands of a call that is refused, would refuse every later call.)"""
+    s = _layer()
+    k, v, q = TOKENS
+    with pytest.raises(Exception):
+        s.rotate(k[:1], q[:, :3], kvr.make_rotation(s.desc))
+    for buffer, like in ((s.k_turned, k), (s.q_turned, q)):
+        assert buffer is None or buffer.shape == like.shape
