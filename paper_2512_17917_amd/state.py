@@ -273,7 +273,7 @@ class PagedCache:
         self.device = torch.device(device)
         self.dtype = torch.float32 if desc.dtype == kvr.KVR_F32 else torch.bfloat16
         self.rotation = kvr.make_rotation(desc) if rotation is None else rotation
-        self.axes, self.groups, self.ws_shared = axes, None, None
+        self.axes, self.groups, self.lists, self.ws_shared = axes, None, None, None
         self.k, self.v = (torch.zeros(n_pages, Hkv, page_size, D, dtype=self.dtype, device=self.device) for _ in range(2))
         self.table = torch.full((B, table_cap), -1, dtype=torch.int32, device=self.device) if table is None else table
         self.n_ctx = torch.zeros(B, dtype=torch.int32, device=self.device) if n_ctx is None else n_ctx
@@ -319,17 +319,31 @@ class PagedCache:
 
     def share(self, start, n_shared):
         """From here on what a group's sequences have in common is read once for all of them: sequences start[g] ..
-        start[g + 1] - 1 begin with the same n_shared[g] tokens (see begin_with).  int32 device tensors are taken as they
-        are, and a call goes by what they hold then, a captured one too; lists are copied; no groups, or None, ends it."""
-        self.groups = None
-        if start is None:
-            return
-        i32 = lambda x: x if isinstance(x, torch.Tensor) else torch.tensor(x, dtype=torch.int32, device=self.device)
-        groups = kvr.make_groups(i32(start), i32(n_shared))
-        if groups.n_groups == 0:
-            return
-        if self.ws_shared is None:                  # of every step; it is the same size for all groups
-            self.ws_shared = self._room_to_share(groups, self.desc.batch)
+        start[g + 1] - 1 begin with the same n_shared[g] tokens (see begin_with).  Two int32 device tensors are taken as they
+        are, and a call goes by what they hold then, a captured one too: they have to outlive it.  Lists are copied to
+        tensors of the cache's own, on the current stream, and a call captured with lists goes by those given last (by no
+        groups after tensors or none).  No groups, or None, ends it."""
+        B, n, groups = self.desc.batch, 0, None
+        if isinstance(start, torch.Tensor) and isinstance(n_shared, torch.Tensor):
+            groups = kvr.make_groups(start, n_shared)
+            if groups.n_groups == 0:
+                groups = None
+        elif start is not None:
+            start, n_shared = ([int(i) for i in x] for x in (start, n_shared))
+            n = len(n_shared)
+            if n > B or (n and len(start) <= n) or any(x > y for x, y in zip(start[:n], start[1:])):
+                raise ValueError(f"starts {start} of {n} groups: {B} at most, n + 1 starts that do not fall")
+        if n and self.lists is None:
+            i32 = lambda m: torch.zeros(m, dtype=torch.int32, device=self.device)
+            self.lists = kvr.make_groups(i32(B + 1), i32(B))
+        if n:
+            groups = self.lists
+        if groups is not None and self.ws_shared is None:        # of every step; it is the same size for all groups
+            self.ws_shared = self._room_to_share(groups, B)
+        if self.lists is not None:                  # (groups past the last: of no sequences, or of those that are in none)
+            starts, common = (start[:n + 1], n_shared) if n else ([], [])
+            for to, x, rest in zip(self.lists.tensors, (starts, common), (B, 0)):
+                to.copy_(torch.tensor(x + [rest] * (to.numel() - len(x)), dtype=torch.int32))
         self.groups = groups
 
     def _room_to_share(self, groups, rows):
