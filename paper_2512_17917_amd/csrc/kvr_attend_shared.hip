@@ -30,6 +30,7 @@
 //
 // float32.  A workgroup has 16 columns; its four waves take 16 of a tile's 64 tokens each, with running maxima and sums of
 // their own, and are joined in LDS at a piece's end (the layouts are those of the float32 kernel for prompts).
+#include <cstddef>
 #include <type_traits>
 
 #include "kvr_prompt.h"
@@ -56,10 +57,11 @@ struct SharedLds {
   int4 tile[SH_LIST];                                           // rows that some column may see (two words), first token, flags
   float2 ml[SH_WAVES][32];                                      // waves' maxima and sums
   RowBf16::Scratch scratch;
-  unsigned char odd[SH_BUFS][SH_WAVES];                         // rows with a value that is not finite, a byte a wave
+  alignas(8) unsigned char odd[SH_BUFS][SH_WAVES];              // rows with a value that is not finite, a byte a wave
 };
 constexpr int SH_LDS = sizeof(SharedLds);
 static_assert(SH_LDS <= 160 * 1024);
+static_assert(offsetof(SharedLds, odd) % 8 == 0 && SH_WAVES == 8);      // (eight bytes read at once)
 constexpr float KEEP_MAX = 8.f;
 constexpr float SPLIT = 1.f + 0x1p-20f;                         // (see p above)
 constexpr int SF_WAVES = 4, SF_COLS = 16, SF_KEYS = 64;
