@@ -1205,11 +1205,23 @@ hipError_t launch_attend_shared(const DevDesc& d, int dtype, const SharedArgs& g
     if (e != hipSuccess || !a.scores) return e;
     return single ? launch_shared_scores(d, dtype, s, so.lse, st) : launch_prompt_scores_f32(d, a, so.lse, st);
   }
+  // a launch may ask for more than 64 KB of LDS where the kernel's limit was raised, on each device for itself
+  constexpr int DEVICES = 64;
+  static std::once_flag once[DEVICES];
+  static hipError_t raised[DEVICES];
+  int dev = 0;
+  e = hipGetDevice(&dev);
+  if (e != hipSuccess) return e;
+  if (dev < 0 || dev >= DEVICES) return hipErrorInvalidDevice;
+  std::call_once(once[dev], [&] {
+    for (const void* f : {(const void*)shared_bf16_kernel<EIGHT_A_PAGE>, (const void*)shared_bf16_kernel<ANYWHERE>}) {
+      const hipError_t x = hipFuncSetAttribute(f, hipFuncAttributeMaxDynamicSharedMemorySize, SH_LDS);
+      if (x != hipSuccess) raised[dev] = x;
+    }
+  });
+  if (raised[dev] != hipSuccess) return raised[dev];
   auto launch = [&](auto rows) {
-    constexpr int ROWS = decltype(rows)::value;
-    const hipError_t x = raise_lds_limit((const void*)shared_bf16_kernel<ROWS>, SH_LDS);
-    if (x != hipSuccess) return x;
-    hipLaunchKernelGGL((shared_bf16_kernel<ROWS>), dim3(p.wgs), dim3(64 * SH_WAVES), SH_LDS, st, d, s, so);
+    hipLaunchKernelGGL((shared_bf16_kernel<decltype(rows)::value>), dim3(p.wgs), dim3(64 * SH_WAVES), SH_LDS, st, d, s, so);
     return hipGetLastError();
   };
   e = a.pages.page_size % 8 == 0 ? launch(std::integral_constant<int, EIGHT_A_PAGE>{}) : launch(std::integral_constant<int, ANYWHERE>{});

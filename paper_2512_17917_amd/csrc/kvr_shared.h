@@ -331,25 +331,6 @@ struct WorkRow {
   }
 };
 
-// A kernel may be launched with more than 64 KB of LDS where its limit was raised, on each device for itself.
-inline hipError_t raise_lds_limit(const void* kernel, int bytes) {
-  constexpr int DEVICES = 64, KERNELS = 4;
-  static std::mutex lock;
-  static const void* known[DEVICES][KERNELS];
-  int dev = 0;
-  hipError_t e = hipGetDevice(&dev);
-  if (e != hipSuccess) return e;
-  if (dev < 0 || dev >= DEVICES) return hipErrorInvalidDevice;
-  const std::lock_guard<std::mutex> held(lock);
-  int i = 0;
-  while (i < KERNELS && known[dev][i] != nullptr && known[dev][i] != kernel) ++i;
-  if (i == KERNELS) return hipErrorInvalidValue;
-  if (known[dev][i] == kernel) return hipSuccess;
-  e = hipFuncSetAttribute(kernel, hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
-  if (e == hipSuccess) known[dev][i] = kernel;
-  return e;
-}
-
 // the group that sequence b is in, -1 if in none (wave-uniform b; all lanes call)
 __device__ __forceinline__ int group_of_seq(const SharedArgs& s, int B, int b) {
   const int lane = threadIdx.x & 63;

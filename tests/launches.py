@@ -17,10 +17,15 @@ static std::map<const void*, std::string>& names() {          // (the library's 
   return x;
 }
 extern "C" void __hipRegisterFunction(void**, const void* f, char*, const char* name, unsigned, void*, void*, void*, void*, int*) { names()[f] = name; }
-extern "C" hipError_t hipFuncSetAttribute(const void*, hipFuncAttribute, int) { return hipSuccess; }
-extern "C" hipError_t hipGetDevice(int* dev) { *dev = 0; return hipSuccess; }
-extern "C" hipError_t hipLaunchKernel(const void* f, dim3, dim3, void**, size_t, hipStream_t) {
-  std::printf(" %s", names()[f].c_str());
+static int device;
+static std::map<std::pair<int, const void*>, int> limit;
+extern "C" hipError_t hipFuncSetAttribute(const void* f, hipFuncAttribute a, int value) {
+  if (a == hipFuncAttributeMaxDynamicSharedMemorySize) limit[{device, f}] = value;
+  return hipSuccess;
+}
+extern "C" hipError_t hipGetDevice(int* dev) { *dev = device; return hipSuccess; }
+extern "C" hipError_t hipLaunchKernel(const void* f, dim3, dim3, void**, size_t lds, hipStream_t) {
+  std::printf(" %s:%zu:%d", names()[f].c_str(), lds, limit.count({device, f}) ? limit[{device, f}] : 65536);
   return hipSuccess;
 }
 extern "C" hipError_t __hipPushCallConfiguration(dim3, dim3, size_t lds, hipStream_t) { asked = lds; return hipSuccess; }
@@ -31,7 +36,7 @@ extern "C" hipError_t __hipPopCallConfiguration(dim3* g, dim3* b, size_t* lds, h
 extern "C" hipError_t hipGetLastError() { return hipSuccess; }
 int main() {
   int f32, B, Hq, Hkv, rows, by_start, page, cols, window, sink, groups, scores;
-  while (std::scanf("%d %d %d %d %d %d %d %d %d %d %d %d", &f32, &B, &Hq, &Hkv, &rows, &by_start, &page, &cols, &window, &sink, &groups, &scores) == 12) {
+  while (std::scanf("%d %d %d %d %d %d %d %d %d %d %d %d %d", &f32, &B, &Hq, &Hkv, &rows, &by_start, &page, &cols, &window, &sink, &groups, &scores, &device) == 13) {
     kvr::DevDesc d = {};
     d.B = B; d.Hq = Hq; d.Hkv = Hkv; d.G = Hq / Hkv; d.scale = 1.f;
     static int32_t x[4];                     // no kernel runs: never read
@@ -54,22 +59,23 @@ int main() {
 
 def build_probe(folder):
     """-> ask(list of dicts) -> a list of kernels' names (mangled) each; dicts: f32, B, Hq, Hkv, rows, by_start, page, cols, window,
-    sink, groups, scores."""
+    sink, groups, scores, device (0 if left out).  ask.lds: for each call its launches' dynamic LDS and the limit there."""
     src, exe = str(folder / "launches.hip"), str(folder / "launches")
     open(src, "w").write(PROBE)
     subprocess.run([B._hipcc(), "--offload-host-only", "-std=c++17", "-I", B.CSRC, src, "-L", os.path.dirname(B.OUT),
                     "-l:" + os.path.basename(B.OUT), f"-Wl,-rpath,{os.path.dirname(B.OUT)}", "-o", exe], check=True, capture_output=True)
-    order = "f32 B Hq Hkv rows by_start page cols window sink groups scores".split()
+    order = "f32 B Hq Hkv rows by_start page cols window sink groups scores device".split()
 
     def ask(calls):
-        out = subprocess.run([exe], input="".join(" ".join(str(int(c[k])) for k in order) + "\n" for c in calls), capture_output=True, text=True,
+        out = subprocess.run([exe], input="".join(" ".join(str(int(c.get(k, 0))) for k in order) + "\n" for c in calls), capture_output=True, text=True,
                              check=True).stdout.splitlines()
         assert len(out) == len(calls)
-        got = []
+        got, ask.lds = [], []
         for c, line in zip(calls, out):
             *kernels, rc = line.split()
             assert rc == "0", (c, line)
-            got.append(kernels)
+            got.append([k.split(":")[0] for k in kernels])
+            ask.lds.append([tuple(map(int, k.split(":")[1:])) for k in kernels])
         return got
     return ask
 

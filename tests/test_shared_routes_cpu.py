@@ -97,3 +97,13 @@ def test_lists_that_are_filled_again_are_full(tmp_path):
             elif which == 0:
                 assert max(map(sum, tiles.values())) > (128 if page % 8 == 0 else 24), name
     assert cuts > 20
+
+
+def test_launches_stay_within_their_lds_limit(ask):
+    """More than 64 KB only where the limit was raised for the kernel, on the device of the call."""
+    call = dict(B=64, Hq=32, Hkv=8, rows=64, page=16, cols=1000, window=0, sink=0, groups=1)
+    calls = [dict(call, f32=f32, page=page, scores=scores, by_start=by_start, device=dev)
+             for dev in (0, 3, 0) for page in (16, 7) for f32 in (0, 1) for scores in (0, 1) for by_start in (0, 1)]
+    for c, kernels, lds in zip(calls, ask(calls), ask.lds):
+        assert "shared" in kernels[0] and all(asked <= most <= 160 * 1024 for asked, most in lds), (c, kernels, lds)
+        assert c["f32"] or lds[0][0] > 65536
