@@ -1102,11 +1102,11 @@ struct SharedPlan {
   size_t off_ml, off_span, off_lse, off_scores, total;
 };
 
-// the longest row that there can be (the scores' rows have tiles of more columns and heavier ones)
-constexpr int MOST_WEIGHT = 7, MOST_COST = 12;
+// the longest row that there can be (of tiles of 16 columns, which no row's are fewer than)
+static_assert(RowBf16::bounded() && RowF32::bounded() && SF_COLS == 16 && SF_KEYS == SH_KEYS);
 long long most_tiles(const DevDesc& d, long long n_rows, long long cap, int cols, int keys) {
   const long long col_tiles = 2 * ((n_rows * d.G + cols - 1) / cols + d.B);
-  return col_tiles * d.Hkv * (MOST_WEIGHT * ((cap + keys - 1) / keys + 2) + MOST_COST);
+  return col_tiles * d.Hkv * (ROW_WEIGHT * ((cap + keys - 1) / keys + 2) + ROW_COST);
 }
 
 SharedPlan shared_plan(const DevDesc& d, int dtype, long long n_rows, long long cap, long long n_cap) {

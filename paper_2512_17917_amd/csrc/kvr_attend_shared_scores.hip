@@ -40,6 +40,7 @@ __global__ __launch_bounds__(64 * SS_WAVES, 4) void shared_scores_kernel(DevDesc
   extern __shared__ __align__(1024) unsigned char s_mem[];
   ScoresLds<T>& lds = *reinterpret_cast<ScoresLds<T>*>(s_mem);
   typedef WorkRow<SS_COLS, SS_KEYS, true> Row;
+  static_assert(Row::bounded());
   constexpr int BLOCKS = SS_BLOCKS<T>, TURNS = 4 / BLOCKS, STEPS = D * (int)sizeof(T) / 64;      // turns a tile, 64-byte steps of a row
   constexpr int ROW = D * sizeof(T);
   const PagedArgs& a = args.a;

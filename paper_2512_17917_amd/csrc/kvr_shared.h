@@ -97,15 +97,26 @@ struct Share {
   int at, upto, end, n;
 };
 
+// What the host takes the longest row to be, for numbers of 31 bits: of c columns no more than c / 16 + 1 tiles of ROW_WEIGHT a tile of
+// tokens and ROW_COST, whatever a row's own tiles of columns, weights and costs are (WorkRow::bounded).
+constexpr int ROW_WEIGHT = 7, ROW_COST = 12;
+
 // SCORES: the row of the pass that adds scores, which takes longer with every column
 template <int COLS, int KEYS, bool SCORES = false>
 struct WorkRow {
   static constexpr int LIGHT = 4, HEAVY = 10;
   // (queries of more than 16 columns are steps of their own, and more of them are joined and written at the end)
-  __host__ __device__ static __forceinline__ int cost(int cols) { return SCORES || cols > 16 ? 12 : 5; }
-  __host__ __device__ static __forceinline__ int weight(int cols) {
+  __host__ __device__ static constexpr int cost(int cols) { return SCORES || cols > 16 ? 12 : 5; }
+  __host__ __device__ static constexpr int weight(int cols) {
     if (SCORES) return LIGHT + (cols < COLS ? cols : COLS) / 8;
     return cols > COLS / 2 && COLS > 64 ? HEAVY : LIGHT;
+  }
+  static constexpr bool bounded() {               // (from COLS on weights and costs stay, and tiles of columns grow by one in COLS)
+    for (int c = 1; c <= 4 * COLS; ++c) {
+      const int tiles = (c + COLS - 1) / COLS;
+      if (16 * tiles * weight(c) > ROW_WEIGHT * (c + 16) || 16 * tiles * cost(c) > ROW_COST * (c + 16)) return false;
+    }
+    return true;
   }
 
   __host__ __device__ static __forceinline__ int col_tiles(int rows, int G) { return (int)(((long long)rows * G + COLS - 1) / COLS); }
