@@ -449,9 +449,10 @@ constexpr int MAX_ROWS_NEW = 1 << 27;
 // (attention launches two threads a row and head, fewer than 2^32; q and out of more would not fit the memory)
 constexpr long long MAX_HEADS_ROTATED = 0x7fffffffll, MAX_HEADS_ATTENDED = 1ll << 30;
 
-static int32_t check_rows(const kvr_desc* desc, int32_t n_rows, const int32_t* q_start, long long most_heads) {
+// (one_each: without a list of starts the rows are the sequences', one each)
+static int32_t check_rows(const kvr_desc* desc, int32_t n_rows, const int32_t* q_start, long long most_heads, bool one_each = true) {
   if (n_rows < 0 || n_rows > MAX_ROWS_NEW || (long long)n_rows * desc->n_q_heads > most_heads) return KVR_ERR_INVALID_ARG;
-  if (q_start == nullptr && n_rows != desc->batch) return KVR_ERR_INVALID_ARG;
+  if (q_start == nullptr && one_each && n_rows != desc->batch) return KVR_ERR_INVALID_ARG;
   return KVR_OK;
 }
 
@@ -487,7 +488,7 @@ static int32_t rotate_rows(const kvr_desc* desc, const kvr_rotation* rot, const 
     a.axis_stride = axes->n_axes > 1 ? pos_stride : 0;
   }
   // (without a cache and a list of starts the rows are nobody's in particular, however many there are)
-  rc = check_rows(desc, n_rows, placed || q_start != nullptr ? q_start : &desc->batch, MAX_HEADS_ROTATED);
+  rc = check_rows(desc, n_rows, q_start, MAX_HEADS_ROTATED, placed);
   if (rc != KVR_OK) return rc;
   if (pages != nullptr && n_rows > 0) {
     rc = check_pages(desc, pages, a.pages);
