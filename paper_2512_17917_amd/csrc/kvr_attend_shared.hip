@@ -14,11 +14,12 @@
 // A wave computes S = K Q^T (keys x columns, v_mfma_f32_16x16x32_bf16; Q stays in registers), so that a lane holds logits of
 // one column alone; the registers of S, exponentiated and in bf16, are the B operand of O^T = V^T P as they lie (its k
 // index may be counted in any order as long as V^T has the same), with ds_read_b64_tr_b16 fetching groups of four tokens.
-//   p goes to the matrix unit as two bf16 numbers: its upper 16 bits, and the rest, rounded, which leaves an error of 2^-15 p at
-// most.  Their sum, and that of p for l, are in float32.  The rest is taken of p (1 + 2^-20), so that it is never 0 beside an upper part: 0
-// times an infinite value, which belongs to the column, would be NaN (it still is below 2^-106 of the largest weight, where bf16 ends).
-// One number in bf16 was off by half its step, 2^-8, and with it sums that cancel; it took 79 us for 64 on 8k (two: 81), 136 for 256
-// on 4k (145), 46 for 8 x 6 rows on 16k (51), where the bytes bound it the same.
+//   Of several new tokens a sequence p is rounded to bf16, as it is in kvr_attend_prompt, which such a call takes otherwise: the matrix unit
+// takes nothing wider at this rate, and the error is half a step of the output's type at most, relative to sum p |v|.  Of one, which
+// kvr_attend_paged has in float32, it is two bf16 numbers: its upper 16 bits, and the rest, rounded, which leaves an error of 2^-15 p at
+// most; their products cost 64 sequences on 8k 79 -> 81 us and 256 on 4k 136 -> 145 (8 x 12 rows on 16k, bound by products, would be 64 -> 82).
+// The rest is taken of p (1 + 2^-20), so that it is never 0 beside an upper part: 0 times an infinite value, which belongs to the
+// column, would be NaN (it still is below 2^-106 of the largest weight, where bf16 ends).  The sum of p is taken in float32 before.
 //   The running maximum moves only when it is passed by more than 8 (in powers of two): p then stays below 2^8.
 // At a unit's end waves with the same columns are joined in the tile's place in LDS, which is free until the next step.
 //
@@ -45,7 +46,8 @@ constexpr int SH_TILE = SH_KEYS * D * 2;                       // bytes of a til
 constexpr int SH_BUFS = 4;
 constexpr int SH_FEW = 16;                                      // columns whose queries come through LDS, four units ahead
 constexpr int SH_QUERIES = SH_FEW * D * 2;
-typedef WorkRow<SH_COLS, SH_KEYS> RowBf16;
+// (heavy tiles, 64 sequences on 8k and 256 on 4k, FINE: 7 quarters 89 and 160 us, 9 85 and 145, 10 81 and 145, 12 84 and 150)
+template <bool FINE> using RowBf16 = WorkRow<SH_COLS, SH_KEYS, false, FINE ? 10 : 7>;
 constexpr int SH_LIST = 128, SH_LIST_ANY = 24;                  // tiles that are listed at a time (where rows lie anywhere)
 constexpr int SH_ROWS = SH_LIST * 8 > SH_LIST_ANY * SH_KEYS ? SH_LIST * 8 : SH_LIST_ANY * SH_KEYS;      // numbers of their rows' places
 struct SharedLds {
@@ -56,7 +58,7 @@ struct SharedLds {
   int row[SH_ROWS];                                             // of tiles: eight rows' first, or every row
   int4 tile[SH_LIST];                                           // rows that some column may see (two words), first token, flags
   float2 ml[SH_WAVES][32];                                      // waves' maxima and sums
-  RowBf16::Scratch scratch;
+  RowScratch scratch;
   alignas(8) unsigned char odd[SH_BUFS][SH_WAVES];              // rows with a value that is not finite, a byte a wave
 };
 constexpr int SH_LDS = sizeof(SharedLds);
@@ -123,7 +125,8 @@ __device__ __forceinline__ float rows_sum(float x) {
   return __uint_as_float(b[0]) + __uint_as_float(b[1]);
 }
 
-template <int ROWS>
+// FINE: p in two parts
+template <int ROWS, bool FINE>
 __global__ __launch_bounds__(64 * SH_WAVES, 2) void shared_bf16_kernel(DevDesc d, SharedArgs args, SharedOut so) {
   extern __shared__ __align__(1024) unsigned char s_mem[];
   SharedLds& lds = *reinterpret_cast<SharedLds*>(s_mem);
@@ -150,7 +153,7 @@ __global__ __launch_bounds__(64 * SH_WAVES, 2) void shared_bf16_kernel(DevDesc d
   // The list of pieces, and how many tiles they have.
   auto list_pieces = [&] {
     mine.at = mine.upto;
-    RowBf16::list<SH_WAVES>(d, args, mine, lds.list, &lds.scratch);
+    RowBf16<FINE>::template list<SH_WAVES>(d, args, mine, lds.list, &lds.scratch);
     if (wave == 0) {
       const Piece& f = lds.list[lane];
       const int n = lane < mine.n && f.i0 < f.i1 ? f.i1 - f.i0 + query_tiles(f.cols, f.ct) : 0;
@@ -318,7 +321,7 @@ __global__ __launch_bounds__(64 * SH_WAVES, 2) void shared_bf16_kernel(DevDesc d
     const Piece& u = lds.list[now];
     const int bits = uniform(u.bits), ct = uniform(u.ct), cols = uniform(u.cols), row0 = uniform(u.row0), h = uniform(u.h);
     const int some = min(cols - ct * SH_COLS, SH_COLS);
-    const int c0 = RowBf16::place(d, a.n_rows, (bits & PIECE_OWN) != 0, row0, cols, ct, h);
+    const int c0 = RowBf16<FINE>::place(d, a.n_rows, (bits & PIECE_OWN) != 0, row0, cols, ct, h);
     const size_t slot0 = (size_t)SH_COLS * w + c0;
     if (threadIdx.x == 0) {
       if (bits & PIECE_FIRST) so.span[2 * (size_t)c0] = w;
@@ -453,14 +456,20 @@ __global__ __launch_bounds__(64 * SH_WAVES, 2) void shared_bf16_kernel(DevDesc d
 #pragma unroll
         for (int x = 0; x < 4; x += 2) {
           const f32x2_t y = {exp2_(fmaf(s[n][b][x], sc.c, -m_use)), exp2_(fmaf(s[n][b][x + 1], sc.c, -m_use))};
-          const uint32_t y0 = __float_as_uint(y[0]), y1 = __float_as_uint(y[1]);
-          const f32x2_t left = {fmaf(y[0], SPLIT, -__uint_as_float(y0 & 0xffff0000u)), fmaf(y[1], SPLIT, -__uint_as_float(y1 & 0xffff0000u))};
-          const bf16x2_t upper = __builtin_bit_cast(bf16x2_t, __builtin_amdgcn_perm(y1, y0, 0x07060302u)), lower = __builtin_convertvector(left, bf16x2_t);
+          bf16x2_t z;
+          if constexpr (FINE) {
+            const uint32_t y0 = __float_as_uint(y[0]), y1 = __float_as_uint(y[1]);
+            const f32x2_t left = {fmaf(y[0], SPLIT, -__uint_as_float(y0 & 0xffff0000u)), fmaf(y[1], SPLIT, -__uint_as_float(y1 & 0xffff0000u))};
+            const bf16x2_t lower = __builtin_convertvector(left, bf16x2_t);
+            z = __builtin_bit_cast(bf16x2_t, __builtin_amdgcn_perm(y1, y0, 0x07060302u));
+            rest[n][4 * b + x] = lower[0];
+            rest[n][4 * b + x + 1] = lower[1];
+          } else {
+            z = __builtin_convertvector(y, bf16x2_t);
+          }
           l_run[n] += y[0] + y[1];
-          p[n][4 * b + x] = upper[0];
-          p[n][4 * b + x + 1] = upper[1];
-          rest[n][4 * b + x] = lower[0];
-          rest[n][4 * b + x + 1] = lower[1];
+          p[n][4 * b + x] = z[0];
+          p[n][4 * b + x + 1] = z[1];
         }
     }
     // o += V^T p
@@ -470,8 +479,9 @@ __global__ __launch_bounds__(64 * SH_WAVES, 2) void shared_bf16_kernel(DevDesc d
       const bf16x8_t both = __builtin_bit_cast(bf16x8_t, (s16x8_t{x[0], x[1], x[2], x[3], y[0], y[1], y[2], y[3]}));
 #pragma unroll
       for (int n = 0; n < N; ++n) o[n][cb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(both, p[n], o[n][cb], 0, 0, 0);
+      if constexpr (FINE)
 #pragma unroll
-      for (int n = 0; n < N; ++n) o[n][cb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(both, rest[n], o[n][cb], 0, 0, 0);
+        for (int n = 0; n < N; ++n) o[n][cb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(both, rest[n], o[n][cb], 0, 0, 0);
     }
   };
   // Values that are not finite, for the columns that see them; their weights once more, from the keys in LDS.
@@ -607,7 +617,7 @@ __global__ __launch_bounds__(64 * SF_WAVES) void shared_f32_kernel(DevDesc d, Sh
   __shared__ __align__(16) float s_o[SF_WAVES][16][D + 4];
   __shared__ float s_m[SF_WAVES][16], s_l[SF_WAVES][16];
   __shared__ __align__(16) Piece s_list[PIECES];
-  __shared__ RowF32::Scratch s_scratch;
+  __shared__ RowScratch s_scratch;
   const PagedArgs& a = args.a;
   const int lane = threadIdx.x & 63, wave = uniform((int)(threadIdx.x >> 6)), wg = blockIdx.x;
   const int r = lane >> 4, col = lane & 15;
@@ -1103,7 +1113,7 @@ struct SharedPlan {
 };
 
 // the longest row that there can be (of tiles of 16 columns, which no row's are fewer than)
-static_assert(RowBf16::bounded() && RowF32::bounded() && SF_COLS == 16 && SF_KEYS == SH_KEYS);
+static_assert(RowBf16<true>::bounded() && RowBf16<false>::bounded() && RowF32::bounded() && SF_COLS == 16 && SF_KEYS == SH_KEYS);
 long long most_tiles(const DevDesc& d, long long n_rows, long long cap, int cols, int keys) {
   const long long col_tiles = 2 * ((n_rows * d.G + cols - 1) / cols + d.B);
   return col_tiles * d.Hkv * (ROW_WEIGHT * ((cap + keys - 1) / keys + 2) + ROW_COST);
@@ -1214,14 +1224,16 @@ hipError_t launch_attend_shared(const DevDesc& d, int dtype, const SharedArgs& g
   if (e != hipSuccess) return e;
   if (dev < 0 || dev >= DEVICES) return hipErrorInvalidDevice;
   std::call_once(once[dev], [&] {
-    for (const void* f : {(const void*)shared_bf16_kernel<EIGHT_A_PAGE>, (const void*)shared_bf16_kernel<ANYWHERE>}) {
+    for (const void* f : {(const void*)shared_bf16_kernel<EIGHT_A_PAGE, false>, (const void*)shared_bf16_kernel<EIGHT_A_PAGE, true>,
+                          (const void*)shared_bf16_kernel<ANYWHERE, false>, (const void*)shared_bf16_kernel<ANYWHERE, true>}) {
       const hipError_t x = hipFuncSetAttribute(f, hipFuncAttributeMaxDynamicSharedMemorySize, SH_LDS);
       if (x != hipSuccess) raised[dev] = x;
     }
   });
   if (raised[dev] != hipSuccess) return raised[dev];
   auto launch = [&](auto rows) {
-    hipLaunchKernelGGL((shared_bf16_kernel<decltype(rows)::value>), dim3(p.wgs), dim3(64 * SH_WAVES), SH_LDS, st, d, s, so);
+    if (single) hipLaunchKernelGGL((shared_bf16_kernel<decltype(rows)::value, true>), dim3(p.wgs), dim3(64 * SH_WAVES), SH_LDS, st, d, s, so);
+    else hipLaunchKernelGGL((shared_bf16_kernel<decltype(rows)::value, false>), dim3(p.wgs), dim3(64 * SH_WAVES), SH_LDS, st, d, s, so);
     return hipGetLastError();
   };
   e = a.pages.page_size % 8 == 0 ? launch(std::integral_constant<int, EIGHT_A_PAGE>{}) : launch(std::integral_constant<int, ANYWHERE>{});

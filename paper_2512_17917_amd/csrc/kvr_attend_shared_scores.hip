@@ -29,7 +29,7 @@ struct ScoresLds {
   float lse[SS_COLS];
   int pos[SS_COLS];                              // last token that a column sees, -1: none of the unit's
   Piece list[PIECES];
-  typename WorkRow<SS_COLS, SS_KEYS, true>::Scratch scratch;
+  RowScratch scratch;
 };
 
 // tokens of a wave's turn: keys of as many blocks of 16 as registers hold

@@ -101,10 +101,15 @@ struct Share {
 // tokens and ROW_COST, whatever a row's own tiles of columns, weights and costs are (WorkRow::bounded).
 constexpr int ROW_WEIGHT = 7, ROW_COST = 12;
 
+// What the waves that list a workgroup's pieces tell each other.
+struct RowScratch {
+  int length[16], heavy[16], pieces[16], upto;
+};
+
 // SCORES: the row of the pass that adds scores, which takes longer with every column
-template <int COLS, int KEYS, bool SCORES = false>
+template <int COLS, int KEYS, bool SCORES = false, int MANY = 10>
 struct WorkRow {
-  static constexpr int LIGHT = 4, HEAVY = 10;
+  static constexpr int LIGHT = 4, HEAVY = MANY;
   // (queries of more than 16 columns are steps of their own, and more of them are joined and written at the end)
   __host__ __device__ static constexpr int cost(int cols) { return SCORES || cols > 16 ? 12 : 5; }
   __host__ __device__ static constexpr int weight(int cols) {
@@ -227,14 +232,10 @@ struct WorkRow {
     }
     return common;
   }
-  // What the waves tell each other.
-  struct Scratch {
-    int length[16], heavy[16], pieces[16], upto;
-  };
   // The workgroup's part of the row (r.end = 0 asks for it), and the pieces of its next ones, as many as the list holds; all waves
   // call, each with 64 entries of the row at a time.  (The host has made sure that the row's length fits 31 bits.)
   template <int WAVES>
-  __device__ static __forceinline__ void list(const DevDesc& d, const SharedArgs& s, Share& r, Piece* to, Scratch* x) {
+  __device__ static __forceinline__ void list(const DevDesc& d, const SharedArgs& s, Share& r, Piece* to, RowScratch* x) {
     const int lane = threadIdx.x & 63, wave = uniform((int)(threadIdx.x >> 6));
     const int of_groups = (s.n_groups + 63) >> 6, chunks = of_groups + ((d.B + 63) >> 6), rounds = (chunks + WAVES - 1) / WAVES;
     Entry e = no_entry();
