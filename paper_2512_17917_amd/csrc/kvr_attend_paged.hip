@@ -227,7 +227,10 @@ __device__ __forceinline__ void widen(const u32x4_t* piece, float (&o)[8]) {
   }
 }
 
-template <typename T>
+// FOUR: float32 products in four sums of 32 channels each, which lose half of what a chain of 128 does.  (Where registers are left for
+// them: one head a key head, 0.3e-6 against up to 1.5e-6 of the norm over 9 sequences on 2344 tokens, in the same time; in the kernel
+// for few tokens 200 on 60 would take 22.5 us for 16.7, with two heads 16 on 4000 with scores 108 for 100.)
+template <typename T, bool FOUR>
 __device__ __forceinline__ f32x4_t tile_logits(const u32x4_t (&k)[Tile<T>::N], const u32x4_t (&q)[Tile<T>::N]) {
   f32x4_t s = {0.f, 0.f, 0.f, 0.f};
   if constexpr (sizeof(T) == 2) {
@@ -235,11 +238,15 @@ __device__ __forceinline__ f32x4_t tile_logits(const u32x4_t (&k)[Tile<T>::N], c
     for (int i = 0; i < 4; ++i)
       s = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, k[i]), __builtin_bit_cast(bf16x8_t, q[i]), s, 0, 0, 0);
   } else {
+    f32x4_t t[4] = {s, s, s, s};
 #pragma unroll
     for (int i = 0; i < 8; ++i)
 #pragma unroll
-      for (int e = 0; e < 4; ++e)
-        s = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(k[i][e]), __uint_as_float(q[i][e]), s, 0, 0, 0);
+      for (int e = 0; e < 4; ++e) {
+        f32x4_t& to = FOUR ? t[e] : s;
+        to = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(k[i][e]), __uint_as_float(q[i][e]), to, 0, 0, 0);
+      }
+    if constexpr (FOUR) s = (t[0] + t[1]) + (t[2] + t[3]);
   }
   return s;
 }
@@ -253,7 +260,7 @@ struct Sums {
 
 // A wave walks over every STEP-th tile of a unit from tile ti to t_end.  keep.put(s) gets a tile's logits, keep.after(ti, more)
 // comes at the tile's end, behind the requests for the next one.
-template <typename T, int G, bool ONE, int STEP, typename Keep>
+template <typename T, int G, bool ONE, int STEP, bool FOUR, typename Keep>
 __device__ __forceinline__ void walk(const DevDesc& d, const PagedArgs& a, int b, int h, int n, const TileRange& tr, int ti, int t_end,
                                      Sums<G>& w, Keep&& keep) {
   constexpr int PER = sizeof(T) / 2;                  // 16-byte pieces of eight channels
@@ -278,7 +285,7 @@ __device__ __forceinline__ void walk(const DevDesc& d, const PagedArgs& a, int b
   load_v<T, ONE>(t, a.pages.v, now, j, n, r16, col);
   if (ti + STEP < t_end) entry = tile_entry<ONE>(a, b, tile_token<16>(tr, ti + STEP), n, col);
   for (; ti < t_end; ti += STEP) {
-    const f32x4_t s4 = tile_logits<T>(t.k, q);
+    const f32x4_t s4 = tile_logits<T, FOUR>(t.k, q);
     const bool more = ti + STEP < t_end;
     const int jn = more ? tile_token<16>(tr, ti + STEP) : j;
     const uint32_t there = now.there;
@@ -461,7 +468,7 @@ __global__ __launch_bounds__(64 * PG_WAVES, paged_per_cu(sizeof(T), G)) void pag
     const int u = b * d.Hkv + h;
     Sums<G> sums;
     KeepFar<G> keep = {s_log[wave], logits ? logits + (size_t)u * most_tiles * 16 * G : nullptr, 0};
-    walk<T, G, ONE, PG_WAVES>(d, a, b, h, n, tr, 4 * c0 + wave, min(4 * (c0 + len), tr.n), sums, keep);
+    walk<T, G, ONE, PG_WAVES, sizeof(T) == 4 && G == 1>(d, a, b, h, n, tr, 4 * c0 + wave, min(4 * (c0 + len), tr.n), sums, keep);
     to_shared<G>(sums, s_o[wave], s_m[wave], s_l[wave]);
     __syncthreads();
     const bool all = len == chunks;             // the whole unit: no other workgroup has a part of it
@@ -511,7 +518,7 @@ __global__ __launch_bounds__(64 * short_waves(sizeof(T), G)) void paged_short_ke
   const TileRange tr = unit_tiles(a, b, n);
   Sums<G> sums;
   KeepNear<G> keep = {a.scores ? s_log : nullptr};
-  walk<T, G, ONE, WAVES>(d, a, b, h, n, tr, wave, tr.n, sums, keep);
+  walk<T, G, ONE, WAVES, false>(d, a, b, h, n, tr, wave, tr.n, sums, keep);
   to_shared<G>(sums, s_o[wave], s_m[wave], s_l[wave]);
   __syncthreads();
   for (int i = threadIdx.x; i < G * D; i += 64 * WAVES) put_out<T>(d, a, b, h * G + i / D, i % D, join_waves<WAVES, G>(s_o, s_m, s_l, i / D, i % D));

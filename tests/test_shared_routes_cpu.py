@@ -107,3 +107,10 @@ def test_launches_stay_within_their_lds_limit(ask):
     for c, kernels, lds in zip(calls, ask(calls), ask.lds):
         assert "shared" in kernels[0] and all(asked <= most <= 160 * 1024 for asked, most in lds), (c, kernels, lds)
         assert c["f32"] or lds[0][0] > 65536
+
+
+def test_float32(ask):
+    from tests import test_gpu_shared_float32 as t
+    for groups, heads, page, room in t.CASES:
+        b = Batch(groups, heads, page, F32, 0, rows=False, room=room)
+        _names(ask, [launches.call_of(b, True, scores=False)], "shared_f32_kernel" if room else "12paged_kernel", "join_kernel")
