@@ -3,9 +3,9 @@
 //   out = sum_j exp(s_j - m) v_j / sum_j exp(s_j - m), whose sums over the common tokens and over a sequence's own are formed apart,
 // each with the maximum m that it has come to, and added as exp(m1 - m), exp(m2 - m) times each.
 // Bound by the bytes of what is shared, once a group, and of each sequence's own up to some 200 columns (rows times G), by products
-// beyond: 64 sequences on 8192 tokens, 32 heads on 8, 302 MB, 70 us = 4.3 TB/s; 10 ragged groups 767 MB, 157 us = 4.9; 2 on
-// 131072 540 MB, 102 us = 5.3; 256 on 4096 (1024 columns a head, 512 own tokens each) 554 MB, 128 us = 4.3, the matrix units busy for a
-// tenth of it.  Beside the tiles (1 us each with few columns, 1.9 with 256) a launch pays 4 us for the list and 1 to 2 for each piece's
+// beyond: 64 sequences on 8192 tokens, 32 heads on 8, 302 MB, 72 us = 4.2 TB/s; 10 ragged groups 767 MB, 160 us = 4.8; 2 on
+// 131072 540 MB, 103 us = 5.2; 256 on 4096 (1024 columns a head, 512 own tokens each) 554 MB, 137 us = 4.0, the matrix units busy for a
+// seventh of it.  Beside the tiles (1 us each with few columns, 2.5 with 256, 1.9 of several new tokens a sequence) a launch pays 4 us for the list and 1 to 2 for each piece's
 // start and end.
 //
 // bf16.  A workgroup has up to 256 columns of a unit and walks over the unit's tokens in tiles of 64, which go from the pages
@@ -906,7 +906,7 @@ __global__ __launch_bounds__(256) void shared_join_kernel(DevDesc d, SharedArgs 
 // ---- the same for many sequences of one new row each, with their own tokens where those are few: four waves for a sequence and kv head
 // take 64 tokens each, keys and values straight from the pages.
 // (As units these are a tile or two and a start and an end that cost more than those: 1212 sequences with 94 tokens each behind 768, 16
-// heads on 8, with scores, 348 and 210 us, 378 with one behind 878 134 and 79; a large batch is at the bytes of its ends, 4 to 5 TB/s.)
+// heads on 8, with scores, 356 and 215 us, 378 with one behind 878 122 and 82; a large batch is at the bytes of its ends, 4 to 5 TB/s.)
 // Logits as S = Q K^T, four heads of a token in a lane; softmax with a token a lane; p v in float32, 16 bytes of a row a lane; then a wave
 // joins a head's parts with the pieces of what is shared, and the tokens' scores are added, whose logits the lanes still have.
 constexpr int SO_WAVES = 4, SO_MOST = 64 * SO_WAVES;
@@ -1098,8 +1098,8 @@ template <typename T, int COLS, int KEYS>
 hipError_t launch_join(const DevDesc& d, const SharedArgs& s, const SharedOut& so, hipStream_t st) {
   if (s.own_most > 0) return launch_own<T, COLS, KEYS>(d, s, so, st);
   const long long heads = (long long)s.a.n_rows * d.Hq;
-  // (one wave or four, whole calls: 64 rows and heads of 66 pieces 113 and 111 us, 512 of 30 95.6 and 94.7, 1792 105.8 and 107.6,
-  // 2048 78.1 and 79.3)
+  // (one wave or four, whole calls: 64 rows and heads of 66 pieces 115.5 and 112.9 us, 512 of 30 96.4 and 95.1, 1856 109.6 and
+  // 111.5, 2048 80.8 and 82.0)
   if (heads <= 1024) hipLaunchKernelGGL((shared_join_kernel<T, COLS, KEYS, 4>), dim3((unsigned)heads), dim3(256), 0, st, d, s, so);
   else hipLaunchKernelGGL((shared_join_kernel<T, COLS, KEYS, 1>), dim3((unsigned)((heads + 3) / 4)), dim3(256), 0, st, d, s, so);
   return hipGetLastError();
@@ -1144,10 +1144,12 @@ bool attend_shared_fits(const DevDesc& d, long long n_rows, long long cap) {
 }
 // Whose kernels a call takes.  Small caches are read sooner by every sequence for itself: what counts is the cache that a batch of
 // the longest sequences would read, by the room that it has (the lengths only the device knows).  One token per sequence, 32 heads on 8,
-// each for itself and shared: 66 MB (4 x 4000) 19.9 and 21.7 us, 68 MB (16 x 1000) 22.2 and 20.1, 131 MB (2 x 16000) 37.5 and
-// 31.7; with scores, whose pass is a launch more, 131 MB 40.0 and 43.9, 145 MB (32 x 1100) 47.1 and 41.1; float32 66 MB 23.0 and
-// 29.9, 132 MB 40.4 and 31.1.  Room for few tokens, where the paged kernels need one launch: 134 MB (64 x 500) 22.3 and 34.1, with scores 29.3 and
-// 43.9, 268 MB (128 x 500) 45.6 and 38.3, 58.5 and 54.2; 98 MB (250 x 90, whose ends the join takes) 25.4 and 17.9; float32 268 MB (64 x 500)
+// each for itself and shared: 66 MB (4 x 4000) 19.3 and 20.0 us, 68 MB (16 x 1000) 21.8 and 20.1, 131 MB (2 x 16000) 37.8 and
+// 30.1; with scores, whose pass is a launch more, 131 MB 40.4 and 42.1, 149 MB (32 x 1100) 39.4 and 34.7; float32 67 MB (4 x 2000) 21.2 and
+// 22.6, 132 MB (4 x 4000) 40.1 and 27.2, with scores 67 MB 21.7 and 31.2, 134 MB (8 x 2000) 44.9 and 38.8, 167 MB (10 x 2000) 37.5 and 40.9, 201 MB
+// (12 x 2000) 39.1 and 45.0, 204 MB (24 x 1000) 55.6 and 48.4, 232 MB (7 x 4000) 63.4 and 47.5.  Room for few tokens, where the paged kernels
+// need one launch: 131 MB (64 x 500) 20.8 and 31.4, with scores 25.7 and 40.3, 262 MB (128 x 500) 39.9 and 35.0, 49.5 and 46.3; 98 MB
+// (250 x 90, whose ends the join takes) 25.4 and 17.9; float32 268 MB (64 x 500)
 // 37.9 and 46.2, 42.6 and 63.8, 838 MB (808 x 19) 157 and 111.  Several tokens: the prompt's kernel pads a sequence's columns to 256, and is as fast where they are many
 // (8 x 4000 tokens with 2 rows each, 8 columns, 32.1 and 24.1, with 6 rows 32.4 and 31.9, with 12 35.9 and 41.5; 8 x 16000 with 12
 // 87 and 64, with 24 92 and 98; many sequences, whose starts and ends add up: 64 of 100 + 400 with 3 rows 36 and 54, 128 of 500 + 100 with 4 76
@@ -1188,8 +1190,8 @@ hipError_t launch_attend_shared(const DevDesc& d, int dtype, const SharedArgs& g
   const PagedArgs& a = s.a;
   const bool single = a.q_start == nullptr;                     // one new token per sequence
   const long long units = (long long)d.B * d.Hkv;
-  // (units of their own and in the join, 32 heads on 8, 4096 shared: 32 sequences with 8 or 60 tokens more each 27 and 29 to 32 us, with scores,
-  // whose pass is rid of them too, 46 and 49; 64 34 and 36, 74 and 64; 128 48 and 44; 256 75 and 63, with 200 tokens 104 and 97)
+  // (units of their own and in the join, 32 heads on 8, 4096 shared: 32 sequences with 8 or 60 tokens more each 28 and 31 to 34 us, with scores,
+  // whose pass is rid of them too, 48 and 49; 64 39 and 40, 62 and 64; 128 54 and 49, 93 and 86; 256 90 and 80, with 200 tokens 113 and 102)
   s.own_most = single && units >= (a.scores ? 512 : 1024) && units <= 1 << 23 ? SO_MOST : 0;
   const Route r = route(d, dtype, a.n_rows, a.pages.cap, a.vis, s.n_groups, single, a.scores != nullptr);
   if (r == PAGED) return launch_attend_paged(d, dtype, a, st);
