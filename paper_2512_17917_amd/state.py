@@ -149,23 +149,26 @@ class LayerState:
         could not evict (see check_evictions)."""
         if rotation is None and (axes is not None or pos is not None):
             raise ValueError("axes and pos are a rotation's, and there is none")
-        if bump_n_ctx:
-            self.n_ctx += 1
-        if rotation is not None:
-            try:
-                k_new, q = self.rotate(k_new, q, rotation, axes, pos)
-            except Exception:                                  # refused: the token is not counted, and may be given again
-                if bump_n_ctx:
-                    self.n_ctx -= 1
-                raise
-        # Algorithm 3, first branch: does the Recent queue hand its overhang on to the Candidates?
-        self.r_size = kvr.kvr_recent_size(self.r_size + 1, self.n_recent, self.slack)
         if fused is None:
             fused = self.ret_cap <= 32768 and self.evict_cap <= 64
-        if fused:
-            self.step_update(k_new, v_new)
-        else:
-            self.append(k_new, v_new)
+        r_size = self.r_size
+        if bump_n_ctx:
+            self.n_ctx += 1
+        try:
+            if rotation is not None:
+                k_new, q = self.rotate(k_new, q, rotation, axes, pos)
+            # Algorithm 3, first branch: does the Recent queue hand its overhang on to the Candidates?
+            self.r_size = kvr.kvr_recent_size(r_size + 1, self.n_recent, self.slack)
+            if fused:
+                self.step_update(k_new, v_new)
+            else:
+                self.append(k_new, v_new)
+        except Exception:                                  # refused: the token is not counted, and may be given again
+            self.r_size = r_size
+            if bump_n_ctx:
+                self.n_ctx -= 1
+            raise
+        if not fused:
             self.select()
             self.encode()
         if check:

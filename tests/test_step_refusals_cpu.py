@@ -68,3 +68,24 @@ def test_a_refused_rotation_leaves_buffers_of_the_right_size():
         s.rotate(k[:1], q[:, :3], kvr.make_rotation(s.desc))
     for buffer, like in ((s.k_turned, k), (s.q_turned, q)):
         assert buffer is None or buffer.shape == like.shape
+
+
+@pytest.mark.parametrize("bump", [True, False])
+@pytest.mark.parametrize("fused", [True, False, None])
+def test_a_token_that_is_refused_is_not_in_the_recent_queue(bump, fused):
+    """A key or value that the update refuses: neither n_ctx nor the queue's size has moved, and the step can be made again."""
+    s = _layer()
+    s.n_recent, s.slack, s.ret_cap, s.evict_cap, done = 4, 0, 10, 8, []
+    s.select = s.encode = s.attend = lambda *a, **kw: done.append(1)
+    refuse = True
+
+    def update(k, v):
+        if refuse:
+            raise ValueError("k_new")
+    s.step_update = s.append = update
+    with pytest.raises(ValueError):
+        s.decode_step(*TOKENS, bump_n_ctx=bump, fused=fused)
+    assert s.n_ctx.tolist() == [7, 7] and s.r_size == 3 and not done
+    refuse = False
+    s.decode_step(*TOKENS, bump_n_ctx=bump, fused=fused)
+    assert s.n_ctx.tolist() == [7 + bump] * 2 and s.r_size == 4 and len(done) == (3 if fused is False else 1)
